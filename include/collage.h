@@ -378,6 +378,133 @@ collage_status_t collage_wait_timeout_selftest(uint32_t limit_ms, void* stream);
  * Errors: ERR_NULL, ERR_ARCH, ERR_CUDA. */
 collage_status_t collage_selftest(uint64_t out_host[6], void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a training step's forward and backward pass, next to the optimizer step that consumes
+ * their gradients: residual addition + RMS norm, rounding of rows to 8 bits, the gated feed-forward
+ * projections, and distillation from a teacher's top logits.  The paper describes none of them.
+ *
+ * Unlike Algorithm 2 they are ordinary mixed precision: operands are bfloat16 (or e4m3 where a name says
+ * so), products, sums, statistics and exponentials are held in float, and a result is rounded once, when
+ * it is stored.  All sums have a fixed order: a call repeated on the same device gives the same bits.
+ *
+ * Matrices are described by collage_matrix_t (a HOST struct, read during the call): row-major, element
+ * (i, j) at data + i * ld + j elements, ld >= cols.  Rows and columns are below 2^31 (ERR_LIMIT), offsets
+ * are 64-bit.  Pointers and strides need no alignment beyond their element's; matrices whose rows all
+ * begin on 16 bytes are faster.  An output may overlap another array of the call only where it says so
+ * (ERR_ALIAS; two matrices that interleave by columns of a common stride, such as the halves of one
+ * [rows, 2 n] buffer, do not overlap).  Inputs may overlap each other.
+ * Errors common to all: ERR_NULL (a required pointer), ERR_ARG (shapes that do not fit together, ld < cols,
+ * misaligned elements, values out of range), ERR_LIMIT, ERR_ALIAS, ERR_ARCH, ERR_CUDA.
+ * All of them only launch kernels and may be recorded by stream capture. */
+typedef struct collage_matrix {
+    void* data;
+    uint64_t rows, cols;
+    uint64_t ld;             /* elements from one row's beginning to the next one's */
+} collage_matrix_t;
+
+/* r = x + residual;  rstd_i = 1 / sqrt(mean_j r_ij^2 + eps);  y_ij = r_ij * rstd_i * weight_j.
+ *   x, residual : bfloat16 [rows, cols]; residual may be NULL (r = x).
+ *   weight      : DEVICE bfloat16[cols].       eps >= 0 and finite.
+ *   residual_out: bfloat16 [rows, cols] or NULL: r rounded, the stream that the next layer adds to.  Only
+ *                 with a residual.  y is computed from r as it was before that rounding.
+ *   y           : bfloat16 [rows, cols] or NULL.
+ *   y8, y8_scale: e4m3 [rows, cols] and float[rows], or both NULL: y rounded to 8 bits as by
+ *                 collage_quantize_rows, y ~ y8 * y8_scale.  At least one of y and y8 is given.
+ *   rstd        : DEVICE float[rows] or NULL (the backward pass needs it).
+ * residual_out may be the array of x or of residual, y that of x (same data, same ld).
+ * A row that holds a NaN or an infinity gives NaNs (IEEE arithmetic). */
+collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_matrix_t* residual, const void* weight,
+                                      double eps, const collage_matrix_t* residual_out, const collage_matrix_t* y,
+                                      const collage_matrix_t* y8, float* y8_scale, float* rstd, void* stream);
+
+/* Its backward pass.  With n = r * rstd and g = weight * dy:
+ *   dx = rstd * (g - n * mean_j(g n)) + dresidual      (the gradient of x and of residual alike)
+ *   dweight_j = sum_i dy_ij * n_ij
+ *   dy          : bfloat16 [rows, cols], gradient of y.   r: residual_out of the forward call (x without a
+ *                 residual).   rstd: of the forward call.
+ *   dresidual   : bfloat16 [rows, cols] or NULL: gradient that reached residual_out on its own way.
+ *   dx          : bfloat16 [rows, cols] or NULL; may be the array of dy or of dresidual.
+ *   dweight     : DEVICE bfloat16[cols] or NULL (zeros if rows == 0).  One of dx and dweight is given.
+ *   workspace   : DEVICE scratch of at least collage_rms_norm_workspace_bytes(cols), 16-byte aligned, needed
+ *                 with dweight; nothing in it is kept between calls (ERR_WORKSPACE).
+ * A gradient of 8-bit outputs passes straight through: dy is the gradient of y8 * y8_scale. */
+size_t collage_rms_norm_workspace_bytes(uint64_t cols);
+collage_status_t collage_add_rms_norm_backward(const collage_matrix_t* dy, const collage_matrix_t* r, const float* rstd,
+                                               const void* weight, const collage_matrix_t* dresidual,
+                                               const collage_matrix_t* dx, void* dweight, void* workspace,
+                                               size_t workspace_bytes, void* stream);
+
+/* One scale a row: scale_i = max_j |x_ij| / 448, q_ij = e4m3(x_ij / scale_i), to nearest even.  A row of zeros
+ * has scale 0 and zeros.  A row with a NaN or an infinity has that as its scale (NaN before infinity), and q
+ * follows by IEEE division: NaN where x_ij is NaN or infinite, so that q * scale is NaN in all of the row.
+ *   x: bfloat16 [rows, cols];  q: e4m3 [rows, cols], one byte each;  scale: DEVICE float[rows]. */
+collage_status_t collage_quantize_rows(const collage_matrix_t* x, const collage_matrix_t* q, float* scale, void* stream);
+
+typedef enum {
+    COLLAGE_ACT_SILU = 0,        /* a(g) = g / (1 + exp(-g))                                                  */
+    COLLAGE_ACT_GELU_TANH = 1    /* a(g) = g / 2 * (1 + tanh(sqrt(2/pi) * (g + 0.044715 g^3)))                 */
+} collage_activation_t;
+
+/* Gated feed-forward projections: gate = x w_gate^T, up = x w_up^T, h = a(gate) * up, in one kernel.
+ *   x: bfloat16 [tokens, width];  w_gate, w_up: bfloat16 [ffn, width];  h: bfloat16 [tokens, ffn].
+ *   gate, up: bfloat16 [tokens, ffn], or both NULL: kept for the backward pass.  h is computed from the
+ *   float products, before these are rounded. */
+collage_status_t collage_gated_ffn(const collage_matrix_t* x, const collage_matrix_t* w_gate, const collage_matrix_t* w_up,
+                                   const collage_matrix_t* h, const collage_matrix_t* gate, const collage_matrix_t* up,
+                                   collage_activation_t activation, void* stream);
+
+/* Its backward pass: dgate = dh * up * a'(gate), dup = dh * a(gate), rounded to bfloat16, then
+ *   dx = dgate w_gate + dup w_up,   dw_gate = dgate^T x,   dw_up = dup^T x.
+ *   dh: bfloat16 [tokens, ffn];  x, w_gate, w_up, gate, up: of the forward call.
+ *   dgate, dup: bfloat16 [tokens, ffn], written; they may be the arrays of gate and up (in that order).
+ *   dx: bfloat16 [tokens, width] or NULL (w_gate and w_up are then not used and may be NULL).
+ *   dw_gate, dw_up: bfloat16 [ffn, width], or both NULL (x is then not used and may be NULL). */
+collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const collage_matrix_t* x,
+                                            const collage_matrix_t* w_gate, const collage_matrix_t* w_up,
+                                            const collage_matrix_t* gate, const collage_matrix_t* up,
+                                            const collage_matrix_t* dgate, const collage_matrix_t* dup,
+                                            const collage_matrix_t* dx, const collage_matrix_t* dw_gate,
+                                            const collage_matrix_t* dw_up, collage_activation_t activation, void* stream);
+
+/* The projections with 8-bit operands: gate_tf = x_scale_t * w_gate_scale_f * sum_d x8_td w_gate8_fd, up likewise;
+ * h = a(gate) * up in bfloat16.  x8 [tokens, width], w_gate8, w_up8 [ffn, width] are e4m3; the scales are DEVICE
+ * float[tokens], float[ffn], float[ffn], as collage_add_rms_norm and collage_quantize_rows write them. */
+collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float* x_scale, const collage_matrix_t* w_gate8,
+                                        const float* w_gate_scale, const collage_matrix_t* w_up8, const float* w_up_scale,
+                                        const collage_matrix_t* h, collage_activation_t activation, void* stream);
+
+/* Distillation from a teacher's top logits.  For row i with temperature t, over its entries k with an index
+ * in [0, vocab):
+ *   p_k  = softmax_k(top_logits_ik / t)         the teacher, renormalised over the entries that it has
+ *   q_j  = softmax_j(logits_ij / t)             the student, over the whole vocabulary
+ *   loss_i     = t^2 * sum_k p_k (log p_k - log q_index(k))
+ *   dlogits_ij = g_i * t * (q_j - sum_{k: index(k) = j} p_k)        with g_i the gradient of loss_i
+ * Entries whose index is negative or not below vocab are absent, entries of logit -infinity have p_k = 0; a
+ * row with no entry of a positive p_k has loss 0 and gradient 0 whatever its logits are.  An index may appear
+ * more than once in a row.  A row with g_i = 0 gets zeros whatever its logits are.  Otherwise NaN and
+ * infinity propagate per IEEE 754. */
+typedef enum { COLLAGE_DTYPE_BF16 = 0, COLLAGE_DTYPE_F32 = 1 } collage_dtype_t;
+typedef struct collage_distill {
+    collage_matrix_t logits;         /* [rows, vocab] in logits_dtype                                       */
+    collage_matrix_t top_index;      /* [rows, k] of int32_t or int64_t (top_index_bytes = 4 or 8)          */
+    collage_matrix_t top_logits;     /* [rows, k] of float; k <= COLLAGE_DISTILL_MAX_TOP (ERR_LIMIT)        */
+    collage_dtype_t logits_dtype;
+    uint32_t top_index_bytes;
+    double temperature;              /* > 0 and finite                                                      */
+} collage_distill_t;
+#define COLLAGE_DISTILL_MAX_TOP 1024
+
+/* loss: DEVICE float[rows].  lse: DEVICE float[rows] or NULL: log sum_j exp(logits_ij / t), for the backward call. */
+collage_status_t collage_distill_loss(const collage_distill_t* in, float* loss, float* lse, void* stream);
+/* grad_loss: DEVICE float[rows], g_i.  dlogits: [rows, vocab] in logits_dtype; may be the array of logits. */
+collage_status_t collage_distill_loss_backward(const collage_distill_t* in, const float* lse, const float* grad_loss,
+                                               const collage_matrix_t* dlogits, void* stream);
+/* Both in one pass over the logits for the objective sum_i row_weight_i * loss_i: loss[i] receives
+ * row_weight_i * loss_i (0 where the weight is 0, and the row's logits are then not read), dlogits the gradient with
+ * g_i = row_weight_i.  dlogits may be the array of logits. */
+collage_status_t collage_distill_loss_and_grad(const collage_distill_t* in, const float* row_weight, float* loss,
+                                               const collage_matrix_t* dlogits, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

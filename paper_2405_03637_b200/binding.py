@@ -16,6 +16,9 @@ BF16, LIGHT, PLUS, KAHAN, PLUS_FP32_REGISTERS = 0, 1, 2, 3, 4
 FLAG_EPS_INSIDE_SQRT, FLAG_TWOSUM_GROW, FLAG_DECAY_BY_GROW = 1, 2, 4
 FLAG_PIPELINE_KERNEL, FLAG_DIRECT_KERNEL, FLAG_LARGE_TILES = 8, 16, 32
 OP_ADD, OP_SUB, OP_MUL, OP_DIV, OP_SQRT, OP_FMA = range(6)
+ACT_SILU, ACT_GELU_TANH = 0, 1
+DTYPE_BF16, DTYPE_F32 = 0, 1
+DISTILL_MAX_TOP = 1024
 SCALAR_NAMES = ("b1", "c1", "b2", "c2", "b2h", "b2l", "bc1", "bc2", "a", "lam", "eps")
 
 EXPORTS = (
@@ -27,6 +30,9 @@ EXPORTS = (
     "collage_scaling", "collage_mul", "collage_renormalize", "collage_rounded_op", "collage_edq",
     "collage_selftest", "collage_pipeline_fault", "collage_edq_static", "collage_wait_timeout_selftest",
     "collage_workspace_init", "collage_edq_combine", "collage_build_flavor", "collage_enable_peer_access",
+    "collage_add_rms_norm", "collage_add_rms_norm_backward", "collage_rms_norm_workspace_bytes", "collage_quantize_rows",
+    "collage_gated_ffn", "collage_gated_ffn_backward", "collage_gated_ffn_e4m3",
+    "collage_distill_loss", "collage_distill_loss_backward", "collage_distill_loss_and_grad",
 )
 
 
@@ -51,6 +57,17 @@ class Tensor(ctypes.Structure):
     _fields_ = [("x_hi", ctypes.c_void_p), ("x_lo", ctypes.c_void_p), ("m", ctypes.c_void_p),
                 ("v_hi", ctypes.c_void_p), ("v_lo", ctypes.c_void_p), ("grad", ctypes.c_void_p),
                 ("n", ctypes.c_uint64)]
+
+
+class Matrix(ctypes.Structure):
+    """collage_matrix_t"""
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("ld", ctypes.c_uint64)]
+
+
+class Distill(ctypes.Structure):
+    """collage_distill_t"""
+    _fields_ = [("logits", Matrix), ("top_index", Matrix), ("top_logits", Matrix), ("logits_dtype", ctypes.c_int),
+                ("top_index_bytes", ctypes.c_uint32), ("temperature", ctypes.c_double)]
 
 
 class CollageError(RuntimeError):
@@ -122,6 +139,19 @@ def lib() -> ctypes.CDLL:
         L.collage_build_flavor.restype = ctypes.c_char_p
         L.collage_build_flavor.argtypes = []
         L.collage_enable_peer_access.argtypes = [i32]
+        mp = ctypes.POINTER(Matrix)
+        L.collage_add_rms_norm.argtypes = [mp, mp, vp, ctypes.c_double, mp, mp, mp, vp, vp, vp]
+        L.collage_rms_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.collage_rms_norm_workspace_bytes.argtypes = [u64]
+        L.collage_add_rms_norm_backward.argtypes = [mp, mp, vp, vp, mp, mp, vp, vp, ctypes.c_size_t, vp]
+        L.collage_quantize_rows.argtypes = [mp, mp, vp, vp]
+        L.collage_gated_ffn.argtypes = [mp, mp, mp, mp, mp, mp, i32, vp]
+        L.collage_gated_ffn_backward.argtypes = [mp] * 11 + [i32, vp]
+        L.collage_gated_ffn_e4m3.argtypes = [mp, vp, mp, vp, mp, vp, mp, i32, vp]
+        dp = ctypes.POINTER(Distill)
+        L.collage_distill_loss.argtypes = [dp, vp, vp, vp]
+        L.collage_distill_loss_backward.argtypes = [dp, vp, vp, mp, vp]
+        L.collage_distill_loss_and_grad.argtypes = [dp, vp, vp, mp, vp]
         _lib = L
     return _lib
 
@@ -329,3 +359,139 @@ def read_edq(edq_dev) -> dict:
     """Copy a device collage_edq_t (a >= EDQ_RECORD_BYTES torch.uint8 CUDA tensor) to the host and decode it."""
     raw = edq_dev.detach().cpu().numpy().tobytes()
     return _record(Edq.from_buffer_copy(raw[:ctypes.sizeof(Edq)]))
+
+
+# ------------------------------------------------------------------------------------------------------------------------
+# Operators of the forward and backward pass.  Matrices are CUDA tensors of two or more dimensions whose last one is
+# contiguous; leading dimensions are flattened into rows (a view, never a copy).  What a tensor cannot be described as, or
+# is not on the device or of the type that the operator reads, raises CollageError(ERR_ARG) here; all other checks are the
+# library's.
+
+def _refuse(where: str):
+    raise CollageError(ERR_ARG, where)
+
+
+def _matrix(t, dtype: str, where: str, required: bool = False):
+    """collage_matrix_t of a tensor, or None for None."""
+    if t is None:
+        if required:
+            raise CollageError(ERR_NULL, where)
+        return None
+    if not t.is_cuda or str(t.dtype) != dtype or t.dim() < 2:
+        _refuse(where)
+    if t.dim() > 2:
+        try:
+            t = t.view(-1, t.shape[-1])
+        except RuntimeError:
+            _refuse(where)
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if rows <= 1:
+        ld = cols                              # the stride of a single row means nothing
+    if cols <= 1:
+        inner = 1
+    if inner != 1 or ld < cols:
+        _refuse(where)
+    return Matrix(t.data_ptr(), rows, cols, ld)
+
+
+def _vector(t, dtype: str, length: int, where: str):
+    """Address of a contiguous vector of that many elements, or None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda or str(t.dtype) != dtype or t.numel() != length or not t.is_contiguous():
+        _refuse(where)
+    return t.data_ptr()
+
+
+_BF16, _F32, _E4M3 = "torch.bfloat16", "torch.float32", "torch.float8_e4m3fn"
+
+
+def add_rms_norm(x, residual, weight, eps: float, residual_out=None, y=None, y8=None, y8_scale=None, rstd=None, stream=None):
+    """r = x + residual; y = r / sqrt(mean(r^2) + eps) * weight in bfloat16 (y) and / or in 8 bits (y8, y8_scale)."""
+    w = "collage_add_rms_norm"
+    mx = _matrix(x, _BF16, w, True)
+    _check(lib().collage_add_rms_norm(mx, _matrix(residual, _BF16, w), _vector(weight, _BF16, mx.cols, w), eps,
+                                      _matrix(residual_out, _BF16, w), _matrix(y, _BF16, w), _matrix(y8, _E4M3, w),
+                                      _vector(y8_scale, _F32, mx.rows, w), _vector(rstd, _F32, mx.rows, w), _ptr(stream)), w)
+
+
+def rms_norm_workspace_bytes(cols: int) -> int:
+    return int(lib().collage_rms_norm_workspace_bytes(cols))
+
+
+def add_rms_norm_backward(dy, r, rstd, weight, dx, dweight, workspace, dresidual=None, stream=None):
+    """Gradients of add_rms_norm: r is its residual_out (or x without a residual); dx or dweight may be None."""
+    w = "collage_add_rms_norm_backward"
+    mdy = _matrix(dy, _BF16, w, True)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().collage_add_rms_norm_backward(mdy, _matrix(r, _BF16, w), _vector(rstd, _F32, mdy.rows, w),
+                                               _vector(weight, _BF16, mdy.cols, w), _matrix(dresidual, _BF16, w),
+                                               _matrix(dx, _BF16, w), _vector(dweight, _BF16, mdy.cols, w), _ptr(workspace),
+                                               ws_bytes, _ptr(stream)), w)
+
+
+def quantize_rows(x, q, scale, stream=None):
+    """q, scale: x in 8 bits (torch.float8_e4m3fn) with one float scale a row."""
+    w = "collage_quantize_rows"
+    mx = _matrix(x, _BF16, w, True)
+    _check(lib().collage_quantize_rows(mx, _matrix(q, _E4M3, w), _vector(scale, _F32, mx.rows, w), _ptr(stream)), w)
+
+
+def gated_ffn(x, w_gate, w_up, h, gate=None, up=None, activation: int = ACT_SILU, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T); gate and up, if given, keep the two products for the backward pass."""
+    w = "collage_gated_ffn"
+    _check(lib().collage_gated_ffn(_matrix(x, _BF16, w), _matrix(w_gate, _BF16, w), _matrix(w_up, _BF16, w), _matrix(h, _BF16, w),
+                                   _matrix(gate, _BF16, w), _matrix(up, _BF16, w), activation, _ptr(stream)), w)
+
+
+def gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dgate, dup, dx=None, dw_gate=None, dw_up=None, activation: int = ACT_SILU,
+                       stream=None):
+    """Gradients of gated_ffn; dgate and dup receive the gradients of the two products (they may be gate and up themselves)."""
+    w = "collage_gated_ffn_backward"
+    m = [_matrix(t, _BF16, w) for t in (dh, x, w_gate, w_up, gate, up, dgate, dup, dx, dw_gate, dw_up)]
+    _check(lib().collage_gated_ffn_backward(*m, activation, _ptr(stream)), w)
+
+
+def gated_ffn_e4m3(x8, x_scale, w_gate8, w_gate_scale, w_up8, w_up_scale, h, activation: int = ACT_SILU, stream=None):
+    """gated_ffn on 8-bit operands with a scale for each token and each channel, as quantize_rows writes them."""
+    w = "collage_gated_ffn_e4m3"
+    mx, mg, mu = _matrix(x8, _E4M3, w, True), _matrix(w_gate8, _E4M3, w, True), _matrix(w_up8, _E4M3, w, True)
+    _check(lib().collage_gated_ffn_e4m3(mx, _vector(x_scale, _F32, mx.rows, w), mg, _vector(w_gate_scale, _F32, mg.rows, w), mu,
+                                        _vector(w_up_scale, _F32, mu.rows, w), _matrix(h, _BF16, w), activation, _ptr(stream)), w)
+
+
+def _distill(logits, top_index, top_logits, temperature, where) -> Distill:
+    if logits is None or top_index is None or top_logits is None:
+        raise CollageError(ERR_NULL, where)
+    dtype, index = str(logits.dtype), str(top_index.dtype)
+    if dtype not in (_BF16, _F32) or index not in ("torch.int32", "torch.int64"):
+        _refuse(where)
+    return Distill(_matrix(logits, dtype, where), _matrix(top_index, index, where), _matrix(top_logits, _F32, where),
+                   DTYPE_BF16 if dtype == _BF16 else DTYPE_F32, 4 if index == "torch.int32" else 8, temperature)
+
+
+def distill_loss(logits, top_index, top_logits, temperature: float, loss, lse=None, stream=None):
+    """loss[i] = temperature^2 KL(teacher's renormalised top entries || softmax(logits / temperature)) for each row."""
+    w = "collage_distill_loss"
+    d = _distill(logits, top_index, top_logits, temperature, w)
+    n = d.logits.rows
+    _check(lib().collage_distill_loss(ctypes.byref(d), _vector(loss, _F32, n, w), _vector(lse, _F32, n, w), _ptr(stream)), w)
+
+
+def distill_loss_backward(logits, top_index, top_logits, temperature: float, lse, grad_loss, dlogits, stream=None):
+    """dlogits from grad_loss (one value a row) and the lse of distill_loss; dlogits may be the logits' own array."""
+    w = "collage_distill_loss_backward"
+    d = _distill(logits, top_index, top_logits, temperature, w)
+    n = d.logits.rows
+    _check(lib().collage_distill_loss_backward(ctypes.byref(d), _vector(lse, _F32, n, w), _vector(grad_loss, _F32, n, w),
+                                               _matrix(dlogits, str(logits.dtype), w), _ptr(stream)), w)
+
+
+def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row_weight, loss, dlogits, stream=None):
+    """loss[i] = row_weight[i] * the row's loss, and dlogits, in one pass; dlogits may be the logits' own array."""
+    w = "collage_distill_loss_and_grad"
+    d = _distill(logits, top_index, top_logits, temperature, w)
+    n = d.logits.rows
+    _check(lib().collage_distill_loss_and_grad(ctypes.byref(d), _vector(row_weight, _F32, n, w), _vector(loss, _F32, n, w),
+                                               _matrix(dlogits, str(logits.dtype), w), _ptr(stream)), w)

@@ -1,0 +1,293 @@
+// Gated feed-forward projections: h = a(x w_gate^T) * (x w_up^T), the backward pass, and the same with e4m3 operands.
+#include "ops_common.cuh"
+
+namespace collage {
+namespace ops {
+
+// An operand of a product, element (i, k) at data + i * row + k * col: either of the two strides may be 1.
+struct Operand {
+    const void* data;
+    uint64_t row, col;
+};
+
+struct ProductArgs {
+    Operand a[2], b[2];              // PAIRED: two products with a common a; otherwise a sum of `terms` products
+    const float* a_scale;
+    const float* b_scale[2];
+    uint16_t* out[3];                // PAIRED: h, gate, up (the last two may be NULL)
+    uint64_t ldo[3];
+    uint64_t m, n, k;
+    int terms, activation;
+};
+
+constexpr float kGeluC = 0.7978845608028654f;      // sqrt(2 / pi)
+constexpr float kGeluD = 0.044715f;
+
+// tanh's argument for GELU.  Beyond |g| = 16 the tanh is 1 to the last bit: the clamp keeps g^3 and the slope's factors finite.
+__device__ __forceinline__ float gelu_clamped(float g) { return fminf(fmaxf(g, -16.0f), 16.0f); }
+
+__device__ __forceinline__ float activate(int kind, float g) {
+    if (kind == COLLAGE_ACT_SILU) return g / (1.0f + expf(-g));
+    const float c = g != g ? g : gelu_clamped(g);
+    return 0.5f * g * (1.0f + tanhf(kGeluC * __fmaf_rn(kGeluD * c * c, c, c)));
+}
+// a(g) and a'(g)
+__device__ __forceinline__ float2 activate_and_slope(int kind, float g) {
+    if (kind == COLLAGE_ACT_SILU) {
+        const float s = 1.0f / (1.0f + expf(-g));
+        return make_float2(g * s, s * (1.0f + g * (1.0f - s)));
+    }
+    const float c = g != g ? g : gelu_clamped(g);
+    const float t = tanhf(kGeluC * __fmaf_rn(kGeluD * c * c, c, c));
+    return make_float2(0.5f * g * (1.0f + t), 0.5f * (1.0f + t) + 0.5f * c * (1.0f - t * t) * kGeluC * (1.0f + 3.0f * kGeluD * c * c));
+}
+
+__device__ __forceinline__ float element(const uint16_t* p) { return bf16_value(*p); }
+__device__ __forceinline__ float element(const uint8_t* p) {
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3)));
+}
+
+constexpr int kTile = 64, kStep = 16;
+
+// 64 x 64 outputs a block, 4 x 4 a thread, operands staged as floats.
+template <typename T, bool PAIRED>
+__global__ void __launch_bounds__(256) product_any_kernel(const __grid_constant__ ProductArgs p) {
+    __shared__ float sa[kStep][kTile + 4], sb[PAIRED ? 2 : 1][kStep][kTile + 4];
+    const uint64_t m0 = blockIdx.x * static_cast<uint64_t>(kTile), n0 = blockIdx.y * static_cast<uint64_t>(kTile);
+    const int tm = threadIdx.x & 15, tn = threadIdx.x >> 4;
+    float acc[PAIRED ? 2 : 1][4][4] = {};
+    auto load = [&](const Operand& o, uint64_t i0, uint64_t limit, uint64_t k0, float (*dst)[kTile + 4]) {
+        for (int e = threadIdx.x; e < kTile * kStep; e += 256) {
+            const int i = o.col == 1 ? e / kStep : e % kTile, k = o.col == 1 ? e % kStep : e / kTile;
+            const bool in = i0 + i < limit && k0 + k < p.k;
+            dst[k][i] = in ? element(static_cast<const T*>(o.data) + (i0 + i) * o.row + (k0 + k) * o.col) : 0.0f;
+        }
+    };
+    for (int term = 0; term < (PAIRED ? 1 : p.terms); ++term)
+        for (uint64_t k0 = 0; k0 < p.k; k0 += kStep) {
+            load(p.a[term], m0, p.m, k0, sa);
+            load(p.b[term], n0, p.n, k0, sb[0]);
+            if constexpr (PAIRED) load(p.b[1], n0, p.n, k0, sb[1]);
+            __syncthreads();
+            for (int k = 0; k < kStep; ++k)
+                for (int i = 0; i < 4; ++i)
+                    for (int j = 0; j < 4; ++j)
+                        for (int s = 0; s < (PAIRED ? 2 : 1); ++s)
+                            acc[s][i][j] = __fmaf_rn(sa[k][tm * 4 + i], sb[s][k][tn * 4 + j], acc[s][i][j]);
+            __syncthreads();
+        }
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j) {
+            const uint64_t m = m0 + tm * 4 + i, n = n0 + tn * 4 + j;
+            if (m >= p.m || n >= p.n) continue;
+            float v = acc[0][i][j];
+            if constexpr (PAIRED) {
+                float u = acc[1][i][j];
+                if (p.a_scale) {
+                    v *= p.a_scale[m] * p.b_scale[0][n];
+                    u *= p.a_scale[m] * p.b_scale[1][n];
+                }
+                if (p.out[1]) {
+                    p.out[1][m * p.ldo[1] + n] = to_bf16(v);
+                    p.out[2][m * p.ldo[2] + n] = to_bf16(u);
+                }
+                v = activate(p.activation, v) * u;
+            }
+            p.out[0][m * p.ldo[0] + n] = to_bf16(v);
+        }
+}
+
+struct GateArgs {
+    const uint16_t *dh, *gate, *up;
+    uint16_t *dgate, *dup;
+    uint64_t lddh, ldg, ldu, lddg, lddu, cols;
+    int activation;
+};
+
+__global__ void __launch_bounds__(256) gate_backward_any_kernel(const __grid_constant__ GateArgs a) {
+    const uint64_t row = blockIdx.x;
+    for (uint64_t j = threadIdx.x; j < a.cols; j += 256) {
+        const float dh = bf16_value(a.dh[row * a.lddh + j]), u = bf16_value(a.up[row * a.ldu + j]);
+        const float2 as = activate_and_slope(a.activation, bf16_value(a.gate[row * a.ldg + j]));
+        a.dgate[row * a.lddg + j] = to_bf16(dh * u * as.y);
+        a.dup[row * a.lddu + j] = to_bf16(dh * as.x);
+    }
+}
+
+inline Operand by_row(const collage_matrix_t* m) { return {m->data, m->ld, 1}; }        // i = row of the matrix
+inline Operand by_col(const collage_matrix_t* m) { return {m->data, 1, m->ld}; }        // i = column
+
+template <typename T, bool PAIRED>
+collage_status_t launch_product(const ProductArgs& p, cudaStream_t s) {
+    if (p.m == 0 || p.n == 0) return COLLAGE_OK;
+    const dim3 grid(static_cast<unsigned>((p.m + kTile - 1) / kTile), static_cast<unsigned>((p.n + kTile - 1) / kTile));
+    product_any_kernel<T, PAIRED><<<grid, 256, 0, s>>>(p);
+    return launch_status();
+}
+
+static bool known(collage_activation_t a) { return a == COLLAGE_ACT_SILU || a == COLLAGE_ACT_GELU_TANH; }
+
+// Shapes of x [tokens, width], two weights [ffn, width] and an output [tokens, ffn]
+static bool shapes_fit(const collage_matrix_t* x, const collage_matrix_t* wg, const collage_matrix_t* wu, const collage_matrix_t* h) {
+    return same_shape(wg, wu) && x->cols == wg->cols && h->rows == x->rows && h->cols == wg->rows;
+}
+
+template <int N>
+static collage_status_t check_all(const collage_matrix_t* const (&m)[N], uint32_t elem_bytes) {
+    for (const collage_matrix_t* x : m)
+        if (x)
+            if (const collage_status_t st = check_matrix(x, elem_bytes); st != COLLAGE_OK) return st;
+    return COLLAGE_OK;
+}
+
+}  // namespace ops
+}  // namespace collage
+
+using namespace collage;
+using namespace collage::ops;
+
+extern "C" {
+
+collage_status_t collage_gated_ffn(const collage_matrix_t* x, const collage_matrix_t* w_gate, const collage_matrix_t* w_up,
+                                   const collage_matrix_t* h, const collage_matrix_t* gate, const collage_matrix_t* up,
+                                   collage_activation_t activation, void* stream) {
+    if (!x || !w_gate || !w_up || !h || !gate != !up) return COLLAGE_ERR_NULL;
+    if (!known(activation) || !shapes_fit(x, w_gate, w_up, h)) return COLLAGE_ERR_ARG;
+    if (gate && !(same_shape(gate, h) && same_shape(up, h))) return COLLAGE_ERR_ARG;
+    const collage_matrix_t* all[6] = {x, w_gate, w_up, h, gate, up};
+    collage_status_t st = check_all(all, 2);
+    if (st != COLLAGE_OK) return st;
+    AliasCheck alias;
+    for (int i = 0; i < 6; ++i)
+        if (all[i]) alias.add(span_of(all[i], 2), i >= 3);
+    if (alias.clash()) return COLLAGE_ERR_ALIAS;
+    DeviceInfo dev;
+    if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    ProductArgs p = {};
+    p.a[0] = by_row(x);
+    p.b[0] = by_row(w_gate);
+    p.b[1] = by_row(w_up);
+    p.out[0] = static_cast<uint16_t*>(h->data);
+    p.ldo[0] = h->ld;
+    if (gate) {
+        p.out[1] = static_cast<uint16_t*>(gate->data);
+        p.out[2] = static_cast<uint16_t*>(up->data);
+        p.ldo[1] = gate->ld;
+        p.ldo[2] = up->ld;
+    }
+    p.m = x->rows;
+    p.n = w_gate->rows;
+    p.k = x->cols;
+    p.activation = activation;
+    return launch_product<uint16_t, true>(p, static_cast<cudaStream_t>(stream));
+}
+
+collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float* x_scale, const collage_matrix_t* w_gate8,
+                                        const float* w_gate_scale, const collage_matrix_t* w_up8, const float* w_up_scale,
+                                        const collage_matrix_t* h, collage_activation_t activation, void* stream) {
+    if (!x8 || !w_gate8 || !w_up8 || !h) return COLLAGE_ERR_NULL;
+    if ((!x_scale && x8->rows) || (!w_gate_scale && w_gate8->rows) || (!w_up_scale && w_up8->rows)) return COLLAGE_ERR_NULL;
+    if (!known(activation) || !shapes_fit(x8, w_gate8, w_up8, h)) return COLLAGE_ERR_ARG;
+    const collage_matrix_t* in[3] = {x8, w_gate8, w_up8};
+    const float* scales[3] = {x_scale, w_gate_scale, w_up_scale};
+    collage_status_t st = check_all(in, 1);
+    if (st == COLLAGE_OK) st = check_matrix(h, 2);
+    if (st != COLLAGE_OK) return st;
+    AliasCheck alias;
+    for (int i = 0; i < 3; ++i) {
+        if (reinterpret_cast<uintptr_t>(scales[i]) % 4) return COLLAGE_ERR_ARG;
+        alias.add(span_of(in[i], 1), false);
+        alias.add(span_of(scales[i], 4 * in[i]->rows), false);
+    }
+    alias.add(span_of(h, 2), true);
+    if (alias.clash()) return COLLAGE_ERR_ALIAS;
+    DeviceInfo dev;
+    if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    ProductArgs p = {};
+    p.a[0] = by_row(x8);
+    p.b[0] = by_row(w_gate8);
+    p.b[1] = by_row(w_up8);
+    p.a_scale = x_scale;
+    p.b_scale[0] = w_gate_scale;
+    p.b_scale[1] = w_up_scale;
+    p.out[0] = static_cast<uint16_t*>(h->data);
+    p.ldo[0] = h->ld;
+    p.m = x8->rows;
+    p.n = w_gate8->rows;
+    p.k = x8->cols;
+    p.activation = activation;
+    return launch_product<uint8_t, true>(p, static_cast<cudaStream_t>(stream));
+}
+
+collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const collage_matrix_t* x, const collage_matrix_t* w_gate,
+                                            const collage_matrix_t* w_up, const collage_matrix_t* gate, const collage_matrix_t* up,
+                                            const collage_matrix_t* dgate, const collage_matrix_t* dup, const collage_matrix_t* dx,
+                                            const collage_matrix_t* dw_gate, const collage_matrix_t* dw_up,
+                                            collage_activation_t activation, void* stream) {
+    if (!dh || !gate || !up || !dgate || !dup || !dw_gate != !dw_up) return COLLAGE_ERR_NULL;
+    if ((dx && (!w_gate || !w_up)) || (dw_gate && !x)) return COLLAGE_ERR_NULL;
+    if (!known(activation)) return COLLAGE_ERR_ARG;
+    if (!same_shape(gate, dh) || !same_shape(up, dh) || !same_shape(dgate, dh) || !same_shape(dup, dh)) return COLLAGE_ERR_ARG;
+    if (dx && !shapes_fit(dx, w_gate, w_up, dh)) return COLLAGE_ERR_ARG;
+    if (dw_gate && !shapes_fit(x, dw_gate, dw_up, dh)) return COLLAGE_ERR_ARG;
+    if (!dx) w_gate = w_up = nullptr;                      // not used
+    if (!dw_gate) x = nullptr;
+    const collage_matrix_t* all[11] = {dh, x, w_gate, w_up, gate, up, dgate, dup, dx, dw_gate, dw_up};
+    collage_status_t st = check_all(all, 2);
+    if (st != COLLAGE_OK) return st;
+    AliasCheck alias;
+    int at[11];
+    for (int i = 0; i < 11; ++i) at[i] = all[i] ? alias.add(span_of(all[i], 2), i >= 6) : -1;
+    const int pairs[2][2] = {{at[4], at[6]}, {at[5], at[7]}};
+    if (alias.clash(pairs)) return COLLAGE_ERR_ALIAS;
+    DeviceInfo dev;
+    if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dh->rows && dh->cols) {
+        GateArgs g = {};
+        g.dh = static_cast<const uint16_t*>(dh->data);
+        g.gate = static_cast<const uint16_t*>(gate->data);
+        g.up = static_cast<const uint16_t*>(up->data);
+        g.dgate = static_cast<uint16_t*>(dgate->data);
+        g.dup = static_cast<uint16_t*>(dup->data);
+        g.lddh = dh->ld;
+        g.ldg = gate->ld;
+        g.ldu = up->ld;
+        g.lddg = dgate->ld;
+        g.lddu = dup->ld;
+        g.cols = dh->cols;
+        g.activation = activation;
+        gate_backward_any_kernel<<<static_cast<unsigned>(dh->rows), 256, 0, s>>>(g);
+        if ((st = launch_status()) != COLLAGE_OK) return st;
+    }
+    if (dx) {
+        ProductArgs p = {};
+        p.a[0] = by_row(dgate);
+        p.a[1] = by_row(dup);
+        p.b[0] = by_col(w_gate);
+        p.b[1] = by_col(w_up);
+        p.out[0] = static_cast<uint16_t*>(dx->data);
+        p.ldo[0] = dx->ld;
+        p.m = dx->rows;
+        p.n = dx->cols;
+        p.k = dh->cols;
+        p.terms = 2;
+        if ((st = launch_product<uint16_t, false>(p, s)) != COLLAGE_OK) return st;
+    }
+    for (int half = 0; half < 2 && dw_gate; ++half) {
+        const collage_matrix_t* out = half ? dw_up : dw_gate;
+        ProductArgs p = {};
+        p.a[0] = by_col(half ? dup : dgate);
+        p.b[0] = by_col(x);
+        p.out[0] = static_cast<uint16_t*>(out->data);
+        p.ldo[0] = out->ld;
+        p.m = out->rows;
+        p.n = out->cols;
+        p.k = dh->rows;
+        p.terms = 1;
+        if ((st = launch_product<uint16_t, false>(p, s)) != COLLAGE_OK) return st;
+    }
+    return COLLAGE_OK;
+}
+
+}  // extern "C"
