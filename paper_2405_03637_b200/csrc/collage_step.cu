@@ -778,6 +778,7 @@ static void push_edq_ranges(std::vector<ByteRange>& ranges, const collage_hyper_
 
 namespace collage {
 cudaError_t read_clear_fault32(unsigned int* out);
+cudaError_t read_clear_product_fault(unsigned int* out);
 }
 using namespace collage;
 
@@ -1186,11 +1187,12 @@ uint64_t collage_plan_num_chunks(const collage_plan_t* plan) { return plan ? pla
 
 collage_status_t collage_pipeline_fault(uint32_t* out_host) {
     if (!out_host) return COLLAGE_ERR_NULL;
-    unsigned int v = 0, v32 = 0, zero = 0;
+    unsigned int v = 0, v32 = 0, vp = 0, zero = 0;
     if (cudaMemcpyFromSymbol(&v, g_pipeline_fault, sizeof v) != cudaSuccess) return COLLAGE_ERR_CUDA;
     if (v && cudaMemcpyToSymbol(g_pipeline_fault, &zero, sizeof zero) != cudaSuccess) return COLLAGE_ERR_CUDA;
     if (read_clear_fault32(&v32) != cudaSuccess) return COLLAGE_ERR_CUDA;    // the float comparator's pipeline
-    *out_host = v ? v : v32;
+    if (read_clear_product_fault(&vp) != cudaSuccess) return COLLAGE_ERR_CUDA;   // the feed-forward products' pipeline
+    *out_host = v ? v : v32 ? v32 : vp;
     return COLLAGE_OK;
 }
 

@@ -1,7 +1,14 @@
 // Gated feed-forward projections: h = a(x w_gate^T) * (x w_up^T), the backward pass, and the same with e4m3 operands.
-#include "ops_common.cuh"
+#include "product_tile.cuh"
 
 namespace collage {
+
+cudaError_t read_clear_product_fault(unsigned int* out) {
+    const unsigned int zero = 0;
+    const cudaError_t e = cudaMemcpyFromSymbol(out, ops::g_product_fault, sizeof *out);
+    return e != cudaSuccess || *out == 0 ? e : cudaMemcpyToSymbol(ops::g_product_fault, &zero, sizeof zero);
+}
+
 namespace ops {
 
 // An operand of a product, element (i, k) at data + i * row + k * col: either of the two strides may be 1.
@@ -19,28 +26,6 @@ struct ProductArgs {
     uint64_t m, n, k;
     int terms, activation;
 };
-
-constexpr float kGeluC = 0.7978845608028654f;      // sqrt(2 / pi)
-constexpr float kGeluD = 0.044715f;
-
-// tanh's argument for GELU.  Beyond |g| = 16 the tanh is 1 to the last bit: the clamp keeps g^3 and the slope's factors finite.
-__device__ __forceinline__ float gelu_clamped(float g) { return fminf(fmaxf(g, -16.0f), 16.0f); }
-
-__device__ __forceinline__ float activate(int kind, float g) {
-    if (kind == COLLAGE_ACT_SILU) return g / (1.0f + expf(-g));
-    const float c = g != g ? g : gelu_clamped(g);
-    return 0.5f * g * (1.0f + tanhf(kGeluC * __fmaf_rn(kGeluD * c * c, c, c)));
-}
-// a(g) and a'(g)
-__device__ __forceinline__ float2 activate_and_slope(int kind, float g) {
-    if (kind == COLLAGE_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
-        return make_float2(g * s, s * (1.0f + g * (1.0f - s)));
-    }
-    const float c = g != g ? g : gelu_clamped(g);
-    const float t = tanhf(kGeluC * __fmaf_rn(kGeluD * c * c, c, c));
-    return make_float2(0.5f * g * (1.0f + t), 0.5f * (1.0f + t) + 0.5f * c * (1.0f - t * t) * kGeluC * (1.0f + 3.0f * kGeluD * c * c));
-}
 
 __device__ __forceinline__ float element(const uint16_t* p) { return bf16_value(*p); }
 __device__ __forceinline__ float element(const uint8_t* p) {
@@ -117,6 +102,137 @@ __global__ void __launch_bounds__(256) gate_backward_any_kernel(const __grid_con
 inline Operand by_row(const collage_matrix_t* m) { return {m->data, m->ld, 1}; }        // i = row of the matrix
 inline Operand by_col(const collage_matrix_t* m) { return {m->data, 1, m->ld}; }        // i = column
 
+// ---- tensor-map path -------------------------------------------------------------------------------------------------
+
+using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
+
+static EncodeTiled encode_tiled() {
+    static std::atomic<void*> cached{nullptr};
+    void* fn = cached.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        cached.store(fn, std::memory_order_release);
+    }
+    return reinterpret_cast<EncodeTiled>(fn);
+}
+
+// The matrix as a two-dimensional tensor read in boxes of box_cols x box_rows; outside it a load gives zeros and a store
+// writes nothing.
+static bool make_map(CUtensorMap* map, const collage_matrix_t* m, bool bytes, uint32_t box_cols, uint32_t box_rows, bool output) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t size = bytes ? 1 : 2;
+    const cuuint64_t dims[2] = {m->cols, m->rows};
+    const cuuint64_t strides[1] = {m->rows > 1 ? m->ld * size : (m->cols * size + 15) / 16 * 16};
+    const cuuint32_t box[2] = {box_cols, box_rows}, one[2] = {1, 1};
+    return encode(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m->data, dims, strides, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, output ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Can tensor maps describe it?  Rows on 16 bytes and of whole 16 bytes (a tile store writes no less), a stride below 2^40 bytes.
+static bool mappable(const collage_matrix_t* m, uint32_t elem_bytes) {
+    return rows_aligned(m, elem_bytes, 16) && m->cols * elem_bytes % 16 == 0 && (m->rows <= 1 || m->ld * elem_bytes < (1ull << 40));
+}
+
+// Once per kernel and device: leave to use the shared memory that it takes.
+template <auto Kernel>
+static cudaError_t allow_smem(int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+    if (done.load(std::memory_order_acquire) >> (dev & 63) & 1) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
+    return e;
+}
+
+template <bool E4M3, bool A_MN, bool B_MN, bool GATED, int CTAS>
+static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) {
+    constexpr uint32_t out_cols = (GATED ? 64 : 128) * CTAS;
+    t.m_tiles = (t.m + 128 * CTAS - 1) / (128 * CTAS);
+    t.n_tiles = (t.n + out_cols - 1) / out_cols;
+    const uint64_t tiles = static_cast<uint64_t>(t.problems) * t.m_tiles * t.n_tiles;
+    if (tiles >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
+    t.group = 8;
+    constexpr auto kernel = &tile_kernel<E4M3, A_MN, B_MN, GATED, CTAS>;
+    if (allow_smem<kernel>(kTileSmem) != cudaSuccess) return COLLAGE_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min<uint64_t>(tiles, sm_count / CTAS)) * CTAS);
+    cfg.blockDim = dim3(kTileThreads);
+    cfg.dynamicSmemBytes = kTileSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {CTAS, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, t) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
+}
+
+// The forward products with 16-byte aligned rows.
+template <bool E4M3>
+static collage_status_t tiles_forward(const collage_matrix_t* x, const collage_matrix_t* wg, const collage_matrix_t* wu,
+                                      const collage_matrix_t* h, const collage_matrix_t* gate, const collage_matrix_t* up,
+                                      const float* const (&scales)[3], int activation, int sm_count, cudaStream_t s) {
+    TileArgs t = {};
+    const bool pair = x->rows > 128;
+    const uint32_t k = E4M3 ? 128 : 64;
+    bool ok = make_map(&t.a[0], x, E4M3, k, 128, false) && make_map(&t.b[0], wg, E4M3, k, pair ? 128 : 64, false) &&
+              make_map(&t.b[1], wu, E4M3, k, pair ? 128 : 64, false) && make_map(&t.out[0], h, false, kUnitCols, 128, true);
+    t.a[1] = t.a[0];
+    if (gate) ok = ok && make_map(&t.out[1], gate, false, kUnitCols, 128, true) && make_map(&t.out[2], up, false, kUnitCols, 128, true);
+    if (!ok) return COLLAGE_ERR_CUDA;
+    t.a_scale = scales[0];
+    t.b_scale[0] = scales[1];
+    t.b_scale[1] = scales[2];
+    t.m = static_cast<uint32_t>(x->rows);
+    t.n = static_cast<uint32_t>(wg->rows);
+    t.problems = t.terms = 1;
+    t.k_blocks = static_cast<uint32_t>((x->cols + k - 1) / k);
+    t.keep = gate != nullptr;
+    t.activation = activation;
+    return pair ? launch_tiles<E4M3, false, false, true, 2>(t, sm_count, s) : launch_tiles<E4M3, false, false, true, 1>(t, sm_count, s);
+}
+
+// dx = dgate w_gate + dup w_up
+static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_matrix_t* dup, const collage_matrix_t* wg,
+                                 const collage_matrix_t* wu, const collage_matrix_t* dx, int sm_count, cudaStream_t s) {
+    TileArgs t = {};
+    if (!(make_map(&t.a[0], dgate, false, 64, 128, false) && make_map(&t.a[1], dup, false, 64, 128, false) &&
+          make_map(&t.b[0], wg, false, 64, 64, false) && make_map(&t.b[1], wu, false, 64, 64, false) &&
+          make_map(&t.out[0], dx, false, kUnitCols, 128, true)))
+        return COLLAGE_ERR_CUDA;
+    t.m = static_cast<uint32_t>(dx->rows);
+    t.n = static_cast<uint32_t>(dx->cols);
+    t.problems = 1;
+    t.terms = 2;
+    t.k_blocks = static_cast<uint32_t>((dgate->cols + 63) / 64);
+    return t.m > 128 ? launch_tiles<false, false, true, false, 2>(t, sm_count, s) : launch_tiles<false, false, true, false, 1>(t, sm_count, s);
+}
+
+// dw_gate = dgate^T x and dw_up = dup^T x
+static collage_status_t tiles_dw(const collage_matrix_t* dgate, const collage_matrix_t* dup, const collage_matrix_t* x,
+                                 const collage_matrix_t* dwg, const collage_matrix_t* dwu, int sm_count, cudaStream_t s) {
+    TileArgs t = {};
+    if (!(make_map(&t.a[0], dgate, false, 64, 64, false) && make_map(&t.a[1], dup, false, 64, 64, false) &&
+          make_map(&t.b[0], x, false, 64, 64, false) && make_map(&t.out[0], dwg, false, kUnitCols, 128, true) &&
+          make_map(&t.out[1], dwu, false, kUnitCols, 128, true)))
+        return COLLAGE_ERR_CUDA;
+    t.b[1] = t.b[0];
+    t.m = static_cast<uint32_t>(dwg->rows);
+    t.n = static_cast<uint32_t>(dwg->cols);
+    t.problems = 2;
+    t.terms = 1;
+    t.k_blocks = static_cast<uint32_t>((x->rows + 63) / 64);
+    return t.m > 128 ? launch_tiles<false, true, true, false, 2>(t, sm_count, s) : launch_tiles<false, true, true, false, 1>(t, sm_count, s);
+}
+
+// ---- any alignment ---------------------------------------------------------------------------------------------------
+
 template <typename T, bool PAIRED>
 collage_status_t launch_product(const ProductArgs& p, cudaStream_t s) {
     if (p.m == 0 || p.n == 0) return COLLAGE_OK;
@@ -163,6 +279,16 @@ collage_status_t collage_gated_ffn(const collage_matrix_t* x, const collage_matr
     if (alias.clash()) return COLLAGE_ERR_ALIAS;
     DeviceInfo dev;
     if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (h->rows == 0 || h->cols == 0) return COLLAGE_OK;
+    if (x->cols == 0) {                                    // sums over no terms: gate = up = 0, h = a(0) * 0
+        for (int i = 3; i < 6 && st == COLLAGE_OK; ++i)
+            if (all[i]) st = clear_matrix(all[i], 2, s);
+        return st;
+    }
+    bool maps = true;
+    for (const collage_matrix_t* m : all) maps = maps && (!m || mappable(m, 2));
+    if (maps) return tiles_forward<false>(x, w_gate, w_up, h, gate, up, {nullptr, nullptr, nullptr}, activation, dev.sm_count, s);
     ProductArgs p = {};
     p.a[0] = by_row(x);
     p.b[0] = by_row(w_gate);
@@ -179,7 +305,7 @@ collage_status_t collage_gated_ffn(const collage_matrix_t* x, const collage_matr
     p.n = w_gate->rows;
     p.k = x->cols;
     p.activation = activation;
-    return launch_product<uint16_t, true>(p, static_cast<cudaStream_t>(stream));
+    return launch_product<uint16_t, true>(p, s);
 }
 
 collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float* x_scale, const collage_matrix_t* w_gate8,
@@ -203,6 +329,11 @@ collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float*
     if (alias.clash()) return COLLAGE_ERR_ALIAS;
     DeviceInfo dev;
     if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (h->rows == 0 || h->cols == 0) return COLLAGE_OK;
+    if (x8->cols == 0) return clear_matrix(h, 2, s);
+    if (mappable(x8, 1) && mappable(w_gate8, 1) && mappable(w_up8, 1) && mappable(h, 2))
+        return tiles_forward<true>(x8, w_gate8, w_up8, h, nullptr, nullptr, {x_scale, w_gate_scale, w_up_scale}, activation, dev.sm_count, s);
     ProductArgs p = {};
     p.a[0] = by_row(x8);
     p.b[0] = by_row(w_gate8);
@@ -216,7 +347,7 @@ collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float*
     p.n = w_gate8->rows;
     p.k = x8->cols;
     p.activation = activation;
-    return launch_product<uint8_t, true>(p, static_cast<cudaStream_t>(stream));
+    return launch_product<uint8_t, true>(p, s);
 }
 
 collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const collage_matrix_t* x, const collage_matrix_t* w_gate,
@@ -259,6 +390,22 @@ collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const co
         g.activation = activation;
         gate_backward_any_kernel<<<static_cast<unsigned>(dh->rows), 256, 0, s>>>(g);
         if ((st = launch_status()) != COLLAGE_OK) return st;
+    }
+    // a product over no tokens or no channels is zero
+    if (dh->rows == 0 || dh->cols == 0) {
+        if (dx) st = clear_matrix(dx, 2, s);
+        if (dw_gate && st == COLLAGE_OK) st = clear_matrix(dw_gate, 2, s);
+        if (dw_gate && st == COLLAGE_OK) st = clear_matrix(dw_up, 2, s);
+        return st;
+    }
+    const bool maps = mappable(dgate, 2) && mappable(dup, 2);
+    if (dx && dx->cols && maps && mappable(dx, 2) && mappable(w_gate, 2) && mappable(w_up, 2)) {
+        if ((st = tiles_dx(dgate, dup, w_gate, w_up, dx, dev.sm_count, s)) != COLLAGE_OK) return st;
+        dx = nullptr;
+    }
+    if (dw_gate && x->cols && maps && mappable(x, 2) && mappable(dw_gate, 2) && mappable(dw_up, 2)) {
+        if ((st = tiles_dw(dgate, dup, x, dw_gate, dw_up, dev.sm_count, s)) != COLLAGE_OK) return st;
+        dw_gate = nullptr;
     }
     if (dx) {
         ProductArgs p = {};
