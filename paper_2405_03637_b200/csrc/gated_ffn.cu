@@ -138,18 +138,6 @@ static bool mappable(const collage_matrix_t* m, uint32_t elem_bytes) {
     return rows_aligned(m, elem_bytes, 16) && m->cols * elem_bytes % 16 == 0 && (m->rows <= 1 || m->ld * elem_bytes < (1ull << 40));
 }
 
-// Once per kernel and device: leave to use the shared memory that it takes.
-template <auto Kernel>
-static cudaError_t allow_smem(int bytes) {
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
-    if (done.load(std::memory_order_acquire) >> (dev & 63) & 1) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
-    return e;
-}
-
 template <bool E4M3, bool A_MN, bool B_MN, bool GATED, int CTAS>
 static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) {
     constexpr uint32_t out_cols = (GATED ? 64 : 128) * CTAS;

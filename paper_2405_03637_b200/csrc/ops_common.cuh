@@ -100,6 +100,18 @@ inline collage_status_t clear_matrix(const collage_matrix_t* m, uint32_t elem_by
                                                                                                                   : COLLAGE_ERR_CUDA;
 }
 
+// Once per kernel and device: leave to use the shared memory that it takes.
+template <auto Kernel>
+static cudaError_t allow_smem(int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+    if (done.load(std::memory_order_acquire) >> (dev & 63) & 1) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
+    return e;
+}
+
 // ------------------------------------------------------------------------------------------------- device helpers ---
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
