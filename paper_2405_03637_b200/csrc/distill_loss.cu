@@ -27,7 +27,8 @@ struct DistillArgs {
     float inv_t, t;
 };
 
-constexpr int kDistillThreads = 512;
+constexpr int kDistillThreads = 256, kStagedThreads = 192;
+constexpr uint32_t kSeenWords = 512;           // two bitmaps over the indexes of a row, modulo 2^14
 constexpr uint32_t kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 // A stored lse of this size or more is rounded too coarsely to give q to 2^-17 (an infinite one to give it at all): the
@@ -35,36 +36,87 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLargeLse = 128.0f;
 // Up to this size of m c the exponent's argument is one fma, z c - m c; beyond it m c could overflow.
 constexpr float kLargeShift = 1e30f;
-constexpr size_t kMaxSmem = 227 * 1024 - 1024;                 // dynamic shared memory a block may take, beside its static part
-constexpr size_t kSliceBytes = 74 * 1024;                     // three blocks an SM
+constexpr size_t kSmSmem = 228 * 1024, kMaxSmem = 227 * 1024 - 5 * 1024;   // of an SM; dynamic part that a block may take
+constexpr size_t kSliceBytes = 74 * 1024 - 4608;             // dynamic part of a third of an SM
+
+// Two floats in a 64-bit register: one instruction works on both.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 floats_of(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 
 template <typename T>
-struct Vec;                      // 16 bytes of logits
+struct Vec;                      // 16 bytes of logits, as kPairs pairs of floats
 template <>
 struct Vec<uint16_t> {
-    static constexpr uint32_t kN = 8;
+    static constexpr uint32_t kN = 8, kPairs = 4;
     static constexpr uint32_t kLowest = 0xFF80FF80u;          // minus infinity
-    static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[8]) {
+    static __device__ __forceinline__ void unpack(const uint4& q, uint64_t (&f)[4]) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
+        for (int i = 0; i < 4; ++i) f[i] = pair_of(bf16_lo(w[i]), bf16_hi(w[i]));
     }
-    static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
-        return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    static __device__ __forceinline__ uint4 pack(const uint64_t (&f)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = floats_of(f[i]);
+            w[i] = pack_bf16(v.x, v.y);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    // the largest so far, kept as it is stored (two running maxima); a NaN is passed over
+    using Most = uint32_t;
+    static __device__ __forceinline__ Most lowest() { return kLowest; }
+    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ Most most(Most m, const uint4& q) { return max2(max2(max2(q.x, q.y), max2(q.z, q.w)), m); }
+    static __device__ __forceinline__ float most_value(Most m) { return fmaxf(bf16_lo(m), bf16_hi(m)); }
     static __device__ __forceinline__ float value(uint16_t v) { return bf16_value(v); }
     static __device__ __forceinline__ uint16_t rounded(float v) { return to_bf16(v); }
 };
 template <>
 struct Vec<float> {
-    static constexpr uint32_t kN = 4;
+    static constexpr uint32_t kN = 4, kPairs = 2;
     static constexpr uint32_t kLowest = 0xFF800000u;
-    static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[4]) {
-        f[0] = __uint_as_float(q.x); f[1] = __uint_as_float(q.y); f[2] = __uint_as_float(q.z); f[3] = __uint_as_float(q.w);
+    static __device__ __forceinline__ void unpack(const uint4& q, uint64_t (&f)[2]) {
+        f[0] = pair_of(__uint_as_float(q.x), __uint_as_float(q.y));
+        f[1] = pair_of(__uint_as_float(q.z), __uint_as_float(q.w));
     }
-    static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    static __device__ __forceinline__ uint4 pack(const uint64_t (&f)[2]) {
+        const float2 a = floats_of(f[0]), b = floats_of(f[1]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
     }
+    using Most = float;
+    static __device__ __forceinline__ Most lowest() { return -INFINITY; }
+    static __device__ __forceinline__ Most most(Most m, const uint4& q) {
+        return fmaxf(fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w))), m);
+    }
+    static __device__ __forceinline__ float most_value(Most m) { return m; }
     static __device__ __forceinline__ float value(float v) { return v; }
     static __device__ __forceinline__ float rounded(float v) { return v; }
 };
@@ -84,6 +136,29 @@ __device__ __forceinline__ float warp_max(float v) {
 __device__ __forceinline__ float rescaled(float s, float m, float to, float c) {
     return m == to ? s : m == -INFINITY ? (s != s ? s : 0.0f) : s * exp2f((m - to) * c);
 }
+
+// Adds exp2((f - m) c) over a vector to `total`.  SMALL: m c cannot overflow (|m c| < kLargeShift), the argument is an fma.
+template <typename T, bool SMALL>
+__device__ __forceinline__ void add_exps(const uint4& q, float m, float c, uint64_t& total) {
+    uint64_t f[Vec<T>::kPairs];
+    Vec<T>::unpack(q, f);
+    if constexpr (SMALL) {
+        const uint64_t c2 = pair_of(c, c), s2 = pair_of(-m * c, -m * c);
+#pragma unroll
+        for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
+            const float2 x = floats_of(fma_pair(f[i], c2, s2));
+            total = add_pair(total, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+        }
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
+            const float2 x = floats_of(f[i]);
+            total = add_pair(total, pair_of(x.x == m && m == -INFINITY ? 0.0f : fast_exp2((x.x - m) * c),
+                                            x.y == m && m == -INFINITY ? 0.0f : fast_exp2((x.y - m) * c)));
+        }
+    }
+}
+__device__ __forceinline__ bool small_shift(float m, float c) { return fabsf(m * c) < kLargeShift; }
 
 // What a row's blocks share, apart from the row itself.
 struct DistillShared {
@@ -108,6 +183,9 @@ struct RowVectors {
     }
     __device__ uint32_t count() const { return (off + vocab + kN - 1) / kN; }
     __device__ bool inside(uint32_t v) const { return (v || !off) && (v + 1) * kN <= off + vocab; }
+    // vectors [whole_begin, whole_end) of the row lie inside it; at most one before and one behind them do not
+    __device__ uint32_t whole_begin() const { return off ? 1 : 0; }
+    __device__ uint32_t whole_end() const { return (off + vocab) / kN; }
     // a vector at the row's edge, missing elements as minus infinity
     __device__ uint4 edge(uint32_t v) const {
         union { uint4 q; uint32_t w[4]; T e[kN]; } u;
@@ -122,17 +200,16 @@ struct RowVectors {
     __device__ uint4 load(uint32_t v) const { return inside(v) ? base[v] : edge(v); }
 };
 
-// A row of `vocab` logits by a cluster of blocks, each with a slice of it.  MODE 0: loss (and lse).  1: gradient from a
-// stored lse.  2: both.  STAGED: the slice stays in shared memory between the two passes over it; otherwise it is read
-// from global memory each time.
-template <typename T, int MODE, bool STAGED>
+// A row of `vocab` logits by a cluster of blocks, each with a slice of it that it streams from global memory, once for
+// maximum and sum and once for the gradient.  MODE 0: loss (and lse).  1: gradient from a stored lse.  2: both (rows
+// that are too long to be staged).
+template <typename T, int MODE>
 __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_constant__ DistillArgs a) {
     using V = Vec<T>;
     constexpr uint32_t kN = V::kN;
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ DistillShared sh;
-    uint4* stage = reinterpret_cast<uint4*>(dynamic);                                    // [slice]
-    float* tp = reinterpret_cast<float*>(dynamic + (STAGED ? 16ull * a.slice : 0));      // teacher: p, student's logit, index
+    float* tp = reinterpret_cast<float*>(dynamic);              // teacher: p, student's logit, index
     float* tz = tp + a.k;
     int* ti = reinterpret_cast<int*>(tz + a.k);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -143,38 +220,56 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
     const uint32_t first = rank * a.slice, end = min(first + a.slice, z.count());        // this block's vectors
     const float g = MODE ? a.row_scale[row] : 1.0f;
 
-    constexpr uint32_t kAhead = 4;              // vectors in flight for a thread that reads global memory
+    constexpr uint32_t kAhead = 4;              // vectors in flight for a thread
     const uint4 lowest = make_uint4(V::kLowest, V::kLowest, V::kLowest, V::kLowest);
+    // Whole vectors of the slice; the row's first and last one may be cut and are then left to one thread, by elements.
+    const uint32_t whole = first + (first < end && !z.inside(first)), whole_end = max(whole, end - (first < end && !z.inside(end - 1)));
+    auto each_cut = [&](auto&& f) {
+        if (threadIdx.x == 0 && whole > first && first < end) f(first);
+        if (threadIdx.x == 0 && whole_end < end && end - 1 >= whole) f(end - 1);
+    };
     // Gradients of the slice: `load(v)` gives a vector of logits, `value(f)` puts gradients in their place.
     auto write_row = [&](auto&& load, auto&& value) {
-        const bool alike = z.off == dz.off;
-        for (uint32_t v0 = first + threadIdx.x; v0 < end; v0 += kDistillThreads * kAhead) {
-            uint4 q[kAhead];
+        auto by_elements = [&](uint32_t v) {
+            uint64_t f[V::kPairs];
+            V::unpack(load(v), f);
+            value(f);
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i) q[i] = v0 + i * kDistillThreads < end ? load(v0 + i * kDistillThreads) : lowest;
+            for (uint32_t i = 0; i < kN; ++i) {
+                const int64_t e = static_cast<int64_t>(v) * kN + i - z.off;
+                const float2 g2 = floats_of(f[i / 2]);
+                if (e >= 0 && e < a.vocab) dz.row[e] = V::rounded(i % 2 ? g2.y : g2.x);
+            }
+        };
+        if (z.off == dz.off) {
+            uint32_t v = whole + threadIdx.x;
+            for (; v + (kAhead - 1) * kDistillThreads < whole_end; v += kDistillThreads * kAhead) {
+                uint4 q[kAhead];
 #pragma unroll
-            for (uint32_t n = 0; n < kAhead; ++n) {
-                const uint32_t v = v0 + n * kDistillThreads;
-                if (v >= end) break;
-                float f[kN];
-                V::unpack(q[n], f);
-                value(f);
-                if (alike && z.inside(v)) {
-                    dz.base[v] = V::pack(f);
-                } else {
+                for (uint32_t i = 0; i < kAhead; ++i) q[i] = load(v + i * kDistillThreads);
 #pragma unroll
-                    for (uint32_t i = 0; i < kN; ++i) {
-                        const int64_t e = static_cast<int64_t>(v) * kN + i - z.off;
-                        if (e >= 0 && e < a.vocab) dz.row[e] = V::rounded(f[i]);
-                    }
+                for (uint32_t i = 0; i < kAhead; ++i) {
+                    uint64_t f[V::kPairs];
+                    V::unpack(q[i], f);
+                    value(f);
+                    dz.base[v + i * kDistillThreads] = V::pack(f);
                 }
             }
+            for (; v < whole_end; v += kDistillThreads) {
+                uint64_t f[V::kPairs];
+                V::unpack(load(v), f);
+                value(f);
+                dz.base[v] = V::pack(f);
+            }
+            each_cut(by_elements);
+        } else {
+            for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads) by_elements(v);
         }
     };
     auto zeros = [&] {
-        write_row([&](uint32_t) { return lowest; }, [](float (&f)[kN]) {
+        write_row([&](uint32_t) { return lowest; }, [](uint64_t (&f)[V::kPairs]) {
 #pragma unroll
-            for (uint32_t i = 0; i < kN; ++i) f[i] = 0.0f;
+            for (uint32_t i = 0; i < V::kPairs; ++i) f[i] = 0;
         });
     };
     if (MODE && g == 0.0f) {
@@ -182,17 +277,8 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         if (MODE == 2 && rank == 0 && threadIdx.x == 0) a.loss[row] = 0.0f;
         return;
     }
-    if (a.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");     // this block runs
-    if constexpr (STAGED) {
-        for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads) {
-            if (z.inside(v))
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(umma::smem_addr(stage + v - first)), "l"(z.base + v) : "memory");
-            else
-                stage[v - first] = z.edge(v);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    auto vector = [&](uint32_t v) { return STAGED ? stage[v - first] : z.load(v); };
+    if (a.cluster > 1) umma::cluster_arrive_all();                       // this block runs
+    auto vector = [&](uint32_t v) { return z.load(v); };
 
     if (warp == 0) {                            // the teacher's entries: p over all of them, in every block of the row
         float most = -INFINITY;
@@ -231,68 +317,37 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         // maximum and sum of this thread's vectors, joined over the warp, the block and the cluster
         m = -INFINITY;
         sum = 0.0f;
-        if constexpr (STAGED) {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");          // a thread reads the vectors that it copied
-            for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads) {
-                float f[kN];
-                V::unpack(stage[v - first], f);
+        uint64_t total = 0;
+        auto take = [&](const uint4 (&q)[kAhead]) {
+            typename V::Most most = V::lowest();
 #pragma unroll
-                for (uint32_t i = 0; i < kN; ++i) m = fmaxf(m, f[i]);
+            for (uint32_t i = 0; i < kAhead; ++i) most = V::most(most, q[i]);
+            const float to = fmaxf(m, V::most_value(most));
+            if (to != m) {                  // a new maximum: what is summed so far is taken relative to it
+                const float2 so_far = floats_of(total);
+                total = pair_of(rescaled(so_far.x, m, to, c), rescaled(so_far.y, m, to, c));
+                m = to;
             }
-            const float shift = -m * c;
-            if (fabsf(shift) < kLargeShift) {
-                for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads) {
-                    float f[kN];
-                    V::unpack(stage[v - first], f);
+            if (small_shift(m, c)) {
 #pragma unroll
-                    for (uint32_t i = 0; i < kN; ++i) sum += fast_exp2(__fmaf_rn(f[i], c, shift));
-                }
+                for (uint32_t i = 0; i < kAhead; ++i) add_exps<T, true>(q[i], m, c, total);
             } else {
-                for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads) {
-                    float f[kN];
-                    V::unpack(stage[v - first], f);
 #pragma unroll
-                    for (uint32_t i = 0; i < kN; ++i) sum += f[i] == m && m == -INFINITY ? 0.0f : fast_exp2((f[i] - m) * c);
-                }
+                for (uint32_t i = 0; i < kAhead; ++i) add_exps<T, false>(q[i], m, c, total);
             }
-        } else {
-            for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads * kAhead) {
-                uint4 q[kAhead];
+        };
+        for (uint32_t v = whole + threadIdx.x; v < whole_end; v += kDistillThreads * kAhead) {
+            uint4 q[kAhead];
 #pragma unroll
-                for (uint32_t i = 0; i < kAhead; ++i) {
-                    const uint32_t at = v + i * kDistillThreads;
-                    q[i] = at < end ? z.load(at) : lowest;
-                }
-                float most = m;
-#pragma unroll
-                for (uint32_t i = 0; i < kAhead; ++i) {
-                    float f[kN];
-                    V::unpack(q[i], f);
-#pragma unroll
-                    for (uint32_t e = 0; e < kN; ++e) most = fmaxf(most, f[e]);
-                }
-                sum = rescaled(sum, m, most, c);
-                m = most;
-                const float shift = -m * c;
-                if (fabsf(shift) < kLargeShift) {
-#pragma unroll
-                    for (uint32_t i = 0; i < kAhead; ++i) {
-                        float f[kN];
-                        V::unpack(q[i], f);
-#pragma unroll
-                        for (uint32_t e = 0; e < kN; ++e) sum += fast_exp2(__fmaf_rn(f[e], c, shift));
-                    }
-                } else {
-#pragma unroll
-                    for (uint32_t i = 0; i < kAhead; ++i) {
-                        float f[kN];
-                        V::unpack(q[i], f);
-#pragma unroll
-                        for (uint32_t e = 0; e < kN; ++e) sum += f[e] == m && m == -INFINITY ? 0.0f : fast_exp2((f[e] - m) * c);
-                    }
-                }
-            }
+            for (uint32_t i = 0; i < kAhead; ++i) q[i] = v + i * kDistillThreads < whole_end ? z.base[v + i * kDistillThreads] : lowest;
+            take(q);
         }
+        each_cut([&](uint32_t v) {
+            uint4 q[kAhead] = {z.edge(v), lowest, lowest, lowest};
+            take(q);
+        });
+        const float2 sums = floats_of(total);
+        sum = sums.x + sums.y;
         float most = warp_max(m);
         sum = warp_sum(rescaled(sum, m, most, c));
         if (lane == 0) sh.warp[warp] = make_float2(most, sum);
@@ -301,19 +356,19 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         m = warp_max(w.x);
         sum = warp_sum(rescaled(w.y, w.x, m, c));
         if (a.cluster > 1) {
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");           // all blocks of the row run
+            umma::cluster_wait_all();           // all blocks of the row run
             if (threadIdx.x < a.cluster) {
                 const uint32_t to = umma::cluster_addr(&sh.part[rank], threadIdx.x);
                 asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(sum) : "memory");
             }
-            umma::cluster_sync();
+            umma::cluster_sync_any();
             const float2 r = lane < a.cluster ? sh.part[lane] : make_float2(-INFINITY, 0.0f);
             m = warp_max(r.x);
             sum = warp_sum(rescaled(r.y, r.x, m, c));
         }
     } else {
         __syncthreads();
-        if (a.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (a.cluster > 1) umma::cluster_wait_all();
     }
     // (a NaN is in no maximum, but in the sum; a row of -infinity has the sum 0 and no distribution)
     if (MODE == 0 && a.lse_out && rank == 0 && threadIdx.x == 0) a.lse_out[row] = m == -INFINITY && sum == 0.0f ? m : m * a.inv_t + logf(sum);
@@ -340,7 +395,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         for (uint32_t k = lane; k < a.k; k += 32) {
             const int i = ti[k];
             if (!mine(i)) continue;
-            const float v = V::value(STAGED ? reinterpret_cast<const T*>(stage)[static_cast<uint32_t>(i) + z.off - first * kN] : z.row[i]);
+            const float v = V::value(z.row[i]);
             const float p = tp[k];
             if (MODE != 1 && !(p == 0.0f)) loss = __fmaf_rn(p, tz[k] - sh.log_psum - ((v - m) * a.inv_t - logsum), loss);
             tz[k] = v;
@@ -355,7 +410,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         }
     }
     if (a.cluster > 1) {                        // (also: the whole row has been read before any of it is overwritten)
-        umma::cluster_sync();
+        umma::cluster_sync_any();
         if (MODE != 1 && rank == 0 && threadIdx.x == 0) {
             float loss = 0.0f;
             for (uint32_t r = 0; r < a.cluster; ++r) loss += sh.loss[r];
@@ -367,14 +422,21 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
     if (MODE) {
         const float gt = g * a.t;
         if (small) {
-            write_row(vector, [&](float (&f)[kN]) {
+            const uint64_t c2 = pair_of(c, c), s2 = pair_of(shift, shift), g2 = pair_of(gt, gt);
+            write_row(vector, [&](uint64_t (&f)[V::kPairs]) {
 #pragma unroll
-                for (uint32_t i = 0; i < kN; ++i) f[i] = gt * fast_exp2(__fmaf_rn(f[i], c, shift));
+                for (uint32_t i = 0; i < V::kPairs; ++i) {
+                    const float2 x = floats_of(fma_pair(f[i], c2, s2));
+                    f[i] = mul_pair(g2, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+                }
             });
         } else {
-            write_row(vector, [&](float (&f)[kN]) {
+            write_row(vector, [&](uint64_t (&f)[V::kPairs]) {
 #pragma unroll
-                for (uint32_t i = 0; i < kN; ++i) f[i] = gt * q_of(f[i]);
+                for (uint32_t i = 0; i < V::kPairs; ++i) {
+                    const float2 x = floats_of(f[i]);
+                    f[i] = pair_of(gt * q_of(x.x), gt * q_of(x.y));
+                }
             });
         }
         __syncthreads();                        // the dense part is written; now the teacher's entries over it
@@ -389,51 +451,332 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
     }
 }
 
-template <typename T, int MODE, bool STAGED>
-static collage_status_t launch_distill_as(DistillArgs& a, uint64_t rows, size_t smem, cudaStream_t s) {
-    constexpr auto kernel = &distill_kernel<T, MODE, STAGED>;
-    if (allow_smem<kernel>(kMaxSmem) != cudaSuccess) return COLLAGE_ERR_CUDA;
-    if (rows * a.cluster >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
+// Loss and gradient of rows that fit the shared memory of a cluster: each block keeps its slice of a row between the two
+// passes over it and walks over rows.  A thread owns the same places of the slice for every row: as soon as it has made
+// the gradient of a place it sends for the next row's vector, so loads, exponentials and stores of two rows overlap.
+struct StagedShared {
+    float2 warp[kStagedThreads / 32];
+    float2 part[2][kMaxCluster];          // (maximum, sum) of each block of the cluster; two rows' worth
+    float loss[2][kMaxCluster];
+    uint32_t seen[kSeenWords], again[kSeenWords];
+    int any_there;
+    float log_psum;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const __grid_constant__ DistillArgs a, uint64_t rows) {
+    using V = Vec<T>;
+    constexpr uint32_t kN = V::kN;
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    __shared__ StagedShared sh;
+    uint4* stage = reinterpret_cast<uint4*>(dynamic);                                     // [slice]
+    int64_t* raw_index = reinterpret_cast<int64_t*>(dynamic + 16ull * a.slice);           // [k], 4 or 8 bytes each: as it came
+    float* raw_top = reinterpret_cast<float*>(raw_index + a.k);                           // [k]
+    float* tp = raw_top + a.k;                                                            // [k] teacher's p
+    float* tz = tp + a.k;                                                                 // [k] student's logit
+    int* ti = reinterpret_cast<int*>(tz + a.k);                                           // [k] index, -1 = absent
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = a.cluster > 1 ? umma::cluster_rank() : 0, first = rank * a.slice;
+    const uint64_t step = gridDim.x / a.cluster;
+    const float c = a.inv_t * kLog2e;
+    const uint32_t stage_addr = umma::smem_addr(stage);
+
+    auto logits_of = [&](uint64_t row) { return RowVectors<T>(const_cast<T*>(static_cast<const T*>(a.logits)) + row * a.ldz, a.vocab); };
+    auto send_for = [&](const RowVectors<T>& z, uint32_t v) {
+        if (z.inside(v))
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(umma::smem_addr(stage + v - first)), "l"(z.base + v) : "memory");
+        else
+            stage[v - first] = z.edge(v);
+    };
+    auto send_for_teacher = [&](uint64_t row) {
+        for (uint32_t k = threadIdx.x; k < a.k; k += kStagedThreads) {
+            const uint64_t at = row * a.ldi + k;
+            if (a.index_bytes == 8)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(umma::smem_addr(raw_index + k)), "l"(static_cast<const int64_t*>(a.top_index) + at) : "memory");
+            else
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(umma::smem_addr(reinterpret_cast<int32_t*>(raw_index) + k)), "l"(static_cast<const int32_t*>(a.top_index) + at) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(umma::smem_addr(raw_top + k)), "l"(a.top_logits + row * a.ldt + k) : "memory");
+        }
+    };
+    auto send_for_row = [&](uint64_t row) {
+        const RowVectors<T> z = logits_of(row);
+        const uint32_t end = min(first + a.slice, z.count());
+        for (uint32_t v = first + threadIdx.x; v < end; v += kStagedThreads) send_for(z, v);
+        send_for_teacher(row);
+    };
+
+    uint64_t row = blockIdx.x / a.cluster;
+    float g = row < rows ? a.row_scale[row] : 0.0f;
+    uint32_t turn = 0;                          // rows with an exchange so far
+    if (a.cluster > 1) umma::cluster_sync_any();    // all blocks run before one writes into another
+    if (g != 0.0f) send_for_row(row);
+    for (; row < rows; row += step) {
+        const RowVectors<T> z = logits_of(row), dz(static_cast<T*>(a.dlogits) + row * a.ldd, a.vocab);
+        const uint32_t end = min(first + a.slice, z.count());
+        const bool more = row + step < rows;
+        const float g_next = more ? a.row_scale[row + step] : 0.0f;
+        const RowVectors<T> zn = logits_of(more ? row + step : row);
+        const uint32_t end_next = g_next != 0.0f ? min(first + a.slice, zn.count()) : 0;
+
+        // Gradients of this thread's places, and the next row into them.  `value(f)` puts gradients in the logits' place.
+        constexpr uint32_t kAhead = 4, kBatch = kAhead * kStagedThreads;
+        const bool alike = z.off == dz.off;
+        // batches of places that are whole vectors of both rows need no further checks
+        const uint32_t plain_begin = max(z.whole_begin(), end_next ? zn.whole_begin() : 0);
+        const uint32_t plain_end = alike ? min(min(z.whole_end(), end), end_next ? min(zn.whole_end(), end_next) : end) : 0;
+        auto write_row = [&](bool staged, auto&& value) {
+            const uint32_t last = max(end, end_next);
+#pragma unroll 1
+            for (uint32_t v0 = first + threadIdx.x; v0 < last; v0 += kBatch) {
+                if (v0 >= plain_begin && v0 + (kBatch - kStagedThreads) < plain_end) {
+                    uint64_t f[kAhead][V::kPairs];
+                    if (staged) {
+#pragma unroll
+                        for (uint32_t n = 0; n < kAhead; ++n) V::unpack(stage[v0 - first + n * kStagedThreads], f[n]);
+                    }
+#pragma unroll
+                    for (uint32_t n = 0; n < kAhead; ++n) value(f[n]);
+                    if (end_next) {
+#pragma unroll
+                        for (uint32_t n = 0; n < kAhead; ++n)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(stage_addr + 16 * (v0 - first + n * kStagedThreads)),
+                                         "l"(zn.base + v0 + n * kStagedThreads)
+                                         : "memory");
+                    }
+#pragma unroll
+                    for (uint32_t n = 0; n < kAhead; ++n) dz.base[v0 + n * kStagedThreads] = V::pack(f[n]);
+                } else {
+#pragma unroll 1
+                    for (uint32_t v = v0; v < min(v0 + kBatch, last); v += kStagedThreads) {
+                        uint64_t f[V::kPairs];
+                        V::unpack(stage[v - first], f);
+                        value(f);
+                        if (v < end_next) send_for(zn, v);
+                        if (v >= end) continue;
+                        if (alike && z.inside(v)) {
+                            dz.base[v] = V::pack(f);
+                        } else {
+#pragma unroll
+                            for (uint32_t i = 0; i < kN; ++i) {
+                                const int64_t e = static_cast<int64_t>(v) * kN + i - z.off;
+                                const float2 p = floats_of(f[i / 2]);
+                                if (e >= 0 && e < a.vocab) dz.row[e] = V::rounded(i % 2 ? p.y : p.x);
+                            }
+                        }
+                    }
+                }
+            }
+            if (end_next) send_for_teacher(row + step);
+        };
+        auto zero = [](uint64_t (&f)[V::kPairs]) {
+#pragma unroll
+            for (uint32_t i = 0; i < V::kPairs; ++i) f[i] = 0;
+        };
+        if (g == 0.0f) {                        // weighs nothing: not read
+            write_row(false, zero);
+            if (rank == 0 && threadIdx.x == 0) a.loss[row] = 0.0f;
+            g = g_next;
+            continue;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();                        // the row and the teacher's entries are there; the last row's are done with
+
+        for (uint32_t i = threadIdx.x; i < kSeenWords; i += kStagedThreads) sh.seen[i] = sh.again[i] = 0;
+        if (warp == 0) {                        // the teacher's p
+            float most = -INFINITY;
+            bool bad = false;
+            for (uint32_t k = lane; k < a.k; k += 32) {
+                const int64_t i = a.index_bytes == 8 ? raw_index[k] : reinterpret_cast<const int32_t*>(raw_index)[k];
+                const bool there = i >= 0 && i < static_cast<int64_t>(a.vocab);
+                const float t = there ? raw_top[k] * a.inv_t : -INFINITY;
+                ti[k] = there ? static_cast<int>(i) : -1;
+                tp[k] = t;
+                most = fmaxf(most, t);
+                bad |= t != t;
+            }
+            most = warp_max(most);
+            const bool any_there = __any_sync(0xFFFFFFFFu, bad) || most > -INFINITY;
+            float psum = 0.0f;
+            for (uint32_t k = lane; k < a.k; k += 32) psum += expf(tp[k] - most);
+            psum = warp_sum(psum);
+            for (uint32_t k = lane; k < a.k; k += 32) {
+                const float shifted = tp[k] - most;
+                tp[k] = expf(shifted) / psum;
+                tz[k] = shifted;                // until the student's logit takes its place
+            }
+            if (lane == 0) {
+                sh.any_there = any_there;
+                sh.log_psum = logf(psum);
+            }
+        }
+        // maximum and sum of this thread's vectors, joined over the warp, the block and the cluster
+        auto each_place = [&](auto&& f) {
+            uint32_t v = threadIdx.x;
+            for (; v + (kBatch - kStagedThreads) < end - first; v += kBatch) {
+                uint4 q[kAhead];
+#pragma unroll
+                for (uint32_t n = 0; n < kAhead; ++n) q[n] = stage[v + n * kStagedThreads];
+#pragma unroll
+                for (uint32_t n = 0; n < kAhead; ++n) f(q[n], n);
+            }
+            for (; v < end - first; v += kStagedThreads) f(stage[v], 0);
+        };
+        float m = -INFINITY;
+        uint64_t total = 0;
+        if (first < end) {
+            typename V::Most largest[2] = {V::lowest(), V::lowest()};
+            each_place([&](const uint4& q, uint32_t n) { largest[n & 1] = V::most(largest[n & 1], q); });
+            m = fmaxf(V::most_value(largest[0]), V::most_value(largest[1]));
+            uint64_t part[2] = {0, 0};
+            if (small_shift(m, c))
+                each_place([&](const uint4& q, uint32_t n) { add_exps<T, true>(q, m, c, part[n & 1]); });
+            else
+                each_place([&](const uint4& q, uint32_t n) { add_exps<T, false>(q, m, c, part[n & 1]); });
+            total = add_pair(part[0], part[1]);
+        }
+        const float2 sums = floats_of(total);
+        float most = warp_max(m), sum = warp_sum(rescaled(sums.x + sums.y, m, most, c));
+        if (lane == 0) sh.warp[warp] = make_float2(most, sum);
+        __syncthreads();
+        const float2 w = lane < kStagedThreads / 32 ? sh.warp[lane] : make_float2(-INFINITY, 0.0f);
+        m = warp_max(w.x);
+        sum = warp_sum(rescaled(w.y, w.x, m, c));
+        if (a.cluster > 1) {
+            if (threadIdx.x < a.cluster) {
+                const uint32_t to = umma::cluster_addr(&sh.part[turn & 1][rank], threadIdx.x);
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(sum) : "memory");
+            }
+            umma::cluster_sync_any();
+            const float2 r = lane < a.cluster ? sh.part[turn & 1][lane] : make_float2(-INFINITY, 0.0f);
+            m = warp_max(r.x);
+            sum = warp_sum(rescaled(r.y, r.x, m, c));
+        }
+        if (m == -INFINITY) sum = NAN;          // a row without any number in it has no distribution
+        const float logsum = logf(sum), log2sum = log2f(sum), shift = -m * c - log2sum;
+        const bool small = fabsf(m * c) < kLargeShift, live = sh.any_there;
+        auto q_of = [&](float v) { return fast_exp2(small ? __fmaf_rn(v, c, shift) : (v - m) * c - log2sum); };
+        auto mine = [&](int i) {
+            const uint32_t v = (static_cast<uint32_t>(i) + z.off) / kN;
+            return i >= 0 && v >= first && v < end;
+        };
+        if (warp == 0) {                        // entries in this block's slice: the student's logit, and their part of the loss
+            float loss = 0.0f;
+            for (uint32_t k = lane; k < a.k; k += 32) {
+                const int i = ti[k];
+                if (!mine(i)) continue;
+                const float v = V::value(reinterpret_cast<const T*>(stage)[static_cast<uint32_t>(i) + z.off - first * kN]);
+                const float p = tp[k];
+                if (!(p == 0.0f)) loss = __fmaf_rn(p, tz[k] - sh.log_psum - ((v - m) * a.inv_t - logsum), loss);
+                tz[k] = v;
+                const uint32_t bit = 1u << (i & 31), word = (static_cast<uint32_t>(i) >> 5) % kSeenWords;
+                if (atomicOr(&sh.seen[word], bit) & bit) atomicOr(&sh.again[word], bit);
+            }
+            loss = warp_sum(loss);
+            if (lane == 0) {
+                if (a.cluster > 1)
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(umma::cluster_addr(&sh.loss[turn & 1][rank], 0)), "f"(loss) : "memory");
+                else
+                    a.loss[row] = live ? g * (loss * a.t * a.t) : 0.0f;
+            }
+        }
+        __syncthreads();                        // the entries' logits are taken: the slice may be overwritten
+        if (a.cluster > 1) umma::cluster_arrive_all();
+        const float gt = g * a.t;
+        if (!live) {                            // nothing to learn from: zeros whatever the logits are
+            write_row(false, zero);
+        } else if (small) {
+            const uint64_t c2 = pair_of(c, c), s2 = pair_of(shift, shift), g2 = pair_of(gt, gt);
+            write_row(true, [&](uint64_t (&f)[V::kPairs]) {
+#pragma unroll
+                for (uint32_t i = 0; i < V::kPairs; ++i) {
+                    const float2 x = floats_of(fma_pair(f[i], c2, s2));
+                    f[i] = mul_pair(g2, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+                }
+            });
+        } else {
+            write_row(true, [&](uint64_t (&f)[V::kPairs]) {
+#pragma unroll
+                for (uint32_t i = 0; i < V::kPairs; ++i) {
+                    const float2 x = floats_of(f[i]);
+                    f[i] = pair_of(gt * q_of(x.x), gt * q_of(x.y));
+                }
+            });
+        }
+        if (a.cluster > 1) {
+            umma::cluster_wait_all();
+            if (rank == 0 && threadIdx.x == 0) {
+                float loss = 0.0f;
+                for (uint32_t r = 0; r < a.cluster; ++r) loss += sh.loss[turn & 1][r];
+                a.loss[row] = live ? g * (loss * a.t * a.t) : 0.0f;
+            }
+        }
+        __syncthreads();                        // the dense part is written; now the teacher's entries over it
+        for (uint32_t k = threadIdx.x; k < a.k && live; k += kStagedThreads) {
+            const int i = ti[k];
+            if (!mine(i)) continue;
+            float p = tp[k];
+            // an index that appears more than once: all its threads add up the same sum.  (Indexes that share a bit are
+            // searched too, and found alone.)
+            if (sh.again[(static_cast<uint32_t>(i) >> 5) % kSeenWords] >> (i & 31) & 1) {
+                p = 0.0f;
+                for (uint32_t o = 0; o < a.k; ++o)
+                    if (ti[o] == i) p += tp[o];
+            }
+            dz.row[i] = V::rounded(gt * (q_of(tz[k]) - p));
+        }
+        g = g_next;
+        ++turn;
+    }
+    if (a.cluster > 1) umma::cluster_sync_any();    // no block leaves while another may still write to it
+}
+
+template <auto Kernel, typename... Args>
+static collage_status_t launch_rows(uint64_t blocks, int threads, uint32_t cluster, size_t smem, cudaStream_t s, Args... args) {
+    if (allow_smem<Kernel>(kMaxSmem) != cudaSuccess) return COLLAGE_ERR_CUDA;
+    if (blocks >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(rows * a.cluster));
-    cfg.blockDim = dim3(kDistillThreads);
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {a.cluster, 1, 1};
+    attr[0].val.clusterDim = {cluster, 1, 1};
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, Kernel, args...) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
 }
 
 template <int MODE>
 static collage_status_t launch_distill(DistillArgs& a, uint64_t rows, collage_dtype_t dtype, int sm_count, void* stream) {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const uint32_t per_vector = dtype == COLLAGE_DTYPE_BF16 ? 8 : 4;
+    const bool bf16 = dtype == COLLAGE_DTYPE_BF16;
+    const uint32_t per_vector = bf16 ? 8 : 4;
     const uint32_t vectors = (a.vocab + 2 * per_vector - 2) / per_vector;        // at the worst alignment
-    const size_t teacher = 12ull * a.k;
-    bool staged = MODE == 2;
     a.cluster = 1;
     auto slice = [&] { return (vectors + a.cluster - 1) / a.cluster; };
-    // three blocks of an SM hold their slices; beyond eight of those, one block may take all of the shared memory
-    while (staged && a.cluster < kMaxCluster && 16ull * slice() + teacher > kSliceBytes) a.cluster *= 2;
-    if (staged && 16ull * slice() + teacher > kMaxSmem) {
-        staged = false;
+    // few rows: more blocks for each, down to a vector a thread
+    auto spread = [&](uint32_t threads) {
+        while (a.cluster < kMaxCluster && rows * a.cluster * 2 <= static_cast<uint64_t>(sm_count) && slice() > threads) a.cluster *= 2;
+        a.slice = slice();
+    };
+    if constexpr (MODE == 2) {
+        const size_t teacher = 24ull * a.k;
+        // three blocks of an SM hold their slices; beyond eight of those, one block may take all of the shared memory
+        while (a.cluster < kMaxCluster && 16ull * slice() + teacher > kSliceBytes) a.cluster *= 2;
+        if (16ull * slice() + teacher <= kMaxSmem) {
+            spread(kStagedThreads);
+            const size_t smem = 16ull * a.slice + teacher;
+            const uint64_t fit = std::max<uint64_t>(1, std::min<uint64_t>(3, (kSmSmem - 1024) / (smem + sizeof(StagedShared) + 1024)));
+            const uint64_t groups = std::min<uint64_t>(rows, std::max<uint64_t>(1, fit * sm_count / a.cluster));
+            return bf16 ? launch_rows<&distill_staged_kernel<uint16_t>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows)
+                        : launch_rows<&distill_staged_kernel<float>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows);
+        }
         a.cluster = 1;
     }
-    // few rows: more blocks for each, down to a vector a thread
-    while (a.cluster < kMaxCluster && rows * a.cluster * 2 <= static_cast<uint64_t>(sm_count) && slice() > kDistillThreads) a.cluster *= 2;
-    a.slice = slice();
-    const size_t smem = (staged ? 16ull * a.slice : 0) + teacher;
-    if (dtype == COLLAGE_DTYPE_BF16) {
-        if constexpr (MODE == 2)
-            if (staged) return launch_distill_as<uint16_t, MODE, true>(a, rows, smem, s);
-        return launch_distill_as<uint16_t, MODE, false>(a, rows, smem, s);
-    }
-    if constexpr (MODE == 2)
-        if (staged) return launch_distill_as<float, MODE, true>(a, rows, smem, s);
-    return launch_distill_as<float, MODE, false>(a, rows, smem, s);
+    spread(kDistillThreads);
+    return bf16 ? launch_rows<&distill_kernel<uint16_t, MODE>>(rows * a.cluster, kDistillThreads, a.cluster, 12ull * a.k, s, a)
+                : launch_rows<&distill_kernel<float, MODE>>(rows * a.cluster, kDistillThreads, a.cluster, 12ull * a.k, s, a);
 }
 
 // Everything the three entry points check alike; `read` and `written` are their float[rows] arrays.

@@ -136,33 +136,44 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// Sum over the block in a fixed order, the result in every thread.  `slots`: one float a warp.
-template <int THREADS>
-__device__ __forceinline__ float block_sum(float v, float* slots) {
+// Sum over a block of `warps` warps in a fixed order, the result in every thread.  `slots`: one float a warp.
+__device__ __forceinline__ float block_sum(float v, float* slots, int warps) {
     v = warp_sum(v);
-    if constexpr (THREADS > 32) {
+    if (warps > 1) {
         __syncthreads();
         if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
         __syncthreads();
         const int lane = threadIdx.x & 31;
-        v = warp_sum(lane < THREADS / 32 ? slots[lane] : 0.0f);
+        v = warp_sum(lane < warps ? slots[lane] : 0.0f);
     }
     return v;
 }
 
 // Largest unsigned word over the block.  On the bits of |x| this orders NaN above infinity above every number.
-template <int THREADS>
-__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* slots) {
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* slots, int warps) {
     v = __reduce_max_sync(0xFFFFFFFFu, v);
-    if constexpr (THREADS > 32) {
+    if (warps > 1) {
         __syncthreads();
         if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
         __syncthreads();
         const int lane = threadIdx.x & 31;
-        v = __reduce_max_sync(0xFFFFFFFFu, lane < THREADS / 32 ? slots[lane] : 0u);
+        v = __reduce_max_sync(0xFFFFFFFFu, lane < warps ? slots[lane] : 0u);
     }
     return v;
 }
+
+// x / d for many x: Markstein's division by a correctly rounded reciprocal.  q = RN(x r) is off by a unit at most, its
+// remainder x - q d is exact in an fma, and RN(q + remainder r) is the correctly rounded quotient, where nothing leaves
+// the normal range (`plain`); elsewhere the division itself.
+struct Divisor {
+    float d, r;
+    bool plain;
+    __device__ __forceinline__ explicit Divisor(float divisor) : d(divisor), r(1.0f / divisor), plain(divisor > 0x1p-100f && divisor < 0x1p100f) {}
+    __device__ __forceinline__ float quotient(float x) const {
+        const float q = x * r;
+        return __fmaf_rn(__fmaf_rn(-q, d, x), r, q);
+    }
+};
 
 }  // namespace ops
 }  // namespace collage

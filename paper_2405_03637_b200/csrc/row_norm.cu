@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
             const float r = value(j);
             sum = __fmaf_rn(r, r, sum);
         }
-        sum = block_sum<kRowThreads>(sum, slots);
+        sum = block_sum(sum, slots, kRowThreads / 32);
         rstd = 1.0f / sqrtf(sum / static_cast<float>(a.cols) + a.eps);
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     }
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
         uint32_t most = 0;
         for (uint64_t j = threadIdx.x; j < a.cols; j += kRowThreads)
             most = max(most, __float_as_uint(normed(value(j), j)) & 0x7FFFFFFFu);
-        most = block_max<kRowThreads>(most, reinterpret_cast<uint32_t*>(slots));
+        most = block_max(most, reinterpret_cast<uint32_t*>(slots), kRowThreads / 32);
         scale = __uint_as_float(most) / kE4m3Max;
         if (threadIdx.x == 0) a.scale[row] = scale;
     }
@@ -56,6 +56,123 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
         if (a.y) a.y[row * a.ldy + j] = to_bf16(y);
         if (a.y8) a.y8[row * a.ldy8 + j] = scale == 0.0f ? 0 : to_e4m3(y / scale);
     }
+}
+
+__device__ __forceinline__ void unpack8(const uint4& q, float (&f)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// Rows of whole 16-byte vectors, read once and kept in registers: PER vectors a thread, a row by one warp (WARP: four rows a
+// block) or by a block of as many warps as it takes.
+template <int PER, bool NORM, bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) row_kernel(const __grid_constant__ RowArgs a, uint64_t rows) {
+    __shared__ float slots[32];
+    const uint64_t row = WARP ? blockIdx.x * 4ull + (threadIdx.x >> 5) : blockIdx.x;
+    if (WARP && row >= rows) return;
+    const int t = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x, warps = threads >> 5;
+    const int vectors = static_cast<int>(a.cols >> 3);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    float r[PER][8];
+    uint4 q[PER], qr[PER], qw[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * threads;
+        q[i] = v < vectors ? reinterpret_cast<const uint4*>(a.x + row * a.ldx)[v] : none;
+        if (NORM && a.residual) qr[i] = v < vectors ? reinterpret_cast<const uint4*>(a.residual + row * a.ldres)[v] : none;
+    }
+    if (NORM) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) qw[i] = t + i * threads < vectors ? __ldg(reinterpret_cast<const uint4*>(a.weight) + t + i * threads) : none;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        unpack8(q[i], r[i]);
+        if (NORM && a.residual) {
+            float s[8];
+            unpack8(qr[i], s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[i][e] += s[e];
+        }
+    }
+    if (NORM) {
+        float part[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            part[i] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[i] = __fmaf_rn(r[i][e], r[i][e], part[i]);
+        }
+        float sum = part[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) sum += part[i];
+        sum = block_sum(sum, slots, warps);
+        const float rstd = 1.0f / sqrtf(sum / static_cast<float>(a.cols) + a.eps);
+        if (a.rstd && t == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * threads;
+            if (a.residual_out && v < vectors) reinterpret_cast<uint4*>(a.residual_out + row * a.ldro)[v] = pack8(r[i]);
+            float w[8];
+            unpack8(qw[i], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[i][e] = r[i][e] * rstd * w[e];
+            if (a.y && v < vectors) reinterpret_cast<uint4*>(a.y + row * a.ldy)[v] = pack8(r[i]);
+        }
+    }
+    if (a.y8) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(r[i][e]) & 0x7FFFFFFFu);
+        most = block_max(most, reinterpret_cast<uint32_t*>(slots), warps);
+        const float scale = __uint_as_float(most) / kE4m3Max;
+        if (t == 0) a.scale[row] = scale;
+        const Divisor by(scale);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * threads;
+            if (v >= vectors) continue;
+            uint32_t w[2] = {0, 0};
+            if (by.plain) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) w[e >> 2] |= pack_e4m3(by.quotient(r[i][e]), by.quotient(r[i][e + 1])) << (8 * (e & 2));
+            } else if (scale != 0.0f) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) w[e >> 2] |= pack_e4m3(r[i][e] / scale, r[i][e + 1] / scale) << (8 * (e & 2));
+            }
+            reinterpret_cast<uint2*>(a.y8 + row * a.ldy8)[v] = make_uint2(w[0], w[1]);
+        }
+    }
+}
+
+// A row's vectors over warps: with many rows four vectors a thread (more loads in flight, fewer warps to join), with few rows
+// one (the shortest way through a row), as far as 1024 or 512 threads reach.
+template <bool NORM>
+static collage_status_t launch_rows(const RowArgs& a, uint64_t rows, bool vectors_fit, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3, n = rows;
+    const bool many = rows > 2ull * sm_count;
+    if (!vectors_fit || v > 4096) {
+        row_any_kernel<NORM><<<static_cast<unsigned>(rows), kRowThreads, 0, s>>>(a);
+    } else if (many && v <= 128) {
+        const unsigned grid = static_cast<unsigned>((rows + 3) / 4);
+        if (v <= 32) row_kernel<1, NORM, true><<<grid, 128, 0, s>>>(a, n);
+        else if (v <= 64) row_kernel<2, NORM, true><<<grid, 128, 0, s>>>(a, n);
+        else row_kernel<4, NORM, true><<<grid, 128, 0, s>>>(a, n);
+    } else {
+        const uint64_t per = v > 2048 ? 8 : many ? 4 : v > 1024 ? 2 : 1;
+        const unsigned threads = static_cast<unsigned>((v + per * 32 - 1) / (per * 32) * 32), grid = static_cast<unsigned>(rows);
+        if (per == 1) row_kernel<1, NORM, false><<<grid, threads, 0, s>>>(a, n);
+        else if (per == 2) row_kernel<2, NORM, false><<<grid, threads, 0, s>>>(a, n);
+        else if (per == 4) row_kernel<4, NORM, false><<<grid, threads, 0, s>>>(a, n);
+        else row_kernel<8, NORM, false><<<grid, threads, 0, s>>>(a, n);
+    }
+    return launch_status();
 }
 
 struct RowBackwardArgs {
@@ -82,7 +199,7 @@ __global__ void __launch_bounds__(kRowThreads) row_backward_any_kernel(const __g
     float sum = 0.0f;
     for (uint64_t j = threadIdx.x; j < a.cols; j += kRowThreads)
         sum = __fmaf_rn(bf16_value(dy[j]) * bf16_value(a.weight[j]), bf16_value(r[j]) * rstd, sum);
-    const float mean = block_sum<kRowThreads>(sum, slots) / static_cast<float>(a.cols);
+    const float mean = block_sum(sum, slots, kRowThreads / 32) / static_cast<float>(a.cols);
     for (uint64_t j = threadIdx.x; j < a.cols; j += kRowThreads) {
         float d = rstd * __fmaf_rn(-bf16_value(r[j]) * rstd, mean, bf16_value(dy[j]) * bf16_value(a.weight[j]));
         if (dres) d += bf16_value(dres[j]);
@@ -90,7 +207,7 @@ __global__ void __launch_bounds__(kRowThreads) row_backward_any_kernel(const __g
     }
 }
 
-constexpr int kWeightChunks = 256;        // row chunks whose sums are kept apart
+constexpr int kWeightChunks = 320;        // row chunks whose sums are kept apart
 
 // Sums of dy * n over a chunk of rows, 32 columns a block.
 __global__ void __launch_bounds__(kRowThreads) row_dweight_any_kernel(const __grid_constant__ RowBackwardArgs a) {
@@ -111,12 +228,176 @@ __global__ void __launch_bounds__(kRowThreads) row_dweight_any_kernel(const __gr
     }
 }
 
+// Gradients of rows of whole vectors in one pass: blocks walk over rows, one at a time for each group of `group` threads.
+// A thread owns PER vectors of columns: it sends for its own of the next two rows ahead (so loads go on while the row's
+// sum is joined), and keeps its columns' part of dweight in registers until the end.
+constexpr int kBackwardThreads = 512, kDepth = 2;
+
+template <int PER, int THREADS>
+__global__ void __launch_bounds__(THREADS, PER > 1 ? 1 : 2) row_backward_kernel(const __grid_constant__ RowBackwardArgs a, int group_threads) {
+    __shared__ float slots[2][32];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
+    const int lane = threadIdx.x & 31, group_warps = group_threads >> 5, warp0 = group * group_warps;
+    const int vectors = static_cast<int>(a.cols >> 3);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    uint4* mine = reinterpret_cast<uint4*>(dynamic) + threadIdx.x;      // [kDepth][3][PER] places, blockDim.x apart
+    auto place = [&](int stage, int array, int i) { return mine + ((stage * 3 + array) * PER + i) * blockDim.x; };
+    uint4 qw[PER];
+    float dw[PER][8];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        qw[i] = t + i * group_threads < vectors ? reinterpret_cast<const uint4*>(a.weight)[t + i * group_threads] : none;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+        for (int d = 0; d < kDepth; ++d)
+            for (int k = 0; k < 3; ++k) *place(d, k, i) = none;         // places that no load fills
+    }
+    const bool with_res = a.dresidual && a.dx;
+    const uint64_t first = blockIdx.x * static_cast<uint64_t>(groups) + group, step = static_cast<uint64_t>(gridDim.x) * groups;
+    auto send_for = [&](uint64_t row, int stage) {
+        if (row < a.rows) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int v = t + i * group_threads;
+                if (v >= vectors) continue;
+                auto copy = [&](int k, const uint16_t* base, uint64_t ld) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(place(stage, k, i)))),
+                                 "l"(reinterpret_cast<const uint4*>(base + row * ld) + v)
+                                 : "memory");
+                };
+                copy(0, a.dy, a.lddy);
+                copy(1, a.r, a.ldr);
+                if (with_res) copy(2, a.dresidual, a.lddres);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) send_for(first + d * step, d);
+    const float per_col = 1.0f / static_cast<float>(a.cols);
+    int stage = 0, turn = 0;
+    float rstd_next = first < a.rows ? a.rstd[first] : 0.0f;
+    for (uint64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        const float rstd = rstd_next;
+        rstd_next = row + step < a.rows ? a.rstd[row + step] : 0.0f;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+        uint4 qy[PER], qr[PER], qd[PER];        // kept as they are: unpacked once for the sum and once for dx
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            qy[i] = *place(stage, 0, i);
+            qr[i] = *place(stage, 1, i);
+            if (with_res) qd[i] = *place(stage, 2, i);
+            float y[8], r[8], w[8];
+            unpack8(qy[i], y);
+            unpack8(qr[i], r);
+            unpack8(qw[i], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float n = r[e] * rstd;
+                dw[i][e] = __fmaf_rn(y[e], n, dw[i][e]);
+                sum = __fmaf_rn(y[e] * w[e], n, sum);
+            }
+        }
+        send_for(row + kDepth * step, stage);
+        stage = stage + 1 == kDepth ? 0 : stage + 1;
+        if (!a.dx) continue;
+        sum = warp_sum(sum);
+        if (group_warps > 1) {
+            if (lane == 0) slots[turn][threadIdx.x >> 5] = sum;
+            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
+            sum = warp_sum(lane < group_warps ? slots[turn][warp0 + lane] : 0.0f);
+        }
+        const float mean = sum * per_col;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+            if (v >= vectors) continue;
+            float y[8], r[8], w[8], d[8];
+            unpack8(qy[i], y);
+            unpack8(qr[i], r);
+            unpack8(qw[i], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = rstd * __fmaf_rn(-r[e] * rstd, mean, y[e] * w[e]);
+            if (with_res) {
+                float s[8];
+                unpack8(qd[i], s);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] += s[e];
+            }
+            reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack8(d);
+        }
+    }
+    if (!a.dweight) return;
+    // the block's groups in order, then one row of partial sums a block
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    float* joined = reinterpret_cast<float*>(dynamic);                  // [groups - 1][cols]
+    if (group > 0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+            if (v >= vectors) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) joined[(group - 1) * a.cols + v * 8 + e] = dw[i][e];
+        }
+    }
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+            if (v >= vectors) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                for (int g = 1; g < groups; ++g) dw[i][e] += joined[(g - 1) * a.cols + v * 8 + e];
+            float4* out = reinterpret_cast<float4*>(a.partial + blockIdx.x * a.cols + v * 8);
+            out[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
+            out[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
+        }
+    }
+}
+
+// Sums of the blocks' parts, in order: 32 columns a block, a thread takes every eighth part of one.
 __global__ void __launch_bounds__(kRowThreads) row_dweight_finish_kernel(const float* partial, int chunks, uint64_t cols, uint16_t* dweight) {
-    const uint64_t j = blockIdx.x * static_cast<uint64_t>(kRowThreads) + threadIdx.x;
-    if (j >= cols) return;
+    __shared__ float part[kRowThreads / 32][32];
+    const uint64_t j = blockIdx.x * 32ull + (threadIdx.x & 31);
+    const int first = threadIdx.x >> 5;
     float sum = 0.0f;
-    for (int k = 0; k < chunks; ++k) sum += partial[k * cols + j];
-    dweight[j] = to_bf16(sum);
+    if (j < cols) {
+#pragma unroll 8
+        for (int k = first; k < chunks; k += kRowThreads / 32) sum += partial[k * cols + j];
+    }
+    part[first][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (first == 0 && j < cols) {
+#pragma unroll
+        for (int k = 1; k < kRowThreads / 32; ++k) sum += part[k][threadIdx.x];
+        dweight[j] = to_bf16(sum);
+    }
+}
+
+template <int PER, int THREADS>
+static unsigned launch_backward_as(const RowBackwardArgs& a, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3;
+    const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), groups = std::max(1, std::min(kBackwardThreads / group, 15));
+    // the places hold the groups' dweight too: 4 cols bytes a group, against 48 kDepth bytes for each 8 columns
+    constexpr int place_bytes = kDepth * 3 * PER * 16;
+    if (allow_smem<&row_backward_kernel<PER, THREADS>>(place_bytes * THREADS) != cudaSuccess) return 0;
+    const uint64_t resident = std::min<uint64_t>(kWeightChunks, (PER > 1 ? 1ull : 2ull) * sm_count);
+    const unsigned grid = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, resident));
+    row_backward_kernel<PER, THREADS><<<grid, group * groups, place_bytes * group * groups, s>>>(a, group);
+    return grid;
+}
+// Returns the number of partial rows of dweight, 0 after an error.  Rows of up to 256 columns are a warp's, without barriers;
+// longer ones take two vectors a thread (half the barriers and joins of one: 50 against 58 us at 8191 x 4096).
+static unsigned launch_backward(const RowBackwardArgs& a, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3;
+    return v <= 32 ? launch_backward_as<1, 512>(a, sm_count, s)
+         : v <= 1024 ? launch_backward_as<2, 512>(a, sm_count, s)
+         : v <= 1536 ? launch_backward_as<2, 768>(a, sm_count, s)
+                     : launch_backward_as<2, 1024>(a, sm_count, s);
 }
 
 }  // namespace ops
@@ -164,8 +445,10 @@ collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_m
     a.rstd = rstd;
     a.cols = x->cols;
     a.eps = static_cast<float>(eps);
-    row_any_kernel<true><<<static_cast<unsigned>(x->rows), kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return launch_status();
+    bool fit = x->cols % 8 == 0 && reinterpret_cast<uintptr_t>(weight) % 16 == 0 && rows_aligned(x, 2, 16);
+    for (int i = 0; i < 4; ++i)
+        if (others[i]) fit = fit && rows_aligned(others[i], i == 3 ? 1 : 2, i == 3 ? 8 : 16);
+    return launch_rows<true>(a, x->rows, fit, dev.sm_count, static_cast<cudaStream_t>(stream));
 }
 
 collage_status_t collage_quantize_rows(const collage_matrix_t* x, const collage_matrix_t* q, float* scale, void* stream) {
@@ -191,8 +474,8 @@ collage_status_t collage_quantize_rows(const collage_matrix_t* x, const collage_
     a.ldy8 = q->ld;
     a.scale = scale;
     a.cols = x->cols;
-    row_any_kernel<false><<<static_cast<unsigned>(x->rows), kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return launch_status();
+    const bool fit = x->cols % 8 == 0 && rows_aligned(x, 2, 16) && rows_aligned(q, 1, 8);
+    return launch_rows<false>(a, x->rows, fit, dev.sm_count, static_cast<cudaStream_t>(stream));
 }
 
 size_t collage_rms_norm_workspace_bytes(uint64_t cols) { return static_cast<size_t>(kWeightChunks) * 4 * cols; }
@@ -242,13 +525,20 @@ collage_status_t collage_add_rms_norm_backward(const collage_matrix_t* dy, const
     a.partial = static_cast<float*>(workspace);
     a.rows = dy->rows;
     a.cols = dy->cols;
+    bool fit = dy->cols % 8 == 0 && dy->cols <= 16384 && reinterpret_cast<uintptr_t>(weight) % 16 == 0 && rows_aligned(dy, 2, 16);
+    for (const collage_matrix_t* m : others) fit = fit && (!m || rows_aligned(m, 2, 16));
+    const unsigned finish_blocks = static_cast<unsigned>((a.cols + 31) / 32);
+    if (fit) {
+        const unsigned parts = launch_backward(a, dev.sm_count, s);
+        if (!parts) return COLLAGE_ERR_CUDA;
+        if (dweight) row_dweight_finish_kernel<<<finish_blocks, kRowThreads, 0, s>>>(a.partial, static_cast<int>(parts), a.cols, a.dweight);
+        return launch_status();
+    }
     if (dweight) {                            // before dx, which may take dy's place
-        const uint64_t blocks = (a.cols + 31) / 32;
-        uint64_t chunks = (8ull * dev.sm_count + blocks - 1) / blocks;
+        uint64_t chunks = (8ull * dev.sm_count + finish_blocks - 1) / finish_blocks;
         chunks = std::min<uint64_t>({chunks, (a.rows + 7) / 8, static_cast<uint64_t>(kWeightChunks)});
-        row_dweight_any_kernel<<<dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(chunks)), kRowThreads, 0, s>>>(a);
-        row_dweight_finish_kernel<<<static_cast<unsigned>((a.cols + kRowThreads - 1) / kRowThreads), kRowThreads, 0, s>>>(
-            a.partial, static_cast<int>(chunks), a.cols, a.dweight);
+        row_dweight_any_kernel<<<dim3(finish_blocks, static_cast<unsigned>(chunks)), kRowThreads, 0, s>>>(a);
+        row_dweight_finish_kernel<<<finish_blocks, kRowThreads, 0, s>>>(a.partial, static_cast<int>(chunks), a.cols, a.dweight);
     }
     if (dx) row_backward_any_kernel<<<static_cast<unsigned>(a.rows), kRowThreads, 0, s>>>(a);
     return launch_status();

@@ -146,6 +146,13 @@ __device__ __forceinline__ bool named_all(int id, int threads, bool ok) {
                  : "memory");
     return r != 0;
 }
+// The same for threads of a warp that may have parted ways.
+__device__ __forceinline__ void cluster_arrive_all() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait_all() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync_any() {
+    cluster_arrive_all();
+    cluster_wait_all();
+}
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 }  // namespace umma
