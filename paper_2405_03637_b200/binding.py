@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes
 from pathlib import Path
 
+import torch
+
 _LIB_PATH = Path(__file__).resolve().parent / "libcollage_b200.so"      # the in-tree build
 
 OK, ERR_NULL, ERR_ARG, ERR_ALIAS, ERR_ARCH, ERR_CUDA, ERR_WORKSPACE, ERR_LIMIT = range(8)
@@ -371,40 +373,42 @@ def _refuse(where: str):
     raise CollageError(ERR_ARG, where)
 
 
-def _matrix(t, dtype: str, where: str, required: bool = False):
+def _matrix(t, dtype, where: str, required: bool = False):
     """collage_matrix_t of a tensor, or None for None."""
     if t is None:
         if required:
             raise CollageError(ERR_NULL, where)
         return None
-    if not t.is_cuda or str(t.dtype) != dtype or t.dim() < 2:
+    if t.dtype is not dtype or not t.is_cuda:
         _refuse(where)
-    if t.dim() > 2:
+    shape = t.shape
+    if len(shape) != 2:
         try:
-            t = t.view(-1, t.shape[-1])
-        except RuntimeError:
+            t = t.view(-1, shape[-1])
+        except (RuntimeError, IndexError):
             _refuse(where)
-    rows, cols = t.shape
+        if len(shape) < 2:
+            _refuse(where)
+        shape = t.shape
+    rows, cols = shape
     ld, inner = t.stride()
     if rows <= 1:
         ld = cols                              # the stride of a single row means nothing
-    if cols <= 1:
-        inner = 1
-    if inner != 1 or ld < cols:
+    if (inner != 1 and cols > 1) or ld < cols:
         _refuse(where)
     return Matrix(t.data_ptr(), rows, cols, ld)
 
 
-def _vector(t, dtype: str, length: int, where: str):
+def _vector(t, dtype, length: int, where: str):
     """Address of a contiguous vector of that many elements, or None for None."""
     if t is None:
         return None
-    if not t.is_cuda or str(t.dtype) != dtype or t.numel() != length or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or t.numel() != length or not t.is_contiguous():
         _refuse(where)
     return t.data_ptr()
 
 
-_BF16, _F32, _E4M3 = "torch.bfloat16", "torch.float32", "torch.float8_e4m3fn"
+_BF16, _F32, _E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
 
 
 def add_rms_norm(x, residual, weight, eps: float, residual_out=None, y=None, y8=None, y8_scale=None, rstd=None, stream=None):
@@ -464,11 +468,11 @@ def gated_ffn_e4m3(x8, x_scale, w_gate8, w_gate_scale, w_up8, w_up_scale, h, act
 def _distill(logits, top_index, top_logits, temperature, where) -> Distill:
     if logits is None or top_index is None or top_logits is None:
         raise CollageError(ERR_NULL, where)
-    dtype, index = str(logits.dtype), str(top_index.dtype)
-    if dtype not in (_BF16, _F32) or index not in ("torch.int32", "torch.int64"):
+    dtype, index = logits.dtype, top_index.dtype
+    if dtype not in (_BF16, _F32) or index not in (torch.int32, torch.int64):
         _refuse(where)
     return Distill(_matrix(logits, dtype, where), _matrix(top_index, index, where), _matrix(top_logits, _F32, where),
-                   DTYPE_BF16 if dtype == _BF16 else DTYPE_F32, 4 if index == "torch.int32" else 8, temperature)
+                   DTYPE_BF16 if dtype is _BF16 else DTYPE_F32, 4 if index is torch.int32 else 8, temperature)
 
 
 def distill_loss(logits, top_index, top_logits, temperature: float, loss, lse=None, stream=None):
@@ -485,7 +489,7 @@ def distill_loss_backward(logits, top_index, top_logits, temperature: float, lse
     d = _distill(logits, top_index, top_logits, temperature, w)
     n = d.logits.rows
     _check(lib().collage_distill_loss_backward(ctypes.byref(d), _vector(lse, _F32, n, w), _vector(grad_loss, _F32, n, w),
-                                               _matrix(dlogits, str(logits.dtype), w), _ptr(stream)), w)
+                                               _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
 
 
 def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row_weight, loss, dlogits, stream=None):
@@ -494,4 +498,4 @@ def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row
     d = _distill(logits, top_index, top_logits, temperature, w)
     n = d.logits.rows
     _check(lib().collage_distill_loss_and_grad(ctypes.byref(d), _vector(row_weight, _F32, n, w), _vector(loss, _F32, n, w),
-                                               _matrix(dlogits, str(logits.dtype), w), _ptr(stream)), w)
+                                               _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)

@@ -99,6 +99,38 @@ __global__ void __launch_bounds__(256) gate_backward_any_kernel(const __grid_con
     }
 }
 
+// The same on rows of whole 16-byte vectors: a vector a thread and turn, the next one's loads sent before this one's results.
+__global__ void __launch_bounds__(256) gate_backward_kernel(const __grid_constant__ GateArgs a, uint64_t rows) {
+    const uint64_t vectors = a.cols >> 3, total = rows * vectors, step = gridDim.x * 256ull;
+    auto at = [](const uint16_t* p, uint64_t ld, uint64_t row, uint64_t v) { return reinterpret_cast<const uint4*>(p + row * ld) + v; };
+    uint4 next[3];
+    uint64_t row = 0, v = 0;
+    auto load = [&](uint64_t i) {
+        row = i / vectors;
+        v = i - row * vectors;
+        next[0] = __ldcs(at(a.dh, a.lddh, row, v));
+        next[1] = *at(a.gate, a.ldg, row, v);
+        next[2] = *at(a.up, a.ldu, row, v);
+    };
+    uint64_t i = blockIdx.x * 256ull + threadIdx.x;
+    if (i < total) load(i);
+    for (; i < total; i += step) {
+        const uint32_t d[4] = {next[0].x, next[0].y, next[0].z, next[0].w}, g[4] = {next[1].x, next[1].y, next[1].z, next[1].w},
+                       u[4] = {next[2].x, next[2].y, next[2].z, next[2].w};
+        const uint64_t this_row = row, this_v = v;
+        if (i + step < total) load(i + step);
+        uint32_t dg[4], du[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 lo = activate_and_slope(a.activation, bf16_lo(g[e])), hi = activate_and_slope(a.activation, bf16_hi(g[e]));
+            dg[e] = pack_bf16(bf16_lo(d[e]) * bf16_lo(u[e]) * lo.y, bf16_hi(d[e]) * bf16_hi(u[e]) * hi.y);
+            du[e] = pack_bf16(bf16_lo(d[e]) * lo.x, bf16_hi(d[e]) * hi.x);
+        }
+        reinterpret_cast<uint4*>(a.dgate + this_row * a.lddg)[this_v] = make_uint4(dg[0], dg[1], dg[2], dg[3]);
+        reinterpret_cast<uint4*>(a.dup + this_row * a.lddu)[this_v] = make_uint4(du[0], du[1], du[2], du[3]);
+    }
+}
+
 inline Operand by_row(const collage_matrix_t* m) { return {m->data, m->ld, 1}; }        // i = row of the matrix
 inline Operand by_col(const collage_matrix_t* m) { return {m->data, 1, m->ld}; }        // i = column
 
@@ -376,7 +408,14 @@ collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const co
         g.lddu = dup->ld;
         g.cols = dh->cols;
         g.activation = activation;
-        gate_backward_any_kernel<<<static_cast<unsigned>(dh->rows), 256, 0, s>>>(g);
+        bool vectors = dh->cols % 8 == 0;
+        for (const collage_matrix_t* m : {dh, gate, up, dgate, dup}) vectors = vectors && rows_aligned(m, 2, 16);
+        if (vectors) {
+            const uint64_t blocks = (dh->rows * (dh->cols / 8) + 255) / 256;
+            gate_backward_kernel<<<static_cast<unsigned>(std::min<uint64_t>(blocks, 8ull * dev.sm_count)), 256, 0, s>>>(g, dh->rows);
+        } else {
+            gate_backward_any_kernel<<<static_cast<unsigned>(dh->rows), 256, 0, s>>>(g);
+        }
         if ((st = launch_status()) != COLLAGE_OK) return st;
     }
     // a product over no tokens or no channels is zero

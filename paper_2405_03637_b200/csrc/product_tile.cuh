@@ -110,15 +110,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     umma::fence_after();
     const uint32_t tmem = bars->tmem;
 
+    // The first two warps run their loops as a whole, so that addresses and descriptors stay in uniform registers, and one
+    // thread issues.
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t stage = 0, phase = 0, used = 0;
-            bool ok = true;
-            for (uint32_t tile = first; tile < tiles && ok; tile += step) {
-                const TilePlace at = place_of(p, tile);
-                const int m0 = static_cast<int>(at.m * 128 * CTAS + rank * 128), n0 = static_cast<int>(at.n * kOut);
-                for (uint32_t kb = 0; kb < blocks; ++kb) {
-                    if (!(ok = pipe::mbar_wait(&bars->empty[stage], phase ^ 1, 200, &g_product_fault))) break;
+        uint32_t stage = 0, phase = 0, used = 0;
+        bool ok = true;
+        for (uint32_t tile = first; tile < tiles && ok; tile += step) {
+            const TilePlace at = place_of(p, tile);
+            const int m0 = static_cast<int>(at.m * 128 * CTAS + rank * 128), n0 = static_cast<int>(at.n * kOut);
+            for (uint32_t kb = 0; kb < blocks; ++kb) {
+                if (!(ok = pipe::mbar_wait(&bars->empty[stage], phase ^ 1, 200, &g_product_fault))) break;
+                if (umma::elected()) {
                     if (rank == 0) pipe::mbar_arrive_expect_tx(&bars->full[stage], kStageBytes * CTAS);
                     const uint32_t bar = CTAS == 2 ? umma::cluster_addr(&bars->full[stage], 0) : umma::smem_addr(&bars->full[stage]);
                     uint8_t *sa = smem + stage * kStageBytes, *sb = sa + kOperandBytes;
@@ -141,40 +143,43 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         umma::tile_load<CTAS>(sb, &p.b[term], n, k, bar);
                         umma::tile_load<CTAS>(sb + kOperandBytes / 2, &p.b[term], n + 64, k, bar);
                     }
-                    used = min(used + 1, static_cast<uint32_t>(kStages));
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
-            }
-            // the last uses of the stages: nothing arrives in this block any more once they are over
-            for (uint32_t i = 0; i < used && ok; ++i) {
-                stage = stage ? stage - 1 : kStages - 1;
-                if (stage == kStages - 1) phase ^= 1;
-                ok = pipe::mbar_wait(&bars->empty[stage], phase, 201, &g_product_fault);
+                __syncwarp();
+                used = min(used + 1, static_cast<uint32_t>(kStages));
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
         }
+        // the last uses of the stages: nothing arrives in this block any more once they are over
+        for (uint32_t i = 0; i < used && ok; ++i) {
+            stage = stage ? stage - 1 : kStages - 1;
+            if (stage == kStages - 1) phase ^= 1;
+            ok = pipe::mbar_wait(&bars->empty[stage], phase, 201, &g_product_fault);
+        }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            uint32_t stage = 0, phase = 0, n_tile = 0;
-            bool ok = true;
-            for (uint32_t tile = first; tile < tiles && ok; tile += step, ++n_tile) {
-                const uint32_t acc = n_tile & 1;
-                if (!(ok = pipe::mbar_wait(&bars->drained[acc], ((n_tile >> 1) & 1) ^ 1, 202, &g_product_fault))) break;
+        uint32_t stage = 0, phase = 0, n_tile = 0;
+        bool ok = rank == 0;
+        const uint32_t smem0 = umma::smem_addr(smem);
+        for (uint32_t tile = first; tile < tiles && ok; tile += step, ++n_tile) {
+            const uint32_t acc = n_tile & 1;
+            if (!(ok = pipe::mbar_wait(&bars->drained[acc], ((n_tile >> 1) & 1) ^ 1, 202, &g_product_fault))) break;
+            umma::fence_after();
+            const uint32_t d = tmem + acc * kN;
+            for (uint32_t kb = 0; kb < blocks; ++kb) {
+                if (!(ok = pipe::mbar_wait(&bars->full[stage], phase, 203, &g_product_fault))) break;
                 umma::fence_after();
-                const uint32_t d = tmem + acc * kN;
-                for (uint32_t kb = 0; kb < blocks; ++kb) {
-                    if (!(ok = pipe::mbar_wait(&bars->full[stage], phase, 203, &g_product_fault))) break;
-                    umma::fence_after();
-                    const uint32_t sa = umma::smem_addr(smem + stage * kStageBytes), sb = sa + kOperandBytes;
-                    const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024);
-                    const uint64_t db = umma::operand_desc(sb, B_MN ? kOperandBytes / 2 : 16, 1024);
+                const uint32_t sa = smem0 + stage * kStageBytes, sb = sa + kOperandBytes;
+                const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024);
+                const uint64_t db = umma::operand_desc(sb, B_MN ? kOperandBytes / 2 : 16, 1024);
+                if (umma::elected()) {
                     // one instruction takes 32 bytes of K: 32 bytes along the rows, or 16 rows of 128 bytes
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
                         umma::mma<CTAS, E4M3>(d, da + i * (A_MN ? 2048 : 32) / 16, db + i * (B_MN ? 2048 : 32) / 16, kIdesc, kb > 0 || i > 0);
                     umma::commit<CTAS>(&bars->empty[stage]);
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                    if (kb + 1 == blocks) umma::commit<CTAS>(&bars->done[acc]);
                 }
-                if (ok) umma::commit<CTAS>(&bars->done[acc]);
+                __syncwarp();
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
         }
     } else if (warp >= 4) {

@@ -120,6 +120,12 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
+// One thread of a warp whose threads are together.
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 // Address of the same shared-memory object in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
     uint32_t r;
