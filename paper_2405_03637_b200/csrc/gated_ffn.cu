@@ -1,5 +1,5 @@
 // Gated feed-forward projections: h = a(x w_gate^T) * (x w_up^T), the backward pass, and the same with e4m3 operands.
-#include "product_tile.cuh"
+#include "product_slim.cuh"
 
 namespace collage {
 
@@ -193,34 +193,110 @@ static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) 
     return cudaLaunchKernelEx(&cfg, kernel, t) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
 }
 
+template <bool E4M3, bool A_MN, bool GATED, int NT>
+static collage_status_t launch_slim_as(const SlimArgs& t, uint64_t blocks, cudaStream_t s) {
+    constexpr auto kernel = &slim_kernel<E4M3, A_MN, GATED, NT>;
+    if (blocks >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
+    if (allow_smem<kernel>(slim_smem<NT>()) != cudaSuccess) return COLLAGE_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(kSlimThreads);
+    cfg.dynamicSmemBytes = slim_smem<NT>();
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {t.split, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, t) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
+}
+
+static uint32_t slim_tokens(uint64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128; }
+
+// The sum over K is split until there is a block for every SM, as long as each has eight blocks of K.
+template <bool E4M3, bool A_MN, bool GATED>
+static collage_status_t launch_slim(SlimArgs& t, int sm_count, cudaStream_t s) {
+    const uint32_t nt = slim_tokens(t.n), blocks = t.terms * t.k_blocks;
+    t.token_tiles = (t.n + nt - 1) / nt;
+    const uint64_t tiles = static_cast<uint64_t>(t.token_tiles) * ((t.m + (GATED ? 63 : 127)) / (GATED ? 64 : 128));
+    t.split = 1;
+    while (t.split < 8 && tiles * t.split < static_cast<uint64_t>(sm_count) && blocks / (2 * t.split) >= 8) t.split *= 2;
+    switch (nt) {
+        case 16: return launch_slim_as<E4M3, A_MN, GATED, 16>(t, tiles * t.split, s);
+        case 32: return launch_slim_as<E4M3, A_MN, GATED, 32>(t, tiles * t.split, s);
+        case 64: return launch_slim_as<E4M3, A_MN, GATED, 64>(t, tiles * t.split, s);
+        default: return launch_slim_as<E4M3, A_MN, GATED, 128>(t, tiles * t.split, s);
+    }
+}
+
+// Slim tiles where there are few tokens, or too few pairs' tiles to fill the GPU.
+static bool slim(uint64_t tokens, uint64_t pair_tiles, int sm_count) {
+    return tokens <= 128 || pair_tiles * 4 < 3ull * (sm_count / 2);
+}
+
 // The forward products with 16-byte aligned rows.
 template <bool E4M3>
 static collage_status_t tiles_forward(const collage_matrix_t* x, const collage_matrix_t* wg, const collage_matrix_t* wu,
                                       const collage_matrix_t* h, const collage_matrix_t* gate, const collage_matrix_t* up,
                                       const float* const (&scales)[3], int activation, int sm_count, cudaStream_t s) {
-    TileArgs t = {};
-    const bool pair = x->rows > 128;
     const uint32_t k = E4M3 ? 128 : 64;
-    bool ok = make_map(&t.a[0], x, E4M3, k, 128, false) && make_map(&t.b[0], wg, E4M3, k, pair ? 128 : 64, false) &&
-              make_map(&t.b[1], wu, E4M3, k, pair ? 128 : 64, false) && make_map(&t.out[0], h, false, kUnitCols, 128, true);
-    t.a[1] = t.a[0];
-    if (gate) ok = ok && make_map(&t.out[1], gate, false, kUnitCols, 128, true) && make_map(&t.out[2], up, false, kUnitCols, 128, true);
+    const uint32_t k_blocks = static_cast<uint32_t>((x->cols + k - 1) / k);
+    const collage_matrix_t* outs[3] = {h, gate, up};
+    if (slim(x->rows, (x->rows + 255) / 256 * ((h->cols + 127) / 128), sm_count)) {
+        SlimArgs t = {};
+        if (!(make_map(&t.a[0], wg, E4M3, k, 64, false) && make_map(&t.a[1], wu, E4M3, k, 64, false) &&
+              make_map(&t.b[0], x, E4M3, k, slim_tokens(x->rows), false)))
+            return COLLAGE_ERR_CUDA;
+        for (int i = 0; i < 3 && outs[i]; ++i) {
+            t.out[i] = static_cast<uint16_t*>(outs[i]->data);
+            t.ldo[i] = outs[i]->ld;
+        }
+        t.token_scale = scales[0];
+        t.row_scale[0] = scales[1];
+        t.row_scale[1] = scales[2];
+        t.m = static_cast<uint32_t>(h->cols);
+        t.n = static_cast<uint32_t>(x->rows);
+        t.k_blocks = k_blocks;
+        t.terms = 1;
+        t.keep = gate != nullptr;
+        t.activation = activation;
+        return launch_slim<E4M3, false, true>(t, sm_count, s);
+    }
+    TileArgs t = {};
+    bool ok = make_map(&t.a[0], x, E4M3, k, 128, false) && make_map(&t.b[0], wg, E4M3, k, 128, false) && make_map(&t.b[1], wu, E4M3, k, 128, false);
+    for (int i = 0; i < 3 && outs[i]; ++i) ok = ok && make_map(&t.out[i], outs[i], false, kUnitCols, 128, true);
     if (!ok) return COLLAGE_ERR_CUDA;
+    t.a[1] = t.a[0];
     t.a_scale = scales[0];
     t.b_scale[0] = scales[1];
     t.b_scale[1] = scales[2];
     t.m = static_cast<uint32_t>(x->rows);
     t.n = static_cast<uint32_t>(wg->rows);
     t.problems = t.terms = 1;
-    t.k_blocks = static_cast<uint32_t>((x->cols + k - 1) / k);
+    t.k_blocks = k_blocks;
     t.keep = gate != nullptr;
     t.activation = activation;
-    return pair ? launch_tiles<E4M3, false, false, true, 2>(t, sm_count, s) : launch_tiles<E4M3, false, false, true, 1>(t, sm_count, s);
+    return launch_tiles<E4M3, false, false, true, 2>(t, sm_count, s);
 }
 
 // dx = dgate w_gate + dup w_up
 static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_matrix_t* dup, const collage_matrix_t* wg,
                                  const collage_matrix_t* wu, const collage_matrix_t* dx, int sm_count, cudaStream_t s) {
+    const uint32_t k_blocks = static_cast<uint32_t>((dgate->cols + 63) / 64);
+    if (slim(dx->rows, (dx->rows + 255) / 256 * ((dx->cols + 255) / 256), sm_count)) {
+        SlimArgs t = {};
+        const uint32_t nt = slim_tokens(dx->rows);
+        if (!(make_map(&t.a[0], wg, false, 64, 64, false) && make_map(&t.a[1], wu, false, 64, 64, false) &&
+              make_map(&t.b[0], dgate, false, 64, nt, false) && make_map(&t.b[1], dup, false, 64, nt, false)))
+            return COLLAGE_ERR_CUDA;
+        t.out[0] = static_cast<uint16_t*>(dx->data);
+        t.ldo[0] = dx->ld;
+        t.m = static_cast<uint32_t>(dx->cols);
+        t.n = static_cast<uint32_t>(dx->rows);
+        t.k_blocks = k_blocks;
+        t.terms = 2;
+        return launch_slim<false, true, false>(t, sm_count, s);
+    }
     TileArgs t = {};
     if (!(make_map(&t.a[0], dgate, false, 64, 128, false) && make_map(&t.a[1], dup, false, 64, 128, false) &&
           make_map(&t.b[0], wg, false, 64, 64, false) && make_map(&t.b[1], wu, false, 64, 64, false) &&
@@ -230,8 +306,8 @@ static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_ma
     t.n = static_cast<uint32_t>(dx->cols);
     t.problems = 1;
     t.terms = 2;
-    t.k_blocks = static_cast<uint32_t>((dgate->cols + 63) / 64);
-    return t.m > 128 ? launch_tiles<false, false, true, false, 2>(t, sm_count, s) : launch_tiles<false, false, true, false, 1>(t, sm_count, s);
+    t.k_blocks = k_blocks;
+    return launch_tiles<false, false, true, false, 2>(t, sm_count, s);
 }
 
 // dw_gate = dgate^T x and dw_up = dup^T x
@@ -248,7 +324,7 @@ static collage_status_t tiles_dw(const collage_matrix_t* dgate, const collage_ma
     t.problems = 2;
     t.terms = 1;
     t.k_blocks = static_cast<uint32_t>((x->rows + 63) / 64);
-    return t.m > 128 ? launch_tiles<false, true, true, false, 2>(t, sm_count, s) : launch_tiles<false, true, true, false, 1>(t, sm_count, s);
+    return launch_tiles<false, true, true, false, 2>(t, sm_count, s);
 }
 
 // ---- any alignment ---------------------------------------------------------------------------------------------------

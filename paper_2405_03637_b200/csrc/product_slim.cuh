@@ -1,0 +1,165 @@
+// The products of few tokens: weights as the 128 rows of a tile, tokens as its columns, the sum over K split over a cluster.
+#pragma once
+#include "product_tile.cuh"
+
+namespace collage {
+namespace ops {
+
+// out[t, i] for tokens t < n and weight indexes i < m.  GATED: a[0] and a[1] are the two weights, 64 indexes of each in a
+// tile, out[0] = h (out[1], out[2] = gate, up if kept).  Otherwise the sum over `terms` of A_s B_s^T, 128 indexes a tile.
+struct SlimArgs {
+    CUtensorMap a[2], b[2];
+    const float* row_scale[2];           // of the weights (e4m3)
+    const float* token_scale;
+    uint16_t* out[3];
+    uint64_t ldo[3];
+    uint32_t m, n, token_tiles, k_blocks, terms, split;
+    int keep, activation;
+};
+
+constexpr int kSlimThreads = 128;
+
+template <int NT>
+__host__ __device__ constexpr int slim_stage_bytes() { return kOperandBytes + NT * static_cast<int>(umma::kRowBytes); }
+// As many stages as leave room for two blocks on an SM; the sums over the tile take their place afterwards.
+template <int NT>
+__host__ __device__ constexpr int slim_stages() { return NT <= 16 ? 6 : NT <= 32 ? 5 : NT <= 64 ? 4 : 3; }
+template <int NT>
+__host__ __device__ constexpr int slim_smem() { return 1024 + slim_stages<NT>() * slim_stage_bytes<NT>(); }
+
+template <bool E4M3, bool A_MN, bool GATED, int NT>
+__global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constant__ SlimArgs p) {
+    constexpr uint32_t kStagesHere = slim_stages<NT>(), kBytes = slim_stage_bytes<NT>();
+    constexpr uint32_t kK = E4M3 ? 128 : 64, kColumns = NT < 32 ? 32 : NT, kIndexes = GATED ? 64 : 128;
+    constexpr uint32_t kIdesc = umma::instr_desc(E4M3 ? 0 : 1, A_MN, false, 128, NT);
+    static_assert(kStagesHere * kBytes >= NT * 512, "the tile's sums fit the stages");
+    extern __shared__ uint8_t raw_smem[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
+    __shared__ uint64_t full[kStagesHere], empty[kStagesHere], done;
+    __shared__ uint32_t tmem_slot;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = p.split > 1 ? umma::cluster_rank() : 0, tile = blockIdx.x / p.split;
+    const uint32_t t0 = tile % p.token_tiles * NT, i0 = tile / p.token_tiles * kIndexes;
+    const uint32_t blocks = p.terms * p.k_blocks;
+    const uint32_t begin = static_cast<uint32_t>(static_cast<uint64_t>(blocks) * rank / p.split);
+    const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(blocks) * (rank + 1) / p.split);
+
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < kStagesHere; ++i) {
+            pipe::mbar_init(&full[i], 1);
+            pipe::mbar_init(&empty[i], 1);
+        }
+        pipe::mbar_init(&done, 1);
+        pipe::mbar_init_fence();
+    }
+    if (warp == 2) umma::tmem_alloc<1>(&tmem_slot, kColumns);
+    umma::fence_before();
+    __syncthreads();
+    umma::fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp == 0) {
+        uint32_t stage = 0, phase = 0;
+        for (uint32_t kb = begin; kb < end; ++kb) {
+            if (!pipe::mbar_wait(&empty[stage], phase ^ 1, 210, &g_product_fault)) break;
+            if (umma::elected()) {
+                pipe::mbar_arrive_expect_tx(&full[stage], kBytes);
+                const uint32_t bar = umma::smem_addr(&full[stage]);
+                uint8_t *sa = smem + stage * kBytes, *sb = sa + kOperandBytes;
+                const uint32_t term = kb / p.k_blocks;
+                const int k = static_cast<int>((kb - term * p.k_blocks) * kK);
+                if constexpr (GATED) {
+                    umma::tile_load<1>(sa, &p.a[0], k, static_cast<int>(i0), bar);
+                    umma::tile_load<1>(sa + kOperandBytes / 2, &p.a[1], k, static_cast<int>(i0), bar);
+                } else if constexpr (A_MN) {
+                    umma::tile_load<1>(sa, &p.a[term], static_cast<int>(i0), k, bar);
+                    umma::tile_load<1>(sa + kOperandBytes / 2, &p.a[term], static_cast<int>(i0) + 64, k, bar);
+                }
+                umma::tile_load<1>(sb, &p.b[term], k, static_cast<int>(t0), bar);
+            }
+            __syncwarp();
+            if (++stage == kStagesHere) { stage = 0; phase ^= 1; }
+        }
+    } else if (warp == 1) {
+        uint32_t stage = 0, phase = 0;
+        const uint32_t smem0 = umma::smem_addr(smem);
+        bool ok = true;
+        for (uint32_t kb = begin; kb < end; ++kb) {
+            if (!(ok = pipe::mbar_wait(&full[stage], phase, 211, &g_product_fault))) break;
+            umma::fence_after();
+            const uint32_t sa = smem0 + stage * kBytes;
+            const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024), db = umma::operand_desc(sa + kOperandBytes, 16, 1024);
+            if (umma::elected()) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    umma::mma<1, E4M3>(tmem, da + i * (A_MN ? 2048 : 32) / 16, db + i * 2, kIdesc, kb > begin || i > 0);
+                umma::commit<1>(&empty[stage]);
+                if (kb + 1 == end) umma::commit<1>(&done);
+            }
+            __syncwarp();
+            if (++stage == kStagesHere) { stage = 0; phase ^= 1; }
+        }
+        if (ok) pipe::mbar_wait(&done, 0, 212, &g_product_fault);
+    }
+    __syncthreads();                                 // the sums are complete and the stages free
+    umma::fence_after();
+    float* sums = reinterpret_cast<float*>(smem);    // [NT][128]: a token's 128 indexes
+    const uint32_t row = threadIdx.x;
+#pragma unroll 1
+    for (uint32_t c = 0; c < NT; c += 16) {
+        float v[16];
+        umma::tmem_load16(tmem + (warp << 21) + c, v);
+        umma::tmem_wait(v);
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) sums[(c + i) * 128 + row] = v[i];
+    }
+    umma::fence_before();
+    if (p.split > 1) umma::cluster_sync();
+    else __syncthreads();
+    umma::fence_after();
+    if (warp == 2) umma::tmem_free<1>(tmem, kColumns);
+
+    // tokens over the cluster's blocks and their warps; parts of the sum in the order of K
+    const uint32_t tokens = min(static_cast<uint32_t>(NT), p.n - t0);
+    for (uint32_t t = rank * 4 + warp; t < tokens; t += p.split * 4) {
+        const uint64_t token = t0 + t;
+        if constexpr (GATED) {
+            const uint32_t i = i0 + 2 * lane;        // two indexes a thread
+            float2 g = {0.0f, 0.0f}, u = {0.0f, 0.0f};
+            for (uint32_t r = 0; r < p.split; ++r) {
+                const uint32_t at = umma::cluster_addr(sums + t * 128 + 2 * lane, r);
+                float2 pg, pu;
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(pg.x), "=f"(pg.y) : "r"(at));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(pu.x), "=f"(pu.y) : "r"(at + 256));
+                g.x += pg.x; g.y += pg.y; u.x += pu.x; u.y += pu.y;
+            }
+            if (i >= p.m) continue;                  // m is a multiple of 8
+            if constexpr (E4M3) {
+                const float s = p.token_scale[token];
+                g.x *= s * p.row_scale[0][i]; g.y *= s * p.row_scale[0][i + 1];
+                u.x *= s * p.row_scale[1][i]; u.y *= s * p.row_scale[1][i + 1];
+            }
+            if (p.keep) {
+                *reinterpret_cast<uint32_t*>(p.out[1] + token * p.ldo[1] + i) = pack_bf16(g.x, g.y);
+                *reinterpret_cast<uint32_t*>(p.out[2] + token * p.ldo[2] + i) = pack_bf16(u.x, u.y);
+            }
+            *reinterpret_cast<uint32_t*>(p.out[0] + token * p.ldo[0] + i) =
+                pack_bf16(activate(p.activation, g.x) * u.x, activate(p.activation, g.y) * u.y);
+        } else {
+            const uint32_t i = i0 + 4 * lane;        // four indexes a thread
+            float4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (uint32_t r = 0; r < p.split; ++r) {
+                const uint32_t at = umma::cluster_addr(sums + t * 128 + 4 * lane, r);
+                float4 q;
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(at));
+                v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
+            }
+            if (i >= p.m) continue;
+            *reinterpret_cast<uint2*>(p.out[0] + token * p.ldo[0] + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        }
+    }
+    if (p.split > 1) umma::cluster_sync_any();       // no block leaves while another reads its sums
+}
+
+}  // namespace ops
+}  // namespace collage

@@ -89,11 +89,18 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
           "=f"(v[31])
         : "r"(addr));
 }
-// Values of earlier tmem_load32 calls are ready behind this.  The operand list keeps their uses behind it as well.
-__device__ __forceinline__ void tmem_wait(float (&v)[32]) {
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                   "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                 : "r"(addr));
+}
+// Values of earlier tmem_load calls are ready behind this.  The operand list keeps their uses behind it as well.
+template <int N>
+__device__ __forceinline__ void tmem_wait(float (&v)[N]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]));
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
 }
 
 // Two-dimensional tile load, counted in bytes on `bar` (a shared::cluster address; with CTAS = 2 it may be the
