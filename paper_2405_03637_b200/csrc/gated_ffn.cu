@@ -264,7 +264,7 @@ static collage_status_t tiles_forward(const collage_matrix_t* x, const collage_m
     }
     TileArgs t = {};
     bool ok = make_map(&t.a[0], x, E4M3, k, 128, false) && make_map(&t.b[0], wg, E4M3, k, 128, false) && make_map(&t.b[1], wu, E4M3, k, 128, false);
-    for (int i = 0; i < 3 && outs[i]; ++i) ok = ok && make_map(&t.out[i], outs[i], false, kUnitCols, 128, true);
+    for (int i = 0; i < 3 && outs[i]; ++i) ok = ok && make_map(&t.out[i], outs[i], false, kUnitCols, 32, true);
     if (!ok) return COLLAGE_ERR_CUDA;
     t.a[1] = t.a[0];
     t.a_scale = scales[0];
@@ -300,7 +300,7 @@ static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_ma
     TileArgs t = {};
     if (!(make_map(&t.a[0], dgate, false, 64, 128, false) && make_map(&t.a[1], dup, false, 64, 128, false) &&
           make_map(&t.b[0], wg, false, 64, 64, false) && make_map(&t.b[1], wu, false, 64, 64, false) &&
-          make_map(&t.out[0], dx, false, kUnitCols, 128, true)))
+          make_map(&t.out[0], dx, false, kUnitCols, 32, true)))
         return COLLAGE_ERR_CUDA;
     t.m = static_cast<uint32_t>(dx->rows);
     t.n = static_cast<uint32_t>(dx->cols);
@@ -315,8 +315,8 @@ static collage_status_t tiles_dw(const collage_matrix_t* dgate, const collage_ma
                                  const collage_matrix_t* dwg, const collage_matrix_t* dwu, int sm_count, cudaStream_t s) {
     TileArgs t = {};
     if (!(make_map(&t.a[0], dgate, false, 64, 64, false) && make_map(&t.a[1], dup, false, 64, 64, false) &&
-          make_map(&t.b[0], x, false, 64, 64, false) && make_map(&t.out[0], dwg, false, kUnitCols, 128, true) &&
-          make_map(&t.out[1], dwu, false, kUnitCols, 128, true)))
+          make_map(&t.b[0], x, false, 64, 64, false) && make_map(&t.out[0], dwg, false, kUnitCols, 32, true) &&
+          make_map(&t.out[1], dwu, false, kUnitCols, 32, true)))
         return COLLAGE_ERR_CUDA;
     t.b[1] = t.b[0];
     t.m = static_cast<uint32_t>(dwg->rows);

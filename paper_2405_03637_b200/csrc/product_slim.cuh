@@ -119,43 +119,57 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
     umma::fence_after();
     if (warp == 2) umma::tmem_free<1>(tmem, kColumns);
 
-    // tokens over the cluster's blocks and their warps; parts of the sum in the order of K
+    // Tokens over the cluster's blocks and their warps, four at a time; parts of the sum in the order of K.
     const uint32_t tokens = min(static_cast<uint32_t>(NT), p.n - t0);
-    for (uint32_t t = rank * 4 + warp; t < tokens; t += p.split * 4) {
-        const uint64_t token = t0 + t;
+    auto part = [&](uint32_t r, uint32_t t, uint32_t i) {               // four floats of block r's sums
+        float4 q;
+        if (p.split == 1) return *reinterpret_cast<const float4*>(sums + t * 128 + i);
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(umma::cluster_addr(sums + t * 128 + i, r)));
+        return q;
+    };
+    for (uint32_t first = rank * 16 + warp * 4; first < tokens; first += p.split * 16) {
+        float4 v[4] = {};
+        for (uint32_t r = 0; r < p.split; ++r) {
+            float4 q[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) q[e] = part(r, first + e, 4 * lane);      // NT is a multiple of 4
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) { v[e].x += q[e].x; v[e].y += q[e].y; v[e].z += q[e].z; v[e].w += q[e].w; }
+        }
         if constexpr (GATED) {
-            const uint32_t i = i0 + 2 * lane;        // two indexes a thread
-            float2 g = {0.0f, 0.0f}, u = {0.0f, 0.0f};
-            for (uint32_t r = 0; r < p.split; ++r) {
-                const uint32_t at = umma::cluster_addr(sums + t * 128 + 2 * lane, r);
-                float2 pg, pu;
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(pg.x), "=f"(pg.y) : "r"(at));
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(pu.x), "=f"(pu.y) : "r"(at + 256));
-                g.x += pg.x; g.y += pg.y; u.x += pu.x; u.y += pu.y;
+            // lanes 0-15 have four gates each, lanes 16-31 the ups that belong to them: the lower two of four to the lower lane
+            const bool low = lane < 16;
+            const uint32_t i = i0 + 4 * (lane & 15) + (low ? 0 : 2);
+            float2 row_g = {1.0f, 1.0f}, row_u = {1.0f, 1.0f};
+            if constexpr (E4M3)
+                if (i < p.m) {
+                    row_g = make_float2(p.row_scale[0][i], p.row_scale[0][i + 1]);
+                    row_u = make_float2(p.row_scale[1][i], p.row_scale[1][i + 1]);
+                }
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const float a = __shfl_xor_sync(0xFFFFFFFFu, low ? v[e].z : v[e].x, 16), b = __shfl_xor_sync(0xFFFFFFFFu, low ? v[e].w : v[e].y, 16);
+                float2 g = low ? make_float2(v[e].x, v[e].y) : make_float2(a, b), u = low ? make_float2(a, b) : make_float2(v[e].z, v[e].w);
+                if (first + e >= tokens || i >= p.m) continue;                          // m is a multiple of 8
+                const uint64_t token = t0 + first + e;
+                if constexpr (E4M3) {
+                    const float s = p.token_scale[token];
+                    g.x *= s * row_g.x; g.y *= s * row_g.y;
+                    u.x *= s * row_u.x; u.y *= s * row_u.y;
+                }
+                if (p.keep) {
+                    *reinterpret_cast<uint32_t*>(p.out[1] + token * p.ldo[1] + i) = pack_bf16(g.x, g.y);
+                    *reinterpret_cast<uint32_t*>(p.out[2] + token * p.ldo[2] + i) = pack_bf16(u.x, u.y);
+                }
+                *reinterpret_cast<uint32_t*>(p.out[0] + token * p.ldo[0] + i) =
+                    pack_bf16(activate(p.activation, g.x) * u.x, activate(p.activation, g.y) * u.y);
             }
-            if (i >= p.m) continue;                  // m is a multiple of 8
-            if constexpr (E4M3) {
-                const float s = p.token_scale[token];
-                g.x *= s * p.row_scale[0][i]; g.y *= s * p.row_scale[0][i + 1];
-                u.x *= s * p.row_scale[1][i]; u.y *= s * p.row_scale[1][i + 1];
-            }
-            if (p.keep) {
-                *reinterpret_cast<uint32_t*>(p.out[1] + token * p.ldo[1] + i) = pack_bf16(g.x, g.y);
-                *reinterpret_cast<uint32_t*>(p.out[2] + token * p.ldo[2] + i) = pack_bf16(u.x, u.y);
-            }
-            *reinterpret_cast<uint32_t*>(p.out[0] + token * p.ldo[0] + i) =
-                pack_bf16(activate(p.activation, g.x) * u.x, activate(p.activation, g.y) * u.y);
         } else {
-            const uint32_t i = i0 + 4 * lane;        // four indexes a thread
-            float4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (uint32_t r = 0; r < p.split; ++r) {
-                const uint32_t at = umma::cluster_addr(sums + t * 128 + 4 * lane, r);
-                float4 q;
-                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(at));
-                v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
-            }
-            if (i >= p.m) continue;
-            *reinterpret_cast<uint2*>(p.out[0] + token * p.ldo[0] + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            const uint32_t i = i0 + 4 * lane;
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                if (first + e < tokens && i < p.m)
+                    *reinterpret_cast<uint2*>(p.out[0] + (t0 + first + e) * p.ldo[0] + i) = make_uint2(pack_bf16(v[e].x, v[e].y), pack_bf16(v[e].z, v[e].w));
         }
     }
     if (p.split > 1) umma::cluster_sync_any();       // no block leaves while another reads its sums

@@ -51,11 +51,12 @@ struct TileArgs {
 constexpr int kOperandBytes = 128 * umma::kRowBytes;          // 128 indexes x 128 bytes of K: 16 KiB
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kStages = 6;
-constexpr int kUnitCols = 32;                                 // columns of one output store: 64 bytes
-constexpr int kUnitBytes = 128 * 2 * kUnitCols;
-constexpr int kUnits = 4;
-constexpr int kTileThreads = 256;                             // warp 0 loads, 1 multiplies, 2 owns tensor memory, 4-7 store
-constexpr int kTileSmem = 1024 + kStages * kStageBytes + kUnits * kUnitBytes + 256;
+constexpr int kUnitCols = 32;                                 // columns of one output store, 64 bytes, of a warp's 32 rows
+constexpr int kUnitBytes = 32 * 2 * kUnitCols;
+constexpr int kUnits = 2;                                     // of each storing warp
+constexpr int kStoreWarps = 8;
+constexpr int kTileThreads = 128 + 32 * kStoreWarps;          // warp 0 loads, 1 multiplies, 2 owns tensor memory, 4-11 store
+constexpr int kTileSmem = 1024 + kStages * kStageBytes + kStoreWarps * kUnits * kUnitBytes + 256;
 
 struct TileBarriers {
     uint64_t full[kStages], empty[kStages], done[2], drained[2];
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     extern __shared__ uint8_t raw_smem[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t* staging = smem + kStages * kStageBytes;
-    TileBarriers* bars = reinterpret_cast<TileBarriers*>(staging + kUnits * kUnitBytes);
+    TileBarriers* bars = reinterpret_cast<TileBarriers*>(staging + kStoreWarps * kUnits * kUnitBytes);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? umma::cluster_rank() : 0;
     const uint32_t tiles = p.problems * p.m_tiles * p.n_tiles, first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
         for (int i = 0; i < 2; ++i) {
             pipe::mbar_init(&bars->done[i], 1);
-            pipe::mbar_init(&bars->drained[i], 4 * CTAS);
+            pipe::mbar_init(&bars->drained[i], kStoreWarps * CTAS);
         }
         pipe::mbar_init_fence();
         for (int i = 0; i < 2; ++i) {
@@ -183,21 +184,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             }
         }
     } else if (warp >= 4) {
-        const uint32_t row = (warp - 4) * 32 + lane;          // of the block's 128, and the tensor-memory lane
-        const uint32_t lane_base = tmem + ((warp - 4) << 21);
+        // Two warps for each quarter of the rows (the quarter of tensor memory that a warp can read is its number's), each
+        // with half of the columns.  A warp stages and stores its 32 rows by itself.
+        const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t lane_base = tmem + (quarter << 21), c_begin = half * (kOut / 2), c_end = c_begin + kOut / 2;
+        uint8_t* slots = staging + (warp - 4) * kUnits * kUnitBytes;
         uint32_t unit = 0, n_tile = 0;
         // 32 columns of this thread's row, as 16 words, through shared memory to the output
         auto store_unit = [&](const CUtensorMap* map, int x, int y, const uint32_t (&w)[16]) {
-            uint8_t* slot = staging + (unit % kUnits) * kUnitBytes;
-            if (threadIdx.x == 128) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kUnits - 1) : "memory");
-            umma::named_sync(1, 128);
-            uint4* line = reinterpret_cast<uint4*>(slot + row * 64);
+            uint8_t* slot = slots + (unit % kUnits) * kUnitBytes;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kUnits - 1) : "memory");
+            __syncwarp();
+            uint4* line = reinterpret_cast<uint4*>(slot + lane * 64);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) line[c ^ ((row >> 1) & 3)] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+            for (int c = 0; c < 4; ++c) line[c ^ ((lane >> 1) & 3)] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
             pipe::fence_async_smem();
-            umma::named_sync(1, 128);
-            if (threadIdx.x == 128 && y < static_cast<int>(p.m)) {
-                umma::tile_store(map, x, y, slot);
+            __syncwarp();
+            if (lane == 0) {
+                if (y < static_cast<int>(p.m)) umma::tile_store(map, x, y, slot);
                 pipe::bulk_commit();
             }
             ++unit;
@@ -208,19 +212,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         };
         for (uint32_t tile = first; tile < tiles; tile += step, ++n_tile) {
             const uint32_t acc = n_tile & 1;
-            // a wait that gave up in one thread ends the loop in all: they meet at barriers
-            if (!umma::named_all(1, 128, pipe::mbar_wait(&bars->done[acc], (n_tile >> 1) & 1, 204, &g_product_fault))) break;
+            if (!pipe::mbar_wait(&bars->done[acc], (n_tile >> 1) & 1, 204, &g_product_fault)) break;
+            __syncwarp();
             umma::fence_after();
             const TilePlace at = place_of(p, tile);
-            const int m0 = static_cast<int>(at.m * 128 * CTAS + rank * 128);
+            const int m0 = static_cast<int>(at.m * 128 * CTAS + rank * 128 + quarter * 32);
             const uint32_t n0 = at.n * kOut;
             const uint32_t cols = min(kOut, p.n - n0);
             float row_scale = 0.0f;
             if constexpr (E4M3)
-                if (m0 + row < p.m) row_scale = p.a_scale[m0 + row];
+                if (m0 + lane < p.m) row_scale = p.a_scale[m0 + lane];
             uint32_t w[16];
 #pragma unroll 1
-            for (uint32_t c = 0; c < kOut; c += kUnitCols) {
+            for (uint32_t c = c_begin; c < c_end; c += kUnitCols) {
                 float v[32];
                 umma::tmem_load32(lane_base + acc * kN + c, v);
                 if constexpr (GATED) {
@@ -228,7 +232,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     umma::tmem_load32(lane_base + acc * kN + kOut + c, u);
                     umma::tmem_wait(v);
                     umma::tmem_wait(u);
-                    if (c + kUnitCols == kOut) {              // the accumulators are read: they may be overwritten
+                    if (c + kUnitCols == c_end) {             // the accumulators are read: they may be overwritten
                         umma::fence_before();
                         __syncwarp();
                         if (lane == 0) umma::cluster_arrive(umma::cluster_addr(&bars->drained[acc], 0));
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     store_unit(&p.out[0], static_cast<int>(n0 + c), m0, w);
                 } else {
                     umma::tmem_wait(v);
-                    if (c + kUnitCols == kOut) {
+                    if (c + kUnitCols == c_end) {
                         umma::fence_before();
                         __syncwarp();
                         if (lane == 0) umma::cluster_arrive(umma::cluster_addr(&bars->drained[acc], 0));
@@ -265,7 +269,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
             }
         }
-        if (threadIdx.x == 128) pipe::bulk_wait_all();
+        if (lane == 0) pipe::bulk_wait_all();
     }
     __syncwarp();
     umma::fence_before();
