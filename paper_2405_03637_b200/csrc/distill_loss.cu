@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
     constexpr uint32_t kN = V::kN;
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ DistillShared sh;
+    after_previous();
     float* tp = reinterpret_cast<float*>(dynamic);              // teacher: p, student's logit, index
     float* tz = tp + a.k;
     int* ti = reinterpret_cast<int*>(tz + a.k);
@@ -469,6 +470,7 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
     constexpr uint32_t kN = V::kN;
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ StagedShared sh;
+    after_previous();
     uint4* stage = reinterpret_cast<uint4*>(dynamic);                                     // [slice]
     int64_t* raw_index = reinterpret_cast<int64_t*>(dynamic + 16ull * a.slice);           // [k], 4 or 8 bytes each: as it came
     float* raw_top = reinterpret_cast<float*>(raw_index + a.k);                           // [k]
@@ -730,23 +732,6 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
     if (a.cluster > 1) umma::cluster_sync_any();    // no block leaves while another may still write to it
 }
 
-template <auto Kernel, typename... Args>
-static collage_status_t launch_rows(uint64_t blocks, int threads, uint32_t cluster, size_t smem, cudaStream_t s, Args... args) {
-    if (allow_smem<Kernel>(kMaxSmem) != cudaSuccess) return COLLAGE_ERR_CUDA;
-    if (blocks >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {cluster, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, Kernel, args...) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
-}
-
 template <int MODE>
 static collage_status_t launch_distill(DistillArgs& a, uint64_t rows, collage_dtype_t dtype, int sm_count, void* stream) {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -769,14 +754,14 @@ static collage_status_t launch_distill(DistillArgs& a, uint64_t rows, collage_dt
             const size_t smem = 16ull * a.slice + teacher;
             const uint64_t fit = std::max<uint64_t>(1, std::min<uint64_t>(3, (kSmSmem - 1024) / (smem + sizeof(StagedShared) + 1024)));
             const uint64_t groups = std::min<uint64_t>(rows, std::max<uint64_t>(1, fit * sm_count / a.cluster));
-            return bf16 ? launch_rows<&distill_staged_kernel<uint16_t>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows)
-                        : launch_rows<&distill_staged_kernel<float>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows);
+            return bf16 ? launch<&distill_staged_kernel<uint16_t>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows)
+                        : launch<&distill_staged_kernel<float>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows);
         }
         a.cluster = 1;
     }
     spread(kDistillThreads);
-    return bf16 ? launch_rows<&distill_kernel<uint16_t, MODE>>(rows * a.cluster, kDistillThreads, a.cluster, 12ull * a.k, s, a)
-                : launch_rows<&distill_kernel<float, MODE>>(rows * a.cluster, kDistillThreads, a.cluster, 12ull * a.k, s, a);
+    return bf16 ? launch<&distill_kernel<uint16_t, MODE>>(rows * a.cluster, kDistillThreads, a.cluster, 12ull * a.k, s, a)
+                : launch<&distill_kernel<float, MODE>>(rows * a.cluster, kDistillThreads, a.cluster, 12ull * a.k, s, a);
 }
 
 // Everything the three entry points check alike; `read` and `written` are their float[rows] arrays.

@@ -36,9 +36,10 @@ constexpr int kTile = 64, kStep = 16;
 
 // 64 x 64 outputs a block, 4 x 4 a thread, operands staged as floats.
 template <typename T, bool PAIRED>
-__global__ void __launch_bounds__(256) product_any_kernel(const __grid_constant__ ProductArgs p) {
+__global__ void __launch_bounds__(256) product_any_kernel(const __grid_constant__ ProductArgs p, uint32_t m_tiles) {
+    after_previous();
     __shared__ float sa[kStep][kTile + 4], sb[PAIRED ? 2 : 1][kStep][kTile + 4];
-    const uint64_t m0 = blockIdx.x * static_cast<uint64_t>(kTile), n0 = blockIdx.y * static_cast<uint64_t>(kTile);
+    const uint64_t m0 = blockIdx.x % m_tiles * static_cast<uint64_t>(kTile), n0 = blockIdx.x / m_tiles * static_cast<uint64_t>(kTile);
     const int tm = threadIdx.x & 15, tn = threadIdx.x >> 4;
     float acc[PAIRED ? 2 : 1][4][4] = {};
     auto load = [&](const Operand& o, uint64_t i0, uint64_t limit, uint64_t k0, float (*dst)[kTile + 4]) {
@@ -90,6 +91,7 @@ struct GateArgs {
 };
 
 __global__ void __launch_bounds__(256) gate_backward_any_kernel(const __grid_constant__ GateArgs a) {
+    after_previous();
     const uint64_t row = blockIdx.x;
     for (uint64_t j = threadIdx.x; j < a.cols; j += 256) {
         const float dh = bf16_value(a.dh[row * a.lddh + j]), u = bf16_value(a.up[row * a.ldu + j]);
@@ -101,6 +103,7 @@ __global__ void __launch_bounds__(256) gate_backward_any_kernel(const __grid_con
 
 // The same on rows of whole 16-byte vectors: a vector a thread and turn, the next one's loads sent before this one's results.
 __global__ void __launch_bounds__(256) gate_backward_kernel(const __grid_constant__ GateArgs a, uint64_t rows) {
+    after_previous();
     const uint64_t vectors = a.cols >> 3, total = rows * vectors, step = gridDim.x * 256ull;
     auto at = [](const uint16_t* p, uint64_t ld, uint64_t row, uint64_t v) { return reinterpret_cast<const uint4*>(p + row * ld) + v; };
     uint4 next[3];
@@ -178,42 +181,19 @@ static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) 
     const uint64_t tiles = static_cast<uint64_t>(t.problems) * t.m_tiles * t.n_tiles;
     if (tiles >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
     t.group = 8;
-    constexpr auto kernel = &tile_kernel<E4M3, A_MN, B_MN, GATED, CTAS>;
-    if (allow_smem<kernel>(kTileSmem) != cudaSuccess) return COLLAGE_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(std::min<uint64_t>(tiles, sm_count / CTAS)) * CTAS);
-    cfg.blockDim = dim3(kTileThreads);
-    cfg.dynamicSmemBytes = kTileSmem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {CTAS, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, t) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
+    const uint64_t blocks = std::min<uint64_t>(tiles, sm_count / CTAS) * CTAS;
+    return launch<&tile_kernel<E4M3, A_MN, B_MN, GATED, CTAS>>(blocks, kTileThreads, CTAS, kTileSmem, s, t);
 }
 
 template <bool E4M3, bool A_MN, bool GATED, int NT>
 static collage_status_t launch_slim_as(const SlimArgs& t, uint64_t blocks, cudaStream_t s) {
-    constexpr auto kernel = &slim_kernel<E4M3, A_MN, GATED, NT>;
-    if (blocks >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
-    if (allow_smem<kernel>(slim_smem<NT>()) != cudaSuccess) return COLLAGE_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-    cfg.blockDim = dim3(kSlimThreads);
-    cfg.dynamicSmemBytes = slim_smem<NT>();
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {t.split, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, t) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
+    return launch<&slim_kernel<E4M3, A_MN, GATED, NT>>(blocks, kSlimThreads, t.split, slim_smem<NT>(), s, t);
 }
 
 static uint32_t slim_tokens(uint64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128; }
 
-// The sum over K is split until there is a block for every SM, as long as each has eight blocks of K.
+// The sum over K is split until there is a block for every SM, as long as each has eight blocks of K; of the narrowest tiles,
+// three of which fit an SM, once more where enough of K is left (one token x 4096 x 11008: 33 against 35 us).
 template <bool E4M3, bool A_MN, bool GATED>
 static collage_status_t launch_slim(SlimArgs& t, int sm_count, cudaStream_t s) {
     const uint32_t nt = slim_tokens(t.n), blocks = t.terms * t.k_blocks;
@@ -221,6 +201,7 @@ static collage_status_t launch_slim(SlimArgs& t, int sm_count, cudaStream_t s) {
     const uint64_t tiles = static_cast<uint64_t>(t.token_tiles) * ((t.m + (GATED ? 63 : 127)) / (GATED ? 64 : 128));
     t.split = 1;
     while (t.split < 8 && tiles * t.split < static_cast<uint64_t>(sm_count) && blocks / (2 * t.split) >= 8) t.split *= 2;
+    if (nt == 16 && t.split < 8 && tiles * t.split < 2ull * sm_count && blocks / (2 * t.split) >= 24) t.split *= 2;
     switch (nt) {
         case 16: return launch_slim_as<E4M3, A_MN, GATED, 16>(t, tiles * t.split, s);
         case 32: return launch_slim_as<E4M3, A_MN, GATED, 32>(t, tiles * t.split, s);
@@ -330,11 +311,10 @@ static collage_status_t tiles_dw(const collage_matrix_t* dgate, const collage_ma
 // ---- any alignment ---------------------------------------------------------------------------------------------------
 
 template <typename T, bool PAIRED>
-collage_status_t launch_product(const ProductArgs& p, cudaStream_t s) {
+static collage_status_t launch_product(const ProductArgs& p, cudaStream_t s) {
     if (p.m == 0 || p.n == 0) return COLLAGE_OK;
-    const dim3 grid(static_cast<unsigned>((p.m + kTile - 1) / kTile), static_cast<unsigned>((p.n + kTile - 1) / kTile));
-    product_any_kernel<T, PAIRED><<<grid, 256, 0, s>>>(p);
-    return launch_status();
+    const uint64_t m_tiles = (p.m + kTile - 1) / kTile, n_tiles = (p.n + kTile - 1) / kTile;
+    return launch<&product_any_kernel<T, PAIRED>>(m_tiles * n_tiles, 256, 1, 0, s, p, static_cast<uint32_t>(m_tiles));
 }
 
 static bool known(collage_activation_t a) { return a == COLLAGE_ACT_SILU || a == COLLAGE_ACT_GELU_TANH; }
@@ -486,13 +466,10 @@ collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const co
         g.activation = activation;
         bool vectors = dh->cols % 8 == 0;
         for (const collage_matrix_t* m : {dh, gate, up, dgate, dup}) vectors = vectors && rows_aligned(m, 2, 16);
-        if (vectors) {
-            const uint64_t blocks = (dh->rows * (dh->cols / 8) + 255) / 256;
-            gate_backward_kernel<<<static_cast<unsigned>(std::min<uint64_t>(blocks, 8ull * dev.sm_count)), 256, 0, s>>>(g, dh->rows);
-        } else {
-            gate_backward_any_kernel<<<static_cast<unsigned>(dh->rows), 256, 0, s>>>(g);
-        }
-        if ((st = launch_status()) != COLLAGE_OK) return st;
+        const uint64_t blocks = (dh->rows * (dh->cols / 8) + 255) / 256;
+        st = vectors ? launch<&gate_backward_kernel>(std::min<uint64_t>(blocks, 8ull * dev.sm_count), 256, 1, 0, s, g, dh->rows)
+                     : launch<&gate_backward_any_kernel>(dh->rows, 256, 1, 0, s, g);
+        if (st != COLLAGE_OK) return st;
     }
     // a product over no tokens or no channels is zero
     if (dh->rows == 0 || dh->cols == 0) {

@@ -91,7 +91,41 @@ inline bool rows_aligned(const collage_matrix_t* m, uint32_t elem_bytes, uint32_
     return reinterpret_cast<uintptr_t>(m->data) % bytes == 0 && (m->rows <= 1 || m->ld * elem_bytes % bytes == 0);
 }
 
-inline collage_status_t launch_status() { return cudaGetLastError() == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA; }
+// Once per kernel and device: leave to use all of the shared memory that it does not declare statically.
+template <auto Kernel>
+static cudaError_t allow_smem() {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+    if (done.load(std::memory_order_acquire) >> (dev & 63) & 1) return cudaSuccess;
+    cudaFuncAttributes attr;
+    if (const cudaError_t e = cudaFuncGetAttributes(&attr, Kernel); e != cudaSuccess) return e;
+    const int bytes = 227 * 1024 - static_cast<int>(attr.sharedSizeBytes);
+    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
+    return e;
+}
+
+// Launches a kernel in clusters of `cluster` blocks.  Its blocks may be set up while the stream's previous kernel still runs
+// (programmatic dependent launch): every kernel launched here begins with after_previous(), before it touches memory.
+template <auto Kernel, typename... Args>
+static collage_status_t launch(uint64_t blocks, int threads, uint32_t cluster, size_t smem, cudaStream_t stream, const Args&... args) {
+    if (blocks >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
+    if (smem > 48 * 1024 && allow_smem<Kernel>() != cudaSuccess) return COLLAGE_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, Kernel, args...) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
+}
 
 // Zeros in a matrix of 2-byte or 4-byte elements (asynchronous).
 inline collage_status_t clear_matrix(const collage_matrix_t* m, uint32_t elem_bytes, cudaStream_t stream) {
@@ -100,20 +134,13 @@ inline collage_status_t clear_matrix(const collage_matrix_t* m, uint32_t elem_by
                                                                                                                   : COLLAGE_ERR_CUDA;
 }
 
-// Once per kernel and device: leave to use the shared memory that it takes.
-template <auto Kernel>
-static cudaError_t allow_smem(int bytes) {
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
-    if (done.load(std::memory_order_acquire) >> (dev & 63) & 1) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
-    return e;
-}
-
 // ------------------------------------------------------------------------------------------------- device helpers ---
 
+// Everything that the stream's previous kernel wrote is visible behind this, and the next one may be set up.
+__device__ __forceinline__ void after_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float bf16_value(uint16_t h) { return __uint_as_float(static_cast<uint32_t>(h) << 16); }

@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     __syncthreads();
     if constexpr (CTAS == 2) umma::cluster_sync();            // the other block's barriers exist
     umma::fence_after();
+    after_previous();
     const uint32_t tmem = bars->tmem;
 
     // The first two warps run their loops as a whole, so that addresses and descriptors stay in uniform registers, and one

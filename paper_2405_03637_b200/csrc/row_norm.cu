@@ -24,6 +24,7 @@ constexpr int kRowThreads = 256;
 template <bool NORM>
 __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_constant__ RowArgs a) {
     __shared__ float slots[kRowThreads / 32];
+    after_previous();
     const uint64_t row = blockIdx.x;
     const uint16_t* x = a.x + row * a.ldx;
     const uint16_t* res = a.residual ? a.residual + row * a.ldres : nullptr;
@@ -72,6 +73,7 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
 template <int PER, bool NORM, bool WARP>
 __global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) row_kernel(const __grid_constant__ RowArgs a, uint64_t rows) {
     __shared__ float slots[32];
+    after_previous();
     const uint64_t row = WARP ? blockIdx.x * 4ull + (threadIdx.x >> 5) : blockIdx.x;
     if (WARP && row >= rows) return;
     const int t = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x, warps = threads >> 5;
@@ -155,24 +157,21 @@ __global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) row_kernel(
 // one (the shortest way through a row), as far as 1024 or 512 threads reach.
 template <bool NORM>
 static collage_status_t launch_rows(const RowArgs& a, uint64_t rows, bool vectors_fit, int sm_count, cudaStream_t s) {
-    const uint64_t v = a.cols >> 3, n = rows;
+    const uint64_t v = a.cols >> 3;
     const bool many = rows > 2ull * sm_count;
-    if (!vectors_fit || v > 4096) {
-        row_any_kernel<NORM><<<static_cast<unsigned>(rows), kRowThreads, 0, s>>>(a);
-    } else if (many && v <= 128) {
-        const unsigned grid = static_cast<unsigned>((rows + 3) / 4);
-        if (v <= 32) row_kernel<1, NORM, true><<<grid, 128, 0, s>>>(a, n);
-        else if (v <= 64) row_kernel<2, NORM, true><<<grid, 128, 0, s>>>(a, n);
-        else row_kernel<4, NORM, true><<<grid, 128, 0, s>>>(a, n);
-    } else {
-        const uint64_t per = v > 2048 ? 8 : many ? 4 : v > 1024 ? 2 : 1;
-        const unsigned threads = static_cast<unsigned>((v + per * 32 - 1) / (per * 32) * 32), grid = static_cast<unsigned>(rows);
-        if (per == 1) row_kernel<1, NORM, false><<<grid, threads, 0, s>>>(a, n);
-        else if (per == 2) row_kernel<2, NORM, false><<<grid, threads, 0, s>>>(a, n);
-        else if (per == 4) row_kernel<4, NORM, false><<<grid, threads, 0, s>>>(a, n);
-        else row_kernel<8, NORM, false><<<grid, threads, 0, s>>>(a, n);
+    if (!vectors_fit || v > 4096) return launch<&row_any_kernel<NORM>>(rows, kRowThreads, 1, 0, s, a);
+    if (many && v <= 128) {
+        const uint64_t grid = (rows + 3) / 4;
+        return v <= 32   ? launch<&row_kernel<1, NORM, true>>(grid, 128, 1, 0, s, a, rows)
+               : v <= 64 ? launch<&row_kernel<2, NORM, true>>(grid, 128, 1, 0, s, a, rows)
+                         : launch<&row_kernel<4, NORM, true>>(grid, 128, 1, 0, s, a, rows);
     }
-    return launch_status();
+    const uint64_t per = v > 2048 ? 8 : many ? 4 : v > 1024 ? 2 : 1;
+    const int threads = static_cast<int>((v + per * 32 - 1) / (per * 32) * 32);
+    return per == 1   ? launch<&row_kernel<1, NORM, false>>(rows, threads, 1, 0, s, a, rows)
+           : per == 2 ? launch<&row_kernel<2, NORM, false>>(rows, threads, 1, 0, s, a, rows)
+           : per == 4 ? launch<&row_kernel<4, NORM, false>>(rows, threads, 1, 0, s, a, rows)
+                      : launch<&row_kernel<8, NORM, false>>(rows, threads, 1, 0, s, a, rows);
 }
 
 struct RowBackwardArgs {
@@ -191,6 +190,7 @@ struct RowBackwardArgs {
 // dx of one row: one block, element by element.
 __global__ void __launch_bounds__(kRowThreads) row_backward_any_kernel(const __grid_constant__ RowBackwardArgs a) {
     __shared__ float slots[kRowThreads / 32];
+    after_previous();
     const uint64_t row = blockIdx.x;
     const uint16_t* dy = a.dy + row * a.lddy;
     const uint16_t* r = a.r + row * a.ldr;
@@ -210,12 +210,14 @@ __global__ void __launch_bounds__(kRowThreads) row_backward_any_kernel(const __g
 constexpr int kWeightChunks = 320;        // row chunks whose sums are kept apart
 
 // Sums of dy * n over a chunk of rows, 32 columns a block.
-__global__ void __launch_bounds__(kRowThreads) row_dweight_any_kernel(const __grid_constant__ RowBackwardArgs a) {
+__global__ void __launch_bounds__(kRowThreads) row_dweight_any_kernel(const __grid_constant__ RowBackwardArgs a, uint32_t chunks) {
     __shared__ float part[kRowThreads / 32][32];
-    const uint64_t j = blockIdx.x * 32ull + (threadIdx.x & 31);
+    after_previous();
+    const uint32_t chunk = blockIdx.x % chunks;
+    const uint64_t j = blockIdx.x / chunks * 32ull + (threadIdx.x & 31);
     const int lane_row = threadIdx.x >> 5;
-    const uint64_t per = (a.rows + gridDim.y - 1) / gridDim.y;
-    const uint64_t begin = blockIdx.y * per, end = min(begin + per, a.rows);
+    const uint64_t per = (a.rows + chunks - 1) / chunks;
+    const uint64_t begin = chunk * per, end = min(begin + per, a.rows);
     float sum = 0.0f;
     if (j < a.cols)
         for (uint64_t i = begin + lane_row; i < end; i += kRowThreads / 32)
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(kRowThreads) row_dweight_any_kernel(const __gr
     __syncthreads();
     if (lane_row == 0 && j < a.cols) {
         for (int k = 1; k < kRowThreads / 32; ++k) sum += part[k][threadIdx.x];
-        a.partial[blockIdx.y * a.cols + j] = sum;
+        a.partial[chunk * a.cols + j] = sum;
     }
 }
 
@@ -237,6 +239,7 @@ template <int PER, int THREADS>
 __global__ void __launch_bounds__(THREADS, PER > 1 ? 1 : 2) row_backward_kernel(const __grid_constant__ RowBackwardArgs a, int group_threads) {
     __shared__ float slots[2][32];
     extern __shared__ __align__(16) uint8_t dynamic[];
+    after_previous();
     const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
     const int lane = threadIdx.x & 31, group_warps = group_threads >> 5, warp0 = group * group_warps;
     const int vectors = static_cast<int>(a.cols >> 3);
@@ -362,6 +365,7 @@ __global__ void __launch_bounds__(THREADS, PER > 1 ? 1 : 2) row_backward_kernel(
 // Sums of the blocks' parts, in order: 32 columns a block, a thread takes every eighth part of one.
 __global__ void __launch_bounds__(kRowThreads) row_dweight_finish_kernel(const float* partial, int chunks, uint64_t cols, uint16_t* dweight) {
     __shared__ float part[kRowThreads / 32][32];
+    after_previous();
     const uint64_t j = blockIdx.x * 32ull + (threadIdx.x & 31);
     const int first = threadIdx.x >> 5;
     float sum = 0.0f;
@@ -384,11 +388,10 @@ static unsigned launch_backward_as(const RowBackwardArgs& a, int sm_count, cudaS
     const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), groups = std::max(1, std::min(kBackwardThreads / group, 15));
     // the places hold the groups' dweight too: 4 cols bytes a group, against 48 kDepth bytes for each 8 columns
     constexpr int place_bytes = kDepth * 3 * PER * 16;
-    if (allow_smem<&row_backward_kernel<PER, THREADS>>(place_bytes * THREADS) != cudaSuccess) return 0;
     const uint64_t resident = std::min<uint64_t>(kWeightChunks, (PER > 1 ? 1ull : 2ull) * sm_count);
     const unsigned grid = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, resident));
-    row_backward_kernel<PER, THREADS><<<grid, group * groups, place_bytes * group * groups, s>>>(a, group);
-    return grid;
+    const collage_status_t st = launch<&row_backward_kernel<PER, THREADS>>(grid, group * groups, 1, place_bytes * group * groups, s, a, group);
+    return st == COLLAGE_OK ? grid : 0;
 }
 // Returns the number of partial rows of dweight, 0 after an error.  Rows of up to 256 columns are a warp's, without barriers;
 // longer ones take two vectors a thread (half the barriers and joins of one: 50 against 58 us at 8191 x 4096).
@@ -531,17 +534,18 @@ collage_status_t collage_add_rms_norm_backward(const collage_matrix_t* dy, const
     if (fit) {
         const unsigned parts = launch_backward(a, dev.sm_count, s);
         if (!parts) return COLLAGE_ERR_CUDA;
-        if (dweight) row_dweight_finish_kernel<<<finish_blocks, kRowThreads, 0, s>>>(a.partial, static_cast<int>(parts), a.cols, a.dweight);
-        return launch_status();
+        return dweight ? launch<&row_dweight_finish_kernel>(finish_blocks, kRowThreads, 1, 0, s, static_cast<const float*>(a.partial), static_cast<int>(parts), a.cols, a.dweight)
+                       : COLLAGE_OK;
     }
     if (dweight) {                            // before dx, which may take dy's place
         uint64_t chunks = (8ull * dev.sm_count + finish_blocks - 1) / finish_blocks;
         chunks = std::min<uint64_t>({chunks, (a.rows + 7) / 8, static_cast<uint64_t>(kWeightChunks)});
-        row_dweight_any_kernel<<<dim3(finish_blocks, static_cast<unsigned>(chunks)), kRowThreads, 0, s>>>(a);
-        row_dweight_finish_kernel<<<finish_blocks, kRowThreads, 0, s>>>(a.partial, static_cast<int>(chunks), a.cols, a.dweight);
+        st = launch<&row_dweight_any_kernel>(finish_blocks * chunks, kRowThreads, 1, 0, s, a, static_cast<uint32_t>(chunks));
+        if (st == COLLAGE_OK)
+            st = launch<&row_dweight_finish_kernel>(finish_blocks, kRowThreads, 1, 0, s, static_cast<const float*>(a.partial), static_cast<int>(chunks), a.cols, a.dweight);
     }
-    if (dx) row_backward_any_kernel<<<static_cast<unsigned>(a.rows), kRowThreads, 0, s>>>(a);
-    return launch_status();
+    if (dx && st == COLLAGE_OK) st = launch<&row_backward_any_kernel>(a.rows, kRowThreads, 1, 0, s, a);
+    return st;
 }
 
 }  // extern "C"
