@@ -27,7 +27,10 @@ struct DistillArgs {
     float inv_t, t;
 };
 
-constexpr int kDistillThreads = 256, kStagedThreads = 192;
+#ifndef DT
+#define DT 256
+#endif
+constexpr int kDistillThreads = DT, kStagedThreads = 192;
 constexpr uint32_t kSeenWords = 512;           // two bitmaps over the indexes of a row, modulo 2^14
 constexpr uint32_t kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;

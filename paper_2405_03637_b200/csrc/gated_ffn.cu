@@ -186,33 +186,46 @@ static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) 
 }
 
 template <bool E4M3, bool A_MN, bool GATED, int NT>
-static collage_status_t launch_slim_as(const SlimArgs& t, uint64_t blocks, cudaStream_t s) {
-    return launch<&slim_kernel<E4M3, A_MN, GATED, NT>>(blocks, kSlimThreads, t.split, slim_smem<NT>(), s, t);
+static collage_status_t launch_slim_as(SlimArgs& t, uint64_t blocks, int sm_count, cudaStream_t s) {
+    const bool alone = blocks <= static_cast<uint64_t>(sm_count);
+    t.stages = std::min(kMaxSlimStages, slim_stages<NT>(alone));
+    return launch<&slim_kernel<E4M3, A_MN, GATED, NT>>(blocks, kSlimThreads, t.split, slim_smem<NT>(alone), s, t);
 }
 
-static uint32_t slim_tokens(uint64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128; }
+// The most parts that a sum over `blocks` blocks of K is split into: at least eight blocks each.
+static uint32_t most_split(uint32_t blocks) { return blocks >= 64 ? 8 : blocks >= 32 ? 4 : blocks >= 16 ? 2 : 1; }
+
+// Tokens of a slim tile: all of them up to 128, fewer where even with K split SMs would be left without a tile (there are
+// `weight_tiles` for each tile of tokens).  333 x 768 x 2048 forward: 10.8 us with 64 tokens, 13.3 with 128; but its dx, whose K
+// can be split, loses by narrow tiles, which read the weights more often (160 x 4096 x 11008: 120 us against 55).
+static uint32_t slim_tokens(uint64_t tokens, uint64_t weight_tiles, uint32_t blocks, int sm_count) {
+    uint32_t nt = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+    while (nt > 32 && tokens > nt / 2 && (tokens + nt - 1) / nt * weight_tiles * most_split(blocks) < static_cast<uint64_t>(sm_count)) nt /= 2;
+    return nt;
+}
 
 // The sum over K is split until there is a block for every SM, as long as each has eight blocks of K; of the narrowest tiles,
 // three of which fit an SM, once more where enough of K is left (one token x 4096 x 11008: 33 against 35 us).
 template <bool E4M3, bool A_MN, bool GATED>
-static collage_status_t launch_slim(SlimArgs& t, int sm_count, cudaStream_t s) {
-    const uint32_t nt = slim_tokens(t.n), blocks = t.terms * t.k_blocks;
+static collage_status_t launch_slim(SlimArgs& t, uint32_t nt, uint64_t weight_tiles, int sm_count, cudaStream_t s) {
+    const uint32_t blocks = t.terms * t.k_blocks;
     t.token_tiles = (t.n + nt - 1) / nt;
-    const uint64_t tiles = static_cast<uint64_t>(t.token_tiles) * ((t.m + (GATED ? 63 : 127)) / (GATED ? 64 : 128));
+    const uint64_t tiles = t.token_tiles * weight_tiles;
     t.split = 1;
-    while (t.split < 8 && tiles * t.split < static_cast<uint64_t>(sm_count) && blocks / (2 * t.split) >= 8) t.split *= 2;
+    while (t.split < most_split(blocks) && tiles * t.split < static_cast<uint64_t>(sm_count)) t.split *= 2;
     if (nt == 16 && t.split < 8 && tiles * t.split < 2ull * sm_count && blocks / (2 * t.split) >= 24) t.split *= 2;
     switch (nt) {
-        case 16: return launch_slim_as<E4M3, A_MN, GATED, 16>(t, tiles * t.split, s);
-        case 32: return launch_slim_as<E4M3, A_MN, GATED, 32>(t, tiles * t.split, s);
-        case 64: return launch_slim_as<E4M3, A_MN, GATED, 64>(t, tiles * t.split, s);
-        default: return launch_slim_as<E4M3, A_MN, GATED, 128>(t, tiles * t.split, s);
+        case 16: return launch_slim_as<E4M3, A_MN, GATED, 16>(t, tiles * t.split, sm_count, s);
+        case 32: return launch_slim_as<E4M3, A_MN, GATED, 32>(t, tiles * t.split, sm_count, s);
+        case 64: return launch_slim_as<E4M3, A_MN, GATED, 64>(t, tiles * t.split, sm_count, s);
+        default: return launch_slim_as<E4M3, A_MN, GATED, 128>(t, tiles * t.split, sm_count, s);
     }
 }
 
-// Slim tiles where there are few tokens, or too few pairs' tiles to fill the GPU.
+// Slim tiles where there are few tokens, or too few pairs' tiles to keep the GPU busy (at 700 x 4096 x 11008 dx has 48 of them
+// for 74 pairs: 115 us against 160 in slim tiles; at 384 it has 32: 90 us in slim tiles against 100).
 static bool slim(uint64_t tokens, uint64_t pair_tiles, int sm_count) {
-    return tokens <= 128 || pair_tiles * 4 < 3ull * (sm_count / 2);
+    return tokens <= 128 || pair_tiles * 18 < 5ull * sm_count;
 }
 
 // The forward products with 16-byte aligned rows.
@@ -225,8 +238,10 @@ static collage_status_t tiles_forward(const collage_matrix_t* x, const collage_m
     const collage_matrix_t* outs[3] = {h, gate, up};
     if (slim(x->rows, (x->rows + 255) / 256 * ((h->cols + 127) / 128), sm_count)) {
         SlimArgs t = {};
+        const uint64_t weight_tiles = (h->cols + 63) / 64;
+        const uint32_t nt = slim_tokens(x->rows, weight_tiles, k_blocks, sm_count);
         if (!(make_map(&t.a[0], wg, E4M3, k, 64, false) && make_map(&t.a[1], wu, E4M3, k, 64, false) &&
-              make_map(&t.b[0], x, E4M3, k, slim_tokens(x->rows), false)))
+              make_map(&t.b[0], x, E4M3, k, nt, false)))
             return COLLAGE_ERR_CUDA;
         for (int i = 0; i < 3 && outs[i]; ++i) {
             t.out[i] = static_cast<uint16_t*>(outs[i]->data);
@@ -241,7 +256,7 @@ static collage_status_t tiles_forward(const collage_matrix_t* x, const collage_m
         t.terms = 1;
         t.keep = gate != nullptr;
         t.activation = activation;
-        return launch_slim<E4M3, false, true>(t, sm_count, s);
+        return launch_slim<E4M3, false, true>(t, nt, weight_tiles, sm_count, s);
     }
     TileArgs t = {};
     bool ok = make_map(&t.a[0], x, E4M3, k, 128, false) && make_map(&t.b[0], wg, E4M3, k, 128, false) && make_map(&t.b[1], wu, E4M3, k, 128, false);
@@ -266,7 +281,8 @@ static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_ma
     const uint32_t k_blocks = static_cast<uint32_t>((dgate->cols + 63) / 64);
     if (slim(dx->rows, (dx->rows + 255) / 256 * ((dx->cols + 255) / 256), sm_count)) {
         SlimArgs t = {};
-        const uint32_t nt = slim_tokens(dx->rows);
+        const uint64_t weight_tiles = (dx->cols + 127) / 128;
+        const uint32_t nt = slim_tokens(dx->rows, weight_tiles, 2 * k_blocks, sm_count);
         if (!(make_map(&t.a[0], wg, false, 64, 64, false) && make_map(&t.a[1], wu, false, 64, 64, false) &&
               make_map(&t.b[0], dgate, false, 64, nt, false) && make_map(&t.b[1], dup, false, 64, nt, false)))
             return COLLAGE_ERR_CUDA;
@@ -276,7 +292,7 @@ static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_ma
         t.n = static_cast<uint32_t>(dx->rows);
         t.k_blocks = k_blocks;
         t.terms = 2;
-        return launch_slim<false, true, false>(t, sm_count, s);
+        return launch_slim<false, true, false>(t, nt, weight_tiles, sm_count, s);
     }
     TileArgs t = {};
     if (!(make_map(&t.a[0], dgate, false, 64, 128, false) && make_map(&t.a[1], dup, false, 64, 128, false) &&

@@ -13,7 +13,7 @@ struct SlimArgs {
     const float* token_scale;
     uint16_t* out[3];
     uint64_t ldo[3];
-    uint32_t m, n, token_tiles, k_blocks, terms, split;
+    uint32_t m, n, token_tiles, k_blocks, terms, split, stages;
     int keep, activation;
 };
 
@@ -21,21 +21,26 @@ constexpr int kSlimThreads = 128;
 
 template <int NT>
 __host__ __device__ constexpr int slim_stage_bytes() { return kOperandBytes + NT * static_cast<int>(umma::kRowBytes); }
-// As many stages as leave room for two blocks on an SM (three of the narrowest: 33 against 36 us for one token); the sums over the tile take their place afterwards.
+// Stages (the sums over the tile take their place afterwards): as many as leave room for two blocks on an SM, three of the
+// narrowest (33 against 36 us for one token x 4096 x 11008), or all that fit where there is at most one block for an SM.
+constexpr int kMaxSlimStages = 10;
 template <int NT>
-__host__ __device__ constexpr int slim_stages() { return NT <= 16 ? 4 : NT <= 32 ? 5 : NT <= 64 ? 4 : 3; }
+__host__ __device__ constexpr int slim_stages(bool alone) {
+    return alone ? 212 * 1024 / slim_stage_bytes<NT>() : NT <= 16 ? 4 : NT <= 32 ? 5 : NT <= 64 ? 4 : 3;
+}
 template <int NT>
-__host__ __device__ constexpr int slim_smem() { return 1024 + slim_stages<NT>() * slim_stage_bytes<NT>(); }
+constexpr int slim_smem(bool alone) { return 1024 + (slim_stages<NT>(alone) > kMaxSlimStages ? kMaxSlimStages : slim_stages<NT>(alone)) * slim_stage_bytes<NT>(); }
 
 template <bool E4M3, bool A_MN, bool GATED, int NT>
 __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constant__ SlimArgs p) {
-    constexpr uint32_t kStagesHere = slim_stages<NT>(), kBytes = slim_stage_bytes<NT>();
+    constexpr uint32_t kBytes = slim_stage_bytes<NT>();
     constexpr uint32_t kK = E4M3 ? 128 : 64, kColumns = NT < 32 ? 32 : NT, kIndexes = GATED ? 64 : 128;
     constexpr uint32_t kIdesc = umma::instr_desc(E4M3 ? 0 : 1, A_MN, false, 128, NT);
-    static_assert(kStagesHere * kBytes >= NT * 512, "the tile's sums fit the stages");
+    static_assert(slim_stages<NT>(false) * kBytes >= NT * 512, "the tile's sums fit the stages");
+    const uint32_t stages = p.stages;
     extern __shared__ uint8_t raw_smem[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
-    __shared__ uint64_t full[kStagesHere], empty[kStagesHere], done;
+    __shared__ uint64_t full[kMaxSlimStages], empty[kMaxSlimStages], done;
     __shared__ uint32_t tmem_slot;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = p.split > 1 ? umma::cluster_rank() : 0, tile = blockIdx.x / p.split;
@@ -45,7 +50,7 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
     const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(blocks) * (rank + 1) / p.split);
 
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < kStagesHere; ++i) {
+        for (uint32_t i = 0; i < stages; ++i) {
             pipe::mbar_init(&full[i], 1);
             pipe::mbar_init(&empty[i], 1);
         }
@@ -79,7 +84,7 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
                 umma::tile_load<1>(sb, &p.b[term], k, static_cast<int>(t0), bar);
             }
             __syncwarp();
-            if (++stage == kStagesHere) { stage = 0; phase ^= 1; }
+            if (++stage == stages) { stage = 0; phase ^= 1; }
         }
     } else if (warp == 1) {
         uint32_t stage = 0, phase = 0;
@@ -98,7 +103,7 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
                 if (kb + 1 == end) umma::commit<1>(&done);
             }
             __syncwarp();
-            if (++stage == kStagesHere) { stage = 0; phase ^= 1; }
+            if (++stage == stages) { stage = 0; phase ^= 1; }
         }
         if (ok) pipe::mbar_wait(&done, 0, 212, &g_product_fault);
     }

@@ -362,24 +362,23 @@ __global__ void __launch_bounds__(THREADS, PER > 1 ? 1 : 2) row_backward_kernel(
     }
 }
 
-// Sums of the blocks' parts, in order: 32 columns a block, a thread takes every eighth part of one.
-__global__ void __launch_bounds__(kRowThreads) row_dweight_finish_kernel(const float* partial, int chunks, uint64_t cols, uint16_t* dweight) {
-    __shared__ float part[kRowThreads / 32][32];
+// Sums of the blocks' parts, in order: 32 columns a block, each of its 32 warps takes every 32nd part.
+constexpr int kFinishSums = 1024;
+__global__ void __launch_bounds__(kFinishSums) row_dweight_finish_kernel(const float* partial, int chunks, uint64_t cols, uint16_t* dweight) {
+    __shared__ float part[kFinishSums / 32][33];
     after_previous();
-    const uint64_t j = blockIdx.x * 32ull + (threadIdx.x & 31);
-    const int first = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint64_t j = blockIdx.x * 32ull + lane;
     float sum = 0.0f;
     if (j < cols) {
-#pragma unroll 8
-        for (int k = first; k < chunks; k += kRowThreads / 32) sum += partial[k * cols + j];
+#pragma unroll 5
+        for (int k = warp; k < chunks; k += kFinishSums / 32) sum += partial[k * cols + j];
     }
-    part[first][threadIdx.x & 31] = sum;
+    part[warp][lane] = sum;
     __syncthreads();
-    if (first == 0 && j < cols) {
-#pragma unroll
-        for (int k = 1; k < kRowThreads / 32; ++k) sum += part[k][threadIdx.x];
-        dweight[j] = to_bf16(sum);
-    }
+    sum = warp_sum(part[lane][warp]);                        // column `warp` of the block's
+    const uint64_t out = blockIdx.x * 32ull + warp;
+    if (lane == 0 && out < cols) dweight[out] = to_bf16(sum);
 }
 
 template <int PER, int THREADS>
@@ -534,7 +533,7 @@ collage_status_t collage_add_rms_norm_backward(const collage_matrix_t* dy, const
     if (fit) {
         const unsigned parts = launch_backward(a, dev.sm_count, s);
         if (!parts) return COLLAGE_ERR_CUDA;
-        return dweight ? launch<&row_dweight_finish_kernel>(finish_blocks, kRowThreads, 1, 0, s, static_cast<const float*>(a.partial), static_cast<int>(parts), a.cols, a.dweight)
+        return dweight ? launch<&row_dweight_finish_kernel>(finish_blocks, kFinishSums, 1, 0, s, static_cast<const float*>(a.partial), static_cast<int>(parts), a.cols, a.dweight)
                        : COLLAGE_OK;
     }
     if (dweight) {                            // before dx, which may take dy's place
@@ -542,7 +541,7 @@ collage_status_t collage_add_rms_norm_backward(const collage_matrix_t* dy, const
         chunks = std::min<uint64_t>({chunks, (a.rows + 7) / 8, static_cast<uint64_t>(kWeightChunks)});
         st = launch<&row_dweight_any_kernel>(finish_blocks * chunks, kRowThreads, 1, 0, s, a, static_cast<uint32_t>(chunks));
         if (st == COLLAGE_OK)
-            st = launch<&row_dweight_finish_kernel>(finish_blocks, kRowThreads, 1, 0, s, static_cast<const float*>(a.partial), static_cast<int>(chunks), a.cols, a.dweight);
+            st = launch<&row_dweight_finish_kernel>(finish_blocks, kFinishSums, 1, 0, s, static_cast<const float*>(a.partial), static_cast<int>(chunks), a.cols, a.dweight);
     }
     if (dx && st == COLLAGE_OK) st = launch<&row_backward_any_kernel>(a.rows, kRowThreads, 1, 0, s, a);
     return st;
