@@ -1,5 +1,5 @@
 // Gated feed-forward projections: h = a(x w_gate^T) * (x w_up^T), the backward pass, and the same with e4m3 operands.
-#include "product_slim.cuh"
+#include "product_any.cuh"
 
 namespace collage {
 
@@ -10,78 +10,6 @@ cudaError_t read_clear_product_fault(unsigned int* out) {
 }
 
 namespace ops {
-
-// An operand of a product, element (i, k) at data + i * row + k * col: either of the two strides may be 1.
-struct Operand {
-    const void* data;
-    uint64_t row, col;
-};
-
-struct ProductArgs {
-    Operand a[2], b[2];              // PAIRED: two products with a common a; otherwise a sum of `terms` products
-    const float* a_scale;
-    const float* b_scale[2];
-    uint16_t* out[3];                // PAIRED: h, gate, up (the last two may be NULL)
-    uint64_t ldo[3];
-    uint64_t m, n, k;
-    int terms, activation;
-};
-
-__device__ __forceinline__ float element(const uint16_t* p) { return bf16_value(*p); }
-__device__ __forceinline__ float element(const uint8_t* p) {
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3)));
-}
-
-constexpr int kTile = 64, kStep = 16;
-
-// 64 x 64 outputs a block, 4 x 4 a thread, operands staged as floats.
-template <typename T, bool PAIRED>
-__global__ void __launch_bounds__(256) product_any_kernel(const __grid_constant__ ProductArgs p, uint32_t m_tiles) {
-    after_previous();
-    __shared__ float sa[kStep][kTile + 4], sb[PAIRED ? 2 : 1][kStep][kTile + 4];
-    const uint64_t m0 = blockIdx.x % m_tiles * static_cast<uint64_t>(kTile), n0 = blockIdx.x / m_tiles * static_cast<uint64_t>(kTile);
-    const int tm = threadIdx.x & 15, tn = threadIdx.x >> 4;
-    float acc[PAIRED ? 2 : 1][4][4] = {};
-    auto load = [&](const Operand& o, uint64_t i0, uint64_t limit, uint64_t k0, float (*dst)[kTile + 4]) {
-        for (int e = threadIdx.x; e < kTile * kStep; e += 256) {
-            const int i = o.col == 1 ? e / kStep : e % kTile, k = o.col == 1 ? e % kStep : e / kTile;
-            const bool in = i0 + i < limit && k0 + k < p.k;
-            dst[k][i] = in ? element(static_cast<const T*>(o.data) + (i0 + i) * o.row + (k0 + k) * o.col) : 0.0f;
-        }
-    };
-    for (int term = 0; term < (PAIRED ? 1 : p.terms); ++term)
-        for (uint64_t k0 = 0; k0 < p.k; k0 += kStep) {
-            load(p.a[term], m0, p.m, k0, sa);
-            load(p.b[term], n0, p.n, k0, sb[0]);
-            if constexpr (PAIRED) load(p.b[1], n0, p.n, k0, sb[1]);
-            __syncthreads();
-            for (int k = 0; k < kStep; ++k)
-                for (int i = 0; i < 4; ++i)
-                    for (int j = 0; j < 4; ++j)
-                        for (int s = 0; s < (PAIRED ? 2 : 1); ++s)
-                            acc[s][i][j] = __fmaf_rn(sa[k][tm * 4 + i], sb[s][k][tn * 4 + j], acc[s][i][j]);
-            __syncthreads();
-        }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const uint64_t m = m0 + tm * 4 + i, n = n0 + tn * 4 + j;
-            if (m >= p.m || n >= p.n) continue;
-            float v = acc[0][i][j];
-            if constexpr (PAIRED) {
-                float u = acc[1][i][j];
-                if (p.a_scale) {
-                    v *= p.a_scale[m] * p.b_scale[0][n];
-                    u *= p.a_scale[m] * p.b_scale[1][n];
-                }
-                if (p.out[1]) {
-                    p.out[1][m * p.ldo[1] + n] = to_bf16(v);
-                    p.out[2][m * p.ldo[2] + n] = to_bf16(u);
-                }
-                v = activate(p.activation, v) * u;
-            }
-            p.out[0][m * p.ldo[0] + n] = to_bf16(v);
-        }
-}
 
 struct GateArgs {
     const uint16_t *dh, *gate, *up;
@@ -133,9 +61,6 @@ __global__ void __launch_bounds__(256) gate_backward_kernel(const __grid_constan
         reinterpret_cast<uint4*>(a.dup + this_row * a.lddu)[this_v] = make_uint4(du[0], du[1], du[2], du[3]);
     }
 }
-
-inline Operand by_row(const collage_matrix_t* m) { return {m->data, m->ld, 1}; }        // i = row of the matrix
-inline Operand by_col(const collage_matrix_t* m) { return {m->data, 1, m->ld}; }        // i = column
 
 // ---- tensor-map path -------------------------------------------------------------------------------------------------
 
@@ -326,11 +251,63 @@ static collage_status_t tiles_dw(const collage_matrix_t* dgate, const collage_ma
 
 // ---- any alignment ---------------------------------------------------------------------------------------------------
 
-template <typename T, bool PAIRED>
-static collage_status_t launch_product(const ProductArgs& p, cudaStream_t s) {
+static Operand by_row(const collage_matrix_t* m) { return {m->data, m->ld, 1}; }        // i = row of the matrix
+static Operand by_col(const collage_matrix_t* m) { return {m->data, 1, m->ld}; }        // i = column
+
+// p's operands, outputs, scales, m, n, k and terms are set.
+template <bool E4M3, bool GATED>
+static collage_status_t launch_any(AnyArgs& p, int sm_count, cudaStream_t s) {
     if (p.m == 0 || p.n == 0) return COLLAGE_OK;
-    const uint64_t m_tiles = (p.m + kTile - 1) / kTile, n_tiles = (p.n + kTile - 1) / kTile;
-    return launch<&product_any_kernel<T, PAIRED>>(m_tiles * n_tiles, 256, 1, 0, s, p, static_cast<uint32_t>(m_tiles));
+    const uint32_t nt = p.n <= 32 ? 32 : 128, k = E4M3 ? 128 : 64;
+    p.token_tiles = (p.n + nt - 1) / nt;
+    p.k_blocks = (p.k + k - 1) / k;
+    const uint64_t tiles = static_cast<uint64_t>(p.token_tiles) * ((p.m + (GATED ? 63ull : 127ull)) / (GATED ? 64 : 128));
+    p.split = 1;
+    while (p.split < most_split(p.terms * p.k_blocks) && tiles * p.split < static_cast<uint64_t>(sm_count)) p.split *= 2;
+    return nt == 32 ? launch<&any_kernel<E4M3, GATED, 32>>(tiles * p.split, kAnyThreads, p.split, any_smem<32>(), s, p)
+                    : launch<&any_kernel<E4M3, GATED, 128>>(tiles * p.split, kAnyThreads, p.split, any_smem<128>(), s, p);
+}
+
+template <bool E4M3>
+static collage_status_t any_forward(const collage_matrix_t* x, const collage_matrix_t* wg, const collage_matrix_t* wu, const collage_matrix_t* h,
+                                    const collage_matrix_t* gate, const collage_matrix_t* up, const float* const (&scales)[3], int activation,
+                                    int sm_count, cudaStream_t s) {
+    AnyArgs p = {};
+    p.a[0] = by_row(wg);
+    p.a[1] = by_row(wu);
+    p.b[0] = by_row(x);
+    const collage_matrix_t* outs[3] = {h, gate, up};
+    for (int i = 0; i < 3 && outs[i]; ++i) {
+        p.out[i] = static_cast<uint16_t*>(outs[i]->data);
+        p.ldo[i] = outs[i]->ld;
+    }
+    p.token_scale = scales[0];
+    p.row_scale[0] = scales[1];
+    p.row_scale[1] = scales[2];
+    p.m = static_cast<uint32_t>(h->cols);
+    p.n = static_cast<uint32_t>(h->rows);
+    p.k = static_cast<uint32_t>(x->cols);
+    p.terms = 1;
+    p.keep = gate != nullptr;
+    p.activation = activation;
+    return launch_any<E4M3, true>(p, sm_count, s);
+}
+
+// out[t, i] = sum over terms and k of a[i, k] b[t, k]
+static collage_status_t any_product(const Operand (&a)[2], const Operand (&b)[2], uint32_t terms, uint64_t k, const collage_matrix_t* out,
+                                    int sm_count, cudaStream_t s) {
+    AnyArgs p = {};
+    for (uint32_t i = 0; i < terms; ++i) {
+        p.a[i] = a[i];
+        p.b[i] = b[i];
+    }
+    p.out[0] = static_cast<uint16_t*>(out->data);
+    p.ldo[0] = out->ld;
+    p.m = static_cast<uint32_t>(out->cols);
+    p.n = static_cast<uint32_t>(out->rows);
+    p.k = static_cast<uint32_t>(k);
+    p.terms = terms;
+    return launch_any<false, false>(p, sm_count, s);
 }
 
 static bool known(collage_activation_t a) { return a == COLLAGE_ACT_SILU || a == COLLAGE_ACT_GELU_TANH; }
@@ -381,23 +358,7 @@ collage_status_t collage_gated_ffn(const collage_matrix_t* x, const collage_matr
     bool maps = true;
     for (const collage_matrix_t* m : all) maps = maps && (!m || mappable(m, 2));
     if (maps) return tiles_forward<false>(x, w_gate, w_up, h, gate, up, {nullptr, nullptr, nullptr}, activation, dev.sm_count, s);
-    ProductArgs p = {};
-    p.a[0] = by_row(x);
-    p.b[0] = by_row(w_gate);
-    p.b[1] = by_row(w_up);
-    p.out[0] = static_cast<uint16_t*>(h->data);
-    p.ldo[0] = h->ld;
-    if (gate) {
-        p.out[1] = static_cast<uint16_t*>(gate->data);
-        p.out[2] = static_cast<uint16_t*>(up->data);
-        p.ldo[1] = gate->ld;
-        p.ldo[2] = up->ld;
-    }
-    p.m = x->rows;
-    p.n = w_gate->rows;
-    p.k = x->cols;
-    p.activation = activation;
-    return launch_product<uint16_t, true>(p, s);
+    return any_forward<false>(x, w_gate, w_up, h, gate, up, {nullptr, nullptr, nullptr}, activation, dev.sm_count, s);
 }
 
 collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float* x_scale, const collage_matrix_t* w_gate8,
@@ -426,20 +387,7 @@ collage_status_t collage_gated_ffn_e4m3(const collage_matrix_t* x8, const float*
     if (x8->cols == 0) return clear_matrix(h, 2, s);
     if (mappable(x8, 1) && mappable(w_gate8, 1) && mappable(w_up8, 1) && mappable(h, 2))
         return tiles_forward<true>(x8, w_gate8, w_up8, h, nullptr, nullptr, {x_scale, w_gate_scale, w_up_scale}, activation, dev.sm_count, s);
-    ProductArgs p = {};
-    p.a[0] = by_row(x8);
-    p.b[0] = by_row(w_gate8);
-    p.b[1] = by_row(w_up8);
-    p.a_scale = x_scale;
-    p.b_scale[0] = w_gate_scale;
-    p.b_scale[1] = w_up_scale;
-    p.out[0] = static_cast<uint16_t*>(h->data);
-    p.ldo[0] = h->ld;
-    p.m = x8->rows;
-    p.n = w_gate8->rows;
-    p.k = x8->cols;
-    p.activation = activation;
-    return launch_product<uint8_t, true>(p, s);
+    return any_forward<true>(x8, w_gate8, w_up8, h, nullptr, nullptr, {x_scale, w_gate_scale, w_up_scale}, activation, dev.sm_count, s);
 }
 
 collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const collage_matrix_t* x, const collage_matrix_t* w_gate,
@@ -503,33 +451,10 @@ collage_status_t collage_gated_ffn_backward(const collage_matrix_t* dh, const co
         if ((st = tiles_dw(dgate, dup, x, dw_gate, dw_up, dev.sm_count, s)) != COLLAGE_OK) return st;
         dw_gate = nullptr;
     }
-    if (dx) {
-        ProductArgs p = {};
-        p.a[0] = by_row(dgate);
-        p.a[1] = by_row(dup);
-        p.b[0] = by_col(w_gate);
-        p.b[1] = by_col(w_up);
-        p.out[0] = static_cast<uint16_t*>(dx->data);
-        p.ldo[0] = dx->ld;
-        p.m = dx->rows;
-        p.n = dx->cols;
-        p.k = dh->cols;
-        p.terms = 2;
-        if ((st = launch_product<uint16_t, false>(p, s)) != COLLAGE_OK) return st;
-    }
-    for (int half = 0; half < 2 && dw_gate; ++half) {
-        const collage_matrix_t* out = half ? dw_up : dw_gate;
-        ProductArgs p = {};
-        p.a[0] = by_col(half ? dup : dgate);
-        p.b[0] = by_col(x);
-        p.out[0] = static_cast<uint16_t*>(out->data);
-        p.ldo[0] = out->ld;
-        p.m = out->rows;
-        p.n = out->cols;
-        p.k = dh->rows;
-        p.terms = 1;
-        if ((st = launch_product<uint16_t, false>(p, s)) != COLLAGE_OK) return st;
-    }
+    if (dx && dx->cols)
+        if ((st = any_product({by_col(w_gate), by_col(w_up)}, {by_row(dgate), by_row(dup)}, 2, dh->cols, dx, dev.sm_count, s)) != COLLAGE_OK) return st;
+    for (int half = 0; half < 2 && dw_gate && x->cols; ++half)
+        if ((st = any_product({by_col(x), {}}, {by_col(half ? dup : dgate), {}}, 1, dh->rows, half ? dw_up : dw_gate, dev.sm_count, s)) != COLLAGE_OK) return st;
     return COLLAGE_OK;
 }
 

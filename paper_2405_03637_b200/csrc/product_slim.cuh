@@ -31,10 +31,104 @@ __host__ __device__ constexpr int slim_stages(bool alone) {
 template <int NT>
 constexpr int slim_smem(bool alone) { return 1024 + (slim_stages<NT>(alone) > kMaxSlimStages ? kMaxSlimStages : slim_stages<NT>(alone)) * slim_stage_bytes<NT>(); }
 
+// The end of a slim tile, by all threads of the block: its accumulators to shared memory, the cluster's parts joined in the
+// order of K, the results stored.  VECTORS: whole vectors fit the outputs.
+template <bool E4M3, bool GATED, int NT, bool VECTORS, typename Args>
+__device__ __forceinline__ void finish_slim_tile(const Args& p, uint8_t* smem, uint32_t tmem, uint32_t rank, uint32_t t0, uint32_t i0) {
+    __syncthreads();                                 // the sums are complete and the stages free
+    umma::fence_after();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float* sums = reinterpret_cast<float*>(smem);    // [NT][128]: a token's 128 indexes
+    const uint32_t row = threadIdx.x;
+#pragma unroll 1
+    for (uint32_t c = 0; c < NT && warp < 4; c += 16) {
+        float v[16];
+        umma::tmem_load16(tmem + (warp << 21) + c, v);
+        umma::tmem_wait(v);
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) sums[(c + i) * 128 + row] = v[i];
+    }
+    umma::fence_before();
+    if (p.split > 1) umma::cluster_sync();
+    else __syncthreads();
+    umma::fence_after();
+    if (warp == 2) umma::tmem_free<1>(tmem, NT < 32 ? 32 : NT);
+
+    // Tokens over the cluster's blocks and their warps, four at a time; parts of the sum in the order of K.
+    const uint32_t tokens = min(static_cast<uint32_t>(NT), p.n - t0);
+    auto store2 = [&](uint16_t* at, uint32_t i, float a, float b) {     // indexes i and i + 1
+        if constexpr (VECTORS) {                     // m is a multiple of 8, rows begin on 16 bytes
+            *reinterpret_cast<uint32_t*>(at) = pack_bf16(a, b);
+        } else {
+            at[0] = to_bf16(a);
+            if (i + 1 < p.m) at[1] = to_bf16(b);
+        }
+    };
+    auto part = [&](uint32_t r, uint32_t t, uint32_t i) {               // four floats of block r's sums
+        float4 q;
+        if (p.split == 1) return *reinterpret_cast<const float4*>(sums + t * 128 + i);
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(umma::cluster_addr(sums + t * 128 + i, r)));
+        return q;
+    };
+    for (uint32_t first = rank * 16 + warp * 4; first < tokens && warp < 4; first += p.split * 16) {
+        float4 v[4] = {};
+        for (uint32_t r = 0; r < p.split; ++r) {
+            float4 q[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) q[e] = part(r, first + e, 4 * lane);      // NT is a multiple of 4
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) { v[e].x += q[e].x; v[e].y += q[e].y; v[e].z += q[e].z; v[e].w += q[e].w; }
+        }
+        if constexpr (GATED) {
+            // lanes 0-15 have four gates each, lanes 16-31 the ups that belong to them: the lower two of four to the lower lane
+            const bool low = lane < 16;
+            const uint32_t i = i0 + 4 * (lane & 15) + (low ? 0 : 2);
+            float2 row_g = {1.0f, 1.0f}, row_u = {1.0f, 1.0f};
+            if constexpr (E4M3)
+                if (i < p.m) {
+                    const uint32_t n = min(i + 1, p.m - 1);
+                    row_g = make_float2(p.row_scale[0][i], p.row_scale[0][n]);
+                    row_u = make_float2(p.row_scale[1][i], p.row_scale[1][n]);
+                }
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const float a = __shfl_xor_sync(0xFFFFFFFFu, low ? v[e].z : v[e].x, 16), b = __shfl_xor_sync(0xFFFFFFFFu, low ? v[e].w : v[e].y, 16);
+                float2 g = low ? make_float2(v[e].x, v[e].y) : make_float2(a, b), u = low ? make_float2(a, b) : make_float2(v[e].z, v[e].w);
+                if (first + e >= tokens || i >= p.m) continue;
+                const uint64_t token = t0 + first + e;
+                if constexpr (E4M3) {
+                    const float s = p.token_scale[token];
+                    g.x *= s * row_g.x; g.y *= s * row_g.y;
+                    u.x *= s * row_u.x; u.y *= s * row_u.y;
+                }
+                if (p.keep) {
+                    store2(p.out[1] + token * p.ldo[1] + i, i, g.x, g.y);
+                    store2(p.out[2] + token * p.ldo[2] + i, i, u.x, u.y);
+                }
+                store2(p.out[0] + token * p.ldo[0] + i, i, activate(p.activation, g.x) * u.x, activate(p.activation, g.y) * u.y);
+            }
+        } else {
+            const uint32_t i = i0 + 4 * lane;
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                if (first + e < tokens && i < p.m) {
+                    uint16_t* at = p.out[0] + (t0 + first + e) * p.ldo[0] + i;
+                    if constexpr (VECTORS) {
+                        *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16(v[e].x, v[e].y), pack_bf16(v[e].z, v[e].w));
+                    } else {
+                        store2(at, i, v[e].x, v[e].y);
+                        if (i + 2 < p.m) store2(at + 2, i + 2, v[e].z, v[e].w);
+                    }
+                }
+        }
+    }
+    if (p.split > 1) umma::cluster_sync_any();       // no block leaves while another reads its sums
+}
+
 template <bool E4M3, bool A_MN, bool GATED, int NT>
 __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constant__ SlimArgs p) {
     constexpr uint32_t kBytes = slim_stage_bytes<NT>();
-    constexpr uint32_t kK = E4M3 ? 128 : 64, kColumns = NT < 32 ? 32 : NT, kIndexes = GATED ? 64 : 128;
+    constexpr uint32_t kK = E4M3 ? 128 : 64, kIndexes = GATED ? 64 : 128;
     constexpr uint32_t kIdesc = umma::instr_desc(E4M3 ? 0 : 1, A_MN, false, 128, NT);
     static_assert(slim_stages<NT>(false) * kBytes >= NT * 512, "the tile's sums fit the stages");
     const uint32_t stages = p.stages;
@@ -42,7 +136,7 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
     __shared__ uint64_t full[kMaxSlimStages], empty[kMaxSlimStages], done;
     __shared__ uint32_t tmem_slot;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = threadIdx.x >> 5;
     const uint32_t rank = p.split > 1 ? umma::cluster_rank() : 0, tile = blockIdx.x / p.split;
     const uint32_t t0 = tile % p.token_tiles * NT, i0 = tile / p.token_tiles * kIndexes;
     const uint32_t blocks = p.terms * p.k_blocks;
@@ -57,7 +151,7 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
         pipe::mbar_init(&done, 1);
         pipe::mbar_init_fence();
     }
-    if (warp == 2) umma::tmem_alloc<1>(&tmem_slot, kColumns);
+    if (warp == 2) umma::tmem_alloc<1>(&tmem_slot, NT < 32 ? 32 : NT);
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
@@ -107,78 +201,7 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
         }
         if (ok) pipe::mbar_wait(&done, 0, 212, &g_product_fault);
     }
-    __syncthreads();                                 // the sums are complete and the stages free
-    umma::fence_after();
-    float* sums = reinterpret_cast<float*>(smem);    // [NT][128]: a token's 128 indexes
-    const uint32_t row = threadIdx.x;
-#pragma unroll 1
-    for (uint32_t c = 0; c < NT; c += 16) {
-        float v[16];
-        umma::tmem_load16(tmem + (warp << 21) + c, v);
-        umma::tmem_wait(v);
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) sums[(c + i) * 128 + row] = v[i];
-    }
-    umma::fence_before();
-    if (p.split > 1) umma::cluster_sync();
-    else __syncthreads();
-    umma::fence_after();
-    if (warp == 2) umma::tmem_free<1>(tmem, kColumns);
-
-    // Tokens over the cluster's blocks and their warps, four at a time; parts of the sum in the order of K.
-    const uint32_t tokens = min(static_cast<uint32_t>(NT), p.n - t0);
-    auto part = [&](uint32_t r, uint32_t t, uint32_t i) {               // four floats of block r's sums
-        float4 q;
-        if (p.split == 1) return *reinterpret_cast<const float4*>(sums + t * 128 + i);
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(umma::cluster_addr(sums + t * 128 + i, r)));
-        return q;
-    };
-    for (uint32_t first = rank * 16 + warp * 4; first < tokens; first += p.split * 16) {
-        float4 v[4] = {};
-        for (uint32_t r = 0; r < p.split; ++r) {
-            float4 q[4];
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) q[e] = part(r, first + e, 4 * lane);      // NT is a multiple of 4
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) { v[e].x += q[e].x; v[e].y += q[e].y; v[e].z += q[e].z; v[e].w += q[e].w; }
-        }
-        if constexpr (GATED) {
-            // lanes 0-15 have four gates each, lanes 16-31 the ups that belong to them: the lower two of four to the lower lane
-            const bool low = lane < 16;
-            const uint32_t i = i0 + 4 * (lane & 15) + (low ? 0 : 2);
-            float2 row_g = {1.0f, 1.0f}, row_u = {1.0f, 1.0f};
-            if constexpr (E4M3)
-                if (i < p.m) {
-                    row_g = make_float2(p.row_scale[0][i], p.row_scale[0][i + 1]);
-                    row_u = make_float2(p.row_scale[1][i], p.row_scale[1][i + 1]);
-                }
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-                const float a = __shfl_xor_sync(0xFFFFFFFFu, low ? v[e].z : v[e].x, 16), b = __shfl_xor_sync(0xFFFFFFFFu, low ? v[e].w : v[e].y, 16);
-                float2 g = low ? make_float2(v[e].x, v[e].y) : make_float2(a, b), u = low ? make_float2(a, b) : make_float2(v[e].z, v[e].w);
-                if (first + e >= tokens || i >= p.m) continue;                          // m is a multiple of 8
-                const uint64_t token = t0 + first + e;
-                if constexpr (E4M3) {
-                    const float s = p.token_scale[token];
-                    g.x *= s * row_g.x; g.y *= s * row_g.y;
-                    u.x *= s * row_u.x; u.y *= s * row_u.y;
-                }
-                if (p.keep) {
-                    *reinterpret_cast<uint32_t*>(p.out[1] + token * p.ldo[1] + i) = pack_bf16(g.x, g.y);
-                    *reinterpret_cast<uint32_t*>(p.out[2] + token * p.ldo[2] + i) = pack_bf16(u.x, u.y);
-                }
-                *reinterpret_cast<uint32_t*>(p.out[0] + token * p.ldo[0] + i) =
-                    pack_bf16(activate(p.activation, g.x) * u.x, activate(p.activation, g.y) * u.y);
-            }
-        } else {
-            const uint32_t i = i0 + 4 * lane;
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e)
-                if (first + e < tokens && i < p.m)
-                    *reinterpret_cast<uint2*>(p.out[0] + (t0 + first + e) * p.ldo[0] + i) = make_uint2(pack_bf16(v[e].x, v[e].y), pack_bf16(v[e].z, v[e].w));
-        }
-    }
-    if (p.split > 1) umma::cluster_sync_any();       // no block leaves while another reads its sums
+    finish_slim_tile<E4M3, GATED, NT, true>(p, smem, tmem, rank, t0, i0);
 }
 
 }  // namespace ops
