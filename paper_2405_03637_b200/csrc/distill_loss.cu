@@ -27,11 +27,8 @@ struct DistillArgs {
     float inv_t, t;
 };
 
-#ifndef DT
-#define DT 256
-#endif
-constexpr int kDistillThreads = DT, kStagedThreads = 192;
-constexpr uint32_t kSeenWords = 512;           // two bitmaps over the indexes of a row, modulo 2^14
+constexpr int kDistillThreads = 256;
+constexpr uint32_t kSeenWords = 256;           // bitmaps over the indexes of a row, modulo 2^13
 constexpr uint32_t kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 // A stored lse of this size or more is rounded too coarsely to give q to 2^-17 (an infinite one to give it at all): the
@@ -171,6 +168,20 @@ struct DistillShared {
     int any_there;
     float log_psum, most;
 };
+
+// Waits until at most `groups` of this thread's copy groups are under way (or 7, where more may be).
+__device__ __forceinline__ void wait_pending(uint32_t groups) {
+    switch (groups) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        case 6: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 7;" ::: "memory"); break;
+    }
+}
 
 // A row as 16-byte vectors of its memory: vector v holds elements v kN - off ... of the row, those outside it do not exist.
 template <typename T>
@@ -458,43 +469,56 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
 // Loss and gradient of rows that fit the shared memory of a cluster: each block keeps its slice of a row between the two
 // passes over it and walks over rows.  A thread owns the same places of the slice for every row: as soon as it has made
 // the gradient of a place it sends for the next row's vector, so loads, exponentials and stores of two rows overlap.
+// One more warp has the teacher's entries: their softmax while the others sum, the student's logits at them before the
+// places are overwritten, then the loss, and one row later, when the dense gradient is surely written, the entries over it.
 struct StagedShared {
-    float2 warp[kStagedThreads / 32];
-    float2 part[2][kMaxCluster];          // (maximum, sum) of each block of the cluster; two rows' worth
+    float2 warp[8];
+    float2 part[2][kMaxCluster];          // (maximum, sum) of each block of the cluster; two rows' worth, as all below
     float loss[2][kMaxCluster];
-    uint32_t seen[kSeenWords], again[kSeenWords];
-    int any_there;
-    float log_psum;
+    uint32_t seen[2][kSeenWords], again[2][kSeenWords];
+    int any_there[2];
+    struct {                              // what is still to be done for the row before
+        void* line;
+        unsigned long long row;
+        float m, shift, log2sum, g;
+        uint32_t off, end;
+        int small, live;
+    } last;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const __grid_constant__ DistillArgs a, uint64_t rows) {
+template <typename T, int kStagedThreads, int BLOCKS>
+__global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_kernel(const __grid_constant__ DistillArgs a, uint64_t rows) {
     using V = Vec<T>;
     constexpr uint32_t kN = V::kN;
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ StagedShared sh;
-    after_previous();
     uint4* stage = reinterpret_cast<uint4*>(dynamic);                                     // [slice]
     int64_t* raw_index = reinterpret_cast<int64_t*>(dynamic + 16ull * a.slice);           // [k], 4 or 8 bytes each: as it came
     float* raw_top = reinterpret_cast<float*>(raw_index + a.k);                           // [k]
-    float* tp = raw_top + a.k;                                                            // [k] teacher's p
-    float* tz = tp + a.k;                                                                 // [k] student's logit
-    int* ti = reinterpret_cast<int*>(tz + a.k);                                           // [k] index, -1 = absent
+    float* all_p = raw_top + a.k;                                                         // [2][k] teacher's p
+    float* all_z = all_p + 2 * a.k;                                                       // [2][k] student's logit
+    int* all_i = reinterpret_cast<int*>(all_z + 2 * a.k);                                 // [2][k] index, -1 = absent
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool teacher = threadIdx.x >= kStagedThreads;
     const uint32_t rank = a.cluster > 1 ? umma::cluster_rank() : 0, first = rank * a.slice;
     const uint64_t step = gridDim.x / a.cluster;
     const float c = a.inv_t * kLog2e;
     const uint32_t stage_addr = umma::smem_addr(stage);
+    after_previous();
 
     auto logits_of = [&](uint64_t row) { return RowVectors<T>(const_cast<T*>(static_cast<const T*>(a.logits)) + row * a.ldz, a.vocab); };
     auto send_for = [&](const RowVectors<T>& z, uint32_t v) {
         if (z.inside(v))
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(umma::smem_addr(stage + v - first)), "l"(z.base + v) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(stage_addr + 16 * (v - first)), "l"(z.base + v) : "memory");
         else
             stage[v - first] = z.edge(v);
     };
+    // A thread's places are taken in batches; its copies are counted by batch too, so that the first of a row can be used
+    // while the last are under way.
+    constexpr uint32_t kAhead = 4, kBatch = kAhead * kStagedThreads;
+    auto batches = [&](uint32_t end) { return (end - min(first, end) + kBatch - 1) / kBatch; };
     auto send_for_teacher = [&](uint64_t row) {
-        for (uint32_t k = threadIdx.x; k < a.k; k += kStagedThreads) {
+        for (uint32_t k = lane; k < a.k; k += 32) {
             const uint64_t at = row * a.ldi + k;
             if (a.index_bytes == 8)
                 asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(umma::smem_addr(raw_index + k)), "l"(static_cast<const int64_t*>(a.top_index) + at) : "memory");
@@ -503,18 +527,53 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(umma::smem_addr(raw_top + k)), "l"(a.top_logits + row * a.ldt + k) : "memory");
         }
     };
-    auto send_for_row = [&](uint64_t row) {
-        const RowVectors<T> z = logits_of(row);
-        const uint32_t end = min(first + a.slice, z.count());
-        for (uint32_t v = first + threadIdx.x; v < end; v += kStagedThreads) send_for(z, v);
-        send_for_teacher(row);
-    };
 
     uint64_t row = blockIdx.x / a.cluster;
     float g = row < rows ? a.row_scale[row] : 0.0f;
-    uint32_t turn = 0;                          // rows with an exchange so far
     if (a.cluster > 1) umma::cluster_sync_any();    // all blocks run before one writes into another
-    if (g != 0.0f) send_for_row(row);
+    if (g != 0.0f) {
+        if (teacher) {
+            send_for_teacher(row);
+        } else {
+            const RowVectors<T> z = logits_of(row);
+            const uint32_t end = min(first + a.slice, z.count());
+            for (uint32_t n = 0; n < batches(end); ++n) {
+                for (uint32_t v = first + n * kBatch + threadIdx.x; v < min(first + (n + 1) * kBatch, end); v += kStagedThreads) send_for(z, v);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+        }
+    }
+    uint32_t turn = 0;                          // rows with a distribution so far
+    auto inside = [&](int i, uint32_t off, uint32_t end) {              // is entry i in this block's slice?
+        const uint32_t v = (static_cast<uint32_t>(i) + off) / kN;
+        return i >= 0 && v >= first && v < end;
+    };
+    auto finish_last = [&](uint32_t b) {        // the teacher's warp, for the row before; b: its buffers
+        const auto& last = sh.last;
+        if (a.cluster > 1 && rank == 0 && lane == 0) {
+            float loss = 0.0f;
+            for (uint32_t r = 0; r < a.cluster; ++r) loss += sh.loss[b][r];
+            a.loss[last.row] = last.live ? last.g * (loss * a.t * a.t) : 0.0f;
+        }
+        if (!last.live) return;
+        const float *tp = all_p + b * a.k, *tz = all_z + b * a.k;
+        const int* ti = all_i + b * a.k;
+        for (uint32_t k = lane; k < a.k; k += 32) {
+            const int i = ti[k];
+            if (!inside(i, last.off, last.end)) continue;
+            float p = tp[k];
+            // an index that appears more than once: all its lanes add up the same sum.  (Indexes that share a bit are searched
+            // too, and found alone.)
+            if (sh.again[b][(static_cast<uint32_t>(i) >> 5) % kSeenWords] >> (i & 31) & 1) {
+                p = 0.0f;
+                for (uint32_t o = 0; o < a.k; ++o)
+                    if (ti[o] == i) p += tp[o];
+            }
+            const float x = last.small ? __fmaf_rn(tz[k], c, last.shift) : (tz[k] - last.m) * c - last.log2sum;
+            static_cast<T*>(last.line)[i] = V::rounded(last.g * a.t * (fast_exp2(x) - p));
+        }
+    };
+
     for (; row < rows; row += step) {
         const RowVectors<T> z = logits_of(row), dz(static_cast<T*>(a.dlogits) + row * a.ldd, a.vocab);
         const uint32_t end = min(first + a.slice, z.count());
@@ -523,16 +582,18 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
         const RowVectors<T> zn = logits_of(more ? row + step : row);
         const uint32_t end_next = g_next != 0.0f ? min(first + a.slice, zn.count()) : 0;
 
+        const uint32_t next_batches = batches(end_next);
         // Gradients of this thread's places, and the next row into them.  `value(f)` puts gradients in the logits' place.
-        constexpr uint32_t kAhead = 4, kBatch = kAhead * kStagedThreads;
         const bool alike = z.off == dz.off;
         // batches of places that are whole vectors of both rows need no further checks
         const uint32_t plain_begin = max(z.whole_begin(), end_next ? zn.whole_begin() : 0);
         const uint32_t plain_end = alike ? min(min(z.whole_end(), end), end_next ? min(zn.whole_end(), end_next) : end) : 0;
         auto write_row = [&](bool staged, auto&& value) {
-            const uint32_t last = max(end, end_next);
+            const uint32_t stop = max(end, end_next);
+            uint32_t n_batch = 0;
 #pragma unroll 1
-            for (uint32_t v0 = first + threadIdx.x; v0 < last; v0 += kBatch) {
+            for (uint32_t begin = first; begin < stop; begin += kBatch, ++n_batch) {
+                const uint32_t v0 = begin + threadIdx.x;
                 if (v0 >= plain_begin && v0 + (kBatch - kStagedThreads) < plain_end) {
                     uint64_t f[kAhead][V::kPairs];
                     if (staged) {
@@ -552,7 +613,7 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
                     for (uint32_t n = 0; n < kAhead; ++n) dz.base[v0 + n * kStagedThreads] = V::pack(f[n]);
                 } else {
 #pragma unroll 1
-                    for (uint32_t v = v0; v < min(v0 + kBatch, last); v += kStagedThreads) {
+                    for (uint32_t v = v0; v < min(v0 + kBatch, stop); v += kStagedThreads) {
                         uint64_t f[V::kPairs];
                         V::unpack(stage[v - first], f);
                         value(f);
@@ -570,25 +631,31 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
                         }
                     }
                 }
+                if (n_batch < next_batches) asm volatile("cp.async.commit_group;" ::: "memory");
             }
-            if (end_next) send_for_teacher(row + step);
         };
         auto zero = [](uint64_t (&f)[V::kPairs]) {
 #pragma unroll
             for (uint32_t i = 0; i < V::kPairs; ++i) f[i] = 0;
         };
         if (g == 0.0f) {                        // weighs nothing: not read
-            write_row(false, zero);
-            if (rank == 0 && threadIdx.x == 0) a.loss[row] = 0.0f;
+            if (!teacher) {
+                write_row(false, zero);
+            } else {
+                if (end_next) send_for_teacher(row + step);
+                if (rank == 0 && lane == 0) a.loss[row] = 0.0f;
+            }
             g = g_next;
             continue;
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        __syncthreads();                        // the row and the teacher's entries are there; the last row's are done with
-
-        for (uint32_t i = threadIdx.x; i < kSeenWords; i += kStagedThreads) sh.seen[i] = sh.again[i] = 0;
-        if (warp == 0) {                        // the teacher's p
-            float most = -INFINITY;
+        const uint32_t b = turn & 1;
+        float *tp = all_p + b * a.k, *tz = all_z + b * a.k;
+        int* ti = all_i + b * a.k;
+        float log_psum = 0.0f, m = -INFINITY, sum = 0.0f;
+        if (teacher) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+            float most = -INFINITY, psum = 0.0f;
             bool bad = false;
             for (uint32_t k = lane; k < a.k; k += 32) {
                 const int64_t i = a.index_bytes == 8 ? raw_index[k] : reinterpret_cast<const int32_t*>(raw_index)[k];
@@ -601,93 +668,102 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
             }
             most = warp_max(most);
             const bool any_there = __any_sync(0xFFFFFFFFu, bad) || most > -INFINITY;
-            float psum = 0.0f;
             for (uint32_t k = lane; k < a.k; k += 32) psum += expf(tp[k] - most);
             psum = warp_sum(psum);
+            log_psum = logf(psum);
             for (uint32_t k = lane; k < a.k; k += 32) {
                 const float shifted = tp[k] - most;
                 tp[k] = expf(shifted) / psum;
                 tz[k] = shifted;                // until the student's logit takes its place
             }
-            if (lane == 0) {
-                sh.any_there = any_there;
-                sh.log_psum = logf(psum);
-            }
-        }
-        // maximum and sum of this thread's vectors, joined over the warp, the block and the cluster
-        auto each_place = [&](auto&& f) {
-            uint32_t v = threadIdx.x;
-            for (; v + (kBatch - kStagedThreads) < end - first; v += kBatch) {
-                uint4 q[kAhead];
+            if (lane == 0) sh.any_there[b] = any_there;
+            for (uint32_t i = lane; i < kSeenWords; i += 32) sh.seen[b][i] = sh.again[b][i] = 0;
+        } else {
+            // Maximum (batch by batch as they come: a thread reads what it has sent for itself), then sum of this thread's vectors.
+            const uint32_t mine = batches(end);
+            auto each_place = [&](bool wait, auto&& f) {
+#pragma unroll 1
+                for (uint32_t n = 0; n < mine; ++n) {
+                    if (wait) wait_pending(mine - 1 - n);
+                    const uint32_t v0 = n * kBatch + threadIdx.x;
+                    if ((n + 1) * kBatch <= end - first) {
+                        uint4 q[kAhead];
 #pragma unroll
-                for (uint32_t n = 0; n < kAhead; ++n) q[n] = stage[v + n * kStagedThreads];
+                        for (uint32_t i = 0; i < kAhead; ++i) q[i] = stage[v0 + i * kStagedThreads];
 #pragma unroll
-                for (uint32_t n = 0; n < kAhead; ++n) f(q[n], n);
-            }
-            for (; v < end - first; v += kStagedThreads) f(stage[v], 0);
-        };
-        float m = -INFINITY;
-        uint64_t total = 0;
-        if (first < end) {
+                        for (uint32_t i = 0; i < kAhead; ++i) f(q[i], i);
+                    } else {
+#pragma unroll
+                        for (uint32_t i = 0; i < kAhead; ++i)
+                            if (v0 + i * kStagedThreads < end - first) f(stage[v0 + i * kStagedThreads], i);
+                    }
+                }
+            };
             typename V::Most largest[2] = {V::lowest(), V::lowest()};
-            each_place([&](const uint4& q, uint32_t n) { largest[n & 1] = V::most(largest[n & 1], q); });
+            each_place(true, [&](const uint4& q, uint32_t i) { largest[i & 1] = V::most(largest[i & 1], q); });
             m = fmaxf(V::most_value(largest[0]), V::most_value(largest[1]));
-            uint64_t part[2] = {0, 0};
+            uint64_t total[2] = {0, 0};
             if (small_shift(m, c))
-                each_place([&](const uint4& q, uint32_t n) { add_exps<T, true>(q, m, c, part[n & 1]); });
+                each_place(false, [&](const uint4& q, uint32_t i) { add_exps<T, true>(q, m, c, total[i & 1]); });
             else
-                each_place([&](const uint4& q, uint32_t n) { add_exps<T, false>(q, m, c, part[n & 1]); });
-            total = add_pair(part[0], part[1]);
+                each_place(false, [&](const uint4& q, uint32_t i) { add_exps<T, false>(q, m, c, total[i & 1]); });
+            const float2 sums = floats_of(add_pair(total[0], total[1]));
+            sum = sums.x + sums.y;
+            const float most = warp_max(m);
+            sum = warp_sum(rescaled(sum, m, most, c));
+            if (lane == 0) sh.warp[warp] = make_float2(most, sum);
         }
-        const float2 sums = floats_of(total);
-        float most = warp_max(m), sum = warp_sum(rescaled(sums.x + sums.y, m, most, c));
-        if (lane == 0) sh.warp[warp] = make_float2(most, sum);
-        __syncthreads();
+        __syncthreads();                        // all sums, the whole slice and the teacher's p are there; the last row's gradient is written
         const float2 w = lane < kStagedThreads / 32 ? sh.warp[lane] : make_float2(-INFINITY, 0.0f);
         m = warp_max(w.x);
         sum = warp_sum(rescaled(w.y, w.x, m, c));
         if (a.cluster > 1) {
             if (threadIdx.x < a.cluster) {
-                const uint32_t to = umma::cluster_addr(&sh.part[turn & 1][rank], threadIdx.x);
+                const uint32_t to = umma::cluster_addr(&sh.part[b][rank], threadIdx.x);
                 asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(sum) : "memory");
             }
             umma::cluster_sync_any();
-            const float2 r = lane < a.cluster ? sh.part[turn & 1][lane] : make_float2(-INFINITY, 0.0f);
+            const float2 r = lane < a.cluster ? sh.part[b][lane] : make_float2(-INFINITY, 0.0f);
             m = warp_max(r.x);
             sum = warp_sum(rescaled(r.y, r.x, m, c));
         }
         if (m == -INFINITY) sum = NAN;          // a row without any number in it has no distribution
-        const float logsum = logf(sum), log2sum = log2f(sum), shift = -m * c - log2sum;
-        const bool small = fabsf(m * c) < kLargeShift, live = sh.any_there;
-        auto q_of = [&](float v) { return fast_exp2(small ? __fmaf_rn(v, c, shift) : (v - m) * c - log2sum); };
-        auto mine = [&](int i) {
-            const uint32_t v = (static_cast<uint32_t>(i) + z.off) / kN;
-            return i >= 0 && v >= first && v < end;
-        };
-        if (warp == 0) {                        // entries in this block's slice: the student's logit, and their part of the loss
-            float loss = 0.0f;
+        const float log2sum = log2f(sum), shift = -m * c - log2sum;
+        const bool small = fabsf(m * c) < kLargeShift, live = sh.any_there[b];
+        float loss = 0.0f;
+        if (teacher) {                          // the student's logits at the entries in this block's slice, and their part of the loss
+            const float logsum = logf(sum);
             for (uint32_t k = lane; k < a.k; k += 32) {
                 const int i = ti[k];
-                if (!mine(i)) continue;
-                const float v = V::value(reinterpret_cast<const T*>(stage)[static_cast<uint32_t>(i) + z.off - first * kN]);
-                const float p = tp[k];
-                if (!(p == 0.0f)) loss = __fmaf_rn(p, tz[k] - sh.log_psum - ((v - m) * a.inv_t - logsum), loss);
+                if (!inside(i, z.off, end)) continue;
+                const float v = V::value(reinterpret_cast<const T*>(stage)[static_cast<uint32_t>(i) + z.off - first * kN]), p = tp[k];
+                if (!(p == 0.0f)) loss = __fmaf_rn(p, tz[k] - log_psum - ((v - m) * a.inv_t - logsum), loss);
                 tz[k] = v;
-                const uint32_t bit = 1u << (i & 31), word = (static_cast<uint32_t>(i) >> 5) % kSeenWords;
-                if (atomicOr(&sh.seen[word], bit) & bit) atomicOr(&sh.again[word], bit);
             }
+        }
+        __syncthreads();                        // the slice may be overwritten
+        const float gt = g * a.t;
+        if (teacher) {
+            if (turn > 0) finish_last(b ^ 1);
             loss = warp_sum(loss);
             if (lane == 0) {
                 if (a.cluster > 1)
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(umma::cluster_addr(&sh.loss[turn & 1][rank], 0)), "f"(loss) : "memory");
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(umma::cluster_addr(&sh.loss[b][rank], 0)), "f"(loss) : "memory");
                 else
                     a.loss[row] = live ? g * (loss * a.t * a.t) : 0.0f;
             }
-        }
-        __syncthreads();                        // the entries' logits are taken: the slice may be overwritten
-        if (a.cluster > 1) umma::cluster_arrive_all();
-        const float gt = g * a.t;
-        if (!live) {                            // nothing to learn from: zeros whatever the logits are
+            for (uint32_t k = lane; k < a.k; k += 32) {
+                const int i = ti[k];
+                if (!inside(i, z.off, end)) continue;
+                const uint32_t bit = 1u << (i & 31), word = (static_cast<uint32_t>(i) >> 5) % kSeenWords;
+                if (atomicOr(&sh.seen[b][word], bit) & bit) atomicOr(&sh.again[b][word], bit);
+            }
+            __syncwarp();
+            if (end_next) send_for_teacher(row + step);
+            __syncwarp();
+            if (lane == 0) sh.last = {dz.row, row, m, shift, log2sum, g, z.off, end, small, live};
+            __syncwarp();
+        } else if (!live) {                     // nothing to learn from: zeros whatever the logits are
             write_row(false, zero);
         } else if (small) {
             const uint64_t c2 = pair_of(c, c), s2 = pair_of(shift, shift), g2 = pair_of(gt, gt);
@@ -703,36 +779,31 @@ __global__ void __launch_bounds__(kStagedThreads, 3) distill_staged_kernel(const
 #pragma unroll
                 for (uint32_t i = 0; i < V::kPairs; ++i) {
                     const float2 x = floats_of(f[i]);
-                    f[i] = pair_of(gt * q_of(x.x), gt * q_of(x.y));
+                    f[i] = pair_of(gt * fast_exp2((x.x - m) * c - log2sum), gt * fast_exp2((x.y - m) * c - log2sum));
                 }
             });
-        }
-        if (a.cluster > 1) {
-            umma::cluster_wait_all();
-            if (rank == 0 && threadIdx.x == 0) {
-                float loss = 0.0f;
-                for (uint32_t r = 0; r < a.cluster; ++r) loss += sh.loss[turn & 1][r];
-                a.loss[row] = live ? g * (loss * a.t * a.t) : 0.0f;
-            }
-        }
-        __syncthreads();                        // the dense part is written; now the teacher's entries over it
-        for (uint32_t k = threadIdx.x; k < a.k && live; k += kStagedThreads) {
-            const int i = ti[k];
-            if (!mine(i)) continue;
-            float p = tp[k];
-            // an index that appears more than once: all its threads add up the same sum.  (Indexes that share a bit are
-            // searched too, and found alone.)
-            if (sh.again[(static_cast<uint32_t>(i) >> 5) % kSeenWords] >> (i & 31) & 1) {
-                p = 0.0f;
-                for (uint32_t o = 0; o < a.k; ++o)
-                    if (ti[o] == i) p += tp[o];
-            }
-            dz.row[i] = V::rounded(gt * (q_of(tz[k]) - p));
         }
         g = g_next;
         ++turn;
     }
-    if (a.cluster > 1) umma::cluster_sync_any();    // no block leaves while another may still write to it
+    __syncthreads();                            // the last row's gradient is written
+    if (a.cluster > 1) umma::cluster_sync_any();    // its losses have come; no block leaves while another may still write to it
+    if (teacher && turn > 0) finish_last((turn - 1) & 1);
+}
+
+template <typename T, int THREADS, int BLOCKS>
+static collage_status_t launch_staged_as(const DistillArgs& a, uint64_t rows, int sm_count, cudaStream_t s) {
+    const size_t smem = 16ull * a.slice + 36ull * a.k;
+    const uint64_t fit = std::max<uint64_t>(1, std::min<uint64_t>(BLOCKS, kSmSmem / (smem + sizeof(StagedShared) + 1024)));
+    const uint64_t groups = std::min<uint64_t>(rows, std::max<uint64_t>(1, fit * sm_count / a.cluster));
+    return launch<&distill_staged_kernel<T, THREADS, BLOCKS>>(groups * a.cluster, THREADS + 32, a.cluster, smem, s, a, rows);
+}
+// Threads by the slice's vectors: about twenty each of the longest; short rows by smaller blocks, more of them on an SM.
+template <typename T>
+static collage_status_t launch_staged(const DistillArgs& a, uint64_t rows, int sm_count, cudaStream_t s) {
+    return a.slice <= 512    ? launch_staged_as<T, 64, 8>(a, rows, sm_count, s)
+           : a.slice <= 1536 ? launch_staged_as<T, 128, 5>(a, rows, sm_count, s)
+                             : launch_staged_as<T, 256, 3>(a, rows, sm_count, s);
 }
 
 template <int MODE>
@@ -749,16 +820,12 @@ static collage_status_t launch_distill(DistillArgs& a, uint64_t rows, collage_dt
         a.slice = slice();
     };
     if constexpr (MODE == 2) {
-        const size_t teacher = 24ull * a.k;
+        const size_t teacher = 36ull * a.k;
         // three blocks of an SM hold their slices; beyond eight of those, one block may take all of the shared memory
         while (a.cluster < kMaxCluster && 16ull * slice() + teacher > kSliceBytes) a.cluster *= 2;
         if (16ull * slice() + teacher <= kMaxSmem) {
-            spread(kStagedThreads);
-            const size_t smem = 16ull * a.slice + teacher;
-            const uint64_t fit = std::max<uint64_t>(1, std::min<uint64_t>(3, (kSmSmem - 1024) / (smem + sizeof(StagedShared) + 1024)));
-            const uint64_t groups = std::min<uint64_t>(rows, std::max<uint64_t>(1, fit * sm_count / a.cluster));
-            return bf16 ? launch<&distill_staged_kernel<uint16_t>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows)
-                        : launch<&distill_staged_kernel<float>>(groups * a.cluster, kStagedThreads, a.cluster, smem, s, a, rows);
+            spread(256);
+            return bf16 ? launch_staged<uint16_t>(a, rows, sm_count, s) : launch_staged<float>(a, rows, sm_count, s);
         }
         a.cluster = 1;
     }

@@ -120,12 +120,12 @@ static collage_status_t launch_slim_as(SlimArgs& t, uint64_t blocks, int sm_coun
 // The most parts that a sum over `blocks` blocks of K is split into: at least eight blocks each.
 static uint32_t most_split(uint32_t blocks) { return blocks >= 64 ? 8 : blocks >= 32 ? 4 : blocks >= 16 ? 2 : 1; }
 
-// Tokens of a slim tile: all of them up to 128, fewer where even with K split SMs would be left without a tile (there are
-// `weight_tiles` for each tile of tokens).  333 x 768 x 2048 forward: 10.8 us with 64 tokens, 13.3 with 128; but its dx, whose K
+// Tokens of a slim tile: all of them up to 128, fewer where even with K split a third of the SMs would be left without a tile
+// (there are `weight_tiles` for each tile of tokens).  333 x 768 x 2048 forward: 10.8 us with 64 tokens, 13.3 with 128; but its dx, whose K
 // can be split, loses by narrow tiles, which read the weights more often (160 x 4096 x 11008: 120 us against 55).
 static uint32_t slim_tokens(uint64_t tokens, uint64_t weight_tiles, uint32_t blocks, int sm_count) {
     uint32_t nt = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
-    while (nt > 32 && tokens > nt / 2 && (tokens + nt - 1) / nt * weight_tiles * most_split(blocks) < static_cast<uint64_t>(sm_count)) nt /= 2;
+    while (nt > 32 && tokens > nt / 2 && (tokens + nt - 1) / nt * weight_tiles * most_split(blocks) * 3 < 2ull * sm_count) nt /= 2;
     return nt;
 }
 
