@@ -112,7 +112,8 @@ static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) 
 
 template <bool E4M3, bool A_MN, bool GATED, int NT>
 static collage_status_t launch_slim_as(SlimArgs& t, uint64_t blocks, int sm_count, cudaStream_t s) {
-    const bool alone = blocks <= static_cast<uint64_t>(sm_count);
+    // (larger clusters of blocks that need an SM each leave SMs of a cluster's part of the GPU unused, and then take a second turn)
+    const bool alone = blocks <= static_cast<uint64_t>(sm_count) && t.split <= 2;
     t.stages = std::min(kMaxSlimStages, slim_stages<NT>(alone));
     return launch<&slim_kernel<E4M3, A_MN, GATED, NT>>(blocks, kSlimThreads, t.split, slim_smem<NT>(alone), s, t);
 }

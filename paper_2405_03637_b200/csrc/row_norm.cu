@@ -435,7 +435,9 @@ collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_m
     if (alias.clash(pairs)) return COLLAGE_ERR_ALIAS;
     DeviceInfo dev;
     if ((st = current_device(&dev)) != COLLAGE_OK) return st;
-    if (x->rows == 0 || x->cols == 0) return COLLAGE_OK;
+    if (x->rows == 0) return COLLAGE_OK;
+    if (x->cols == 0)
+        return !y8 || cudaMemsetAsync(y8_scale, 0, 4 * x->rows, static_cast<cudaStream_t>(stream)) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
     RowArgs a = {};
     a.x = static_cast<const uint16_t*>(x->data);
     a.ldx = x->ld;

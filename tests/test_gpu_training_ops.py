@@ -65,6 +65,17 @@ def test_norm_matches_definition(rows, cols, pad, shift):
     check_norm(rows, cols, pad, shift, residual=False, seed=9, out8=False)
 
 
+@pytest.mark.parametrize("rows,cols", [(300, 64), (1025, 136), (301, 520), (700, 1024), (310, 257), (400, 4096), (299, 8192), (330, 16384), (300, 20000)])
+def test_norm_and_quantise_many_rows(rows, cols):
+    check_norm(rows, cols, 0, 0, residual=True)
+    check_norm(rows, cols, 8, 0, residual=False, seed=3)
+    x, q, scale = Box(rows, cols, BF16, cols, 0, normal(5, rows, cols, std=0.02)), Box(rows, cols, E4M3), vec(rows)
+    B.quantize_rows(x.t, q.t, scale)
+    amax = x.t.float().abs().amax(1)
+    assert torch.equal(scale, amax / torch.full_like(amax, 448))
+    assert torch.equal(q.t.view(torch.uint8), (x.t.float() / scale[:, None]).to(E4M3).view(torch.uint8)) and q.untouched_outside()
+
+
 @pytest.mark.parametrize("rows,cols", [(5, 64), (3, 1000), (3, 4096), (2, 5121), (2, 40000)])
 def test_norm_in_place(rows, cols):
     check_norm(rows, cols, 0, 0, residual=True, in_place=True)
@@ -182,7 +193,7 @@ def test_quantize_rows_every_value_of_the_format_and_non_finite_rows():
 
 GATED_SHAPES = [(1, 1, 1), (1, 8, 8), (3, 5, 7), (2, 64, 64), (16, 64, 136), (5, 33, 130), (8, 1024, 200), (1, 4096, 1000), (31, 512, 96),
                 (64, 72, 1032), (100, 200, 104), (127, 96, 200), (128, 128, 128), (129, 136, 264), (200, 48, 257), (257, 768, 520),
-                (300, 72, 1032), (640, 256, 384), (1000, 136, 264)]
+                (300, 72, 1032), (640, 256, 384), (1000, 136, 264), (1300, 2008, 1000), (1537, 1800, 904)]
 GATED_LAYOUTS = [(0, 0), (8, 0), (0, 1)]
 
 
@@ -244,7 +255,7 @@ def test_gated_forward_and_backward_match_definition(tokens, width, ffn, pad, sh
     assert torch.equal(gate.t, dgate.t) and torch.equal(up.t, dup.t)
 
 
-@pytest.mark.parametrize("tokens,width,ffn", GATED_SHAPES + [(16, 256, 512), (130, 1040, 272)])
+@pytest.mark.parametrize("tokens,width,ffn", GATED_SHAPES + [(16, 256, 512), (130, 1040, 272), (1300, 272, 1040), (1793, 4096, 800)])
 @pytest.mark.parametrize("pad,shift", [(0, 0), (16, 0), (0, 1)])
 def test_gated_8_bits_matches_definition(tokens, width, ffn, pad, shift):
     def rows8(seed, rows, std):
@@ -424,7 +435,8 @@ def check_distill(z, at, top, tau, weight=None, box_args=None, what=""):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (2, 2, 2), (3, 17, 5), (5, 1000, 16), (4, 4099, 100), (3, 32000, 64), (9, 50257, 21),
-                                          (2, 65544, 8), (2, 131072, 257), (1, 200_003, 1024)])
+                                          (2, 65544, 8), (2, 131072, 257), (1, 200_003, 1024), (2, 900_001, 4), (600, 300, 7),
+                                          (1300, 1030, 33), (500, 5001, 12), (450, 17_003, 20)])
 def test_distill_matches_definition(rows, vocab, k, dtype):
     z = normal(rows + vocab, rows, vocab, std=2.0, dtype=dtype)
     at, top = teacher(1, rows, vocab, k)
@@ -570,6 +582,7 @@ def test_repeated_calls_side_streams_and_graphs_give_the_same_bits():
                 launch(torch.cuda.current_stream())
             graph.replay()
         now = bits_of(o)
+        assert B.pipeline_fault() == 0
         assert all(torch.equal(first[k], now[k]) for k in first), how
     del graph
 
