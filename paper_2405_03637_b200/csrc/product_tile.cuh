@@ -1,5 +1,14 @@
-// The tensor-core kernel behind the gated feed-forward operators: C = sum over terms of A_s B_s^T on tiles, operands
-// streamed by tensor-map copies, accumulators in tensor memory.
+// The tensor-core kernel behind the gated feed-forward operators: C = sum over terms of A_s B_s^T, many tokens.
+//
+// Two blocks of a cluster share a tile of 256 x 256 accumulators: each holds 128 rows of A and 128 of B in shared memory, and
+// the pair's first block issues the matrix instructions for both (half the operand traffic of single blocks with 128 x 256
+// tiles).  Operands come by tensor-map copies in 128-byte rows of K, six stages ahead; the accumulators of two tiles
+// alternate in tensor memory, so that eight warps store one tile while the next one is multiplied.  Blocks walk over tiles.
+//
+// What bounds it: the tensor pipe, then the GPU's power limit.  8192 x 4096 x 11008 forward takes 1.03 ms in a short run
+// (1440 TFLOP/s) and 1.10 ms in a sustained one (1340 TFLOP/s: the pipe is 87 % busy and the clock is down to 1.28 GHz; a
+// library product of the same operands sustains 1400).  With e4m3 operands the copies bound it: a stage is multiplied in 256
+// clocks, in which a pair wants 64 KiB from L2 (4095 x 4096 x 11008: 0.31 ms, the copies alone 0.21 ms).
 #pragma once
 #include "ops_common.cuh"
 #include "umma.cuh"
@@ -74,9 +83,11 @@ __device__ __forceinline__ TilePlace place_of(const TileArgs& p, uint32_t tile) 
     return {problem, g * p.group + r % rows, r / rows};
 }
 
-template <bool E4M3, bool A_MN, bool B_MN, bool GATED, int CTAS>
+// A_MN: A is stored with its rows' index contiguous (a transposed operand); B is, where the kernel is not GATED.
+template <bool E4M3, bool A_MN, bool GATED>
 __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ TileArgs p) {
-    constexpr uint32_t kN = 128 * CTAS;                       // accumulator columns
+    constexpr bool B_MN = !GATED;
+    constexpr uint32_t CTAS = 2, kN = 128 * CTAS;             // blocks of a tile, accumulator columns
     constexpr uint32_t kOut = GATED ? kN / 2 : kN;            // output columns of a tile
     constexpr uint32_t kK = E4M3 ? 128 : 64;                  // K elements in 128 bytes
     constexpr uint32_t kIdesc = umma::instr_desc(E4M3 ? 0 : 1, A_MN, B_MN, 128 * CTAS, kN);
@@ -85,7 +96,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     uint8_t* staging = smem + kStages * kStageBytes;
     TileBarriers* bars = reinterpret_cast<TileBarriers*>(staging + kStoreWarps * kUnits * kUnitBytes);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CTAS == 2 ? umma::cluster_rank() : 0;
+    const uint32_t rank = umma::cluster_rank();
     const uint32_t tiles = p.problems * p.m_tiles * p.n_tiles, first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
     const uint32_t blocks = p.terms * p.k_blocks;
 
@@ -107,13 +118,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     if (warp == 2) umma::tmem_alloc<CTAS>(&bars->tmem, 2 * kN);
     umma::fence_before();
     __syncthreads();
-    if constexpr (CTAS == 2) umma::cluster_sync();            // the other block's barriers exist
+    umma::cluster_sync();                                     // the other block's barriers exist
     umma::fence_after();
     after_previous();
     const uint32_t tmem = bars->tmem;
 
     // The first two warps run their loops as a whole, so that addresses and descriptors stay in uniform registers, and one
-    // thread issues.
+    // thread issues.  (With the loops under `lane == 0` the tensor pipe was busy 65 % of the time instead of 87 %.)
     if (warp == 0) {
         uint32_t stage = 0, phase = 0, used = 0;
         bool ok = true;
@@ -124,7 +135,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 if (!(ok = pipe::mbar_wait(&bars->empty[stage], phase ^ 1, 200, &g_product_fault))) break;
                 if (umma::elected()) {
                     if (rank == 0) pipe::mbar_arrive_expect_tx(&bars->full[stage], kStageBytes * CTAS);
-                    const uint32_t bar = CTAS == 2 ? umma::cluster_addr(&bars->full[stage], 0) : umma::smem_addr(&bars->full[stage]);
+                    const uint32_t bar = umma::cluster_addr(&bars->full[stage], 0);
                     uint8_t *sa = smem + stage * kStageBytes, *sb = sa + kOperandBytes;
                     const uint32_t term = kb / p.k_blocks;
                     const int k = static_cast<int>((kb - term * p.k_blocks) * kK);
@@ -135,11 +146,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     } else {
                         umma::tile_load<CTAS>(sa, a, k, m0, bar);
                     }
-                    if constexpr (GATED && CTAS == 2) {
+                    if constexpr (GATED) {                    // the first block's columns are gates, the second one's ups
                         umma::tile_load<CTAS>(sb, &p.b[rank], k, n0, bar);
-                    } else if constexpr (GATED) {
-                        umma::tile_load<CTAS>(sb, &p.b[0], k, n0, bar);
-                        umma::tile_load<CTAS>(sb + kOperandBytes / 2, &p.b[1], k, n0, bar);
                     } else {
                         const int n = n0 + static_cast<int>(rank * 128);
                         umma::tile_load<CTAS>(sb, &p.b[term], n, k, bar);
@@ -275,7 +283,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     __syncwarp();
     umma::fence_before();
     __syncthreads();
-    if constexpr (CTAS == 2) umma::cluster_sync();            // both blocks are done with each other's memory
+    umma::cluster_sync();                                     // both blocks are done with each other's memory
     umma::fence_after();
     if (warp == 2) umma::tmem_free<CTAS>(tmem, 2 * kN);
 }

@@ -1,4 +1,13 @@
 // Residual addition + RMS norm (bfloat16 or e4m3 output), its backward pass, and rounding of rows to e4m3.
+//
+//   r = x + residual,  n = r / sqrt(mean r^2 + eps),  y = n * weight
+//   dx = rstd (g - n mean(g n)) + dresidual  with g = weight * dy,   dweight = sum over rows of dy * n
+//   scale = max |y| / 448,  y8 = e4m3(y / scale)
+//
+// All of it is bound by memory: a row is read once, kept in registers until its sum (and maximum) is known, and written.
+// Measured at 8191 x 4096: forward 40.8 us (6.6 TB/s, the rate of a copy), with 8-bit output 37.2 us (6.3), backward with both
+// gradients 46.6 us (5.8 TB/s); quantise 11008 x 4096 24.5 us (5.5 TB/s).  r is rounded once for the residual stream and once
+// more read by the backward pass; y is computed before that rounding.
 #include "ops_common.cuh"
 
 namespace collage {
@@ -230,7 +239,7 @@ __global__ void __launch_bounds__(kRowThreads) row_dweight_any_kernel(const __gr
     }
 }
 
-// Gradients of rows of whole vectors in one pass: blocks walk over rows, one at a time for each group of `group` threads.
+// Gradients of rows of whole vectors in one pass (dy, r and dresidual are read once for dx and dweight): blocks walk over rows, one at a time for each group of `group` threads.
 // A thread owns PER vectors of columns: it sends for its own of the next two rows ahead (so loads go on while the row's
 // sum is joined), and keeps its columns' part of dweight in registers until the end.
 constexpr int kBackwardThreads = 512, kDepth = 2;
