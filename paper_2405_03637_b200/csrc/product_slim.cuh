@@ -39,9 +39,9 @@ template <int NT>
 constexpr int slim_smem(bool alone) { return 1024 + (slim_stages<NT>(alone) > kMaxSlimStages ? kMaxSlimStages : slim_stages<NT>(alone)) * slim_stage_bytes<NT>(); }
 
 // The end of a slim tile, by all threads of the block: its accumulators to shared memory, the cluster's parts joined in the
-// order of K, the results stored.  VECTORS: whole vectors fit the outputs.
+// order of K, the results stored (a sum of products in out[which]).  VECTORS: whole vectors fit the outputs.
 template <bool E4M3, bool GATED, int NT, bool VECTORS, typename Args>
-__device__ __forceinline__ void finish_slim_tile(const Args& p, uint8_t* smem, uint32_t tmem, uint32_t rank, uint32_t t0, uint32_t i0) {
+__device__ __forceinline__ void finish_slim_tile(const Args& p, uint8_t* smem, uint32_t tmem, uint32_t rank, uint32_t t0, uint32_t i0, uint32_t which = 0) {
     __syncthreads();                                 // the sums are complete and the stages free
     umma::fence_after();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -119,7 +119,7 @@ __device__ __forceinline__ void finish_slim_tile(const Args& p, uint8_t* smem, u
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e)
                 if (first + e < tokens && i < p.m) {
-                    uint16_t* at = p.out[0] + (t0 + first + e) * p.ldo[0] + i;
+                    uint16_t* at = p.out[which] + (t0 + first + e) * p.ldo[which] + i;
                     if constexpr (VECTORS) {
                         *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16(v[e].x, v[e].y), pack_bf16(v[e].z, v[e].w));
                     } else {
@@ -132,11 +132,12 @@ __device__ __forceinline__ void finish_slim_tile(const Args& p, uint8_t* smem, u
     if (p.split > 1) umma::cluster_sync_any();       // no block leaves while another reads its sums
 }
 
-template <bool E4M3, bool A_MN, bool GATED, int NT>
-__global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constant__ SlimArgs p) {
+// One tile by one block (`rank` of its cluster's `split`).  A_MN, B_MN: the operand is stored with its index contiguous.
+template <bool E4M3, bool A_MN, bool B_MN, bool GATED, int NT>
+__device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint32_t rank) {
     constexpr uint32_t kBytes = slim_stage_bytes<NT>();
     constexpr uint32_t kK = E4M3 ? 128 : 64, kIndexes = GATED ? 64 : 128;
-    constexpr uint32_t kIdesc = umma::instr_desc(E4M3 ? 0 : 1, A_MN, false, 128, NT);
+    constexpr uint32_t kIdesc = umma::instr_desc(E4M3 ? 0 : 1, A_MN, B_MN, 128, NT);
     static_assert(slim_stages<NT>(false) * kBytes >= NT * 512, "the tile's sums fit the stages");
     const uint32_t stages = p.stages;
     extern __shared__ uint8_t raw_smem[];
@@ -144,8 +145,10 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
     __shared__ uint64_t full[kMaxSlimStages], empty[kMaxSlimStages], done;
     __shared__ uint32_t tmem_slot;
     const uint32_t warp = threadIdx.x >> 5;
-    const uint32_t rank = p.split > 1 ? umma::cluster_rank() : 0, tile = blockIdx.x / p.split;
-    const uint32_t t0 = tile % p.token_tiles * NT, i0 = tile / p.token_tiles * kIndexes;
+    static_assert(!B_MN || NT % 64 == 0, "an operand stored by its index comes in boxes of 64 indexes");
+    // with several outputs (B_MN) the tiles of the first come first
+    const uint32_t per = p.token_tiles * ((p.m + kIndexes - 1) / kIndexes), which = B_MN ? tile / per : 0, place = B_MN ? tile % per : tile;
+    const uint32_t t0 = place % p.token_tiles * NT, i0 = place / p.token_tiles * kIndexes;
     const uint32_t blocks = p.terms * p.k_blocks;
     const uint32_t begin = static_cast<uint32_t>(static_cast<uint64_t>(blocks) * rank / p.split);
     const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(blocks) * (rank + 1) / p.split);
@@ -182,7 +185,12 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
                     umma::tile_load<1>(sa, &p.a[term], static_cast<int>(i0), k, bar);
                     umma::tile_load<1>(sa + kOperandBytes / 2, &p.a[term], static_cast<int>(i0) + 64, k, bar);
                 }
-                umma::tile_load<1>(sb, &p.b[term], k, static_cast<int>(t0), bar);
+                if constexpr (B_MN) {
+#pragma unroll
+                    for (int n = 0; n < NT / 64; ++n) umma::tile_load<1>(sb + n * (kOperandBytes / 2), &p.b[which], static_cast<int>(t0) + 64 * n, k, bar);
+                } else {
+                    umma::tile_load<1>(sb, &p.b[term], k, static_cast<int>(t0), bar);
+                }
             }
             __syncwarp();
             if (++stage == stages) { stage = 0; phase ^= 1; }
@@ -195,11 +203,11 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
             if (!(ok = pipe::mbar_wait(&full[stage], phase, 211, &g_product_fault))) break;
             umma::fence_after();
             const uint32_t sa = smem0 + stage * kBytes;
-            const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024), db = umma::operand_desc(sa + kOperandBytes, 16, 1024);
+            const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024), db = umma::operand_desc(sa + kOperandBytes, B_MN ? kOperandBytes / 2 : 16, 1024);
             if (umma::elected()) {
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i)
-                    umma::mma<1, E4M3>(tmem, da + i * (A_MN ? 2048 : 32) / 16, db + i * 2, kIdesc, kb > begin || i > 0);
+                    umma::mma<1, E4M3>(tmem, da + i * (A_MN ? 2048 : 32) / 16, db + i * (B_MN ? 2048 : 32) / 16, kIdesc, kb > begin || i > 0);
                 umma::commit<1>(&empty[stage]);
                 if (kb + 1 == end) umma::commit<1>(&done);
             }
@@ -208,7 +216,23 @@ __global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constan
         }
         if (ok) pipe::mbar_wait(&done, 0, 212, &g_product_fault);
     }
-    finish_slim_tile<E4M3, GATED, NT, true>(p, smem, tmem, rank, t0, i0);
+    finish_slim_tile<E4M3, GATED, NT, true>(p, smem, tmem, rank, t0, i0, which);
+}
+
+template <bool E4M3, bool A_MN, bool GATED, int NT>
+__global__ void __launch_bounds__(kSlimThreads) slim_kernel(const __grid_constant__ SlimArgs p) {
+    slim_tile<E4M3, A_MN, false, GATED, NT>(p, blockIdx.x / p.split, p.split > 1 ? umma::cluster_rank() : 0);
+}
+
+// The gradients of small layers in one launch: the first blocks make dx = dgate w_gate + dup w_up, the others, which need not
+// wait for them, tiles of dw_gate = dgate^T x and dw_up = dup^T x (tokens are K there, ffn takes the tokens' place).
+template <int NT>
+__global__ void __launch_bounds__(kSlimThreads) slim_backward_kernel(const __grid_constant__ SlimArgs dx, const __grid_constant__ SlimArgs dw, uint32_t dx_blocks,
+                                                                     uint32_t dw_tiles) {
+    if (blockIdx.x < dx_blocks)
+        slim_tile<false, true, false, false, NT>(dx, blockIdx.x / dx.split, dx.split > 1 ? umma::cluster_rank() : 0);
+    else if (blockIdx.x - dx_blocks < dw_tiles)
+        slim_tile<false, true, true, false, 128>(dw, blockIdx.x - dx_blocks, 0);
 }
 
 }  // namespace ops
