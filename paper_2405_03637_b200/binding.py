@@ -7,6 +7,7 @@ There is no fallback: if the shared library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
 
 import torch
@@ -79,6 +80,7 @@ class CollageError(RuntimeError):
 
 
 _lib = None
+_packed = None              # the same library; its functions take collage_matrix_t and collage_distill_t as packed bytes
 _lib_path = _LIB_PATH
 
 
@@ -97,7 +99,7 @@ def load(path) -> ctypes.CDLL:
 
 def lib() -> ctypes.CDLL:
     """The loaded CUDA library; raises if it has not been built (there is no other path)."""
-    global _lib
+    global _lib, _packed
     if _lib is None:
         if not _lib_path.exists():
             raise RuntimeError(f"{_lib_path} is missing: build it with `python -m paper_2405_03637_b200.build` "
@@ -141,21 +143,33 @@ def lib() -> ctypes.CDLL:
         L.collage_build_flavor.restype = ctypes.c_char_p
         L.collage_build_flavor.argtypes = []
         L.collage_enable_peer_access.argtypes = [i32]
-        mp = ctypes.POINTER(Matrix)
-        L.collage_add_rms_norm.argtypes = [mp, mp, vp, ctypes.c_double, mp, mp, mp, vp, vp, vp]
-        L.collage_rms_norm_workspace_bytes.restype = ctypes.c_size_t
-        L.collage_rms_norm_workspace_bytes.argtypes = [u64]
-        L.collage_add_rms_norm_backward.argtypes = [mp, mp, vp, vp, mp, mp, vp, vp, ctypes.c_size_t, vp]
-        L.collage_quantize_rows.argtypes = [mp, mp, vp, vp]
-        L.collage_gated_ffn.argtypes = [mp, mp, mp, mp, mp, mp, i32, vp]
-        L.collage_gated_ffn_backward.argtypes = [mp] * 11 + [i32, vp]
-        L.collage_gated_ffn_e4m3.argtypes = [mp, vp, mp, vp, mp, vp, mp, i32, vp]
-        dp = ctypes.POINTER(Distill)
-        L.collage_distill_loss.argtypes = [dp, vp, vp, vp]
-        L.collage_distill_loss_backward.argtypes = [dp, vp, vp, mp, vp]
-        L.collage_distill_loss_and_grad.argtypes = [dp, vp, vp, mp, vp]
+        _declare_operators(L, ctypes.POINTER(Matrix), ctypes.POINTER(Distill))
+        _packed = ctypes.CDLL(str(_lib_path))
+        _declare_operators(_packed, ctypes.c_char_p, ctypes.c_char_p)
         _lib = L
     return _lib
+
+
+def _declare_operators(L, mp, dp):
+    """Argument types of the training-step operators; `mp`, `dp`: how matrices and distillation arguments are passed."""
+    vp, i32 = ctypes.c_void_p, ctypes.c_int
+    L.collage_add_rms_norm.argtypes = [mp, mp, vp, ctypes.c_double, mp, mp, mp, vp, vp, vp]
+    L.collage_rms_norm_workspace_bytes.restype = ctypes.c_size_t
+    L.collage_rms_norm_workspace_bytes.argtypes = [ctypes.c_uint64]
+    L.collage_add_rms_norm_backward.argtypes = [mp, mp, vp, vp, mp, mp, vp, vp, ctypes.c_size_t, vp]
+    L.collage_quantize_rows.argtypes = [mp, mp, vp, vp]
+    L.collage_gated_ffn.argtypes = [mp, mp, mp, mp, mp, mp, i32, vp]
+    L.collage_gated_ffn_backward.argtypes = [mp] * 11 + [i32, vp]
+    L.collage_gated_ffn_e4m3.argtypes = [mp, vp, mp, vp, mp, vp, mp, i32, vp]
+    L.collage_distill_loss.argtypes = [dp, vp, vp, vp]
+    L.collage_distill_loss_backward.argtypes = [dp, vp, vp, mp, vp]
+    L.collage_distill_loss_and_grad.argtypes = [dp, vp, vp, mp, vp]
+
+
+def _operators() -> ctypes.CDLL:
+    if _lib is None:
+        lib()
+    return _packed
 
 
 def _ptr(t):
@@ -373,8 +387,12 @@ def _refuse(where: str):
     raise CollageError(ERR_ARG, where)
 
 
+_pack_matrix = struct.Struct("QQQQ").pack          # collage_matrix_t: a third of the time that a ctypes structure takes
+_pack_distill = struct.Struct("iId").pack
+
+
 def _matrix(t, dtype, where: str, required: bool = False):
-    """collage_matrix_t of a tensor, or None for None."""
+    """collage_matrix_t of a tensor, packed, or None for None."""
     if t is None:
         if required:
             raise CollageError(ERR_NULL, where)
@@ -383,20 +401,27 @@ def _matrix(t, dtype, where: str, required: bool = False):
         _refuse(where)
     shape = t.shape
     if len(shape) != 2:
+        if len(shape) < 2:
+            _refuse(where)
         try:
             t = t.view(-1, shape[-1])
-        except (RuntimeError, IndexError):
-            _refuse(where)
-        if len(shape) < 2:
+        except RuntimeError:
             _refuse(where)
         shape = t.shape
     rows, cols = shape
     ld, inner = t.stride()
-    if rows <= 1:
-        ld = cols                              # the stride of a single row means nothing
-    if (inner != 1 and cols > 1) or ld < cols:
-        _refuse(where)
-    return Matrix(t.data_ptr(), rows, cols, ld)
+    if inner != 1 or ld < cols or rows <= 1:
+        if rows <= 1:
+            ld = cols                          # the stride of a single row means nothing, nor that within a single column
+        if (inner != 1 and cols > 1) or ld < cols:
+            _refuse(where)
+    return _pack_matrix(t.data_ptr(), rows, cols, ld)
+
+
+def _extents(t):
+    """Rows and columns of a tensor that _matrix has taken."""
+    shape = t.shape
+    return shape if len(shape) == 2 else t.view(-1, shape[-1]).shape
 
 
 def _vector(t, dtype, length: int, where: str):
@@ -415,9 +440,10 @@ def add_rms_norm(x, residual, weight, eps: float, residual_out=None, y=None, y8=
     """r = x + residual; y = r / sqrt(mean(r^2) + eps) * weight in bfloat16 (y) and / or in 8 bits (y8, y8_scale)."""
     w = "collage_add_rms_norm"
     mx = _matrix(x, _BF16, w, True)
-    _check(lib().collage_add_rms_norm(mx, _matrix(residual, _BF16, w), _vector(weight, _BF16, mx.cols, w), eps,
-                                      _matrix(residual_out, _BF16, w), _matrix(y, _BF16, w), _matrix(y8, _E4M3, w),
-                                      _vector(y8_scale, _F32, mx.rows, w), _vector(rstd, _F32, mx.rows, w), _ptr(stream)), w)
+    rows, cols = _extents(x)
+    _check(_operators().collage_add_rms_norm(mx, _matrix(residual, _BF16, w), _vector(weight, _BF16, cols, w), eps,
+                                             _matrix(residual_out, _BF16, w), _matrix(y, _BF16, w), _matrix(y8, _E4M3, w),
+                                             _vector(y8_scale, _F32, rows, w), _vector(rstd, _F32, rows, w), _ptr(stream)), w)
 
 
 def rms_norm_workspace_bytes(cols: int) -> int:
@@ -429,24 +455,25 @@ def add_rms_norm_backward(dy, r, rstd, weight, dx, dweight, workspace, dresidual
     w = "collage_add_rms_norm_backward"
     mdy = _matrix(dy, _BF16, w, True)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().collage_add_rms_norm_backward(mdy, _matrix(r, _BF16, w), _vector(rstd, _F32, mdy.rows, w),
-                                               _vector(weight, _BF16, mdy.cols, w), _matrix(dresidual, _BF16, w),
-                                               _matrix(dx, _BF16, w), _vector(dweight, _BF16, mdy.cols, w), _ptr(workspace),
-                                               ws_bytes, _ptr(stream)), w)
+    rows, cols = _extents(dy)
+    _check(_operators().collage_add_rms_norm_backward(mdy, _matrix(r, _BF16, w), _vector(rstd, _F32, rows, w),
+                                                      _vector(weight, _BF16, cols, w), _matrix(dresidual, _BF16, w),
+                                                      _matrix(dx, _BF16, w), _vector(dweight, _BF16, cols, w), _ptr(workspace),
+                                                      ws_bytes, _ptr(stream)), w)
 
 
 def quantize_rows(x, q, scale, stream=None):
     """q, scale: x in 8 bits (torch.float8_e4m3fn) with one float scale a row."""
     w = "collage_quantize_rows"
     mx = _matrix(x, _BF16, w, True)
-    _check(lib().collage_quantize_rows(mx, _matrix(q, _E4M3, w), _vector(scale, _F32, mx.rows, w), _ptr(stream)), w)
+    _check(_operators().collage_quantize_rows(mx, _matrix(q, _E4M3, w), _vector(scale, _F32, _extents(x)[0], w), _ptr(stream)), w)
 
 
 def gated_ffn(x, w_gate, w_up, h, gate=None, up=None, activation: int = ACT_SILU, stream=None):
     """h = act(x w_gate^T) * (x w_up^T); gate and up, if given, keep the two products for the backward pass."""
     w = "collage_gated_ffn"
-    _check(lib().collage_gated_ffn(_matrix(x, _BF16, w), _matrix(w_gate, _BF16, w), _matrix(w_up, _BF16, w), _matrix(h, _BF16, w),
-                                   _matrix(gate, _BF16, w), _matrix(up, _BF16, w), activation, _ptr(stream)), w)
+    _check(_operators().collage_gated_ffn(_matrix(x, _BF16, w), _matrix(w_gate, _BF16, w), _matrix(w_up, _BF16, w), _matrix(h, _BF16, w),
+                                          _matrix(gate, _BF16, w), _matrix(up, _BF16, w), activation, _ptr(stream)), w)
 
 
 def gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dgate, dup, dx=None, dw_gate=None, dw_up=None, activation: int = ACT_SILU,
@@ -454,48 +481,49 @@ def gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dgate, dup, dx=None, dw_ga
     """Gradients of gated_ffn; dgate and dup receive the gradients of the two products (they may be gate and up themselves)."""
     w = "collage_gated_ffn_backward"
     m = [_matrix(t, _BF16, w) for t in (dh, x, w_gate, w_up, gate, up, dgate, dup, dx, dw_gate, dw_up)]
-    _check(lib().collage_gated_ffn_backward(*m, activation, _ptr(stream)), w)
+    _check(_operators().collage_gated_ffn_backward(*m, activation, _ptr(stream)), w)
 
 
 def gated_ffn_e4m3(x8, x_scale, w_gate8, w_gate_scale, w_up8, w_up_scale, h, activation: int = ACT_SILU, stream=None):
     """gated_ffn on 8-bit operands with a scale for each token and each channel, as quantize_rows writes them."""
     w = "collage_gated_ffn_e4m3"
     mx, mg, mu = _matrix(x8, _E4M3, w, True), _matrix(w_gate8, _E4M3, w, True), _matrix(w_up8, _E4M3, w, True)
-    _check(lib().collage_gated_ffn_e4m3(mx, _vector(x_scale, _F32, mx.rows, w), mg, _vector(w_gate_scale, _F32, mg.rows, w), mu,
-                                        _vector(w_up_scale, _F32, mu.rows, w), _matrix(h, _BF16, w), activation, _ptr(stream)), w)
+    _check(_operators().collage_gated_ffn_e4m3(mx, _vector(x_scale, _F32, _extents(x8)[0], w), mg,
+                                               _vector(w_gate_scale, _F32, _extents(w_gate8)[0], w), mu,
+                                               _vector(w_up_scale, _F32, _extents(w_up8)[0], w), _matrix(h, _BF16, w), activation,
+                                               _ptr(stream)), w)
 
 
-def _distill(logits, top_index, top_logits, temperature, where) -> Distill:
+def _distill(logits, top_index, top_logits, temperature, where):
+    """collage_distill_t, packed, and the number of rows."""
     if logits is None or top_index is None or top_logits is None:
         raise CollageError(ERR_NULL, where)
     dtype, index = logits.dtype, top_index.dtype
     if dtype not in (_BF16, _F32) or index not in (torch.int32, torch.int64):
         _refuse(where)
-    return Distill(_matrix(logits, dtype, where), _matrix(top_index, index, where), _matrix(top_logits, _F32, where),
-                   DTYPE_BF16 if dtype is _BF16 else DTYPE_F32, 4 if index is torch.int32 else 8, temperature)
+    packed = (_matrix(logits, dtype, where) + _matrix(top_index, index, where) + _matrix(top_logits, _F32, where) +
+              _pack_distill(DTYPE_BF16 if dtype is _BF16 else DTYPE_F32, 4 if index is torch.int32 else 8, temperature))
+    return packed, _extents(logits)[0]
 
 
 def distill_loss(logits, top_index, top_logits, temperature: float, loss, lse=None, stream=None):
     """loss[i] = temperature^2 KL(teacher's renormalised top entries || softmax(logits / temperature)) for each row."""
     w = "collage_distill_loss"
-    d = _distill(logits, top_index, top_logits, temperature, w)
-    n = d.logits.rows
-    _check(lib().collage_distill_loss(ctypes.byref(d), _vector(loss, _F32, n, w), _vector(lse, _F32, n, w), _ptr(stream)), w)
+    d, n = _distill(logits, top_index, top_logits, temperature, w)
+    _check(_operators().collage_distill_loss(d, _vector(loss, _F32, n, w), _vector(lse, _F32, n, w), _ptr(stream)), w)
 
 
 def distill_loss_backward(logits, top_index, top_logits, temperature: float, lse, grad_loss, dlogits, stream=None):
     """dlogits from grad_loss (one value a row) and the lse of distill_loss; dlogits may be the logits' own array."""
     w = "collage_distill_loss_backward"
-    d = _distill(logits, top_index, top_logits, temperature, w)
-    n = d.logits.rows
-    _check(lib().collage_distill_loss_backward(ctypes.byref(d), _vector(lse, _F32, n, w), _vector(grad_loss, _F32, n, w),
-                                               _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
+    d, n = _distill(logits, top_index, top_logits, temperature, w)
+    _check(_operators().collage_distill_loss_backward(d, _vector(lse, _F32, n, w), _vector(grad_loss, _F32, n, w),
+                                                      _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
 
 
 def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row_weight, loss, dlogits, stream=None):
     """loss[i] = row_weight[i] * the row's loss, and dlogits, in one pass; dlogits may be the logits' own array."""
     w = "collage_distill_loss_and_grad"
-    d = _distill(logits, top_index, top_logits, temperature, w)
-    n = d.logits.rows
-    _check(lib().collage_distill_loss_and_grad(ctypes.byref(d), _vector(row_weight, _F32, n, w), _vector(loss, _F32, n, w),
-                                               _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
+    d, n = _distill(logits, top_index, top_logits, temperature, w)
+    _check(_operators().collage_distill_loss_and_grad(d, _vector(row_weight, _F32, n, w), _vector(loss, _F32, n, w),
+                                                      _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
