@@ -20,14 +20,17 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libcollage_b200.so"
-SOURCES = ["collage_step.cu", "collage_primitives.cu", "collage_edq_static.cu", "collage_fp32_master.cu",
-           "row_norm.cu", "gated_ffn.cu", "distill_loss.cu"]
+SOURCES = ["collage_step.cu", "collage_primitives.cu", "collage_edq_static.cu", "collage_fp32_master.cu"]
+# The training-step operators: each kernel compiled by itself.  (Split by the host's cores, as below, several kernels share a
+# part, and the code that they get varies with the cut: up to a tenth of a kernel's time.)
+OPERATOR_SOURCES = ["row_norm.cu", "gated_ffn.cu", "distill_loss.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-fmad=false", "-ftz=false", "-prec-div=true", "-prec-sqrt=true",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
-    "--split-compile", "0", "-t", "0",      # compile the many kernel instantiations on all host cores
+    "-Xcompiler", "-fPIC", "-cudart", "static",
 ]
+OPERATOR_FLAGS = ["--split-compile", "64"]
+SPLIT_FLAGS = ["--split-compile", "0", "-t", "0"]      # compile the many kernel instantiations on all host cores
 
 
 def _newest_source_mtime() -> float:
@@ -43,12 +46,23 @@ def build(force: bool = False, verbose: bool = False, defines: tuple = (), out: 
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = lib.with_suffix(f".so.tmp{os.getpid()}")
-    cmd = [nvcc, *NVCC_FLAGS, *[f"-D{d}" for d in defines], *(["-Xptxas", "-v"] if verbose else []), "-o", str(tmp),
-           *[str(CSRC / s) for s in SOURCES]]
-    proc = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or proc.returncode:
-        sys.stderr.write(proc.stdout + proc.stderr)
-    if proc.returncode:
+    extra = [*[f"-D{d}" for d in defines], *(["-Xptxas", "-v"] if verbose else [])]
+    objects = [lib.parent / f"{Path(s).stem}.tmp{os.getpid()}.o" for s in OPERATOR_SOURCES]
+    try:
+        procs = [subprocess.Popen([nvcc, *NVCC_FLAGS, *OPERATOR_FLAGS, *extra, "-c", "-o", str(o), str(CSRC / s)], stdout=subprocess.PIPE,
+                                  stderr=subprocess.STDOUT, text=True) for s, o in zip(OPERATOR_SOURCES, objects)]
+        done = [(p.communicate()[0], p.returncode) for p in procs]
+        if all(rc == 0 for _, rc in done):
+            p = subprocess.run([nvcc, *NVCC_FLAGS, *SPLIT_FLAGS, *extra, "-shared", "-o", str(tmp), *[str(CSRC / s) for s in SOURCES],
+                                *[str(o) for o in objects]], capture_output=True, text=True)
+            done.append((p.stdout + p.stderr, p.returncode))
+    finally:
+        for o in objects:
+            o.unlink(missing_ok=True)
+    failed = any(rc for _, rc in done)
+    if verbose or failed:
+        sys.stderr.write("".join(text for text, _ in done))
+    if failed:
         raise RuntimeError("nvcc failed building the Collage CUDA library")
     os.replace(tmp, lib)
     return lib

@@ -36,7 +36,7 @@ constexpr float kLargeLse = 128.0f;
 // Up to this size of m c the exponent's argument is one fma, z c - m c; beyond it m c could overflow.
 constexpr float kLargeShift = 1e30f;
 constexpr size_t kSmSmem = 228 * 1024, kMaxSmem = 227 * 1024 - 5 * 1024;   // of an SM; dynamic part that a block may take
-constexpr size_t kSliceBytes = 74 * 1024 - 4608;             // dynamic part of a third of an SM
+constexpr size_t kThird = 74 * 1024 - 4608, kHalf = 112 * 1024 - 4608;     // dynamic parts of a third and of half an SM
 
 // Two floats in a 64-bit register: one instruction works on both.
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
 // One more warp has the teacher's entries: their softmax while the others sum, the student's logits at them before the
 // places are overwritten, then the loss, and one row later, when the dense gradient is surely written, the entries over it.
 struct StagedShared {
-    float2 warp[8];
+    float2 warp[12];
     float2 part[2][kMaxCluster];          // (maximum, sum) of each block of the cluster; two rows' worth, as all below
     float loss[2][kMaxCluster];
     uint32_t seen[2][kSeenWords], again[2][kSeenWords];
@@ -797,12 +797,14 @@ static collage_status_t launch_staged_as(const DistillArgs& a, uint64_t rows, in
     const uint64_t groups = std::min<uint64_t>(rows, std::max<uint64_t>(1, fit * sm_count / a.cluster));
     return launch<&distill_staged_kernel<T, THREADS, BLOCKS>>(groups * a.cluster, THREADS + 32, a.cluster, smem, s, a, rows);
 }
-// Threads by the slice's vectors: about twenty each of the longest; short rows by smaller blocks, more of them on an SM.
+// Threads by the slice's vectors: about twenty each of the longest; short rows by smaller blocks, more of them on an SM.  Rows of
+// which only two fit an SM are still faster whole than halved over a cluster: 1306 x 100352 127 us against 173.
 template <typename T>
 static collage_status_t launch_staged(const DistillArgs& a, uint64_t rows, int sm_count, cudaStream_t s) {
     return a.slice <= 512    ? launch_staged_as<T, 64, 8>(a, rows, sm_count, s)
            : a.slice <= 1536 ? launch_staged_as<T, 128, 5>(a, rows, sm_count, s)
-                             : launch_staged_as<T, 256, 3>(a, rows, sm_count, s);
+           : 16ull * a.slice + 36ull * a.k <= kThird ? launch_staged_as<T, 256, 3>(a, rows, sm_count, s)
+                                                     : launch_staged_as<T, 384, 2>(a, rows, sm_count, s);
 }
 
 // Short rows by smaller blocks, more of them on an SM: 16384 x 4000 backward 87 us by 128 threads, 153 by 256.
@@ -831,8 +833,8 @@ static collage_status_t launch_distill(DistillArgs& a, uint64_t rows, collage_dt
     };
     if constexpr (MODE == 2) {
         const size_t teacher = 36ull * a.k;
-        // three blocks of an SM hold their slices; beyond eight of those, one block may take all of the shared memory
-        while (a.cluster < kMaxCluster && 16ull * slice() + teacher > kSliceBytes) a.cluster *= 2;
+        // two or three blocks of an SM hold their slices; beyond eight of those, one block may take all of the shared memory
+        while (a.cluster < kMaxCluster && 16ull * slice() + teacher > kHalf) a.cluster *= 2;
         if (16ull * slice() + teacher <= kMaxSmem) {
             spread(1, 256);
             return bf16 ? launch_staged<uint16_t>(a, rows, sm_count, s) : launch_staged<float>(a, rows, sm_count, s);
