@@ -21,15 +21,14 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libcollage_b200.so"
 SOURCES = ["collage_step.cu", "collage_primitives.cu", "collage_edq_static.cu", "collage_fp32_master.cu"]
-# The training-step operators: each kernel compiled by itself.  (Split by the host's cores, as below, several kernels share a
-# part, and the code that they get varies with the cut: up to a tenth of a kernel's time.)
+# The training-step operators, each file compiled in one piece and the files at once.  (Split compilation, as below, gave one
+# of two codes from the same file, from build to build: up to a tenth of a kernel's time.)
 OPERATOR_SOURCES = ["row_norm.cu", "gated_ffn.cu", "distill_loss.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-fmad=false", "-ftz=false", "-prec-div=true", "-prec-sqrt=true",
     "-Xcompiler", "-fPIC", "-cudart", "static",
 ]
-OPERATOR_FLAGS = ["--split-compile", "64"]
 SPLIT_FLAGS = ["--split-compile", "0", "-t", "0"]      # compile the many kernel instantiations on all host cores
 
 
@@ -49,7 +48,7 @@ def build(force: bool = False, verbose: bool = False, defines: tuple = (), out: 
     extra = [*[f"-D{d}" for d in defines], *(["-Xptxas", "-v"] if verbose else [])]
     objects = [lib.parent / f"{Path(s).stem}.tmp{os.getpid()}.o" for s in OPERATOR_SOURCES]
     try:
-        procs = [subprocess.Popen([nvcc, *NVCC_FLAGS, *OPERATOR_FLAGS, *extra, "-c", "-o", str(o), str(CSRC / s)], stdout=subprocess.PIPE,
+        procs = [subprocess.Popen([nvcc, *NVCC_FLAGS, *extra, "-c", "-o", str(o), str(CSRC / s)], stdout=subprocess.PIPE,
                                   stderr=subprocess.STDOUT, text=True) for s, o in zip(OPERATOR_SOURCES, objects)]
         done = [(p.communicate()[0], p.returncode) for p in procs]
         if all(rc == 0 for _, rc in done):

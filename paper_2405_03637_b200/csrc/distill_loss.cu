@@ -189,18 +189,18 @@ struct RowVectors {
     uint4* base;                       // the row's first byte rounded down to 16
     T* row;
     uint32_t off, vocab;
-    __device__ RowVectors(T* r, uint32_t n) : row(r), vocab(n) {
+    __device__ __forceinline__ RowVectors(T* r, uint32_t n) : row(r), vocab(n) {
         const uintptr_t a = reinterpret_cast<uintptr_t>(r);
         base = reinterpret_cast<uint4*>(a & ~static_cast<uintptr_t>(15));
         off = static_cast<uint32_t>(a & 15) / sizeof(T);
     }
-    __device__ uint32_t count() const { return (off + vocab + kN - 1) / kN; }
-    __device__ bool inside(uint32_t v) const { return (v || !off) && (v + 1) * kN <= off + vocab; }
+    __device__ __forceinline__ uint32_t count() const { return (off + vocab + kN - 1) / kN; }
+    __device__ __forceinline__ bool inside(uint32_t v) const { return (v || !off) && (v + 1) * kN <= off + vocab; }
     // vectors [whole_begin, whole_end) of the row lie inside it; at most one before and one behind them do not
-    __device__ uint32_t whole_begin() const { return off ? 1 : 0; }
-    __device__ uint32_t whole_end() const { return (off + vocab) / kN; }
+    __device__ __forceinline__ uint32_t whole_begin() const { return off ? 1 : 0; }
+    __device__ __forceinline__ uint32_t whole_end() const { return (off + vocab) / kN; }
     // a vector at the row's edge, missing elements as minus infinity
-    __device__ uint4 edge(uint32_t v) const {
+    __device__ __forceinline__ uint4 edge(uint32_t v) const {
         union { uint4 q; uint32_t w[4]; T e[kN]; } u;
         u.q = make_uint4(Vec<T>::kLowest, Vec<T>::kLowest, Vec<T>::kLowest, Vec<T>::kLowest);
 #pragma unroll
@@ -210,7 +210,6 @@ struct RowVectors {
         }
         return u.q;
     }
-    __device__ uint4 load(uint32_t v) const { return inside(v) ? base[v] : edge(v); }
 };
 
 // A row of `vocab` logits by a cluster of blocks, each with a slice of it that it streams from global memory, once for
@@ -236,55 +235,39 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
 
     constexpr uint32_t kAhead = 4;              // vectors in flight for a thread
     const uint4 lowest = make_uint4(V::kLowest, V::kLowest, V::kLowest, V::kLowest);
-    // Whole vectors of the slice; the row's first and last one may be cut and are then left to one thread, by elements.
+    // Whole vectors of the slice; the row's first and last one may be cut.
     const uint32_t whole = first + (first < end && !z.inside(first)), whole_end = max(whole, end - (first < end && !z.inside(end - 1)));
-    auto each_cut = [&](auto&& f) {
-        if (threadIdx.x == 0 && whole > first && first < end) f(first);
-        if (threadIdx.x == 0 && whole_end < end && end - 1 >= whole) f(end - 1);
-    };
-    // Gradients of the slice: `load(v)` gives a vector of logits, `value(f)` puts gradients in their place.
-    auto write_row = [&](auto&& load, auto&& value) {
-        auto by_elements = [&](uint32_t v) {
-            uint64_t f[V::kPairs];
-            V::unpack(load(v), f);
-            value(f);
-#pragma unroll
-            for (uint32_t i = 0; i < kN; ++i) {
-                const int64_t e = static_cast<int64_t>(v) * kN + i - z.off;
-                const float2 g2 = floats_of(f[i / 2]);
-                if (e >= 0 && e < a.vocab) dz.row[e] = V::rounded(i % 2 ? g2.y : g2.x);
-            }
+    // Gradients of the slice: `load(v)` gives a whole vector of logits, `element(e)` one of them, `value` turns a pair of
+    // logits into gradients.  Cut vectors, and rows whose gradients lie otherwise in their vectors, go by elements.
+    auto write_row = [&](auto&& load, auto&& element, auto&& value) {
+        auto by_elements = [&](uint32_t lo, uint32_t hi) {
+#pragma unroll 1
+            for (uint32_t e = lo + threadIdx.x; e < hi; e += kDistillThreads) dz.row[e] = V::rounded(floats_of(value(pair_of(element(e), 0.0f))).x);
         };
-        if (z.off == dz.off) {
-            uint32_t v = whole + threadIdx.x;
-            for (; v + (kAhead - 1) * kDistillThreads < whole_end; v += kDistillThreads * kAhead) {
-                uint4 q[kAhead];
+        const uint32_t lo = first ? first * kN - z.off : 0, hi = min(end * kN - z.off, a.vocab);
+        if (z.off != dz.off) return by_elements(lo, hi);
+        auto put = [&](uint32_t v, const uint4& q) {
+            uint64_t f[V::kPairs];
+            V::unpack(q, f);
 #pragma unroll
-                for (uint32_t i = 0; i < kAhead; ++i) q[i] = load(v + i * kDistillThreads);
+            for (uint32_t i = 0; i < V::kPairs; ++i) f[i] = value(f[i]);
+            dz.base[v] = V::pack(f);
+        };
+        uint32_t v = whole + threadIdx.x;
+        for (; v + (kAhead - 1) * kDistillThreads < whole_end; v += kDistillThreads * kAhead) {
+            uint4 q[kAhead];
 #pragma unroll
-                for (uint32_t i = 0; i < kAhead; ++i) {
-                    uint64_t f[V::kPairs];
-                    V::unpack(q[i], f);
-                    value(f);
-                    dz.base[v + i * kDistillThreads] = V::pack(f);
-                }
-            }
-            for (; v < whole_end; v += kDistillThreads) {
-                uint64_t f[V::kPairs];
-                V::unpack(load(v), f);
-                value(f);
-                dz.base[v] = V::pack(f);
-            }
-            each_cut(by_elements);
-        } else {
-            for (uint32_t v = first + threadIdx.x; v < end; v += kDistillThreads) by_elements(v);
+            for (uint32_t i = 0; i < kAhead; ++i) q[i] = load(v + i * kDistillThreads);
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) put(v + i * kDistillThreads, q[i]);
         }
+#pragma unroll 1
+        for (; v < whole_end; v += kDistillThreads) put(v, load(v));
+        if (whole > first) by_elements(lo, min(whole * kN - z.off, hi));
+        if (whole_end < end) by_elements(whole_end * kN - z.off, hi);
     };
     auto zeros = [&] {
-        write_row([&](uint32_t) { return lowest; }, [](uint64_t (&f)[V::kPairs]) {
-#pragma unroll
-            for (uint32_t i = 0; i < V::kPairs; ++i) f[i] = 0;
-        });
+        write_row([&](uint32_t) { return lowest; }, [](uint32_t) { return 0.0f; }, [](uint64_t) -> uint64_t { return 0; });
     };
     if (MODE && g == 0.0f) {
         zeros();
@@ -292,7 +275,8 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
         return;
     }
     if (a.cluster > 1) umma::cluster_arrive_all();                       // this block runs
-    auto vector = [&](uint32_t v) { return z.load(v); };
+    auto vector = [&](uint32_t v) { return z.base[v]; };
+    auto element = [&](uint32_t e) { return V::value(z.row[e]); };
 
     if (warp == 0) {                            // the teacher's entries: p over all of them, in every block of the row
         float most = -INFINITY;
@@ -356,10 +340,10 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
             for (uint32_t i = 0; i < kAhead; ++i) q[i] = v + i * kDistillThreads < whole_end ? z.base[v + i * kDistillThreads] : lowest;
             take(q);
         }
-        each_cut([&](uint32_t v) {
-            uint4 q[kAhead] = {z.edge(v), lowest, lowest, lowest};
+        if (threadIdx.x ? threadIdx.x == 1 && whole_end < end : whole > first) {       // cut vectors: one thread for each
+            uint4 q[kAhead] = {z.edge(threadIdx.x ? end - 1 : first), lowest, lowest, lowest};
             take(q);
-        });
+        }
         const float2 sums = floats_of(total);
         sum = sums.x + sums.y;
         float most = warp_max(m);
@@ -437,20 +421,14 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
         const float gt = g * a.t;
         if (small) {
             const uint64_t c2 = pair_of(c, c), s2 = pair_of(shift, shift), g2 = pair_of(gt, gt);
-            write_row(vector, [&](uint64_t (&f)[V::kPairs]) {
-#pragma unroll
-                for (uint32_t i = 0; i < V::kPairs; ++i) {
-                    const float2 x = floats_of(fma_pair(f[i], c2, s2));
-                    f[i] = mul_pair(g2, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
-                }
+            write_row(vector, element, [&](uint64_t f) {
+                const float2 x = floats_of(fma_pair(f, c2, s2));
+                return mul_pair(g2, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
             });
         } else {
-            write_row(vector, [&](uint64_t (&f)[V::kPairs]) {
-#pragma unroll
-                for (uint32_t i = 0; i < V::kPairs; ++i) {
-                    const float2 x = floats_of(f[i]);
-                    f[i] = pair_of(gt * q_of(x.x), gt * q_of(x.y));
-                }
+            write_row(vector, element, [&](uint64_t f) {
+                const float2 x = floats_of(f);
+                return pair_of(gt * q_of(x.x), gt * q_of(x.y));
             });
         }
         __syncthreads();                        // the dense part is written; now the teacher's entries over it
