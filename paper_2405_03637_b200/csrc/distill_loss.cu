@@ -2,7 +2,7 @@
 //
 // With z = logits / t and lse = log sum_j exp(z_j) over the vocabulary, the teacher's p over its own entries:
 //   loss = t^2 sum_k p_k (log p_k - z_index(k) + lse),   dlogits_j = g t (exp(z_j - lse) - sum_{index(k) = j} p_k).
-// The softmax is taken on differences from the row's largest logit m, before the division by t: a row whose logits all
+// Both softmaxes are taken on differences from the row's largest logit m, before the division by t: a row whose logits all
 // are the type's lowest value is uniform, although neither m / t nor lse can be held to any use there.
 #include "ops_common.cuh"
 #include "umma.cuh"
@@ -25,6 +25,7 @@ struct DistillArgs {
     uint32_t cluster;           // blocks of a row
     int index_bytes;
     float inv_t, t;
+    float inv_t_rest;           // what inv_t lacks of 1 / t
 };
 
 constexpr uint32_t kSeenWords = 256;           // bitmaps over the indexes of a row, modulo 2^13
@@ -129,6 +130,15 @@ __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
     return v;
+}
+
+// exp((x - most) / t), and the exponent rounded to `shifted`.  Its roundings (of the difference, of 1 / t and of their product)
+// are followed up: in the loss an entry's p may be multiplied by a -log q of any size.
+__device__ __forceinline__ float teacher_exp(float x, float most, const DistillArgs& a, float& shifted) {
+    const float d = x - most, back = x - d, rest = (x - (d + back)) + (back - most);
+    shifted = d * a.inv_t;
+    const float lost = __fmaf_rn(d, a.inv_t, -shifted) + __fmaf_rn(rest, a.inv_t, d * a.inv_t_rest), e = expf(shifted);
+    return shifted > -128.0f ? __fmaf_rn(e, lost, e) : e;             // (below, e is 0 and what is lost may be infinite; a NaN passes)
 }
 
 // Sum of exp2((z - m) c) over parts with maxima of their own: `s` relative to `m` becomes relative to `to`.
@@ -285,7 +295,7 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
             const uint64_t at = row * a.ldi + k;
             const int64_t i = a.index_bytes == 8 ? static_cast<const int64_t*>(a.top_index)[at] : static_cast<const int32_t*>(a.top_index)[at];
             const bool there = i >= 0 && i < static_cast<int64_t>(a.vocab);
-            const float t = there ? a.top_logits[row * a.ldt + k] * a.inv_t : -INFINITY;
+            const float t = there ? a.top_logits[row * a.ldt + k] : -INFINITY;
             ti[k] = there ? static_cast<int>(i) : -1;
             tp[k] = t;
             most = fmaxf(most, t);
@@ -294,13 +304,12 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
         most = warp_max(most);
         const bool any_there = __any_sync(0xFFFFFFFFu, bad) || most > -INFINITY;
         float psum = 0.0f;
-        for (uint32_t k = lane; k < a.k; k += 32) psum += expf(tp[k] - most);
-        psum = warp_sum(psum);
         for (uint32_t k = lane; k < a.k; k += 32) {
-            const float shifted = tp[k] - most;
-            tp[k] = expf(shifted) / psum;
-            tz[k] = shifted;                    // until the student's logit takes its place
+            tp[k] = teacher_exp(tp[k], most, a, tz[k]);      // (tz: until the student's logit takes its place)
+            psum += tp[k];
         }
+        psum = warp_sum(psum);
+        for (uint32_t k = lane; k < a.k; k += 32) tp[k] /= psum;
         if (lane == 0) {
             sh.any_there = any_there;
             sh.log_psum = logf(psum);
@@ -637,7 +646,7 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
             for (uint32_t k = lane; k < a.k; k += 32) {
                 const int64_t i = a.index_bytes == 8 ? raw_index[k] : reinterpret_cast<const int32_t*>(raw_index)[k];
                 const bool there = i >= 0 && i < static_cast<int64_t>(a.vocab);
-                const float t = there ? raw_top[k] * a.inv_t : -INFINITY;
+                const float t = there ? raw_top[k] : -INFINITY;
                 ti[k] = there ? static_cast<int>(i) : -1;
                 tp[k] = t;
                 most = fmaxf(most, t);
@@ -645,14 +654,13 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
             }
             most = warp_max(most);
             const bool any_there = __any_sync(0xFFFFFFFFu, bad) || most > -INFINITY;
-            for (uint32_t k = lane; k < a.k; k += 32) psum += expf(tp[k] - most);
+            for (uint32_t k = lane; k < a.k; k += 32) {
+                tp[k] = teacher_exp(tp[k], most, a, tz[k]);  // (tz: until the student's logit takes its place)
+                psum += tp[k];
+            }
             psum = warp_sum(psum);
             log_psum = logf(psum);
-            for (uint32_t k = lane; k < a.k; k += 32) {
-                const float shifted = tp[k] - most;
-                tp[k] = expf(shifted) / psum;
-                tz[k] = shifted;                // until the student's logit takes its place
-            }
+            for (uint32_t k = lane; k < a.k; k += 32) tp[k] /= psum;
             if (lane == 0) sh.any_there[b] = any_there;
             for (uint32_t i = lane; i < kSeenWords; i += 32) sh.seen[b][i] = sh.again[b][i] = 0;
         } else {
@@ -869,6 +877,7 @@ static collage_status_t prepare_distill(const collage_distill_t* in, const float
     out->index_bytes = static_cast<int>(in->top_index_bytes);
     out->t = t;
     out->inv_t = inv_t;
+    out->inv_t_rest = static_cast<float>(1.0 / in->temperature - inv_t);
     return COLLAGE_OK;
 }
 
