@@ -34,8 +34,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 // A stored lse of this size or more is rounded too coarsely to give q to 2^-17 (an infinite one to give it at all): the
 // backward pass then takes maximum and sum from the row again.
 constexpr float kLargeLse = 128.0f;
-// Up to this size of m c the exponent's argument is one fma, z c - m c; beyond it m c could overflow.
-constexpr float kLargeShift = 1e30f;
 constexpr size_t kSmSmem = 228 * 1024, kMaxSmem = 227 * 1024 - 5 * 1024;   // of an SM; dynamic part that a block may take
 constexpr size_t kThird = 74 * 1024 - 4608, kHalf = 112 * 1024 - 4608;     // dynamic parts of a third and of half an SM
 
@@ -146,28 +144,39 @@ __device__ __forceinline__ float rescaled(float s, float m, float to, float c) {
     return m == to ? s : m == -INFINITY ? (s != s ? s : 0.0f) : s * exp2f((m - to) * c);
 }
 
-// Adds exp2((f - m) c) over a vector to `total`.  SMALL: m c cannot overflow (|m c| < kLargeShift), the argument is an fma.
-template <typename T, bool SMALL>
+// exp2((f - m) c) of two logits.  The difference is taken first: z c - m c, an fma, would be rounded at the size of m c, however
+// close z is to m.  `minus_m2` and `c2` are pairs of -m and c.
+__device__ __forceinline__ float2 exps(uint64_t f, uint64_t minus_m2, uint64_t c2) {
+    const float2 x = floats_of(mul_pair(add_pair(f, minus_m2), c2));
+    return make_float2(fast_exp2(x.x), fast_exp2(x.y));
+}
+// exp2(f c - base) of two logits
+__device__ __forceinline__ float2 based_exps(uint64_t f, uint64_t minus_base2, uint64_t c2) {
+    const float2 x = floats_of(fma_pair(f, c2, minus_base2));
+    return make_float2(fast_exp2(x.x), fast_exp2(x.y));
+}
+// Staged bfloat16 rows, which instructions bound, take the fma all the same, with RN(m c) as the base, as long as what that lacks of m c
+// (lack(), exact) is a quarter at most: every exponential is off by the factor exp2(lack) then, and sums are divided by it.
+// (4096 x 32000: 105 us, 115 by differences; in float 219 us by differences, 234 by the fma.)
+constexpr float kLargeShift = 0x1p22f;
+template <typename T>
+__device__ __forceinline__ bool by_base(float m, float c) { return sizeof(T) == 2 && fabsf(m * c) < kLargeShift; }
+template <typename T>
+__device__ __forceinline__ float lack(float m, float c) { return by_base<T>(m, c) ? __fmaf_rn(m, c, -(m * c)) : 0.0f; }
+
+// Adds exp2((f - m) c) over a vector to `total`, or exp2(f c - RN(m c)) if BASED.  While there is no number yet (m = -infinity) every f is
+// -infinity or NaN, and is taken as it is.
+template <typename T, bool BASED>
 __device__ __forceinline__ void add_exps(const uint4& q, float m, float c, uint64_t& total) {
     uint64_t f[Vec<T>::kPairs];
     Vec<T>::unpack(q, f);
-    if constexpr (SMALL) {
-        const uint64_t c2 = pair_of(c, c), s2 = pair_of(-m * c, -m * c);
+    const float minus_m = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
-        for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
-            const float2 x = floats_of(fma_pair(f[i], c2, s2));
-            total = add_pair(total, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
-        }
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
-            const float2 x = floats_of(f[i]);
-            total = add_pair(total, pair_of(x.x == m && m == -INFINITY ? 0.0f : fast_exp2((x.x - m) * c),
-                                            x.y == m && m == -INFINITY ? 0.0f : fast_exp2((x.y - m) * c)));
-        }
+    for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
+        const float2 e = BASED ? based_exps(f[i], pair_of(-m * c, -m * c), pair_of(c, c)) : exps(f[i], pair_of(minus_m, minus_m), pair_of(c, c));
+        total = add_pair(total, pair_of(e.x, e.y));
     }
 }
-__device__ __forceinline__ bool small_shift(float m, float c) { return fabsf(m * c) < kLargeShift; }
 
 // What a row's blocks share, apart from the row itself.
 struct DistillShared {
@@ -335,13 +344,8 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
                 total = pair_of(rescaled(so_far.x, m, to, c), rescaled(so_far.y, m, to, c));
                 m = to;
             }
-            if (small_shift(m, c)) {
 #pragma unroll
-                for (uint32_t i = 0; i < kAhead; ++i) add_exps<T, true>(q[i], m, c, total);
-            } else {
-#pragma unroll
-                for (uint32_t i = 0; i < kAhead; ++i) add_exps<T, false>(q[i], m, c, total);
-            }
+            for (uint32_t i = 0; i < kAhead; ++i) add_exps<T, false>(q[i], m, c, total);
         };
         for (uint32_t v = whole + threadIdx.x; v < whole_end; v += kDistillThreads * kAhead) {
             uint4 q[kAhead];
@@ -386,11 +390,10 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
         if (MODE != 1 && rank == 0 && threadIdx.x == 0) a.loss[row] = 0.0f;
         return;
     }
-    // log2 q_j = (z_j - m) c - log2sum, by an fma where nothing can overflow
-    const float log2sum = MODE == 1 && !from_row ? lse * kLog2e : log2f(sum);
-    const float shift = -m * c - log2sum;
-    const bool small = fabsf(m * c) < kLargeShift;
-    auto q_of = [&](float v) { return fast_exp2(small ? __fmaf_rn(v, c, shift) : (v - m) * c - log2sum); };
+    // q_j = exp2((z_j - m) c) / sum, or exp2(z_j c - log2sum) by a stored lse
+    const bool stored = MODE == 1 && !from_row;
+    const float log2sum = lse * kLog2e, scale = __fdividef(1.0f, sum);
+    auto q_of = [&](float v) { return stored ? fast_exp2(__fmaf_rn(v, c, -log2sum)) : fast_exp2((v - m) * c) * scale; };
 
     // entries in this block's slice: the student's logit, and their part of the loss
     auto mine = [&](int i) {
@@ -427,17 +430,19 @@ __global__ void __launch_bounds__(kDistillThreads, (MODE == 0 ? 2048 : 1280) / k
         __syncthreads();
     }
     if (MODE) {
-        const float gt = g * a.t;
-        if (small) {
-            const uint64_t c2 = pair_of(c, c), s2 = pair_of(shift, shift), g2 = pair_of(gt, gt);
+        const float gt = g * a.t, gs = gt * scale;
+        const uint64_t c2 = pair_of(c, c), g2 = pair_of(gs, gs);
+        if (stored) {                           // (sum and scale are 1)
+            const uint64_t s2 = pair_of(-log2sum, -log2sum);
             write_row(vector, element, [&](uint64_t f) {
-                const float2 x = floats_of(fma_pair(f, c2, s2));
-                return mul_pair(g2, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+                const float2 e = based_exps(f, s2, c2);
+                return mul_pair(g2, pair_of(e.x, e.y));
             });
         } else {
+            const uint64_t m2 = pair_of(-m, -m);
             write_row(vector, element, [&](uint64_t f) {
-                const float2 x = floats_of(f);
-                return pair_of(gt * q_of(x.x), gt * q_of(x.y));
+                const float2 e = exps(f, m2, c2);
+                return mul_pair(g2, pair_of(e.x, e.y));
             });
         }
         __syncthreads();                        // the dense part is written; now the teacher's entries over it
@@ -466,7 +471,7 @@ struct StagedShared {
     struct {                              // what is still to be done for the row before
         void* line;
         unsigned long long row;
-        float m, shift, log2sum, g;
+        float m, scale, g;
         uint32_t off, end;
         int small, live;
     } last;
@@ -555,8 +560,8 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
                 for (uint32_t o = 0; o < a.k; ++o)
                     if (ti[o] == i) p += tp[o];
             }
-            const float x = last.small ? __fmaf_rn(tz[k], c, last.shift) : (tz[k] - last.m) * c - last.log2sum;
-            static_cast<T*>(last.line)[i] = V::rounded(last.g * a.t * (fast_exp2(x) - p));
+            const float x = last.small ? __fmaf_rn(tz[k], c, -last.m * c) : (tz[k] - last.m) * c;
+            static_cast<T*>(last.line)[i] = V::rounded(last.g * a.t * (fast_exp2(x) * last.scale - p));
         }
     };
 
@@ -688,12 +693,12 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
             each_place(true, [&](const uint4& q, uint32_t i) { largest[i & 1] = V::most(largest[i & 1], q); });
             m = fmaxf(V::most_value(largest[0]), V::most_value(largest[1]));
             uint64_t total[2] = {0, 0};
-            if (small_shift(m, c))
+            if (by_base<T>(m, c))
                 each_place(false, [&](const uint4& q, uint32_t i) { add_exps<T, true>(q, m, c, total[i & 1]); });
             else
                 each_place(false, [&](const uint4& q, uint32_t i) { add_exps<T, false>(q, m, c, total[i & 1]); });
             const float2 sums = floats_of(add_pair(total[0], total[1]));
-            sum = sums.x + sums.y;
+            sum = (sums.x + sums.y) * fast_exp2(-lack<T>(m, c));
             const float most = warp_max(m);
             sum = warp_sum(rescaled(sum, m, most, c));
             if (lane == 0) sh.warp[warp] = make_float2(most, sum);
@@ -713,8 +718,7 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
             sum = warp_sum(rescaled(r.y, r.x, m, c));
         }
         if (m == -INFINITY) sum = NAN;          // a row without any number in it has no distribution
-        const float log2sum = log2f(sum), shift = -m * c - log2sum;
-        const bool small = fabsf(m * c) < kLargeShift, live = sh.any_there[b];
+        const bool small = by_base<T>(m, c), live = sh.any_there[b];
         float loss = 0.0f;
         if (teacher) {                          // the student's logits at the entries in this block's slice, and their part of the loss
             const float logsum = logf(sum);
@@ -727,7 +731,7 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
             }
         }
         __syncthreads();                        // the slice may be overwritten
-        const float gt = g * a.t;
+        const float scale = __fdividef(fast_exp2(-lack<T>(m, c)), sum), gs = g * a.t * scale;           // turns exponentials into q, and into gradients
         if (teacher) {
             if (turn > 0) finish_last(b ^ 1);
             loss = warp_sum(loss);
@@ -746,25 +750,30 @@ __global__ void __launch_bounds__(kStagedThreads + 32, BLOCKS) distill_staged_ke
             __syncwarp();
             if (end_next) send_for_teacher(row + step);
             __syncwarp();
-            if (lane == 0) sh.last = {dz.row, row, m, shift, log2sum, g, z.off, end, small, live};
+            if (lane == 0) sh.last = {dz.row, row, m, scale, g, z.off, end, small, live};
             __syncwarp();
         } else if (!live) {                     // nothing to learn from: zeros whatever the logits are
             write_row(false, zero);
         } else if (small) {
-            const uint64_t c2 = pair_of(c, c), s2 = pair_of(shift, shift), g2 = pair_of(gt, gt);
+            const uint64_t c2 = pair_of(c, c), b2 = pair_of(-m * c, -m * c), g2 = pair_of(gs, gs);
             write_row(true, [&](uint64_t (&f)[V::kPairs]) {
 #pragma unroll
                 for (uint32_t i = 0; i < V::kPairs; ++i) {
-                    const float2 x = floats_of(fma_pair(f[i], c2, s2));
-                    f[i] = mul_pair(g2, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+                    const float2 e = based_exps(f[i], b2, c2);
+                    f[i] = mul_pair(g2, pair_of(e.x, e.y));
                 }
             });
         } else {
             write_row(true, [&](uint64_t (&f)[V::kPairs]) {
 #pragma unroll
                 for (uint32_t i = 0; i < V::kPairs; ++i) {
-                    const float2 x = floats_of(f[i]);
-                    f[i] = pair_of(gt * fast_exp2((x.x - m) * c - log2sum), gt * fast_exp2((x.y - m) * c - log2sum));
+                    if constexpr (sizeof(T) == 2) {     // (rare here, and in packed instructions it would cost the ordinary rows registers)
+                        const float2 x = floats_of(f[i]);
+                        f[i] = pair_of(gs * fast_exp2((x.x - m) * c), gs * fast_exp2((x.y - m) * c));
+                    } else {
+                        const float2 e = exps(f[i], pair_of(-m, -m), pair_of(c, c));
+                        f[i] = mul_pair(pair_of(gs, gs), pair_of(e.x, e.y));
+                    }
                 }
             });
         }

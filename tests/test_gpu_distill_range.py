@@ -53,6 +53,18 @@ def check(z, at, top, tau, what):
     close(loss, loss64 * weight.double(), ltol * weight.double(), what + " loss in one pass")
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,vocab,k", [(4, 1031, 9), (300, 1031, 9), (5, 33_001, 20), (2, 900_001, 5)])
+def test_rows_of_logits_far_from_zero(rows, vocab, k, dtype):
+    spread = normal(rows + vocab, rows, vocab, std=2.0, dtype=F32)
+    at, top = teacher(1, rows, vocab, k)
+    for tau in (0.05, 0.7, 4.0) if vocab < 100_000 else (0.7,):
+        for far in (-1e9, -1e5, -1e3, 1e3, 1e5, 1e6, 1e12, 1e20):
+            z = (spread + far).to(dtype)                     # (from 1e5 on, where a unit of the type is larger than that, mostly all alike)
+            z[1::2, ::7] -= abs(far) * 2.0 ** -7             # and in every other row a seventh of them a unit of bfloat16 below
+            check(z, at, top, tau, f"{far:g} at {tau}:")
+
+
 @pytest.mark.parametrize("rows,vocab,k", [(3, 1031, 9), (3, 90_001, 40)])
 def test_teachers_logits_far_from_zero(rows, vocab, k):
     z = normal(3, rows, vocab, std=2.0)
