@@ -111,7 +111,8 @@ static cudaError_t allow_smem() {
 template <auto Kernel, typename... Args>
 static collage_status_t launch(uint64_t blocks, int threads, uint32_t cluster, size_t smem, cudaStream_t stream, const Args&... args) {
     if (blocks >= (1ull << 31)) return COLLAGE_ERR_LIMIT;
-    if (smem > 48 * 1024 && allow_smem<Kernel>() != cudaSuccess) return COLLAGE_ERR_CUDA;
+    // without leave a block has 48 KB, of which what the kernel declares statically (5 KB at most here) is taken off
+    if (smem > 40 * 1024 && allow_smem<Kernel>() != cudaSuccess) return COLLAGE_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(threads);
