@@ -191,7 +191,7 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* slots, int w
 }
 
 // x / d for many x: Markstein's division by a correctly rounded reciprocal.  q = RN(x r) is off by a unit at most, its
-// remainder x - q d is exact in an fma, and RN(q + remainder r) is the correctly rounded quotient, where nothing leaves
+// remainder q d - x is exact in an fma, and RN(q - remainder r) is the correctly rounded quotient, where nothing leaves
 // the normal range (`plain`); elsewhere the division itself.
 struct Divisor {
     float d, r;
@@ -199,7 +199,7 @@ struct Divisor {
     __device__ __forceinline__ explicit Divisor(float divisor) : d(divisor), r(1.0f / divisor), plain(divisor > 0x1p-100f && divisor < 0x1p100f) {}
     __device__ __forceinline__ float quotient(float x) const {
         const float q = x * r;
-        return __fmaf_rn(__fmaf_rn(-q, d, x), r, q);
+        return __fmaf_rn(-__fmaf_rn(q, d, -x), r, q);        // (in these signs a remainder of zero leaves -0 as it is)
     }
 };
 

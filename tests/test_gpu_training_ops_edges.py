@@ -5,6 +5,10 @@ import sys
 from pathlib import Path
 
 import pytest
+import torch
+
+from ops_util import BF16, E4M3, normal
+from paper_2405_03637_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 ROOT = Path(__file__).resolve().parent.parent
@@ -28,3 +32,20 @@ for dtype, vocab in ((torch.bfloat16, 24_000), (torch.float32, 12_000)):
 def test_first_launches_of_every_size_of_shared_memory():
     p = subprocess.run([sys.executable, "-c", FIRST_LAUNCHES], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert p.returncode == 0, p.stderr[-2000:]
+
+
+@pytest.mark.parametrize("cols", [300, 304, 4096])
+def test_rounding_to_8_bits_keeps_the_sign_of_zero(cols):
+    # every code of the format, both zeros among them, in rows that go by elements and by vectors: the scale is 1
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda")
+    codes = codes[~codes.view(E4M3).float().isnan()]
+    x = torch.zeros(3, cols, dtype=BF16, device="cuda")
+    x[:, :codes.numel()] = codes.view(E4M3).float().to(BF16)
+    x[1] *= 0.37
+    x[2, codes.numel():] = -0.0
+    x[2, :codes.numel()] = normal(1, codes.numel(), std=1e-38)       # beyond the divisors of the shortcut
+    q, scale = torch.empty_like(x, dtype=E4M3), torch.empty(3, device="cuda")
+    B.quantize_rows(x, q, scale)
+    assert scale[0] == 1 and torch.equal(q[0, :codes.numel()].view(torch.uint8), codes)
+    want = (x.float() / scale[:, None]).to(E4M3)
+    assert torch.equal(q.view(torch.uint8), want.view(torch.uint8))
