@@ -29,6 +29,11 @@ struct RowArgs {
 
 constexpr int kRowThreads = 256;
 
+// Squares leave a float's range beyond 2^64 and lose digits below 2^-63.  Where the mean of a row's squares (and eps) shows that, the
+// row is taken times a power of two, and its sum again.
+__device__ __forceinline__ bool squares_fit(float mean) { return mean > 0x1p-100f && mean < INFINITY; }
+__device__ __forceinline__ float rescue_factor(float mean) { return mean > 1.0f ? 0x1p-80f : 0x1p80f; }
+
 // One block per row, element by element, the row read again for each stage: any length, stride and alignment.
 template <bool NORM>
 __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_constant__ RowArgs a) {
@@ -40,13 +45,17 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
     auto value = [&](uint64_t j) { return res ? bf16_value(x[j]) + bf16_value(res[j]) : bf16_value(x[j]); };
     float rstd = 1.0f;
     if (NORM) {
-        float sum = 0.0f;
-        for (uint64_t j = threadIdx.x; j < a.cols; j += kRowThreads) {
-            const float r = value(j);
-            sum = __fmaf_rn(r, r, sum);
-        }
-        sum = block_sum(sum, slots, kRowThreads / 32);
-        rstd = 1.0f / sqrtf(sum / static_cast<float>(a.cols) + a.eps);
+        auto mean_of = [&](float f) {
+            float sum = 0.0f;
+            for (uint64_t j = threadIdx.x; j < a.cols; j += kRowThreads) {
+                const float r = value(j) * f;
+                sum = __fmaf_rn(r, r, sum);
+            }
+            return block_sum(sum, slots, kRowThreads / 32) / static_cast<float>(a.cols) + a.eps * f * f;
+        };
+        float mean = mean_of(1.0f), f = 1.0f;
+        if (!squares_fit(mean)) mean = mean_of(f = rescue_factor(mean));
+        rstd = f / sqrtf(mean);
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     }
     auto normed = [&](float r, uint64_t j) { return NORM ? r * rstd * bf16_value(a.weight[j]) : r; };
@@ -111,23 +120,37 @@ __global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) row_kernel(
         }
     }
     if (NORM) {
-        float part[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            part[i] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) part[i] = __fmaf_rn(r[i][e], r[i][e], part[i]);
-        }
-        float sum = part[0];
-#pragma unroll
-        for (int i = 1; i < PER; ++i) sum += part[i];
-        sum = block_sum(sum, slots, warps);
-        const float rstd = 1.0f / sqrtf(sum / static_cast<float>(a.cols) + a.eps);
-        if (a.rstd && t == 0) a.rstd[row] = rstd;
+        float f = 1.0f, rstd;                        // rstd: of the row times f
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int v = t + i * threads;
             if (a.residual_out && v < vectors) reinterpret_cast<uint4*>(a.residual_out + row * a.ldro)[v] = pack8(r[i]);
+        }
+#pragma unroll 1
+        for (;;) {
+            float part[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                part[i] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part[i] = __fmaf_rn(r[i][e], r[i][e], part[i]);
+            }
+            float sum = part[0];
+#pragma unroll
+            for (int i = 1; i < PER; ++i) sum += part[i];
+            const float mean = block_sum(sum, slots, warps) / static_cast<float>(a.cols) + a.eps * f * f;
+            rstd = 1.0f / sqrtf(mean);
+            if (squares_fit(mean) || f != 1.0f) break;
+            f = rescue_factor(mean);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r[i][e] *= f;
+        }
+        if (a.rstd && t == 0) a.rstd[row] = f * rstd;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * threads;
             float w[8];
             unpack8(qw[i], w);
 #pragma unroll

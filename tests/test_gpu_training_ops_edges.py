@@ -7,7 +7,7 @@ from pathlib import Path
 import pytest
 import torch
 
-from ops_util import BF16, E4M3, normal
+from ops_util import BF16, E4M3, U, close, normal
 from paper_2405_03637_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +49,33 @@ def test_rounding_to_8_bits_keeps_the_sign_of_zero(cols):
     assert scale[0] == 1 and torch.equal(q[0, :codes.numel()].view(torch.uint8), codes)
     want = (x.float() / scale[:, None]).to(E4M3)
     assert torch.equal(q.view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("rows,cols", [(6, 257), (6, 1000), (6, 4096), (6, 16384), (6, 33_000), (600, 256), (600, 1024)])
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+def test_norm_of_rows_whose_squares_no_float_holds(rows, cols, eps):
+    x, dy, weight = normal(1, rows, cols), normal(2, rows, cols), normal(3, cols)
+    for i, size in enumerate((1e20, -3e37, 1e-25, 1e-12)):
+        x[i::6] *= size
+    x[4::6] = torch.finfo(BF16).max
+    new = lambda *s, dtype=torch.float32: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+    y, y8, scale, rstd = torch.empty_like(x), torch.empty_like(x, dtype=E4M3), new(rows), new(rows)
+    B.add_rms_norm(x, None, weight, eps, y=y, y8=y8, y8_scale=scale, rstd=rstd)
+    r, w = x.double(), weight.double()
+    rstd64 = 1 / torch.sqrt((r * r).mean(1) + eps)
+    y64 = r * rstd64[:, None] * w
+    # the sum of squares as for ordinary rows; 1 / 3e38 is a subnormal float of 22 bits
+    deep = (cols / 32 + 16) * 2.0 ** -23 + 2.0 ** -22
+    close(rstd, rstd64, deep * rstd64, "rstd")
+    close(y, y64, (U * 1.001 + 2 * deep) * y64.abs() + 2.0 ** -133, "y")       # (half of bfloat16's smallest step is 2^-134)
+    scale64 = y64.abs().amax(1) / 448
+    close(scale, scale64, (2 * deep + 2.0 ** -22) * scale64, "scale")
+    close(y8.double() * scale.double()[:, None], y64, y64.abs() * (2.0 ** -4 + 4 * deep) + scale64[:, None] * 2.0 ** -10 * 1.001, "y8")
+    dx, dweight = torch.empty_like(x), new(cols, dtype=BF16)
+    B.add_rms_norm_backward(dy, x, rstd, weight, dx, dweight, torch.empty(B.rms_norm_workspace_bytes(cols), dtype=torch.uint8, device="cuda"))
+    n, g = r * rstd.double()[:, None], dy.double() * w
+    want = (g - n * (g * n).mean(1, keepdim=True)) * rstd.double()[:, None]
+    terms = rstd.double()[:, None] * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True))
+    close(dx, want, U * 1.001 * want.abs() + (deep + 2.0 ** -20) * terms + 2.0 ** -133, "dx")
+    dw64, mag = (dy.double() * n).sum(0), (dy.double() * n).abs().sum(0)
+    close(dweight, dw64, U * 1.001 * dw64.abs() + (rows + 8) * 2.0 ** -23 * mag, "dweight")
