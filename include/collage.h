@@ -412,7 +412,7 @@ typedef struct collage_matrix {
  *   y           : bfloat16 [rows, cols] or NULL.
  *   y8, y8_scale: e4m3 [rows, cols] and float[rows], or both NULL: y rounded to 8 bits as by
  *                 collage_quantize_rows, y ~ y8 * y8_scale.  At least one of y and y8 is given.
- *   rstd        : DEVICE float[rows] or NULL (the backward pass needs it).
+ *   rstd        : DEVICE float[rows] or NULL (the backward pass needs it).  NaN in rows of no columns.
  * residual_out may be the array of x or of residual, y that of x (same data, same ld).
  * A row that holds a NaN or an infinity gives NaNs (IEEE arithmetic). */
 collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_matrix_t* residual, const void* weight,

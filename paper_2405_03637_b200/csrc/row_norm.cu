@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
     }
     auto normed = [&](float r, uint64_t j) { return NORM ? r * rstd * bf16_value(a.weight[j]) : r; };
     float scale = 0.0f;
-    if (a.y8) {
+    if (a.scale) {
         uint32_t most = 0;
         for (uint64_t j = threadIdx.x; j < a.cols; j += kRowThreads)
             most = max(most, __float_as_uint(normed(value(j), j)) & 0x7FFFFFFFu);
@@ -468,8 +468,6 @@ collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_m
     DeviceInfo dev;
     if ((st = current_device(&dev)) != COLLAGE_OK) return st;
     if (x->rows == 0) return COLLAGE_OK;
-    if (x->cols == 0)
-        return !y8 || cudaMemsetAsync(y8_scale, 0, 4 * x->rows, static_cast<cudaStream_t>(stream)) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
     RowArgs a = {};
     a.x = static_cast<const uint16_t*>(x->data);
     a.ldx = x->ld;
@@ -481,7 +479,8 @@ collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_m
     a.rstd = rstd;
     a.cols = x->cols;
     a.eps = static_cast<float>(eps);
-    bool fit = x->cols % 8 == 0 && reinterpret_cast<uintptr_t>(weight) % 16 == 0 && rows_aligned(x, 2, 16);
+    // (rows without columns go by elements: rstd is NaN, the scale 0)
+    bool fit = x->cols && x->cols % 8 == 0 && reinterpret_cast<uintptr_t>(weight) % 16 == 0 && rows_aligned(x, 2, 16);
     for (int i = 0; i < 4; ++i)
         if (others[i]) fit = fit && rows_aligned(others[i], i == 3 ? 1 : 2, i == 3 ? 8 : 16);
     return launch_rows<true>(a, x->rows, fit, dev.sm_count, static_cast<cudaStream_t>(stream));

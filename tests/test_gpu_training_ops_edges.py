@@ -79,3 +79,10 @@ def test_norm_of_rows_whose_squares_no_float_holds(rows, cols, eps):
     close(dx, want, U * 1.001 * want.abs() + (deep + 2.0 ** -20) * terms + 2.0 ** -133, "dx")
     dw64, mag = (dy.double() * n).sum(0), (dy.double() * n).abs().sum(0)
     close(dweight, dw64, U * 1.001 * dw64.abs() + (rows + 8) * 2.0 ** -23 * mag, "dweight")
+
+
+def test_norm_of_rows_without_columns_writes_what_it_promises():
+    x, w = torch.empty(3, 0, dtype=BF16, device="cuda"), torch.empty(0, dtype=BF16, device="cuda")
+    rstd, scale = torch.full((3,), 7.0, device="cuda"), torch.full((3,), 7.0, device="cuda")
+    B.add_rms_norm(x, None, w, 1e-5, y=torch.empty_like(x), y8=torch.empty_like(x, dtype=E4M3), y8_scale=scale, rstd=rstd)
+    assert rstd.isnan().all() and (scale == 0).all()         # the mean of nothing, and the largest of nothing
