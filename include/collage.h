@@ -495,7 +495,7 @@ typedef struct collage_distill {
     collage_matrix_t top_logits;     /* [rows, k] of float; k <= COLLAGE_DISTILL_MAX_TOP (ERR_LIMIT)        */
     collage_dtype_t logits_dtype;
     uint32_t top_index_bytes;
-    double temperature;              /* > 0 and finite                                                      */
+    double temperature;              /* > 0 and finite, as is 1 / (temperature ln 2), in float (ERR_ARG)    */
 } collage_distill_t;
 #define COLLAGE_DISTILL_MAX_TOP 1024
 

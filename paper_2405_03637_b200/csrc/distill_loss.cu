@@ -848,7 +848,7 @@ static collage_status_t prepare_distill(const collage_distill_t* in, const float
     if (in->top_index_bytes != 4 && in->top_index_bytes != 8) return COLLAGE_ERR_ARG;
     if (!(std::isfinite(in->temperature) && in->temperature > 0.0)) return COLLAGE_ERR_ARG;
     const float t = static_cast<float>(in->temperature), inv_t = static_cast<float>(1.0 / in->temperature);
-    if (!(t > 0.0f && std::isfinite(t) && inv_t > 0.0f && std::isfinite(inv_t))) return COLLAGE_ERR_ARG;
+    if (!(t > 0.0f && std::isfinite(t) && inv_t > 0.0f && std::isfinite(inv_t * kLog2e))) return COLLAGE_ERR_ARG;
     if (!same_shape(&in->top_index, &in->top_logits) || in->top_index.rows != in->logits.rows) return COLLAGE_ERR_ARG;
     if (dlogits && !same_shape(dlogits, &in->logits)) return COLLAGE_ERR_ARG;
     collage_status_t st = check_matrix(&in->logits, size);

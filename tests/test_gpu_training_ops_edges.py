@@ -86,3 +86,13 @@ def test_norm_of_rows_without_columns_writes_what_it_promises():
     rstd, scale = torch.full((3,), 7.0, device="cuda"), torch.full((3,), 7.0, device="cuda")
     B.add_rms_norm(x, None, w, 1e-5, y=torch.empty_like(x), y8=torch.empty_like(x, dtype=E4M3), y8_scale=scale, rstd=rstd)
     assert rstd.isnan().all() and (scale == 0).all()         # the mean of nothing, and the largest of nothing
+
+
+def test_temperatures_whose_reciprocal_is_too_large_are_refused():
+    z, at, top, loss = normal(1, 2, 64), torch.zeros(2, 1, dtype=torch.int32, device="cuda"), torch.zeros(2, 1, device="cuda"), torch.zeros(2, device="cuda")
+    for tau in (3.2e-39, 4.2e-39):                           # 1 / t is a float, 1 / (t ln 2) is not
+        with pytest.raises(B.CollageError) as e:
+            B.distill_loss(z, at, top, tau, loss)
+        assert e.value.status == B.ERR_ARG
+    B.distill_loss(z, at, top, 4.4e-39, loss)
+    assert not loss.isnan().any()
