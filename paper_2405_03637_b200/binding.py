@@ -7,6 +7,7 @@ There is no fallback: if the shared library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import struct
 from pathlib import Path
 
@@ -397,6 +398,12 @@ _pack_matrix = struct.Struct("QQQQ").pack          # collage_matrix_t: a third o
 _pack_distill = struct.Struct("iId").pack
 
 
+def _flat(t):
+    """Leading dimensions as rows (RuntimeError where a view cannot be had)."""
+    *lead, cols = t.shape
+    return t.view(-1, cols) if cols else t.view(math.prod(lead), 0)
+
+
 def _matrix(t, dtype, where: str, required: bool = False):
     """collage_matrix_t of a tensor, packed, or None for None."""
     if t is None:
@@ -410,7 +417,7 @@ def _matrix(t, dtype, where: str, required: bool = False):
         if len(shape) < 2:
             _refuse(where)
         try:
-            t = t.view(-1, shape[-1])
+            t = _flat(t)
         except RuntimeError:
             _refuse(where)
         shape = t.shape
@@ -427,7 +434,7 @@ def _matrix(t, dtype, where: str, required: bool = False):
 def _extents(t):
     """Rows and columns of a tensor that _matrix has taken."""
     shape = t.shape
-    return shape if len(shape) == 2 else t.view(-1, shape[-1]).shape
+    return shape if len(shape) == 2 else _flat(t).shape
 
 
 def _vector(t, dtype, length: int, where: str):

@@ -96,3 +96,14 @@ def test_temperatures_whose_reciprocal_is_too_large_are_refused():
         assert e.value.status == B.ERR_ARG
     B.distill_loss(z, at, top, 4.4e-39, loss)
     assert not loss.isnan().any()
+
+
+def test_three_dimensions_without_columns():
+    # [2, 3, 0] is six rows of nothing, as [6, 0] is
+    x, q, scale = torch.empty(2, 3, 0, dtype=BF16, device="cuda"), torch.empty(2, 3, 0, dtype=E4M3, device="cuda"), torch.full((6,), 7.0, device="cuda")
+    B.quantize_rows(x, q, scale)
+    assert (scale == 0).all()
+    h = torch.full((2, 3, 8), 7.0, dtype=BF16, device="cuda")
+    none = torch.empty(8, 0, dtype=BF16, device="cuda")
+    B.gated_ffn(x, none, none, h)
+    assert (h == 0).all()
