@@ -373,25 +373,27 @@ def read_edq(edq_dev) -> dict:
 # ------------------------------------------------------------------------------------------------------------------------
 # Operators of the forward and backward pass.  Matrices are CUDA tensors of two or more dimensions whose last one is
 # contiguous; leading dimensions are flattened into rows (a view, never a copy).  What a tensor cannot be described as, or
-# is not on the device or of the type that the operator reads, raises CollageError(ERR_ARG) here; all other checks are the
-# library's.
+# is not on the current device or of the type that the operator reads, raises CollageError(ERR_ARG) here; all other checks are
+# the library's.
 
 def _refuse(where: str):
     raise CollageError(ERR_ARG, where)
 
 
 _BF16 = _F32 = _E4M3 = _I32 = _I64 = None           # torch's types, from the first operator on: the rest of this module does without torch
+_current_device = None
 
 
-def _operators() -> ctypes.CDLL:
-    """The library as the operators call it.  First of all in each of them."""
-    global _BF16, _F32, _E4M3, _I32, _I64
+def _operators():
+    """The library as the operators call it and the current device's number.  First of all in each of them."""
+    global _BF16, _F32, _E4M3, _I32, _I64, _current_device
     if _BF16 is None:
         import torch
         lib()
+        _current_device = torch.cuda.current_device if torch.cuda.is_available() else lambda: None
         _F32, _E4M3, _I32, _I64 = torch.float32, torch.float8_e4m3fn, torch.int32, torch.int64
         _BF16 = torch.bfloat16
-    return _packed
+    return _packed, _current_device()
 
 
 _pack_matrix = struct.Struct("QQQQ").pack          # collage_matrix_t: a third of the time that a ctypes structure takes
@@ -404,13 +406,13 @@ def _flat(t):
     return t.view(-1, cols) if cols else t.view(math.prod(lead), 0)
 
 
-def _matrix(t, dtype, where: str, required: bool = False):
+def _matrix(t, dtype, dev, where: str, required: bool = False):
     """collage_matrix_t of a tensor, packed, or None for None."""
     if t is None:
         if required:
             raise CollageError(ERR_NULL, where)
         return None
-    if t.dtype is not dtype or not t.is_cuda:
+    if t.dtype is not dtype or t.get_device() != dev:
         _refuse(where)
     shape = t.shape
     if len(shape) != 2:
@@ -437,23 +439,23 @@ def _extents(t):
     return shape if len(shape) == 2 else _flat(t).shape
 
 
-def _vector(t, dtype, length: int, where: str):
+def _vector(t, dtype, length: int, dev, where: str):
     """Address of a contiguous vector of that many elements, or None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda or t.numel() != length or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() != length or not t.is_contiguous():
         _refuse(where)
     return t.data_ptr()
 
 
 def add_rms_norm(x, residual, weight, eps: float, residual_out=None, y=None, y8=None, y8_scale=None, rstd=None, stream=None):
     """r = x + residual; y = r / sqrt(mean(r^2) + eps) * weight in bfloat16 (y) and / or in 8 bits (y8, y8_scale)."""
-    w, L = "collage_add_rms_norm", _operators()
-    mx = _matrix(x, _BF16, w, True)
+    w, (L, dev) = "collage_add_rms_norm", _operators()
+    mx = _matrix(x, _BF16, dev, w, True)
     rows, cols = _extents(x)
-    _check(L.collage_add_rms_norm(mx, _matrix(residual, _BF16, w), _vector(weight, _BF16, cols, w), eps,
-                                  _matrix(residual_out, _BF16, w), _matrix(y, _BF16, w), _matrix(y8, _E4M3, w),
-                                  _vector(y8_scale, _F32, rows, w), _vector(rstd, _F32, rows, w), _ptr(stream)), w)
+    _check(L.collage_add_rms_norm(mx, _matrix(residual, _BF16, dev, w), _vector(weight, _BF16, cols, dev, w), eps,
+                                  _matrix(residual_out, _BF16, dev, w), _matrix(y, _BF16, dev, w), _matrix(y8, _E4M3, dev, w),
+                                  _vector(y8_scale, _F32, rows, dev, w), _vector(rstd, _F32, rows, dev, w), _ptr(stream)), w)
 
 
 def rms_norm_workspace_bytes(cols: int) -> int:
@@ -462,78 +464,82 @@ def rms_norm_workspace_bytes(cols: int) -> int:
 
 def add_rms_norm_backward(dy, r, rstd, weight, dx, dweight, workspace, dresidual=None, stream=None):
     """Gradients of add_rms_norm: r is its residual_out (or x without a residual); dx or dweight may be None."""
-    w, L = "collage_add_rms_norm_backward", _operators()
-    mdy = _matrix(dy, _BF16, w, True)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    w, (L, dev) = "collage_add_rms_norm_backward", _operators()
+    mdy = _matrix(dy, _BF16, dev, w, True)
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            _refuse(w)
     rows, cols = _extents(dy)
-    _check(L.collage_add_rms_norm_backward(mdy, _matrix(r, _BF16, w), _vector(rstd, _F32, rows, w),
-                                           _vector(weight, _BF16, cols, w), _matrix(dresidual, _BF16, w),
-                                           _matrix(dx, _BF16, w), _vector(dweight, _BF16, cols, w), _ptr(workspace),
+    _check(L.collage_add_rms_norm_backward(mdy, _matrix(r, _BF16, dev, w), _vector(rstd, _F32, rows, dev, w),
+                                           _vector(weight, _BF16, cols, dev, w), _matrix(dresidual, _BF16, dev, w),
+                                           _matrix(dx, _BF16, dev, w), _vector(dweight, _BF16, cols, dev, w), _ptr(workspace),
                                            ws_bytes, _ptr(stream)), w)
 
 
 def quantize_rows(x, q, scale, stream=None):
     """q, scale: x in 8 bits (torch.float8_e4m3fn) with one float scale a row."""
-    w, L = "collage_quantize_rows", _operators()
-    mx = _matrix(x, _BF16, w, True)
-    _check(L.collage_quantize_rows(mx, _matrix(q, _E4M3, w), _vector(scale, _F32, _extents(x)[0], w), _ptr(stream)), w)
+    w, (L, dev) = "collage_quantize_rows", _operators()
+    mx = _matrix(x, _BF16, dev, w, True)
+    _check(L.collage_quantize_rows(mx, _matrix(q, _E4M3, dev, w), _vector(scale, _F32, _extents(x)[0], dev, w), _ptr(stream)), w)
 
 
 def gated_ffn(x, w_gate, w_up, h, gate=None, up=None, activation: int = ACT_SILU, stream=None):
     """h = act(x w_gate^T) * (x w_up^T); gate and up, if given, keep the two products for the backward pass."""
-    w, L = "collage_gated_ffn", _operators()
-    _check(L.collage_gated_ffn(_matrix(x, _BF16, w), _matrix(w_gate, _BF16, w), _matrix(w_up, _BF16, w), _matrix(h, _BF16, w),
-                               _matrix(gate, _BF16, w), _matrix(up, _BF16, w), activation, _ptr(stream)), w)
+    w, (L, dev) = "collage_gated_ffn", _operators()
+    _check(L.collage_gated_ffn(_matrix(x, _BF16, dev, w), _matrix(w_gate, _BF16, dev, w), _matrix(w_up, _BF16, dev, w), _matrix(h, _BF16, dev, w),
+                               _matrix(gate, _BF16, dev, w), _matrix(up, _BF16, dev, w), activation, _ptr(stream)), w)
 
 
 def gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dgate, dup, dx=None, dw_gate=None, dw_up=None, activation: int = ACT_SILU,
                        stream=None):
     """Gradients of gated_ffn; dgate and dup receive the gradients of the two products (they may be gate and up themselves)."""
-    w, L = "collage_gated_ffn_backward", _operators()
-    m = [_matrix(t, _BF16, w) for t in (dh, x, w_gate, w_up, gate, up, dgate, dup, dx, dw_gate, dw_up)]
+    w, (L, dev) = "collage_gated_ffn_backward", _operators()
+    m = [_matrix(t, _BF16, dev, w) for t in (dh, x, w_gate, w_up, gate, up, dgate, dup, dx, dw_gate, dw_up)]
     _check(L.collage_gated_ffn_backward(*m, activation, _ptr(stream)), w)
 
 
 def gated_ffn_e4m3(x8, x_scale, w_gate8, w_gate_scale, w_up8, w_up_scale, h, activation: int = ACT_SILU, stream=None):
     """gated_ffn on 8-bit operands with a scale for each token and each channel, as quantize_rows writes them."""
-    w, L = "collage_gated_ffn_e4m3", _operators()
-    mx, mg, mu = _matrix(x8, _E4M3, w, True), _matrix(w_gate8, _E4M3, w, True), _matrix(w_up8, _E4M3, w, True)
-    _check(L.collage_gated_ffn_e4m3(mx, _vector(x_scale, _F32, _extents(x8)[0], w), mg,
-                                    _vector(w_gate_scale, _F32, _extents(w_gate8)[0], w), mu,
-                                    _vector(w_up_scale, _F32, _extents(w_up8)[0], w), _matrix(h, _BF16, w), activation,
+    w, (L, dev) = "collage_gated_ffn_e4m3", _operators()
+    mx, mg, mu = _matrix(x8, _E4M3, dev, w, True), _matrix(w_gate8, _E4M3, dev, w, True), _matrix(w_up8, _E4M3, dev, w, True)
+    _check(L.collage_gated_ffn_e4m3(mx, _vector(x_scale, _F32, _extents(x8)[0], dev, w), mg,
+                                    _vector(w_gate_scale, _F32, _extents(w_gate8)[0], dev, w), mu,
+                                    _vector(w_up_scale, _F32, _extents(w_up8)[0], dev, w), _matrix(h, _BF16, dev, w), activation,
                                     _ptr(stream)), w)
 
 
-def _distill(logits, top_index, top_logits, temperature, where):
+def _distill(logits, top_index, top_logits, temperature, dev, where):
     """collage_distill_t, packed, and the number of rows."""
     if logits is None or top_index is None or top_logits is None:
         raise CollageError(ERR_NULL, where)
     dtype, index = logits.dtype, top_index.dtype
     if dtype not in (_BF16, _F32) or index not in (_I32, _I64):
         _refuse(where)
-    packed = (_matrix(logits, dtype, where) + _matrix(top_index, index, where) + _matrix(top_logits, _F32, where) +
+    packed = (_matrix(logits, dtype, dev, where) + _matrix(top_index, index, dev, where) + _matrix(top_logits, _F32, dev, where) +
               _pack_distill(DTYPE_BF16 if dtype is _BF16 else DTYPE_F32, 4 if index is _I32 else 8, temperature))
     return packed, _extents(logits)[0]
 
 
 def distill_loss(logits, top_index, top_logits, temperature: float, loss, lse=None, stream=None):
     """loss[i] = temperature^2 KL(teacher's renormalised top entries || softmax(logits / temperature)) for each row."""
-    w, L = "collage_distill_loss", _operators()
-    d, n = _distill(logits, top_index, top_logits, temperature, w)
-    _check(L.collage_distill_loss(d, _vector(loss, _F32, n, w), _vector(lse, _F32, n, w), _ptr(stream)), w)
+    w, (L, dev) = "collage_distill_loss", _operators()
+    d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
+    _check(L.collage_distill_loss(d, _vector(loss, _F32, n, dev, w), _vector(lse, _F32, n, dev, w), _ptr(stream)), w)
 
 
 def distill_loss_backward(logits, top_index, top_logits, temperature: float, lse, grad_loss, dlogits, stream=None):
     """dlogits from grad_loss (one value a row) and the lse of distill_loss; dlogits may be the logits' own array."""
-    w, L = "collage_distill_loss_backward", _operators()
-    d, n = _distill(logits, top_index, top_logits, temperature, w)
-    _check(L.collage_distill_loss_backward(d, _vector(lse, _F32, n, w), _vector(grad_loss, _F32, n, w),
-                                           _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
+    w, (L, dev) = "collage_distill_loss_backward", _operators()
+    d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
+    _check(L.collage_distill_loss_backward(d, _vector(lse, _F32, n, dev, w), _vector(grad_loss, _F32, n, dev, w),
+                                           _matrix(dlogits, logits.dtype, dev, w), _ptr(stream)), w)
 
 
 def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row_weight, loss, dlogits, stream=None):
     """loss[i] = row_weight[i] * the row's loss, and dlogits, in one pass; dlogits may be the logits' own array."""
-    w, L = "collage_distill_loss_and_grad", _operators()
-    d, n = _distill(logits, top_index, top_logits, temperature, w)
-    _check(L.collage_distill_loss_and_grad(d, _vector(row_weight, _F32, n, w), _vector(loss, _F32, n, w),
-                                           _matrix(dlogits, logits.dtype, w), _ptr(stream)), w)
+    w, (L, dev) = "collage_distill_loss_and_grad", _operators()
+    d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
+    _check(L.collage_distill_loss_and_grad(d, _vector(row_weight, _F32, n, dev, w), _vector(loss, _F32, n, dev, w),
+                                           _matrix(dlogits, logits.dtype, dev, w), _ptr(stream)), w)
