@@ -374,23 +374,29 @@ def read_edq(edq_dev) -> dict:
 # Operators of the forward and backward pass.  Matrices are CUDA tensors of two or more dimensions whose last one is
 # contiguous; leading dimensions are flattened into rows (a view, never a copy).  What a tensor cannot be described as, or
 # is not on the current device or of the type that the operator reads, raises CollageError(ERR_ARG) here; all other checks are
-# the library's.
+# the library's.  As everywhere in this module, stream=None is the device's default stream; torch's streams do not wait for that
+# one, so where another is current (torch.cuda.stream, a graph's capture) the operators want their stream named (ERR_ARG).
 
 def _refuse(where: str):
     raise CollageError(ERR_ARG, where)
 
 
 _BF16 = _F32 = _E4M3 = _I32 = _I64 = None           # torch's types, from the first operator on: the rest of this module does without torch
-_current_device = None
+_current_device = _current_stream = None
 
 
 def _operators():
     """The library as the operators call it and the current device's number.  First of all in each of them."""
-    global _BF16, _F32, _E4M3, _I32, _I64, _current_device
+    global _BF16, _F32, _E4M3, _I32, _I64, _current_device, _current_stream
     if _BF16 is None:
         import torch
         lib()
-        _current_device = torch.cuda.current_device if torch.cuda.is_available() else lambda: None
+        # (the plain numbers, without checks or objects around them, where torch gives them: 0.1 us in place of 1)
+        _current_device, _current_stream = lambda: None, lambda dev: 0
+        if torch.cuda.is_available():
+            torch.cuda.init()
+            _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         _F32, _E4M3, _I32, _I64 = torch.float32, torch.float8_e4m3fn, torch.int32, torch.int64
         _BF16 = torch.bfloat16
     return _packed, _current_device()
@@ -448,6 +454,17 @@ def _vector(t, dtype, length: int, dev, where: str):
     return t.data_ptr()
 
 
+def _stream(stream, dev, where: str):
+    """Address of a stream of the current device, or None for the default stream where that is torch's current one."""
+    if stream is None:
+        if _current_stream(dev):
+            _refuse(f"{where}: stream=None while torch's current stream is not the default one")
+        return None
+    if getattr(stream, "device_index", dev) != dev:
+        _refuse(f"{where}: a stream of another device")
+    return _ptr(stream)
+
+
 def add_rms_norm(x, residual, weight, eps: float, residual_out=None, y=None, y8=None, y8_scale=None, rstd=None, stream=None):
     """r = x + residual; y = r / sqrt(mean(r^2) + eps) * weight in bfloat16 (y) and / or in 8 bits (y8, y8_scale)."""
     w, (L, dev) = "collage_add_rms_norm", _operators()
@@ -455,7 +472,7 @@ def add_rms_norm(x, residual, weight, eps: float, residual_out=None, y=None, y8=
     rows, cols = _extents(x)
     _check(L.collage_add_rms_norm(mx, _matrix(residual, _BF16, dev, w), _vector(weight, _BF16, cols, dev, w), eps,
                                   _matrix(residual_out, _BF16, dev, w), _matrix(y, _BF16, dev, w), _matrix(y8, _E4M3, dev, w),
-                                  _vector(y8_scale, _F32, rows, dev, w), _vector(rstd, _F32, rows, dev, w), _ptr(stream)), w)
+                                  _vector(y8_scale, _F32, rows, dev, w), _vector(rstd, _F32, rows, dev, w), _stream(stream, dev, w)), w)
 
 
 def rms_norm_workspace_bytes(cols: int) -> int:
@@ -475,21 +492,21 @@ def add_rms_norm_backward(dy, r, rstd, weight, dx, dweight, workspace, dresidual
     _check(L.collage_add_rms_norm_backward(mdy, _matrix(r, _BF16, dev, w), _vector(rstd, _F32, rows, dev, w),
                                            _vector(weight, _BF16, cols, dev, w), _matrix(dresidual, _BF16, dev, w),
                                            _matrix(dx, _BF16, dev, w), _vector(dweight, _BF16, cols, dev, w), _ptr(workspace),
-                                           ws_bytes, _ptr(stream)), w)
+                                           ws_bytes, _stream(stream, dev, w)), w)
 
 
 def quantize_rows(x, q, scale, stream=None):
     """q, scale: x in 8 bits (torch.float8_e4m3fn) with one float scale a row."""
     w, (L, dev) = "collage_quantize_rows", _operators()
     mx = _matrix(x, _BF16, dev, w, True)
-    _check(L.collage_quantize_rows(mx, _matrix(q, _E4M3, dev, w), _vector(scale, _F32, _extents(x)[0], dev, w), _ptr(stream)), w)
+    _check(L.collage_quantize_rows(mx, _matrix(q, _E4M3, dev, w), _vector(scale, _F32, _extents(x)[0], dev, w), _stream(stream, dev, w)), w)
 
 
 def gated_ffn(x, w_gate, w_up, h, gate=None, up=None, activation: int = ACT_SILU, stream=None):
     """h = act(x w_gate^T) * (x w_up^T); gate and up, if given, keep the two products for the backward pass."""
     w, (L, dev) = "collage_gated_ffn", _operators()
     _check(L.collage_gated_ffn(_matrix(x, _BF16, dev, w), _matrix(w_gate, _BF16, dev, w), _matrix(w_up, _BF16, dev, w), _matrix(h, _BF16, dev, w),
-                               _matrix(gate, _BF16, dev, w), _matrix(up, _BF16, dev, w), activation, _ptr(stream)), w)
+                               _matrix(gate, _BF16, dev, w), _matrix(up, _BF16, dev, w), activation, _stream(stream, dev, w)), w)
 
 
 def gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dgate, dup, dx=None, dw_gate=None, dw_up=None, activation: int = ACT_SILU,
@@ -497,7 +514,7 @@ def gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dgate, dup, dx=None, dw_ga
     """Gradients of gated_ffn; dgate and dup receive the gradients of the two products (they may be gate and up themselves)."""
     w, (L, dev) = "collage_gated_ffn_backward", _operators()
     m = [_matrix(t, _BF16, dev, w) for t in (dh, x, w_gate, w_up, gate, up, dgate, dup, dx, dw_gate, dw_up)]
-    _check(L.collage_gated_ffn_backward(*m, activation, _ptr(stream)), w)
+    _check(L.collage_gated_ffn_backward(*m, activation, _stream(stream, dev, w)), w)
 
 
 def gated_ffn_e4m3(x8, x_scale, w_gate8, w_gate_scale, w_up8, w_up_scale, h, activation: int = ACT_SILU, stream=None):
@@ -507,7 +524,7 @@ def gated_ffn_e4m3(x8, x_scale, w_gate8, w_gate_scale, w_up8, w_up_scale, h, act
     _check(L.collage_gated_ffn_e4m3(mx, _vector(x_scale, _F32, _extents(x8)[0], dev, w), mg,
                                     _vector(w_gate_scale, _F32, _extents(w_gate8)[0], dev, w), mu,
                                     _vector(w_up_scale, _F32, _extents(w_up8)[0], dev, w), _matrix(h, _BF16, dev, w), activation,
-                                    _ptr(stream)), w)
+                                    _stream(stream, dev, w)), w)
 
 
 def _distill(logits, top_index, top_logits, temperature, dev, where):
@@ -526,7 +543,7 @@ def distill_loss(logits, top_index, top_logits, temperature: float, loss, lse=No
     """loss[i] = temperature^2 KL(teacher's renormalised top entries || softmax(logits / temperature)) for each row."""
     w, (L, dev) = "collage_distill_loss", _operators()
     d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
-    _check(L.collage_distill_loss(d, _vector(loss, _F32, n, dev, w), _vector(lse, _F32, n, dev, w), _ptr(stream)), w)
+    _check(L.collage_distill_loss(d, _vector(loss, _F32, n, dev, w), _vector(lse, _F32, n, dev, w), _stream(stream, dev, w)), w)
 
 
 def distill_loss_backward(logits, top_index, top_logits, temperature: float, lse, grad_loss, dlogits, stream=None):
@@ -534,7 +551,7 @@ def distill_loss_backward(logits, top_index, top_logits, temperature: float, lse
     w, (L, dev) = "collage_distill_loss_backward", _operators()
     d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
     _check(L.collage_distill_loss_backward(d, _vector(lse, _F32, n, dev, w), _vector(grad_loss, _F32, n, dev, w),
-                                           _matrix(dlogits, logits.dtype, dev, w), _ptr(stream)), w)
+                                           _matrix(dlogits, logits.dtype, dev, w), _stream(stream, dev, w)), w)
 
 
 def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row_weight, loss, dlogits, stream=None):
@@ -542,4 +559,4 @@ def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row
     w, (L, dev) = "collage_distill_loss_and_grad", _operators()
     d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
     _check(L.collage_distill_loss_and_grad(d, _vector(row_weight, _F32, n, dev, w), _vector(loss, _F32, n, dev, w),
-                                           _matrix(dlogits, logits.dtype, dev, w), _ptr(stream)), w)
+                                           _matrix(dlogits, logits.dtype, dev, w), _stream(stream, dev, w)), w)

@@ -107,3 +107,19 @@ def test_three_dimensions_without_columns():
     none = torch.empty(8, 0, dtype=BF16, device="cuda")
     B.gated_ffn(x, none, none, h)
     assert (h == 0).all()
+
+
+def test_the_operators_want_their_stream_named_beside_the_default_one():
+    x, q, scale = normal(1, 4, 64), torch.zeros(4, 64, dtype=E4M3, device="cuda"), torch.zeros(4, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with pytest.raises(B.CollageError) as e:
+            B.quantize_rows(x, q, scale)
+        assert e.value.status == B.ERR_ARG and "stream" in str(e.value)
+        B.quantize_rows(x, q, scale, stream=torch.cuda.current_stream())
+    side.synchronize()
+    assert (scale > 0).all()
+    with torch.cuda.stream(side):
+        B.quantize_rows(x, q, scale, stream=torch.cuda.default_stream())
+    torch.cuda.synchronize()

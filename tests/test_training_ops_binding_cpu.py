@@ -68,6 +68,7 @@ def calls(monkeypatch):
     c = Calls()
     monkeypatch.setattr(B, "_packed", c)
     monkeypatch.setattr(B, "_current_device", lambda: 0, raising=False)
+    monkeypatch.setattr(B, "_current_stream", lambda dev: 0, raising=False)
     return c
 
 
@@ -128,3 +129,25 @@ def test_a_workspace_with_gaps_is_refused(calls):
     with pytest.raises(B.CollageError) as e:
         f(*args[:6], Fake(*args[6].shape, dtype=torch.uint8, contiguous=False), **kwargs)
     assert e.value.status == B.ERR_ARG and calls.count == 0
+
+
+class FakeStream:
+    def __init__(self, address, device=0):
+        self.cuda_stream, self.device_index = address, device
+
+
+@pytest.mark.parametrize("name", OPERATORS)
+def test_the_stream_has_to_be_named_where_another_than_the_default_is_current(calls, monkeypatch, name):
+    f, args, kwargs = OPERATORS[name]
+    monkeypatch.setattr(B, "_current_stream", lambda dev: 0x5000, raising=False)
+
+    def refused(stream):
+        with pytest.raises(B.CollageError) as e:
+            f(*args, **kwargs, stream=stream)
+        assert e.value.status == B.ERR_ARG
+    refused(None)
+    refused(FakeStream(0x5000, device=1))
+    assert calls.count == 0
+    for stream in (FakeStream(0x5000), FakeStream(0), 0x5000, 0):      # the current one, the default one by its name, addresses
+        f(*args, **kwargs, stream=stream)
+    assert calls.count == 4
