@@ -121,6 +121,8 @@ def run(steps=60, tokens=512, width=256, ffn=640, layers=2, vocab=4099, top=16, 
     B.distill_loss(student.logits, at, tl, TEMPERATURE, loss)
     B.distill_loss(student.logits_in_8_bits(ids), at, tl, TEMPERATURE, loss8)
     B.plan_destroy(student.plan)
+    if code := B.pipeline_fault():                                                # (waits for the GPU: at the end, or at a checkpoint)
+        raise RuntimeError(f"a kernel gave up a wait (code {code}): weights and losses are undefined")
     return [x.item() for x in losses], loss.mean().item(), loss8.mean().item()
 
 
