@@ -7,6 +7,7 @@ from pathlib import Path
 import pytest
 import torch
 
+import test_gpu_training_ops as ops
 from ops_util import BF16, E4M3, U, close, normal
 from paper_2405_03637_b200 import binding as B
 
@@ -123,3 +124,44 @@ def test_the_operators_want_their_stream_named_beside_the_default_one():
     with torch.cuda.stream(side):
         B.quantize_rows(x, q, scale, stream=torch.cuda.default_stream())
     torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------- several turns of the kernels that walk over their work ---
+
+@pytest.mark.parametrize("rows,cols", [(25_000, 64), (6000, 1000), (1700, 4096), (750, 12_288), (750, 16_384)])
+def test_norm_backward_over_five_rows_a_group(rows, cols):
+    ops.test_norm_backward_matches_definition(rows, cols, 0, 0)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(700, 32_000, torch.float32), (700, 70_001, BF16), (80, 400_003, BF16)])
+def test_distillation_over_several_rows_a_cluster(rows, vocab, dtype):
+    z = normal(5, rows, vocab, std=2.0, dtype=dtype)
+    at, top = ops.teacher(6, rows, vocab, 24)
+    at[2::7] = -1                                            # rows without entries, and rows that weigh nothing, between others
+    weight = torch.linspace(0.5, 1.5, rows, device="cuda")
+    weight[::5] = 0
+    ops.check_distill(z, at, top, 2.0, weight)
+
+
+# 74 pairs of blocks: tiles for more than three turns, in the forward pass, in dx or in the weight gradients, with few and many
+# blocks of K, and more than eight rows of tiles with an incomplete last group
+@pytest.mark.parametrize("tokens,width,ffn", [(4900, 136, 2056), (4095, 1032, 2056), (4095, 4104, 264), (1300, 2056, 4104)])
+def test_feed_forward_over_several_tiles_a_pair(tokens, width, ffn):
+    ops.test_gated_forward_and_backward_match_definition(tokens, width, ffn, 0, 0, B.ACT_SILU)
+
+
+@pytest.mark.parametrize("tokens,width,ffn", [(4900, 144, 2064), (4095, 1040, 2064)])
+def test_feed_forward_in_8_bits_over_several_tiles_a_pair(tokens, width, ffn):
+    ops.test_gated_8_bits_matches_definition(tokens, width, ffn, 0, 0)
+
+
+def test_many_tiles_give_the_same_bits_again():
+    launch, o = ops.one_of_each(tokens=4900, width=1032, ffn=2056, vocab=4099)
+    launch()
+    first = ops.bits_of(o)
+    for _ in range(3):
+        for v in o.values():
+            v.view(torch.uint8).zero_()
+        launch()
+        now = ops.bits_of(o)
+        assert all(torch.equal(first[k], now[k]) for k in first) and B.pipeline_fault() == 0
