@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kAnyThreads) any_kernel(const __grid_constant_
         const uint32_t smem0 = umma::smem_addr(smem);
         bool ok = true;
         for (uint32_t kb = begin; kb < end; ++kb) {
-            if (!(ok = pipe::mbar_wait(&full[stage], phase, 221, &g_product_fault))) break;
+            if (!(ok = umma::warp_wait(&full[stage], phase, 221, &g_product_fault))) break;
             umma::fence_after();
             const uint32_t sa = smem0 + stage * kBytes;
             const uint64_t da = umma::operand_desc(sa, 16, 1024), db = umma::operand_desc(sa + kOperandBytes, 16, 1024);
@@ -130,7 +130,8 @@ __global__ void __launch_bounds__(kAnyThreads) any_kernel(const __grid_constant_
             __syncwarp();
             if (++stage == kAnyStages) { stage = 0; phase ^= 1; }
         }
-        if (ok) pipe::mbar_wait(&done, 0, 222, &g_product_fault);
+        if (!ok && umma::elected()) umma::commit<1>(&done);        // of what has been issued
+        umma::warp_wait(&done, 0, 222, &g_product_fault);
     }
     finish_slim_tile<E4M3, GATED, NT, false>(p, smem, tmem, rank, t0, i0);
 }

@@ -169,9 +169,10 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
     const uint32_t tmem = tmem_slot;
 
     if (warp == 0) {
-        uint32_t stage = 0, phase = 0;
+        uint32_t stage = 0, phase = 0, used = 0;
         for (uint32_t kb = begin; kb < end; ++kb) {
-            if (!pipe::mbar_wait(&empty[stage], phase ^ 1, 210, &g_product_fault)) break;
+            if (!umma::warp_wait(&empty[stage], phase ^ 1, 210, &g_product_fault)) break;
+            used = min(used + 1, stages);
             if (umma::elected()) {
                 pipe::mbar_arrive_expect_tx(&full[stage], kBytes);
                 const uint32_t bar = umma::smem_addr(&full[stage]);
@@ -195,12 +196,18 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
             __syncwarp();
             if (++stage == stages) { stage = 0; phase ^= 1; }
         }
+        // no copy is under way when the stages are given up, even where the multiplying warp has given up a wait
+        for (uint32_t i = 0; i < used; ++i) {
+            stage = stage ? stage - 1 : stages - 1;
+            if (stage == stages - 1) phase ^= 1;
+            umma::warp_wait(&full[stage], phase, 213, &g_product_fault);
+        }
     } else if (warp == 1) {
         uint32_t stage = 0, phase = 0;
         const uint32_t smem0 = umma::smem_addr(smem);
         bool ok = true;
         for (uint32_t kb = begin; kb < end; ++kb) {
-            if (!(ok = pipe::mbar_wait(&full[stage], phase, 211, &g_product_fault))) break;
+            if (!(ok = umma::warp_wait(&full[stage], phase, 211, &g_product_fault))) break;
             umma::fence_after();
             const uint32_t sa = smem0 + stage * kBytes;
             const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024), db = umma::operand_desc(sa + kOperandBytes, B_MN ? kOperandBytes / 2 : 16, 1024);
@@ -214,7 +221,8 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
             __syncwarp();
             if (++stage == stages) { stage = 0; phase ^= 1; }
         }
-        if (ok) pipe::mbar_wait(&done, 0, 212, &g_product_fault);
+        if (!ok && umma::elected()) umma::commit<1>(&done);        // of what has been issued
+        umma::warp_wait(&done, 0, 212, &g_product_fault);
     }
     finish_slim_tile<E4M3, GATED, NT, true>(p, smem, tmem, rank, t0, i0, which);
 }

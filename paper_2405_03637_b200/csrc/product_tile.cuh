@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const TilePlace at = place_of(p, tile);
             const int m0 = static_cast<int>(at.m * 128 * CTAS + rank * 128), n0 = static_cast<int>(at.n * kOut);
             for (uint32_t kb = 0; kb < blocks; ++kb) {
-                if (!(ok = pipe::mbar_wait(&bars->empty[stage], phase ^ 1, 200, &g_product_fault))) break;
+                if (!(ok = umma::warp_wait(&bars->empty[stage], phase ^ 1, 200, &g_product_fault))) break;
                 if (umma::elected()) {
                     if (rank == 0) pipe::mbar_arrive_expect_tx(&bars->full[stage], kStageBytes * CTAS);
                     const uint32_t bar = umma::cluster_addr(&bars->full[stage], 0);
@@ -159,23 +159,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
         }
-        // the last uses of the stages: nothing arrives in this block any more once they are over
-        for (uint32_t i = 0; i < used && ok; ++i) {
+        // The last uses of the stages: nothing arrives in this block any more once they are over.  After a wait that was given up
+        // they may never be; then the copies themselves are waited for: both blocks' by the first block, on whose barriers they are
+        // counted, and a millisecond by the second, for what it has sent for beyond those.
+        for (uint32_t i = 0; i < used; ++i) {
             stage = stage ? stage - 1 : kStages - 1;
             if (stage == kStages - 1) phase ^= 1;
-            ok = pipe::mbar_wait(&bars->empty[stage], phase, 201, &g_product_fault);
+            if (ok) ok = umma::warp_wait(&bars->empty[stage], phase, 201, &g_product_fault);
+            if (!ok && rank == 0) umma::warp_wait(&bars->full[stage], phase, 206, &g_product_fault);
         }
+        if (!ok && rank == 1)
+            for (const unsigned long long t0 = pipe::global_ns(); pipe::global_ns() - t0 < 1000000;) {}
     } else if (warp == 1) {
-        uint32_t stage = 0, phase = 0, n_tile = 0;
+        uint32_t stage = 0, phase = 0, n_tile = 0, committed = 0;
         bool ok = rank == 0;
         const uint32_t smem0 = umma::smem_addr(smem);
         for (uint32_t tile = first; tile < tiles && ok; tile += step, ++n_tile) {
             const uint32_t acc = n_tile & 1;
-            if (!(ok = pipe::mbar_wait(&bars->drained[acc], ((n_tile >> 1) & 1) ^ 1, 202, &g_product_fault))) break;
+            if (!(ok = umma::warp_wait(&bars->drained[acc], ((n_tile >> 1) & 1) ^ 1, 202, &g_product_fault))) break;
             umma::fence_after();
             const uint32_t d = tmem + acc * kN;
             for (uint32_t kb = 0; kb < blocks; ++kb) {
-                if (!(ok = pipe::mbar_wait(&bars->full[stage], phase, 203, &g_product_fault))) break;
+                if (!(ok = umma::warp_wait(&bars->full[stage], phase, 203, &g_product_fault))) {
+                    if (umma::elected()) umma::commit<CTAS>(&bars->done[acc]);      // of what has been issued
+                    break;
+                }
                 umma::fence_after();
                 const uint32_t sa = smem0 + stage * kStageBytes, sb = sa + kOperandBytes;
                 const uint64_t da = umma::operand_desc(sa, A_MN ? kOperandBytes / 2 : 16, 1024);
@@ -191,7 +199,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 __syncwarp();
                 if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
+            ++committed;
         }
+        // no matrix instruction is under way when operands and accumulators are given up
+        if (committed) umma::warp_wait(&bars->done[(committed - 1) & 1], ((committed - 1) >> 1) & 1, 205, &g_product_fault);
     } else if (warp >= 4) {
         // Two warps for each quarter of the rows (the quarter of tensor memory that a warp can read is its number's), each
         // with half of the columns.  A warp stages and stores its 32 rows by itself.
@@ -221,8 +232,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         };
         for (uint32_t tile = first; tile < tiles; tile += step, ++n_tile) {
             const uint32_t acc = n_tile & 1;
-            if (!pipe::mbar_wait(&bars->done[acc], (n_tile >> 1) & 1, 204, &g_product_fault)) break;
-            __syncwarp();
+            if (!umma::warp_wait(&bars->done[acc], (n_tile >> 1) & 1, 204, &g_product_fault)) break;
             umma::fence_after();
             const TilePlace at = place_of(p, tile);
             const int m0 = static_cast<int>(at.m * 128 * CTAS + rank * 128 + quarter * 32);

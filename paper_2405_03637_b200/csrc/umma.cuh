@@ -127,6 +127,10 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
+// A bounded wait by a whole warp: the same answer in all its threads, so that they leave a loop together.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned int who, unsigned int* fault_word) {
+    return __all_sync(0xFFFFFFFFu, pipe::mbar_wait(bar, parity, who, fault_word));
+}
 // One thread of a warp whose threads are together.
 __device__ __forceinline__ bool elected() {
     uint32_t r;
