@@ -143,7 +143,7 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
     extern __shared__ uint8_t raw_smem[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
     __shared__ uint64_t full[kMaxSlimStages], empty[kMaxSlimStages], done;
-    __shared__ uint32_t tmem_slot;
+    __shared__ uint32_t tmem_slot, lost;             // lost: a wait was given up
     const uint32_t warp = threadIdx.x >> 5;
     static_assert(!B_MN || NT % 64 == 0, "an operand stored by its index comes in boxes of 64 indexes");
     // with several outputs (B_MN) the tiles of the first come first
@@ -160,6 +160,7 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
         }
         pipe::mbar_init(&done, 1);
         pipe::mbar_init_fence();
+        lost = 0;
     }
     if (warp == 2) umma::tmem_alloc<1>(&tmem_slot, NT < 32 ? 32 : NT);
     umma::fence_before();
@@ -168,11 +169,13 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
     after_previous();
     const uint32_t tmem = tmem_slot;
 
+    uint32_t stage = 0, phase = 0, kb = begin;
     if (warp == 0) {
-        uint32_t stage = 0, phase = 0, used = 0;
-        for (uint32_t kb = begin; kb < end; ++kb) {
-            if (!umma::warp_wait(&empty[stage], phase ^ 1, 210, &g_product_fault)) break;
-            used = min(used + 1, stages);
+        for (; kb < end; ++kb) {
+            if (!umma::warp_wait(&empty[stage], phase ^ 1, 210, &g_product_fault)) {
+                lost = 1;
+                break;
+            }
             if (umma::elected()) {
                 pipe::mbar_arrive_expect_tx(&full[stage], kBytes);
                 const uint32_t bar = umma::smem_addr(&full[stage]);
@@ -196,17 +199,10 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
             __syncwarp();
             if (++stage == stages) { stage = 0; phase ^= 1; }
         }
-        // no copy is under way when the stages are given up, even where the multiplying warp has given up a wait
-        for (uint32_t i = 0; i < used; ++i) {
-            stage = stage ? stage - 1 : stages - 1;
-            if (stage == stages - 1) phase ^= 1;
-            umma::warp_wait(&full[stage], phase, 213, &g_product_fault);
-        }
     } else if (warp == 1) {
-        uint32_t stage = 0, phase = 0;
         const uint32_t smem0 = umma::smem_addr(smem);
         bool ok = true;
-        for (uint32_t kb = begin; kb < end; ++kb) {
+        for (; kb < end; ++kb) {
             if (!(ok = umma::warp_wait(&full[stage], phase, 211, &g_product_fault))) break;
             umma::fence_after();
             const uint32_t sa = smem0 + stage * kBytes;
@@ -222,9 +218,17 @@ __device__ __forceinline__ void slim_tile(const SlimArgs& p, uint32_t tile, uint
             if (++stage == stages) { stage = 0; phase ^= 1; }
         }
         if (!ok && umma::elected()) umma::commit<1>(&done);        // of what has been issued
-        umma::warp_wait(&done, 0, 212, &g_product_fault);
+        if (!umma::warp_wait(&done, 0, 212, &g_product_fault) || !ok) lost = 1;
     }
     finish_slim_tile<E4M3, GATED, NT, true>(p, smem, tmem, rank, t0, i0, which);
+    // Where a wait was given up, copies may still be under way that nobody has waited for, the last uses of the stages: the block
+    // stays until they have come.
+    if (warp == 0 && lost)
+        for (uint32_t used = min(kb - begin, stages); used > 0; --used) {
+            stage = stage ? stage - 1 : stages - 1;
+            if (stage == stages - 1) phase ^= 1;
+            umma::warp_wait(&full[stage], phase, 213, &g_product_fault);
+        }
 }
 
 template <bool E4M3, bool A_MN, bool GATED, int NT>
