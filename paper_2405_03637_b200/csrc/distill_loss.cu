@@ -184,7 +184,7 @@ struct DistillShared {
     float2 part[kMaxCluster];          // (maximum, sum) of each block of the cluster
     float loss[kMaxCluster];
     int any_there;
-    float log_psum, most;
+    float log_psum;
 };
 
 // Waits until at most `groups` of this thread's copy groups are under way (or 7, where more may be).

@@ -154,23 +154,13 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Barrier of `threads` threads; true in all of them if `ok` was true in all of them.
-__device__ __forceinline__ bool named_all(int id, int threads, bool ok) {
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %3, 0;\n\tbarrier.cta.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r)
-                 : "r"(id), "r"(threads), "r"(static_cast<uint32_t>(ok))
-                 : "memory");
-    return r != 0;
-}
-// The same for threads of a warp that may have parted ways.
+// The same for threads of a warp that may have parted ways, as arrival and wait or both.
 __device__ __forceinline__ void cluster_arrive_all() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait_all() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync_any() {
     cluster_arrive_all();
     cluster_wait_all();
 }
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 }  // namespace umma
 }  // namespace collage
