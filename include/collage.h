@@ -397,7 +397,9 @@ collage_status_t collage_selftest(uint64_t out_host[6], void* stream);
  * Errors common to all: ERR_NULL (a required pointer), ERR_ARG (shapes that do not fit together, ld < cols,
  * misaligned elements, values out of range), ERR_LIMIT, ERR_ALIAS, ERR_ARCH, ERR_CUDA.
  * All of them only launch kernels (and clear small arrays) on `stream` and may be recorded by stream capture.  A kernel's
- * blocks may be set up while the stream's previous kernel still runs; it touches memory only after that one's end. */
+ * blocks may be set up while the stream's previous kernel still runs; it touches memory only after that one's end.
+ * The feed-forward products wait with a bound, as the step does: one that gives up has long returned COLLAGE_OK, and only
+ * collage_pipeline_fault tells that its outputs are undefined.  Ask it where a training loop reads its losses or saves. */
 typedef struct collage_matrix {
     void* data;
     uint64_t rows, cols;
@@ -414,7 +416,9 @@ typedef struct collage_matrix {
  *                 collage_quantize_rows, y ~ y8 * y8_scale.  At least one of y and y8 is given.
  *   rstd        : DEVICE float[rows] or NULL (the backward pass needs it).  NaN in rows of no columns.
  * residual_out may be the array of x or of residual, y that of x (same data, same ld).
- * A row that holds a NaN or an infinity gives NaNs (IEEE arithmetic). */
+ * A row that holds a NaN gives NaNs; one that holds an infinity has rstd 0, NaN where the infinity is and zeros elsewhere
+ * (IEEE arithmetic).  Squares are held to a float's precision whatever their size: finite rows may have values up to the
+ * type's largest, and with eps = 0 any rows of which 1 / rms is a float. */
 collage_status_t collage_add_rms_norm(const collage_matrix_t* x, const collage_matrix_t* residual, const void* weight,
                                       double eps, const collage_matrix_t* residual_out, const collage_matrix_t* y,
                                       const collage_matrix_t* y8, float* y8_scale, float* rstd, void* stream);

@@ -376,6 +376,8 @@ def read_edq(edq_dev) -> dict:
 # is not on the current device or of the type that the operator reads, raises CollageError(ERR_ARG) here; all other checks are
 # the library's.  As everywhere in this module, stream=None is the device's default stream; torch's streams do not wait for that
 # one, so where another is current (torch.cuda.stream, a graph's capture) the operators want their stream named (ERR_ARG).
+# They read and write through addresses: autograd records nothing of them (the backward functions are called by hand or from a
+# torch.autograd.Function), and tensors written in the place of others, such as dgate over gate, change without its knowledge.
 
 def _refuse(where: str):
     raise CollageError(ERR_ARG, where)

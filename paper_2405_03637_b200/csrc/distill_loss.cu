@@ -793,7 +793,7 @@ static collage_status_t launch_staged_as(const DistillArgs& a, uint64_t rows, in
     return launch<&distill_staged_kernel<T, THREADS, BLOCKS>>(groups * a.cluster, THREADS + 32, a.cluster, smem, s, a, rows);
 }
 // Threads by the slice's vectors: about twenty each of the longest; short rows by smaller blocks, more of them on an SM.  Rows of
-// which only two fit an SM are still faster whole than halved over a cluster: 1306 x 100352 127 us against 173.
+// which only two fit an SM are still faster whole than halved over a cluster: 1306 x 100352 129 us against 173.
 template <typename T>
 static collage_status_t launch_staged(const DistillArgs& a, uint64_t rows, int sm_count, cudaStream_t s) {
     return a.slice <= 512    ? launch_staged_as<T, 64, 8>(a, rows, sm_count, s)
@@ -802,7 +802,7 @@ static collage_status_t launch_staged(const DistillArgs& a, uint64_t rows, int s
                                                      : launch_staged_as<T, 384, 2>(a, rows, sm_count, s);
 }
 
-// Short rows by smaller blocks, more of them on an SM: 16384 x 4000 backward 87 us by 128 threads, 153 by 256.
+// Short rows by smaller blocks, more of them on an SM: 16384 x 4000 backward 82 us by 128 threads, 122 by 256; the loss 43 and 76.
 template <typename T, int MODE>
 static collage_status_t launch_streamed(const DistillArgs& a, uint64_t rows, cudaStream_t s) {
     const size_t smem = 12ull * a.k;
@@ -836,7 +836,7 @@ static collage_status_t launch_distill(DistillArgs& a, uint64_t rows, collage_dt
         }
         a.cluster = 1;
     }
-    spread(4, 512);                      // (115 x 71270 float: loss 22 -> 13 us, backward 27 -> 18 us, against one for each SM)
+    spread(4, 512);                      // (115 x 71270 float: loss 14 us, backward 17; 22 and 24 with one block for each SM)
     return bf16 ? launch_streamed<uint16_t, MODE>(a, rows, s) : launch_streamed<float, MODE>(a, rows, s);
 }
 

@@ -121,7 +121,7 @@ static collage_status_t launch_slim_as(SlimArgs& t, uint64_t blocks, int sm_coun
 static uint32_t most_split(uint32_t blocks) { return blocks >= 64 ? 8 : blocks >= 32 ? 4 : blocks >= 16 ? 2 : 1; }
 
 // Tokens of a slim tile: all of them up to 128, fewer where even with K split a third of the SMs would be left without a tile
-// (there are `weight_tiles` for each tile of tokens).  333 x 768 x 2048 forward: 10.8 us with 64 tokens, 13.3 with 128; but its dx, whose K
+// (there are `weight_tiles` for each tile of tokens).  333 x 768 x 2048 forward: 10.9 us with 64 tokens, 14.4 with 128; but its dx, whose K
 // can be split, loses by narrow tiles, which read the weights more often (160 x 4096 x 11008: 120 us against 55).
 static uint32_t slim_tokens(uint64_t tokens, uint64_t weight_tiles, uint32_t blocks, int sm_count) {
     uint32_t nt = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
@@ -217,8 +217,8 @@ static bool slim_dx_args(SlimArgs& t, uint32_t& nt, const collage_matrix_t* dgat
            make_map(&t.b[0], dgate, false, 64, nt, false) && make_map(&t.b[1], dup, false, 64, nt, false);
 }
 
-// Both gradients in one launch pay where each is bound by its latencies: 333 x 768 x 2048 backward 20.5 us against 25.5, 2 x 1512 x
-// 2136 19 against 23.6; but 1000 x 1024 x 2816 49 against 42, whose weight gradients the pairs' tiles make faster.
+// Both gradients in one launch pay where each is bound by its latencies: 333 x 768 x 2048 backward 21.0 us against 28.4, 2 x 1512 x
+// 2136 19.6 against 22.4; but 1000 x 1024 x 2816 49 against 43, whose weight gradients the pairs' tiles make faster.
 static bool small_layer(uint64_t tokens, const collage_matrix_t* dw, int sm_count) {
     return tokens <= 512 && 2 * ((dw->rows + 127) / 128) * ((dw->cols + 127) / 128) <= 3ull * sm_count;
 }

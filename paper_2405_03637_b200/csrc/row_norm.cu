@@ -5,9 +5,11 @@
 //   scale = max |y| / 448,  y8 = e4m3(y / scale)
 //
 // All of it is bound by memory: a row is read once, kept in registers until its sum (and maximum) is known, and written.
-// Measured at 8191 x 4096: forward 40.8 us (6.6 TB/s, the rate of a copy), with 8-bit output 37.2 us (6.3), backward with both
-// gradients 46.6 us (5.8 TB/s); quantise 11008 x 4096 24.5 us (5.5 TB/s).  r is rounded once for the residual stream and once
-// more read by the backward pass; y is computed before that rounding.
+// Measured at 8191 x 4096: forward 40.9 us (6.6 TB/s, the rate of a copy), with 8-bit output 38.4 us (6.1), backward with both
+// gradients 47.3 us (5.7 TB/s); quantise 11008 x 4096 24.8 us (5.5 TB/s).
+// r is rounded to bfloat16 for the residual stream, and it is those values that the backward pass reads, while y and rstd belong
+// to r before the rounding.  A training program keeps no second copy of the stream; dx and dweight carry the rounding (2.2e-3
+// from the definition in the relative 2-norm at 8191 x 4096, 1.7e-3 with r in float).
 #include "ops_common.cuh"
 
 namespace collage {
@@ -34,7 +36,8 @@ constexpr int kRowThreads = 256;
 __device__ __forceinline__ bool squares_fit(float mean) { return mean > 0x1p-100f && mean < INFINITY; }
 __device__ __forceinline__ float rescue_factor(float mean) { return mean > 1.0f ? 0x1p-80f : 0x1p80f; }
 
-// One block per row, element by element, the row read again for each stage: any length, stride and alignment.
+// One block per row, element by element, the row read again for each stage: any length, stride and alignment.  8191 x 4097 forward
+// 74 us (3.6 TB/s), to 8 bits 96 us; quantise 51 us (2.0 TB/s): the loads of two bytes bound it.
 template <bool NORM>
 __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_constant__ RowArgs a) {
     __shared__ float slots[kRowThreads / 32];
@@ -425,7 +428,9 @@ static unsigned launch_backward_as(const RowBackwardArgs& a, int sm_count, cudaS
     return st == COLLAGE_OK ? grid : 0;
 }
 // Returns the number of partial rows of dweight, 0 after an error.  Rows of up to 256 columns are a warp's, without barriers;
-// longer ones take two vectors a thread (half the barriers and joins of one: 50 against 58 us at 8191 x 4096).
+// longer ones take two vectors a thread (half the barriers and joins of one: 50 against 58 us at 8191 x 4096).  Beyond 8192 columns
+// a block of 768 or 1024 threads has too few registers for that and spills 88 and 180 bytes: 4096 x 12288 104 us (3.9 TB/s), 2048 x
+// 16384 89 us (3.0), against 262 and 182 element by element (12289 and 16383 columns).
 static unsigned launch_backward(const RowBackwardArgs& a, int sm_count, cudaStream_t s) {
     const uint64_t v = a.cols >> 3;
     return v <= 32 ? launch_backward_as<1, 512>(a, sm_count, s)
