@@ -503,7 +503,9 @@ typedef struct collage_distill {
 } collage_distill_t;
 #define COLLAGE_DISTILL_MAX_TOP 1024
 
-/* loss: DEVICE float[rows].  lse: DEVICE float[rows] or NULL: log sum_j exp(logits_ij / t), for the backward call. */
+/* loss: DEVICE float[rows].  lse: DEVICE float[rows] or NULL: log sum_j exp(logits_ij / t), for the backward call.  What its
+ * rounding to float takes, 2^-24 of its size, comes back twice as the relative error of q there; where that would pass 2^-17 (lse of 128 or
+ * more) the backward call takes maximum and sum from the row itself. */
 collage_status_t collage_distill_loss(const collage_distill_t* in, float* loss, float* lse, void* stream);
 /* grad_loss: DEVICE float[rows], g_i.  dlogits: [rows, vocab] in logits_dtype; may be the array of logits. */
 collage_status_t collage_distill_loss_backward(const collage_distill_t* in, const float* lse, const float* grad_loss,
