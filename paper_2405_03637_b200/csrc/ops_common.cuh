@@ -158,6 +158,20 @@ __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
 }
 __device__ __forceinline__ uint8_t to_e4m3(float f) { return static_cast<uint8_t>(__nv_cvt_float_to_fp8(f, __NV_SATFINITE, __NV_E4M3)); }
 
+__device__ __forceinline__ void unpack8(const uint4& q, float (&f)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// Squares leave a float's range beyond 2^64 and lose digits below 2^-63.  Where the mean of a row's squares (and eps) shows that, the
+// row is taken times a power of two, and its sum again.
+__device__ __forceinline__ bool squares_fit(float mean) { return mean > 0x1p-100f && mean < INFINITY; }
+__device__ __forceinline__ float rescue_factor(float mean) { return mean > 1.0f ? 0x1p-80f : 0x1p80f; }
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);

@@ -31,11 +31,6 @@ struct RowArgs {
 
 constexpr int kRowThreads = 256;
 
-// Squares leave a float's range beyond 2^64 and lose digits below 2^-63.  Where the mean of a row's squares (and eps) shows that, the
-// row is taken times a power of two, and its sum again.
-__device__ __forceinline__ bool squares_fit(float mean) { return mean > 0x1p-100f && mean < INFINITY; }
-__device__ __forceinline__ float rescue_factor(float mean) { return mean > 1.0f ? 0x1p-80f : 0x1p80f; }
-
 // One block per row, element by element, the row read again for each stage: any length, stride and alignment.  8191 x 4097 forward
 // 74 us (3.6 TB/s), to 8 bits 96 us; quantise 51 us (2.0 TB/s): the loads of two bytes bound it.
 template <bool NORM>
@@ -78,15 +73,6 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
         if (a.y) a.y[row * a.ldy + j] = to_bf16(y);
         if (a.y8) a.y8[row * a.ldy8 + j] = scale == 0.0f ? 0 : to_e4m3(y / scale);
     }
-}
-
-__device__ __forceinline__ void unpack8(const uint4& q, float (&f)[8]) {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 
 // Rows of whole 16-byte vectors, read once and kept in registers: PER vectors a thread, a row by one warp (WARP: four rows a
