@@ -516,6 +516,176 @@ collage_status_t collage_distill_loss_backward(const collage_distill_t* in, cons
 collage_status_t collage_distill_loss_and_grad(const collage_distill_t* in, const float* row_weight, float* loss,
                                                const collage_matrix_t* dlogits, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Norms around a block.  A block's output o joins the stream x, normed, gated and scaled, and the stream is normed for the next
+ * block; both norms, the gate and either scale are optional:
+ *   n = o / sqrt(mean_j o^2 + eps) * post_weight      (o without post_weight)
+ *   r = residual_scale * x + block_scale * A(gate) * n     (without the factor A where there is no gate)
+ *   y = r / sqrt(mean_j r^2 + eps) * pre_weight
+ * in the arithmetic of the section above, whose rules on matrices, overlaps, errors, streams and capture hold here too. */
+typedef enum {
+    COLLAGE_GATE_NONE = 0,       /* A(g) = g                    */
+    COLLAGE_GATE_SIGMOID = 1,    /* A(g) = 1 / (1 + exp(-g))    */
+    COLLAGE_GATE_SILU = 2        /* A(g) = g / (1 + exp(-g))    */
+} collage_gate_activation_t;
+typedef struct collage_block_norm {
+    collage_matrix_t block;          /* o: bfloat16 [rows, cols]                                            */
+    collage_matrix_t gate;           /* bfloat16: [rows, cols], [1, cols] (one for each channel), or data NULL: none */
+    const void* post_weight;         /* DEVICE bfloat16[cols], or NULL: no norm after the block            */
+    const void* pre_weight;          /* DEVICE bfloat16[cols], or NULL: no norm before the next one        */
+    double eps;                      /* >= 0 and finite                                                      */
+    double residual_scale, block_scale;    /* finite in float                                                */
+    collage_gate_activation_t activation;
+} collage_block_norm_t;
+
+/*   x       : bfloat16 [rows, cols].    r: bfloat16 [rows, cols], the new stream, rounded.  It may be the array of x or of o.
+ *   y       : bfloat16 [rows, cols] or NULL, from r as it was before that rounding; may be the array of o.
+ *   y8, y8_scale: y in e4m3 with a scale a row as in collage_add_rms_norm, or both NULL.  y and y8 need pre_weight.
+ *   rstd_post, rstd_pre: DEVICE float[rows] or NULL: 1 / rms of o and of r for the backward pass, each only with its weight.
+ * Rows of large, small or non-finite values: as in collage_add_rms_norm, for both norms. */
+collage_status_t collage_block_norm(const collage_block_norm_t* in, const collage_matrix_t* x, const collage_matrix_t* r,
+                                    const collage_matrix_t* y, const collage_matrix_t* y8, float* y8_scale, float* rstd_post,
+                                    float* rstd_pre, void* stream);
+
+/* Its backward pass; `in` as in the forward call (eps is not used).
+ *   dy      : bfloat16 [rows, cols], gradient of y, or NULL: none came that way (pre_weight, r and rstd_pre are then not used).
+ *   dr      : bfloat16 [rows, cols], gradient that reached r on its own way, or NULL.  One of dy and dr is given.
+ *   r, rstd_post, rstd_pre: of the forward call; rstd_post with post_weight only.
+ *   dx, dblock: bfloat16 [rows, cols] or NULL: gradients of x and o.  Either may be the array of dy or of dr.
+ *   dgate   : bfloat16, shaped like the gate, or NULL; for a gate of channels the sum over the rows.
+ *   dpost_weight, dpre_weight: DEVICE bfloat16[cols] or NULL.  (Sums over no rows are zeros.)
+ *   workspace: DEVICE scratch of at least collage_block_norm_workspace_bytes(cols), 16-byte aligned, needed with dpost_weight,
+ *             dpre_weight or the gradient of a gate of channels; nothing in it is kept between calls (ERR_WORKSPACE).
+ * A gradient of 8-bit outputs passes straight through. */
+size_t collage_block_norm_workspace_bytes(uint64_t cols);
+collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
+                                             const collage_matrix_t* r, const float* rstd_post, const float* rstd_pre,
+                                             const collage_matrix_t* dx, const collage_matrix_t* dblock, const collage_matrix_t* dgate,
+                                             void* dpost_weight, void* dpre_weight, void* workspace, size_t workspace_bytes,
+                                             void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Losses on the log-probabilities of sampled tokens: what a token had under the model, the clipped policy objective with a
+ * KL term, and the preference loss of pairs of answers.  The rules of the sections above hold.
+ *   logp_i = z_iy - log sum_j exp(z_ij),   z = logits / temperature, y = target_i
+ * A row whose target is negative or not below vocab is a prompt or padding: its logits are not read, its logp is 0 and its gradient zeros.
+ * Rows are taken relative to their largest logit: only differences within a row count, at any size of the logits; entries of
+ * -infinity have no probability.  NaN and infinity otherwise propagate per IEEE 754. */
+typedef struct collage_tokens {
+    collage_matrix_t logits;         /* [rows, vocab] in logits_dtype                                       */
+    const void* target;              /* DEVICE int32_t[rows] or int64_t[rows] (target_bytes = 4 or 8)       */
+    collage_dtype_t logits_dtype;
+    uint32_t target_bytes;
+    double temperature;              /* > 0 and finite, as is 1 / (temperature ln 2), in float (ERR_ARG)    */
+} collage_tokens_t;
+
+/* logp: DEVICE float[rows].  stats: DEVICE float[rows][2], 8-byte aligned, or NULL, for the backward call: the row's largest logit, and the
+ * sum of exp((logit - largest) / temperature) over the row; zeros in rows that are not read. */
+collage_status_t collage_token_logp(const collage_tokens_t* in, float* logp, float* stats, void* stream);
+/* grad_logp: DEVICE float[rows].  dlogits_ij = grad_logp_i / temperature * ([j = y] - exp(logp of token j)): [rows, vocab] in
+ * logits_dtype; may be the array of logits.  A row of grad_logp 0 gets zeros whatever its logits are. */
+collage_status_t collage_token_logp_backward(const collage_tokens_t* in, const float* stats, const float* grad_logp,
+                                             const collage_matrix_t* dlogits, void* stream);
+
+/* With ratio_i = exp(logp_i - old_logp_i) and k_i = ref_logp_i - logp_i,
+ *   L_i  = -min(ratio_i A_i, min(max(ratio_i, 1 - clip_low), 1 + clip_high) A_i) + kl_weight * kl_i,    kl_i = exp(k_i) - k_i - 1
+ *   loss_i = row_weight_i * L_i,   dlogits = the gradient of sum_i loss_i, old_logp, ref_logp and A being constants.
+ * Where both terms of the minimum are equal the gradient is that of the first.  A row with A_i = 0 has no policy term.
+ * Without old_logp the samples are the model's own: ratio is 1, with the gradient of a ratio.  Without ref_logp there is no KL
+ * term (kl_weight has to be 0, kl NULL).  Everything a row's scalars need is taken from logp in 64 bits. */
+typedef struct collage_policy {
+    const float* old_logp;           /* DEVICE float[rows] or NULL    */
+    const float* ref_logp;           /* DEVICE float[rows] or NULL    */
+    const float* advantage;          /* A: DEVICE float[rows]         */
+    const float* row_weight;         /* DEVICE float[rows]            */
+    double clip_low, clip_high;      /* 0 <= clip_low <= 1, clip_high >= 0 (infinity: no bound), in float     */
+    double kl_weight;                /* >= 0 and finite, in float     */
+} collage_policy_t;
+/* One pass over the logits.  loss: DEVICE float[rows].  logp, kl: DEVICE float[rows] or NULL.  dlogits: [rows, vocab] in
+ * logits_dtype; may be the array of logits.  A row of weight 0 (or without a target) is not read: loss, logp and kl are 0 there,
+ * its gradient zeros. */
+collage_status_t collage_policy_loss_and_grad(const collage_tokens_t* in, const collage_policy_t* policy, float* loss, float* logp,
+                                              float* kl, const collage_matrix_t* dlogits, void* stream);
+
+/* Pairs of answers: sequence 2p is the preferred and 2p + 1 the other answer of pair p; sequence s has rows [offsets[s], offsets[s+1]).
+ *   S_s = sum over its rows that have a target of (logp - ref_logp), divided by their number (at least 1) if average
+ *   log_ratio_p = S_2p - S_2p+1,   h = beta * log_ratio_p - margin
+ *   loss_p = pair_weight_p * (-(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h))
+ *   grad_logp = the gradient of sum_p loss_p; 0 in rows without a target and in rows of no sequence.
+ * offsets ascend within [0, rows]; others are taken into that range and a sequence that would end before it begins as empty (then
+ * the gradients of rows that several sequences or none would own are undefined).  Sums are in 64 bits and in a fixed order. */
+typedef struct collage_preference {
+    const float* logp;               /* DEVICE float[rows]                                                   */
+    const float* ref_logp;           /* DEVICE float[rows] or NULL: zeros                                    */
+    const void* target;              /* of collage_tokens_t, with its vocab: which rows count                */
+    const void* offsets;             /* DEVICE int32_t or int64_t [2 * pairs + 1] (offset_bytes = 4 or 8)    */
+    const float* pair_weight;        /* DEVICE float[pairs] or NULL: ones                                    */
+    uint64_t rows, vocab, pairs;     /* below 2^31 (ERR_LIMIT)                                               */
+    uint32_t target_bytes, offset_bytes;
+    double beta, margin, label_smoothing;      /* finite in float; 0 <= label_smoothing <= 1                 */
+    int average;
+} collage_preference_t;
+/* loss: DEVICE float[pairs].  log_ratio: DEVICE float[pairs] or NULL.  grad_logp: DEVICE float[rows] or NULL. */
+collage_status_t collage_preference_loss(const collage_preference_t* in, float* loss, float* log_ratio, float* grad_logp, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * AdamW over many tensors at once, with optimizer states in 8 bits or in 32, and the gradients' norm for clipping.  Ordinary mixed
+ * precision next to Algorithm 2, for the storage forms that it does not have; scalars are evaluated in double and cast to float.
+ *   g = grad * grad_scale;   m' = beta1 m + (1 - beta1) g;   v' = beta2 v + (1 - beta2) g^2
+ *   x' = x - lr (m' / (1 - beta1^t) / (sqrt(v' / (1 - beta2^t)) + eps) + weight_decay x)
+ * The parameter, by `rest`: NONE  x = theta, theta' = RN_bf16(x');
+ *                           BF16  x = theta + rest, a pair as in option B: theta' = RN_bf16(x'), rest' = RN_bf16(x' - theta'),
+ *                                 with x' as the unrounded sum of theta and (rest + update), the latter in float;
+ *                           F32   x = rest, a master weight: rest' = x', theta' = RN_bf16(x') (theta is not read).
+ * The states, by `state`: F32   m and v are floats; with rest NONE or F32 the results are collage_adamw_step_fp32's, bit for bit.
+ *                         E4M3  m and v are codes of 8 bits with a float scale for each 256 elements of their tensor (the last
+ *                               group of a tensor may be shorter):  m = m_code * m_scale,  sqrt(v) = v_code * v_scale, stored again
+ *                               as scale = max / 448 and codes of m' / scale, to nearest even, and of u = sqrt(v') / scale, u at least 2^-9
+ *                               where v' is not 0, rounded down to a multiple of its spacing s after s * d has been added, 0 <= d < 1
+ *                               random (448 at most).  The root moves by less than a code's step in a step of beta2 = 0.999; rounding to nearest would never
+ *                               move it.  A group whose largest |m'| (or sqrt(v')) is below 2^-100 is stored as zeros with scale 0.
+ *                               A gradient whose square is no finite float makes its group's states NaN from then on.
+ * d has 16 bits, of a fixed function of seed, step and position: with mix(x) on 32 bits x ^= x >> 16, x *= 0x6A09E667,
+ * x ^= x >> 15, x *= 0xB504F333, x ^= x >> 16 and key = mix(seed_lo + mix(seed_hi + mix(step_lo + mix(step_hi)))), element P of
+ * the plan has the lower (even P) or upper half of mix(lo + mix(hi + key)), where hi and lo are the words of P / 2.  A plan counts its
+ * elements tensor by tensor in the order given, each tensor's beginning rounded up to a multiple of 256.  The same call gives the same bits.
+ * Of hyper->flags EPS_INSIDE_SQRT is taken, and the kernel-choice flags are ignored; hyper->edq_out has to be NULL (ERR_ARG). */
+typedef enum { COLLAGE_STATE_F32 = 0, COLLAGE_STATE_E4M3 = 1 } collage_adam_state_t;
+typedef enum { COLLAGE_REST_NONE = 0, COLLAGE_REST_BF16 = 1, COLLAGE_REST_F32 = 2 } collage_adam_rest_t;
+typedef struct collage_adam_tensor {
+    void* theta;             /* DEVICE bfloat16[n]                                                                   */
+    void* rest;              /* DEVICE bfloat16[n] or float[n] by the plan's form; NULL for REST_NONE                 */
+    void* m;                 /* DEVICE float[n], or e4m3[n], one byte each                                            */
+    void* v;                 /* as m                                                                                 */
+    float* m_scale;          /* DEVICE float[(n + 255) / 256] for STATE_E4M3, else NULL                               */
+    float* v_scale;
+    const void* grad;        /* DEVICE bfloat16[n], read only                                                        */
+    uint64_t n;
+} collage_adam_tensor_t;
+typedef struct collage_adam_plan collage_adam_plan_t;   /* opaque; owns a small device table */
+
+/* As collage_plan_create: copies the HOST array, allocates and synchronises; the plan belongs to the current device.  States begin as zeros
+ * (codes, scales and floats alike).
+ * Errors: ERR_NULL, ERR_ARG (num < 0, unknown form, arrays that the form does not have, misaligned elements, more than 2^32 - 1
+ * chunks of 4096 elements), ERR_ALIAS, ERR_LIMIT (no host memory), ERR_ARCH, ERR_CUDA. */
+collage_status_t collage_adam_plan_create(const collage_adam_tensor_t* tensors, int num, collage_adam_state_t state,
+                                          collage_adam_rest_t rest, collage_adam_plan_t** out_plan);
+collage_status_t collage_adam_plan_destroy(collage_adam_plan_t* plan);
+
+/* One step of all the plan's tensors in one launch.  grad_scale: DEVICE float or NULL (1): what every gradient is taken times, such
+ * as the factor of collage_adam_grad_norm.  `seed` matters for STATE_E4M3 only.  Scalars, step and seed are recorded by stream capture.
+ * Errors: ERR_NULL, ERR_ARG (step 0, hyper range, another device than the plan's), ERR_ALIAS (grad_scale within an array that is
+ * written), ERR_ARCH, ERR_CUDA. */
+collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collage_hyper_t* hyper, uint64_t step, uint64_t seed,
+                                   const float* grad_scale, void* stream);
+
+/* norm: DEVICE float: sqrt of the sum of squares of all gradients of the plan.  grad_scale: DEVICE float or NULL: min(1, max_norm /
+ * norm), 1 for a norm of 0, NaN for a NaN.  max_norm > 0 (infinity: never clipped).  Squares and sums do not overflow; the order of sums is fixed.
+ * `workspace` is one of collage_workspace_bytes(), cleared once by collage_workspace_init, as for the EDQ reduction.
+ * Errors: ERR_NULL, ERR_ARG, ERR_ALIAS, ERR_WORKSPACE, ERR_ARCH, ERR_CUDA. */
+collage_status_t collage_adam_grad_norm(const collage_adam_plan_t* plan, double max_norm, float* norm, float* grad_scale,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,10 @@ OP_ADD, OP_SUB, OP_MUL, OP_DIV, OP_SQRT, OP_FMA = range(6)
 ACT_SILU, ACT_GELU_TANH = 0, 1
 DTYPE_BF16, DTYPE_F32 = 0, 1
 DISTILL_MAX_TOP = 1024
+GATE_NONE, GATE_SIGMOID, GATE_SILU = 0, 1, 2
+STATE_F32, STATE_E4M3 = 0, 1
+REST_NONE, REST_BF16, REST_F32 = 0, 1, 2
+ADAM_GROUP = 256            # elements of a tensor that share a scale of its 8-bit states
 SCALAR_NAMES = ("b1", "c1", "b2", "c2", "b2h", "b2l", "bc1", "bc2", "a", "lam", "eps")
 
 EXPORTS = (
@@ -35,6 +39,9 @@ EXPORTS = (
     "collage_add_rms_norm", "collage_add_rms_norm_backward", "collage_rms_norm_workspace_bytes", "collage_quantize_rows",
     "collage_gated_ffn", "collage_gated_ffn_backward", "collage_gated_ffn_e4m3",
     "collage_distill_loss", "collage_distill_loss_backward", "collage_distill_loss_and_grad",
+    "collage_block_norm", "collage_block_norm_backward", "collage_block_norm_workspace_bytes",
+    "collage_token_logp", "collage_token_logp_backward", "collage_policy_loss_and_grad", "collage_preference_loss",
+    "collage_adam_plan_create", "collage_adam_plan_destroy", "collage_adam_step", "collage_adam_grad_norm",
 )
 
 
@@ -70,6 +77,38 @@ class Distill(ctypes.Structure):
     """collage_distill_t"""
     _fields_ = [("logits", Matrix), ("top_index", Matrix), ("top_logits", Matrix), ("logits_dtype", ctypes.c_int),
                 ("top_index_bytes", ctypes.c_uint32), ("temperature", ctypes.c_double)]
+
+
+class BlockNorm(ctypes.Structure):
+    """collage_block_norm_t"""
+    _fields_ = [("block", Matrix), ("gate", Matrix), ("post_weight", ctypes.c_void_p), ("pre_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_double), ("residual_scale", ctypes.c_double), ("block_scale", ctypes.c_double), ("activation", ctypes.c_int)]
+
+
+class Tokens(ctypes.Structure):
+    """collage_tokens_t"""
+    _fields_ = [("logits", Matrix), ("target", ctypes.c_void_p), ("logits_dtype", ctypes.c_int), ("target_bytes", ctypes.c_uint32),
+                ("temperature", ctypes.c_double)]
+
+
+class Policy(ctypes.Structure):
+    """collage_policy_t"""
+    _fields_ = [("old_logp", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p), ("advantage", ctypes.c_void_p), ("row_weight", ctypes.c_void_p),
+                ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_weight", ctypes.c_double)]
+
+
+class Preference(ctypes.Structure):
+    """collage_preference_t"""
+    _fields_ = [("logp", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p), ("target", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+                ("pair_weight", ctypes.c_void_p), ("rows", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("pairs", ctypes.c_uint64),
+                ("target_bytes", ctypes.c_uint32), ("offset_bytes", ctypes.c_uint32), ("beta", ctypes.c_double), ("margin", ctypes.c_double),
+                ("label_smoothing", ctypes.c_double), ("average", ctypes.c_int)]
+
+
+class AdamTensor(ctypes.Structure):
+    """collage_adam_tensor_t"""
+    _fields_ = [("theta", ctypes.c_void_p), ("rest", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("n", ctypes.c_uint64)]
 
 
 class CollageError(RuntimeError):
@@ -142,16 +181,28 @@ def lib() -> ctypes.CDLL:
         L.collage_build_flavor.restype = ctypes.c_char_p
         L.collage_build_flavor.argtypes = []
         L.collage_enable_peer_access.argtypes = [i32]
-        _declare_operators(L, ctypes.POINTER(Matrix), ctypes.POINTER(Distill))
+        L.collage_adam_plan_create.argtypes = [ctypes.POINTER(AdamTensor), i32, i32, i32, ctypes.POINTER(vp)]
+        L.collage_adam_plan_destroy.argtypes = [vp]
+        _declare_operators(L, *[ctypes.POINTER(s) for s in (Matrix, Distill, BlockNorm, Tokens, Policy, Preference)])
         _packed = ctypes.CDLL(str(_lib_path))
-        _declare_operators(_packed, ctypes.c_char_p, ctypes.c_char_p)
+        _declare_operators(_packed, *[ctypes.c_char_p] * 6)
         _lib = L
     return _lib
 
 
-def _declare_operators(L, mp, dp):
-    """Argument types of the training-step operators; `mp`, `dp`: how matrices and distillation arguments are passed."""
-    vp, i32 = ctypes.c_void_p, ctypes.c_int
+def _declare_operators(L, mp, dp, bp, tp, pp, rp):
+    """Argument types of the training-step operators; `mp`, `dp`, ...: how matrices and the structures of arguments are passed."""
+    vp, i32, f64, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_double, ctypes.c_size_t
+    L.collage_block_norm.argtypes = [bp, mp, mp, mp, mp, vp, vp, vp, vp]
+    L.collage_block_norm_workspace_bytes.restype = size
+    L.collage_block_norm_workspace_bytes.argtypes = [ctypes.c_uint64]
+    L.collage_block_norm_backward.argtypes = [bp, mp, mp, mp, vp, vp, mp, mp, mp, vp, vp, vp, size, vp]
+    L.collage_token_logp.argtypes = [tp, vp, vp, vp]
+    L.collage_token_logp_backward.argtypes = [tp, vp, vp, mp, vp]
+    L.collage_policy_loss_and_grad.argtypes = [tp, pp, vp, vp, vp, mp, vp]
+    L.collage_preference_loss.argtypes = [rp, vp, vp, vp, vp]
+    L.collage_adam_step.argtypes = [vp, ctypes.POINTER(Hyper), ctypes.c_uint64, ctypes.c_uint64, vp, vp]
+    L.collage_adam_grad_norm.argtypes = [vp, f64, vp, vp, vp, size, vp]
     L.collage_add_rms_norm.argtypes = [mp, mp, vp, ctypes.c_double, mp, mp, mp, vp, vp, vp]
     L.collage_rms_norm_workspace_bytes.restype = ctypes.c_size_t
     L.collage_rms_norm_workspace_bytes.argtypes = [ctypes.c_uint64]
@@ -406,6 +457,11 @@ def _operators():
 
 _pack_matrix = struct.Struct("QQQQ").pack          # collage_matrix_t: a third of the time that a ctypes structure takes
 _pack_distill = struct.Struct("iId").pack
+_pack_block_norm = struct.Struct("QQdddi4x").pack      # what follows the matrices in collage_block_norm_t
+_pack_tokens = struct.Struct("QiId").pack              # and in collage_tokens_t
+_pack_policy = struct.Struct("QQQQddd").pack
+_pack_preference = struct.Struct("QQQQQQQQIIdddi4x").pack
+_NO_MATRIX = _pack_matrix(0, 0, 0, 0)
 
 
 def _flat(t):
@@ -562,3 +618,165 @@ def distill_loss_and_grad(logits, top_index, top_logits, temperature: float, row
     d, n = _distill(logits, top_index, top_logits, temperature, dev, w)
     _check(L.collage_distill_loss_and_grad(d, _vector(row_weight, _F32, n, dev, w), _vector(loss, _F32, n, dev, w),
                                            _matrix(dlogits, logits.dtype, dev, w), _stream(stream, dev, w)), w)
+
+
+def _scratch(workspace, dev, where: str):
+    """Address and bytes of a workspace of the current device, or None and 0."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(where)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _block_norm(block, gate, post_weight, pre_weight, eps, residual_scale, block_scale, activation, dev, where):
+    """collage_block_norm_t, packed, and the block's rows and columns."""
+    mb, mg = _matrix(block, _BF16, dev, where, True), _matrix(gate, _BF16, dev, where)
+    rows, cols = _extents(block)
+    return (mb + (mg or _NO_MATRIX) + _pack_block_norm(_vector(post_weight, _BF16, cols, dev, where) or 0, _vector(pre_weight, _BF16, cols, dev, where) or 0,
+                                                       eps, residual_scale, block_scale, activation)), rows, cols
+
+
+def block_norm(x, block, r, gate=None, post_weight=None, pre_weight=None, y=None, y8=None, y8_scale=None, rstd_post=None, rstd_pre=None,
+               eps: float = 1e-6, residual_scale: float = 1.0, block_scale: float = 1.0, activation: int = GATE_NONE, stream=None):
+    """r = residual_scale x + block_scale A(gate) norm(block) post_weight; y = norm(r) pre_weight in bfloat16 (y) and / or 8 bits (y8, y8_scale).
+
+    gate: one row for all, or a row for each; without post_weight the block's output is not normed, without pre_weight there is no y.
+    """
+    w, (L, dev) = "collage_block_norm", _operators()
+    s, rows, _ = _block_norm(block, gate, post_weight, pre_weight, eps, residual_scale, block_scale, activation, dev, w)
+    _check(L.collage_block_norm(s, _matrix(x, _BF16, dev, w, True), _matrix(r, _BF16, dev, w, True), _matrix(y, _BF16, dev, w), _matrix(y8, _E4M3, dev, w),
+                                _vector(y8_scale, _F32, rows, dev, w), _vector(rstd_post, _F32, rows, dev, w), _vector(rstd_pre, _F32, rows, dev, w),
+                                _stream(stream, dev, w)), w)
+
+
+def block_norm_workspace_bytes(cols: int) -> int:
+    return int(lib().collage_block_norm_workspace_bytes(cols))
+
+
+def block_norm_backward(dy, r, block, rstd_post, rstd_pre, dx, dblock, dr=None, gate=None, post_weight=None, pre_weight=None, dgate=None,
+                        dpost_weight=None, dpre_weight=None, workspace=None, residual_scale: float = 1.0, block_scale: float = 1.0,
+                        activation: int = GATE_NONE, stream=None):
+    """Gradients of block_norm from that of y (dy) and that which reached r on its own way (dr); outputs that are None are not computed."""
+    w, (L, dev) = "collage_block_norm_backward", _operators()
+    s, rows, cols = _block_norm(block, gate, post_weight, pre_weight, 0.0, residual_scale, block_scale, activation, dev, w)
+    ws, ws_bytes = _scratch(workspace, dev, w)
+    _check(L.collage_block_norm_backward(s, _matrix(dy, _BF16, dev, w), _matrix(dr, _BF16, dev, w), _matrix(r, _BF16, dev, w),
+                                         _vector(rstd_post, _F32, rows, dev, w), _vector(rstd_pre, _F32, rows, dev, w), _matrix(dx, _BF16, dev, w),
+                                         _matrix(dblock, _BF16, dev, w), _matrix(dgate, _BF16, dev, w), _vector(dpost_weight, _BF16, cols, dev, w),
+                                         _vector(dpre_weight, _BF16, cols, dev, w), ws, ws_bytes, _stream(stream, dev, w)), w)
+
+
+def _index(t, length, dev, where):
+    """Address of a contiguous vector of int32 or int64, and the bytes of its elements."""
+    if t is None:
+        raise CollageError(ERR_NULL, where)
+    dtype = t.dtype
+    if dtype is not _I32 and dtype is not _I64:
+        _refuse(where)
+    return _vector(t, dtype, length, dev, where), 4 if dtype is _I32 else 8
+
+
+def _tokens(logits, target, temperature, dev, where):
+    """collage_tokens_t, packed, and the number of rows."""
+    if logits is None:
+        raise CollageError(ERR_NULL, where)
+    dtype = logits.dtype
+    if dtype is not _BF16 and dtype is not _F32:
+        _refuse(where)
+    m = _matrix(logits, dtype, dev, where)
+    rows = _extents(logits)[0]
+    at, size = _index(target, rows, dev, where)
+    return m + _pack_tokens(at, DTYPE_BF16 if dtype is _BF16 else DTYPE_F32, size, temperature), rows
+
+
+def token_logp(logits, target, temperature: float, logp, stats=None, stream=None):
+    """logp[i] = log softmax(logits[i] / temperature)[target[i]], 0 where target[i] is no token; stats [rows, 2] for the backward call."""
+    w, (L, dev) = "collage_token_logp", _operators()
+    t, n = _tokens(logits, target, temperature, dev, w)
+    _check(L.collage_token_logp(t, _vector(logp, _F32, n, dev, w), _vector(stats, _F32, 2 * n, dev, w), _stream(stream, dev, w)), w)
+
+
+def token_logp_backward(logits, target, temperature: float, stats, grad_logp, dlogits, stream=None):
+    """dlogits from grad_logp (one value a row) and the stats of token_logp; dlogits may be the logits' own array."""
+    w, (L, dev) = "collage_token_logp_backward", _operators()
+    t, n = _tokens(logits, target, temperature, dev, w)
+    _check(L.collage_token_logp_backward(t, _vector(stats, _F32, 2 * n, dev, w), _vector(grad_logp, _F32, n, dev, w),
+                                         _matrix(dlogits, logits.dtype, dev, w), _stream(stream, dev, w)), w)
+
+
+def policy_loss_and_grad(logits, target, temperature: float, advantage, row_weight, loss, dlogits, old_logp=None, ref_logp=None,
+                         clip_low: float = 0.2, clip_high: float = 0.2, kl_weight: float = 0.0, logp=None, kl=None, stream=None):
+    """loss[i] = row_weight[i] * (clipped policy loss + kl_weight * kl[i]) of each token, and dlogits, in one pass; dlogits may be the logits' own array."""
+    w, (L, dev) = "collage_policy_loss_and_grad", _operators()
+    t, n = _tokens(logits, target, temperature, dev, w)
+    p = _pack_policy(_vector(old_logp, _F32, n, dev, w) or 0, _vector(ref_logp, _F32, n, dev, w) or 0, _vector(advantage, _F32, n, dev, w) or 0,
+                     _vector(row_weight, _F32, n, dev, w) or 0, clip_low, clip_high, kl_weight)
+    _check(L.collage_policy_loss_and_grad(t, p, _vector(loss, _F32, n, dev, w), _vector(logp, _F32, n, dev, w), _vector(kl, _F32, n, dev, w),
+                                          _matrix(dlogits, logits.dtype, dev, w), _stream(stream, dev, w)), w)
+
+
+def preference_loss(logp, target, vocab: int, offsets, beta: float, loss, grad_logp=None, ref_logp=None, pair_weight=None, margin: float = 0.0,
+                    label_smoothing: float = 0.0, average: bool = False, log_ratio=None, stream=None):
+    """loss[p] = -log sigmoid(beta (S_2p - S_2p+1) - margin) of pairs of sequences [offsets[s], offsets[s + 1]) of rows, S summing logp - ref_logp; and grad_logp."""
+    w, (L, dev) = "collage_preference_loss", _operators()
+    if logp is None or offsets is None:
+        raise CollageError(ERR_NULL, w)
+    rows, edges = logp.numel(), offsets.numel()
+    if edges % 2 == 0 or not 0 <= vocab < 1 << 64:
+        _refuse(w)
+    pairs = edges // 2
+    at, size = _index(target, rows, dev, w)
+    edge, edge_size = _index(offsets, edges, dev, w)
+    p = _pack_preference(_vector(logp, _F32, rows, dev, w), _vector(ref_logp, _F32, rows, dev, w) or 0, at, edge,
+                         _vector(pair_weight, _F32, pairs, dev, w) or 0, rows, vocab, pairs, size, edge_size, beta, margin, label_smoothing, bool(average))
+    _check(L.collage_preference_loss(p, _vector(loss, _F32, pairs, dev, w), _vector(log_ratio, _F32, pairs, dev, w), _vector(grad_logp, _F32, rows, dev, w),
+                                     _stream(stream, dev, w)), w)
+
+
+# ------------------------------------------------------------------------------------------------------------------------
+# AdamW over many tensors with states in 8 or 32 bits.  As plan_create's, a plan's tensors have to outlive it.
+
+def adam_plan_create(tensors) -> int:
+    """tensors: list of (theta, rest, m, v, m_scale, v_scale, grad), contiguous CUDA tensors of the current device; returns the plan's handle.
+
+    theta, grad: bfloat16.  rest: None, bfloat16 (a pair's second part) or float32 (master weights), alike for all.  m, v: float32 with
+    m_scale and v_scale None, or torch.float8_e4m3fn with a float32 scale for each ADAM_GROUP elements, alike for all; zeros to begin with.
+    """
+    w, (_, dev) = "collage_adam_plan_create", _operators()
+    arr = (AdamTensor * max(len(tensors), 1))()
+    state = rest_kind = None
+    for i, (theta, rest, m, v, m_scale, v_scale, grad) in enumerate(tensors):
+        if theta is None or m is None or v is None or grad is None:
+            raise CollageError(ERR_NULL, w)
+        kinds = (STATE_F32 if m.dtype is _F32 else STATE_E4M3, REST_NONE if rest is None else REST_BF16 if rest.dtype is _BF16 else REST_F32)
+        if i and kinds != (state, rest_kind):
+            _refuse(f"{w}: tensors of different forms")
+        state, rest_kind = kinds
+        n = theta.numel()
+        groups = -(-n // ADAM_GROUP)
+        code = _F32 if state == STATE_F32 else _E4M3
+        arr[i] = AdamTensor(_vector(theta, _BF16, n, dev, w), _vector(rest, _BF16 if rest_kind == REST_BF16 else _F32, n, dev, w), _vector(m, code, n, dev, w),
+                            _vector(v, code, n, dev, w), _vector(m_scale, _F32, groups, dev, w), _vector(v_scale, _F32, groups, dev, w),
+                            _vector(grad, _BF16, n, dev, w), n)
+    plan = ctypes.c_void_p()
+    _check(lib().collage_adam_plan_create(arr, len(tensors), state or 0, rest_kind or 0, ctypes.byref(plan)), w)
+    return plan.value
+
+
+def adam_plan_destroy(plan: int):
+    _check(lib().collage_adam_plan_destroy(plan), "collage_adam_plan_destroy")
+
+
+def adam_step(plan: int, hyper: Hyper, step: int, seed: int = 0, grad_scale=None, stream=None):
+    """One step of all the plan's tensors; grad_scale: a float32 CUDA tensor of one element that the gradients are taken times."""
+    w, (L, dev) = "collage_adam_step", _operators()
+    _check(L.collage_adam_step(plan, ctypes.byref(hyper), step, seed, _vector(grad_scale, _F32, 1, dev, w), _stream(stream, dev, w)), w)
+
+
+def adam_grad_norm(plan: int, max_norm: float, norm, grad_scale, workspace, stream=None):
+    """norm of all the plan's gradients and grad_scale = min(1, max_norm / norm), float32 CUDA tensors of one element; workspace as for EDQ."""
+    w, (L, dev) = "collage_adam_grad_norm", _operators()
+    ws, ws_bytes = _scratch(workspace, dev, w)
+    _check(L.collage_adam_grad_norm(plan, max_norm, _vector(norm, _F32, 1, dev, w), _vector(grad_scale, _F32, 1, dev, w), ws, ws_bytes,
+                                    _stream(stream, dev, w)), w)

@@ -23,7 +23,7 @@ LIB = HERE / "libcollage_b200.so"
 SOURCES = ["collage_step.cu", "collage_primitives.cu", "collage_edq_static.cu", "collage_fp32_master.cu"]
 # The training-step operators, each file compiled in one piece and the files at once.  (Split compilation, as below, gave one
 # of two codes from the same file, from build to build: up to a tenth of a kernel's time.)
-OPERATOR_SOURCES = ["row_norm.cu", "gated_ffn.cu", "distill_loss.cu"]
+OPERATOR_SOURCES = ["row_norm.cu", "gated_ffn.cu", "distill_loss.cu", "block_norm.cu", "token_loss.cu", "adam_multi.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-fmad=false", "-ftz=false", "-prec-div=true", "-prec-sqrt=true",

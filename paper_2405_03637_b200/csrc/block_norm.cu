@@ -1,0 +1,519 @@
+// Norm after a block, its gate and scales, the residual addition and the norm before the next block, in one pass; and its backward pass.
+//
+//   n = o / sqrt(mean o^2 + eps) * w_post        (o itself without w_post)
+//   r = alpha x + beta A(gate) n,                 y = r / sqrt(mean r^2 + eps) * w_pre
+// Backward, with nr = r rstd_pre, q = w_pre dy, no = o rstd_post:
+//   D = rstd_pre (q - nr mean(q nr)) + dr,        dx = alpha D,     u = beta D
+//   h = u A(gate) w_post,                         do = rstd_post (h - no mean(h no))
+//   dw_pre = sum dy nr,   dw_post = sum u A no,   dgate = A'(gate) u n  (summed over the rows for a gate of channels)
+// where every sum without an index is over the rows.
+//
+// All of it is bound by memory: a row of each array is read once and kept in registers through both of its sums.
+// As in the residual norm, y belongs to r before r is rounded for the stream, and the backward pass reads the rounded r.
+#include "ops_common.cuh"
+
+namespace collage {
+namespace ops {
+
+struct BlockNormArgs {
+    const uint16_t *x, *o, *gate, *post, *pre;
+    uint16_t *r, *y;
+    uint8_t* y8;
+    float *scale, *rstd_post, *rstd_pre;
+    uint64_t ldx, ldo, ldg, ldr, ldy, ldy8;      // ldg = 0: one row of gates for all
+    uint64_t cols;
+    float eps, alpha, beta;
+    int activation;
+};
+
+__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// A(g), and its derivative; the kind is the same for all threads
+__device__ __forceinline__ float gate_value(int kind, float g) {
+    if (kind == COLLAGE_GATE_NONE) return g;
+    const float s = sigmoid(g);
+    return kind == COLLAGE_GATE_SIGMOID ? s : g == -INFINITY ? -0.0f : g * s;
+}
+__device__ __forceinline__ float gate_slope(int kind, float g) {
+    if (kind == COLLAGE_GATE_NONE) return 1.0f;
+    const float s = sigmoid(g), back = sigmoid(-g);          // 1 - s, also where s is nearly 1
+    if (kind == COLLAGE_GATE_SIGMOID) return s * back;
+    return fabsf(g) == INFINITY ? s : s + g * s * back;
+}
+
+constexpr int kBlockThreads = 256;
+
+// One block per row, element by element, the row read again for each stage: any length, stride and alignment.
+__global__ void __launch_bounds__(kBlockThreads) block_norm_any_kernel(const __grid_constant__ BlockNormArgs a) {
+    __shared__ float slots[kBlockThreads / 32];
+    after_previous();
+    const uint64_t row = blockIdx.x;
+    const uint16_t *x = a.x + row * a.ldx, *o = a.o + row * a.ldo, *gate = a.gate ? a.gate + row * a.ldg : nullptr;
+    float fo = 1.0f, rstd_o = 1.0f, fr = 1.0f, rstd_r = 1.0f;
+    auto mean_of = [&](auto&& value, float f) {
+        float sum = 0.0f;
+        for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads) {
+            const float v = value(j) * f;
+            sum = __fmaf_rn(v, v, sum);
+        }
+        return block_sum(sum, slots, kBlockThreads / 32) / static_cast<float>(a.cols) + a.eps * f * f;
+    };
+    auto rstd_of = [&](auto&& value, float& f) {
+        float mean = mean_of(value, 1.0f);
+        if (!squares_fit(mean)) mean = mean_of(value, f = rescue_factor(mean));
+        return 1.0f / sqrtf(mean);
+    };
+    if (a.post) {
+        rstd_o = rstd_of([&](uint64_t j) { return bf16_value(o[j]); }, fo);
+        if (a.rstd_post && threadIdx.x == 0) a.rstd_post[row] = fo * rstd_o;
+    }
+    auto stream = [&](uint64_t j) {
+        float n = bf16_value(o[j]);
+        if (a.post) n = n * fo * rstd_o * bf16_value(a.post[j]);
+        if (gate) n *= gate_value(a.activation, bf16_value(gate[j]));
+        return __fmaf_rn(a.alpha, bf16_value(x[j]), a.beta * n);
+    };
+    if (a.pre) {
+        rstd_r = rstd_of(stream, fr);
+        if (a.rstd_pre && threadIdx.x == 0) a.rstd_pre[row] = fr * rstd_r;
+    }
+    auto normed = [&](float r, uint64_t j) { return r * fr * rstd_r * bf16_value(a.pre[j]); };
+    float scale = 0.0f;
+    if (a.y8) {
+        uint32_t most = 0;
+        for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads)
+            most = max(most, __float_as_uint(normed(stream(j), j)) & 0x7FFFFFFFu);
+        most = block_max(most, reinterpret_cast<uint32_t*>(slots), kBlockThreads / 32);
+        scale = __uint_as_float(most) / kE4m3Max;
+        if (threadIdx.x == 0) a.scale[row] = scale;
+    }
+    // outputs last, element for element: r may be the array of x or of o, y that of o
+    for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads) {
+        const float r = stream(j), y = a.pre ? normed(r, j) : 0.0f;
+        a.r[row * a.ldr + j] = to_bf16(r);
+        if (a.y) a.y[row * a.ldy + j] = to_bf16(y);
+        if (a.y8) a.y8[row * a.ldy8 + j] = scale == 0.0f ? 0 : to_e4m3(y / scale);
+    }
+}
+
+// Rows of whole 16-byte vectors, read once and kept in registers: PER vectors a thread, a row by one warp (WARP: four rows a
+// block) or by a block of as many warps as it takes.
+template <int PER, bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) block_norm_kernel(const __grid_constant__ BlockNormArgs a, uint64_t rows) {
+    __shared__ float slots[32];
+    after_previous();
+    const uint64_t row = WARP ? blockIdx.x * 4ull + (threadIdx.x >> 5) : blockIdx.x;
+    if (WARP && row >= rows) return;
+    const int t = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x, warps = threads >> 5;
+    const int vectors = static_cast<int>(a.cols >> 3);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    uint4 qx[PER], qo[PER], qg[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * threads;
+        qo[i] = v < vectors ? reinterpret_cast<const uint4*>(a.o + row * a.ldo)[v] : none;
+        qx[i] = v < vectors ? reinterpret_cast<const uint4*>(a.x + row * a.ldx)[v] : none;
+        if (a.gate) qg[i] = v < vectors ? reinterpret_cast<const uint4*>(a.gate + row * a.ldg)[v] : none;
+    }
+    float r[PER][8];
+    // 1 / rms of the values in r, which come out times a power of two where their squares need one (returned in f)
+    auto rstd_of = [&](float& f) {
+        f = 1.0f;
+#pragma unroll 1
+        for (;;) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                float part = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part = __fmaf_rn(r[i][e], r[i][e], part);
+                sum += part;
+            }
+            const float mean = block_sum(sum, slots, warps) / static_cast<float>(a.cols) + a.eps * f * f;
+            if (squares_fit(mean) || f != 1.0f) return 1.0f / sqrtf(mean);
+            f = rescue_factor(mean);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r[i][e] *= f;
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < PER; ++i) unpack8(qo[i], r[i]);
+    if (a.post) {
+        uint4 qw[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) qw[i] = t + i * threads < vectors ? __ldg(reinterpret_cast<const uint4*>(a.post) + t + i * threads) : none;
+        float f;
+        const float rstd = rstd_of(f);
+        if (a.rstd_post && t == 0) a.rstd_post[row] = f * rstd;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            float w[8];
+            unpack8(qw[i], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[i][e] = r[i][e] * rstd * w[e];
+        }
+    }
+    if (a.gate) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            float g[8];
+            unpack8(qg[i], g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[i][e] *= gate_value(a.activation, g[e]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * threads;
+        float x[8];
+        unpack8(qx[i], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[i][e] = v < vectors ? __fmaf_rn(a.alpha, x[e], a.beta * r[i][e]) : 0.0f;
+        if (v < vectors) reinterpret_cast<uint4*>(a.r + row * a.ldr)[v] = pack8(r[i]);
+    }
+    if (!a.pre) return;
+    {
+        uint4 qw[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) qw[i] = t + i * threads < vectors ? __ldg(reinterpret_cast<const uint4*>(a.pre) + t + i * threads) : none;
+        float f;
+        const float rstd = rstd_of(f);
+        if (a.rstd_pre && t == 0) a.rstd_pre[row] = f * rstd;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * threads;
+            float w[8];
+            unpack8(qw[i], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[i][e] = r[i][e] * rstd * w[e];
+            if (a.y && v < vectors) reinterpret_cast<uint4*>(a.y + row * a.ldy)[v] = pack8(r[i]);
+        }
+    }
+    if (a.y8) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(r[i][e]) & 0x7FFFFFFFu);
+        most = block_max(most, reinterpret_cast<uint32_t*>(slots), warps);
+        const float scale = __uint_as_float(most) / kE4m3Max;
+        if (t == 0) a.scale[row] = scale;
+        const Divisor by(scale);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * threads;
+            if (v >= vectors) continue;
+            uint32_t w[2] = {0, 0};
+            if (by.plain) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) w[e >> 2] |= pack_e4m3(by.quotient(r[i][e]), by.quotient(r[i][e + 1])) << (8 * (e & 2));
+            } else if (scale != 0.0f) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) w[e >> 2] |= pack_e4m3(r[i][e] / scale, r[i][e + 1] / scale) << (8 * (e & 2));
+            }
+            reinterpret_cast<uint2*>(a.y8 + row * a.ldy8)[v] = make_uint2(w[0], w[1]);
+        }
+    }
+}
+
+// A row's vectors over warps, as in the residual norm: with many rows four vectors a thread, with few rows one.
+static collage_status_t launch_block_norm(const BlockNormArgs& a, uint64_t rows, bool vectors_fit, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3;
+    const bool many = rows > 2ull * sm_count;
+    if (!vectors_fit || v > 4096) return launch<&block_norm_any_kernel>(rows, kBlockThreads, 1, 0, s, a);
+    if (many && v <= 128) {
+        const uint64_t grid = (rows + 3) / 4;
+        return v <= 32   ? launch<&block_norm_kernel<1, true>>(grid, 128, 1, 0, s, a, rows)
+               : v <= 64 ? launch<&block_norm_kernel<2, true>>(grid, 128, 1, 0, s, a, rows)
+                         : launch<&block_norm_kernel<4, true>>(grid, 128, 1, 0, s, a, rows);
+    }
+    const uint64_t per = v > 2048 ? 8 : many ? 4 : v > 1024 ? 2 : 1;
+    const int threads = static_cast<int>((v + per * 32 - 1) / (per * 32) * 32);
+    return per == 1   ? launch<&block_norm_kernel<1, false>>(rows, threads, 1, 0, s, a, rows)
+           : per == 2 ? launch<&block_norm_kernel<2, false>>(rows, threads, 1, 0, s, a, rows)
+           : per == 4 ? launch<&block_norm_kernel<4, false>>(rows, threads, 1, 0, s, a, rows)
+                      : launch<&block_norm_kernel<8, false>>(rows, threads, 1, 0, s, a, rows);
+}
+
+// ------------------------------------------------------------------------------------------------------- backward ---
+
+struct BlockNormBackwardArgs {
+    const uint16_t *dy, *dr, *r, *o, *gate, *post, *pre;
+    const float *rstd_post, *rstd_pre;
+    uint16_t *dx, *dblock, *dgate;        // dgate: a gate for each token; gates of channels come from the sums
+    float* partial;                       // [blocks][2][cols]: sum dy nr, and the sum that post_weight and a gate of channels share
+    uint64_t lddy, lddr, ldr, ldo, ldg, lddx, lddo, lddg;
+    uint64_t rows, cols;
+    float alpha, beta;
+    int activation, sums;                 // sums: bit 0 for pre_weight, bit 1 for post_weight and gates of channels
+    int token_gate;
+};
+
+constexpr int kBlockParts = 320;          // blocks whose sums over rows are kept apart
+enum { kSumPre = 1, kSumPost = 2 };
+
+// Walks over rows, one block for each, element by element; the sums over its rows are added up in its own part of the workspace.
+__global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(const __grid_constant__ BlockNormBackwardArgs a) {
+    __shared__ float slots[kBlockThreads / 32];
+    after_previous();
+    float* sum_pre = a.partial + blockIdx.x * 2 * a.cols;
+    float* sum_post = sum_pre + a.cols;
+    const float per_col = 1.0f / static_cast<float>(a.cols);
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const bool first = row == blockIdx.x;
+        const float rstd_r = a.pre ? a.rstd_pre[row] : 0.0f, rstd_o = a.post ? a.rstd_post[row] : 1.0f;
+        float mean_r = 0.0f, mean_o = 0.0f;
+        if (a.pre) {
+            float sum = 0.0f;
+            for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads)
+                sum = __fmaf_rn(bf16_value(a.dy[row * a.lddy + j]) * bf16_value(a.pre[j]), bf16_value(a.r[row * a.ldr + j]) * rstd_r, sum);
+            mean_r = block_sum(sum, slots, kBlockThreads / 32) * per_col;
+        }
+        auto stream_grad = [&](uint64_t j) {
+            float d = 0.0f;
+            if (a.pre) d = rstd_r * __fmaf_rn(-bf16_value(a.r[row * a.ldr + j]) * rstd_r, mean_r, bf16_value(a.dy[row * a.lddy + j]) * bf16_value(a.pre[j]));
+            return a.dr ? d + bf16_value(a.dr[row * a.lddr + j]) : d;
+        };
+        auto gate_of = [&](uint64_t j) { return bf16_value(a.gate[row * a.ldg + j]); };
+        auto gated = [&](uint64_t j, float d) { return a.gate ? a.beta * d * gate_value(a.activation, gate_of(j)) : a.beta * d; };
+        if (a.post && a.dblock) {
+            float sum = 0.0f;
+            for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads)
+                sum = __fmaf_rn(gated(j, stream_grad(j)) * bf16_value(a.post[j]), bf16_value(a.o[row * a.ldo + j]) * rstd_o, sum);
+            mean_o = block_sum(sum, slots, kBlockThreads / 32) * per_col;
+        }
+        // outputs last, element for element: they may be the arrays of the gradients that come in
+        for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads) {
+            const float d = stream_grad(j), n = a.o ? bf16_value(a.o[row * a.ldo + j]) * rstd_o : 0.0f;
+            const float du = gated(j, d), w = a.post ? bf16_value(a.post[j]) : 1.0f;
+            if (a.sums & kSumPre) {
+                const float s = bf16_value(a.dy[row * a.lddy + j]) * (bf16_value(a.r[row * a.ldr + j]) * rstd_r);
+                sum_pre[j] = first ? s : sum_pre[j] + s;
+            }
+            if (a.sums & kSumPost) {
+                const float s = (a.token_gate ? du : a.beta * d) * n;
+                sum_post[j] = first ? s : sum_post[j] + s;
+            }
+            if (a.dgate) a.dgate[row * a.lddg + j] = to_bf16(a.beta * d * n * w * gate_slope(a.activation, gate_of(j)));
+            if (a.dx) a.dx[row * a.lddx + j] = to_bf16(a.alpha * d);
+            if (a.dblock) a.dblock[row * a.lddo + j] = to_bf16(a.post ? rstd_o * __fmaf_rn(-n, mean_o, du * w) : du);
+        }
+        __syncthreads();
+    }
+}
+
+// The blocks' parts added up in order: 32 columns a block, each of its 32 warps takes every 32nd part.  From the shared sum
+// S = sum u n: dpost = A S and dgate = A' w S for a gate of channels, dpost = S otherwise.
+struct BlockNormFinishArgs {
+    const float* partial;
+    const uint16_t *gate, *post;          // gate: of channels, or null
+    uint16_t *dpre, *dpost, *dgate;
+    uint64_t cols;
+    int parts, activation;
+};
+constexpr int kBlockFinish = 1024;
+__global__ void __launch_bounds__(kBlockFinish) block_norm_finish_kernel(const __grid_constant__ BlockNormFinishArgs a, uint32_t column_blocks, int first_kind) {
+    __shared__ float part[kBlockFinish / 32][33];
+    after_previous();
+    const int kind = blockIdx.x / column_blocks + first_kind;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint64_t begin = (blockIdx.x % column_blocks) * 32ull, j = begin + lane;
+    float sum = 0.0f;
+    if (j < a.cols) {
+#pragma unroll 5
+        for (int k = warp; k < a.parts; k += kBlockFinish / 32) sum += a.partial[(2ull * k + kind) * a.cols + j];
+    }
+    part[warp][lane] = sum;
+    __syncthreads();
+    sum = warp_sum(part[lane][warp]);                        // column `warp` of the block's
+    const uint64_t out = begin + warp;
+    if (lane || out >= a.cols) return;
+    if (kind == 0) {
+        a.dpre[out] = to_bf16(sum);
+        return;
+    }
+    const float g = a.gate ? bf16_value(a.gate[out]) : 1.0f;
+    if (a.dpost) a.dpost[out] = to_bf16(a.gate ? gate_value(a.activation, g) * sum : sum);
+    if (a.dgate) a.dgate[out] = to_bf16((a.post ? bf16_value(a.post[out]) : 1.0f) * sum * gate_slope(a.activation, g));
+}
+
+}  // namespace ops
+}  // namespace collage
+
+using namespace collage;
+using namespace collage::ops;
+
+namespace {
+// A gate is absent (no data), one row for all, or a row for each.
+bool has_gate(const collage_block_norm_t* in) { return in->gate.data != nullptr; }
+bool gate_of_channels(const collage_block_norm_t* in) { return has_gate(in) && in->gate.rows == 1 && in->block.rows != 1; }
+
+collage_status_t check_block_norm(const collage_block_norm_t* in, uint64_t rows, uint64_t cols) {
+    auto scale_fits = [](double v) { return std::isfinite(v) && std::isfinite(static_cast<float>(v)); };
+    if (!scale_fits(in->residual_scale) || !scale_fits(in->block_scale) || !(scale_fits(in->eps) && in->eps >= 0.0)) return COLLAGE_ERR_ARG;
+    if (in->activation < COLLAGE_GATE_NONE || in->activation > COLLAGE_GATE_SILU) return COLLAGE_ERR_ARG;
+    if (has_gate(in) && (in->gate.cols != cols || (in->gate.rows != 1 && in->gate.rows != rows))) return COLLAGE_ERR_ARG;
+    if (reinterpret_cast<uintptr_t>(in->post_weight) % 2 || reinterpret_cast<uintptr_t>(in->pre_weight) % 2) return COLLAGE_ERR_ARG;
+    return has_gate(in) ? check_matrix(&in->gate, 2) : COLLAGE_OK;
+}
+bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+}  // namespace
+
+extern "C" {
+
+collage_status_t collage_block_norm(const collage_block_norm_t* in, const collage_matrix_t* x, const collage_matrix_t* r, const collage_matrix_t* y,
+                                    const collage_matrix_t* y8, float* y8_scale, float* rstd_post, float* rstd_pre, void* stream) {
+    if (!in || !x || !r || (y8 && !y8_scale && x->rows)) return COLLAGE_ERR_NULL;
+    if (!in->pre_weight && x->cols && (y || y8)) return COLLAGE_ERR_NULL;
+    if ((y8_scale && !y8) || (rstd_post && !in->post_weight && x->cols) || (rstd_pre && !in->pre_weight && x->cols)) return COLLAGE_ERR_ARG;
+    const collage_matrix_t* all[5] = {x, &in->block, r, y, y8};
+    collage_status_t st = COLLAGE_OK;
+    for (int i = 0; i < 5 && st == COLLAGE_OK; ++i)
+        if (all[i]) st = !same_shape(x, all[i]) ? COLLAGE_ERR_ARG : check_matrix(all[i], i == 4 ? 1 : 2);
+    if (st == COLLAGE_OK) st = check_block_norm(in, x->rows, x->cols);
+    if (st != COLLAGE_OK) return st;
+    if (reinterpret_cast<uintptr_t>(y8_scale) % 4 || reinterpret_cast<uintptr_t>(rstd_post) % 4 || reinterpret_cast<uintptr_t>(rstd_pre) % 4)
+        return COLLAGE_ERR_ARG;
+    AliasCheck alias;
+    const int ix = alias.add(span_of(x, 2), false), io = alias.add(span_of(&in->block, 2), false);
+    if (has_gate(in)) alias.add(span_of(&in->gate, 2), false);
+    alias.add(span_of(in->post_weight, 2 * x->cols), false);
+    alias.add(span_of(in->pre_weight, 2 * x->cols), false);
+    const int ir = alias.add(span_of(r, 2), true), iy = y ? alias.add(span_of(y, 2), true) : -1;
+    if (y8) alias.add(span_of(y8, 1), true);
+    if (y8_scale) alias.add(span_of(y8_scale, 4 * x->rows), true);
+    if (rstd_post) alias.add(span_of(rstd_post, 4 * x->rows), true);
+    if (rstd_pre) alias.add(span_of(rstd_pre, 4 * x->rows), true);
+    const int pairs[3][2] = {{ir, ix}, {ir, io}, {iy, io}};
+    if (alias.clash(pairs)) return COLLAGE_ERR_ALIAS;
+    DeviceInfo dev;
+    if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    if (x->rows == 0) return COLLAGE_OK;
+    BlockNormArgs a = {};
+    a.x = static_cast<const uint16_t*>(x->data);
+    a.ldx = x->ld;
+    a.o = static_cast<const uint16_t*>(in->block.data);
+    a.ldo = in->block.ld;
+    if (has_gate(in)) { a.gate = static_cast<const uint16_t*>(in->gate.data); a.ldg = in->gate.rows == 1 ? 0 : in->gate.ld; }
+    a.post = static_cast<const uint16_t*>(in->post_weight);
+    a.pre = static_cast<const uint16_t*>(in->pre_weight);
+    a.r = static_cast<uint16_t*>(r->data);
+    a.ldr = r->ld;
+    if (y) { a.y = static_cast<uint16_t*>(y->data); a.ldy = y->ld; }
+    if (y8) { a.y8 = static_cast<uint8_t*>(y8->data); a.ldy8 = y8->ld; a.scale = y8_scale; }
+    a.rstd_post = rstd_post;
+    a.rstd_pre = rstd_pre;
+    a.cols = x->cols;
+    a.eps = static_cast<float>(in->eps);
+    a.alpha = static_cast<float>(in->residual_scale);
+    a.beta = static_cast<float>(in->block_scale);
+    a.activation = in->activation;
+    if (x->cols == 0) {                        // no values: scales of 0, no rms
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        if (y8_scale && cudaMemsetAsync(y8_scale, 0, 4 * x->rows, s) != cudaSuccess) return COLLAGE_ERR_CUDA;
+        for (float* p : {rstd_post, rstd_pre})
+            if (p && cudaMemsetAsync(p, 0xFF, 4 * x->rows, s) != cudaSuccess) return COLLAGE_ERR_CUDA;      // (a NaN)
+        return COLLAGE_OK;
+    }
+    bool fit = x->cols % 8 == 0 && aligned(a.post) && aligned(a.pre) && (!a.gate || rows_aligned(&in->gate, 2, 16));
+    for (int i = 0; i < 5; ++i)
+        if (all[i]) fit = fit && rows_aligned(all[i], i == 4 ? 1 : 2, i == 4 ? 8 : 16);
+    return launch_block_norm(a, x->rows, fit, dev.sm_count, static_cast<cudaStream_t>(stream));
+}
+
+size_t collage_block_norm_workspace_bytes(uint64_t cols) { return static_cast<size_t>(kBlockParts) * 8 * cols; }
+
+collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
+                                             const collage_matrix_t* r, const float* rstd_post, const float* rstd_pre,
+                                             const collage_matrix_t* dx, const collage_matrix_t* dblock, const collage_matrix_t* dgate,
+                                             void* dpost_weight, void* dpre_weight, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!in) return COLLAGE_ERR_NULL;
+    const collage_matrix_t* o = &in->block;
+    const uint64_t rows = o->rows, cols = o->cols;
+    if (cols && ((!dy && !dr) || (!dx && !dblock && !dgate && !dpost_weight && !dpre_weight))) return COLLAGE_ERR_NULL;
+    if (cols && rows && ((dy && (!r || !rstd_pre || !in->pre_weight)) || (in->post_weight && !rstd_post))) return COLLAGE_ERR_NULL;
+    if ((dpre_weight && !dy) || (dpost_weight && !in->post_weight) || (dgate && !has_gate(in))) return COLLAGE_ERR_ARG;
+    const collage_matrix_t* all[6] = {o, dy, dr, r, dx, dblock};
+    collage_status_t st = COLLAGE_OK;
+    for (int i = 0; i < 6 && st == COLLAGE_OK; ++i)
+        if (all[i]) st = !same_shape(o, all[i]) ? COLLAGE_ERR_ARG : check_matrix(all[i], 2);
+    if (st == COLLAGE_OK) st = check_block_norm(in, rows, cols);
+    if (st == COLLAGE_OK && dgate) st = !same_shape(&in->gate, dgate) ? COLLAGE_ERR_ARG : check_matrix(dgate, 2);
+    if (st != COLLAGE_OK) return st;
+    if (reinterpret_cast<uintptr_t>(rstd_post) % 4 || reinterpret_cast<uintptr_t>(rstd_pre) % 4 || reinterpret_cast<uintptr_t>(dpost_weight) % 2 ||
+        reinterpret_cast<uintptr_t>(dpre_weight) % 2)
+        return COLLAGE_ERR_ARG;
+    const bool channels = gate_of_channels(in), channel_grad = dgate && channels;
+    const int sums = (dpre_weight ? kSumPre : 0) | (dpost_weight || channel_grad ? kSumPost : 0);
+    const size_t need = collage_block_norm_workspace_bytes(cols);
+    if (sums && need && (!workspace || workspace_bytes < need || !aligned(workspace))) return COLLAGE_ERR_WORKSPACE;
+    AliasCheck alias;
+    alias.add(span_of(o, 2), false);
+    if (has_gate(in)) alias.add(span_of(&in->gate, 2), false);
+    alias.add(span_of(in->post_weight, 2 * cols), false);
+    alias.add(span_of(in->pre_weight, 2 * cols), false);
+    const int idy = dy ? alias.add(span_of(dy, 2), false) : -1, idr = dr ? alias.add(span_of(dr, 2), false) : -1;
+    if (dy && r) alias.add(span_of(r, 2), false);
+    if (rstd_post) alias.add(span_of(rstd_post, 4 * rows), false);
+    if (rstd_pre) alias.add(span_of(rstd_pre, 4 * rows), false);
+    const int idx = dx ? alias.add(span_of(dx, 2), true) : -1, ido = dblock ? alias.add(span_of(dblock, 2), true) : -1;
+    if (dgate) alias.add(span_of(dgate, 2), true);
+    if (dpost_weight) alias.add(span_of(dpost_weight, 2 * cols), true);
+    if (dpre_weight) alias.add(span_of(dpre_weight, 2 * cols), true);
+    if (sums) alias.add(span_of(workspace, need), true);
+    const int pairs[4][2] = {{idx, idy}, {idx, idr}, {ido, idy}, {ido, idr}};
+    if (alias.clash(pairs)) return COLLAGE_ERR_ALIAS;
+    DeviceInfo dev;
+    if ((st = current_device(&dev)) != COLLAGE_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (cols == 0) return COLLAGE_OK;
+    if (rows == 0) {                           // sums over nothing
+        for (void* p : {dpost_weight, dpre_weight, channel_grad ? dgate->data : nullptr})
+            if (p && cudaMemsetAsync(p, 0, 2 * cols, s) != cudaSuccess) return COLLAGE_ERR_CUDA;
+        return COLLAGE_OK;
+    }
+    BlockNormBackwardArgs a = {};
+    auto set = [](const collage_matrix_t* m, const uint16_t*& p, uint64_t& ld) { if (m) { p = static_cast<const uint16_t*>(m->data); ld = m->ld; } };
+    auto set_out = [](const collage_matrix_t* m, uint16_t*& p, uint64_t& ld) { if (m) { p = static_cast<uint16_t*>(m->data); ld = m->ld; } };
+    set(dr, a.dr, a.lddr);
+    if (dy) {
+        set(dy, a.dy, a.lddy);
+        set(r, a.r, a.ldr);
+        a.pre = static_cast<const uint16_t*>(in->pre_weight);
+        a.rstd_pre = rstd_pre;
+    }
+    set(o, a.o, a.ldo);
+    if (has_gate(in)) { a.gate = static_cast<const uint16_t*>(in->gate.data); a.ldg = in->gate.rows == 1 ? 0 : in->gate.ld; }
+    a.token_gate = has_gate(in) && !channels;
+    a.post = static_cast<const uint16_t*>(in->post_weight);
+    a.rstd_post = rstd_post;
+    set_out(dx, a.dx, a.lddx);
+    set_out(dblock, a.dblock, a.lddo);
+    if (!channels) set_out(dgate, a.dgate, a.lddg);
+    a.partial = static_cast<float*>(workspace);
+    a.rows = rows;
+    a.cols = cols;
+    a.alpha = static_cast<float>(in->residual_scale);
+    a.beta = static_cast<float>(in->block_scale);
+    a.activation = in->activation;
+    a.sums = sums;
+    const unsigned parts = static_cast<unsigned>(std::min<uint64_t>({rows, static_cast<uint64_t>(kBlockParts), 2ull * dev.sm_count}));
+    st = launch<&block_norm_backward_any_kernel>(parts, kBlockThreads, 1, 0, s, a);
+    if (st != COLLAGE_OK || !sums) return st;
+    BlockNormFinishArgs f = {};
+    f.partial = a.partial;
+    f.gate = channels ? a.gate : nullptr;
+    f.post = a.post;
+    f.dpre = static_cast<uint16_t*>(dpre_weight);
+    f.dpost = static_cast<uint16_t*>(dpost_weight);
+    f.dgate = channel_grad ? static_cast<uint16_t*>(dgate->data) : nullptr;
+    f.cols = cols;
+    f.parts = static_cast<int>(parts);
+    f.activation = in->activation;
+    const uint32_t column_blocks = static_cast<uint32_t>((cols + 31) / 32);
+    const int kinds = (sums & kSumPre ? 1 : 0) + (sums & kSumPost ? 1 : 0);
+    return launch<&block_norm_finish_kernel>(static_cast<uint64_t>(column_blocks) * kinds, kBlockFinish, 1, 0, s, f, column_blocks, sums & kSumPre ? 0 : 1);
+}
+
+}  // extern "C"

@@ -7,6 +7,7 @@
 // shared memory (cp.async.bulk + mbarrier, three stages), 512 consumers compute and write back, the
 // producer bulk-stores.  Traffic per parameter: D 28 B (reads g 2, m 4, v 4, w 4; writes theta 2,
 // m 4, v 4, w 4), D^-MW 22 B.
+#include "adamw_float.cuh"
 #include "bulk_pipe.cuh"
 #include "host_common.cuh"
 #include "edq_reduce.cuh"
@@ -20,11 +21,6 @@ void launch_edq_finalize(const EdqPartial* partials, int count, uint64_t n, coll
 // collage_pipeline_fault reports it together with the bfloat16 step's
 static __device__ unsigned int g_pipeline_fault32 = 0;
 
-
-struct Fp32Scalars {
-    float b1, c1, b2, c2, bc1, bc2, neg_a, lam, eps;
-    uint32_t flags;
-};
 
 struct Fp32Params {
     uint16_t* theta;
@@ -82,27 +78,6 @@ struct Fp32Smem {
     unsigned long long red_lost[kCons / 32];
     EdqFinishSmem finish;
 };
-
-// One parameter: Algorithm 2 lines 8-13 in float.  Returns the update; w is the stored float
-// parameter (master weight, or the widened bfloat16 parameter), updated in place.
-__device__ __forceinline__ float adamw_fp32_element(float& m, float& v, float& w, float g, const Fp32Scalars& k) {
-    m = __fadd_rn(__fmul_rn(k.b1, m), __fmul_rn(k.c1, g));
-    v = __fadd_rn(__fmul_rn(k.b2, v), __fmul_rn(k.c2, __fmul_rn(g, g)));
-    const float mhat = __fdiv_rn(m, k.bc1);
-    const float vhat = __fdiv_rn(v, k.bc2);
-    const float den = (k.flags & 1u) ? __fsqrt_rn(__fadd_rn(vhat, k.eps)) : __fadd_rn(__fsqrt_rn(vhat), k.eps);
-    const float u = __fadd_rn(__fdiv_rn(mhat, den), __fmul_rn(k.lam, w));
-    const float delta = __fmul_rn(k.neg_a, u);
-    w = __fadd_rn(w, delta);
-    return delta;
-}
-
-__device__ __forceinline__ uint16_t to_bf16_rn(float x) {
-    uint16_t h;
-    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(x));
-    return h;
-}
-__device__ __forceinline__ float from_bf16(uint16_t h) { return __uint_as_float(static_cast<uint32_t>(h) << 16); }
 
 struct Fp32Acc {
     float dot, sq;
@@ -379,17 +354,7 @@ extern "C" collage_status_t collage_adamw_step_fp32(void* theta, void* master, v
     p.n = n;
     p.aligned = ((reinterpret_cast<uintptr_t>(theta) | reinterpret_cast<uintptr_t>(master) | reinterpret_cast<uintptr_t>(m) |
                   reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(grad)) & 15u) == 0;
-    const double t = static_cast<double>(step);
-    p.k.b1 = static_cast<float>(hyper->beta1);
-    p.k.c1 = static_cast<float>(1.0 - hyper->beta1);
-    p.k.b2 = static_cast<float>(hyper->beta2);
-    p.k.c2 = static_cast<float>(1.0 - hyper->beta2);
-    p.k.bc1 = static_cast<float>(1.0 - std::pow(hyper->beta1, t));
-    p.k.bc2 = static_cast<float>(1.0 - std::pow(hyper->beta2, t));
-    p.k.neg_a = -static_cast<float>(hyper->lr);
-    p.k.lam = static_cast<float>(hyper->weight_decay);
-    p.k.eps = static_cast<float>(hyper->eps);
-    p.k.flags = hyper->flags & COLLAGE_FLAG_EPS_INSIDE_SQRT;
+    p.k = fp32_scalars(hyper, step);
     if (hyper->edq_out) {
         p.fin.partials = static_cast<EdqPartial*>(hyper->workspace);
         p.fin.ticket = reinterpret_cast<unsigned int*>(static_cast<char*>(hyper->workspace) + kTicketOffset);

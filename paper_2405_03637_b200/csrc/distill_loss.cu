@@ -54,20 +54,6 @@ __device__ __forceinline__ bool by_base(float m, float c) { return sizeof(T) == 
 template <typename T>
 __device__ __forceinline__ float lack(float m, float c) { return by_base<T>(m, c) ? __fmaf_rn(m, c, -(m * c)) : 0.0f; }
 
-// Adds exp2((f - m) c) over a vector to `total`, or exp2(f c - RN(m c)) if BASED.  While there is no number yet (m = -infinity) every f is
-// -infinity or NaN, and is taken as it is.
-template <typename T, bool BASED>
-__device__ __forceinline__ void add_exps(const uint4& q, float m, float c, uint64_t& total) {
-    uint64_t f[Vec<T>::kPairs];
-    Vec<T>::unpack(q, f);
-    const float minus_m = m == -INFINITY ? 0.0f : -m;
-#pragma unroll
-    for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
-        const float2 e = BASED ? based_exps(f[i], pair_of(-m * c, -m * c), pair_of(c, c)) : exps(f[i], pair_of(minus_m, minus_m), pair_of(c, c));
-        total = add_pair(total, pair_of(e.x, e.y));
-    }
-}
-
 // What a row's blocks share, apart from the row itself.
 struct DistillShared {
     float2 warp[8];

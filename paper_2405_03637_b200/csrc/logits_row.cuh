@@ -117,6 +117,20 @@ __device__ __forceinline__ float2 based_exps(uint64_t f, uint64_t minus_base2, u
     const float2 x = floats_of(fma_pair(f, c2, minus_base2));
     return make_float2(fast_exp2(x.x), fast_exp2(x.y));
 }
+// Adds exp2((f - m) c) over a vector to `total`, or exp2(f c - RN(m c)) if BASED.  While there is no number yet (m = -infinity) every f is
+// -infinity or NaN, and is taken as it is.
+template <typename T, bool BASED>
+__device__ __forceinline__ void add_exps(const uint4& q, float m, float c, uint64_t& total) {
+    uint64_t f[Vec<T>::kPairs];
+    Vec<T>::unpack(q, f);
+    const float minus_m = m == -INFINITY ? 0.0f : -m;
+#pragma unroll
+    for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
+        const float2 e = BASED ? based_exps(f[i], pair_of(-m * c, -m * c), pair_of(c, c)) : exps(f[i], pair_of(minus_m, minus_m), pair_of(c, c));
+        total = add_pair(total, pair_of(e.x, e.y));
+    }
+}
+
 // Waits until at most `groups` of this thread's copy groups are under way (or 7, where more may be).
 __device__ __forceinline__ void wait_pending(uint32_t groups) {
     switch (groups) {
