@@ -17,7 +17,7 @@ namespace collage {
 namespace ops {
 
 constexpr uint32_t kGroup = 256;               // elements that share a scale: a warp's, eight a lane
-constexpr uint32_t kAdamChunk = 4096;          // elements of a block's turn
+constexpr uint32_t kAdamChunk = 4096;          // elements of the norm's turns
 constexpr int kAdamThreads = 256;
 
 struct AdamRec {
@@ -40,8 +40,9 @@ struct AdamScalars {
 
 struct AdamArgs {
     const AdamRec* tensors;
-    const AdamChunk* chunks;
-    uint64_t num_chunks;
+    const AdamChunk* tasks;                    // task: task_groups groups of a tensor, for one warp
+    uint64_t num_tasks;
+    uint32_t task_groups;
     const float* grad_scale;
     AdamScalars k;
 };
@@ -54,154 +55,322 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float fast_root(float x) {
-    float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
+__device__ __forceinline__ uint64_t pair_of(float v) { return ops::pair_of(v, v); }
+__device__ __forceinline__ uint64_t sub_pair(uint64_t a, uint64_t b) { return fma_pair(b, pair_of(-1.0f), a); }
+__device__ __forceinline__ uint64_t bf16_pair(uint32_t word) { return ops::pair_of(bf16_lo(word), bf16_hi(word)); }
+__device__ __forceinline__ uint64_t e4m3_pair(uint32_t two) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    return ops::pair_of(f.x, f.y);
 }
 
-// (theta, rest) + delta: the nearest bfloat16 to theta + RN(rest + delta), and what that lacks.  The sum is rounded to odd before it
-// is rounded to bfloat16 (to nearest at once it would go astray at every tie of the float).
-__device__ __forceinline__ void add_to_pair(float& theta, float& rest, float delta, uint32_t& theta_bits, uint32_t& rest_bits) {
-    const float t = rest + delta, s = theta + t, back = s - theta;
-    const float lost = (theta - (s - back)) + (t - back);                  // exact
-    uint32_t bits = __float_as_uint(s);
-    if (lost != 0.0f && fabsf(lost) < INFINITY) bits = (bits - ((__float_as_uint(lost) ^ bits) >> 31)) | 1u;
-    theta_bits = to_bf16(__uint_as_float(bits));
-    rest_bits = to_bf16((s - bf16_value(static_cast<uint16_t>(theta_bits))) + lost);
+// Square roots: y = rsqrt(v) gives r = v y, and a step of Newton's method on r^2 = v, whose remainder r^2 - v is exact in an fma, the
+// correctly rounded root but for a few in a million (in half the instructions of one that always is).
+__device__ __forceinline__ uint64_t root_pair(uint64_t v) {
+    const float2 f = floats_of(v);
+    float2 y;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(f.x, 0x1p-149f)));         // (of 0: 0 times a finite number)
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(f.y, 0x1p-149f)));
+    const uint64_t y2 = ops::pair_of(y.x, y.y), r = mul_pair(v, y2);
+    return fma_pair(fma_pair(r, r, mul_pair(v, pair_of(-1.0f))), mul_pair(y2, pair_of(-0.5f)), r);
+}
+__device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
+    float2 f = floats_of(v);
+    asm("rcp.approx.f32 %0, %0;" : "+f"(f.x));
+    asm("rcp.approx.f32 %0, %0;" : "+f"(f.y));
+    return ops::pair_of(f.x, f.y);
 }
 
-// What a lane holds of a group: values for eight elements, which ones those are is the caller's.
-template <int STATE, int REST>
+// (theta, rest) + delta: theta' is the bfloat16 nearest to theta + RN(rest + delta), rest' what that lacks.
+__device__ __forceinline__ void add_to_pair(uint64_t theta, uint64_t rest, uint64_t delta, uint32_t& theta_word, uint32_t& rest_word) {
+    const uint64_t t = add_pair(rest, delta), s = add_pair(theta, t), back = sub_pair(s, theta);
+    const uint64_t lost = add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back));                  // exact: theta + t = s + lost
+    const float2 sum = floats_of(s);
+    theta_word = pack_bf16(sum.x, sum.y);
+    // A float half-way between two bfloat16 values: which one is nearer hangs on what the float has lost.  It is rounded to odd first,
+    // towards the sum's own side.  (One in 65536; the test finds a half-word of 0x8000, and now and then another.)
+    const uint32_t low = __byte_perm(__float_as_uint(sum.x), __float_as_uint(sum.y), 0x5410) ^ 0x80008000u;
+    if ((low - 0x00010001u) & ~low & 0x80008000u) {
+        const float2 l = floats_of(lost);
+        auto odd = [](float f, float rest_of) {
+            const uint32_t bits = __float_as_uint(f);
+            const bool off = rest_of != 0.0f && fabsf(rest_of) < INFINITY;
+            return __uint_as_float(off ? (bits - ((__float_as_uint(rest_of) ^ bits) >> 31)) | 1u : bits);
+        };
+        theta_word = pack_bf16(odd(sum.x, l.x), odd(sum.y, l.y));
+    }
+    const float2 r = floats_of(add_pair(sub_pair(s, bf16_pair(theta_word)), lost));
+    rest_word = pack_bf16(r.x, r.y);
+}
+
+// Eight elements of a lane, in pairs, before and behind the update.  With states in 8 bits v is its root.
 struct Octet {
-    float g[8], theta[8], rest[8], m[8], v[8];           // STATE_E4M3: v is its root
-    uint32_t theta_out[8], rest_out[8];                  // bits
+    uint64_t g[4], theta[4], rest[4], m[4], v[4];
+    uint32_t theta_out[4], rest_out[4];                  // two bfloat16 each
 };
 
 template <int STATE, int REST>
-__device__ __forceinline__ void update(Octet<STATE, REST>& o, const AdamScalars& k, float grad_scale) {
+__device__ __forceinline__ void update(Octet& o, const AdamScalars& k, float grad_scale) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float g = o.g[e] * grad_scale;
-        const float x = REST == COLLAGE_REST_F32 ? o.rest[e] : REST == COLLAGE_REST_BF16 ? o.theta[e] + o.rest[e] : o.theta[e];
-        float delta;
+    for (int p = 0; p < 4; ++p) {
+        const uint64_t g = mul_pair(o.g[p], pair_of(grad_scale));
+        const uint64_t x = REST == COLLAGE_REST_F32 ? o.rest[p] : REST == COLLAGE_REST_BF16 ? add_pair(o.theta[p], o.rest[p]) : o.theta[p];
+        uint64_t delta;
         if (STATE == COLLAGE_STATE_F32) {
-            delta = adamw_fp32_delta(o.m[e], o.v[e], x, g, k.f);
+            float2 m = floats_of(o.m[p]), v = floats_of(o.v[p]);
+            const float2 gf = floats_of(g), xf = floats_of(x);
+            const float lo = adamw_fp32_delta(m.x, v.x, xf.x, gf.x, k.f), hi = adamw_fp32_delta(m.y, v.y, xf.y, gf.y, k.f);
+            delta = ops::pair_of(lo, hi);
+            o.m[p] = ops::pair_of(m.x, m.y);
+            o.v[p] = ops::pair_of(v.x, v.y);
         } else {
-            const float m = __fmaf_rn(k.f.b1, o.m[e], k.f.c1 * g), v = __fmaf_rn(k.f.b2, o.v[e] * o.v[e], k.f.c2 * (g * g));
-            const float root = fast_root(v);
-            const float den = k.f.flags & COLLAGE_FLAG_EPS_INSIDE_SQRT ? fast_root(__fmaf_rn(v, k.inv_bc2, k.f.eps)) : __fmaf_rn(root, k.inv_root_bc2, k.f.eps);
-            delta = k.f.neg_a * __fmaf_rn(k.f.lam, x, __fdividef(m * k.inv_bc1, den));
-            o.m[e] = m;
-            o.v[e] = root;
+            // every product and sum of the states is rounded once, so that their codes hang on nothing but the formulas
+            const uint64_t m = add_pair(mul_pair(o.m[p], pair_of(k.f.b1)), mul_pair(g, pair_of(k.f.c1)));
+            const uint64_t v = add_pair(mul_pair(mul_pair(o.v[p], o.v[p]), pair_of(k.f.b2)), mul_pair(mul_pair(g, g), pair_of(k.f.c2)));
+            const uint64_t root = root_pair(v);
+            uint64_t den;
+            if (k.f.flags & COLLAGE_FLAG_EPS_INSIDE_SQRT)
+                den = root_pair(fma_pair(v, pair_of(k.inv_bc2), pair_of(k.f.eps)));
+            else
+                den = fma_pair(root, pair_of(k.inv_root_bc2), pair_of(k.f.eps));
+            const uint64_t part = mul_pair(mul_pair(m, pair_of(k.inv_bc1)), reciprocal_pair(den));
+            delta = mul_pair(fma_pair(x, pair_of(k.f.lam), part), pair_of(k.f.neg_a));
+            o.m[p] = m;
+            o.v[p] = root;
         }
         if (REST == COLLAGE_REST_BF16) {
-            add_to_pair(o.theta[e], o.rest[e], delta, o.theta_out[e], o.rest_out[e]);
+            add_to_pair(o.theta[p], o.rest[p], delta, o.theta_out[p], o.rest_out[p]);
         } else {
-            const float to = x + delta;
-            o.rest[e] = to;
-            o.theta_out[e] = to_bf16(to);
+            o.rest[p] = add_pair(x, delta);
+            const float2 to = floats_of(o.rest[p]);
+            o.theta_out[p] = pack_bf16(to.x, to.y);
         }
     }
 }
 
+// Largest absolute value of eight over the warp; NaN where there is one.
+__device__ __forceinline__ uint32_t largest(const uint64_t (&f)[4]) {
+    float most = 0.0f;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const float2 v = floats_of(f[p]);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v.x)));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v.y)));
+    }
+    return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
+}
 // Scale of a group from the bits of its largest absolute value, and what its values are taken times.
 __device__ __forceinline__ float group_scale(uint32_t most, float& factor) {
     const float v = __uint_as_float(most);
-    factor = v < 0x1p-100f ? 0.0f : most >= 0x7F800000u ? NAN : kE4m3Max / v;
+    factor = v < 0x1p-100f ? 0.0f : most >= 0x7F800000u ? NAN : 1.0f / v * kE4m3Max;
     return v < 0x1p-100f ? 0.0f : most >= 0x7F800000u ? NAN : v * (1.0f / kE4m3Max);
 }
-// Code of a root before its last rounding, which is exact: rounded down after `random` (16 bits) of a step has been added.
-// Below 2^-6 the codes are equally spaced, as they are from 2^-6 to 2^-5.
-__device__ __forceinline__ float root_code(float root, float factor, uint32_t random) {
-    const float u = root > 0.0f ? fmaxf(root * factor, 0x1p-9f) : 0.0f;
-    const float shift = u < 0x1p-6f ? 0x1p-6f : 0.0f;
-    return __uint_as_float((__float_as_uint(u + shift) + (random << 4)) & 0xFFF00000u) - shift;
-}
-
-__device__ __forceinline__ float2 e4m3_pair(uint32_t two) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
-    return __half22float2(__half2(h));
-}
-
-// Eight consecutive floats
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(f[4], f[5], f[6], f[7]));
-}
-__device__ __forceinline__ uint4 pack_words(const uint32_t (&b)[8]) {
-    return make_uint4(b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16);
-}
-
-// One group of a tensor by a warp: whole and aligned, eight consecutive elements a lane.
-template <int STATE, int REST>
-__device__ __forceinline__ void whole_group(const AdamRec& t, uint64_t group, const AdamScalars& k, float grad_scale) {
-    const int lane = threadIdx.x & 31;
-    const uint64_t at = group * kGroup + lane * 8;
-    Octet<STATE, REST> o;
-    const uint4 qg = __ldcs(reinterpret_cast<const uint4*>(t.grad + at));
-    uint4 qt = make_uint4(0, 0, 0, 0), qr = qt;
-    uint2 qm = make_uint2(0, 0), qv = qm;
-    float m_scale = 0.0f, v_scale = 0.0f;
-    if (REST != COLLAGE_REST_F32) qt = __ldcs(reinterpret_cast<const uint4*>(t.theta + at));
-    if (REST == COLLAGE_REST_BF16) qr = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(t.rest) + at));
-    if (REST == COLLAGE_REST_F32) load8(static_cast<const float*>(t.rest) + at, o.rest);
-    if (STATE == COLLAGE_STATE_F32) {
-        load8(static_cast<const float*>(t.m) + at, o.m);
-        load8(static_cast<const float*>(t.v) + at, o.v);
-    } else {
-        qm = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + at));
-        qv = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at));
-        m_scale = t.m_scale[group];
-        v_scale = t.v_scale[group];
-    }
-    unpack8(qg, o.g);
-    if (REST != COLLAGE_REST_F32) unpack8(qt, o.theta);
-    if (REST == COLLAGE_REST_BF16) unpack8(qr, o.rest);
-    if (STATE == COLLAGE_STATE_E4M3) {
+// Codes of values to nearest even, as bytes.
+__device__ __forceinline__ uint2 nearest_codes(const uint64_t (&f)[4], float factor) {
+    uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const float2 m = e4m3_pair((e < 4 ? qm.x : qm.y) >> (8 * (e & 2))), v = e4m3_pair((e < 4 ? qv.x : qv.y) >> (8 * (e & 2)));
-            o.m[e] = m.x * m_scale; o.m[e + 1] = m.y * m_scale;
-            o.v[e] = v.x * v_scale; o.v[e + 1] = v.y * v_scale;
+    for (int p = 0; p < 4; ++p) {
+        const float2 v = floats_of(mul_pair(f[p], pair_of(factor)));
+        w[p] = pack_e4m3(v.x, v.y);
+    }
+    return make_uint2(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+}
+// Codes of roots, rounded down after `random` (16 bits for each; two in a word) of a step has been added.  From 2^-6 on a code is the
+// upper bits of the float, less the difference of the exponents' biases; below, codes are equally spaced, as they are from 2^-6 to 2^-5.
+__device__ __forceinline__ uint2 random_codes(const uint64_t (&f)[4], float factor, const uint32_t (&random)[4]) {
+    float u[8], least = INFINITY;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const float2 v = floats_of(mul_pair(f[p], pair_of(factor)));
+        u[2 * p] = v.x;
+        u[2 * p + 1] = v.y;
+        least = fminf(least, fminf(v.x, v.y));
+    }
+    uint32_t code[8];
+    if (least >= 0x1p-6f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {              // random << 8 below, 0x40 above: (127 - 7) << 27 less, modulo 2^32
+            const uint32_t r = __byte_perm(random[e / 2], 0x40u, e & 1 ? 0x4325 : 0x4105);
+            code[e] = (__float_as_uint(u[e]) << 4) + r;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float2 root = floats_of(f[e / 2]);
+            const float v = (e & 1 ? root.y : root.x) > 0.0f ? fmaxf(u[e], 0x1p-9f) : 0.0f, shift = v < 0x1p-6f ? 0x1p-6f : 0.0f;
+            const uint32_t part = e & 1 ? random[e / 2] >> 16 : random[e / 2] & 0xFFFFu;
+            code[e] = static_cast<uint32_t>(to_e4m3(__uint_as_float((__float_as_uint(v + shift) + (part << 4)) & 0xFFF00000u) - shift)) << 24;
         }
     }
+    uint32_t w[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) w[p] = __byte_perm(code[2 * p], code[2 * p + 1], 0x7373);
+    return make_uint2(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+}
+__device__ __forceinline__ uint32_t random_word(uint64_t pair, uint32_t key) {
+    return mix32(static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + key));
+}
+
+// Which elements of a whole group a lane has: eight in a row, or, where some array is of floats, four in a row of each half, so that
+// every access of a warp is to consecutive bytes.  A lane's bytes of a group of each array in shared memory, `kStages` groups ahead.
+template <int STATE, int REST>
+struct Form {
+    static constexpr bool kHalves = STATE == COLLAGE_STATE_F32 || REST == COLLAGE_REST_F32;
+    static constexpr bool kTheta = REST != COLLAGE_REST_F32;
+    static constexpr uint32_t kStateBytes = STATE == COLLAGE_STATE_F32 ? 4 : 1, kRestBytes = REST == COLLAGE_REST_F32 ? 4 : REST == COLLAGE_REST_BF16 ? 2 : 0;
+    // offsets of the arrays in a stage
+    static constexpr uint32_t kG = 0, kT = kG + 2 * kGroup, kR = kT + (kTheta ? 2 * kGroup : 0), kM = kR + kRestBytes * kGroup, kV = kM + kStateBytes * kGroup,
+                              kScales = kV + kStateBytes * kGroup, kStage = kScales + 16;
+    static constexpr int kStages = 3;
+    static __device__ __forceinline__ uint32_t element(int lane, int half) { return kHalves ? half * (kGroup / 2) + lane * 4 : lane * 8 + half * 4; }
+};
+constexpr int kAdamWarps = kAdamThreads / 32;
+
+template <uint32_t BYTES>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+
+// Sends for a lane's part of one array of a whole group, which begins at `from`.
+template <typename F, uint32_t BYTES>
+__device__ __forceinline__ void send_array(uint32_t stage, const void* from, int lane) {
+    const char* p = static_cast<const char*>(from);
+    if constexpr (F::kHalves) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) copy_async<4 * BYTES>(stage + F::element(lane, h) * BYTES, p + F::element(lane, h) * BYTES);
+    } else {
+        copy_async<8 * BYTES>(stage + lane * 8 * BYTES, p + lane * 8 * BYTES);
+    }
+}
+// Its eight elements, in 16, 32 or 64 bytes of words
+template <typename F, uint32_t BYTES>
+__device__ __forceinline__ void fetch_array(const uint8_t* stage, int lane, uint32_t (&w)[2 * BYTES]) {
+    constexpr int kHalf = BYTES;               // words of four elements
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(stage + F::element(lane, h) * BYTES);
+        if constexpr (kHalf == 4) {
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
+            w[h * 4] = q.x; w[h * 4 + 1] = q.y; w[h * 4 + 2] = q.z; w[h * 4 + 3] = q.w;
+        } else if constexpr (kHalf == 2) {
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
+            w[h * 2] = q.x; w[h * 2 + 1] = q.y;
+        } else {
+            w[h] = *p;
+        }
+    }
+}
+template <typename F, uint32_t BYTES>
+__device__ __forceinline__ void store_array(void* to, int lane, const uint32_t (&w)[2 * BYTES]) {
+    char* p = static_cast<char*>(to);
+    if constexpr (!F::kHalves && BYTES == 2) {
+        __stcs(reinterpret_cast<uint4*>(p + lane * 16), make_uint4(w[0], w[1], w[2], w[3]));
+    } else if constexpr (!F::kHalves && BYTES == 1) {
+        __stcs(reinterpret_cast<uint2*>(p + lane * 8), make_uint2(w[0], w[1]));
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            char* q = p + F::element(lane, h) * BYTES;
+            if constexpr (BYTES == 4) __stcs(reinterpret_cast<uint4*>(q), make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
+            if constexpr (BYTES == 2) __stcs(reinterpret_cast<uint2*>(q), make_uint2(w[2 * h], w[2 * h + 1]));
+            if constexpr (BYTES == 1) __stcs(reinterpret_cast<uint32_t*>(q), w[h]);
+        }
+    }
+}
+__device__ __forceinline__ void floats_to_words(const uint64_t (&f)[4], uint32_t (&w)[8]) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const float2 v = floats_of(f[p]);
+        w[2 * p] = __float_as_uint(v.x);
+        w[2 * p + 1] = __float_as_uint(v.y);
+    }
+}
+__device__ __forceinline__ void words_to_floats(const uint32_t (&w)[8], uint64_t (&f)[4]) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) f[p] = ops::pair_of(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
+}
+
+template <int STATE, int REST>
+__device__ __forceinline__ void send_group(const AdamRec& t, uint64_t group, uint32_t stage, int lane) {
+    using F = Form<STATE, REST>;
+    const uint64_t at = group * kGroup;
+    send_array<F, 2>(stage + F::kG, t.grad + at, lane);
+    if constexpr (F::kTheta) send_array<F, 2>(stage + F::kT, t.theta + at, lane);
+    if constexpr (F::kRestBytes) send_array<F, F::kRestBytes>(stage + F::kR, static_cast<const char*>(t.rest) + at * F::kRestBytes, lane);
+    send_array<F, F::kStateBytes>(stage + F::kM, static_cast<const char*>(t.m) + at * F::kStateBytes, lane);
+    send_array<F, F::kStateBytes>(stage + F::kV, static_cast<const char*>(t.v) + at * F::kStateBytes, lane);
+    if (STATE == COLLAGE_STATE_E4M3 && lane < 2) copy_async<4>(stage + F::kScales + 4 * lane, (lane ? t.v_scale : t.m_scale) + group);
+}
+
+// One group of a tensor by a warp: whole and aligned, its bytes in shared memory.
+template <int STATE, int REST>
+__device__ __forceinline__ void whole_group(const AdamRec& t, uint64_t group, const uint8_t* stage, const AdamScalars& k, float grad_scale, int lane) {
+    using F = Form<STATE, REST>;
+    const uint64_t at = group * kGroup;
+    Octet o;
+    uint32_t w[4];
+    fetch_array<F, 2>(stage + F::kG, lane, w);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) o.g[p] = bf16_pair(w[p]);
+    if constexpr (F::kTheta) {
+        fetch_array<F, 2>(stage + F::kT, lane, w);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o.theta[p] = bf16_pair(w[p]);
+    }
+    if constexpr (REST == COLLAGE_REST_BF16) {
+        fetch_array<F, 2>(stage + F::kR, lane, w);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o.rest[p] = bf16_pair(w[p]);
+    }
+    uint32_t wide[8];
+    if constexpr (REST == COLLAGE_REST_F32) {
+        fetch_array<F, 4>(stage + F::kR, lane, wide);
+        words_to_floats(wide, o.rest);
+    }
+    if constexpr (STATE == COLLAGE_STATE_F32) {
+        fetch_array<F, 4>(stage + F::kM, lane, wide);
+        words_to_floats(wide, o.m);
+        fetch_array<F, 4>(stage + F::kV, lane, wide);
+        words_to_floats(wide, o.v);
+    } else {
+        const float2 scales = *reinterpret_cast<const float2*>(stage + F::kScales);
+        uint32_t c[2];
+        fetch_array<F, 1>(stage + F::kM, lane, c);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o.m[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(scales.x));
+        fetch_array<F, 1>(stage + F::kV, lane, c);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o.v[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(scales.y));
+    }
     update<STATE, REST>(o, k, grad_scale);
-    __stcs(reinterpret_cast<uint4*>(t.theta + at), pack_words(o.theta_out));
-    if (REST == COLLAGE_REST_BF16) __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(t.rest) + at), pack_words(o.rest_out));
-    if (REST == COLLAGE_REST_F32) store8(static_cast<float*>(t.rest) + at, o.rest);
-    if (STATE == COLLAGE_STATE_F32) {
-        store8(static_cast<float*>(t.m) + at, o.m);
-        store8(static_cast<float*>(t.v) + at, o.v);
-        return;
+    store_array<F, 2>(t.theta + at, lane, o.theta_out);
+    if constexpr (REST == COLLAGE_REST_BF16) store_array<F, 2>(static_cast<uint16_t*>(t.rest) + at, lane, o.rest_out);
+    if constexpr (REST == COLLAGE_REST_F32) {
+        floats_to_words(o.rest, wide);
+        store_array<F, 4>(static_cast<float*>(t.rest) + at, lane, wide);
     }
-    uint32_t most_m = 0, most_v = 0;
+    if constexpr (STATE == COLLAGE_STATE_F32) {
+        floats_to_words(o.m, wide);
+        store_array<F, 4>(static_cast<float*>(t.m) + at, lane, wide);
+        floats_to_words(o.v, wide);
+        store_array<F, 4>(static_cast<float*>(t.v) + at, lane, wide);
+    } else {
+        float m_factor, v_factor;
+        const float m_scale = group_scale(largest(o.m), m_factor), v_scale = group_scale(largest(o.v), v_factor);
+        // the group's pairs begin at a multiple of 128, so their upper word is one
+        const uint64_t pair = (t.first + at) >> 1;
+        const uint32_t base = static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + k.key);
+        uint32_t random[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        most_m = max(most_m, __float_as_uint(o.m[e]) & 0x7FFFFFFFu);
-        most_v = max(most_v, __float_as_uint(o.v[e]) & 0x7FFFFFFFu);
-    }
-    float m_factor, v_factor;
-    m_scale = group_scale(__reduce_max_sync(0xFFFFFFFFu, most_m), m_factor);
-    v_scale = group_scale(__reduce_max_sync(0xFFFFFFFFu, most_v), v_factor);
-    const uint64_t pair = (t.first + at) >> 1;
-    const uint32_t base = static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + k.key);
-    uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        const uint32_t h = mix32(base + e / 2);                // (four pairs from a multiple of four on: no carry)
-        wm[e >> 2] |= pack_e4m3(o.m[e] * m_factor, o.m[e + 1] * m_factor) << (8 * (e & 2));
-        wv[e >> 2] |= pack_e4m3(root_code(o.v[e], v_factor, h & 0xFFFFu), root_code(o.v[e + 1], v_factor, h >> 16)) << (8 * (e & 2));
-    }
-    __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.m) + at), make_uint2(wm[0], wm[1]));
-    __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at), make_uint2(wv[0], wv[1]));
-    if (lane == 0) {
-        t.m_scale[group] = m_scale;
-        t.v_scale[group] = v_scale;
+        for (int p = 0; p < 4; ++p) random[p] = mix32(base + F::element(lane, p / 2) / 2 + (p & 1));
+        const uint2 cm = nearest_codes(o.m, m_factor), cv = random_codes(o.v, v_factor, random);
+        const uint32_t wm[2] = {cm.x, cm.y}, wv[2] = {cv.x, cv.y};
+        store_array<F, 1>(static_cast<uint8_t*>(t.m) + at, lane, wm);
+        store_array<F, 1>(static_cast<uint8_t*>(t.v) + at, lane, wv);
+        if (lane < 2) (lane ? t.v_scale : t.m_scale)[group] = lane ? v_scale : m_scale;
     }
 }
 
@@ -209,78 +378,150 @@ __device__ __forceinline__ void whole_group(const AdamRec& t, uint64_t group, co
 template <int STATE, int REST>
 __device__ __noinline__ void any_group(const AdamRec& t, uint64_t group, const AdamScalars& k, float grad_scale) {
     const int lane = threadIdx.x & 31;
-    const uint64_t begin = group * kGroup;
-    Octet<STATE, REST> o;
+    const uint64_t begin = group * kGroup + lane;
+    Octet o;
     float m_scale = 0.0f, v_scale = 0.0f;
     if (STATE == COLLAGE_STATE_E4M3) { m_scale = t.m_scale[group]; v_scale = t.v_scale[group]; }
+    auto gather = [&](uint64_t (&to)[4], auto&& value) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint64_t i = begin + e * 32 + lane;
-        o.g[e] = o.theta[e] = o.rest[e] = o.m[e] = o.v[e] = 0.0f;
-        if (i >= t.n) continue;
-        o.g[e] = bf16_value(t.grad[i]);
-        if (REST != COLLAGE_REST_F32) o.theta[e] = bf16_value(t.theta[i]);
-        if (REST == COLLAGE_REST_BF16) o.rest[e] = bf16_value(static_cast<const uint16_t*>(t.rest)[i]);
-        if (REST == COLLAGE_REST_F32) o.rest[e] = static_cast<const float*>(t.rest)[i];
-        if (STATE == COLLAGE_STATE_F32) {
-            o.m[e] = static_cast<const float*>(t.m)[i];
-            o.v[e] = static_cast<const float*>(t.v)[i];
-        } else {
-            o.m[e] = e4m3_pair(static_cast<const uint8_t*>(t.m)[i]).x * m_scale;
-            o.v[e] = e4m3_pair(static_cast<const uint8_t*>(t.v)[i]).x * v_scale;
+        for (int p = 0; p < 4; ++p) {
+            const uint64_t i = begin + p * 64, j = i + 32;
+            to[p] = ops::pair_of(i < t.n ? value(i) : 0.0f, j < t.n ? value(j) : 0.0f);
         }
+    };
+    auto code = [](const void* p, uint64_t i) { return floats_of(e4m3_pair(static_cast<const uint8_t*>(p)[i])).x; };
+    gather(o.g, [&](uint64_t i) { return bf16_value(t.grad[i]); });
+    if (REST != COLLAGE_REST_F32) gather(o.theta, [&](uint64_t i) { return bf16_value(t.theta[i]); });
+    if (REST == COLLAGE_REST_BF16) gather(o.rest, [&](uint64_t i) { return bf16_value(static_cast<const uint16_t*>(t.rest)[i]); });
+    if (REST == COLLAGE_REST_F32) gather(o.rest, [&](uint64_t i) { return static_cast<const float*>(t.rest)[i]; });
+    if (STATE == COLLAGE_STATE_F32) {
+        gather(o.m, [&](uint64_t i) { return static_cast<const float*>(t.m)[i]; });
+        gather(o.v, [&](uint64_t i) { return static_cast<const float*>(t.v)[i]; });
+    } else {
+        gather(o.m, [&](uint64_t i) { return code(t.m, i) * m_scale; });
+        gather(o.v, [&](uint64_t i) { return code(t.v, i) * v_scale; });
     }
     update<STATE, REST>(o, k, grad_scale);
-    uint32_t most_m = 0, most_v = 0;
+    auto scatter = [&](auto&& put) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint64_t i = begin + e * 32 + lane;
-        if (i >= t.n) continue;
-        t.theta[i] = static_cast<uint16_t>(o.theta_out[e]);
-        if (REST == COLLAGE_REST_BF16) static_cast<uint16_t*>(t.rest)[i] = static_cast<uint16_t>(o.rest_out[e]);
-        if (REST == COLLAGE_REST_F32) static_cast<float*>(t.rest)[i] = o.rest[e];
-        if (STATE == COLLAGE_STATE_F32) {
-            static_cast<float*>(t.m)[i] = o.m[e];
-            static_cast<float*>(t.v)[i] = o.v[e];
+        for (int p = 0; p < 4; ++p) {
+            const uint64_t i = begin + p * 64;
+            if (i < t.n) put(i, p, 0);
+            if (i + 32 < t.n) put(i + 32, p, 1);
         }
-        most_m = max(most_m, __float_as_uint(o.m[e]) & 0x7FFFFFFFu);
-        most_v = max(most_v, __float_as_uint(o.v[e]) & 0x7FFFFFFFu);
-    }
+    };
+    auto half = [](const uint64_t f, int h) { const float2 v = floats_of(f); return h ? v.y : v.x; };
+    scatter([&](uint64_t i, int p, int h) {
+        t.theta[i] = static_cast<uint16_t>(o.theta_out[p] >> (16 * h));
+        if (REST == COLLAGE_REST_BF16) static_cast<uint16_t*>(t.rest)[i] = static_cast<uint16_t>(o.rest_out[p] >> (16 * h));
+        if (REST == COLLAGE_REST_F32) static_cast<float*>(t.rest)[i] = half(o.rest[p], h);
+        if (STATE == COLLAGE_STATE_F32) {
+            static_cast<float*>(t.m)[i] = half(o.m[p], h);
+            static_cast<float*>(t.v)[i] = half(o.v[p], h);
+        }
+    });
     if (STATE == COLLAGE_STATE_F32) return;
+    // (elements behind the end: m = beta1 0 + ... 0 and a root of 0, which no scale minds)
     float m_factor, v_factor;
-    m_scale = group_scale(__reduce_max_sync(0xFFFFFFFFu, most_m), m_factor);
-    v_scale = group_scale(__reduce_max_sync(0xFFFFFFFFu, most_v), v_factor);
+    m_scale = group_scale(largest(o.m), m_factor);
+    v_scale = group_scale(largest(o.v), v_factor);
+    uint32_t random[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint64_t i = begin + e * 32 + lane;
-        if (i >= t.n) continue;
-        const uint64_t pair = (t.first + i) >> 1;
-        const uint32_t h = mix32(static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + k.key));
-        static_cast<uint8_t*>(t.m)[i] = to_e4m3(o.m[e] * m_factor);
-        static_cast<uint8_t*>(t.v)[i] = to_e4m3(root_code(o.v[e], v_factor, i & 1 ? h >> 16 : h & 0xFFFFu));
+    for (int p = 0; p < 4; ++p) {
+        const uint64_t i = t.first + begin + p * 64;
+        const uint32_t lo = random_word(i >> 1, k.key), hi = random_word((i + 32) >> 1, k.key);
+        random[p] = i & 1 ? __byte_perm(lo, hi, 0x7632) : __byte_perm(lo, hi, 0x5410);
     }
+    const uint2 cm = nearest_codes(o.m, m_factor), cv = random_codes(o.v, v_factor, random);
+    scatter([&](uint64_t i, int p, int h) {
+        const int shift = 8 * (2 * (p & 1) + h);
+        static_cast<uint8_t*>(t.m)[i] = static_cast<uint8_t>((p < 2 ? cm.x : cm.y) >> shift);
+        static_cast<uint8_t*>(t.v)[i] = static_cast<uint8_t>((p < 2 ? cv.x : cv.y) >> shift);
+    });
     if (lane == 0) {
         t.m_scale[group] = m_scale;
         t.v_scale[group] = v_scale;
     }
 }
 
-template <int STATE, int REST>
-__global__ void __launch_bounds__(kAdamThreads) adam_step_kernel(const __grid_constant__ AdamArgs a) {
-    after_previous();
-    const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
-    for (uint64_t c = blockIdx.x; c < a.num_chunks; c += gridDim.x) {
-        const AdamChunk chunk = a.chunks[c];
-        const AdamRec& t = a.tensors[chunk.tensor];
-        const uint64_t first = chunk.index * static_cast<uint64_t>(kAdamChunk / kGroup), end = (t.n + kGroup - 1) / kGroup;
-        const bool aligned = t.aligned;
-        for (uint64_t g = first + (threadIdx.x >> 5); g < min(first + kAdamChunk / kGroup, end); g += kAdamThreads / 32) {
-            if (aligned && (g + 1) * kGroup <= t.n)
-                whole_group<STATE, REST>(t, g, a.k, grad_scale);
-            else
-                any_group<STATE, REST>(t, g, a.k, grad_scale);
-        }
+// A warp's way through the groups of its tasks.
+struct Walk {
+    uint64_t task;
+    AdamChunk now;
+    uint32_t g, groups;
+    __device__ __forceinline__ void begin(const AdamArgs& a) {
+        if (task >= a.num_tasks) return;
+        now = a.tasks[task];
+        const uint64_t all = (a.tensors[now.tensor].n + kGroup - 1) / kGroup, first = static_cast<uint64_t>(now.index) * a.task_groups;
+        groups = static_cast<uint32_t>(min(static_cast<uint64_t>(a.task_groups), all - first));
+        g = 0;
     }
+    __device__ __forceinline__ void next(const AdamArgs& a, uint64_t stride) {
+        if (++g < groups) return;
+        task += stride;
+        begin(a);
+    }
+    __device__ __forceinline__ uint64_t group(const AdamArgs& a) const { return static_cast<uint64_t>(now.index) * a.task_groups + g; }
+};
+
+// Every warp by itself: it sends for the arrays of groups ahead of the one that it works on, each lane for its own bytes.
+template <int STATE, int REST>
+__global__ void __launch_bounds__(kAdamThreads, 3) adam_step_kernel(const __grid_constant__ AdamArgs a) {
+    using F = Form<STATE, REST>;
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    after_previous();
+    const int lane = threadIdx.x & 31;
+    uint8_t* stages = dynamic + (threadIdx.x >> 5) * (F::kStages * F::kStage);
+    const uint32_t stages_at = static_cast<uint32_t>(__cvta_generic_to_shared(stages));
+    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kAdamWarps;
+    const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
+    Walk ahead;
+    ahead.task = static_cast<uint64_t>(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+    ahead.begin(a);
+    Walk here = ahead;
+    auto is_whole = [](const AdamRec& t, uint64_t group) { return t.aligned && (group + 1) * kGroup <= t.n; };
+    auto send = [&](int stage) {
+        if (ahead.task < a.num_tasks) {
+            const AdamRec& t = a.tensors[ahead.now.tensor];
+            const uint64_t group = ahead.group(a);
+            if (is_whole(t, group)) send_group<STATE, REST>(t, group, stages_at + stage * F::kStage, lane);
+            ahead.next(a, stride);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int s = 0; s < F::kStages; ++s) send(s);
+    for (int stage = 0; here.task < a.num_tasks; here.next(a, stride)) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 1) : "memory");
+        __syncwarp();
+        const AdamRec& t = a.tensors[here.now.tensor];
+        const uint64_t group = here.group(a);
+        if (is_whole(t, group))
+            whole_group<STATE, REST>(t, group, stages + stage * F::kStage, a.k, grad_scale, lane);
+        else
+            any_group<STATE, REST>(t, group, a.k, grad_scale);
+        __syncwarp();
+        send(stage);
+        stage = stage + 1 == F::kStages ? 0 : stage + 1;
+    }
+}
+
+template <int STATE, int REST>
+static collage_status_t launch_adam(const AdamArgs& a, int sm_count, cudaStream_t s) {
+    using F = Form<STATE, REST>;
+    constexpr size_t smem = static_cast<size_t>(kAdamWarps) * F::kStages * F::kStage;
+    static std::atomic<int> per_device[64];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return COLLAGE_ERR_CUDA;
+    int resident = per_device[device].load(std::memory_order_acquire);
+    if (resident == 0) {
+        if (allow_smem<&adam_step_kernel<STATE, REST>>() != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, &adam_step_kernel<STATE, REST>, kAdamThreads, smem) != cudaSuccess)
+            return COLLAGE_ERR_CUDA;
+        resident = std::max(resident, 1);
+        per_device[device].store(resident, std::memory_order_release);
+    }
+    const uint64_t grid = std::min<uint64_t>((a.num_tasks + kAdamWarps - 1) / kAdamWarps, static_cast<uint64_t>(resident) * sm_count);
+    return launch<&adam_step_kernel<STATE, REST>>(grid, kAdamThreads, 1, smem, s, a);
 }
 
 // ---------------------------------------------------------------------------------------------------------- norm ---
@@ -375,13 +616,15 @@ using namespace collage::ops;
 
 struct collage_adam_plan {
     AdamRec* d_tensors = nullptr;
-    AdamChunk* d_chunks = nullptr;
-    uint64_t num_chunks = 0;
+    AdamChunk *d_chunks = nullptr, *d_tasks = nullptr;
+    uint64_t num_chunks = 0, num_tasks = 0;
+    uint32_t task_groups = 1;
     std::vector<ByteRange> ranges, written;    // sorted by address: all arrays, and those that a step writes
     int state = 0, rest = 0, device = -1;
     ~collage_adam_plan() {
         cudaFree(d_tensors);
         cudaFree(d_chunks);
+        cudaFree(d_tasks);
     }
 };
 
@@ -391,7 +634,7 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     const uint64_t state_bytes = state == COLLAGE_STATE_F32 ? 4 : 1, rest_bytes = rest == COLLAGE_REST_F32 ? 4 : 2;
     std::vector<ByteRange> ranges, written;
     std::vector<AdamRec> recs;
-    std::vector<AdamChunk> chunks;
+    std::vector<AdamChunk> chunks, tasks;
     uint64_t first = 0, num_chunks = 0;
     for (int i = 0; i < num; ++i) {
         const collage_adam_tensor_t& t = tensors[i];
@@ -436,8 +679,17 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     any_overlap(written);                      // (sorts)
     DeviceInfo dev;
     if (const collage_status_t st = current_device(&dev); st != COLLAGE_OK) return st;
+    // groups of a warp's turn: 16 where every warp of the device has several turns of that, fewer for small plans
+    uint32_t task_groups = 16;
+    while (task_groups > 1 && first / kGroup < static_cast<uint64_t>(task_groups) * 128 * dev.sm_count) task_groups /= 2;
+    for (size_t i = 0; i < recs.size(); ++i) {
+        const uint64_t own = ((recs[i].n + kGroup - 1) / kGroup + task_groups - 1) / task_groups;
+        for (uint64_t c = 0; c < own; ++c) tasks.push_back({static_cast<uint32_t>(i), static_cast<uint32_t>(c)});
+    }
     collage_adam_plan* plan = new collage_adam_plan;
     plan->num_chunks = num_chunks;
+    plan->num_tasks = tasks.size();
+    plan->task_groups = task_groups;
     plan->ranges = std::move(ranges);
     plan->written = std::move(written);
     plan->state = state;
@@ -445,6 +697,8 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     if (cudaGetDevice(&plan->device) != cudaSuccess ||
         (num_chunks && (cudaMalloc(&plan->d_tensors, recs.size() * sizeof(AdamRec)) != cudaSuccess ||
                         cudaMalloc(&plan->d_chunks, chunks.size() * sizeof(AdamChunk)) != cudaSuccess ||
+                        cudaMalloc(&plan->d_tasks, tasks.size() * sizeof(AdamChunk)) != cudaSuccess ||
+                        cudaMemcpy(plan->d_tasks, tasks.data(), tasks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_tensors, recs.data(), recs.size() * sizeof(AdamRec), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess))) {
         delete plan;
@@ -494,8 +748,9 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     if (plan->num_chunks == 0) return COLLAGE_OK;
     AdamArgs a = {};
     a.tensors = plan->d_tensors;
-    a.chunks = plan->d_chunks;
-    a.num_chunks = plan->num_chunks;
+    a.tasks = plan->d_tasks;
+    a.num_tasks = plan->num_tasks;
+    a.task_groups = plan->task_groups;
     a.grad_scale = grad_scale;
     a.k.f = fp32_scalars(hyper, step);
     const double t = static_cast<double>(step), bc1 = 1.0 - std::pow(hyper->beta1, t), bc2 = 1.0 - std::pow(hyper->beta2, t);
@@ -505,15 +760,14 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     uint32_t key = mix32(static_cast<uint32_t>(step >> 32));
     for (const uint64_t word : {step, seed >> 32, seed}) key = mix32(static_cast<uint32_t>(word) + key);
     a.k.key = key;
-    const uint64_t grid = std::min<uint64_t>(plan->num_chunks, (1ull << 31) - 1);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     switch (plan->state * 3 + plan->rest) {
-        case 0: return launch<&adam_step_kernel<0, 0>>(grid, kAdamThreads, 1, 0, s, a);
-        case 1: return launch<&adam_step_kernel<0, 1>>(grid, kAdamThreads, 1, 0, s, a);
-        case 2: return launch<&adam_step_kernel<0, 2>>(grid, kAdamThreads, 1, 0, s, a);
-        case 3: return launch<&adam_step_kernel<1, 0>>(grid, kAdamThreads, 1, 0, s, a);
-        case 4: return launch<&adam_step_kernel<1, 1>>(grid, kAdamThreads, 1, 0, s, a);
-        default: return launch<&adam_step_kernel<1, 2>>(grid, kAdamThreads, 1, 0, s, a);
+        case 0: return launch_adam<0, 0>(a, dev.sm_count, s);
+        case 1: return launch_adam<0, 1>(a, dev.sm_count, s);
+        case 2: return launch_adam<0, 2>(a, dev.sm_count, s);
+        case 3: return launch_adam<1, 0>(a, dev.sm_count, s);
+        case 4: return launch_adam<1, 1>(a, dev.sm_count, s);
+        default: return launch_adam<1, 2>(a, dev.sm_count, s);
     }
 }
 

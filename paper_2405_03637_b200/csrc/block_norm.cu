@@ -26,19 +26,25 @@ struct BlockNormArgs {
     int activation;
 };
 
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// 1 / (1 + exp(-g)) and what it lacks of 1, both to a float's precision wherever g is
+__device__ __forceinline__ float2 sigmoids(float g) {
+    const float t = __expf(-fabsf(g)), large = __fdividef(1.0f, 1.0f + t), small = t * large;
+    return g < 0.0f ? make_float2(small, large) : make_float2(large, small);
+}
 // A(g), and its derivative; the kind is the same for all threads
 __device__ __forceinline__ float gate_value(int kind, float g) {
     if (kind == COLLAGE_GATE_NONE) return g;
-    const float s = sigmoid(g);
+    const float s = sigmoids(g).x;
     return kind == COLLAGE_GATE_SIGMOID ? s : g == -INFINITY ? -0.0f : g * s;
 }
-__device__ __forceinline__ float gate_slope(int kind, float g) {
-    if (kind == COLLAGE_GATE_NONE) return 1.0f;
-    const float s = sigmoid(g), back = sigmoid(-g);          // 1 - s, also where s is nearly 1
-    if (kind == COLLAGE_GATE_SIGMOID) return s * back;
-    return fabsf(g) == INFINITY ? s : s + g * s * back;
+__device__ __forceinline__ float2 gate_value_and_slope(int kind, float g) {
+    if (kind == COLLAGE_GATE_NONE) return make_float2(g, 1.0f);
+    const float2 s = sigmoids(g);
+    if (kind == COLLAGE_GATE_SIGMOID) return make_float2(s.x, s.x * s.y);
+    if (fabsf(g) == INFINITY) return make_float2(g < 0.0f ? -0.0f : g, s.x);
+    return make_float2(g * s.x, __fmaf_rn(g * s.x, s.y, s.x));
 }
+__device__ __forceinline__ float gate_slope(int kind, float g) { return gate_value_and_slope(kind, g).y; }
 
 constexpr int kBlockThreads = 256;
 
@@ -303,6 +309,231 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
     }
 }
 
+// Rows of whole vectors in one pass: blocks walk over rows, one at a time for each group of `group_threads`.  A thread owns PER vectors of
+// columns: it sends for its own of the next two rows ahead, so that loads go on while a row's two sums are joined, and keeps its columns'
+// sums over rows in registers until the end.
+constexpr int kBackwardDepth = 2;
+
+template <int PER, int THREADS, bool TOKEN_GATE>
+__global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads) {
+    constexpr int kArrays = TOKEN_GATE ? 5 : 4;
+    __shared__ float slots[2][THREADS / 32];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    after_previous();
+    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
+    const int lane = threadIdx.x & 31, group_warps = group_threads >> 5, warp0 = group * group_warps;
+    const int vectors = static_cast<int>(a.cols >> 3);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    uint4* mine = reinterpret_cast<uint4*>(dynamic) + threadIdx.x;      // [kBackwardDepth][kArrays][PER] places, blockDim.x apart
+    auto place = [&](int stage, int array, int i) { return mine + ((stage * kArrays + array) * PER + i) * blockDim.x; };
+    // factors of the columns, in floats, for the block's groups alike: post_weight, and the gate's value where it is one of channels
+    uint4 qpre[PER], qpost[PER];
+    float sum_pre[PER][8], sum_post[PER][8];
+    const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * group_threads;
+        qpre[i] = a.pre && v < vectors ? reinterpret_cast<const uint4*>(a.pre)[v] : none;
+        qpost[i] = v < vectors ? (a.post ? reinterpret_cast<const uint4*>(a.post)[v] : ones) : none;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum_pre[i][e] = sum_post[i][e] = 0.0f;
+        for (int d = 0; d < kBackwardDepth; ++d)
+            for (int k = 0; k < kArrays; ++k) *place(d, k, i) = none;         // places that no load fills
+    }
+    float* channel = reinterpret_cast<float*>(mine - threadIdx.x + kBackwardDepth * kArrays * PER * blockDim.x);     // [cols] A(gate), with a gate of channels
+    const bool channels = !TOKEN_GATE && a.gate;
+    if (channels) {
+        for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) channel[j] = gate_value(a.activation, bf16_value(a.gate[j]));
+        __syncthreads();
+    }
+    const uint64_t first = blockIdx.x * static_cast<uint64_t>(groups) + group, step = static_cast<uint64_t>(gridDim.x) * groups;
+    auto send_for = [&](uint64_t row, int stage) {
+        if (row < a.rows) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int v = t + i * group_threads;
+                if (v >= vectors) continue;
+                auto copy = [&](int k, const uint16_t* base, uint64_t ld) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(place(stage, k, i)))),
+                                 "l"(reinterpret_cast<const uint4*>(base + row * ld) + v)
+                                 : "memory");
+                };
+                if (a.dy) {
+                    copy(0, a.dy, a.lddy);
+                    copy(1, a.r, a.ldr);
+                }
+                if (a.dr) copy(2, a.dr, a.lddr);
+                copy(3, a.o, a.ldo);
+                if (TOKEN_GATE) copy(4, a.gate, a.ldg);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int d = 0; d < kBackwardDepth; ++d) send_for(first + d * step, d);
+    const float per_col = 1.0f / static_cast<float>(a.cols);
+    // over the group; the two sums of a row have slots of their own, so that one barrier each is enough
+    auto joined = [&](float v, int which) {
+        v = warp_sum(v);
+        if (group_warps > 1) {
+            if (lane == 0) slots[which][threadIdx.x >> 5] = v;
+            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
+            v = warp_sum(lane < group_warps ? slots[which][warp0 + lane] : 0.0f);
+        }
+        return v;
+    };
+    int stage = 0;
+    const bool second = a.post && a.dblock;
+    for (uint64_t row = first; row < a.rows; row += step) {
+        const float rstd_r = a.dy ? a.rstd_pre[row] : 0.0f, rstd_o = a.post ? a.rstd_post[row] : 1.0f;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kBackwardDepth - 1) : "memory");
+        float mean = 0.0f;
+        if (a.dy) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                float dy[8], r[8], w[8];
+                unpack8(*place(stage, 0, i), dy);
+                unpack8(*place(stage, 1, i), r);
+                unpack8(qpre[i], w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float n = r[e] * rstd_r;
+                    sum_pre[i][e] = __fmaf_rn(dy[e], n, sum_pre[i][e]);
+                    sum = __fmaf_rn(dy[e] * w[e], n, sum);
+                }
+            }
+            mean = joined(sum, 0) * per_col;
+        }
+        float d[PER][8];                        // the stream's gradient, then h
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[i][e] = 0.0f;
+            if (a.dy) {
+                float dy[8], r[8], w[8];
+                unpack8(*place(stage, 0, i), dy);
+                unpack8(*place(stage, 1, i), r);
+                unpack8(qpre[i], w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[i][e] = rstd_r * __fmaf_rn(-r[e] * rstd_r, mean, dy[e] * w[e]);
+            }
+            if (a.dr) {
+                float dr[8];
+                unpack8(*place(stage, 2, i), dr);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[i][e] += dr[e];
+            }
+            if (a.dx && v < vectors) {
+                float dx[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dx[e] = a.alpha * d[i][e];
+                reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack8(dx);
+            }
+            float o[8], w[8];
+            unpack8(*place(stage, 3, i), o);
+            unpack8(qpost[i], w);
+            if (TOKEN_GATE) {
+                float g[8], dg[8];
+                unpack8(*place(stage, 4, i), g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 gate = gate_value_and_slope(a.activation, g[e]);
+                    const float n = o[e] * rstd_o, u = a.beta * d[i][e];
+                    dg[e] = u * n * w[e] * gate.y;
+                    d[i][e] = u * gate.x;
+                    sum_post[i][e] = __fmaf_rn(d[i][e], n, sum_post[i][e]);
+                    d[i][e] *= w[e];
+                    sum = __fmaf_rn(d[i][e], n, sum);
+                }
+                if (a.dgate && v < vectors) reinterpret_cast<uint4*>(a.dgate + row * a.lddg)[v] = pack8(dg);
+            } else {
+                float A[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+                if (channels && v < vectors) {
+                    const float4 lo = reinterpret_cast<const float4*>(channel)[2 * v], hi = reinterpret_cast<const float4*>(channel)[2 * v + 1];
+                    A[0] = lo.x; A[1] = lo.y; A[2] = lo.z; A[3] = lo.w; A[4] = hi.x; A[5] = hi.y; A[6] = hi.z; A[7] = hi.w;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float n = o[e] * rstd_o, u = a.beta * d[i][e];
+                    sum_post[i][e] = __fmaf_rn(u, n, sum_post[i][e]);
+                    d[i][e] = u * A[e] * w[e];
+                    sum = __fmaf_rn(d[i][e], n, sum);
+                }
+            }
+        }
+        if (a.dblock) {
+            mean = second ? joined(sum, 1) * per_col : 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int v = t + i * group_threads;
+                if (a.post) {
+                    float o[8];
+                    unpack8(*place(stage, 3, i), o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[i][e] = rstd_o * __fmaf_rn(-o[e] * rstd_o, mean, d[i][e]);
+                }
+                if (v < vectors) reinterpret_cast<uint4*>(a.dblock + row * a.lddo)[v] = pack8(d[i]);
+            }
+        }
+        send_for(row + kBackwardDepth * step, stage);
+        stage = stage + 1 == kBackwardDepth ? 0 : stage + 1;
+        // (of two sums, each one's barrier parts the other's slots between rows; one alone needs a second barrier)
+        if (group_warps > 1 && (a.dy != nullptr) != second) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
+    }
+    if (!a.sums) return;
+    // the block's groups in order, then one row of partial sums a block
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    float* shared_sums = reinterpret_cast<float*>(dynamic);             // [groups - 1][2][cols]
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * group_threads;
+        if (group == 0 || v >= vectors) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            shared_sums[(2 * group - 2) * a.cols + v * 8 + e] = sum_pre[i][e];
+            shared_sums[(2 * group - 1) * a.cols + v * 8 + e] = sum_post[i][e];
+        }
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * group_threads;
+        if (v >= vectors) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            for (int g = 1; g < groups; ++g) {
+                sum_pre[i][e] += shared_sums[(2 * g - 2) * a.cols + v * 8 + e];
+                sum_post[i][e] += shared_sums[(2 * g - 1) * a.cols + v * 8 + e];
+            }
+        for (int k = 0; k < 2; ++k) {
+            float4* out = reinterpret_cast<float4*>(a.partial + (2ull * blockIdx.x + k) * a.cols + v * 8);
+            const float* s = k ? sum_post[i] : sum_pre[i];
+            out[0] = make_float4(s[0], s[1], s[2], s[3]);
+            out[1] = make_float4(s[4], s[5], s[6], s[7]);
+        }
+    }
+}
+
+template <int PER, int THREADS, bool TOKEN_GATE>
+static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3;
+    const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), groups = std::max(1, std::min(THREADS / group, 15));
+    // the places hold the groups' sums too: 8 cols bytes a group, against 64 kBackwardDepth bytes for each 8 columns
+    const size_t smem = static_cast<size_t>(kBackwardDepth) * (TOKEN_GATE ? 5 : 4) * PER * 16 * group * groups + (!TOKEN_GATE && a.gate ? 4 * a.cols : 0);
+    *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
+    return launch<&block_norm_backward_kernel<PER, THREADS, TOKEN_GATE>>(*parts, group * groups, 1, smem, s, a, group);
+}
+// Rows of up to 256 columns are a warp's, without barriers; longer ones take two vectors a thread.
+template <bool TOKEN_GATE>
+static collage_status_t launch_block_backward(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
+    return a.cols <= 256 ? launch_block_backward_as<1, 512, TOKEN_GATE>(a, parts, sm_count, s) : launch_block_backward_as<2, 512, TOKEN_GATE>(a, parts, sm_count, s);
+}
+
 // The blocks' parts added up in order: 32 columns a block, each of its 32 warps takes every 32nd part.  From the shared sum
 // S = sum u n: dpost = A S and dgate = A' w S for a gate of channels, dpost = S otherwise.
 struct BlockNormFinishArgs {
@@ -498,8 +729,14 @@ collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, con
     a.beta = static_cast<float>(in->block_scale);
     a.activation = in->activation;
     a.sums = sums;
-    const unsigned parts = static_cast<unsigned>(std::min<uint64_t>({rows, static_cast<uint64_t>(kBlockParts), 2ull * dev.sm_count}));
-    st = launch<&block_norm_backward_any_kernel>(parts, kBlockThreads, 1, 0, s, a);
+    bool fit = cols % 8 == 0 && cols <= 8192 && aligned(a.post) && aligned(a.pre) && (!a.gate || rows_aligned(&in->gate, 2, 16)) &&
+               (!a.dgate || rows_aligned(dgate, 2, 16));
+    for (const collage_matrix_t* m : all) fit = fit && (!m || rows_aligned(m, 2, 16));
+    unsigned parts = static_cast<unsigned>(std::min<uint64_t>({rows, static_cast<uint64_t>(kBlockParts), 2ull * dev.sm_count}));
+    if (!fit)
+        st = launch<&block_norm_backward_any_kernel>(parts, kBlockThreads, 1, 0, s, a);
+    else
+        st = a.token_gate ? launch_block_backward<true>(a, &parts, dev.sm_count, s) : launch_block_backward<false>(a, &parts, dev.sm_count, s);
     if (st != COLLAGE_OK || !sums) return st;
     BlockNormFinishArgs f = {};
     f.partial = a.partial;
