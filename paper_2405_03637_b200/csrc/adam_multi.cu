@@ -9,6 +9,7 @@
 // m moves by a tenth of what separates it from the gradient and is rounded to nearest.
 // All of it is bound by memory: 10 (theta alone) to 16 bytes a parameter with 8-bit states, 22 to 28 with floats.
 #include "adamw_float.cuh"
+#include "bulk_pipe.cuh"
 #include "ops_common.cuh"
 
 #include <new>
@@ -17,7 +18,7 @@ namespace collage {
 namespace ops {
 
 constexpr uint32_t kGroup = 256;               // elements that share a scale: a warp's, eight a lane
-constexpr uint32_t kAdamChunk = 4096;          // elements of the norm's turns
+constexpr uint32_t kAdamChunk = 4096;          // elements of a block's turn
 constexpr int kAdamThreads = 256;
 
 struct AdamRec {
@@ -26,7 +27,7 @@ struct AdamRec {
     float *m_scale, *v_scale;
     const uint16_t* grad;
     uint64_t n, first;                         // first: position of its first element in the plan
-    uint64_t aligned;                          // all arrays on 16 bytes (codes on 8)
+    uint64_t aligned;                          // all arrays but the scales begin on 16 bytes
 };
 struct AdamChunk {
     uint32_t tensor, index;
@@ -34,15 +35,15 @@ struct AdamChunk {
 
 struct AdamScalars {
     Fp32Scalars f;
-    float inv_bc1, inv_bc2, inv_root_bc2;      // 1 / bc1, 1 / bc2, 1 / sqrt(bc2)
+    float rate, decay;                         // -a / bc1, -a lam
+    float inv_bc2, inv_root_bc2;               // 1 / bc2, 1 / sqrt(bc2)
     uint32_t key;
 };
 
 struct AdamArgs {
     const AdamRec* tensors;
-    const AdamChunk* tasks;                    // task: task_groups groups of a tensor, for one warp
-    uint64_t num_tasks;
-    uint32_t task_groups;
+    const AdamChunk* chunks;
+    uint64_t num_chunks;
     const float* grad_scale;
     AdamScalars k;
 };
@@ -56,7 +57,21 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
 }
 
 __device__ __forceinline__ uint64_t pair_of(float v) { return ops::pair_of(v, v); }
-__device__ __forceinline__ uint64_t sub_pair(uint64_t a, uint64_t b) { return fma_pair(b, pair_of(-1.0f), a); }
+__device__ __forceinline__ uint64_t sub_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// times a constant of the call, plus another
+__device__ __forceinline__ uint64_t scaled_pair(uint64_t a, float c) {
+    return mul_pair(a, pair_of(c));
+}
+__device__ __forceinline__ uint64_t scaled_plus(uint64_t a, float c, float d) {
+    return fma_pair(a, pair_of(c), pair_of(d));
+}
+__device__ __forceinline__ uint64_t scaled_plus(uint64_t a, float c, uint64_t d) {
+    return fma_pair(a, pair_of(c), d);
+}
 __device__ __forceinline__ uint64_t bf16_pair(uint32_t word) { return ops::pair_of(bf16_lo(word), bf16_hi(word)); }
 __device__ __forceinline__ uint64_t e4m3_pair(uint32_t two) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
@@ -72,7 +87,8 @@ __device__ __forceinline__ uint64_t root_pair(uint64_t v) {
     asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(f.x, 0x1p-149f)));         // (of 0: 0 times a finite number)
     asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(f.y, 0x1p-149f)));
     const uint64_t y2 = ops::pair_of(y.x, y.y), r = mul_pair(v, y2);
-    return fma_pair(fma_pair(r, r, mul_pair(v, pair_of(-1.0f))), mul_pair(y2, pair_of(-0.5f)), r);
+    const float2 q = floats_of(r);
+    return ops::pair_of(__fmaf_rn(__fmaf_rn(-q.x, q.x, f.x), 0.5f * y.x, q.x), __fmaf_rn(__fmaf_rn(-q.y, q.y, f.y), 0.5f * y.y, q.y));
 }
 __device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
     float2 f = floats_of(v);
@@ -81,27 +97,31 @@ __device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
     return ops::pair_of(f.x, f.y);
 }
 
-// (theta, rest) + delta: theta' is the bfloat16 nearest to theta + RN(rest + delta), rest' what that lacks.
-__device__ __forceinline__ void add_to_pair(uint64_t theta, uint64_t rest, uint64_t delta, uint32_t& theta_word, uint32_t& rest_word) {
+// (theta, rest) + delta: theta' is the bfloat16 nearest to theta + RN(rest + delta), rest' what that lacks.  A float half-way between two
+// bfloat16 values does not tell which one is nearer: that hangs on what the float has lost.  With TIES it is rounded to odd first, towards
+// the sum's own side; without, `low` takes the smallest of the sums' lower half-words (as signed numbers), which is -32768 if there is
+// such a float among them (one in 65536).
+template <bool TIES>
+__device__ __forceinline__ void add_to_pair(uint64_t theta, uint64_t rest, uint64_t delta, uint32_t& theta_word, uint32_t& rest_word, uint32_t& low) {
     const uint64_t t = add_pair(rest, delta), s = add_pair(theta, t), back = sub_pair(s, theta);
     const uint64_t lost = add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back));                  // exact: theta + t = s + lost
-    const float2 sum = floats_of(s);
-    theta_word = pack_bf16(sum.x, sum.y);
-    // A float half-way between two bfloat16 values: which one is nearer hangs on what the float has lost.  It is rounded to odd first,
-    // towards the sum's own side.  (One in 65536; the test finds a half-word of 0x8000, and now and then another.)
-    const uint32_t low = __byte_perm(__float_as_uint(sum.x), __float_as_uint(sum.y), 0x5410) ^ 0x80008000u;
-    if ((low - 0x00010001u) & ~low & 0x80008000u) {
+    float2 sum = floats_of(s);
+    if (TIES) {
         const float2 l = floats_of(lost);
         auto odd = [](float f, float rest_of) {
             const uint32_t bits = __float_as_uint(f);
             const bool off = rest_of != 0.0f && fabsf(rest_of) < INFINITY;
             return __uint_as_float(off ? (bits - ((__float_as_uint(rest_of) ^ bits) >> 31)) | 1u : bits);
         };
-        theta_word = pack_bf16(odd(sum.x, l.x), odd(sum.y, l.y));
+        sum = make_float2(odd(sum.x, l.x), odd(sum.y, l.y));
+    } else {
+        low = __vmins2(low, __byte_perm(__float_as_uint(sum.x), __float_as_uint(sum.y), 0x5410));
     }
+    theta_word = pack_bf16(sum.x, sum.y);
     const float2 r = floats_of(add_pair(sub_pair(s, bf16_pair(theta_word)), lost));
     rest_word = pack_bf16(r.x, r.y);
 }
+__device__ __forceinline__ bool has_tie(uint32_t low) { return (low & 0xFFFFu) == 0x8000u || low >> 16 == 0x8000u; }
 
 // Eight elements of a lane, in pairs, before and behind the update.  With states in 8 bits v is its root.
 struct Octet {
@@ -109,11 +129,12 @@ struct Octet {
     uint32_t theta_out[4], rest_out[4];                  // two bfloat16 each
 };
 
-template <int STATE, int REST>
-__device__ __forceinline__ void update(Octet& o, const AdamScalars& k, float grad_scale) {
+template <int STATE, int REST, bool INSIDE, bool TIES>
+__device__ __forceinline__ uint32_t update(Octet& o, const AdamScalars& k, float grad_scale) {
+    uint32_t low = 0;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const uint64_t g = mul_pair(o.g[p], pair_of(grad_scale));
+        const uint64_t g = scaled_pair(o.g[p], grad_scale);
         const uint64_t x = REST == COLLAGE_REST_F32 ? o.rest[p] : REST == COLLAGE_REST_BF16 ? add_pair(o.theta[p], o.rest[p]) : o.theta[p];
         uint64_t delta;
         if (STATE == COLLAGE_STATE_F32) {
@@ -125,27 +146,23 @@ __device__ __forceinline__ void update(Octet& o, const AdamScalars& k, float gra
             o.v[p] = ops::pair_of(v.x, v.y);
         } else {
             // every product and sum of the states is rounded once, so that their codes hang on nothing but the formulas
-            const uint64_t m = add_pair(mul_pair(o.m[p], pair_of(k.f.b1)), mul_pair(g, pair_of(k.f.c1)));
-            const uint64_t v = add_pair(mul_pair(mul_pair(o.v[p], o.v[p]), pair_of(k.f.b2)), mul_pair(mul_pair(g, g), pair_of(k.f.c2)));
+            const uint64_t m = add_pair(scaled_pair(o.m[p], k.f.b1), scaled_pair(g, k.f.c1));
+            const uint64_t v = add_pair(scaled_pair(mul_pair(o.v[p], o.v[p]), k.f.b2), scaled_pair(mul_pair(g, g), k.f.c2));
             const uint64_t root = root_pair(v);
-            uint64_t den;
-            if (k.f.flags & COLLAGE_FLAG_EPS_INSIDE_SQRT)
-                den = root_pair(fma_pair(v, pair_of(k.inv_bc2), pair_of(k.f.eps)));
-            else
-                den = fma_pair(root, pair_of(k.inv_root_bc2), pair_of(k.f.eps));
-            const uint64_t part = mul_pair(mul_pair(m, pair_of(k.inv_bc1)), reciprocal_pair(den));
-            delta = mul_pair(fma_pair(x, pair_of(k.f.lam), part), pair_of(k.f.neg_a));
+            const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : scaled_plus(root, k.inv_root_bc2, k.f.eps);
+            delta = scaled_plus(x, k.decay, scaled_pair(mul_pair(m, reciprocal_pair(den)), k.rate));
             o.m[p] = m;
             o.v[p] = root;
         }
         if (REST == COLLAGE_REST_BF16) {
-            add_to_pair(o.theta[p], o.rest[p], delta, o.theta_out[p], o.rest_out[p]);
+            add_to_pair<TIES>(o.theta[p], o.rest[p], delta, o.theta_out[p], o.rest_out[p], low);
         } else {
             o.rest[p] = add_pair(x, delta);
             const float2 to = floats_of(o.rest[p]);
             o.theta_out[p] = pack_bf16(to.x, to.y);
         }
     }
+    return low;
 }
 
 // Largest absolute value of eight over the warp; NaN where there is one.
@@ -154,16 +171,19 @@ __device__ __forceinline__ uint32_t largest(const uint64_t (&f)[4]) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const float2 v = floats_of(f[p]);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v.x)));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v.y)));
+        asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(fabsf(v.x)), "f"(fabsf(v.y)));
     }
     return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
 }
 // Scale of a group from the bits of its largest absolute value, and what its values are taken times.
 __device__ __forceinline__ float group_scale(uint32_t most, float& factor) {
     const float v = __uint_as_float(most);
-    factor = v < 0x1p-100f ? 0.0f : most >= 0x7F800000u ? NAN : 1.0f / v * kE4m3Max;
-    return v < 0x1p-100f ? 0.0f : most >= 0x7F800000u ? NAN : v * (1.0f / kE4m3Max);
+    float r;                                   // 1 / v, by a step of Newton's method
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    r = __fmaf_rn(__fmaf_rn(-v, r, 1.0f), r, r);
+    const bool none = v < 0x1p-100f, off = most >= 0x7F800000u;
+    factor = none ? 0.0f : off ? NAN : r * kE4m3Max;
+    return none ? 0.0f : off ? NAN : v * (1.0f / kE4m3Max);
 }
 // Codes of values to nearest even, as bytes.
 __device__ __forceinline__ uint2 nearest_codes(const uint64_t (&f)[4], float factor) {
@@ -184,7 +204,7 @@ __device__ __forceinline__ uint2 random_codes(const uint64_t (&f)[4], float fact
         const float2 v = floats_of(mul_pair(f[p], pair_of(factor)));
         u[2 * p] = v.x;
         u[2 * p + 1] = v.y;
-        least = fminf(least, fminf(v.x, v.y));
+        asm("min.f32 %0, %0, %1, %2;" : "+f"(least) : "f"(v.x), "f"(v.y));
     }
     uint32_t code[8];
     if (least >= 0x1p-6f) {
@@ -211,72 +231,81 @@ __device__ __forceinline__ uint32_t random_word(uint64_t pair, uint32_t key) {
     return mix32(static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + key));
 }
 
-// Which elements of a whole group a lane has: eight in a row, or, where some array is of floats, four in a row of each half, so that
-// every access of a warp is to consecutive bytes.  A lane's bytes of a group of each array in shared memory, `kStages` groups ahead.
+// A stage of the copy pipeline: a tile's bytes of each array.  Of a whole group a lane has eight elements in a row, or, where some array
+// is of floats, four in a row of each half, so that a warp's accesses are to consecutive bytes.
 template <int STATE, int REST>
 struct Form {
     static constexpr bool kHalves = STATE == COLLAGE_STATE_F32 || REST == COLLAGE_REST_F32;
-    static constexpr bool kTheta = REST != COLLAGE_REST_F32;
+    static constexpr bool kReadsTheta = REST != COLLAGE_REST_F32;
     static constexpr uint32_t kStateBytes = STATE == COLLAGE_STATE_F32 ? 4 : 1, kRestBytes = REST == COLLAGE_REST_F32 ? 4 : REST == COLLAGE_REST_BF16 ? 2 : 0;
     // offsets of the arrays in a stage
-    static constexpr uint32_t kG = 0, kT = kG + 2 * kGroup, kR = kT + (kTheta ? 2 * kGroup : 0), kM = kR + kRestBytes * kGroup, kV = kM + kStateBytes * kGroup,
-                              kScales = kV + kStateBytes * kGroup, kStage = kScales + 16;
-    static constexpr int kStages = 3;
+    static constexpr uint32_t kG = 0, kT = kG + 2 * kAdamChunk, kR = kT + 2 * kAdamChunk, kM = kR + kRestBytes * kAdamChunk, kV = kM + kStateBytes * kAdamChunk,
+                              kStage = kV + kStateBytes * kAdamChunk;
+    // As many stages as 200 KB hold (three to eight).  With 110 KB 134 M parameters take 345 us instead of 329 (8-bit states, pairs), 429 instead
+    // of 320 (8-bit states, master weights).
+    static constexpr int kStages = 200 * 1024 / kStage;
+    // Warps beside the one that copies.  One more than a multiple of four would cost all of them registers: a quarter of an SM would have
+    // one warp more to share its own among.  Of 15, 19, 23, 27 these measured best: 15 where there are master weights (67 M parameters, float
+    // states: 288 us, 19 take 305), 19 elsewhere (272 us with pairs, 15 take 288).
+    static constexpr int kWarps = REST == COLLAGE_REST_F32 ? 15 : 19;
     static __device__ __forceinline__ uint32_t element(int lane, int half) { return kHalves ? half * (kGroup / 2) + lane * 4 : lane * 8 + half * 4; }
 };
-constexpr int kAdamWarps = kAdamThreads / 32;
+constexpr uint32_t kTileGroups = kAdamChunk / kGroup;
 
-template <uint32_t BYTES>
-__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
-    if constexpr (BYTES == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-    else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
-}
+// What consumers have to know of the tile in a stage.
+struct AdamTile {
+    const AdamRec* tensor;
+    uint64_t first_group;                      // of the tensor
+    uint32_t groups, whole;                    // in the tile; of these, in shared memory
+    uint32_t random;                           // what its pairs' numbers are added to before they are mixed
+    float scales[2 * kTileGroups];             // of m, then of the root
+};
+template <int STATE, int REST>
+struct AdamSmem {
+    using F = Form<STATE, REST>;
+    alignas(128) uint8_t bytes[F::kStages][F::kStage];
+    AdamTile tile[F::kStages];
+    alignas(8) uint64_t full[F::kStages], done[F::kStages];
+};
 
-// Sends for a lane's part of one array of a whole group, which begins at `from`.
+// A lane's eight elements of one array of a group, in 8, 16 or 32 bytes of words
 template <typename F, uint32_t BYTES>
-__device__ __forceinline__ void send_array(uint32_t stage, const void* from, int lane) {
-    const char* p = static_cast<const char*>(from);
-    if constexpr (F::kHalves) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) copy_async<4 * BYTES>(stage + F::element(lane, h) * BYTES, p + F::element(lane, h) * BYTES);
+__device__ __forceinline__ void fetch_array(const uint8_t* group, int lane, uint32_t (&w)[2 * BYTES]) {
+    if constexpr (!F::kHalves && BYTES == 2) {
+        const uint4 q = *reinterpret_cast<const uint4*>(group + lane * 16);
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else if constexpr (!F::kHalves && BYTES == 1) {
+        const uint2 q = *reinterpret_cast<const uint2*>(group + lane * 8);
+        w[0] = q.x; w[1] = q.y;
     } else {
-        copy_async<8 * BYTES>(stage + lane * 8 * BYTES, p + lane * 8 * BYTES);
-    }
-}
-// Its eight elements, in 16, 32 or 64 bytes of words
-template <typename F, uint32_t BYTES>
-__device__ __forceinline__ void fetch_array(const uint8_t* stage, int lane, uint32_t (&w)[2 * BYTES]) {
-    constexpr int kHalf = BYTES;               // words of four elements
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(stage + F::element(lane, h) * BYTES);
-        if constexpr (kHalf == 4) {
-            const uint4 q = *reinterpret_cast<const uint4*>(p);
-            w[h * 4] = q.x; w[h * 4 + 1] = q.y; w[h * 4 + 2] = q.z; w[h * 4 + 3] = q.w;
-        } else if constexpr (kHalf == 2) {
-            const uint2 q = *reinterpret_cast<const uint2*>(p);
-            w[h * 2] = q.x; w[h * 2 + 1] = q.y;
-        } else {
-            w[h] = *p;
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(group + F::element(lane, h) * BYTES);
+            if constexpr (BYTES == 4) {
+                const uint4 q = *reinterpret_cast<const uint4*>(p);
+                w[h * 4] = q.x; w[h * 4 + 1] = q.y; w[h * 4 + 2] = q.z; w[h * 4 + 3] = q.w;
+            } else if constexpr (BYTES == 2) {
+                const uint2 q = *reinterpret_cast<const uint2*>(p);
+                w[h * 2] = q.x; w[h * 2 + 1] = q.y;
+            } else {
+                w[h] = *p;
+            }
         }
     }
 }
 template <typename F, uint32_t BYTES>
-__device__ __forceinline__ void store_array(void* to, int lane, const uint32_t (&w)[2 * BYTES]) {
-    char* p = static_cast<char*>(to);
+__device__ __forceinline__ void put_array(uint8_t* group, int lane, const uint32_t (&w)[2 * BYTES]) {
     if constexpr (!F::kHalves && BYTES == 2) {
-        __stcs(reinterpret_cast<uint4*>(p + lane * 16), make_uint4(w[0], w[1], w[2], w[3]));
+        *reinterpret_cast<uint4*>(group + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
     } else if constexpr (!F::kHalves && BYTES == 1) {
-        __stcs(reinterpret_cast<uint2*>(p + lane * 8), make_uint2(w[0], w[1]));
+        *reinterpret_cast<uint2*>(group + lane * 8) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            char* q = p + F::element(lane, h) * BYTES;
-            if constexpr (BYTES == 4) __stcs(reinterpret_cast<uint4*>(q), make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
-            if constexpr (BYTES == 2) __stcs(reinterpret_cast<uint2*>(q), make_uint2(w[2 * h], w[2 * h + 1]));
-            if constexpr (BYTES == 1) __stcs(reinterpret_cast<uint32_t*>(q), w[h]);
+            uint8_t* p = group + F::element(lane, h) * BYTES;
+            if constexpr (BYTES == 4) *reinterpret_cast<uint4*>(p) = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
+            if constexpr (BYTES == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[2 * h], w[2 * h + 1]);
+            if constexpr (BYTES == 1) *reinterpret_cast<uint32_t*>(p) = w[h];
         }
     }
 }
@@ -293,89 +322,99 @@ __device__ __forceinline__ void words_to_floats(const uint32_t (&w)[8], uint64_t
     for (int p = 0; p < 4; ++p) f[p] = ops::pair_of(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
 }
 
+// A lane's part of group `g` of a tile
 template <int STATE, int REST>
-__device__ __forceinline__ void send_group(const AdamRec& t, uint64_t group, uint32_t stage, int lane) {
+__device__ __forceinline__ void fetch_group(uint8_t* stage, const AdamTile& tile, uint32_t g, Octet& o, int lane) {
     using F = Form<STATE, REST>;
-    const uint64_t at = group * kGroup;
-    send_array<F, 2>(stage + F::kG, t.grad + at, lane);
-    if constexpr (F::kTheta) send_array<F, 2>(stage + F::kT, t.theta + at, lane);
-    if constexpr (F::kRestBytes) send_array<F, F::kRestBytes>(stage + F::kR, static_cast<const char*>(t.rest) + at * F::kRestBytes, lane);
-    send_array<F, F::kStateBytes>(stage + F::kM, static_cast<const char*>(t.m) + at * F::kStateBytes, lane);
-    send_array<F, F::kStateBytes>(stage + F::kV, static_cast<const char*>(t.v) + at * F::kStateBytes, lane);
-    if (STATE == COLLAGE_STATE_E4M3 && lane < 2) copy_async<4>(stage + F::kScales + 4 * lane, (lane ? t.v_scale : t.m_scale) + group);
-}
-
-// One group of a tensor by a warp: whole and aligned, its bytes in shared memory.
-template <int STATE, int REST>
-__device__ __forceinline__ void whole_group(const AdamRec& t, uint64_t group, const uint8_t* stage, const AdamScalars& k, float grad_scale, int lane) {
-    using F = Form<STATE, REST>;
-    const uint64_t at = group * kGroup;
-    Octet o;
+    auto of = [&](uint32_t array, uint32_t bytes) { return stage + array + g * (kGroup * bytes); };
     uint32_t w[4];
-    fetch_array<F, 2>(stage + F::kG, lane, w);
+    fetch_array<F, 2>(of(F::kG, 2), lane, w);
 #pragma unroll
     for (int p = 0; p < 4; ++p) o.g[p] = bf16_pair(w[p]);
-    if constexpr (F::kTheta) {
-        fetch_array<F, 2>(stage + F::kT, lane, w);
+    if constexpr (F::kReadsTheta) {
+        fetch_array<F, 2>(of(F::kT, 2), lane, w);
 #pragma unroll
         for (int p = 0; p < 4; ++p) o.theta[p] = bf16_pair(w[p]);
     }
     if constexpr (REST == COLLAGE_REST_BF16) {
-        fetch_array<F, 2>(stage + F::kR, lane, w);
+        fetch_array<F, 2>(of(F::kR, 2), lane, w);
 #pragma unroll
         for (int p = 0; p < 4; ++p) o.rest[p] = bf16_pair(w[p]);
     }
     uint32_t wide[8];
     if constexpr (REST == COLLAGE_REST_F32) {
-        fetch_array<F, 4>(stage + F::kR, lane, wide);
+        fetch_array<F, 4>(of(F::kR, 4), lane, wide);
         words_to_floats(wide, o.rest);
     }
     if constexpr (STATE == COLLAGE_STATE_F32) {
-        fetch_array<F, 4>(stage + F::kM, lane, wide);
+        fetch_array<F, 4>(of(F::kM, 4), lane, wide);
         words_to_floats(wide, o.m);
-        fetch_array<F, 4>(stage + F::kV, lane, wide);
+        fetch_array<F, 4>(of(F::kV, 4), lane, wide);
         words_to_floats(wide, o.v);
     } else {
-        const float2 scales = *reinterpret_cast<const float2*>(stage + F::kScales);
         uint32_t c[2];
-        fetch_array<F, 1>(stage + F::kM, lane, c);
+        fetch_array<F, 1>(of(F::kM, 1), lane, c);
 #pragma unroll
-        for (int p = 0; p < 4; ++p) o.m[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(scales.x));
-        fetch_array<F, 1>(stage + F::kV, lane, c);
+        for (int p = 0; p < 4; ++p) o.m[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(tile.scales[g]));
+        fetch_array<F, 1>(of(F::kV, 1), lane, c);
 #pragma unroll
-        for (int p = 0; p < 4; ++p) o.v[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(scales.y));
+        for (int p = 0; p < 4; ++p) o.v[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(tile.scales[kTileGroups + g]));
     }
-    update<STATE, REST>(o, k, grad_scale);
-    store_array<F, 2>(t.theta + at, lane, o.theta_out);
-    if constexpr (REST == COLLAGE_REST_BF16) store_array<F, 2>(static_cast<uint16_t*>(t.rest) + at, lane, o.rest_out);
+}
+
+// Parameters of a group that has a tie among its sums, once more and with care.
+template <int STATE, int REST, bool INSIDE>
+__device__ __noinline__ void pairs_with_ties(uint8_t* stage, const AdamTile& tile, uint32_t g, const AdamScalars& k, float grad_scale) {
+    using F = Form<STATE, REST>;
+    const int lane = threadIdx.x & 31;
+    Octet o;
+    fetch_group<STATE, REST>(stage, tile, g, o, lane);
+    update<STATE, REST, INSIDE, true>(o, k, grad_scale);
+    put_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, o.theta_out);
+    put_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, o.rest_out);
+}
+
+// A whole group by a warp, in place in the stage.
+template <int STATE, int REST, bool INSIDE>
+__device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile& tile, uint32_t g, const AdamScalars& k, float grad_scale, int lane) {
+    using F = Form<STATE, REST>;
+    auto of = [&](uint32_t array, uint32_t bytes) { return stage + array + g * (kGroup * bytes); };
+    Octet o;
+    fetch_group<STATE, REST>(stage, tile, g, o, lane);
+    uint32_t wide[8];
+    const uint32_t low = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
+    if (REST == COLLAGE_REST_BF16 && __any_sync(0xFFFFFFFFu, has_tie(low))) {
+        pairs_with_ties<STATE, REST, INSIDE>(stage, tile, g, k, grad_scale);
+    } else {
+        put_array<F, 2>(of(F::kT, 2), lane, o.theta_out);
+        if constexpr (REST == COLLAGE_REST_BF16) put_array<F, 2>(of(F::kR, 2), lane, o.rest_out);
+    }
     if constexpr (REST == COLLAGE_REST_F32) {
         floats_to_words(o.rest, wide);
-        store_array<F, 4>(static_cast<float*>(t.rest) + at, lane, wide);
+        put_array<F, 4>(of(F::kR, 4), lane, wide);
     }
     if constexpr (STATE == COLLAGE_STATE_F32) {
         floats_to_words(o.m, wide);
-        store_array<F, 4>(static_cast<float*>(t.m) + at, lane, wide);
+        put_array<F, 4>(of(F::kM, 4), lane, wide);
         floats_to_words(o.v, wide);
-        store_array<F, 4>(static_cast<float*>(t.v) + at, lane, wide);
+        put_array<F, 4>(of(F::kV, 4), lane, wide);
     } else {
         float m_factor, v_factor;
         const float m_scale = group_scale(largest(o.m), m_factor), v_scale = group_scale(largest(o.v), v_factor);
-        // the group's pairs begin at a multiple of 128, so their upper word is one
-        const uint64_t pair = (t.first + at) >> 1;
-        const uint32_t base = static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + k.key);
+        const uint32_t base = tile.random + g * (kGroup / 2);
         uint32_t random[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) random[p] = mix32(base + F::element(lane, p / 2) / 2 + (p & 1));
         const uint2 cm = nearest_codes(o.m, m_factor), cv = random_codes(o.v, v_factor, random);
         const uint32_t wm[2] = {cm.x, cm.y}, wv[2] = {cv.x, cv.y};
-        store_array<F, 1>(static_cast<uint8_t*>(t.m) + at, lane, wm);
-        store_array<F, 1>(static_cast<uint8_t*>(t.v) + at, lane, wv);
-        if (lane < 2) (lane ? t.v_scale : t.m_scale)[group] = lane ? v_scale : m_scale;
+        put_array<F, 1>(of(F::kM, 1), lane, wm);
+        put_array<F, 1>(of(F::kV, 1), lane, wv);
+        if (lane < 2) tile.scales[lane * kTileGroups + g] = lane ? v_scale : m_scale;
     }
 }
 
 // The same for groups that are cut short or not aligned: every 32nd element a lane.  Elements behind the end count as zeros.
-template <int STATE, int REST>
+template <int STATE, int REST, bool INSIDE>
 __device__ __noinline__ void any_group(const AdamRec& t, uint64_t group, const AdamScalars& k, float grad_scale) {
     const int lane = threadIdx.x & 31;
     const uint64_t begin = group * kGroup + lane;
@@ -401,7 +440,7 @@ __device__ __noinline__ void any_group(const AdamRec& t, uint64_t group, const A
         gather(o.m, [&](uint64_t i) { return code(t.m, i) * m_scale; });
         gather(o.v, [&](uint64_t i) { return code(t.v, i) * v_scale; });
     }
-    update<STATE, REST>(o, k, grad_scale);
+    update<STATE, REST, INSIDE, true>(o, k, grad_scale);
     auto scatter = [&](auto&& put) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -444,84 +483,129 @@ __device__ __noinline__ void any_group(const AdamRec& t, uint64_t group, const A
     }
 }
 
-// A warp's way through the groups of its tasks.
-struct Walk {
-    uint64_t task;
-    AdamChunk now;
-    uint32_t g, groups;
-    __device__ __forceinline__ void begin(const AdamArgs& a) {
-        if (task >= a.num_tasks) return;
-        now = a.tasks[task];
-        const uint64_t all = (a.tensors[now.tensor].n + kGroup - 1) / kGroup, first = static_cast<uint64_t>(now.index) * a.task_groups;
-        groups = static_cast<uint32_t>(min(static_cast<uint64_t>(a.task_groups), all - first));
-        g = 0;
-    }
-    __device__ __forceinline__ void next(const AdamArgs& a, uint64_t stride) {
-        if (++g < groups) return;
-        task += stride;
-        begin(a);
-    }
-    __device__ __forceinline__ uint64_t group(const AdamArgs& a) const { return static_cast<uint64_t>(now.index) * a.task_groups + g; }
-};
+// Fault word of this file's waits; collage_pipeline_fault reports it.
+static __device__ unsigned int g_adam_fault = 0;
 
-// Every warp by itself: it sends for the arrays of groups ahead of the one that it works on, each lane for its own bytes.
-template <int STATE, int REST>
-__global__ void __launch_bounds__(kAdamThreads, 3) adam_step_kernel(const __grid_constant__ AdamArgs a) {
+// Blocks walk over tiles of 4096 elements.  A warp brings each tile's whole groups into shared memory by bulk copies, several tiles
+// ahead, and stores them when the others have worked them over in place, a group at a time each; a last group that is cut short, and
+// tensors that no bulk copy can take, go straight from and to memory.
+template <int STATE, int REST, bool INSIDE>
+__global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_step_kernel(const __grid_constant__ AdamArgs a) {
     using F = Form<STATE, REST>;
-    extern __shared__ __align__(16) uint8_t dynamic[];
-    after_previous();
-    const int lane = threadIdx.x & 31;
-    uint8_t* stages = dynamic + (threadIdx.x >> 5) * (F::kStages * F::kStage);
-    const uint32_t stages_at = static_cast<uint32_t>(__cvta_generic_to_shared(stages));
-    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kAdamWarps;
-    const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
-    Walk ahead;
-    ahead.task = static_cast<uint64_t>(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
-    ahead.begin(a);
-    Walk here = ahead;
-    auto is_whole = [](const AdamRec& t, uint64_t group) { return t.aligned && (group + 1) * kGroup <= t.n; };
-    auto send = [&](int stage) {
-        if (ahead.task < a.num_tasks) {
-            const AdamRec& t = a.tensors[ahead.now.tensor];
-            const uint64_t group = ahead.group(a);
-            if (is_whole(t, group)) send_group<STATE, REST>(t, group, stages_at + stage * F::kStage, lane);
-            ahead.next(a, stride);
+    constexpr int kStages = F::kStages, kWarps = F::kWarps;
+    extern __shared__ __align__(128) uint8_t dynamic[];
+    AdamSmem<STATE, REST>& sm = *reinterpret_cast<AdamSmem<STATE, REST>*>(dynamic);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            pipe::mbar_init(&sm.full[s], 1 + (STATE == COLLAGE_STATE_E4M3 ? 32 : 0));
+            pipe::mbar_init(&sm.done[s], kTileGroups);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    for (int s = 0; s < F::kStages; ++s) send(s);
-    for (int stage = 0; here.task < a.num_tasks; here.next(a, stride)) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 1) : "memory");
+        pipe::mbar_init_fence();
+    }
+    __syncthreads();
+    after_previous();
+    if (warp == kWarps) {                      // the copies
+        uint32_t it = 0;
+        bool alive = true;
+        const uint32_t g = lane % kTileGroups;
+        auto store_out = [&](int s) {
+            const AdamTile& tile = sm.tile[s];
+            if (!tile.whole) return;
+            const AdamRec& t = *tile.tensor;
+            if (STATE == COLLAGE_STATE_E4M3 && g < tile.whole) (lane < kTileGroups ? t.m_scale : t.v_scale)[tile.first_group + g] = tile.scales[lane];
+            if (lane) return;
+            const uint64_t at = tile.first_group * kGroup;
+            const uint32_t n = tile.whole * kGroup;
+            pipe::bulk_store(t.theta + at, sm.bytes[s] + F::kT, 2 * n);
+            if (F::kRestBytes) pipe::bulk_store(static_cast<char*>(t.rest) + at * F::kRestBytes, sm.bytes[s] + F::kR, F::kRestBytes * n);
+            pipe::bulk_store(static_cast<char*>(t.m) + at * F::kStateBytes, sm.bytes[s] + F::kM, F::kStateBytes * n);
+            pipe::bulk_store(static_cast<char*>(t.v) + at * F::kStateBytes, sm.bytes[s] + F::kV, F::kStateBytes * n);
+            pipe::bulk_commit();
+        };
+        AdamChunk next = blockIdx.x < a.num_chunks ? a.chunks[blockIdx.x] : AdamChunk{0, 0};
+        for (uint64_t c = blockIdx.x; c < a.num_chunks; c += gridDim.x, ++it) {
+            const int s = it % kStages;
+            const AdamChunk chunk = next;
+            if (c + gridDim.x < a.num_chunks) next = a.chunks[c + gridDim.x];
+            const AdamRec& t = a.tensors[chunk.tensor];
+            const uint64_t first_group = static_cast<uint64_t>(chunk.index) * kTileGroups, left = t.n - first_group * kGroup;
+            const uint32_t groups = static_cast<uint32_t>(min((left + kGroup - 1) / kGroup, static_cast<uint64_t>(kTileGroups)));
+            const uint32_t whole = t.aligned ? static_cast<uint32_t>(min(left / kGroup, static_cast<uint64_t>(kTileGroups))) : 0;
+            if (it >= kStages) {
+                alive = __all_sync(0xFFFFFFFFu, pipe::mbar_wait(&sm.done[s], (it / kStages - 1) & 1u, 300u + s, &g_adam_fault));
+                if (!alive) break;
+                store_out(s);
+                if (lane == 0) pipe::bulk_wait_read_all();
+                __syncwarp();
+            }
+            const uint64_t at = first_group * kGroup;
+            const uint32_t n = whole * kGroup;
+            if (STATE == COLLAGE_STATE_E4M3) {
+                if (g < whole)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pipe::smem_addr(&sm.tile[s].scales[lane])), "l"((lane < kTileGroups ? t.m_scale : t.v_scale) + first_group + g)
+                                 : "memory");
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(pipe::smem_addr(&sm.full[s])) : "memory");
+            }
+            if (lane == 0) {
+                sm.tile[s].tensor = &t;
+                sm.tile[s].first_group = first_group;
+                sm.tile[s].groups = groups;
+                sm.tile[s].whole = whole;
+                // (a tile's pairs begin at a multiple of 128 and are 2048: their lower words may pass 2^32 only at one's beginning)
+                const uint64_t pair = (t.first + at) >> 1;
+                sm.tile[s].random = static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + a.k.key);
+                pipe::mbar_arrive_expect_tx(&sm.full[s], n * (2 + (F::kReadsTheta ? 2 : 0) + F::kRestBytes + 2 * F::kStateBytes));
+                if (n) {
+                    pipe::bulk_load(sm.bytes[s] + F::kG, t.grad + at, 2 * n, &sm.full[s]);
+                    if (F::kReadsTheta) pipe::bulk_load(sm.bytes[s] + F::kT, t.theta + at, 2 * n, &sm.full[s]);
+                    if (F::kRestBytes) pipe::bulk_load(sm.bytes[s] + F::kR, static_cast<const char*>(t.rest) + at * F::kRestBytes, F::kRestBytes * n, &sm.full[s]);
+                    pipe::bulk_load(sm.bytes[s] + F::kM, static_cast<const char*>(t.m) + at * F::kStateBytes, F::kStateBytes * n, &sm.full[s]);
+                    pipe::bulk_load(sm.bytes[s] + F::kV, static_cast<const char*>(t.v) + at * F::kStateBytes, F::kStateBytes * n, &sm.full[s]);
+                }
+            }
+        }
+        for (uint32_t j = it > kStages ? it - kStages : 0; j < it && alive; ++j) {
+            const int s = j % kStages;
+            alive = __all_sync(0xFFFFFFFFu, pipe::mbar_wait(&sm.done[s], (j / kStages) & 1u, 310u + s, &g_adam_fault));
+            if (alive) store_out(s);
+        }
+        // after a wait that was given up: the copies that are still under way
+        for (uint32_t j = it > kStages ? it - kStages : 0; j < it && !alive; ++j)
+            pipe::mbar_wait(&sm.full[j % kStages], (j / kStages) & 1u, 320u + j % kStages, &g_adam_fault);
+        if (lane == 0) pipe::bulk_wait_all();
+        return;
+    }
+    const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
+    // (below 2^32 chunks)
+    const uint32_t tiles = static_cast<uint32_t>((a.num_chunks - blockIdx.x + gridDim.x - 1) / gridDim.x);
+    uint32_t it = warp / kTileGroups, g = warp % kTileGroups, s = it % kStages, phase = it / kStages & 1;
+    while (it < tiles) {
+        if (!__all_sync(0xFFFFFFFFu, pipe::mbar_wait(&sm.full[s], phase, 330u + s, &g_adam_fault))) return;
+        AdamTile& tile = sm.tile[s];
+        if (g < tile.whole) {
+            whole_group<STATE, REST, INSIDE>(sm.bytes[s], tile, g, a.k, grad_scale, lane);
+            pipe::fence_async_smem();
+        } else if (g < tile.groups) {
+            any_group<STATE, REST, INSIDE>(*tile.tensor, tile.first_group + g, a.k, grad_scale);
+        }
         __syncwarp();
-        const AdamRec& t = a.tensors[here.now.tensor];
-        const uint64_t group = here.group(a);
-        if (is_whole(t, group))
-            whole_group<STATE, REST>(t, group, stages + stage * F::kStage, a.k, grad_scale, lane);
-        else
-            any_group<STATE, REST>(t, group, a.k, grad_scale);
-        __syncwarp();
-        send(stage);
-        stage = stage + 1 == F::kStages ? 0 : stage + 1;
+        if (lane == 0) pipe::mbar_arrive(&sm.done[s]);
+        for (g += kWarps; g >= kTileGroups; g -= kTileGroups) {
+            ++it;
+            if (++s == kStages) { s = 0; phase ^= 1; }
+        }
     }
 }
 
 template <int STATE, int REST>
 static collage_status_t launch_adam(const AdamArgs& a, int sm_count, cudaStream_t s) {
-    using F = Form<STATE, REST>;
-    constexpr size_t smem = static_cast<size_t>(kAdamWarps) * F::kStages * F::kStage;
-    static std::atomic<int> per_device[64];
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return COLLAGE_ERR_CUDA;
-    int resident = per_device[device].load(std::memory_order_acquire);
-    if (resident == 0) {
-        if (allow_smem<&adam_step_kernel<STATE, REST>>() != cudaSuccess ||
-            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, &adam_step_kernel<STATE, REST>, kAdamThreads, smem) != cudaSuccess)
-            return COLLAGE_ERR_CUDA;
-        resident = std::max(resident, 1);
-        per_device[device].store(resident, std::memory_order_release);
-    }
-    const uint64_t grid = std::min<uint64_t>((a.num_tasks + kAdamWarps - 1) / kAdamWarps, static_cast<uint64_t>(resident) * sm_count);
-    return launch<&adam_step_kernel<STATE, REST>>(grid, kAdamThreads, 1, smem, s, a);
+    const uint64_t grid = std::min<uint64_t>(a.num_chunks, sm_count);
+    constexpr int threads = Form<STATE, REST>::kWarps * 32 + 32;
+    if constexpr (STATE == COLLAGE_STATE_E4M3)           // (float states look at the flag themselves)
+        if (a.k.f.flags & COLLAGE_FLAG_EPS_INSIDE_SQRT)
+            return launch<&adam_step_kernel<STATE, REST, true>>(grid, threads, 1, sizeof(AdamSmem<STATE, REST>), s, a);
+    return launch<&adam_step_kernel<STATE, REST, false>>(grid, threads, 1, sizeof(AdamSmem<STATE, REST>), s, a);
 }
 
 // ---------------------------------------------------------------------------------------------------------- norm ---
@@ -553,26 +637,43 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
     __shared__ bool is_last;
     after_previous();
     double sum = 0.0;
-    for (uint64_t c = blockIdx.x; c < a.num_chunks; c += gridDim.x) {
+    struct Part {                              // of a chunk: what is left of the tensor from its beginning on
+        const uint16_t* grad;
+        uint64_t left;
+        bool aligned;
+    };
+    auto part_of = [&](uint64_t c) {
+        if (c >= a.num_chunks) return Part{nullptr, 0, false};
         const AdamChunk chunk = a.chunks[c];
         const AdamRec& t = a.tensors[chunk.tensor];
         const uint64_t begin = chunk.index * static_cast<uint64_t>(kAdamChunk);
+        return Part{t.grad + begin, t.n - begin, t.aligned != 0};
+    };
+    Part now = part_of(blockIdx.x);
+    for (uint64_t c = blockIdx.x; c < a.num_chunks; c += gridDim.x) {
         float g[2][8];
-        if (t.aligned && begin + kAdamChunk <= t.n) {
-            const uint4* q = reinterpret_cast<const uint4*>(t.grad + begin) + threadIdx.x;
+        uint4 q[2];
+        const bool whole = now.aligned && now.left >= kAdamChunk;
+        if (whole) {
+            q[0] = __ldcs(reinterpret_cast<const uint4*>(now.grad) + threadIdx.x);
+            q[1] = __ldcs(reinterpret_cast<const uint4*>(now.grad) + threadIdx.x + kAdamThreads);
+        }
+        const Part next = part_of(c + gridDim.x);        // (looked up while the values are under way)
+        if (whole) {
             unpack8(q[0], g[0]);
-            unpack8(q[kAdamThreads], g[1]);
+            unpack8(q[1], g[1]);
         } else {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const uint64_t j = begin + (i * 8 + e) * kAdamThreads + threadIdx.x;
-                    g[i][e] = j < t.n ? bf16_value(t.grad[j]) : 0.0f;
+                    const uint32_t j = (i * 8 + e) * kAdamThreads + threadIdx.x;
+                    g[i][e] = j < now.left ? bf16_value(now.grad[j]) : 0.0f;
                 }
         }
         sum += squares(g[0]);
         sum += squares(g[1]);
+        now = next;
     }
     auto joined = [&](double v) {              // over the block, in a fixed order; the result in the first warp
 #pragma unroll
@@ -616,15 +717,13 @@ using namespace collage::ops;
 
 struct collage_adam_plan {
     AdamRec* d_tensors = nullptr;
-    AdamChunk *d_chunks = nullptr, *d_tasks = nullptr;
-    uint64_t num_chunks = 0, num_tasks = 0;
-    uint32_t task_groups = 1;
+    AdamChunk* d_chunks = nullptr;
+    uint64_t num_chunks = 0;
     std::vector<ByteRange> ranges, written;    // sorted by address: all arrays, and those that a step writes
     int state = 0, rest = 0, device = -1;
     ~collage_adam_plan() {
         cudaFree(d_tensors);
         cudaFree(d_chunks);
-        cudaFree(d_tasks);
     }
 };
 
@@ -634,7 +733,7 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     const uint64_t state_bytes = state == COLLAGE_STATE_F32 ? 4 : 1, rest_bytes = rest == COLLAGE_REST_F32 ? 4 : 2;
     std::vector<ByteRange> ranges, written;
     std::vector<AdamRec> recs;
-    std::vector<AdamChunk> chunks, tasks;
+    std::vector<AdamChunk> chunks;
     uint64_t first = 0, num_chunks = 0;
     for (int i = 0; i < num; ++i) {
         const collage_adam_tensor_t& t = tensors[i];
@@ -670,7 +769,7 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
         r.grad = static_cast<const uint16_t*>(t.grad);
         r.n = t.n;
         r.first = first;
-        r.aligned = !off(t.theta, 16) && !off(t.grad, 16) && !off(t.rest, 16) && !off(t.m, codes ? 8 : 16) && !off(t.v, codes ? 8 : 16);
+        r.aligned = !off(t.theta, 16) && !off(t.grad, 16) && !off(t.rest, 16) && !off(t.m, 16) && !off(t.v, 16);
         first += groups * kGroup;
         for (uint64_t c = 0; c < own_chunks; ++c) chunks.push_back({static_cast<uint32_t>(recs.size()), static_cast<uint32_t>(c)});
         recs.push_back(r);
@@ -679,17 +778,8 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     any_overlap(written);                      // (sorts)
     DeviceInfo dev;
     if (const collage_status_t st = current_device(&dev); st != COLLAGE_OK) return st;
-    // groups of a warp's turn: 16 where every warp of the device has several turns of that, fewer for small plans
-    uint32_t task_groups = 16;
-    while (task_groups > 1 && first / kGroup < static_cast<uint64_t>(task_groups) * 128 * dev.sm_count) task_groups /= 2;
-    for (size_t i = 0; i < recs.size(); ++i) {
-        const uint64_t own = ((recs[i].n + kGroup - 1) / kGroup + task_groups - 1) / task_groups;
-        for (uint64_t c = 0; c < own; ++c) tasks.push_back({static_cast<uint32_t>(i), static_cast<uint32_t>(c)});
-    }
     collage_adam_plan* plan = new collage_adam_plan;
     plan->num_chunks = num_chunks;
-    plan->num_tasks = tasks.size();
-    plan->task_groups = task_groups;
     plan->ranges = std::move(ranges);
     plan->written = std::move(written);
     plan->state = state;
@@ -697,8 +787,6 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     if (cudaGetDevice(&plan->device) != cudaSuccess ||
         (num_chunks && (cudaMalloc(&plan->d_tensors, recs.size() * sizeof(AdamRec)) != cudaSuccess ||
                         cudaMalloc(&plan->d_chunks, chunks.size() * sizeof(AdamChunk)) != cudaSuccess ||
-                        cudaMalloc(&plan->d_tasks, tasks.size() * sizeof(AdamChunk)) != cudaSuccess ||
-                        cudaMemcpy(plan->d_tasks, tasks.data(), tasks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_tensors, recs.data(), recs.size() * sizeof(AdamRec), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess))) {
         delete plan;
@@ -714,6 +802,15 @@ bool on_its_device(const collage_adam_plan* plan) {
 }
 
 }  // namespace
+
+namespace collage {
+cudaError_t read_clear_adam_fault(unsigned int* out) {
+    unsigned int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_adam_fault, sizeof *out);
+    if (e == cudaSuccess && *out) e = cudaMemcpyToSymbol(g_adam_fault, &zero, sizeof zero);
+    return e;
+}
+}  // namespace collage
 
 extern "C" {
 
@@ -748,13 +845,13 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     if (plan->num_chunks == 0) return COLLAGE_OK;
     AdamArgs a = {};
     a.tensors = plan->d_tensors;
-    a.tasks = plan->d_tasks;
-    a.num_tasks = plan->num_tasks;
-    a.task_groups = plan->task_groups;
+    a.chunks = plan->d_chunks;
+    a.num_chunks = plan->num_chunks;
     a.grad_scale = grad_scale;
     a.k.f = fp32_scalars(hyper, step);
     const double t = static_cast<double>(step), bc1 = 1.0 - std::pow(hyper->beta1, t), bc2 = 1.0 - std::pow(hyper->beta2, t);
-    a.k.inv_bc1 = static_cast<float>(1.0 / bc1);
+    a.k.rate = static_cast<float>(-hyper->lr / bc1);
+    a.k.decay = static_cast<float>(-hyper->lr * hyper->weight_decay);
     a.k.inv_bc2 = static_cast<float>(1.0 / bc2);
     a.k.inv_root_bc2 = static_cast<float>(1.0 / std::sqrt(bc2));
     uint32_t key = mix32(static_cast<uint32_t>(step >> 32));

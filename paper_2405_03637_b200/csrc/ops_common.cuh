@@ -170,16 +170,25 @@ __device__ __forceinline__ float2 floats_of(uint64_t v) {
     return r;
 }
 __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+#ifdef SCALAR_PAIRS
+    { const float2 x = floats_of(a), y = floats_of(b); const float2 z = floats_of(c); return pair_of(__fmaf_rn(x.x, y.x, z.x), __fmaf_rn(x.y, y.y, z.y)); }
+#endif
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+#ifdef SCALAR_PAIRS
+    { const float2 x = floats_of(a), y = floats_of(b);  return pair_of(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y)); }
+#endif
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+#ifdef SCALAR_PAIRS
+    { const float2 x = floats_of(a), y = floats_of(b);  return pair_of(__fmul_rn(x.x, y.x), __fmul_rn(x.y, y.y)); }
+#endif
     uint64_t r;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
