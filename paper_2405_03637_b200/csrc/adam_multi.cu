@@ -36,7 +36,8 @@ struct AdamChunk {
 struct AdamScalars {
     Fp32Scalars f;
     float rate, decay;                         // -a / bc1, -a lam
-    float inv_bc2, inv_root_bc2;               // 1 / bc2, 1 / sqrt(bc2)
+    float inv_bc1, inv_bc2, inv_root_bc2;      // 1 / bc1, 1 / bc2, 1 / sqrt(bc2)
+    double a, lam;
     uint32_t key;
 };
 
@@ -61,6 +62,11 @@ __device__ __forceinline__ uint64_t sub_pair(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+// A sum of two products, each rounded.  (The assembler makes a packed product and a packed sum of it one fma; not so of these.)
+__device__ __forceinline__ uint64_t add_rounded(uint64_t a, uint64_t b) {
+    const float2 f = floats_of(a), g = floats_of(b);
+    return ops::pair_of(__fadd_rn(f.x, g.x), __fadd_rn(f.y, g.y));
 }
 // times a constant of the call, plus another
 __device__ __forceinline__ uint64_t scaled_pair(uint64_t a, float c) {
@@ -97,31 +103,65 @@ __device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
     return ops::pair_of(f.x, f.y);
 }
 
-// (theta, rest) + delta: theta' is the bfloat16 nearest to theta + RN(rest + delta), rest' what that lacks.  A float half-way between two
-// bfloat16 values does not tell which one is nearer: that hangs on what the float has lost.  With TIES it is rounded to odd first, towards
-// the sum's own side; without, `low` takes the smallest of the sums' lower half-words (as signed numbers), which is -32768 if there is
-// such a float among them (one in 65536).
-template <bool TIES>
-__device__ __forceinline__ void add_to_pair(uint64_t theta, uint64_t rest, uint64_t delta, uint32_t& theta_word, uint32_t& rest_word, uint32_t& low) {
+// A step of two elements' states: m', sqrt(v') (or v' itself), and the update of parameters x.  Every product and sum of the states is
+// rounded once, so that their codes hang on nothing but the formulas; the quotient is within a few units of the last place.
+template <int STATE, bool INSIDE>
+__device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g, uint64_t x, const AdamScalars& k) {
+    const uint64_t squared = STATE == COLLAGE_STATE_F32 ? v : mul_pair(v, v);
+    m = add_rounded(scaled_pair(m, k.f.b1), scaled_pair(g, k.f.c1));
+    v = add_rounded(scaled_pair(squared, k.f.b2), scaled_pair(mul_pair(g, g), k.f.c2));
+    const uint64_t root = root_pair(v);
+    const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : scaled_plus(root, k.inv_root_bc2, k.f.eps);
+    if (STATE == COLLAGE_STATE_E4M3) v = root;
+    return scaled_plus(x, k.decay, scaled_pair(mul_pair(m, reciprocal_pair(den)), k.rate));
+}
+
+// (theta, rest) + delta: theta' is the bfloat16 nearest to the sum, rest' what that lacks.  In floats theta + RN(rest + delta) is known as s + lost, to a
+// few units of the last place of rest + delta.  Where s is that near to half-way between two bfloat16 values (`kNear` units of s) the
+// sum is taken in 64 bits instead (settled()).
+constexpr uint32_t kNear = 5;
+__device__ __forceinline__ bool is_near(float s) { return ((__float_as_uint(s) - 0x8000u + kNear) & 0xFFFFu) <= 2 * kNear; }
+struct PairSum {
+    uint64_t s, lost;
+};
+__device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, uint64_t delta) {
     const uint64_t t = add_pair(rest, delta), s = add_pair(theta, t), back = sub_pair(s, theta);
-    const uint64_t lost = add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back));                  // exact: theta + t = s + lost
-    float2 sum = floats_of(s);
-    if (TIES) {
-        const float2 l = floats_of(lost);
-        auto odd = [](float f, float rest_of) {
-            const uint32_t bits = __float_as_uint(f);
-            const bool off = rest_of != 0.0f && fabsf(rest_of) < INFINITY;
-            return __uint_as_float(off ? (bits - ((__float_as_uint(rest_of) ^ bits) >> 31)) | 1u : bits);
-        };
-        sum = make_float2(odd(sum.x, l.x), odd(sum.y, l.y));
-    } else {
-        low = __vmins2(low, __byte_perm(__float_as_uint(sum.x), __float_as_uint(sum.y), 0x5410));
-    }
-    theta_word = pack_bf16(sum.x, sum.y);
-    const float2 r = floats_of(add_pair(sub_pair(s, bf16_pair(theta_word)), lost));
+    return {s, add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back))};                  // theta + t = s + lost, exactly
+}
+__device__ __forceinline__ void split_pair(const PairSum& sum, uint32_t& theta_word, uint32_t& rest_word) {
+    const float2 s = floats_of(sum.s);
+    theta_word = pack_bf16(s.x, s.y);
+    const float2 r = floats_of(add_pair(sub_pair(sum.s, bf16_pair(theta_word)), sum.lost));
     rest_word = pack_bf16(r.x, r.y);
 }
-__device__ __forceinline__ bool has_tie(uint32_t low) { return (low & 0xFFFFu) == 0x8000u || low >> 16 == 0x8000u; }
+// The pair of x - a (q + lam x) with x = theta + rest, for the quotient q of m' and v' (or its root) as IEEE operations give it.
+template <int STATE, bool INSIDE>
+__device__ __forceinline__ uint32_t settled(float theta, float rest, float m, float v, const AdamScalars& k) {
+    const float root = STATE == COLLAGE_STATE_E4M3 ? v : __fsqrt_rn(v), square = STATE == COLLAGE_STATE_E4M3 ? v * v : v;
+    const float den = INSIDE ? __fsqrt_rn(__fmaf_rn(square, k.inv_bc2, k.f.eps)) : root * k.inv_root_bc2 + k.f.eps;
+    const double x = static_cast<double>(theta) + rest, to = x - k.a * (__fdiv_rn(m * k.inv_bc1, den) + k.lam * x);
+    // to bfloat16 by way of a float that is rounded to odd
+    float f = __double2float_rz(to);
+    if (static_cast<double>(f) != to && fabsf(f) < INFINITY) f = __uint_as_float(__float_as_uint(f) | 1u);
+    const uint32_t near = to_bf16(f);
+    return near | static_cast<uint32_t>(to_bf16(static_cast<float>(to - bf16_value(static_cast<uint16_t>(near))))) << 16;
+}
+// Both of two words, where their sums are near half-way.
+template <int STATE, bool INSIDE>
+__device__ __forceinline__ void settle(const PairSum& sum, uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, const AdamScalars& k, uint32_t& theta_word,
+                                       uint32_t& rest_word) {
+    const float2 s = floats_of(sum.s), th = floats_of(theta), re = floats_of(rest), mm = floats_of(m), vv = floats_of(v);
+    if (is_near(s.x)) {
+        const uint32_t both = settled<STATE, INSIDE>(th.x, re.x, mm.x, vv.x, k);
+        theta_word = __byte_perm(theta_word, both, 0x3254);
+        rest_word = __byte_perm(rest_word, both, 0x3276);
+    }
+    if (is_near(s.y)) {
+        const uint32_t both = settled<STATE, INSIDE>(th.y, re.y, mm.y, vv.y, k);
+        theta_word = __byte_perm(theta_word, both, 0x5410);
+        rest_word = __byte_perm(rest_word, both, 0x7610);
+    }
+}
 
 // Eight elements of a lane, in pairs, before and behind the update.  With states in 8 bits v is its root.
 struct Octet {
@@ -129,15 +169,27 @@ struct Octet {
     uint32_t theta_out[4], rest_out[4];                  // two bfloat16 each
 };
 
-template <int STATE, int REST, bool INSIDE, bool TIES>
+// SETTLE: sums near half-way are settled here and now; else the result tells whether there may be any: then a half-word of it is below 2 kNear + 2.
+template <int STATE, int REST, bool INSIDE, bool SETTLE>
 __device__ __forceinline__ uint32_t update(Octet& o, const AdamScalars& k, float grad_scale) {
-    uint32_t low = 0;
+    uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const uint64_t g = scaled_pair(o.g[p], grad_scale);
         const uint64_t x = REST == COLLAGE_REST_F32 ? o.rest[p] : REST == COLLAGE_REST_BF16 ? add_pair(o.theta[p], o.rest[p]) : o.theta[p];
+        if (REST == COLLAGE_REST_BF16) {
+            const PairSum sum = sum_of_pair(o.theta[p], o.rest[p], advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k));
+            split_pair(sum, o.theta_out[p], o.rest_out[p]);
+            if (SETTLE) {
+                settle<STATE, INSIDE>(sum, o.theta[p], o.rest[p], o.m[p], o.v[p], k, o.theta_out[p], o.rest_out[p]);
+            } else {                            // (the lower half-word's carry makes the upper one larger by one at most)
+                const float2 s = floats_of(sum.s);
+                least = __vminu2(least, __byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410) + (0x80008000u + kNear * 0x10001u));
+            }
+            continue;
+        }
         uint64_t delta;
-        if (STATE == COLLAGE_STATE_F32) {
+        if (STATE == COLLAGE_STATE_F32) {       // the flat step's operations
             float2 m = floats_of(o.m[p]), v = floats_of(o.v[p]);
             const float2 gf = floats_of(g), xf = floats_of(x);
             const float lo = adamw_fp32_delta(m.x, v.x, xf.x, gf.x, k.f), hi = adamw_fp32_delta(m.y, v.y, xf.y, gf.y, k.f);
@@ -145,25 +197,15 @@ __device__ __forceinline__ uint32_t update(Octet& o, const AdamScalars& k, float
             o.m[p] = ops::pair_of(m.x, m.y);
             o.v[p] = ops::pair_of(v.x, v.y);
         } else {
-            // every product and sum of the states is rounded once, so that their codes hang on nothing but the formulas
-            const uint64_t m = add_pair(scaled_pair(o.m[p], k.f.b1), scaled_pair(g, k.f.c1));
-            const uint64_t v = add_pair(scaled_pair(mul_pair(o.v[p], o.v[p]), k.f.b2), scaled_pair(mul_pair(g, g), k.f.c2));
-            const uint64_t root = root_pair(v);
-            const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : scaled_plus(root, k.inv_root_bc2, k.f.eps);
-            delta = scaled_plus(x, k.decay, scaled_pair(mul_pair(m, reciprocal_pair(den)), k.rate));
-            o.m[p] = m;
-            o.v[p] = root;
+            delta = advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k);
         }
-        if (REST == COLLAGE_REST_BF16) {
-            add_to_pair<TIES>(o.theta[p], o.rest[p], delta, o.theta_out[p], o.rest_out[p], low);
-        } else {
-            o.rest[p] = add_pair(x, delta);
-            const float2 to = floats_of(o.rest[p]);
-            o.theta_out[p] = pack_bf16(to.x, to.y);
-        }
+        o.rest[p] = add_pair(x, delta);
+        const float2 to = floats_of(o.rest[p]);
+        o.theta_out[p] = pack_bf16(to.x, to.y);
     }
-    return low;
+    return least;
 }
+__device__ __forceinline__ bool any_near(uint32_t least) { return (least & 0xFFFFu) <= 2 * kNear + 1 || least >> 16 <= 2 * kNear + 1; }
 
 // Largest absolute value of eight over the warp; NaN where there is one.
 __device__ __forceinline__ uint32_t largest(const uint64_t (&f)[4]) {
@@ -362,16 +404,25 @@ __device__ __forceinline__ void fetch_group(uint8_t* stage, const AdamTile& tile
     }
 }
 
-// Parameters of a group that has a tie among its sums, once more and with care.
-template <int STATE, int REST, bool INSIDE>
-__device__ __noinline__ void pairs_with_ties(uint8_t* stage, const AdamTile& tile, uint32_t g, const AdamScalars& k, float grad_scale) {
-    using F = Form<STATE, REST>;
+// Parameters of a group that may have sums near half-way, once more from its old values; those sums are settled in the stage.
+template <int STATE, bool INSIDE>
+__device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile& tile, uint32_t g, const AdamScalars& k, float grad_scale, uint4 old_theta, uint4 old_rest) {
+    using F = Form<STATE, COLLAGE_REST_BF16>;
     const int lane = threadIdx.x & 31;
     Octet o;
-    fetch_group<STATE, REST>(stage, tile, g, o, lane);
-    update<STATE, REST, INSIDE, true>(o, k, grad_scale);
-    put_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, o.theta_out);
-    put_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, o.rest_out);
+    fetch_group<STATE, COLLAGE_REST_BF16>(stage, tile, g, o, lane);
+    const uint32_t th[4] = {old_theta.x, old_theta.y, old_theta.z, old_theta.w}, re[4] = {old_rest.x, old_rest.y, old_rest.z, old_rest.w};
+    uint32_t theta_out[4], rest_out[4];
+    fetch_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, theta_out);
+    fetch_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, rest_out);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint64_t theta = bf16_pair(th[p]), rest = bf16_pair(re[p]);
+        const uint64_t delta = advance<STATE, INSIDE>(o.m[p], o.v[p], scaled_pair(o.g[p], grad_scale), add_pair(theta, rest), k);
+        settle<STATE, INSIDE>(sum_of_pair(theta, rest, delta), theta, rest, o.m[p], o.v[p], k, theta_out[p], rest_out[p]);
+    }
+    put_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, theta_out);
+    put_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, rest_out);
 }
 
 // A whole group by a warp, in place in the stage.
@@ -382,12 +433,20 @@ __device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile& tile, uint
     Octet o;
     fetch_group<STATE, REST>(stage, tile, g, o, lane);
     uint32_t wide[8];
-    const uint32_t low = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
-    if (REST == COLLAGE_REST_BF16 && __any_sync(0xFFFFFFFFu, has_tie(low))) {
-        pairs_with_ties<STATE, REST, INSIDE>(stage, tile, g, k, grad_scale);
+    const uint32_t least = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
+    if constexpr (REST == COLLAGE_REST_BF16) {
+        uint32_t th[4], re[4];
+        const bool near = __any_sync(0xFFFFFFFFu, any_near(least));
+        if (near) {
+            fetch_array<F, 2>(of(F::kT, 2), lane, th);
+            fetch_array<F, 2>(of(F::kR, 2), lane, re);
+        }
+        put_array<F, 2>(of(F::kT, 2), lane, o.theta_out);
+        put_array<F, 2>(of(F::kR, 2), lane, o.rest_out);
+        if (near)
+            settle_group<STATE, INSIDE>(stage, tile, g, k, grad_scale, make_uint4(th[0], th[1], th[2], th[3]), make_uint4(re[0], re[1], re[2], re[3]));
     } else {
         put_array<F, 2>(of(F::kT, 2), lane, o.theta_out);
-        if constexpr (REST == COLLAGE_REST_BF16) put_array<F, 2>(of(F::kR, 2), lane, o.rest_out);
     }
     if constexpr (REST == COLLAGE_REST_F32) {
         floats_to_words(o.rest, wide);
@@ -602,7 +661,7 @@ template <int STATE, int REST>
 static collage_status_t launch_adam(const AdamArgs& a, int sm_count, cudaStream_t s) {
     const uint64_t grid = std::min<uint64_t>(a.num_chunks, sm_count);
     constexpr int threads = Form<STATE, REST>::kWarps * 32 + 32;
-    if constexpr (STATE == COLLAGE_STATE_E4M3)           // (float states look at the flag themselves)
+    if constexpr (STATE == COLLAGE_STATE_E4M3 || REST == COLLAGE_REST_BF16)          // (elsewhere the flat step's operations look at the flag)
         if (a.k.f.flags & COLLAGE_FLAG_EPS_INSIDE_SQRT)
             return launch<&adam_step_kernel<STATE, REST, true>>(grid, threads, 1, sizeof(AdamSmem<STATE, REST>), s, a);
     return launch<&adam_step_kernel<STATE, REST, false>>(grid, threads, 1, sizeof(AdamSmem<STATE, REST>), s, a);
@@ -850,6 +909,9 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     a.grad_scale = grad_scale;
     a.k.f = fp32_scalars(hyper, step);
     const double t = static_cast<double>(step), bc1 = 1.0 - std::pow(hyper->beta1, t), bc2 = 1.0 - std::pow(hyper->beta2, t);
+    a.k.a = hyper->lr;
+    a.k.lam = hyper->weight_decay;
+    a.k.inv_bc1 = static_cast<float>(1.0 / bc1);
     a.k.rate = static_cast<float>(-hyper->lr / bc1);
     a.k.decay = static_cast<float>(-hyper->lr * hyper->weight_decay);
     a.k.inv_bc2 = static_cast<float>(1.0 / bc2);
