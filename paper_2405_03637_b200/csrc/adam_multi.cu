@@ -18,7 +18,7 @@ namespace collage {
 namespace ops {
 
 constexpr uint32_t kGroup = 256;               // elements that share a scale: a warp's, eight a lane
-constexpr uint32_t kAdamChunk = 4096;          // elements of a block's turn
+constexpr uint32_t kNormChunk = 4096;          // elements of a block's turn in the norm
 constexpr int kAdamThreads = 256;
 
 struct AdamRec {
@@ -43,8 +43,8 @@ struct AdamScalars {
 
 struct AdamArgs {
     const AdamRec* tensors;
-    const AdamChunk* chunks;
-    uint64_t num_chunks;
+    const AdamChunk* tiles;
+    uint64_t num_tiles;
     const float* grad_scale;
     AdamScalars k;
 };
@@ -116,17 +116,25 @@ __device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g
     return scaled_plus(x, k.decay, scaled_pair(mul_pair(m, reciprocal_pair(den)), k.rate));
 }
 
-// (theta, rest) + delta: theta' is the bfloat16 nearest to the sum, rest' what that lacks.  In floats theta + RN(rest + delta) is known as s + lost, to a
-// few units of the last place of rest + delta.  Where s is that near to half-way between two bfloat16 values (`kNear` units of s) the
-// sum is taken in 64 bits instead (settled()).
-constexpr uint32_t kNear = 5;
-__device__ __forceinline__ bool is_near(float s) { return ((__float_as_uint(s) - 0x8000u + kNear) & 0xFFFFu) <= 2 * kNear; }
+// (theta, rest) + delta: theta' is the bfloat16 nearest to the sum, rest' what that lacks.  In floats theta + RN(rest + delta) is known as s + lost, to
+// five units of the last place of t = rest + delta.  Where s is that near to half-way between two bfloat16 values the sum is taken in 64 bits
+// instead (settled()): as a rule within a unit or two of s's own last place; within more (64 at most) where theta and t nearly cancel.
 struct PairSum {
-    uint64_t s, lost;
+    uint64_t s, t, lost;
 };
 __device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, uint64_t delta) {
     const uint64_t t = add_pair(rest, delta), s = add_pair(theta, t), back = sub_pair(s, theta);
-    return {s, add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back))};                  // theta + t = s + lost, exactly
+    return {s, t, add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back))};                  // theta + t = s + lost, exactly
+}
+__device__ __forceinline__ bool is_near(float s, float t) {
+    const int off = static_cast<int>(__float_as_uint(s) & 0xFFFFu) - 0x8000;
+    return abs(off) < 64 && abs(off) * fabsf(s) <= __fmaf_rn(5.0f, fabsf(t), 1.5f * fabsf(s));
+}
+__device__ __forceinline__ bool is_near(const PairSum& sum) {
+    const float2 s = floats_of(sum.s), t = floats_of(sum.t);
+    const uint32_t off = (__byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410) + 0x80408040u) & 0xFF80FF80u;
+    if (((off - 0x00010001u) & ~off & 0x80008000u) == 0) return false;           // no half-word within 64 (the lower one's carry allowed for)
+    return is_near(s.x, t.x) || is_near(s.y, t.y);
 }
 __device__ __forceinline__ void split_pair(const PairSum& sum, uint32_t& theta_word, uint32_t& rest_word) {
     const float2 s = floats_of(sum.s);
@@ -150,13 +158,13 @@ __device__ __forceinline__ uint32_t settled(float theta, float rest, float m, fl
 template <int STATE, bool INSIDE>
 __device__ __forceinline__ void settle(const PairSum& sum, uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, const AdamScalars& k, uint32_t& theta_word,
                                        uint32_t& rest_word) {
-    const float2 s = floats_of(sum.s), th = floats_of(theta), re = floats_of(rest), mm = floats_of(m), vv = floats_of(v);
-    if (is_near(s.x)) {
+    const float2 s = floats_of(sum.s), t = floats_of(sum.t), th = floats_of(theta), re = floats_of(rest), mm = floats_of(m), vv = floats_of(v);
+    if (is_near(s.x, t.x)) {
         const uint32_t both = settled<STATE, INSIDE>(th.x, re.x, mm.x, vv.x, k);
         theta_word = __byte_perm(theta_word, both, 0x3254);
         rest_word = __byte_perm(rest_word, both, 0x3276);
     }
-    if (is_near(s.y)) {
+    if (is_near(s.y, t.y)) {
         const uint32_t both = settled<STATE, INSIDE>(th.y, re.y, mm.y, vv.y, k);
         theta_word = __byte_perm(theta_word, both, 0x5410);
         rest_word = __byte_perm(rest_word, both, 0x7610);
@@ -169,10 +177,10 @@ struct Octet {
     uint32_t theta_out[4], rest_out[4];                  // two bfloat16 each
 };
 
-// SETTLE: sums near half-way are settled here and now; else the result tells whether there may be any: then a half-word of it is below 2 kNear + 2.
+// SETTLE: sums near half-way are settled here and now; else the result tells whether there are any.
 template <int STATE, int REST, bool INSIDE, bool SETTLE>
-__device__ __forceinline__ uint32_t update(Octet& o, const AdamScalars& k, float grad_scale) {
-    uint32_t least = 0xFFFFFFFFu;
+__device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float grad_scale) {
+    bool near = false;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const uint64_t g = scaled_pair(o.g[p], grad_scale);
@@ -180,12 +188,10 @@ __device__ __forceinline__ uint32_t update(Octet& o, const AdamScalars& k, float
         if (REST == COLLAGE_REST_BF16) {
             const PairSum sum = sum_of_pair(o.theta[p], o.rest[p], advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k));
             split_pair(sum, o.theta_out[p], o.rest_out[p]);
-            if (SETTLE) {
+            if (SETTLE)
                 settle<STATE, INSIDE>(sum, o.theta[p], o.rest[p], o.m[p], o.v[p], k, o.theta_out[p], o.rest_out[p]);
-            } else {                            // (the lower half-word's carry makes the upper one larger by one at most)
-                const float2 s = floats_of(sum.s);
-                least = __vminu2(least, __byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410) + (0x80008000u + kNear * 0x10001u));
-            }
+            else
+                near |= is_near(sum);
             continue;
         }
         uint64_t delta;
@@ -203,9 +209,8 @@ __device__ __forceinline__ uint32_t update(Octet& o, const AdamScalars& k, float
         const float2 to = floats_of(o.rest[p]);
         o.theta_out[p] = pack_bf16(to.x, to.y);
     }
-    return least;
+    return near;
 }
-__device__ __forceinline__ bool any_near(uint32_t least) { return (least & 0xFFFFu) <= 2 * kNear + 1 || least >> 16 <= 2 * kNear + 1; }
 
 // Largest absolute value of eight over the warp; NaN where there is one.
 __device__ __forceinline__ uint32_t largest(const uint64_t (&f)[4]) {
@@ -273,6 +278,11 @@ __device__ __forceinline__ uint32_t random_word(uint64_t pair, uint32_t key) {
     return mix32(static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + key));
 }
 
+// Groups of a tile, one for each warp beside the one that copies.  One more than a multiple of four, with that one, would cost all of them
+// registers: a quarter of an SM would have one warp more to share its own among.  134 M parameters in 8 bits with pairs take 356, 380 and 374
+// us by 15, 19 and 23 warps, with master weights 337, 360 and 333; 67 M in floats with pairs 282, 295 and 289, with master weights 307, 292 and 290.
+constexpr int tile_groups(int rest) { return rest == COLLAGE_REST_F32 ? 23 : 15; }
+
 // A stage of the copy pipeline: a tile's bytes of each array.  Of a whole group a lane has eight elements in a row, or, where some array
 // is of floats, four in a row of each half, so that a warp's accesses are to consecutive bytes.
 template <int STATE, int REST>
@@ -280,33 +290,28 @@ struct Form {
     static constexpr bool kHalves = STATE == COLLAGE_STATE_F32 || REST == COLLAGE_REST_F32;
     static constexpr bool kReadsTheta = REST != COLLAGE_REST_F32;
     static constexpr uint32_t kStateBytes = STATE == COLLAGE_STATE_F32 ? 4 : 1, kRestBytes = REST == COLLAGE_REST_F32 ? 4 : REST == COLLAGE_REST_BF16 ? 2 : 0;
+    static constexpr uint32_t kWarps = tile_groups(REST), kTile = kWarps * kGroup;
     // offsets of the arrays in a stage
-    static constexpr uint32_t kG = 0, kT = kG + 2 * kAdamChunk, kR = kT + 2 * kAdamChunk, kM = kR + kRestBytes * kAdamChunk, kV = kM + kStateBytes * kAdamChunk,
-                              kStage = kV + kStateBytes * kAdamChunk;
-    // As many stages as 200 KB hold (three to eight).  With 110 KB 134 M parameters take 345 us instead of 329 (8-bit states, pairs), 429 instead
-    // of 320 (8-bit states, master weights).
-    static constexpr int kStages = 200 * 1024 / kStage;
-    // Warps beside the one that copies.  One more than a multiple of four would cost all of them registers: a quarter of an SM would have
-    // one warp more to share its own among.  Of 15, 19, 23, 27 these measured best: 15 where there are master weights (67 M parameters, float
-    // states: 288 us, 19 take 305), 19 elsewhere (272 us with pairs, 15 take 288).
-    static constexpr int kWarps = REST == COLLAGE_REST_F32 ? 15 : 19;
+    static constexpr uint32_t kG = 0, kT = kG + 2 * kTile, kR = kT + 2 * kTile, kM = kR + kRestBytes * kTile, kV = kM + kStateBytes * kTile,
+                              kStage = kV + kStateBytes * kTile;
+    static constexpr uint32_t kStages = 208 * 1024 / kStage;          // three to seven
     static __device__ __forceinline__ uint32_t element(int lane, int half) { return kHalves ? half * (kGroup / 2) + lane * 4 : lane * 8 + half * 4; }
 };
-constexpr uint32_t kTileGroups = kAdamChunk / kGroup;
 
-// What consumers have to know of the tile in a stage.
+// What the other warps have to know of the tile in a stage.
+template <uint32_t GROUPS>
 struct AdamTile {
     const AdamRec* tensor;
     uint64_t first_group;                      // of the tensor
     uint32_t groups, whole;                    // in the tile; of these, in shared memory
-    uint32_t random;                           // what its pairs' numbers are added to before they are mixed
-    float scales[2 * kTileGroups];             // of m, then of the root
+    uint32_t random[2], passed;                // what pairs' numbers in the tile are added to before they are mixed; from group `passed` on the second
+    float scales[2 * GROUPS];                  // of m, then of the root
 };
 template <int STATE, int REST>
 struct AdamSmem {
     using F = Form<STATE, REST>;
     alignas(128) uint8_t bytes[F::kStages][F::kStage];
-    AdamTile tile[F::kStages];
+    AdamTile<F::kWarps> tile[F::kStages];
     alignas(8) uint64_t full[F::kStages], done[F::kStages];
 };
 
@@ -366,7 +371,7 @@ __device__ __forceinline__ void words_to_floats(const uint32_t (&w)[8], uint64_t
 
 // A lane's part of group `g` of a tile
 template <int STATE, int REST>
-__device__ __forceinline__ void fetch_group(uint8_t* stage, const AdamTile& tile, uint32_t g, Octet& o, int lane) {
+__device__ __forceinline__ void fetch_group(uint8_t* stage, const AdamTile<Form<STATE, REST>::kWarps>& tile, uint32_t g, Octet& o, int lane) {
     using F = Form<STATE, REST>;
     auto of = [&](uint32_t array, uint32_t bytes) { return stage + array + g * (kGroup * bytes); };
     uint32_t w[4];
@@ -400,13 +405,13 @@ __device__ __forceinline__ void fetch_group(uint8_t* stage, const AdamTile& tile
         for (int p = 0; p < 4; ++p) o.m[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(tile.scales[g]));
         fetch_array<F, 1>(of(F::kV, 1), lane, c);
 #pragma unroll
-        for (int p = 0; p < 4; ++p) o.v[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(tile.scales[kTileGroups + g]));
+        for (int p = 0; p < 4; ++p) o.v[p] = mul_pair(e4m3_pair(c[p / 2] >> (16 * (p & 1))), pair_of(tile.scales[F::kWarps + g]));
     }
 }
 
 // Parameters of a group that may have sums near half-way, once more from its old values; those sums are settled in the stage.
 template <int STATE, bool INSIDE>
-__device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile& tile, uint32_t g, const AdamScalars& k, float grad_scale, uint4 old_theta, uint4 old_rest) {
+__device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile<Form<STATE, COLLAGE_REST_BF16>::kWarps>& tile, uint32_t g, const AdamScalars& k, float grad_scale, uint4 old_theta, uint4 old_rest) {
     using F = Form<STATE, COLLAGE_REST_BF16>;
     const int lane = threadIdx.x & 31;
     Octet o;
@@ -427,16 +432,16 @@ __device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile& tile, 
 
 // A whole group by a warp, in place in the stage.
 template <int STATE, int REST, bool INSIDE>
-__device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile& tile, uint32_t g, const AdamScalars& k, float grad_scale, int lane) {
+__device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile<Form<STATE, REST>::kWarps>& tile, uint32_t g, const AdamScalars& k, float grad_scale, int lane) {
     using F = Form<STATE, REST>;
     auto of = [&](uint32_t array, uint32_t bytes) { return stage + array + g * (kGroup * bytes); };
     Octet o;
     fetch_group<STATE, REST>(stage, tile, g, o, lane);
     uint32_t wide[8];
-    const uint32_t least = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
+    const bool mine = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
     if constexpr (REST == COLLAGE_REST_BF16) {
         uint32_t th[4], re[4];
-        const bool near = __any_sync(0xFFFFFFFFu, any_near(least));
+        const bool near = __any_sync(0xFFFFFFFFu, mine);
         if (near) {
             fetch_array<F, 2>(of(F::kT, 2), lane, th);
             fetch_array<F, 2>(of(F::kR, 2), lane, re);
@@ -460,7 +465,7 @@ __device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile& tile, uint
     } else {
         float m_factor, v_factor;
         const float m_scale = group_scale(largest(o.m), m_factor), v_scale = group_scale(largest(o.v), v_factor);
-        const uint32_t base = tile.random + g * (kGroup / 2);
+        const uint32_t base = tile.random[g >= tile.passed] + g * (kGroup / 2);
         uint32_t random[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) random[p] = mix32(base + F::element(lane, p / 2) / 2 + (p & 1));
@@ -468,7 +473,7 @@ __device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile& tile, uint
         const uint32_t wm[2] = {cm.x, cm.y}, wv[2] = {cv.x, cv.y};
         put_array<F, 1>(of(F::kM, 1), lane, wm);
         put_array<F, 1>(of(F::kV, 1), lane, wv);
-        if (lane < 2) tile.scales[lane * kTileGroups + g] = lane ? v_scale : m_scale;
+        if (lane < 2) tile.scales[lane * F::kWarps + g] = lane ? v_scale : m_scale;
     }
 }
 
@@ -545,20 +550,21 @@ __device__ __noinline__ void any_group(const AdamRec& t, uint64_t group, const A
 // Fault word of this file's waits; collage_pipeline_fault reports it.
 static __device__ unsigned int g_adam_fault = 0;
 
-// Blocks walk over tiles of 4096 elements.  A warp brings each tile's whole groups into shared memory by bulk copies, several tiles
-// ahead, and stores them when the others have worked them over in place, a group at a time each; a last group that is cut short, and
-// tensors that no bulk copy can take, go straight from and to memory.
+// Blocks walk over tiles of as many groups as they have warps that work.  One warp more brings each tile's whole groups into shared memory by
+// bulk copies, several tiles ahead, and stores them when the others have worked them over in place, a group each; a last group that is
+// cut short, and tensors that no bulk copy can take, go straight from and to memory.
 template <int STATE, int REST, bool INSIDE>
 __global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_step_kernel(const __grid_constant__ AdamArgs a) {
     using F = Form<STATE, REST>;
-    constexpr int kStages = F::kStages, kWarps = F::kWarps;
+    constexpr uint32_t kStages = F::kStages, kWarps = F::kWarps;
     extern __shared__ __align__(128) uint8_t dynamic[];
     AdamSmem<STATE, REST>& sm = *reinterpret_cast<AdamSmem<STATE, REST>*>(dynamic);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const uint32_t warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (uint32_t s = 0; s < kStages; ++s) {
             pipe::mbar_init(&sm.full[s], 1 + (STATE == COLLAGE_STATE_E4M3 ? 32 : 0));
-            pipe::mbar_init(&sm.done[s], kTileGroups);
+            pipe::mbar_init(&sm.done[s], kWarps);
         }
         pipe::mbar_init_fence();
     }
@@ -567,12 +573,14 @@ __global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_s
     if (warp == kWarps) {                      // the copies
         uint32_t it = 0;
         bool alive = true;
-        const uint32_t g = lane % kTileGroups;
-        auto store_out = [&](int s) {
-            const AdamTile& tile = sm.tile[s];
+        auto scale_at = [](const AdamRec& t, uint32_t i, uint64_t first) { return (i < kWarps ? t.m_scale + i : t.v_scale + (i - kWarps)) + first; };
+        auto store_out = [&](uint32_t s) {
+            const auto& tile = sm.tile[s];
             if (!tile.whole) return;
             const AdamRec& t = *tile.tensor;
-            if (STATE == COLLAGE_STATE_E4M3 && g < tile.whole) (lane < kTileGroups ? t.m_scale : t.v_scale)[tile.first_group + g] = tile.scales[lane];
+            if (STATE == COLLAGE_STATE_E4M3)
+                for (uint32_t i = lane; i < 2 * kWarps; i += 32)
+                    if (i % kWarps < tile.whole) *scale_at(t, i, tile.first_group) = tile.scales[i];
             if (lane) return;
             const uint64_t at = tile.first_group * kGroup;
             const uint32_t n = tile.whole * kGroup;
@@ -582,15 +590,15 @@ __global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_s
             pipe::bulk_store(static_cast<char*>(t.v) + at * F::kStateBytes, sm.bytes[s] + F::kV, F::kStateBytes * n);
             pipe::bulk_commit();
         };
-        AdamChunk next = blockIdx.x < a.num_chunks ? a.chunks[blockIdx.x] : AdamChunk{0, 0};
-        for (uint64_t c = blockIdx.x; c < a.num_chunks; c += gridDim.x, ++it) {
-            const int s = it % kStages;
+        AdamChunk next = blockIdx.x < a.num_tiles ? a.tiles[blockIdx.x] : AdamChunk{0, 0};
+        for (uint64_t c = blockIdx.x; c < a.num_tiles; c += gridDim.x, ++it) {
+            const uint32_t s = it % kStages;
             const AdamChunk chunk = next;
-            if (c + gridDim.x < a.num_chunks) next = a.chunks[c + gridDim.x];
+            if (c + gridDim.x < a.num_tiles) next = a.tiles[c + gridDim.x];
             const AdamRec& t = a.tensors[chunk.tensor];
-            const uint64_t first_group = static_cast<uint64_t>(chunk.index) * kTileGroups, left = t.n - first_group * kGroup;
-            const uint32_t groups = static_cast<uint32_t>(min((left + kGroup - 1) / kGroup, static_cast<uint64_t>(kTileGroups)));
-            const uint32_t whole = t.aligned ? static_cast<uint32_t>(min(left / kGroup, static_cast<uint64_t>(kTileGroups))) : 0;
+            const uint64_t first_group = static_cast<uint64_t>(chunk.index) * kWarps, left = t.n - first_group * kGroup;
+            const uint32_t groups = static_cast<uint32_t>(min((left + kGroup - 1) / kGroup, static_cast<uint64_t>(kWarps)));
+            const uint32_t whole = t.aligned ? static_cast<uint32_t>(min(left / kGroup, static_cast<uint64_t>(kWarps))) : 0;
             if (it >= kStages) {
                 alive = __all_sync(0xFFFFFFFFu, pipe::mbar_wait(&sm.done[s], (it / kStages - 1) & 1u, 300u + s, &g_adam_fault));
                 if (!alive) break;
@@ -601,19 +609,23 @@ __global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_s
             const uint64_t at = first_group * kGroup;
             const uint32_t n = whole * kGroup;
             if (STATE == COLLAGE_STATE_E4M3) {
-                if (g < whole)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pipe::smem_addr(&sm.tile[s].scales[lane])), "l"((lane < kTileGroups ? t.m_scale : t.v_scale) + first_group + g)
-                                 : "memory");
+                for (uint32_t i = lane; i < 2 * kWarps; i += 32)
+                    if (i % kWarps < whole)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pipe::smem_addr(&sm.tile[s].scales[i])), "l"(scale_at(t, i, first_group)) : "memory");
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(pipe::smem_addr(&sm.full[s])) : "memory");
             }
             if (lane == 0) {
-                sm.tile[s].tensor = &t;
-                sm.tile[s].first_group = first_group;
-                sm.tile[s].groups = groups;
-                sm.tile[s].whole = whole;
-                // (a tile's pairs begin at a multiple of 128 and are 2048: their lower words may pass 2^32 only at one's beginning)
+                auto& tile = sm.tile[s];
+                tile.tensor = &t;
+                tile.first_group = first_group;
+                tile.groups = groups;
+                tile.whole = whole;
+                // (a group's pairs begin at a multiple of 128: the lower word of their numbers passes 2^32 between groups only)
                 const uint64_t pair = (t.first + at) >> 1;
-                sm.tile[s].random = static_cast<uint32_t>(pair) + mix32(static_cast<uint32_t>(pair >> 32) + a.k.key);
+                const uint32_t low = static_cast<uint32_t>(pair), high = static_cast<uint32_t>(pair >> 32);
+                tile.random[0] = low + mix32(high + a.k.key);
+                tile.random[1] = low + mix32(high + 1 + a.k.key);
+                tile.passed = low ? (0u - low) / (kGroup / 2) : kWarps;
                 pipe::mbar_arrive_expect_tx(&sm.full[s], n * (2 + (F::kReadsTheta ? 2 : 0) + F::kRestBytes + 2 * F::kStateBytes));
                 if (n) {
                     pipe::bulk_load(sm.bytes[s] + F::kG, t.grad + at, 2 * n, &sm.full[s]);
@@ -625,7 +637,7 @@ __global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_s
             }
         }
         for (uint32_t j = it > kStages ? it - kStages : 0; j < it && alive; ++j) {
-            const int s = j % kStages;
+            const uint32_t s = j % kStages;
             alive = __all_sync(0xFFFFFFFFu, pipe::mbar_wait(&sm.done[s], (j / kStages) & 1u, 310u + s, &g_adam_fault));
             if (alive) store_out(s);
         }
@@ -635,31 +647,27 @@ __global__ void __launch_bounds__(Form<STATE, REST>::kWarps * 32 + 32, 1) adam_s
         if (lane == 0) pipe::bulk_wait_all();
         return;
     }
+    // Every warp takes part in every tile, so none can be a turn of a stage ahead of or behind its barriers.
     const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
-    // (below 2^32 chunks)
-    const uint32_t tiles = static_cast<uint32_t>((a.num_chunks - blockIdx.x + gridDim.x - 1) / gridDim.x);
-    uint32_t it = warp / kTileGroups, g = warp % kTileGroups, s = it % kStages, phase = it / kStages & 1;
-    while (it < tiles) {
+    uint32_t s = 0, phase = 0;
+    for (uint64_t c = blockIdx.x; c < a.num_tiles; c += gridDim.x) {
         if (!__all_sync(0xFFFFFFFFu, pipe::mbar_wait(&sm.full[s], phase, 330u + s, &g_adam_fault))) return;
-        AdamTile& tile = sm.tile[s];
-        if (g < tile.whole) {
-            whole_group<STATE, REST, INSIDE>(sm.bytes[s], tile, g, a.k, grad_scale, lane);
+        auto& tile = sm.tile[s];
+        if (warp < tile.whole) {
+            whole_group<STATE, REST, INSIDE>(sm.bytes[s], tile, warp, a.k, grad_scale, lane);
             pipe::fence_async_smem();
-        } else if (g < tile.groups) {
-            any_group<STATE, REST, INSIDE>(*tile.tensor, tile.first_group + g, a.k, grad_scale);
+        } else if (warp < tile.groups) {
+            any_group<STATE, REST, INSIDE>(*tile.tensor, tile.first_group + warp, a.k, grad_scale);
         }
         __syncwarp();
         if (lane == 0) pipe::mbar_arrive(&sm.done[s]);
-        for (g += kWarps; g >= kTileGroups; g -= kTileGroups) {
-            ++it;
-            if (++s == kStages) { s = 0; phase ^= 1; }
-        }
+        if (++s == kStages) { s = 0; phase ^= 1; }
     }
 }
 
 template <int STATE, int REST>
 static collage_status_t launch_adam(const AdamArgs& a, int sm_count, cudaStream_t s) {
-    const uint64_t grid = std::min<uint64_t>(a.num_chunks, sm_count);
+    const uint64_t grid = std::min<uint64_t>(a.num_tiles, sm_count);
     constexpr int threads = Form<STATE, REST>::kWarps * 32 + 32;
     if constexpr (STATE == COLLAGE_STATE_E4M3 || REST == COLLAGE_REST_BF16)          // (elsewhere the flat step's operations look at the flag)
         if (a.k.f.flags & COLLAGE_FLAG_EPS_INSIDE_SQRT)
@@ -705,14 +713,14 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
         if (c >= a.num_chunks) return Part{nullptr, 0, false};
         const AdamChunk chunk = a.chunks[c];
         const AdamRec& t = a.tensors[chunk.tensor];
-        const uint64_t begin = chunk.index * static_cast<uint64_t>(kAdamChunk);
+        const uint64_t begin = chunk.index * static_cast<uint64_t>(kNormChunk);
         return Part{t.grad + begin, t.n - begin, t.aligned != 0};
     };
     Part now = part_of(blockIdx.x);
     for (uint64_t c = blockIdx.x; c < a.num_chunks; c += gridDim.x) {
         float g[2][8];
         uint4 q[2];
-        const bool whole = now.aligned && now.left >= kAdamChunk;
+        const bool whole = now.aligned && now.left >= kNormChunk;
         if (whole) {
             q[0] = __ldcs(reinterpret_cast<const uint4*>(now.grad) + threadIdx.x);
             q[1] = __ldcs(reinterpret_cast<const uint4*>(now.grad) + threadIdx.x + kAdamThreads);
@@ -776,13 +784,14 @@ using namespace collage::ops;
 
 struct collage_adam_plan {
     AdamRec* d_tensors = nullptr;
-    AdamChunk* d_chunks = nullptr;
-    uint64_t num_chunks = 0;
+    AdamChunk *d_chunks = nullptr, *d_tiles = nullptr;       // turns of the norm, and of the step
+    uint64_t num_chunks = 0, num_tiles = 0;
     std::vector<ByteRange> ranges, written;    // sorted by address: all arrays, and those that a step writes
     int state = 0, rest = 0, device = -1;
     ~collage_adam_plan() {
         cudaFree(d_tensors);
         cudaFree(d_chunks);
+        cudaFree(d_tiles);
     }
 };
 
@@ -792,7 +801,8 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     const uint64_t state_bytes = state == COLLAGE_STATE_F32 ? 4 : 1, rest_bytes = rest == COLLAGE_REST_F32 ? 4 : 2;
     std::vector<ByteRange> ranges, written;
     std::vector<AdamRec> recs;
-    std::vector<AdamChunk> chunks;
+    std::vector<AdamChunk> chunks, tiles;
+    const uint32_t tile = tile_groups(rest);
     uint64_t first = 0, num_chunks = 0;
     for (int i = 0; i < num; ++i) {
         const collage_adam_tensor_t& t = tensors[i];
@@ -804,7 +814,7 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
         auto off = [](const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; };
         if (off(t.theta, 2) || off(t.grad, 2) || off(t.rest, rest_bytes) || off(t.m, state_bytes) || off(t.v, state_bytes) || off(t.m_scale, 4) || off(t.v_scale, 4))
             return COLLAGE_ERR_ARG;
-        const uint64_t groups = (t.n + kGroup - 1) / kGroup, own_chunks = (t.n + kAdamChunk - 1) / kAdamChunk;
+        const uint64_t groups = (t.n + kGroup - 1) / kGroup, own_chunks = (t.n + kNormChunk - 1) / kNormChunk, own_tiles = (groups + tile - 1) / tile;
         num_chunks += own_chunks;
         if (num_chunks > 0xFFFFFFFFull) return COLLAGE_ERR_ARG;
         push_bytes(ranges, t.grad, 2 * t.n);
@@ -830,6 +840,7 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
         r.first = first;
         r.aligned = !off(t.theta, 16) && !off(t.grad, 16) && !off(t.rest, 16) && !off(t.m, 16) && !off(t.v, 16);
         first += groups * kGroup;
+        for (uint64_t c = 0; c < own_tiles; ++c) tiles.push_back({static_cast<uint32_t>(recs.size()), static_cast<uint32_t>(c)});
         for (uint64_t c = 0; c < own_chunks; ++c) chunks.push_back({static_cast<uint32_t>(recs.size()), static_cast<uint32_t>(c)});
         recs.push_back(r);
     }
@@ -839,6 +850,7 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     if (const collage_status_t st = current_device(&dev); st != COLLAGE_OK) return st;
     collage_adam_plan* plan = new collage_adam_plan;
     plan->num_chunks = num_chunks;
+    plan->num_tiles = tiles.size();
     plan->ranges = std::move(ranges);
     plan->written = std::move(written);
     plan->state = state;
@@ -846,6 +858,8 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
     if (cudaGetDevice(&plan->device) != cudaSuccess ||
         (num_chunks && (cudaMalloc(&plan->d_tensors, recs.size() * sizeof(AdamRec)) != cudaSuccess ||
                         cudaMalloc(&plan->d_chunks, chunks.size() * sizeof(AdamChunk)) != cudaSuccess ||
+                        cudaMalloc(&plan->d_tiles, tiles.size() * sizeof(AdamChunk)) != cudaSuccess ||
+                        cudaMemcpy(plan->d_tiles, tiles.data(), tiles.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_tensors, recs.data(), recs.size() * sizeof(AdamRec), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess))) {
         delete plan;
@@ -901,11 +915,11 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     DeviceInfo dev;
     if (const collage_status_t st = current_device(&dev); st != COLLAGE_OK) return st;
     if (!on_its_device(plan)) return COLLAGE_ERR_ARG;
-    if (plan->num_chunks == 0) return COLLAGE_OK;
+    if (plan->num_tiles == 0) return COLLAGE_OK;
     AdamArgs a = {};
     a.tensors = plan->d_tensors;
-    a.chunks = plan->d_chunks;
-    a.num_chunks = plan->num_chunks;
+    a.tiles = plan->d_tiles;
+    a.num_tiles = plan->num_tiles;
     a.grad_scale = grad_scale;
     a.k.f = fp32_scalars(hyper, step);
     const double t = static_cast<double>(step), bc1 = 1.0 - std::pow(hyper->beta1, t), bc2 = 1.0 - std::pow(hyper->beta2, t);

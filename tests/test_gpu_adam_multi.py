@@ -438,18 +438,47 @@ def test_many_small_tensors_and_many_chunks():
 
 
 def test_positions_beyond_33_bits():
-    """A tensor behind 2^33 elements has its own random bits (and its offsets)."""
-    n = (1 << 33) + 2 * GROUP
+    """The random bits change with the upper word of a pair's number, inside a tensor and behind it (and offsets pass 32 bits)."""
+    border, n = 1 << 33, (1 << 33) + 9 * GROUP
     zeros = lambda k, dtype: torch.zeros(k, dtype=dtype, device="cuda")  # noqa: E731
-    groups = n // GROUP
-    huge = (zeros(n, BF16), None, zeros(n, E4M3), zeros(n, E4M3), zeros(groups, F32), zeros(groups, F32), zeros(n, BF16))
-    tail = Tensor(3000, B.STATE_E4M3, B.REST_NONE, seed=4)
-    huge[6][-5:] = 1e-3
+    huge = (zeros(n, BF16), None, zeros(n, E4M3), zeros(n, E4M3), zeros(n // GROUP, F32), zeros(n // GROUP, F32), zeros(n, BF16))
+    tail, begin = Tensor(3000, B.STATE_E4M3, B.REST_NONE, seed=4), border - 40 * GROUP
+    here = Tensor(n - begin, B.STATE_E4M3, B.REST_NONE, seed=9)                       # what the tensor holds around the border
+    parts = [huge[0][begin:], None, huge[2][begin:], huge[3][begin:], huge[4][begin // GROUP:], huge[5][begin // GROUP:], huge[6][begin:]]
+    for part, value in zip(parts, here.row()):
+        if part is not None:
+            part.copy_(value)
     plan = B.adam_plan_create([huge, tail.row()])
-    want = expected(tail, 3)
+    want, want_here = expected(tail, 3), expected(here, 3)
     B.adam_step(plan, hyper(), 3, seed=77)
+    for part, value in zip(parts, here.row()):
+        if part is not None:
+            value.copy_(part)
+    check(here, want_here, begin, 77, 3, "around")
     check(tail, want, n, 77, 3, "behind")
-    assert (huge[0][-5:].float() < 0).all() and int((huge[0][-4096:] != 0).sum()) == 5 and int((huge[0][:4096] != 0).sum()) == 0
+    assert int((huge[0][:begin] != 0).sum()) == 0
     B.adam_plan_destroy(plan)
-    del huge
+    del huge, parts
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("state,rest", FORMS)
+def test_many_steps_over_many_tiles(state, rest):
+    """Blocks that turn over their stages many times, of ragged tensors between: the same as each tensor by itself, step after step."""
+    sizes = [3_000_001, 4864 * 148 * 2, 17, 5000, 3840 * 148 * 3 + 256]
+    together, apart = ([Tensor(n, state, rest, seed=i) for i, n in enumerate(sizes)] for _ in range(2))
+    plan = B.adam_plan_create([t.row() for t in together])
+    alone = [B.adam_plan_create([t.row()]) for t in apart]
+    for step in range(1, 21):
+        B.adam_step(plan, hyper(), step, seed=step)
+        for p in alone:
+            B.adam_step(p, hyper(), step, seed=step)
+    for a, b in zip(together, apart):
+        for k, (x, y) in enumerate(zip(a.row(), b.row())):
+            # (a root's random bits go by its position in the plan: only the first tensor has the same ones)
+            if x is not None and (a is together[0] or state == B.STATE_F32):
+                assert torch.equal(x.view(torch.uint8) if x.dtype is E4M3 else x, y.view(torch.uint8) if y.dtype is E4M3 else y), (a.n, k)
+        assert a.intact() and all(x is None or x.float().isfinite().all() for x in a.row())
+    assert B.pipeline_fault() == 0
+    for p in [plan, *alone]:
+        B.adam_plan_destroy(p)
