@@ -57,16 +57,10 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ uint64_t pair_of(float v) { return ops::pair_of(v, v); }
-__device__ __forceinline__ uint64_t sub_pair(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // A sum of two products, each rounded.  (The assembler makes a packed product and a packed sum of it one fma; not so of these.)
 __device__ __forceinline__ uint64_t add_rounded(uint64_t a, uint64_t b) {
     const float2 f = floats_of(a), g = floats_of(b);
-    return ops::pair_of(__fadd_rn(f.x, g.x), __fadd_rn(f.y, g.y));
+    return pair_of(__fadd_rn(f.x, g.x), __fadd_rn(f.y, g.y));
 }
 // times a constant of the call, plus another
 __device__ __forceinline__ uint64_t scaled_pair(uint64_t a, float c) {
@@ -78,11 +72,10 @@ __device__ __forceinline__ uint64_t scaled_plus(uint64_t a, float c, float d) {
 __device__ __forceinline__ uint64_t scaled_plus(uint64_t a, float c, uint64_t d) {
     return fma_pair(a, pair_of(c), d);
 }
-__device__ __forceinline__ uint64_t bf16_pair(uint32_t word) { return ops::pair_of(bf16_lo(word), bf16_hi(word)); }
 __device__ __forceinline__ uint64_t e4m3_pair(uint32_t two) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
     const float2 f = __half22float2(__half2(h));
-    return ops::pair_of(f.x, f.y);
+    return pair_of(f.x, f.y);
 }
 
 // Square roots: y = rsqrt(v) gives r = v y, and a step of Newton's method on r^2 = v, whose remainder r^2 - v is exact in an fma, the
@@ -92,15 +85,15 @@ __device__ __forceinline__ uint64_t root_pair(uint64_t v) {
     float2 y;
     asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(f.x, 0x1p-149f)));         // (of 0: 0 times a finite number)
     asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(f.y, 0x1p-149f)));
-    const uint64_t y2 = ops::pair_of(y.x, y.y), r = mul_pair(v, y2);
+    const uint64_t y2 = pair_of(y.x, y.y), r = mul_pair(v, y2);
     const float2 q = floats_of(r);
-    return ops::pair_of(__fmaf_rn(__fmaf_rn(-q.x, q.x, f.x), 0.5f * y.x, q.x), __fmaf_rn(__fmaf_rn(-q.y, q.y, f.y), 0.5f * y.y, q.y));
+    return pair_of(__fmaf_rn(__fmaf_rn(-q.x, q.x, f.x), 0.5f * y.x, q.x), __fmaf_rn(__fmaf_rn(-q.y, q.y, f.y), 0.5f * y.y, q.y));
 }
 __device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
     float2 f = floats_of(v);
     asm("rcp.approx.f32 %0, %0;" : "+f"(f.x));
     asm("rcp.approx.f32 %0, %0;" : "+f"(f.y));
-    return ops::pair_of(f.x, f.y);
+    return pair_of(f.x, f.y);
 }
 
 // A step of two elements' states: m', sqrt(v') (or v' itself), and the update of parameters x.  Every product and sum of the states is
@@ -199,9 +192,9 @@ __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float gra
             float2 m = floats_of(o.m[p]), v = floats_of(o.v[p]);
             const float2 gf = floats_of(g), xf = floats_of(x);
             const float lo = adamw_fp32_delta(m.x, v.x, xf.x, gf.x, k.f), hi = adamw_fp32_delta(m.y, v.y, xf.y, gf.y, k.f);
-            delta = ops::pair_of(lo, hi);
-            o.m[p] = ops::pair_of(m.x, m.y);
-            o.v[p] = ops::pair_of(v.x, v.y);
+            delta = pair_of(lo, hi);
+            o.m[p] = pair_of(m.x, m.y);
+            o.v[p] = pair_of(v.x, v.y);
         } else {
             delta = advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k);
         }
@@ -366,7 +359,7 @@ __device__ __forceinline__ void floats_to_words(const uint64_t (&f)[4], uint32_t
 }
 __device__ __forceinline__ void words_to_floats(const uint32_t (&w)[8], uint64_t (&f)[4]) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) f[p] = ops::pair_of(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
+    for (int p = 0; p < 4; ++p) f[p] = pair_of(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
 }
 
 // A lane's part of group `g` of a tile
@@ -489,7 +482,7 @@ __device__ __noinline__ void any_group(const AdamRec& t, uint64_t group, const A
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             const uint64_t i = begin + p * 64, j = i + 32;
-            to[p] = ops::pair_of(i < t.n ? value(i) : 0.0f, j < t.n ? value(j) : 0.0f);
+            to[p] = pair_of(i < t.n ? value(i) : 0.0f, j < t.n ? value(j) : 0.0f);
         }
     };
     auto code = [](const void* p, uint64_t i) { return floats_of(e4m3_pair(static_cast<const uint8_t*>(p)[i])).x; };

@@ -46,6 +46,9 @@ __device__ __forceinline__ float2 gate_value_and_slope(int kind, float g) {
 }
 __device__ __forceinline__ float gate_slope(int kind, float g) { return gate_value_and_slope(kind, g).y; }
 
+#ifndef BN_ROWS
+#define BN_ROWS 1024
+#endif
 constexpr int kBlockThreads = 256;
 
 // One block per row, element by element, the row read again for each stage: any length, stride and alignment.
@@ -223,11 +226,198 @@ __global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) block_norm_
     }
 }
 
+// Many rows of whole vectors: a block on each SM walks over rows, one at a time for each group of `group_threads`, two vectors a thread.  What
+// the columns are multiplied by is laid out in floats once; a thread sends for its vectors of the next two rows ahead.
+constexpr int kRowsDepth = 2;
+
+template <bool TOKEN_GATE, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) block_norm_rows_kernel(const __grid_constant__ BlockNormArgs a, uint64_t rows, int group_threads) {
+    constexpr int kArrays = TOKEN_GATE ? 3 : 2, PER = 2;
+    __shared__ float slots[2][THREADS / 32];
+    __shared__ uint32_t most_slots[THREADS / 32];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    after_previous();
+    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
+    const int lane = threadIdx.x & 31, group_warps = group_threads >> 5, warp0 = group * group_warps;
+    const int vectors = static_cast<int>(a.cols >> 3);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    float* post = reinterpret_cast<float*>(dynamic);            // [cols]: beta * post_weight, and A(gate) where it is one of channels
+    float* pre = post + a.cols;                                 // [cols]
+    uint4* places = reinterpret_cast<uint4*>(dynamic + 8 * a.cols) + threadIdx.x;
+    auto place = [&](int stage, int array, int i) { return places + ((stage * kArrays + array) * PER + i) * blockDim.x; };
+    for (int d = 0; d < kRowsDepth; ++d)
+        for (int k = 0; k < kArrays * PER; ++k) *place(d, 0, k) = none;         // places that no load fills
+    for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) {
+        float k = a.post ? a.beta * bf16_value(a.post[j]) : a.beta;
+        if (!TOKEN_GATE && a.gate) k *= gate_value(a.activation, bf16_value(a.gate[j]));
+        post[j] = k;
+        pre[j] = a.pre ? bf16_value(a.pre[j]) : 0.0f;
+    }
+    const uint64_t first = blockIdx.x * static_cast<uint64_t>(groups) + group, step = static_cast<uint64_t>(gridDim.x) * groups;
+    auto send_for = [&](uint64_t row, int stage) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+            if (row >= rows || v >= vectors) continue;
+            auto copy = [&](int k, const uint16_t* base, uint64_t ld) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(place(stage, k, i)))),
+                             "l"(reinterpret_cast<const uint4*>(base + row * ld) + v)
+                             : "memory");
+            };
+            copy(0, a.o, a.ldo);
+            copy(1, a.x, a.ldx);
+            if (TOKEN_GATE) copy(2, a.gate, a.ldg);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int d = 0; d < kRowsDepth; ++d) send_for(first + d * step, d);
+    __syncthreads();                            // the columns' factors are there
+    auto barrier = [&] { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory"); };
+    auto joined = [&](float s, int which) {
+        s = warp_sum(s);
+        if (group_warps > 1) {
+            if (lane == 0) slots[which][threadIdx.x >> 5] = s;
+            barrier();
+            s = warp_sum(lane < group_warps ? slots[which][warp0 + lane] : 0.0f);
+        }
+        return s;
+    };
+    uint64_t f[PER][4];
+    // 1 / rms of the values in f, which come out times a power of two where their squares need one (returned in `factor`)
+    auto rstd_of = [&](int which, float& factor) {
+        auto mean_of = [&](float by) {
+            uint64_t sum[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                sum[i] = mul_pair(f[i][0], f[i][0]);
+#pragma unroll
+                for (int p = 1; p < 4; ++p) sum[i] = fma_pair(f[i][p], f[i][p], sum[i]);
+            }
+            return joined(sum_of(sum[0]) + sum_of(sum[1]), which) / static_cast<float>(a.cols) + a.eps * by * by;
+        };
+        factor = 1.0f;
+        float mean = mean_of(1.0f);
+        if (!squares_fit(mean)) {
+            factor = rescue_factor(mean);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) f[i][p] = mul_pair(f[i][p], pair_of(factor));
+            if (group_warps > 1) barrier();     // (the slots have been read)
+            mean = mean_of(factor);
+        }
+        return 1.0f / sqrtf(mean);
+    };
+    auto times = [&](const float* k, int v, uint64_t (&g)[4]) {
+        const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(k)[2 * v], hi = reinterpret_cast<const ulonglong2*>(k)[2 * v + 1];
+        g[0] = mul_pair(g[0], lo.x); g[1] = mul_pair(g[1], lo.y); g[2] = mul_pair(g[2], hi.x); g[3] = mul_pair(g[3], hi.y);
+    };
+    int stage = 0;
+    for (uint64_t row = first; row < rows; row += step) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRowsDepth - 1) : "memory");
+#pragma unroll
+        for (int i = 0; i < PER; ++i) unpack_pairs(*place(stage, 0, i), f[i]);
+        float factor, rstd = 1.0f;
+        if (a.post) {
+            rstd = rstd_of(0, factor);
+            if (a.rstd_post && t == 0) a.rstd_post[row] = factor * rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+            uint64_t x[4];
+            unpack_pairs(*place(stage, 1, i), x);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) f[i][p] = mul_pair(f[i][p], pair_of(rstd));
+            if (TOKEN_GATE) {
+                uint64_t g[4];
+                unpack_pairs(*place(stage, 2, i), g);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const float2 gate = floats_of(g[p]);
+                    f[i][p] = mul_pair(f[i][p], pair_of(gate_value(a.activation, gate.x), gate_value(a.activation, gate.y)));
+                }
+            }
+            if (v < vectors) {
+                times(post, v, f[i]);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) f[i][p] = fma_pair(x[p], pair_of(a.alpha), f[i][p]);
+                reinterpret_cast<uint4*>(a.r + row * a.ldr)[v] = pack_pairs(f[i]);
+            } else {
+#pragma unroll
+                for (int p = 0; p < 4; ++p) f[i][p] = 0;
+            }
+        }
+        send_for(row + kRowsDepth * step, stage);
+        stage = stage + 1 == kRowsDepth ? 0 : stage + 1;
+        if (a.pre) {
+            rstd = rstd_of(1, factor);
+            if (a.rstd_pre && t == 0) a.rstd_pre[row] = factor * rstd;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int v = t + i * group_threads;
+                if (v >= vectors) continue;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) f[i][p] = mul_pair(f[i][p], pair_of(rstd));
+                times(pre, v, f[i]);
+                if (a.y) reinterpret_cast<uint4*>(a.y + row * a.ldy)[v] = pack_pairs(f[i]);
+            }
+        }
+        if (a.y8) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const float2 y = floats_of(f[i][p]);
+                    if (t + i * group_threads < vectors) most = max(most, max(__float_as_uint(y.x) & 0x7FFFFFFFu, __float_as_uint(y.y) & 0x7FFFFFFFu));
+                }
+            most = __reduce_max_sync(0xFFFFFFFFu, most);
+            if (group_warps > 1) {
+                if (lane == 0) most_slots[threadIdx.x >> 5] = most;
+                barrier();
+                most = __reduce_max_sync(0xFFFFFFFFu, lane < group_warps ? most_slots[warp0 + lane] : 0u);
+            }
+            const float scale = __uint_as_float(most) / kE4m3Max;
+            if (t == 0) a.scale[row] = scale;
+            const Divisor by(scale);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int v = t + i * group_threads;
+                if (v >= vectors) continue;
+                uint32_t w[2] = {0, 0};
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const float2 y = floats_of(f[i][p]);
+                    if (by.plain)
+                        w[p >> 1] |= pack_e4m3(by.quotient(y.x), by.quotient(y.y)) << (16 * (p & 1));
+                    else if (scale != 0.0f)
+                        w[p >> 1] |= pack_e4m3(y.x / scale, y.y / scale) << (16 * (p & 1));
+                }
+                reinterpret_cast<uint2*>(a.y8 + row * a.ldy8)[v] = make_uint2(w[0], w[1]);
+            }
+        }
+        // (of several joins a row, each one's barrier parts the others' slots between rows; one alone needs a second barrier)
+        if (group_warps > 1 && (a.post != nullptr) + (a.pre != nullptr) == 1) barrier();
+    }
+}
+
+template <bool TOKEN_GATE, int THREADS>
+static collage_status_t launch_rows(const BlockNormArgs& a, uint64_t rows, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3;
+    const int group = static_cast<int>((v + 63) / 64 * 32), groups = std::max(1, std::min(THREADS / group, 15));
+    const size_t smem = 8 * a.cols + static_cast<size_t>(kRowsDepth) * (TOKEN_GATE ? 3 : 2) * 2 * 16 * group * groups;
+    const uint64_t grid = std::min<uint64_t>((rows + groups - 1) / groups, static_cast<uint64_t>(sm_count));
+    return launch<&block_norm_rows_kernel<TOKEN_GATE, THREADS>>(grid, group * groups, 1, smem, s, a, rows, group);
+}
+
 // A row's vectors over warps, as in the residual norm: with many rows four vectors a thread, with few rows one.
 static collage_status_t launch_block_norm(const BlockNormArgs& a, uint64_t rows, bool vectors_fit, int sm_count, cudaStream_t s) {
     const uint64_t v = a.cols >> 3;
     const bool many = rows > 2ull * sm_count;
     if (!vectors_fit || v > 4096) return launch<&block_norm_any_kernel>(rows, kBlockThreads, 1, 0, s, a);
+    if (rows >= BN_ROWS && v <= 1024) return a.gate && a.ldg ? launch_rows<true, 512>(a, rows, sm_count, s) : launch_rows<false, 1024>(a, rows, sm_count, s);
     if (many && v <= 128) {
         const uint64_t grid = (rows + 3) / 4;
         return v <= 32   ? launch<&block_norm_kernel<1, true>>(grid, 128, 1, 0, s, a, rows)
@@ -309,38 +499,29 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
     }
 }
 
-// Rows of whole vectors in one pass: blocks walk over rows, one at a time for each group of `group_threads`.  A thread owns PER vectors of
-// columns: it sends for its own of the next two rows ahead, so that loads go on while a row's two sums are joined, and keeps its columns'
-// sums over rows in registers until the end.
-constexpr int kBackwardDepth = 2;
+// Rows of whole vectors in one pass: a block on each SM walks over rows, one at a time for each group of `group_threads`.  A thread owns a
+// vector of columns (two an instruction in pairs): it sends for its own of the next two rows ahead, so that loads go on while a row's two sums are
+// joined, and keeps its columns' sums over rows in registers until the end.
+constexpr int kBackwardDepth = 2, kBackwardThreads = 1024;
 
-template <int PER, int THREADS, bool TOKEN_GATE>
-__global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads) {
+template <bool TOKEN_GATE>
+__global__ void __launch_bounds__(kBackwardThreads, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads) {
     constexpr int kArrays = TOKEN_GATE ? 5 : 4;
-    __shared__ float slots[2][THREADS / 32];
+    __shared__ float slots[2][kBackwardThreads / 32];
     extern __shared__ __align__(16) uint8_t dynamic[];
     after_previous();
-    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
+    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, v = threadIdx.x % group_threads;
     const int lane = threadIdx.x & 31, group_warps = group_threads >> 5, warp0 = group * group_warps;
-    const int vectors = static_cast<int>(a.cols >> 3);
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    uint4* mine = reinterpret_cast<uint4*>(dynamic) + threadIdx.x;      // [kBackwardDepth][kArrays][PER] places, blockDim.x apart
-    auto place = [&](int stage, int array, int i) { return mine + ((stage * kArrays + array) * PER + i) * blockDim.x; };
-    // factors of the columns, in floats, for the block's groups alike: post_weight, and the gate's value where it is one of channels
-    uint4 qpre[PER], qpost[PER];
-    float sum_pre[PER][8], sum_post[PER][8];
-    const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int v = t + i * group_threads;
-        qpre[i] = a.pre && v < vectors ? reinterpret_cast<const uint4*>(a.pre)[v] : none;
-        qpost[i] = v < vectors ? (a.post ? reinterpret_cast<const uint4*>(a.post)[v] : ones) : none;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum_pre[i][e] = sum_post[i][e] = 0.0f;
-        for (int d = 0; d < kBackwardDepth; ++d)
-            for (int k = 0; k < kArrays; ++k) *place(d, k, i) = none;         // places that no load fills
-    }
-    float* channel = reinterpret_cast<float*>(mine - threadIdx.x + kBackwardDepth * kArrays * PER * blockDim.x);     // [cols] A(gate), with a gate of channels
+    const bool mine = v < static_cast<int>(a.cols >> 3);
+    const uint4 none = make_uint4(0, 0, 0, 0), ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+    uint4* places = reinterpret_cast<uint4*>(dynamic) + threadIdx.x;      // [kBackwardDepth][kArrays], blockDim.x apart
+    auto place = [&](int stage, int array) { return places + (stage * kArrays + array) * blockDim.x; };
+    const uint4 qpre = a.pre && mine ? reinterpret_cast<const uint4*>(a.pre)[v] : none;
+    const uint4 qpost = mine ? (a.post ? reinterpret_cast<const uint4*>(a.post)[v] : ones) : none;
+    uint64_t sum_pre[4] = {0, 0, 0, 0}, sum_post[4] = {0, 0, 0, 0};
+    for (int d = 0; d < kBackwardDepth; ++d)
+        for (int k = 0; k < kArrays; ++k) *place(d, k) = none;            // places that no load fills
+    float* channel = reinterpret_cast<float*>(dynamic) + kBackwardDepth * kArrays * 4 * blockDim.x;       // [cols] A(gate), with a gate of channels
     const bool channels = !TOKEN_GATE && a.gate;
     if (channels) {
         for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) channel[j] = gate_value(a.activation, bf16_value(a.gate[j]));
@@ -348,24 +529,19 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
     }
     const uint64_t first = blockIdx.x * static_cast<uint64_t>(groups) + group, step = static_cast<uint64_t>(gridDim.x) * groups;
     auto send_for = [&](uint64_t row, int stage) {
-        if (row < a.rows) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int v = t + i * group_threads;
-                if (v >= vectors) continue;
-                auto copy = [&](int k, const uint16_t* base, uint64_t ld) {
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(place(stage, k, i)))),
-                                 "l"(reinterpret_cast<const uint4*>(base + row * ld) + v)
-                                 : "memory");
-                };
-                if (a.dy) {
-                    copy(0, a.dy, a.lddy);
-                    copy(1, a.r, a.ldr);
-                }
-                if (a.dr) copy(2, a.dr, a.lddr);
-                copy(3, a.o, a.ldo);
-                if (TOKEN_GATE) copy(4, a.gate, a.ldg);
+        if (row < a.rows && mine) {
+            auto copy = [&](int k, const uint16_t* base, uint64_t ld) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(place(stage, k)))),
+                             "l"(reinterpret_cast<const uint4*>(base + row * ld) + v)
+                             : "memory");
+            };
+            if (a.dy) {
+                copy(0, a.dy, a.lddy);
+                copy(1, a.r, a.ldr);
             }
+            if (a.dr) copy(2, a.dr, a.lddr);
+            copy(3, a.o, a.ldo);
+            if (TOKEN_GATE) copy(4, a.gate, a.ldg);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -373,113 +549,91 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
     for (int d = 0; d < kBackwardDepth; ++d) send_for(first + d * step, d);
     const float per_col = 1.0f / static_cast<float>(a.cols);
     // over the group; the two sums of a row have slots of their own, so that one barrier each is enough
-    auto joined = [&](float v, int which) {
-        v = warp_sum(v);
+    auto joined = [&](float s, int which) {
+        s = warp_sum(s);
         if (group_warps > 1) {
-            if (lane == 0) slots[which][threadIdx.x >> 5] = v;
+            if (lane == 0) slots[which][threadIdx.x >> 5] = s;
             asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
-            v = warp_sum(lane < group_warps ? slots[which][warp0 + lane] : 0.0f);
+            s = warp_sum(lane < group_warps ? slots[which][warp0 + lane] : 0.0f);
         }
-        return v;
+        return s;
     };
     int stage = 0;
     const bool second = a.post && a.dblock;
+    float rstd_r = a.dy && first < a.rows ? a.rstd_pre[first] : 0.0f, rstd_o = a.post && first < a.rows ? a.rstd_post[first] : 1.0f;
     for (uint64_t row = first; row < a.rows; row += step) {
-        const float rstd_r = a.dy ? a.rstd_pre[row] : 0.0f, rstd_o = a.post ? a.rstd_post[row] : 1.0f;
+        const float next_r = a.dy && row + step < a.rows ? a.rstd_pre[row + step] : 0.0f, next_o = a.post && row + step < a.rows ? a.rstd_post[row + step] : 1.0f;
         asm volatile("cp.async.wait_group %0;" ::"n"(kBackwardDepth - 1) : "memory");
+        uint64_t n[4] = {0, 0, 0, 0}, d[4] = {0, 0, 0, 0};      // n of the stream, then of the block; the gradient on its way from y to the block
         float mean = 0.0f;
         if (a.dy) {
-            float sum = 0.0f;
+            uint64_t dy[4], w[4], sum = 0;
+            unpack_pairs(*place(stage, 0), dy);
+            unpack_pairs(*place(stage, 1), n);
+            unpack_pairs(qpre, w);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                float dy[8], r[8], w[8];
-                unpack8(*place(stage, 0, i), dy);
-                unpack8(*place(stage, 1, i), r);
-                unpack8(qpre[i], w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float n = r[e] * rstd_r;
-                    sum_pre[i][e] = __fmaf_rn(dy[e], n, sum_pre[i][e]);
-                    sum = __fmaf_rn(dy[e] * w[e], n, sum);
-                }
+            for (int p = 0; p < 4; ++p) {
+                n[p] = mul_pair(n[p], pair_of(rstd_r));
+                sum_pre[p] = fma_pair(dy[p], n[p], sum_pre[p]);
+                d[p] = mul_pair(dy[p], w[p]);
+                sum = fma_pair(d[p], n[p], sum);
             }
-            mean = joined(sum, 0) * per_col;
+            mean = joined(sum_of(sum), 0) * per_col;
         }
-        float d[PER][8];                        // the stream's gradient, then h
-        float sum = 0.0f;
+        uint64_t sum = 0, dr[4] = {0, 0, 0, 0}, w[4];
+        if (a.dr) unpack_pairs(*place(stage, 2), dr);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int v = t + i * group_threads;
+        for (int p = 0; p < 4; ++p) d[p] = a.dy ? fma_pair(fma_pair(n[p], pair_of(-mean), d[p]), pair_of(rstd_r), dr[p]) : dr[p];
+        if (a.dx && mine) {
+            uint64_t dx[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d[i][e] = 0.0f;
-            if (a.dy) {
-                float dy[8], r[8], w[8];
-                unpack8(*place(stage, 0, i), dy);
-                unpack8(*place(stage, 1, i), r);
-                unpack8(qpre[i], w);
+            for (int p = 0; p < 4; ++p) dx[p] = mul_pair(d[p], pair_of(a.alpha));
+            reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack_pairs(dx);
+        }
+        unpack_pairs(*place(stage, 3), n);
+        unpack_pairs(qpost, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[i][e] = rstd_r * __fmaf_rn(-r[e] * rstd_r, mean, dy[e] * w[e]);
+        for (int p = 0; p < 4; ++p) {
+            n[p] = mul_pair(n[p], pair_of(rstd_o));
+            d[p] = mul_pair(d[p], pair_of(a.beta));
+        }
+        if (TOKEN_GATE) {
+            uint64_t g[4], dg[4];
+            unpack_pairs(*place(stage, 4), g);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const float2 gf = floats_of(g[p]);
+                const float2 lo = gate_value_and_slope(a.activation, gf.x), hi = gate_value_and_slope(a.activation, gf.y);
+                dg[p] = mul_pair(mul_pair(mul_pair(d[p], n[p]), w[p]), pair_of(lo.y, hi.y));
+                d[p] = mul_pair(d[p], pair_of(lo.x, hi.x));
+                sum_post[p] = fma_pair(d[p], n[p], sum_post[p]);
             }
-            if (a.dr) {
-                float dr[8];
-                unpack8(*place(stage, 2, i), dr);
+            if (a.dgate && mine) reinterpret_cast<uint4*>(a.dgate + row * a.lddg)[v] = pack_pairs(dg);
+        } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[i][e] += dr[e];
-            }
-            if (a.dx && v < vectors) {
-                float dx[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dx[e] = a.alpha * d[i][e];
-                reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack8(dx);
-            }
-            float o[8], w[8];
-            unpack8(*place(stage, 3, i), o);
-            unpack8(qpost[i], w);
-            if (TOKEN_GATE) {
-                float g[8], dg[8];
-                unpack8(*place(stage, 4, i), g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 gate = gate_value_and_slope(a.activation, g[e]);
-                    const float n = o[e] * rstd_o, u = a.beta * d[i][e];
-                    dg[e] = u * n * w[e] * gate.y;
-                    d[i][e] = u * gate.x;
-                    sum_post[i][e] = __fmaf_rn(d[i][e], n, sum_post[i][e]);
-                    d[i][e] *= w[e];
-                    sum = __fmaf_rn(d[i][e], n, sum);
-                }
-                if (a.dgate && v < vectors) reinterpret_cast<uint4*>(a.dgate + row * a.lddg)[v] = pack8(dg);
-            } else {
-                float A[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-                if (channels && v < vectors) {
-                    const float4 lo = reinterpret_cast<const float4*>(channel)[2 * v], hi = reinterpret_cast<const float4*>(channel)[2 * v + 1];
-                    A[0] = lo.x; A[1] = lo.y; A[2] = lo.z; A[3] = lo.w; A[4] = hi.x; A[5] = hi.y; A[6] = hi.z; A[7] = hi.w;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float n = o[e] * rstd_o, u = a.beta * d[i][e];
-                    sum_post[i][e] = __fmaf_rn(u, n, sum_post[i][e]);
-                    d[i][e] = u * A[e] * w[e];
-                    sum = __fmaf_rn(d[i][e], n, sum);
-                }
+            for (int p = 0; p < 4; ++p) sum_post[p] = fma_pair(d[p], n[p], sum_post[p]);
+            if (channels && mine) {
+                const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(channel)[2 * v], hi = reinterpret_cast<const ulonglong2*>(channel)[2 * v + 1];
+                d[0] = mul_pair(d[0], lo.x); d[1] = mul_pair(d[1], lo.y); d[2] = mul_pair(d[2], hi.x); d[3] = mul_pair(d[3], hi.y);
             }
         }
         if (a.dblock) {
-            mean = second ? joined(sum, 1) * per_col : 0.0f;
+            if (second) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int v = t + i * group_threads;
-                if (a.post) {
-                    float o[8];
-                    unpack8(*place(stage, 3, i), o);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) d[i][e] = rstd_o * __fmaf_rn(-o[e] * rstd_o, mean, d[i][e]);
+                for (int p = 0; p < 4; ++p) {
+                    d[p] = mul_pair(d[p], w[p]);
+                    sum = fma_pair(d[p], n[p], sum);
                 }
-                if (v < vectors) reinterpret_cast<uint4*>(a.dblock + row * a.lddo)[v] = pack8(d[i]);
+                mean = joined(sum_of(sum), 1) * per_col;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) d[p] = mul_pair(fma_pair(n[p], pair_of(-mean), d[p]), pair_of(rstd_o));
             }
+            if (mine) reinterpret_cast<uint4*>(a.dblock + row * a.lddo)[v] = pack_pairs(d);
         }
         send_for(row + kBackwardDepth * step, stage);
         stage = stage + 1 == kBackwardDepth ? 0 : stage + 1;
+        rstd_r = next_r;
+        rstd_o = next_o;
         // (of two sums, each one's barrier parts the other's slots between rows; one alone needs a second barrier)
         if (group_warps > 1 && (a.dy != nullptr) != second) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
     }
@@ -487,51 +641,40 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
     // the block's groups in order, then one row of partial sums a block
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    float* shared_sums = reinterpret_cast<float*>(dynamic);             // [groups - 1][2][cols]
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int v = t + i * group_threads;
-        if (group == 0 || v >= vectors) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            shared_sums[(2 * group - 2) * a.cols + v * 8 + e] = sum_pre[i][e];
-            shared_sums[(2 * group - 1) * a.cols + v * 8 + e] = sum_post[i][e];
-        }
+    ulonglong2* shared_sums = reinterpret_cast<ulonglong2*>(dynamic);         // [groups][4] for each vector: pairs of both sums
+    if (group > 0 && mine) {
+        ulonglong2* to = shared_sums + (static_cast<uint64_t>(group) * group_threads + v) * 4;
+        to[0] = make_ulonglong2(sum_pre[0], sum_pre[1]);
+        to[1] = make_ulonglong2(sum_pre[2], sum_pre[3]);
+        to[2] = make_ulonglong2(sum_post[0], sum_post[1]);
+        to[3] = make_ulonglong2(sum_post[2], sum_post[3]);
     }
     __syncthreads();
-    if (group > 0) return;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int v = t + i * group_threads;
-        if (v >= vectors) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            for (int g = 1; g < groups; ++g) {
-                sum_pre[i][e] += shared_sums[(2 * g - 2) * a.cols + v * 8 + e];
-                sum_post[i][e] += shared_sums[(2 * g - 1) * a.cols + v * 8 + e];
-            }
-        for (int k = 0; k < 2; ++k) {
-            float4* out = reinterpret_cast<float4*>(a.partial + (2ull * blockIdx.x + k) * a.cols + v * 8);
-            const float* s = k ? sum_post[i] : sum_pre[i];
-            out[0] = make_float4(s[0], s[1], s[2], s[3]);
-            out[1] = make_float4(s[4], s[5], s[6], s[7]);
-        }
+    if (group > 0 || !mine) return;
+    for (int g = 1; g < groups; ++g) {
+        const ulonglong2* from = shared_sums + (static_cast<uint64_t>(g) * group_threads + v) * 4;
+        sum_pre[0] = add_pair(sum_pre[0], from[0].x); sum_pre[1] = add_pair(sum_pre[1], from[0].y);
+        sum_pre[2] = add_pair(sum_pre[2], from[1].x); sum_pre[3] = add_pair(sum_pre[3], from[1].y);
+        sum_post[0] = add_pair(sum_post[0], from[2].x); sum_post[1] = add_pair(sum_post[1], from[2].y);
+        sum_post[2] = add_pair(sum_post[2], from[3].x); sum_post[3] = add_pair(sum_post[3], from[3].y);
     }
+    ulonglong2* out = reinterpret_cast<ulonglong2*>(a.partial + 2ull * blockIdx.x * a.cols + v * 8);
+    out[0] = make_ulonglong2(sum_pre[0], sum_pre[1]);
+    out[1] = make_ulonglong2(sum_pre[2], sum_pre[3]);
+    out = reinterpret_cast<ulonglong2*>(a.partial + (2ull * blockIdx.x + 1) * a.cols + v * 8);
+    out[0] = make_ulonglong2(sum_post[0], sum_post[1]);
+    out[1] = make_ulonglong2(sum_post[2], sum_post[3]);
 }
 
-template <int PER, int THREADS, bool TOKEN_GATE>
-static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
-    const uint64_t v = a.cols >> 3;
-    const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), groups = std::max(1, std::min(THREADS / group, 15));
-    // the places hold the groups' sums too: 8 cols bytes a group, against 64 kBackwardDepth bytes for each 8 columns
-    const size_t smem = static_cast<size_t>(kBackwardDepth) * (TOKEN_GATE ? 5 : 4) * PER * 16 * group * groups + (!TOKEN_GATE && a.gate ? 4 * a.cols : 0);
-    *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
-    return launch<&block_norm_backward_kernel<PER, THREADS, TOKEN_GATE>>(*parts, group * groups, 1, smem, s, a, group);
-}
-// Rows of up to 256 columns are a warp's, without barriers; longer ones take two vectors a thread.
+// Rows of up to 256 columns are a warp's, without barriers.
 template <bool TOKEN_GATE>
 static collage_status_t launch_block_backward(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
-    return a.cols <= 256 ? launch_block_backward_as<1, 512, TOKEN_GATE>(a, parts, sm_count, s) : launch_block_backward_as<2, 512, TOKEN_GATE>(a, parts, sm_count, s);
+    const uint64_t v = a.cols >> 3;
+    const int group = static_cast<int>((v + 31) / 32 * 32), groups = std::max(1, std::min(kBackwardThreads / group, 15));
+    // the places hold the groups' sums too: 64 bytes a thread
+    const size_t smem = static_cast<size_t>(kBackwardDepth) * (TOKEN_GATE ? 5 : 4) * 16 * group * groups + (!TOKEN_GATE && a.gate ? 4 * a.cols : 0);
+    *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
+    return launch<&block_norm_backward_kernel<TOKEN_GATE>>(*parts, group * groups, 1, smem, s, a, group);
 }
 
 // The blocks' parts added up in order: 32 columns a block, each of its 32 warps takes every 32nd part.  From the shared sum

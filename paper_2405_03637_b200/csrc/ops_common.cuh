@@ -170,29 +170,42 @@ __device__ __forceinline__ float2 floats_of(uint64_t v) {
     return r;
 }
 __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
-#ifdef SCALAR_PAIRS
-    { const float2 x = floats_of(a), y = floats_of(b); const float2 z = floats_of(c); return pair_of(__fmaf_rn(x.x, y.x, z.x), __fmaf_rn(x.y, y.y, z.y)); }
-#endif
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
-#ifdef SCALAR_PAIRS
-    { const float2 x = floats_of(a), y = floats_of(b);  return pair_of(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y)); }
-#endif
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
-#ifdef SCALAR_PAIRS
-    { const float2 x = floats_of(a), y = floats_of(b);  return pair_of(__fmul_rn(x.x, y.x), __fmul_rn(x.y, y.y)); }
-#endif
     uint64_t r;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+
+__device__ __forceinline__ uint64_t pair_of(float v) { return pair_of(v, v); }
+__device__ __forceinline__ uint64_t sub_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// (the assembler may make a product and a sum of it one fma of pairs)
+__device__ __forceinline__ uint64_t bf16_pair(uint32_t word) { return pair_of(bf16_lo(word), bf16_hi(word)); }
+__device__ __forceinline__ uint32_t pack_pair(uint64_t f) {
+    const float2 v = floats_of(f);
+    return pack_bf16(v.x, v.y);
+}
+__device__ __forceinline__ float sum_of(uint64_t f) {
+    const float2 v = floats_of(f);
+    return v.x + v.y;
+}
+// 16 bytes of bfloat16 values as four pairs, and back
+__device__ __forceinline__ void unpack_pairs(const uint4& q, uint64_t (&f)[4]) {
+    f[0] = bf16_pair(q.x); f[1] = bf16_pair(q.y); f[2] = bf16_pair(q.z); f[3] = bf16_pair(q.w);
+}
+__device__ __forceinline__ uint4 pack_pairs(const uint64_t (&f)[4]) { return make_uint4(pack_pair(f[0]), pack_pair(f[1]), pack_pair(f[2]), pack_pair(f[3])); }
 
 __device__ __forceinline__ void unpack8(const uint4& q, float (&f)[8]) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
