@@ -10,6 +10,7 @@
 //
 // All of it is bound by memory: a row of each array is read once and kept in registers through both of its sums.
 // As in the residual norm, y belongs to r before r is rounded for the stream, and the backward pass reads the rounded r.
+#include "bulk_pipe.cuh"
 #include "ops_common.cuh"
 
 namespace collage {
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
                 sum_pre[j] = first ? s : sum_pre[j] + s;
             }
             if (a.sums & kSumPost) {
-                const float s = (a.token_gate ? du : a.beta * d) * n;
+                const float s = (a.token_gate ? d * gate_value(a.activation, gate_of(j)) : d) * n;
                 sum_post[j] = first ? s : sum_post[j] + s;
             }
             if (a.dgate) a.dgate[row * a.lddg + j] = to_bf16(a.beta * d * n * w * gate_slope(a.activation, gate_of(j)));
@@ -499,191 +500,260 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
     }
 }
 
-// Rows of whole vectors in one pass: a block on each SM walks over rows, one at a time for each group of `group_threads`.  A thread owns a
-// vector of columns (two an instruction in pairs): it sends for its own of the next two rows ahead, so that loads go on while a row's two sums are
-// joined, and keeps its columns' sums over rows in registers until the end.
-constexpr int kBackwardDepth = 2, kBackwardThreads = 1024;
+// Fault word of this file's waits; collage_pipeline_fault reports it.
+static __device__ unsigned int g_block_norm_fault = 0;
 
-template <bool TOKEN_GATE>
-__global__ void __launch_bounds__(kBackwardThreads, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads) {
+// Rows of whole vectors in one pass: a block on each SM walks over rows, one at a time for each group of `group_threads`.  A thread of the
+// group brings whole rows into shared memory by bulk copies, several rows ahead, so that the others have nothing to do with loads; each of
+// them owns PER vectors of columns, worked on two elements an instruction, and keeps its columns' sums over rows in registers until the end.
+constexpr int kBackwardThreads = 512, kMaxGroups = 15, kMaxDepth = 4;
+
+template <int PER, bool TOKEN_GATE>
+__global__ void __launch_bounds__(kBackwardThreads, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads, int depth) {
     constexpr int kArrays = TOKEN_GATE ? 5 : 4;
     __shared__ float slots[2][kBackwardThreads / 32];
+    __shared__ alignas(8) uint64_t full[kMaxGroups * kMaxDepth];
     extern __shared__ __align__(16) uint8_t dynamic[];
-    after_previous();
-    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, v = threadIdx.x % group_threads;
+    const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
     const int lane = threadIdx.x & 31, group_warps = group_threads >> 5, warp0 = group * group_warps;
-    const bool mine = v < static_cast<int>(a.cols >> 3);
-    const uint4 none = make_uint4(0, 0, 0, 0), ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-    uint4* places = reinterpret_cast<uint4*>(dynamic) + threadIdx.x;      // [kBackwardDepth][kArrays], blockDim.x apart
-    auto place = [&](int stage, int array) { return places + (stage * kArrays + array) * blockDim.x; };
-    const uint4 qpre = a.pre && mine ? reinterpret_cast<const uint4*>(a.pre)[v] : none;
-    const uint4 qpost = mine ? (a.post ? reinterpret_cast<const uint4*>(a.post)[v] : ones) : none;
-    uint64_t sum_pre[4] = {0, 0, 0, 0}, sum_post[4] = {0, 0, 0, 0};
-    for (int d = 0; d < kBackwardDepth; ++d)
-        for (int k = 0; k < kArrays; ++k) *place(d, k) = none;            // places that no load fills
-    float* channel = reinterpret_cast<float*>(dynamic) + kBackwardDepth * kArrays * 4 * blockDim.x;       // [cols] A(gate), with a gate of channels
-    const bool channels = !TOKEN_GATE && a.gate;
-    if (channels) {
-        for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) channel[j] = gate_value(a.activation, bf16_value(a.gate[j]));
-        __syncthreads();
+    const int vectors = static_cast<int>(a.cols >> 3);
+    const uint32_t row_bytes = static_cast<uint32_t>(a.cols * 2), stage_bytes = kArrays * row_bytes;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < groups * depth; ++i) pipe::mbar_init(&full[i], 1);
+        pipe::mbar_init_fence();
     }
+    __syncthreads();
+    after_previous();
+    uint8_t* stages = dynamic + static_cast<size_t>(group) * depth * stage_bytes;          // of this group: [depth][kArrays] rows
+    // what columns are multiplied by, in floats: pre_weight, and beta * post_weight times A(gate) of a gate of channels; a gate for each token
+    // leaves no room for the second, which is then unpacked for each row
+    float* pre = reinterpret_cast<float*>(dynamic + static_cast<size_t>(groups) * depth * stage_bytes);
+    float* post = pre + a.cols;
+    const bool second = a.post && a.dblock;
     const uint64_t first = blockIdx.x * static_cast<uint64_t>(groups) + group, step = static_cast<uint64_t>(gridDim.x) * groups;
-    auto send_for = [&](uint64_t row, int stage) {
-        if (row < a.rows && mine) {
-            auto copy = [&](int k, const uint16_t* base, uint64_t ld) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(place(stage, k)))),
-                             "l"(reinterpret_cast<const uint4*>(base + row * ld) + v)
-                             : "memory");
-            };
-            if (a.dy) {
-                copy(0, a.dy, a.lddy);
-                copy(1, a.r, a.ldr);
-            }
-            if (a.dr) copy(2, a.dr, a.lddr);
-            copy(3, a.o, a.ldo);
-            if (TOKEN_GATE) copy(4, a.gate, a.ldg);
+    const uint32_t sent_bytes = row_bytes * ((a.dy ? 2 : 0) + (a.dr ? 1 : 0) + 1 + (TOKEN_GATE ? 1 : 0));
+    bool alive = true;
+    auto send_for = [&](uint64_t row, int stage) {             // one thread
+        if (row >= a.rows || !alive) return;
+        uint8_t* to = stages + stage * stage_bytes;
+        uint64_t* bar = &full[group * depth + stage];
+        pipe::mbar_arrive_expect_tx(bar, sent_bytes);
+        if (a.dy) {
+            pipe::bulk_load(to, a.dy + row * a.lddy, row_bytes, bar);
+            pipe::bulk_load(to + row_bytes, a.r + row * a.ldr, row_bytes, bar);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (a.dr) pipe::bulk_load(to + 2 * row_bytes, a.dr + row * a.lddr, row_bytes, bar);
+        pipe::bulk_load(to + 3 * row_bytes, a.o + row * a.ldo, row_bytes, bar);
+        if (TOKEN_GATE) pipe::bulk_load(to + 4 * row_bytes, a.gate + row * a.ldg, row_bytes, bar);
     };
+    if (t == 0)
+        for (int d = 0; d < depth; ++d) send_for(first + d * step, d);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    uint4 qpost[PER];
+    uint64_t sum_pre[PER][4], sum_post[PER][4];
 #pragma unroll
-    for (int d = 0; d < kBackwardDepth; ++d) send_for(first + d * step, d);
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * group_threads;
+        if (TOKEN_GATE) qpost[i] = a.post && v < vectors ? reinterpret_cast<const uint4*>(a.post)[v] : make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) sum_pre[i][p] = sum_post[i][p] = 0;
+    }
+    for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) {
+        pre[j] = a.pre ? bf16_value(a.pre[j]) : 0.0f;
+        if (!TOKEN_GATE) post[j] = a.beta * (a.post ? bf16_value(a.post[j]) : 1.0f) * (a.gate ? gate_value(a.activation, bf16_value(a.gate[j])) : 1.0f);
+    }
+    __syncthreads();
     const float per_col = 1.0f / static_cast<float>(a.cols);
+    auto barrier = [&] {
+        if (group_warps > 1)
+            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
+        else
+            __syncwarp();
+    };
     // over the group; the two sums of a row have slots of their own, so that one barrier each is enough
     auto joined = [&](float s, int which) {
         s = warp_sum(s);
         if (group_warps > 1) {
             if (lane == 0) slots[which][threadIdx.x >> 5] = s;
-            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
+            barrier();
             s = warp_sum(lane < group_warps ? slots[which][warp0 + lane] : 0.0f);
         }
         return s;
     };
     int stage = 0;
-    const bool second = a.post && a.dblock;
+    uint32_t phase = 0;
+    uint64_t gave_up = a.rows;
     float rstd_r = a.dy && first < a.rows ? a.rstd_pre[first] : 0.0f, rstd_o = a.post && first < a.rows ? a.rstd_post[first] : 1.0f;
     for (uint64_t row = first; row < a.rows; row += step) {
         const float next_r = a.dy && row + step < a.rows ? a.rstd_pre[row + step] : 0.0f, next_o = a.post && row + step < a.rows ? a.rstd_post[row + step] : 1.0f;
-        asm volatile("cp.async.wait_group %0;" ::"n"(kBackwardDepth - 1) : "memory");
-        uint64_t n[4] = {0, 0, 0, 0}, d[4] = {0, 0, 0, 0};      // n of the stream, then of the block; the gradient on its way from y to the block
+        // (after a wait that was given up all go on together, without waiting: the barriers below are for all of the group)
+        if (alive && !pipe::mbar_wait(&full[group * depth + stage], phase, 400, &g_block_norm_fault)) {
+            alive = false;
+            gave_up = row;
+        }
+        const uint8_t* here = stages + stage * stage_bytes;
+        auto vector = [&](int array, int i) {
+            const int v = t + i * group_threads;
+            return v < vectors ? reinterpret_cast<const uint4*>(here + array * row_bytes)[v] : none;
+        };
+        auto factors = [&](const float* k, int i, uint64_t (&w)[4]) {
+            const int v = min(t + i * group_threads, vectors - 1);          // (the vectors of columns that are not there are zeros)
+            const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(k)[2 * v], hi = reinterpret_cast<const ulonglong2*>(k)[2 * v + 1];
+            w[0] = lo.x; w[1] = lo.y; w[2] = hi.x; w[3] = hi.y;
+        };
+        uint64_t n[PER][4], d[PER][4];          // n of the stream, then of the block; the gradient on its way from y to the block
         float mean = 0.0f;
         if (a.dy) {
-            uint64_t dy[4], w[4], sum = 0;
-            unpack_pairs(*place(stage, 0), dy);
-            unpack_pairs(*place(stage, 1), n);
-            unpack_pairs(qpre, w);
+            uint64_t sum = 0;
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                n[p] = mul_pair(n[p], pair_of(rstd_r));
-                sum_pre[p] = fma_pair(dy[p], n[p], sum_pre[p]);
-                d[p] = mul_pair(dy[p], w[p]);
-                sum = fma_pair(d[p], n[p], sum);
+            for (int i = 0; i < PER; ++i) {
+                uint64_t dy[4], w[4];
+                unpack_pairs(vector(0, i), dy);
+                unpack_pairs(vector(1, i), n[i]);
+                factors(pre, i, w);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    n[i][p] = mul_pair(n[i][p], pair_of(rstd_r));
+                    sum_pre[i][p] = fma_pair(dy[p], n[i][p], sum_pre[i][p]);
+                    d[i][p] = mul_pair(dy[p], w[p]);
+                    sum = fma_pair(d[i][p], n[i][p], sum);
+                }
             }
             mean = joined(sum_of(sum), 0) * per_col;
         }
-        uint64_t sum = 0, dr[4] = {0, 0, 0, 0}, w[4];
-        if (a.dr) unpack_pairs(*place(stage, 2), dr);
+        uint64_t sum = 0;
 #pragma unroll
-        for (int p = 0; p < 4; ++p) d[p] = a.dy ? fma_pair(fma_pair(n[p], pair_of(-mean), d[p]), pair_of(rstd_r), dr[p]) : dr[p];
-        if (a.dx && mine) {
-            uint64_t dx[4];
+        for (int i = 0; i < PER; ++i) {
+            const int v = t + i * group_threads;
+            uint64_t dr[4] = {0, 0, 0, 0};
+            if (a.dr) unpack_pairs(vector(2, i), dr);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) dx[p] = mul_pair(d[p], pair_of(a.alpha));
-            reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack_pairs(dx);
-        }
-        unpack_pairs(*place(stage, 3), n);
-        unpack_pairs(qpost, w);
+            for (int p = 0; p < 4; ++p) d[i][p] = a.dy ? fma_pair(fma_pair(n[i][p], pair_of(-mean), d[i][p]), pair_of(rstd_r), dr[p]) : dr[p];
+            if (a.dx && v < vectors) {
+                uint64_t dx[4];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            n[p] = mul_pair(n[p], pair_of(rstd_o));
-            d[p] = mul_pair(d[p], pair_of(a.beta));
-        }
-        if (TOKEN_GATE) {
-            uint64_t g[4], dg[4];
-            unpack_pairs(*place(stage, 4), g);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const float2 gf = floats_of(g[p]);
-                const float2 lo = gate_value_and_slope(a.activation, gf.x), hi = gate_value_and_slope(a.activation, gf.y);
-                dg[p] = mul_pair(mul_pair(mul_pair(d[p], n[p]), w[p]), pair_of(lo.y, hi.y));
-                d[p] = mul_pair(d[p], pair_of(lo.x, hi.x));
-                sum_post[p] = fma_pair(d[p], n[p], sum_post[p]);
+                for (int p = 0; p < 4; ++p) dx[p] = mul_pair(d[i][p], pair_of(a.alpha));
+                reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack_pairs(dx);
             }
-            if (a.dgate && mine) reinterpret_cast<uint4*>(a.dgate + row * a.lddg)[v] = pack_pairs(dg);
-        } else {
+            uint64_t w[4];
+            unpack_pairs(vector(3, i), n[i]);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) sum_post[p] = fma_pair(d[p], n[p], sum_post[p]);
-            if (channels && mine) {
-                const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(channel)[2 * v], hi = reinterpret_cast<const ulonglong2*>(channel)[2 * v + 1];
-                d[0] = mul_pair(d[0], lo.x); d[1] = mul_pair(d[1], lo.y); d[2] = mul_pair(d[2], hi.x); d[3] = mul_pair(d[3], hi.y);
-            }
-        }
-        if (a.dblock) {
-            if (second) {
+            for (int p = 0; p < 4; ++p) n[i][p] = mul_pair(n[i][p], pair_of(rstd_o));
+            if (TOKEN_GATE) {
+                uint64_t g[4];
+                unpack_pairs(vector(4, i), g);
+                unpack_pairs(qpost[i], w);
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    d[p] = mul_pair(d[p], w[p]);
-                    sum = fma_pair(d[p], n[p], sum);
+                    const float2 gf = floats_of(g[p]);
+                    const float2 lo = gate_value_and_slope(a.activation, gf.x), hi = gate_value_and_slope(a.activation, gf.y);
+                    const uint64_t gated = mul_pair(d[i][p], pair_of(lo.x, hi.x));
+                    sum_post[i][p] = fma_pair(gated, n[i][p], sum_post[i][p]);
+                    w[p] = mul_pair(w[p], pair_of(a.beta));
+                    g[p] = mul_pair(mul_pair(mul_pair(d[i][p], w[p]), n[i][p]), pair_of(lo.y, hi.y));
+                    d[i][p] = mul_pair(gated, w[p]);
                 }
-                mean = joined(sum_of(sum), 1) * per_col;
+                if (a.dgate && v < vectors) reinterpret_cast<uint4*>(a.dgate + row * a.lddg)[v] = pack_pairs(g);
+            } else {
+                factors(post, i, w);
 #pragma unroll
-                for (int p = 0; p < 4; ++p) d[p] = mul_pair(fma_pair(n[p], pair_of(-mean), d[p]), pair_of(rstd_o));
+                for (int p = 0; p < 4; ++p) {
+                    sum_post[i][p] = fma_pair(d[i][p], n[i][p], sum_post[i][p]);
+                    d[i][p] = mul_pair(d[i][p], w[p]);
+                }
             }
-            if (mine) reinterpret_cast<uint4*>(a.dblock + row * a.lddo)[v] = pack_pairs(d);
+            if (second) {
+#pragma unroll
+                for (int p = 0; p < 4; ++p) sum = fma_pair(d[i][p], n[i][p], sum);
+            }
         }
-        send_for(row + kBackwardDepth * step, stage);
-        stage = stage + 1 == kBackwardDepth ? 0 : stage + 1;
+        if (second) {
+            mean = joined(sum_of(sum), 1) * per_col;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) d[i][p] = mul_pair(fma_pair(n[i][p], pair_of(-mean), d[i][p]), pair_of(rstd_o));
+        }
+        // All of the group has read the stage: behind the second sum's barrier, or, without one, behind this.  (It parts the slots of one
+        // row's only sum from the next one's, too; of two, each one's barrier does that for the other.)
+        if (!(second && a.dy) || group_warps == 1) barrier();
+        if (t == 0) send_for(row + depth * step, stage);
+        if (a.dblock) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (t + i * group_threads < vectors) reinterpret_cast<uint4*>(a.dblock + row * a.lddo)[t + i * group_threads] = pack_pairs(d[i]);
+        }
+        if (++stage == depth) { stage = 0; phase ^= 1; }
         rstd_r = next_r;
         rstd_o = next_o;
-        // (of two sums, each one's barrier parts the other's slots between rows; one alone needs a second barrier)
-        if (group_warps > 1 && (a.dy != nullptr) != second) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(group_threads) : "memory");
     }
+    if (!alive && t == 0)                       // the copies that are still under way
+        for (uint64_t row = gave_up, it = (gave_up - first) / step, end = it + depth; row < a.rows && it < end; row += step, ++it)
+            pipe::mbar_wait(&full[group * depth + it % depth], it / depth & 1u, 401, &g_block_norm_fault);
     if (!a.sums) return;
     // the block's groups in order, then one row of partial sums a block
-    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    ulonglong2* shared_sums = reinterpret_cast<ulonglong2*>(dynamic);         // [groups][4] for each vector: pairs of both sums
-    if (group > 0 && mine) {
-        ulonglong2* to = shared_sums + (static_cast<uint64_t>(group) * group_threads + v) * 4;
-        to[0] = make_ulonglong2(sum_pre[0], sum_pre[1]);
-        to[1] = make_ulonglong2(sum_pre[2], sum_pre[3]);
-        to[2] = make_ulonglong2(sum_post[0], sum_post[1]);
-        to[3] = make_ulonglong2(sum_post[2], sum_post[3]);
+    ulonglong2* shared_sums = reinterpret_cast<ulonglong2*>(dynamic);         // [groups][PER][group_threads][4]: pairs of both sums
+    auto part = [&](int g, int i) { return shared_sums + ((static_cast<size_t>(g) * PER + i) * group_threads + t) * 4; };
+    if (group > 0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            ulonglong2* to = part(group, i);
+            to[0] = make_ulonglong2(sum_pre[i][0], sum_pre[i][1]);
+            to[1] = make_ulonglong2(sum_pre[i][2], sum_pre[i][3]);
+            to[2] = make_ulonglong2(sum_post[i][0], sum_post[i][1]);
+            to[3] = make_ulonglong2(sum_post[i][2], sum_post[i][3]);
+        }
     }
     __syncthreads();
-    if (group > 0 || !mine) return;
-    for (int g = 1; g < groups; ++g) {
-        const ulonglong2* from = shared_sums + (static_cast<uint64_t>(g) * group_threads + v) * 4;
-        sum_pre[0] = add_pair(sum_pre[0], from[0].x); sum_pre[1] = add_pair(sum_pre[1], from[0].y);
-        sum_pre[2] = add_pair(sum_pre[2], from[1].x); sum_pre[3] = add_pair(sum_pre[3], from[1].y);
-        sum_post[0] = add_pair(sum_post[0], from[2].x); sum_post[1] = add_pair(sum_post[1], from[2].y);
-        sum_post[2] = add_pair(sum_post[2], from[3].x); sum_post[3] = add_pair(sum_post[3], from[3].y);
+    if (group > 0) return;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int v = t + i * group_threads;
+        if (v >= vectors) continue;
+        for (int g = 1; g < groups; ++g) {
+            const ulonglong2* from = part(g, i);
+            sum_pre[i][0] = add_pair(sum_pre[i][0], from[0].x); sum_pre[i][1] = add_pair(sum_pre[i][1], from[0].y);
+            sum_pre[i][2] = add_pair(sum_pre[i][2], from[1].x); sum_pre[i][3] = add_pair(sum_pre[i][3], from[1].y);
+            sum_post[i][0] = add_pair(sum_post[i][0], from[2].x); sum_post[i][1] = add_pair(sum_post[i][1], from[2].y);
+            sum_post[i][2] = add_pair(sum_post[i][2], from[3].x); sum_post[i][3] = add_pair(sum_post[i][3], from[3].y);
+        }
+        ulonglong2* out = reinterpret_cast<ulonglong2*>(a.partial + 2ull * blockIdx.x * a.cols + v * 8);
+        out[0] = make_ulonglong2(sum_pre[i][0], sum_pre[i][1]);
+        out[1] = make_ulonglong2(sum_pre[i][2], sum_pre[i][3]);
+        out = reinterpret_cast<ulonglong2*>(a.partial + (2ull * blockIdx.x + 1) * a.cols + v * 8);
+        out[0] = make_ulonglong2(sum_post[i][0], sum_post[i][1]);
+        out[1] = make_ulonglong2(sum_post[i][2], sum_post[i][3]);
     }
-    ulonglong2* out = reinterpret_cast<ulonglong2*>(a.partial + 2ull * blockIdx.x * a.cols + v * 8);
-    out[0] = make_ulonglong2(sum_pre[0], sum_pre[1]);
-    out[1] = make_ulonglong2(sum_pre[2], sum_pre[3]);
-    out = reinterpret_cast<ulonglong2*>(a.partial + (2ull * blockIdx.x + 1) * a.cols + v * 8);
-    out[0] = make_ulonglong2(sum_post[0], sum_post[1]);
-    out[1] = make_ulonglong2(sum_post[2], sum_post[3]);
 }
 
-// Rows of up to 256 columns are a warp's, without barriers.
+template <int PER, bool TOKEN_GATE>
+static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
+    const uint64_t v = a.cols >> 3;
+    const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), most = std::max(1, std::min(kBackwardThreads / group, kMaxGroups));
+    // few rows: as many groups as give every SM some
+    const int groups = static_cast<int>(std::max<uint64_t>(1, std::min<uint64_t>(most, (a.rows + sm_count - 1) / sm_count)));
+    const size_t row = (TOKEN_GATE ? 5 : 4) * 2 * a.cols, factors = (TOKEN_GATE ? 4 : 8) * a.cols;
+    const int depth = static_cast<int>(std::min<size_t>(kMaxDepth, (210 * 1024 - factors) / (row * groups)));
+    // the stages hold the groups' sums in the end: 64 PER bytes a thread
+    const size_t smem = std::max<size_t>(depth * row * groups, 64ull * PER * group * groups) + factors;
+    *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
+    return launch<&block_norm_backward_kernel<PER, TOKEN_GATE>>(*parts, group * groups, 1, smem, s, a, group, depth);
+}
+// Rows of up to 256 columns are a warp's, without barriers; longer ones take two vectors a thread.
 template <bool TOKEN_GATE>
 static collage_status_t launch_block_backward(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
-    const uint64_t v = a.cols >> 3;
-    const int group = static_cast<int>((v + 31) / 32 * 32), groups = std::max(1, std::min(kBackwardThreads / group, 15));
-    // the places hold the groups' sums too: 64 bytes a thread
-    const size_t smem = static_cast<size_t>(kBackwardDepth) * (TOKEN_GATE ? 5 : 4) * 16 * group * groups + (!TOKEN_GATE && a.gate ? 4 * a.cols : 0);
-    *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
-    return launch<&block_norm_backward_kernel<TOKEN_GATE>>(*parts, group * groups, 1, smem, s, a, group);
+    return a.cols <= 256 ? launch_block_backward_as<1, TOKEN_GATE>(a, parts, sm_count, s) : launch_block_backward_as<2, TOKEN_GATE>(a, parts, sm_count, s);
 }
 
 // The blocks' parts added up in order: 32 columns a block, each of its 32 warps takes every 32nd part.  From the shared sum
-// S = sum u n: dpost = A S and dgate = A' w S for a gate of channels, dpost = S otherwise.
+// S = beta sum D n: dpost = A S and dgate = A' w S for a gate of channels; otherwise the gate is in the sum and dpost = S.
 struct BlockNormFinishArgs {
     const float* partial;
     const uint16_t *gate, *post;          // gate: of channels, or null
     uint16_t *dpre, *dpost, *dgate;
     uint64_t cols;
+    float beta;
     int parts, activation;
 };
 constexpr int kBlockFinish = 1024;
@@ -707,6 +777,7 @@ __global__ void __launch_bounds__(kBlockFinish) block_norm_finish_kernel(const _
         a.dpre[out] = to_bf16(sum);
         return;
     }
+    sum *= a.beta;
     const float g = a.gate ? bf16_value(a.gate[out]) : 1.0f;
     if (a.dpost) a.dpost[out] = to_bf16(a.gate ? gate_value(a.activation, g) * sum : sum);
     if (a.dgate) a.dgate[out] = to_bf16((a.post ? bf16_value(a.post[out]) : 1.0f) * sum * gate_slope(a.activation, g));
@@ -733,6 +804,14 @@ collage_status_t check_block_norm(const collage_block_norm_t* in, uint64_t rows,
 }
 bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 }  // namespace
+
+namespace collage {
+cudaError_t read_clear_block_norm_fault(unsigned int* out) {
+    const unsigned int zero = 0;
+    const cudaError_t e = cudaMemcpyFromSymbol(out, g_block_norm_fault, sizeof *out);
+    return e != cudaSuccess || *out == 0 ? e : cudaMemcpyToSymbol(g_block_norm_fault, &zero, sizeof zero);
+}
+}  // namespace collage
 
 extern "C" {
 
@@ -889,6 +968,7 @@ collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, con
     f.dpost = static_cast<uint16_t*>(dpost_weight);
     f.dgate = channel_grad ? static_cast<uint16_t*>(dgate->data) : nullptr;
     f.cols = cols;
+    f.beta = a.beta;
     f.parts = static_cast<int>(parts);
     f.activation = in->activation;
     const uint32_t column_blocks = static_cast<uint32_t>((cols + 31) / 32);

@@ -780,6 +780,7 @@ namespace collage {
 cudaError_t read_clear_fault32(unsigned int* out);
 cudaError_t read_clear_product_fault(unsigned int* out);
 cudaError_t read_clear_adam_fault(unsigned int* out);
+cudaError_t read_clear_block_norm_fault(unsigned int* out);
 }
 using namespace collage;
 
@@ -1188,13 +1189,14 @@ uint64_t collage_plan_num_chunks(const collage_plan_t* plan) { return plan ? pla
 
 collage_status_t collage_pipeline_fault(uint32_t* out_host) {
     if (!out_host) return COLLAGE_ERR_NULL;
-    unsigned int v = 0, v32 = 0, vp = 0, va = 0, zero = 0;
+    unsigned int v = 0, v32 = 0, vp = 0, va = 0, vb = 0, zero = 0;
     if (cudaMemcpyFromSymbol(&v, g_pipeline_fault, sizeof v) != cudaSuccess) return COLLAGE_ERR_CUDA;
     if (v && cudaMemcpyToSymbol(g_pipeline_fault, &zero, sizeof zero) != cudaSuccess) return COLLAGE_ERR_CUDA;
     if (read_clear_fault32(&v32) != cudaSuccess) return COLLAGE_ERR_CUDA;    // the float comparator's pipeline
     if (read_clear_product_fault(&vp) != cudaSuccess) return COLLAGE_ERR_CUDA;   // the feed-forward products' pipeline
     if (read_clear_adam_fault(&va) != cudaSuccess) return COLLAGE_ERR_CUDA;      // the multi-tensor AdamW step's
-    *out_host = v ? v : v32 ? v32 : vp ? vp : va;
+    if (read_clear_block_norm_fault(&vb) != cudaSuccess) return COLLAGE_ERR_CUDA;
+    *out_host = v ? v : v32 ? v32 : vp ? vp : va ? va : vb;
     return COLLAGE_OK;
 }
 
