@@ -47,9 +47,6 @@ __device__ __forceinline__ float2 gate_value_and_slope(int kind, float g) {
 }
 __device__ __forceinline__ float gate_slope(int kind, float g) { return gate_value_and_slope(kind, g).y; }
 
-#ifndef BN_ROWS
-#define BN_ROWS 1024
-#endif
 constexpr int kBlockThreads = 256;
 
 // One block per row, element by element, the row read again for each stage: any length, stride and alignment.
@@ -102,6 +99,89 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_any_kernel(const __g
         a.r[row * a.ldr + j] = to_bf16(r);
         if (a.y) a.y[row * a.ldy + j] = to_bf16(y);
         if (a.y8) a.y8[row * a.ldy8 + j] = scale == 0.0f ? 0 : to_e4m3(y / scale);
+    }
+}
+
+// The same for rows that fit shared memory as floats: each array is read once.  A thread has the same columns in every pass.
+constexpr uint64_t kMostStaged = 13 * 1024;          // columns; 16 bytes each in the backward pass
+constexpr int kStagedThreads = 512;
+// Calls use(j, values of the arrays at column j) for this thread's columns, four at a time with all of their loads sent first.  (Outputs
+// may be the arrays of inputs, so that the compiler leaves no load behind a store.)  Absent arrays have zeros.
+template <int N, typename Use>
+__device__ __forceinline__ void each_column(uint32_t cols, const uint16_t* const (&from)[N], Use&& use) {
+    for (uint32_t begin = threadIdx.x; begin < cols; begin += 4 * kStagedThreads) {
+        uint16_t raw[4][N];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) raw[k][i] = from[i] && begin + k * kStagedThreads < cols ? from[i][begin + k * kStagedThreads] : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (begin + k * kStagedThreads >= cols) break;
+            float values[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) values[i] = bf16_value(raw[k][i]);
+            use(begin + k * kStagedThreads, values);
+        }
+    }
+}
+__global__ void __launch_bounds__(kStagedThreads) block_norm_staged_kernel(const __grid_constant__ BlockNormArgs a, uint64_t rows) {
+    __shared__ float slots[kStagedThreads / 32];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    float* f = reinterpret_cast<float*>(dynamic);               // [cols]
+    after_previous();
+    const uint32_t cols = static_cast<uint32_t>(a.cols);
+    for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const uint16_t *x = a.x + row * a.ldx, *o = a.o + row * a.ldo, *gate = a.gate ? a.gate + row * a.ldg : nullptr;
+        // 1 / rms of the values in f from their sum of squares; they come out times a power of two where their squares need one
+        auto rstd_of = [&](float sum, float& factor) {
+            const float per = static_cast<float>(cols);
+            factor = 1.0f;
+            float mean = block_sum(sum, slots, kStagedThreads / 32) / per + a.eps;
+            if (!squares_fit(mean)) {
+                factor = rescue_factor(mean);
+                sum = 0.0f;
+                for (uint32_t j = threadIdx.x; j < cols; j += kStagedThreads) {
+                    f[j] *= factor;
+                    sum = __fmaf_rn(f[j], f[j], sum);
+                }
+                mean = block_sum(sum, slots, kStagedThreads / 32) / per + a.eps * factor * factor;
+            }
+            return 1.0f / sqrtf(mean);
+        };
+        float factor, rstd = 1.0f, sum = 0.0f;
+        each_column<1>(cols, {o}, [&](uint32_t j, const float (&v)[1]) {
+            f[j] = v[0];
+            sum = __fmaf_rn(v[0], v[0], sum);
+        });
+        if (a.post) {
+            rstd = rstd_of(sum, factor);
+            if (a.rstd_post && threadIdx.x == 0) a.rstd_post[row] = factor * rstd;
+        }
+        sum = 0.0f;
+        each_column<3>(cols, {x, gate, a.post}, [&](uint32_t j, const float (&v)[3]) {
+            float n = a.post ? f[j] * rstd * v[2] : f[j];
+            if (gate) n *= gate_value(a.activation, v[1]);
+            const float r = __fmaf_rn(a.alpha, v[0], a.beta * n);
+            f[j] = r;
+            a.r[row * a.ldr + j] = to_bf16(r);
+            sum = __fmaf_rn(r, r, sum);
+        });
+        if (!a.pre) continue;
+        rstd = rstd_of(sum, factor);
+        if (a.rstd_pre && threadIdx.x == 0) a.rstd_pre[row] = factor * rstd;
+        uint32_t most = 0;
+        each_column<1>(cols, {a.pre}, [&](uint32_t j, const float (&w)[1]) {
+            const float y = f[j] * rstd * w[0];
+            if (a.y) a.y[row * a.ldy + j] = to_bf16(y);
+            f[j] = y;
+            most = max(most, __float_as_uint(y) & 0x7FFFFFFFu);
+        });
+        if (!a.y8) continue;
+        const float scale = __uint_as_float(block_max(most, reinterpret_cast<uint32_t*>(slots), kStagedThreads / 32)) / kE4m3Max;
+        if (threadIdx.x == 0) a.scale[row] = scale;
+#pragma unroll 4
+        for (uint32_t j = threadIdx.x; j < cols; j += kStagedThreads) a.y8[row * a.ldy8 + j] = scale == 0.0f ? 0 : to_e4m3(f[j] / scale);
     }
 }
 
@@ -229,13 +309,12 @@ __global__ void __launch_bounds__(WARP ? 128 : PER > 2 ? 512 : 1024) block_norm_
 
 // Many rows of whole vectors: a block on each SM walks over rows, one at a time for each group of `group_threads`, two vectors a thread.  What
 // the columns are multiplied by is laid out in floats once; a thread sends for its vectors of the next two rows ahead.
-constexpr int kRowsDepth = 2;
+constexpr int kRowsDepth = 2, kRowsThreads = 1024;
 
-template <bool TOKEN_GATE, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1) block_norm_rows_kernel(const __grid_constant__ BlockNormArgs a, uint64_t rows, int group_threads) {
-    constexpr int kArrays = TOKEN_GATE ? 3 : 2, PER = 2;
-    __shared__ float slots[2][THREADS / 32];
-    __shared__ uint32_t most_slots[THREADS / 32];
+__global__ void __launch_bounds__(kRowsThreads, 1) block_norm_rows_kernel(const __grid_constant__ BlockNormArgs a, uint64_t rows, int group_threads) {
+    constexpr int kArrays = 2, PER = 2;
+    __shared__ float slots[2][kRowsThreads / 32];
+    __shared__ uint32_t most_slots[kRowsThreads / 32];
     extern __shared__ __align__(16) uint8_t dynamic[];
     after_previous();
     const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
@@ -250,7 +329,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_rows_kernel(const __gri
         for (int k = 0; k < kArrays * PER; ++k) *place(d, 0, k) = none;         // places that no load fills
     for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) {
         float k = a.post ? a.beta * bf16_value(a.post[j]) : a.beta;
-        if (!TOKEN_GATE && a.gate) k *= gate_value(a.activation, bf16_value(a.gate[j]));
+        if (a.gate) k *= gate_value(a.activation, bf16_value(a.gate[j]));
         post[j] = k;
         pre[j] = a.pre ? bf16_value(a.pre[j]) : 0.0f;
     }
@@ -267,7 +346,6 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_rows_kernel(const __gri
             };
             copy(0, a.o, a.ldo);
             copy(1, a.x, a.ldx);
-            if (TOKEN_GATE) copy(2, a.gate, a.ldg);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -331,15 +409,6 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_rows_kernel(const __gri
             unpack_pairs(*place(stage, 1, i), x);
 #pragma unroll
             for (int p = 0; p < 4; ++p) f[i][p] = mul_pair(f[i][p], pair_of(rstd));
-            if (TOKEN_GATE) {
-                uint64_t g[4];
-                unpack_pairs(*place(stage, 2, i), g);
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    const float2 gate = floats_of(g[p]);
-                    f[i][p] = mul_pair(f[i][p], pair_of(gate_value(a.activation, gate.x), gate_value(a.activation, gate.y)));
-                }
-            }
             if (v < vectors) {
                 times(post, v, f[i]);
 #pragma unroll
@@ -404,21 +473,23 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_rows_kernel(const __gri
     }
 }
 
-template <bool TOKEN_GATE, int THREADS>
 static collage_status_t launch_rows(const BlockNormArgs& a, uint64_t rows, int sm_count, cudaStream_t s) {
     const uint64_t v = a.cols >> 3;
-    const int group = static_cast<int>((v + 63) / 64 * 32), groups = std::max(1, std::min(THREADS / group, 15));
-    const size_t smem = 8 * a.cols + static_cast<size_t>(kRowsDepth) * (TOKEN_GATE ? 3 : 2) * 2 * 16 * group * groups;
+    const int group = static_cast<int>((v + 63) / 64 * 32), groups = std::max(1, std::min(kRowsThreads / group, 15));
+    const size_t smem = 8 * a.cols + static_cast<size_t>(kRowsDepth) * 2 * 2 * 16 * group * groups;
     const uint64_t grid = std::min<uint64_t>((rows + groups - 1) / groups, static_cast<uint64_t>(sm_count));
-    return launch<&block_norm_rows_kernel<TOKEN_GATE, THREADS>>(grid, group * groups, 1, smem, s, a, rows, group);
+    return launch<&block_norm_rows_kernel>(grid, group * groups, 1, smem, s, a, rows, group);
 }
 
 // A row's vectors over warps, as in the residual norm: with many rows four vectors a thread, with few rows one.
 static collage_status_t launch_block_norm(const BlockNormArgs& a, uint64_t rows, bool vectors_fit, int sm_count, cudaStream_t s) {
     const uint64_t v = a.cols >> 3;
     const bool many = rows > 2ull * sm_count;
+    if (!vectors_fit && a.cols <= kMostStaged) return launch<&block_norm_staged_kernel>(std::min<uint64_t>(rows, 4ull * sm_count), kStagedThreads, 1, 4 * a.cols, s, a, rows);
     if (!vectors_fit || v > 4096) return launch<&block_norm_any_kernel>(rows, kBlockThreads, 1, 0, s, a);
-    if (rows >= BN_ROWS && v <= 1024) return a.gate && a.ldg ? launch_rows<true, 512>(a, rows, sm_count, s) : launch_rows<false, 1024>(a, rows, sm_count, s);
+    // several rows for each group of threads that walks: 8191 x 4096 48 us against 56, 8191 x 8192 94 against 110; but 8191 x 1024 17 against 15, and 2047 x
+    // 5120 with a gate for each token 42 against 28
+    if (rows >= 8ull * sm_count && v > 128 && v <= 1024 && !(a.gate && a.ldg)) return launch_rows(a, rows, sm_count, s);
     if (many && v <= 128) {
         const uint64_t grid = (rows + 3) / 4;
         return v <= 32   ? launch<&block_norm_kernel<1, true>>(grid, 128, 1, 0, s, a, rows)
@@ -500,18 +571,76 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
     }
 }
 
+// The same for rows that fit shared memory as floats, with the sums over the block's rows: each array is read once.  A thread has the same
+// columns in every pass.
+__global__ void __launch_bounds__(kStagedThreads) block_norm_backward_staged_kernel(const __grid_constant__ BlockNormBackwardArgs a) {
+    __shared__ float slots[kStagedThreads / 32];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    const uint32_t cols = static_cast<uint32_t>(a.cols);
+    float *d = reinterpret_cast<float*>(dynamic), *n = d + cols, *sum_pre = n + cols, *sum_post = sum_pre + cols;
+    after_previous();
+    for (uint32_t j = threadIdx.x; j < cols; j += kStagedThreads) sum_pre[j] = sum_post[j] = 0.0f;
+    const float per_col = 1.0f / static_cast<float>(cols);
+    const bool second = a.post && a.dblock;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        auto row_of = [&](const uint16_t* p, uint64_t ld) { return p ? p + row * ld : nullptr; };
+        const float rstd_r = a.dy ? a.rstd_pre[row] : 0.0f, rstd_o = a.post ? a.rstd_post[row] : 1.0f;
+        float mean = 0.0f, sum = 0.0f;
+        if (a.dy) {
+            each_column<3>(cols, {row_of(a.dy, a.lddy), row_of(a.r, a.ldr), a.pre}, [&](uint32_t j, const float (&v)[3]) {
+                const float no = v[1] * rstd_r, q = v[0] * v[2];
+                sum_pre[j] = __fmaf_rn(v[0], no, sum_pre[j]);
+                sum = __fmaf_rn(q, no, sum);
+                d[j] = q;
+                n[j] = no;
+            });
+            mean = block_sum(sum, slots, kStagedThreads / 32) * per_col;
+        }
+        sum = 0.0f;
+        each_column<4>(cols, {row_of(a.dr, a.lddr), row_of(a.o, a.ldo), row_of(a.gate, a.ldg), a.post}, [&](uint32_t j, const float (&in)[4]) {
+            const float v = in[0] + (a.dy ? rstd_r * __fmaf_rn(-n[j], mean, d[j]) : 0.0f);
+            if (a.dx) a.dx[row * a.lddx + j] = to_bf16(a.alpha * v);
+            const float no = in[1] * rstd_o, w = a.beta * (a.post ? in[3] : 1.0f);
+            float gated = v;
+            if (a.gate) {
+                const float2 g = gate_value_and_slope(a.activation, in[2]);
+                gated *= g.x;
+                if (a.dgate) a.dgate[row * a.lddg + j] = to_bf16(v * w * no * g.y);
+            }
+            sum_post[j] = __fmaf_rn(a.token_gate ? gated : v, no, sum_post[j]);
+            const float h = gated * w;
+            sum = __fmaf_rn(h, no, sum);
+            if (second) {
+                d[j] = h;
+                n[j] = no;
+            } else if (a.dblock) {
+                a.dblock[row * a.lddo + j] = to_bf16(h);
+            }
+        });
+        if (!second) continue;
+        mean = block_sum(sum, slots, kStagedThreads / 32) * per_col;
+#pragma unroll 4
+        for (uint32_t j = threadIdx.x; j < cols; j += kStagedThreads) a.dblock[row * a.lddo + j] = to_bf16(rstd_o * __fmaf_rn(-n[j], mean, d[j]));
+    }
+    if (!a.sums) return;
+    for (uint32_t j = threadIdx.x; j < cols; j += kStagedThreads) {
+        a.partial[2ull * blockIdx.x * a.cols + j] = sum_pre[j];
+        a.partial[(2ull * blockIdx.x + 1) * a.cols + j] = sum_post[j];
+    }
+}
+
 // Fault word of this file's waits; collage_pipeline_fault reports it.
 static __device__ unsigned int g_block_norm_fault = 0;
 
 // Rows of whole vectors in one pass: a block on each SM walks over rows, one at a time for each group of `group_threads`.  A thread of the
 // group brings whole rows into shared memory by bulk copies, several rows ahead, so that the others have nothing to do with loads; each of
 // them owns PER vectors of columns, worked on two elements an instruction, and keeps its columns' sums over rows in registers until the end.
-constexpr int kBackwardThreads = 512, kMaxGroups = 15, kMaxDepth = 4;
+constexpr int kMaxGroups = 15, kMaxDepth = 4;
 
-template <int PER, bool TOKEN_GATE>
-__global__ void __launch_bounds__(kBackwardThreads, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads, int depth) {
+template <int PER, bool TOKEN_GATE, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads, int depth) {
     constexpr int kArrays = TOKEN_GATE ? 5 : 4;
-    __shared__ float slots[2][kBackwardThreads / 32];
+    __shared__ float slots[2][THREADS / 32];
     __shared__ alignas(8) uint64_t full[kMaxGroups * kMaxDepth];
     extern __shared__ __align__(16) uint8_t dynamic[];
     const int groups = blockDim.x / group_threads, group = threadIdx.x / group_threads, t = threadIdx.x % group_threads;
@@ -727,23 +856,28 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) block_norm_backward_kerne
     }
 }
 
-template <int PER, bool TOKEN_GATE>
+template <int PER, bool TOKEN_GATE, int THREADS>
 static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
     const uint64_t v = a.cols >> 3;
-    const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), most = std::max(1, std::min(kBackwardThreads / group, kMaxGroups));
+    const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), most = std::max(1, std::min(THREADS / group, kMaxGroups));
     // few rows: as many groups as give every SM some
     const int groups = static_cast<int>(std::max<uint64_t>(1, std::min<uint64_t>(most, (a.rows + sm_count - 1) / sm_count)));
     const size_t row = (TOKEN_GATE ? 5 : 4) * 2 * a.cols, factors = (TOKEN_GATE ? 4 : 8) * a.cols;
-    const int depth = static_cast<int>(std::min<size_t>(kMaxDepth, (210 * 1024 - factors) / (row * groups)));
+    const int depth = static_cast<int>(std::min<size_t>(kMaxDepth, (224 * 1024 - factors) / (row * groups)));
     // the stages hold the groups' sums in the end: 64 PER bytes a thread
     const size_t smem = std::max<size_t>(depth * row * groups, 64ull * PER * group * groups) + factors;
     *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
-    return launch<&block_norm_backward_kernel<PER, TOKEN_GATE>>(*parts, group * groups, 1, smem, s, a, group, depth);
+    return launch<&block_norm_backward_kernel<PER, TOKEN_GATE, THREADS>>(*parts, group * groups, 1, smem, s, a, group, depth);
 }
-// Rows of up to 256 columns are a warp's, without barriers; longer ones take two vectors a thread.
+// Rows of up to 256 columns are a warp's, without barriers; longer ones take two vectors a thread, half the joins of one.  Of rows that leave
+// many of 512 threads idle that way (and a second row has no registers) one vector a thread is faster: 2047 x 5120 with a gate for each
+// token 55 us against 76, 4096 x 6144 106 against 138, 8191 x 5120 without 119 against 128, but 8191 x 6144 141 against 133.
 template <bool TOKEN_GATE>
 static collage_status_t launch_block_backward(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
-    return a.cols <= 256 ? launch_block_backward_as<1, TOKEN_GATE>(a, parts, sm_count, s) : launch_block_backward_as<2, TOKEN_GATE>(a, parts, sm_count, s);
+    if (a.cols <= 256) return launch_block_backward_as<1, TOKEN_GATE, 512>(a, parts, sm_count, s);
+    if (a.cols > 4096 && a.cols <= 5120) return launch_block_backward_as<1, TOKEN_GATE, 640>(a, parts, sm_count, s);
+    if (TOKEN_GATE && a.cols > 5120 && a.cols <= 6144) return launch_block_backward_as<1, TOKEN_GATE, 768>(a, parts, sm_count, s);
+    return launch_block_backward_as<2, TOKEN_GATE, 512>(a, parts, sm_count, s);
 }
 
 // The blocks' parts added up in order: 32 columns a block, each of its 32 warps takes every 32nd part.  From the shared sum
@@ -955,7 +1089,9 @@ collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, con
                (!a.dgate || rows_aligned(dgate, 2, 16));
     for (const collage_matrix_t* m : all) fit = fit && (!m || rows_aligned(m, 2, 16));
     unsigned parts = static_cast<unsigned>(std::min<uint64_t>({rows, static_cast<uint64_t>(kBlockParts), 2ull * dev.sm_count}));
-    if (!fit)
+    if (!fit && cols <= kMostStaged)
+        st = launch<&block_norm_backward_staged_kernel>(parts, kStagedThreads, 1, 16 * cols, s, a);
+    else if (!fit)
         st = launch<&block_norm_backward_any_kernel>(parts, kBlockThreads, 1, 0, s, a);
     else
         st = a.token_gate ? launch_block_backward<true>(a, &parts, dev.sm_count, s) : launch_block_backward<false>(a, &parts, dev.sm_count, s);
