@@ -7,6 +7,8 @@
 // Rows are taken relative to their largest logit before the division by t, as in distillation.  What a row's loss needs besides is a
 // handful of scalars, which one thread computes in 64 bits: a log-probability of -10 in float would leave the ratio and the KL term
 // (a difference of nearly equal numbers) only five digits.
+#include <limits>
+
 #include "logits_row.cuh"
 #include "umma.cuh"
 
@@ -25,7 +27,7 @@ struct TokenArgs {
     float *logp, *stats, *loss, *kl;
     uint64_t ldz, ldd;
     double inv_t;
-    float c, inv_tf;                             // log2(e) / t, 1 / t
+    float c, c_rest, inv_tf;                     // log2(e) / t and what it lacks, 1 / t
     float clip_low, clip_high, kl_weight;        // bounds of the ratio
     uint32_t vocab, slice, cluster;              // slice: 16-byte vectors of a row for one block; cluster: blocks of a row
     int target_bytes;
@@ -56,6 +58,21 @@ __device__ __forceinline__ PolicyRow policy_row(const TokenArgs& a, uint64_t row
         }
     }
     return {w * loss, kl, w * coef};
+}
+
+// Adds exp((f - m) / t) over a vector to `total`, with log2(e) / t in two floats: what the first one lacks would shift the log-probabilities of
+// all tokens the same way, which a sequence's sum adds up.
+template <typename T>
+__device__ __forceinline__ void add_exact_exps(const uint4& q, float m, const TokenArgs& a, uint64_t& total) {
+    uint64_t f[Vec<T>::kPairs];
+    Vec<T>::unpack(q, f);
+    const float minus_m = m == -INFINITY ? 0.0f : -m;
+#pragma unroll
+    for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
+        const uint64_t d = add_pair(f[i], pair_of(minus_m));
+        const float2 x = floats_of(fma_pair(d, pair_of(a.c), mul_pair(d, pair_of(a.c_rest))));
+        total = add_pair(total, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+    }
 }
 
 struct TokenShared {
@@ -148,7 +165,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
                 m = to;
             }
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i) add_exps<T, false>(q[i], m, a.c, total);
+            for (uint32_t i = 0; i < kAhead; ++i) add_exact_exps<T>(q[i], m, a, total);
         };
         for (uint32_t v = whole + threadIdx.x; v < whole_end; v += THREADS * kAhead) {
             uint4 q[kAhead];
@@ -232,6 +249,10 @@ static collage_status_t launch_token(TokenArgs& a, uint64_t rows, collage_dtype_
     a.cluster = 1;
     // few rows: more blocks for each, up to four on an SM in all and down to 512 vectors each
     while (a.cluster < kTokenCluster && rows * a.cluster * 2 <= 4ull * sm_count && vectors / a.cluster >= 1024) a.cluster *= 2;
+    // Rows that are read twice: as many blocks for each as keep all rows under way in L2 (five blocks an SM).  1024 x 131072: 147 us without,
+    // 120 with four each; 4096 x 32000 in float 234 and 202.  Of shorter rows more blocks cost more than they save (2049 x 50257: 95 and 100).
+    if (MODE == kPolicy)
+        while (a.cluster < kTokenCluster && 5ull * sm_count / a.cluster * vectors * 16 > (80ull << 20) && vectors / a.cluster >= 1024) a.cluster *= 2;
     a.slice = (vectors + a.cluster - 1) / a.cluster;
     return dtype == COLLAGE_DTYPE_BF16 ? launch_token_as<uint16_t, MODE>(a, rows, s) : launch_token_as<float, MODE>(a, rows, s);
 }
@@ -337,8 +358,10 @@ static collage_status_t prepare_tokens(const collage_tokens_t* in, const RowArra
     if (in->target_bytes != 4 && in->target_bytes != 8) return COLLAGE_ERR_ARG;
     if (!(std::isfinite(in->temperature) && in->temperature > 0.0)) return COLLAGE_ERR_ARG;
     const double inv_t = 1.0 / in->temperature;
-    const float t = static_cast<float>(in->temperature), c = static_cast<float>(inv_t * 1.4426950408889634074);
-    if (!(t > 0.0f && std::isfinite(t) && static_cast<float>(inv_t) > 0.0f && std::isfinite(c))) return COLLAGE_ERR_ARG;
+    // log2(e) / t rounded down, so that what it lacks is above 0: a logit of -infinity, times either, is -infinity
+    const double exact_c = inv_t * 1.4426950408889634074;
+    const float t = static_cast<float>(in->temperature), near_c = static_cast<float>(exact_c), c = near_c < exact_c ? near_c : std::nextafterf(near_c, 0.0f);
+    if (!(t > 0.0f && std::isfinite(t) && static_cast<float>(inv_t) > 0.0f && std::isfinite(near_c) && c > 0.0f)) return COLLAGE_ERR_ARG;
     if (dlogits && !same_shape(dlogits, &in->logits)) return COLLAGE_ERR_ARG;
     collage_status_t st = check_matrix(&in->logits, size);
     if (st == COLLAGE_OK && dlogits) st = check_matrix(dlogits, size);
@@ -371,6 +394,7 @@ static collage_status_t prepare_tokens(const collage_tokens_t* in, const RowArra
     out->inv_t = inv_t;
     out->inv_tf = static_cast<float>(inv_t);
     out->c = c;
+    out->c_rest = std::max(static_cast<float>(exact_c - c), std::numeric_limits<float>::denorm_min());
     return COLLAGE_OK;
 }
 
