@@ -579,9 +579,10 @@ typedef struct collage_tokens {
     double temperature;              /* > 0 and finite, as is 1 / (temperature ln 2), in float (ERR_ARG)    */
 } collage_tokens_t;
 
-/* logp: DEVICE float[rows].  stats: DEVICE float[rows][2], 8-byte aligned, or NULL, for the backward call: the row's largest logit, and the
+/* logp: DEVICE float[rows].  logp_rest: DEVICE float[rows] or NULL: what logp's rounding to float took (up to 2^-24 of it, which a sum over
+ * a sequence adds up).  stats: DEVICE float[rows][2], 8-byte aligned, or NULL, for the backward call: the row's largest logit, and the
  * sum of exp((logit - largest) / temperature) over the row; zeros in rows that are not read. */
-collage_status_t collage_token_logp(const collage_tokens_t* in, float* logp, float* stats, void* stream);
+collage_status_t collage_token_logp(const collage_tokens_t* in, float* logp, float* logp_rest, float* stats, void* stream);
 /* grad_logp: DEVICE float[rows].  dlogits_ij = grad_logp_i / temperature * ([j = y] - exp(logp of token j)): [rows, vocab] in
  * logits_dtype; may be the array of logits.  A row of grad_logp 0 gets zeros whatever its logits are. */
 collage_status_t collage_token_logp_backward(const collage_tokens_t* in, const float* stats, const float* grad_logp,
@@ -608,7 +609,7 @@ collage_status_t collage_policy_loss_and_grad(const collage_tokens_t* in, const 
                                               float* kl, const collage_matrix_t* dlogits, void* stream);
 
 /* Pairs of answers: sequence 2p is the preferred and 2p + 1 the other answer of pair p; sequence s has rows [offsets[s], offsets[s+1]).
- *   S_s = sum over its rows that have a target of (logp - ref_logp), divided by their number (at least 1) if average
+ *   S_s = sum over its rows that have a target of (logp + logp_rest - ref_logp), divided by their number (at least 1) if average
  *   log_ratio_p = S_2p - S_2p+1,   h = beta * log_ratio_p - margin
  *   loss_p = pair_weight_p * (-(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h))
  *   grad_logp = the gradient of sum_p loss_p; 0 in rows without a target and in rows of no sequence.
@@ -616,6 +617,7 @@ collage_status_t collage_policy_loss_and_grad(const collage_tokens_t* in, const 
  * the gradients of rows that several sequences or none would own are undefined).  Sums are in 64 bits and in a fixed order. */
 typedef struct collage_preference {
     const float* logp;               /* DEVICE float[rows]                                                   */
+    const float* logp_rest;          /* DEVICE float[rows] or NULL: zeros                                    */
     const float* ref_logp;           /* DEVICE float[rows] or NULL: zeros                                    */
     const void* target;              /* of collage_tokens_t, with its vocab: which rows count                */
     const void* offsets;             /* DEVICE int32_t or int64_t [2 * pairs + 1] (offset_bytes = 4 or 8)    */

@@ -99,7 +99,7 @@ class Policy(ctypes.Structure):
 
 class Preference(ctypes.Structure):
     """collage_preference_t"""
-    _fields_ = [("logp", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p), ("target", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+    _fields_ = [("logp", ctypes.c_void_p), ("logp_rest", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p), ("target", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
                 ("pair_weight", ctypes.c_void_p), ("rows", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("pairs", ctypes.c_uint64),
                 ("target_bytes", ctypes.c_uint32), ("offset_bytes", ctypes.c_uint32), ("beta", ctypes.c_double), ("margin", ctypes.c_double),
                 ("label_smoothing", ctypes.c_double), ("average", ctypes.c_int)]
@@ -197,7 +197,7 @@ def _declare_operators(L, mp, dp, bp, tp, pp, rp):
     L.collage_block_norm_workspace_bytes.restype = size
     L.collage_block_norm_workspace_bytes.argtypes = [ctypes.c_uint64]
     L.collage_block_norm_backward.argtypes = [bp, mp, mp, mp, vp, vp, mp, mp, mp, vp, vp, vp, size, vp]
-    L.collage_token_logp.argtypes = [tp, vp, vp, vp]
+    L.collage_token_logp.argtypes = [tp, vp, vp, vp, vp]
     L.collage_token_logp_backward.argtypes = [tp, vp, vp, mp, vp]
     L.collage_policy_loss_and_grad.argtypes = [tp, pp, vp, vp, vp, mp, vp]
     L.collage_preference_loss.argtypes = [rp, vp, vp, vp, vp]
@@ -460,7 +460,7 @@ _pack_distill = struct.Struct("iId").pack
 _pack_block_norm = struct.Struct("QQdddi4x").pack      # what follows the matrices in collage_block_norm_t
 _pack_tokens = struct.Struct("QiId").pack              # and in collage_tokens_t
 _pack_policy = struct.Struct("QQQQddd").pack
-_pack_preference = struct.Struct("QQQQQQQQIIdddi4x").pack
+_pack_preference = struct.Struct("QQQQQQQQQIIdddi4x").pack
 _NO_MATRIX = _pack_matrix(0, 0, 0, 0)
 
 
@@ -690,11 +690,12 @@ def _tokens(logits, target, temperature, dev, where):
     return m + _pack_tokens(at, DTYPE_BF16 if dtype is _BF16 else DTYPE_F32, size, temperature), rows
 
 
-def token_logp(logits, target, temperature: float, logp, stats=None, stream=None):
-    """logp[i] = log softmax(logits[i] / temperature)[target[i]], 0 where target[i] is no token; stats [rows, 2] for the backward call."""
+def token_logp(logits, target, temperature: float, logp, stats=None, logp_rest=None, stream=None):
+    """logp[i] = log softmax(logits[i] / temperature)[target[i]], 0 where target[i] is no token; stats [rows, 2] for the backward call;
+    logp_rest: what logp's rounding to float took, for preference_loss."""
     w, (L, dev) = "collage_token_logp", _operators()
     t, n = _tokens(logits, target, temperature, dev, w)
-    _check(L.collage_token_logp(t, _vector(logp, _F32, n, dev, w), _vector(stats, _F32, 2 * n, dev, w), _stream(stream, dev, w)), w)
+    _check(L.collage_token_logp(t, _vector(logp, _F32, n, dev, w), _vector(logp_rest, _F32, n, dev, w), _vector(stats, _F32, 2 * n, dev, w), _stream(stream, dev, w)), w)
 
 
 def token_logp_backward(logits, target, temperature: float, stats, grad_logp, dlogits, stream=None):
@@ -717,8 +718,9 @@ def policy_loss_and_grad(logits, target, temperature: float, advantage, row_weig
 
 
 def preference_loss(logp, target, vocab: int, offsets, beta: float, loss, grad_logp=None, ref_logp=None, pair_weight=None, margin: float = 0.0,
-                    label_smoothing: float = 0.0, average: bool = False, log_ratio=None, stream=None):
-    """loss[p] = -log sigmoid(beta (S_2p - S_2p+1) - margin) of pairs of sequences [offsets[s], offsets[s + 1]) of rows, S summing logp - ref_logp; and grad_logp."""
+                    label_smoothing: float = 0.0, average: bool = False, log_ratio=None, logp_rest=None, stream=None):
+    """loss[p] = -log sigmoid(beta (S_2p - S_2p+1) - margin) of pairs of sequences [offsets[s], offsets[s + 1]) of rows, S summing logp + logp_rest - ref_logp;
+    and grad_logp."""
     w, (L, dev) = "collage_preference_loss", _operators()
     if logp is None or offsets is None:
         raise CollageError(ERR_NULL, w)
@@ -728,7 +730,7 @@ def preference_loss(logp, target, vocab: int, offsets, beta: float, loss, grad_l
     pairs = edges // 2
     at, size = _index(target, rows, dev, w)
     edge, edge_size = _index(offsets, edges, dev, w)
-    p = _pack_preference(_vector(logp, _F32, rows, dev, w), _vector(ref_logp, _F32, rows, dev, w) or 0, at, edge,
+    p = _pack_preference(_vector(logp, _F32, rows, dev, w), _vector(logp_rest, _F32, rows, dev, w) or 0, _vector(ref_logp, _F32, rows, dev, w) or 0, at, edge,
                          _vector(pair_weight, _F32, pairs, dev, w) or 0, rows, vocab, pairs, size, edge_size, beta, margin, label_smoothing, bool(average))
     _check(L.collage_preference_loss(p, _vector(loss, _F32, pairs, dev, w), _vector(log_ratio, _F32, pairs, dev, w), _vector(grad_logp, _F32, rows, dev, w),
                                      _stream(stream, dev, w)), w)

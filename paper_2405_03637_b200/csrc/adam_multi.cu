@@ -35,7 +35,7 @@ struct AdamChunk {
 
 struct AdamScalars {
     Fp32Scalars f;
-    float rate, decay;                         // -a / bc1, -a lam
+    float rate, decay, large;                  // -a / bc1, -a lam, 128 a
     float inv_bc1, inv_bc2, inv_root_bc2;      // 1 / bc1, 1 / bc2, 1 / sqrt(bc2)
     double a, lam;
     uint32_t key;
@@ -111,7 +111,8 @@ __device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g
 
 // (theta, rest) + delta: theta' is the bfloat16 nearest to the sum, rest' what that lacks.  In floats theta + RN(rest + delta) is known as s + lost, to
 // five units of the last place of t = rest + delta.  Where s is that near to half-way between two bfloat16 values the sum is taken in 64 bits
-// instead (settled()): as a rule within a unit or two of s's own last place; within more (64 at most) where theta and t nearly cancel.
+// instead (settled()): as a rule within a unit or two of s's own last place, within more where theta and t nearly cancel.  Sums more than 64 units
+// off half-way are looked at only where the update is larger than any but a few (`large`): elsewhere they are nearly nothing.
 struct PairSum {
     uint64_t s, t, lost;
 };
@@ -119,15 +120,15 @@ __device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, ui
     const uint64_t t = add_pair(rest, delta), s = add_pair(theta, t), back = sub_pair(s, theta);
     return {s, t, add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back))};                  // theta + t = s + lost, exactly
 }
-__device__ __forceinline__ bool is_near(float s, float t) {
-    const int off = static_cast<int>(__float_as_uint(s) & 0xFFFFu) - 0x8000;
-    return abs(off) < 64 && abs(off) * fabsf(s) <= __fmaf_rn(5.0f, fabsf(t), 1.5f * fabsf(s));
+__device__ __forceinline__ bool is_near(float s, float t, float delta, float large) {
+    const int off = abs(static_cast<int>(__float_as_uint(s) & 0xFFFFu) - 0x8000);
+    return (off < 64 || fabsf(delta) > large) && off * fabsf(s) <= __fmaf_rn(5.0f, fabsf(t), 1.5f * fabsf(s));
 }
 __device__ __forceinline__ bool is_near(const PairSum& sum) {
     const float2 s = floats_of(sum.s), t = floats_of(sum.t);
     const uint32_t off = (__byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410) + 0x80408040u) & 0xFF80FF80u;
     if (((off - 0x00010001u) & ~off & 0x80008000u) == 0) return false;           // no half-word within 64 (the lower one's carry allowed for)
-    return is_near(s.x, t.x) || is_near(s.y, t.y);
+    return is_near(s.x, t.x, 0.0f, 0.0f) || is_near(s.y, t.y, 0.0f, 0.0f);
 }
 __device__ __forceinline__ void split_pair(const PairSum& sum, uint32_t& theta_word, uint32_t& rest_word) {
     const float2 s = floats_of(sum.s);
@@ -149,15 +150,15 @@ __device__ __forceinline__ uint32_t settled(float theta, float rest, float m, fl
 }
 // Both of two words, where their sums are near half-way.
 template <int STATE, bool INSIDE>
-__device__ __forceinline__ void settle(const PairSum& sum, uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, const AdamScalars& k, uint32_t& theta_word,
+__device__ __forceinline__ void settle(const PairSum& sum, uint64_t delta, uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, const AdamScalars& k, uint32_t& theta_word,
                                        uint32_t& rest_word) {
-    const float2 s = floats_of(sum.s), t = floats_of(sum.t), th = floats_of(theta), re = floats_of(rest), mm = floats_of(m), vv = floats_of(v);
-    if (is_near(s.x, t.x)) {
+    const float2 s = floats_of(sum.s), t = floats_of(sum.t), by = floats_of(delta), th = floats_of(theta), re = floats_of(rest), mm = floats_of(m), vv = floats_of(v);
+    if (is_near(s.x, t.x, by.x, k.large)) {
         const uint32_t both = settled<STATE, INSIDE>(th.x, re.x, mm.x, vv.x, k);
         theta_word = __byte_perm(theta_word, both, 0x3254);
         rest_word = __byte_perm(rest_word, both, 0x3276);
     }
-    if (is_near(s.y, t.y)) {
+    if (is_near(s.y, t.y, by.y, k.large)) {
         const uint32_t both = settled<STATE, INSIDE>(th.y, re.y, mm.y, vv.y, k);
         theta_word = __byte_perm(theta_word, both, 0x5410);
         rest_word = __byte_perm(rest_word, both, 0x7610);
@@ -174,17 +175,22 @@ struct Octet {
 template <int STATE, int REST, bool INSIDE, bool SETTLE>
 __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float grad_scale) {
     bool near = false;
+    float most = 0.0f;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const uint64_t g = scaled_pair(o.g[p], grad_scale);
         const uint64_t x = REST == COLLAGE_REST_F32 ? o.rest[p] : REST == COLLAGE_REST_BF16 ? add_pair(o.theta[p], o.rest[p]) : o.theta[p];
         if (REST == COLLAGE_REST_BF16) {
-            const PairSum sum = sum_of_pair(o.theta[p], o.rest[p], advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k));
+            const uint64_t delta = advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k);
+            const PairSum sum = sum_of_pair(o.theta[p], o.rest[p], delta);
             split_pair(sum, o.theta_out[p], o.rest_out[p]);
             if (SETTLE)
-                settle<STATE, INSIDE>(sum, o.theta[p], o.rest[p], o.m[p], o.v[p], k, o.theta_out[p], o.rest_out[p]);
-            else
+                settle<STATE, INSIDE>(sum, delta, o.theta[p], o.rest[p], o.m[p], o.v[p], k, o.theta_out[p], o.rest_out[p]);
+            else {
+                const float2 by = floats_of(delta);
+                asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(fabsf(by.x)), "f"(fabsf(by.y)));
                 near |= is_near(sum);
+            }
             continue;
         }
         uint64_t delta;
@@ -202,7 +208,7 @@ __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float gra
         const float2 to = floats_of(o.rest[p]);
         o.theta_out[p] = pack_bf16(to.x, to.y);
     }
-    return near;
+    return near || most > k.large;
 }
 
 // Largest absolute value of eight over the warp; NaN where there is one.
@@ -417,7 +423,7 @@ __device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile<Form<ST
     for (int p = 0; p < 4; ++p) {
         const uint64_t theta = bf16_pair(th[p]), rest = bf16_pair(re[p]);
         const uint64_t delta = advance<STATE, INSIDE>(o.m[p], o.v[p], scaled_pair(o.g[p], grad_scale), add_pair(theta, rest), k);
-        settle<STATE, INSIDE>(sum_of_pair(theta, rest, delta), theta, rest, o.m[p], o.v[p], k, theta_out[p], rest_out[p]);
+        settle<STATE, INSIDE>(sum_of_pair(theta, rest, delta), delta, theta, rest, o.m[p], o.v[p], k, theta_out[p], rest_out[p]);
     }
     put_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, theta_out);
     put_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, rest_out);
@@ -921,6 +927,7 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     a.k.inv_bc1 = static_cast<float>(1.0 / bc1);
     a.k.rate = static_cast<float>(-hyper->lr / bc1);
     a.k.decay = static_cast<float>(-hyper->lr * hyper->weight_decay);
+    a.k.large = static_cast<float>(128 * hyper->lr);
     a.k.inv_bc2 = static_cast<float>(1.0 / bc2);
     a.k.inv_root_bc2 = static_cast<float>(1.0 / std::sqrt(bc2));
     uint32_t key = mix32(static_cast<uint32_t>(step >> 32));

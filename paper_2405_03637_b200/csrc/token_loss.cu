@@ -24,7 +24,7 @@ struct TokenArgs {
     const float* stats_in;
     const float* weight;                         // grad_logp, or the policy's row weights
     const float *old_logp, *ref_logp, *advantage;
-    float *logp, *stats, *loss, *kl;
+    float *logp, *logp_rest, *stats, *loss, *kl;
     uint64_t ldz, ldd;
     double inv_t;
     float c, c_rest, inv_tf;                     // log2(e) / t and what it lacks, 1 / t
@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
         if (MODE != kLogp) write_row(false, [](uint64_t) -> uint64_t { return 0; });
         if (MODE != kBackward && rank == 0 && threadIdx.x == 0) {
             if (a.logp) a.logp[row] = 0.0f;
+            if (MODE == kLogp && a.logp_rest) a.logp_rest[row] = 0.0f;
             if (MODE == kLogp && a.stats) reinterpret_cast<float2*>(a.stats)[row] = make_float2(0.0f, 0.0f);
             if (MODE == kPolicy) a.loss[row] = 0.0f;
             if (MODE == kPolicy && a.kl) a.kl[row] = 0.0f;
@@ -203,6 +204,10 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
         if (threadIdx.x == 0 && (MODE == kPolicy || rank == 0)) {
             const double logp = static_cast<double>(at_target - m) * a.inv_t - log(static_cast<double>(sum));
             if (rank == 0 && a.logp) a.logp[row] = static_cast<float>(logp);
+            if (MODE == kLogp && a.logp_rest) {      // (of an infinite one nothing is missing)
+                const float rest = static_cast<float>(logp - static_cast<double>(static_cast<float>(logp)));
+                a.logp_rest[row] = isinf(logp) ? 0.0f : rest;
+            }
             if (MODE == kLogp && a.stats) reinterpret_cast<float2*>(a.stats)[row] = make_float2(m, sum);
             if (MODE == kPolicy) {
                 const PolicyRow r = policy_row(a, row, logp, w);
@@ -260,7 +265,7 @@ static collage_status_t launch_token(TokenArgs& a, uint64_t rows, collage_dtype_
 // ------------------------------------------------------------------------------------------------------- preference ---
 
 struct PreferenceArgs {
-    const float *logp, *ref_logp, *pair_weight;
+    const float *logp, *logp_rest, *ref_logp, *pair_weight;
     const void *target, *offsets;
     float *loss, *log_ratio, *grad_logp;
     uint64_t rows, pairs;
@@ -293,7 +298,7 @@ __global__ void __launch_bounds__(kPreferenceThreads) preference_kernel(const __
     for (int s = 0; s < 2; ++s) {
         for (uint64_t i = edges[s] + threadIdx.x; i < edges[s + 1]; i += kPreferenceThreads) {
             if (!counts(i)) continue;
-            sum[s] += static_cast<double>(a.logp[i]) - (a.ref_logp ? static_cast<double>(a.ref_logp[i]) : 0.0);
+            sum[s] += static_cast<double>(a.logp[i]) + (a.logp_rest ? static_cast<double>(a.logp_rest[i]) : 0.0) - (a.ref_logp ? static_cast<double>(a.ref_logp[i]) : 0.0);
             ++n[s];
         }
 #pragma unroll
@@ -406,13 +411,14 @@ using namespace collage::ops;
 
 extern "C" {
 
-collage_status_t collage_token_logp(const collage_tokens_t* in, float* logp, float* stats, void* stream) {
+collage_status_t collage_token_logp(const collage_tokens_t* in, float* logp, float* logp_rest, float* stats, void* stream) {
     if (!in || (!logp && in->logits.rows)) return COLLAGE_ERR_NULL;
     TokenArgs a;
     DeviceInfo dev;
-    const collage_status_t st = prepare_tokens(in, {{nullptr, 1}, {nullptr, 1}, {nullptr, 1}, {nullptr, 1}}, {{logp, 1}, {stats, 2}, {nullptr, 1}}, nullptr, &a, &dev);
+    const collage_status_t st = prepare_tokens(in, {{nullptr, 1}, {nullptr, 1}, {nullptr, 1}, {nullptr, 1}}, {{logp, 1}, {stats, 2}, {logp_rest, 1}}, nullptr, &a, &dev);
     if (st != COLLAGE_OK || in->logits.rows == 0) return st;
     a.logp = logp;
+    a.logp_rest = logp_rest;
     a.stats = stats;
     return launch_token<kLogp>(a, in->logits.rows, in->logits_dtype, dev.sm_count, static_cast<cudaStream_t>(stream));
 }
@@ -461,11 +467,12 @@ collage_status_t collage_preference_loss(const collage_preference_t* in, float* 
     if ((in->target_bytes != 4 && in->target_bytes != 8) || (in->offset_bytes != 4 && in->offset_bytes != 8)) return COLLAGE_ERR_ARG;
     if ((in->rows && (!in->logp || !in->target)) || (in->pairs && (!loss || !in->offsets))) return COLLAGE_ERR_NULL;
     auto off = [](const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; };
-    if (off(in->logp, 4) || off(in->ref_logp, 4) || off(in->pair_weight, 4) || off(loss, 4) || off(log_ratio, 4) || off(grad_logp, 4) ||
+    if (off(in->logp, 4) || off(in->logp_rest, 4) || off(in->ref_logp, 4) || off(in->pair_weight, 4) || off(loss, 4) || off(log_ratio, 4) || off(grad_logp, 4) ||
         off(in->target, in->target_bytes) || off(in->offsets, in->offset_bytes))
         return COLLAGE_ERR_ARG;
     AliasCheck alias;
     alias.add(span_of(in->logp, 4 * in->rows), false);
+    alias.add(span_of(in->logp_rest, 4 * in->rows), false);
     alias.add(span_of(in->ref_logp, 4 * in->rows), false);
     alias.add(span_of(in->target, in->target_bytes * in->rows), false);
     alias.add(span_of(in->offsets, in->offset_bytes * (2 * in->pairs + 1)), false);
@@ -481,6 +488,7 @@ collage_status_t collage_preference_loss(const collage_preference_t* in, float* 
         return !grad_logp || !in->rows || cudaMemsetAsync(grad_logp, 0, 4 * in->rows, s) == cudaSuccess ? COLLAGE_OK : COLLAGE_ERR_CUDA;
     PreferenceArgs a = {};
     a.logp = in->logp;
+    a.logp_rest = in->logp_rest;
     a.ref_logp = in->ref_logp;
     a.pair_weight = in->pair_weight;
     a.target = in->target;

@@ -13,10 +13,10 @@ OPERATORS = {
                    rstd_post=ROW, rstd_pre=ROW)),
     "block_norm_backward": (B.block_norm_backward, [MAT, MAT, MAT, ROW, ROW, MAT, MAT], dict(dr=MAT, gate=MAT, post_weight=COL, pre_weight=COL, dgate=MAT,
                             dpost_weight=COL, dpre_weight=COL, workspace=Fake(64, dtype=torch.uint8))),
-    "token_logp": (B.token_logp, [LOGITS, TARGET, 1.0, ROW], dict(stats=Fake(4, 2, dtype=F32))),
+    "token_logp": (B.token_logp, [LOGITS, TARGET, 1.0, ROW], dict(stats=Fake(4, 2, dtype=F32), logp_rest=ROW)),
     "token_logp_backward": (B.token_logp_backward, [LOGITS, TARGET, 1.0, Fake(4, 2, dtype=F32), ROW, LOGITS], {}),
     "policy_loss_and_grad": (B.policy_loss_and_grad, [LOGITS, TARGET, 1.0, ROW, ROW, ROW, LOGITS], dict(old_logp=ROW, ref_logp=ROW, logp=ROW, kl=ROW)),
-    "preference_loss": (B.preference_loss, [ROW, TARGET, 99, Fake(5, dtype=torch.int32), 0.1, Fake(2, dtype=F32)], dict(grad_logp=ROW, ref_logp=ROW,
+    "preference_loss": (B.preference_loss, [ROW, TARGET, 99, Fake(5, dtype=torch.int32), 0.1, Fake(2, dtype=F32)], dict(grad_logp=ROW, ref_logp=ROW, logp_rest=ROW,
                         pair_weight=Fake(2, dtype=F32), log_ratio=Fake(2, dtype=F32))),
     "adam_step": (B.adam_step, [0x7000, B.make_hyper(1e-3, 0.9, 0.999, 1e-8, 0.0), 1], dict(grad_scale=Fake(1, dtype=F32))),
     "adam_grad_norm": (B.adam_grad_norm, [0x7000, 1.0, Fake(1, dtype=F32), Fake(1, dtype=F32), Fake(64, dtype=torch.uint8)], {}),

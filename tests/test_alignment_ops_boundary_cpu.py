@@ -27,7 +27,7 @@ def test_packed_structures_have_the_headers_layout():
     assert ctypes.sizeof(B.BlockNorm) == 2 * 32 + len(B._pack_block_norm(0, 0, 0, 0, 0, 0)) == 112
     assert ctypes.sizeof(B.Tokens) == 32 + len(B._pack_tokens(0, 0, 0, 0)) == 56
     assert ctypes.sizeof(B.Policy) == len(B._pack_policy(*[0] * 7)) == 56
-    assert ctypes.sizeof(B.Preference) == len(B._pack_preference(*[0] * 14)) == 104
+    assert ctypes.sizeof(B.Preference) == len(B._pack_preference(*[0] * 15)) == 112
     assert ctypes.sizeof(B.AdamTensor) == 64
 
 
@@ -90,7 +90,7 @@ def tokens(z=mat(0, 6, 100), y=at(1), dtype=B.DTYPE_BF16, size=4, temp=1.0):
 
 def test_token_refusals(L):
     dz = mat(2, 6, 100)
-    logp = lambda t, p=at(3), s=at(4): L.collage_token_logp(t, p, s, None)  # noqa: E731
+    logp = lambda t, p=at(3), s=at(4), rest=at(5): L.collage_token_logp(t, p, rest, s, None)  # noqa: E731
     back = lambda t, s=at(4), g=at(3), d=dz: L.collage_token_logp_backward(t, s, g, d, None)  # noqa: E731
     assert logp(None) == B.ERR_NULL and logp(tokens(), p=None) == B.ERR_NULL and logp(tokens(y=None)) == B.ERR_NULL
     assert back(None) == B.ERR_NULL and back(tokens(), d=None) == B.ERR_NULL and back(tokens(), s=None) == B.ERR_NULL and back(tokens(), g=None) == B.ERR_NULL
@@ -101,7 +101,7 @@ def test_token_refusals(L):
         assert f(tokens(size=8, y=at(1) + 4)) == B.ERR_ARG
         assert f(tokens(), s=at(4) + 4) == B.ERR_ARG                      # pairs of floats
         assert f(tokens(z=mat(0, 6, 100, ld=99))) == B.ERR_ARG
-    assert logp(tokens(), s=at(3)) == B.ERR_ALIAS and logp(tokens(), p=at(0)) == B.ERR_ALIAS
+    assert logp(tokens(), s=at(3)) == B.ERR_ALIAS and logp(tokens(), rest=at(3)) == B.ERR_ALIAS and logp(tokens(), rest=at(5) + 2) == B.ERR_ARG and logp(tokens(), p=at(0)) == B.ERR_ALIAS
     assert back(tokens(), d=mat(2, 6, 99)) == B.ERR_ARG
     assert back(tokens(), d=mat(0, 6, 100, offset=2)) == B.ERR_ALIAS and back(tokens(), d=mat(3, 6, 100)) == B.ERR_ALIAS
 
@@ -121,19 +121,19 @@ def test_policy_refusals(L):
 
 
 def test_preference_refusals(L):
-    def call(logp=at(0), ref=at(1), y=at(2), o=at(3), w=at(4), rows=8, vocab=100, pairs=2, ysize=8, osize=4, beta=0.1, margin=0.0, smooth=0.0, loss=at(5),
+    def call(logp=at(0), rest=at(8), ref=at(1), y=at(2), o=at(3), w=at(4), rows=8, vocab=100, pairs=2, ysize=8, osize=4, beta=0.1, margin=0.0, smooth=0.0, loss=at(5),
              ratio=at(6), grad=at(7), s=True):
-        p = B.Preference(logp, ref, y, o, w, rows, vocab, pairs, ysize, osize, beta, margin, smooth, 0)
+        p = B.Preference(logp, rest, ref, y, o, w, rows, vocab, pairs, ysize, osize, beta, margin, smooth, 0)
         return L.collage_preference_loss(ctypes.byref(p) if s else None, loss, ratio, grad, None)
     assert call(s=False) == B.ERR_NULL
     for k in ("logp", "y", "o", "loss"):
         assert call(**{k: None}) == B.ERR_NULL
-    for k, v in (("beta", NAN), ("beta", 1e39), ("margin", INF), ("smooth", -0.1), ("smooth", 1.1), ("smooth", NAN), ("ysize", 2), ("osize", 1), ("logp", at(0) + 2),
+    for k, v in (("beta", NAN), ("beta", 1e39), ("margin", INF), ("smooth", -0.1), ("smooth", 1.1), ("smooth", NAN), ("ysize", 2), ("osize", 1), ("logp", at(0) + 2), ("rest", at(8) + 1),
                  ("y", at(2) + 4), ("o", at(3) + 2), ("grad", at(7) + 1)):
         assert call(**{k: v}) == B.ERR_ARG, (k, v)
     for k in ("rows", "vocab", "pairs"):
         assert call(**{k: 1 << 31}) == B.ERR_LIMIT
-    assert call(grad=at(0)) == B.ERR_ALIAS and call(loss=at(4)) == B.ERR_ALIAS and call(ratio=at(5)) == B.ERR_ALIAS and call(grad=at(3)) == B.ERR_ALIAS
+    assert call(grad=at(0)) == B.ERR_ALIAS and call(grad=at(8)) == B.ERR_ALIAS and call(loss=at(4)) == B.ERR_ALIAS and call(ratio=at(5)) == B.ERR_ALIAS and call(grad=at(3)) == B.ERR_ALIAS
 
 
 def adam_tensor(i=0, n=1000, state=B.STATE_E4M3, form=B.REST_BF16, **kw):

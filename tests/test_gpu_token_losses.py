@@ -55,7 +55,7 @@ class Rows:
         self.lse = torch.logsumexp(z64, 1)
         at = z64.gather(1, self.safe[:, None])[:, 0]
         self.logp = torch.where(self.counts, at - self.lse, 0.0)
-        self.top = z64.amax(1)
+        self.top, self.at = z64.amax(1), at
         self.logp_off = rel_of(vocab) + 2.0 ** -23 * ((self.top - at).abs() + self.logp.abs()) + 2.0 ** -23
 
     def gradient(self, coef, coef_off):
@@ -78,8 +78,11 @@ def forms(seed):
 def test_logp_and_its_backward_match_definition(rows, vocab, pad, shift):
     for dtype, tau, index in forms(rows):
         r = Rows(rows, vocab, pad, shift, dtype, tau, index)
-        logp, stats, bare = vec(rows), vec(2 * rows).view(rows, 2), vec(rows)
-        B.token_logp(r.z.t, r.y, tau, logp, stats=stats)
+        logp, stats, bare, rest = vec(rows), vec(2 * rows).view(rows, 2), vec(rows), vec(rows)
+        B.token_logp(r.z.t, r.y, tau, logp, stats=stats, logp_rest=rest)
+        assert (rest.abs() <= 2.0 ** -24 * logp.abs()).all()         # half a unit of logp's last place at most
+        # both together: the row's sum is within rel_of(vocab), the rest is in 64 bits but for the difference to the maximum in float
+        close(logp.double() + rest.double(), r.logp, torch.where(r.counts, rel_of(vocab) + 2.0 ** -24 * (r.top - r.at).abs(), 0.0), "logp and rest")
         B.token_logp(r.z.t, r.y, tau, bare)
         assert torch.equal(logp, bare)
         close(logp, r.logp, torch.where(r.counts, r.logp_off, 0.0), "logp")
@@ -281,6 +284,19 @@ def test_preference_matches_definition(lengths, gap, tail, average):
         B.preference_loss(logp, y.to(index), vocab, torch.tensor(o, dtype=offset_type, device="cuda"), 0.1, only, ref_logp=ref if use_ref else None,
                           pair_weight=w if use_w else None, margin=margin, label_smoothing=smooth, average=average)
         assert torch.equal(only, loss)
+
+
+def test_preference_takes_what_logp_lacks():
+    """Log-probabilities of -10 to the last digit of 64 bits: in float alone the mean of 1000 of them would be 2^-21 off at worst."""
+    rows = 1000
+    exact = -10 - torch.rand(rows, dtype=torch.float64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    logp = exact.float()
+    rest = (exact - logp.double()).float()
+    y, o = torch.zeros(rows, dtype=torch.int64, device="cuda"), torch.tensor([0, 999, 1000], device="cuda")
+    loss, ratio = vec(1), vec(1)
+    B.preference_loss(logp, y, 9, o, 1.0, loss, average=True, log_ratio=ratio, logp_rest=rest)
+    want = exact[:999].mean() - exact[999]
+    close(ratio[0], want, 2.0 ** -24 * want.abs() + 2.0 ** -47, "log_ratio")
 
 
 def test_preference_of_nothing_and_of_offsets_out_of_range():
