@@ -424,9 +424,12 @@ def _own(s):
         B.token_logp(s["logits"], s["target"], case["temperature"], s["logp"])
         return {"logp": s["logp"]}
     if op == "preference":
-        B.token_logp(s["logits"], s["target"], case["temperature"], s["logp"], stats=s["stats"])
+        if "logp_rest" not in s:                # what rounding the log-probabilities to float takes, which a sequence's sum adds up
+            s["logp_rest"] = torch.empty_like(s["logp"])
+        B.token_logp(s["logits"], s["target"], case["temperature"], s["logp"], stats=s["stats"], logp_rest=s["logp_rest"])
         B.preference_loss(s["logp"], s["target"], case["vocab"], s["offsets"], BETA, s["loss"], s["grad_logp"], ref_logp=s["ref_logp"],
-                          pair_weight=s["pair_weight"], margin=MARGIN, label_smoothing=SMOOTHING, average=case["average"], log_ratio=s["log_ratio"])
+                          pair_weight=s["pair_weight"], margin=MARGIN, label_smoothing=SMOOTHING, average=case["average"], log_ratio=s["log_ratio"],
+                          logp_rest=s["logp_rest"])
         B.token_logp_backward(s["logits"], s["target"], case["temperature"], s["stats"], s["grad_logp"], s["dlogits"])
         return {n: s[n] for n in ("logp", "log_ratio", "loss", "grad_logp", "dlogits")}
     act = (B.GATE_NONE, B.GATE_SIGMOID, B.GATE_SILU)[ACTIVATIONS.index(case["act"])]
