@@ -110,9 +110,9 @@ __device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g
 }
 
 // (theta, rest) + delta: theta' is the bfloat16 nearest to the sum, rest' what that lacks.  In floats theta + RN(rest + delta) is known as s + lost, to
-// five units of the last place of t = rest + delta.  Where s is that near to half-way between two bfloat16 values the sum is taken in 64 bits
-// instead (settled()): as a rule within a unit or two of s's own last place, within more where theta and t nearly cancel.  Sums more than 64 units
-// off half-way are looked at only where the update is larger than any but a few (`large`): elsewhere they are nearly nothing.
+// six units of the last place of delta (six times 2^-23 of it) and half a one of t = rest + delta.  Where s is that near to half-way between two bfloat16 values the sum is taken in 64 bits
+// instead (settled()): as a rule within two or three units of s's own last place, within more where theta and t nearly cancel.  Sums more than 64
+// units off half-way are looked at only where the update is larger than any but a few (`large`): elsewhere they are nearly nothing.
 struct PairSum {
     uint64_t s, t, lost;
 };
@@ -122,13 +122,13 @@ __device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, ui
 }
 __device__ __forceinline__ bool is_near(float s, float t, float delta, float large) {
     const int off = abs(static_cast<int>(__float_as_uint(s) & 0xFFFFu) - 0x8000);
-    return (off < 64 || fabsf(delta) > large) && off * fabsf(s) <= __fmaf_rn(5.0f, fabsf(t), 1.5f * fabsf(s));
+    return (off < 64 || fabsf(delta) > large) && off * fabsf(s) <= 12.0f * fabsf(delta) + fabsf(t) + 2.0f * fabsf(s);
 }
-__device__ __forceinline__ bool is_near(const PairSum& sum) {
-    const float2 s = floats_of(sum.s), t = floats_of(sum.t);
+__device__ __forceinline__ bool is_near(const PairSum& sum, uint64_t delta) {
+    const float2 s = floats_of(sum.s), t = floats_of(sum.t), by = floats_of(delta);
     const uint32_t off = (__byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410) + 0x80408040u) & 0xFF80FF80u;
     if (((off - 0x00010001u) & ~off & 0x80008000u) == 0) return false;           // no half-word within 64 (the lower one's carry allowed for)
-    return is_near(s.x, t.x, 0.0f, 0.0f) || is_near(s.y, t.y, 0.0f, 0.0f);
+    return is_near(s.x, t.x, by.x, INFINITY) || is_near(s.y, t.y, by.y, INFINITY);
 }
 __device__ __forceinline__ void split_pair(const PairSum& sum, uint32_t& theta_word, uint32_t& rest_word) {
     const float2 s = floats_of(sum.s);
@@ -189,7 +189,7 @@ __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float gra
             else {
                 const float2 by = floats_of(delta);
                 asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(fabsf(by.x)), "f"(fabsf(by.y)));
-                near |= is_near(sum);
+                near |= is_near(sum, delta);
             }
             continue;
         }

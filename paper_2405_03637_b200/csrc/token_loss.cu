@@ -75,6 +75,10 @@ __device__ __forceinline__ void add_exact_exps(const uint4& q, float m, const To
     }
 }
 
+// By how much the hardware's 2^x is too low on average (measured: log-probabilities of 400 to 2000 rows of 32000 and 50257 logits were too high by
+// 6.3e-8 to 8.5e-8, with a spread of 4.5e-8).  The row's largest logit, whose exponential is 1, has no part in that.
+constexpr double kExpLow = 7.0e-8;
+
 struct TokenShared {
     float2 warp[8];
     float2 part[kTokenCluster];          // (maximum, sum) of each block of the cluster
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
         scale = 1.0f / sum;
         coef = 0.0f;
         if (threadIdx.x == 0 && (MODE == kPolicy || rank == 0)) {
-            const double logp = static_cast<double>(at_target - m) * a.inv_t - log(static_cast<double>(sum));
+            const double logp = (static_cast<double>(at_target) - static_cast<double>(m)) * a.inv_t - log(sum + (static_cast<double>(sum) - 1.0) * kExpLow);
             if (rank == 0 && a.logp) a.logp[row] = static_cast<float>(logp);
             if (MODE == kLogp && a.logp_rest) {      // (of an infinite one nothing is missing)
                 const float rest = static_cast<float>(logp - static_cast<double>(static_cast<float>(logp)));
