@@ -37,9 +37,9 @@ struct AdamChunk {
 
 struct AdamScalars {
     Fp32Scalars f;
-    float rate, decay, large;                  // -a / bc1, -a lam, 128 a
+    float rate, decay;                         // -a / bc1, -a lam
+    float a_hi, a_lo;                          // a in two floats
     float inv_bc1, inv_bc2, inv_root_bc2;      // 1 / bc1, 1 / bc2, 1 / sqrt(bc2)
-    double a, lam;
     uint32_t key;
 };
 
@@ -98,73 +98,67 @@ __device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
     return pair_of(f.x, f.y);
 }
 
-// A step of two elements' states: m', sqrt(v') (or v' itself), and the update of parameters x.  Every product and sum of the states is
-// rounded once, so that their codes hang on nothing but the formulas; the quotient is within a few units of the last place.
-template <int STATE, bool INSIDE>
-__device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g, uint64_t x, const AdamScalars& k) {
+// A step of two elements' states: m', and sqrt(v') or v' itself.  Every product and sum is rounded once, so that codes hang on nothing but the
+// formulas.  Returns sqrt(v').
+template <int STATE>
+__device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g, const AdamScalars& k) {
     const uint64_t squared = STATE == COLLAGE_STATE_F32 ? v : mul_pair(v, v);
     m = add_rounded(scaled_pair(m, k.f.b1), scaled_pair(g, k.f.c1));
     v = add_rounded(scaled_pair(squared, k.f.b2), scaled_pair(mul_pair(g, g), k.f.c2));
-    const uint64_t root = root_pair(v);
+    return root_pair(v);
+}
+// The update of parameters x to a few units of its last place.
+template <bool INSIDE>
+__device__ __forceinline__ uint64_t update_of(uint64_t m, uint64_t v, uint64_t root, uint64_t x, const AdamScalars& k) {
     const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : scaled_plus(root, k.inv_root_bc2, k.f.eps);
-    if (STATE == COLLAGE_STATE_E4M3) v = root;
     return scaled_plus(x, k.decay, scaled_pair(mul_pair(m, reciprocal_pair(den)), k.rate));
 }
 
-// (theta, rest) + delta: theta' is the bfloat16 nearest to the sum, rest' what that lacks.  In floats theta + RN(rest + delta) is known as s + lost, to
-// six units of the last place of delta (six times 2^-23 of it) and half a one of t = rest + delta.  Where s is that near to half-way between two bfloat16 values the sum is taken in 64 bits
-// instead (settled()): as a rule within two or three units of s's own last place, within more where theta and t nearly cancel.  Sums more than 64
-// units off half-way are looked at only where the update is larger than any but a few (`large`): elsewhere they are nearly nothing.
+// A bfloat16 pair keeps 16 bits and more of its parameter, and what it keeps is meant to be exact: theta' the nearest bfloat16 to
+//   theta + rest - a (q + lam x),  q = RN(m' / bc1) / RN(sqrt(v' / bc2) + eps) rounded once,
+// rest' what that lacks.  The sum is known here as s + low to about 2^-24 of the decay's part and far less of the rest's: q by Markstein's division
+// (a reciprocal by a step of Newton's method, the quotient's remainder exact in an fma), its product with a (two floats) with the
+// product's remainder, and sums with their remainders (TwoSum).
 struct PairSum {
-    uint64_t s, t, lost;
+    uint64_t s, low;
 };
-__device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, uint64_t delta) {
-    const uint64_t t = add_pair(rest, delta), s = add_pair(theta, t), back = sub_pair(s, theta);
-    return {s, t, add_pair(sub_pair(theta, sub_pair(s, back)), sub_pair(t, back))};                  // theta + t = s + lost, exactly
+template <bool INSIDE>
+__device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, uint64_t root, const AdamScalars& k) {
+    const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : add_rounded(scaled_pair(root, k.inv_root_bc2), pair_of(k.f.eps));
+    const uint64_t num = scaled_pair(m, k.inv_bc1);
+    const float2 d = floats_of(den), n = floats_of(num);
+    float2 r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+    const uint64_t r0 = pair_of(r.x, r.y), r1 = fma_pair(pair_of(__fmaf_rn(-d.x, r.x, 1.0f), __fmaf_rn(-d.y, r.y, 1.0f)), r0, r0);
+    const float2 q0 = floats_of(mul_pair(num, r1));
+    const uint64_t q = fma_pair(pair_of(__fmaf_rn(-d.x, q0.x, n.x), __fmaf_rn(-d.y, q0.y, n.y)), r1, pair_of(q0.x, q0.y));
+    const float2 qf = floats_of(q);
+    const uint64_t p = pair_of(__fmul_rn(qf.x, k.a_hi), __fmul_rn(qf.y, k.a_hi));        // a q, and (negated) its remainder and the decay
+    const uint64_t more = fma_pair(add_pair(theta, rest), pair_of(k.decay), fma_pair(q, pair_of(-k.a_lo), fma_pair(q, pair_of(-k.a_hi), p)));
+    const uint64_t t = sub_pair(rest, p), tb = sub_pair(t, rest), t_low = sub_pair(sub_pair(rest, sub_pair(t, tb)), add_pair(p, tb));
+    const uint64_t s = add_pair(theta, t), sb = sub_pair(s, theta), s_low = add_pair(sub_pair(theta, sub_pair(s, sb)), sub_pair(t, sb));
+    const uint64_t low = add_pair(add_pair(s_low, t_low), more), whole = add_pair(s, low);
+    return {whole, sub_pair(low, sub_pair(whole, s))};
 }
-__device__ __forceinline__ bool is_near(float s, float t, float delta, float large) {
-    const int off = abs(static_cast<int>(__float_as_uint(s) & 0xFFFFu) - 0x8000);
-    return (off < 64 || fabsf(delta) > large) && off * fabsf(s) <= 12.0f * fabsf(delta) + fabsf(t) + 2.0f * fabsf(s);
-}
-__device__ __forceinline__ bool is_near(const PairSum& sum, uint64_t delta) {
-    const float2 s = floats_of(sum.s), t = floats_of(sum.t), by = floats_of(delta);
-    const uint32_t off = (__byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410) + 0x80408040u) & 0xFF80FF80u;
-    if (((off - 0x00010001u) & ~off & 0x80008000u) == 0) return false;           // no half-word within 64 (the lower one's carry allowed for)
-    return is_near(s.x, t.x, by.x, INFINITY) || is_near(s.y, t.y, by.y, INFINITY);
-}
+// A float half-way between two bfloat16 values: `low` tells which one is nearer.  (One in 65536.)
+__device__ __forceinline__ bool is_tie(float s) { return (__float_as_uint(s) & 0xFFFFu) == 0x8000u; }
 __device__ __forceinline__ void split_pair(const PairSum& sum, uint32_t& theta_word, uint32_t& rest_word) {
     const float2 s = floats_of(sum.s);
     theta_word = pack_bf16(s.x, s.y);
-    const float2 r = floats_of(add_pair(sub_pair(sum.s, bf16_pair(theta_word)), sum.lost));
+    const float2 r = floats_of(add_pair(sub_pair(sum.s, bf16_pair(theta_word)), sum.low));
     rest_word = pack_bf16(r.x, r.y);
 }
-// The pair of x - a (q + lam x) with x = theta + rest, for the quotient q of m' and v' (or its root) as IEEE operations give it.
-template <int STATE, bool INSIDE>
-__device__ __forceinline__ uint32_t settled(float theta, float rest, float m, float v, const AdamScalars& k) {
-    const float root = STATE == COLLAGE_STATE_E4M3 ? v : __fsqrt_rn(v), square = STATE == COLLAGE_STATE_E4M3 ? v * v : v;
-    const float den = INSIDE ? __fsqrt_rn(__fmaf_rn(square, k.inv_bc2, k.f.eps)) : root * k.inv_root_bc2 + k.f.eps;
-    const double x = static_cast<double>(theta) + rest, to = x - k.a * (__fdiv_rn(m * k.inv_bc1, den) + k.lam * x);
-    // to bfloat16 by way of a float that is rounded to odd
-    float f = __double2float_rz(to);
-    if (static_cast<double>(f) != to && fabsf(f) < INFINITY) f = __uint_as_float(__float_as_uint(f) | 1u);
-    const uint32_t near = to_bf16(f);
-    return near | static_cast<uint32_t>(to_bf16(static_cast<float>(to - bf16_value(static_cast<uint16_t>(near))))) << 16;
-}
-// Both of two words, where their sums are near half-way.
-template <int STATE, bool INSIDE>
-__device__ __forceinline__ void settle(const PairSum& sum, uint64_t delta, uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, const AdamScalars& k, uint32_t& theta_word,
-                                       uint32_t& rest_word) {
-    const float2 s = floats_of(sum.s), t = floats_of(sum.t), by = floats_of(delta), th = floats_of(theta), re = floats_of(rest), mm = floats_of(m), vv = floats_of(v);
-    if (is_near(s.x, t.x, by.x, k.large)) {
-        const uint32_t both = settled<STATE, INSIDE>(th.x, re.x, mm.x, vv.x, k);
-        theta_word = __byte_perm(theta_word, both, 0x3254);
-        rest_word = __byte_perm(rest_word, both, 0x3276);
-    }
-    if (is_near(s.y, t.y, by.y, k.large)) {
-        const uint32_t both = settled<STATE, INSIDE>(th.y, re.y, mm.y, vv.y, k);
-        theta_word = __byte_perm(theta_word, both, 0x5410);
-        rest_word = __byte_perm(rest_word, both, 0x7610);
-    }
+// Two words again where their sums are ties: theta' by way of a float rounded to odd, towards the sum's own side.
+__device__ __forceinline__ void settle(const PairSum& sum, uint32_t& theta_word, uint32_t& rest_word) {
+    const float2 s = floats_of(sum.s), l = floats_of(sum.low);
+    auto odd = [](float f, float low) {
+        const uint32_t bits = __float_as_uint(f);
+        return is_tie(f) && low != 0.0f && fabsf(low) < INFINITY ? __uint_as_float((bits - ((__float_as_uint(low) ^ bits) >> 31)) | 1u) : f;
+    };
+    theta_word = pack_bf16(odd(s.x, l.x), odd(s.y, l.y));
+    const float2 r = floats_of(add_pair(sub_pair(sum.s, bf16_pair(theta_word)), sum.low));
+    rest_word = pack_bf16(r.x, r.y);
 }
 
 // Eight elements of a lane, in pairs, before and behind the update.  With states in 8 bits v is its root.
@@ -173,28 +167,26 @@ struct Octet {
     uint32_t theta_out[4], rest_out[4];                  // two bfloat16 each
 };
 
-// SETTLE: sums near half-way are settled here and now; else the result tells whether there are any.
+// SETTLE: sums that are ties are settled here and now; else the result tells whether there are any.
 template <int STATE, int REST, bool INSIDE, bool SETTLE>
 __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float grad_scale) {
-    bool near = false;
-    float most = 0.0f;
+    uint32_t least = 0;                         // smallest of the sums' lower half-words as signed numbers: -32768 if one is a tie
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const uint64_t g = scaled_pair(o.g[p], grad_scale);
-        const uint64_t x = REST == COLLAGE_REST_F32 ? o.rest[p] : REST == COLLAGE_REST_BF16 ? add_pair(o.theta[p], o.rest[p]) : o.theta[p];
         if (REST == COLLAGE_REST_BF16) {
-            const uint64_t delta = advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k);
-            const PairSum sum = sum_of_pair(o.theta[p], o.rest[p], delta);
+            const uint64_t root = advance<STATE>(o.m[p], o.v[p], g, k);
+            const PairSum sum = sum_of_pair<INSIDE>(o.theta[p], o.rest[p], o.m[p], o.v[p], root, k);
+            if (STATE == COLLAGE_STATE_E4M3) o.v[p] = root;
             split_pair(sum, o.theta_out[p], o.rest_out[p]);
+            const float2 s = floats_of(sum.s);
             if (SETTLE)
-                settle<STATE, INSIDE>(sum, delta, o.theta[p], o.rest[p], o.m[p], o.v[p], k, o.theta_out[p], o.rest_out[p]);
-            else {
-                const float2 by = floats_of(delta);
-                asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(fabsf(by.x)), "f"(fabsf(by.y)));
-                near |= is_near(sum, delta);
-            }
+                settle(sum, o.theta_out[p], o.rest_out[p]);
+            else
+                least = __vmins2(least, __byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x5410));
             continue;
         }
+        const uint64_t x = REST == COLLAGE_REST_F32 ? o.rest[p] : o.theta[p];
         uint64_t delta;
         if (STATE == COLLAGE_STATE_F32) {       // the flat step's operations
             float2 m = floats_of(o.m[p]), v = floats_of(o.v[p]);
@@ -204,13 +196,15 @@ __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float gra
             o.m[p] = pair_of(m.x, m.y);
             o.v[p] = pair_of(v.x, v.y);
         } else {
-            delta = advance<STATE, INSIDE>(o.m[p], o.v[p], g, x, k);
+            const uint64_t root = advance<STATE>(o.m[p], o.v[p], g, k);
+            delta = update_of<INSIDE>(o.m[p], o.v[p], root, x, k);
+            o.v[p] = root;
         }
         o.rest[p] = add_pair(x, delta);
         const float2 to = floats_of(o.rest[p]);
         o.theta_out[p] = pack_bf16(to.x, to.y);
     }
-    return near || most > k.large;
+    return (least & 0xFFFFu) == 0x8000u || least >> 16 == 0x8000u;
 }
 
 // Largest absolute value of eight over the warp; NaN where there is one.
@@ -411,25 +405,16 @@ __device__ __forceinline__ void fetch_group(uint8_t* stage, const AdamTile<Form<
     }
 }
 
-// Parameters of a group that may have sums near half-way, once more from its old values; those sums are settled in the stage.
+// Parameters of a group that has ties among its sums, once more from its old values.
 template <int STATE, bool INSIDE>
-__device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile<Form<STATE, COLLAGE_REST_BF16>::kWarps>& tile, uint32_t g, const AdamScalars& k, float grad_scale, uint4 old_theta, uint4 old_rest) {
+__device__ __noinline__ void settle_group(uint8_t* stage, const AdamTile<Form<STATE, COLLAGE_REST_BF16>::kWarps>& tile, uint32_t g, const AdamScalars& k, float grad_scale) {
     using F = Form<STATE, COLLAGE_REST_BF16>;
     const int lane = threadIdx.x & 31;
     Octet o;
     fetch_group<STATE, COLLAGE_REST_BF16>(stage, tile, g, o, lane);
-    const uint32_t th[4] = {old_theta.x, old_theta.y, old_theta.z, old_theta.w}, re[4] = {old_rest.x, old_rest.y, old_rest.z, old_rest.w};
-    uint32_t theta_out[4], rest_out[4];
-    fetch_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, theta_out);
-    fetch_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, rest_out);
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const uint64_t theta = bf16_pair(th[p]), rest = bf16_pair(re[p]);
-        const uint64_t delta = advance<STATE, INSIDE>(o.m[p], o.v[p], scaled_pair(o.g[p], grad_scale), add_pair(theta, rest), k);
-        settle<STATE, INSIDE>(sum_of_pair(theta, rest, delta), delta, theta, rest, o.m[p], o.v[p], k, theta_out[p], rest_out[p]);
-    }
-    put_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, theta_out);
-    put_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, rest_out);
+    update<STATE, COLLAGE_REST_BF16, INSIDE, true>(o, k, grad_scale);
+    put_array<F, 2>(stage + F::kT + g * (kGroup * 2), lane, o.theta_out);
+    put_array<F, 2>(stage + F::kR + g * (kGroup * 2), lane, o.rest_out);
 }
 
 // A whole group by a warp, in place in the stage.
@@ -440,18 +425,14 @@ __device__ __forceinline__ void whole_group(uint8_t* stage, AdamTile<Form<STATE,
     Octet o;
     fetch_group<STATE, REST>(stage, tile, g, o, lane);
     uint32_t wide[8];
-    const bool mine = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
+    const bool tie = update<STATE, REST, INSIDE, false>(o, k, grad_scale);
     if constexpr (REST == COLLAGE_REST_BF16) {
-        uint32_t th[4], re[4];
-        const bool near = __any_sync(0xFFFFFFFFu, mine);
-        if (near) {
-            fetch_array<F, 2>(of(F::kT, 2), lane, th);
-            fetch_array<F, 2>(of(F::kR, 2), lane, re);
+        if (__any_sync(0xFFFFFFFFu, tie)) {
+            settle_group<STATE, INSIDE>(stage, tile, g, k, grad_scale);
+        } else {
+            put_array<F, 2>(of(F::kT, 2), lane, o.theta_out);
+            put_array<F, 2>(of(F::kR, 2), lane, o.rest_out);
         }
-        put_array<F, 2>(of(F::kT, 2), lane, o.theta_out);
-        put_array<F, 2>(of(F::kR, 2), lane, o.rest_out);
-        if (near)
-            settle_group<STATE, INSIDE>(stage, tile, g, k, grad_scale, make_uint4(th[0], th[1], th[2], th[3]), make_uint4(re[0], re[1], re[2], re[3]));
     } else {
         put_array<F, 2>(of(F::kT, 2), lane, o.theta_out);
     }
@@ -925,12 +906,11 @@ collage_status_t collage_adam_step(const collage_adam_plan_t* plan, const collag
     a.grad_scale = grad_scale;
     a.k.f = fp32_scalars(hyper, step);
     const double t = static_cast<double>(step), bc1 = 1.0 - std::pow(hyper->beta1, t), bc2 = 1.0 - std::pow(hyper->beta2, t);
-    a.k.a = hyper->lr;
-    a.k.lam = hyper->weight_decay;
     a.k.inv_bc1 = static_cast<float>(1.0 / bc1);
     a.k.rate = static_cast<float>(-hyper->lr / bc1);
     a.k.decay = static_cast<float>(-hyper->lr * hyper->weight_decay);
-    a.k.large = static_cast<float>(128 * hyper->lr);
+    a.k.a_hi = static_cast<float>(hyper->lr);
+    a.k.a_lo = static_cast<float>(hyper->lr - a.k.a_hi);
     a.k.inv_bc2 = static_cast<float>(1.0 / bc2);
     a.k.inv_root_bc2 = static_cast<float>(1.0 / std::sqrt(bc2));
     uint32_t key = mix32(static_cast<uint32_t>(step >> 32));
