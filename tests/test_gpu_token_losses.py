@@ -98,6 +98,22 @@ def test_logp_and_its_backward_match_definition(rows, vocab, pad, shift):
             assert d.untouched_outside()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tau", [0.7, 1.0, 1.3])
+def test_errors_of_logp_do_not_add_up(tau, dtype):
+    """A sequence sums thousands of log-probabilities: their mean is off by less than a rounding of the sum of exponentials, 2^-23 (an
+    exponential is off by up to 2^-22, both ways, and log2(e) / tau in one float by up to 2^-23, which a difference of 8 in the logits
+    would make 2^-20; the 512 rows' own spread adds 2^-22 / sqrt(512))."""
+    rows, vocab = 512, 13304
+    g = torch.Generator(device="cuda").manual_seed(17)
+    z = (torch.randn((rows, vocab), generator=g, device="cuda") * 2).to(dtype)
+    y = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    want = (z.double() / tau).gather(1, y[:, None])[:, 0] - torch.logsumexp(z.double() / tau, 1)
+    logp, rest = vec(rows), vec(rows)
+    B.token_logp(z, y, tau, logp, logp_rest=rest)
+    assert (logp.double() + rest.double() - want).mean().abs() < 2.0 ** -23
+
+
 def policy_inputs(r, seed=3):
     """Ratios on both sides of each bound, none within a hundredth of one; advantages of both signs and zero."""
     pick = torch.arange(r.rows, device="cuda")
