@@ -638,7 +638,8 @@ collage_status_t collage_preference_loss(const collage_preference_t* in, float* 
  *   x' = x - lr (m' / (1 - beta1^t) / (sqrt(v' / (1 - beta2^t)) + eps) + weight_decay x)
  * The parameter, by `rest`: NONE  x = theta, theta' = RN_bf16(x');
  *                           BF16  x = theta + rest, a pair as in option B: theta' = RN_bf16(x'), rest' = RN_bf16(x' - theta'),
- *                                 with x' as the unrounded sum of theta and (rest + update), the latter in float;
+ *                                 with x' as the sum of theta, rest, -lr weight_decay x and -lr q, none of them rounded but q, the
+ *                                 float quotient of the moments' means, so that theta' is the nearest value;
  *                           F32   x = rest, a master weight: rest' = x', theta' = RN_bf16(x') (theta is not read).
  * The states, by `state`: F32   m and v are floats; with rest NONE or F32 the results are collage_adamw_step_fp32's, bit for bit.
  *                         E4M3  m and v are codes of 8 bits with a float scale for each 256 elements of their tensor (the last

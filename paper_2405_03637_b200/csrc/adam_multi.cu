@@ -8,8 +8,8 @@
 // part, since in a step of beta2 = 0.999 it moves by a two-hundredth of a code's step, which rounding to nearest would undo each time;
 // m moves by a tenth of what separates it from the gradient and is rounded to nearest.
 // Bytes a parameter: 10 (theta alone) to 16 with 8-bit states, 22 to 28 with floats.  Measured: 134 M parameters in 8 bits alone 299 us (4.5 TB/s),
-// with pairs 388 us (4.9), with master weights 333 us (6.5); 67 M in floats alone 236 us (6.3), with pairs 273 us (6.4), with master weights 290
-// us (6.5).  The first two are bound by instructions (60 to 80 an element: decoding, sums with their remainders, random bits, codes), the
+// with pairs 388 us (4.9), with master weights 332 us (6.5); 67 M in floats alone 236 us (6.3), with pairs 273 us (6.4), with master weights 292
+// us (6.4).  The first two are bound by instructions (60 to 81 an element: decoding, sums with their remainders, random bits, codes), the
 // others by memory.
 #include "adamw_float.cuh"
 #include "bulk_pipe.cuh"
@@ -276,8 +276,8 @@ __device__ __forceinline__ uint32_t random_word(uint64_t pair, uint32_t key) {
 
 // Groups of a tile, one for each warp beside the one that copies.  One more than a multiple of four, with that one, would cost all of them
 // registers: a quarter of an SM would have one warp more to share its own among.  Measured with 15, 19 and 23: 134 M parameters in 8 bits alone
-// 299, 323 and 300 us, with pairs 399, 400 and 388, with master weights 337, 360 and 333; 67 M in floats alone 236, 235 and 252 us, with pairs
-// 287, 295 and 273, with master weights 307, 292 and 290.
+// 299, 323 and 300 us, with pairs 399, 400 and 388, with master weights 337, 361 and 332; 67 M in floats alone 236, 235 and 252 us, with pairs
+// 287, 295 and 273, with master weights 306, 294 and 292.
 constexpr int tile_groups(int rest) { return rest == COLLAGE_REST_NONE ? 15 : 23; }
 
 // A stage of the copy pipeline: a tile's bytes of each array.  Of a whole group a lane has eight elements in a row, or, where some array
@@ -291,7 +291,7 @@ struct Form {
     // offsets of the arrays in a stage
     static constexpr uint32_t kG = 0, kT = kG + 2 * kTile, kR = kT + 2 * kTile, kM = kR + kRestBytes * kTile, kV = kM + kStateBytes * kTile,
                               kStage = kV + kStateBytes * kTile;
-    static constexpr uint32_t kStages = 208 * 1024 / kStage;          // three to seven
+    static constexpr uint32_t kStages = 208 * 1024 / kStage;          // two to seven
     static __device__ __forceinline__ uint32_t element(int lane, int half) { return kHalves ? half * (kGroup / 2) + lane * 4 : lane * 8 + half * 4; }
 };
 
