@@ -74,10 +74,10 @@ class Policy:
         torch.matmul(dlogits.T, y, out=self.grad["head"])
         dy, dr = dlogits @ self.p["head"], None
         for i in reversed(range(self.layers)):
-            b, before = self.blocks[i], (self.blocks[i - 1]["y"] if i else self.first["y"])
+            b, before, x = self.blocks[i], (self.blocks[i - 1]["y"] if i else self.first["y"]), (self.blocks[i - 1]["r"] if i else self.r0)
             dx, do = torch.empty_like(dy), torch.empty_like(dy)
             g = {n: self.grad[f"{i}.{k}"] for n, k in (("dgate", "channel"), ("dpost_weight", "post"), ("dpre_weight", "pre"))}
-            B.block_norm_backward(dy, b["r"], b["o"], b["rstd_post"], b["rstd_pre"], dx, do, dr=dr, workspace=self.workspace, **g, **self.norms(i))
+            B.block_norm_backward(dy, None, b["o"], b["rstd_post"], b["rstd_pre"], dx, do, dr=dr, workspace=self.workspace, x=x, **g, **self.norms(i))
             dr = dx
             torch.matmul(do.T, b["h"], out=self.grad[f"{i}.down"])
             dh, dy = do @ self.p[f"{i}.down"], torch.empty_like(dx)

@@ -551,19 +551,28 @@ collage_status_t collage_block_norm(const collage_block_norm_t* in, const collag
 /* Its backward pass; `in` as in the forward call (eps is not used).
  *   dy      : bfloat16 [rows, cols], gradient of y, or NULL: none came that way (pre_weight, r and rstd_pre are then not used).
  *   dr      : bfloat16 [rows, cols], gradient that reached r on its own way, or NULL.  One of dy and dr is given.
- *   r, rstd_post, rstd_pre: of the forward call; rstd_post with post_weight only.
+ *   r, rstd_post, rstd_pre: of the forward call; rstd_post with post_weight only.  r is the stream as it was stored, so that 2^-8 of each
+ *             of its values, a rounding to bfloat16, goes into the gradients that have r in them: into dpre_weight above all, a sum of dy r
+ *             rstd_pre, and in less measure into dx, dblock, dpost_weight and dgate by way of dy.
  *   dx, dblock: bfloat16 [rows, cols] or NULL: gradients of x and o.  Either may be the array of dy or of dr.
  *   dgate   : bfloat16, shaped like the gate, or NULL; for a gate of channels the sum over the rows.
  *   dpost_weight, dpre_weight: DEVICE bfloat16[cols] or NULL.  (Sums over no rows are zeros.)
  *   workspace: DEVICE scratch of at least collage_block_norm_workspace_bytes(cols), 16-byte aligned, needed with dpost_weight,
  *             dpre_weight or the gradient of a gate of channels; nothing in it is kept between calls (ERR_WORKSPACE).
- * A gradient of 8-bit outputs passes straight through. */
+ * A gradient of 8-bit outputs passes straight through.
+ * collage_block_norm_backward_from_x takes x of the forward call in the place of r (with the same residual_scale and block_scale), where it is
+ * still there (r was not stored over it), and forms r anew from x and o: gradients of r as it was before its rounding. */
 size_t collage_block_norm_workspace_bytes(uint64_t cols);
 collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
                                              const collage_matrix_t* r, const float* rstd_post, const float* rstd_pre,
                                              const collage_matrix_t* dx, const collage_matrix_t* dblock, const collage_matrix_t* dgate,
                                              void* dpost_weight, void* dpre_weight, void* workspace, size_t workspace_bytes,
                                              void* stream);
+collage_status_t collage_block_norm_backward_from_x(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
+                                                    const collage_matrix_t* x, const float* rstd_post, const float* rstd_pre,
+                                                    const collage_matrix_t* dx, const collage_matrix_t* dblock,
+                                                    const collage_matrix_t* dgate, void* dpost_weight, void* dpre_weight, void* workspace,
+                                                    size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Losses on the log-probabilities of sampled tokens: what a token had under the model, the clipped policy objective with a

@@ -39,7 +39,7 @@ EXPORTS = (
     "collage_add_rms_norm", "collage_add_rms_norm_backward", "collage_rms_norm_workspace_bytes", "collage_quantize_rows",
     "collage_gated_ffn", "collage_gated_ffn_backward", "collage_gated_ffn_e4m3",
     "collage_distill_loss", "collage_distill_loss_backward", "collage_distill_loss_and_grad",
-    "collage_block_norm", "collage_block_norm_backward", "collage_block_norm_workspace_bytes",
+    "collage_block_norm", "collage_block_norm_backward", "collage_block_norm_backward_from_x", "collage_block_norm_workspace_bytes",
     "collage_token_logp", "collage_token_logp_backward", "collage_policy_loss_and_grad", "collage_preference_loss",
     "collage_adam_plan_create", "collage_adam_plan_destroy", "collage_adam_step", "collage_adam_grad_norm",
 )
@@ -197,6 +197,7 @@ def _declare_operators(L, mp, dp, bp, tp, pp, rp):
     L.collage_block_norm_workspace_bytes.restype = size
     L.collage_block_norm_workspace_bytes.argtypes = [ctypes.c_uint64]
     L.collage_block_norm_backward.argtypes = [bp, mp, mp, mp, vp, vp, mp, mp, mp, vp, vp, vp, size, vp]
+    L.collage_block_norm_backward_from_x.argtypes = [bp, mp, mp, mp, vp, vp, mp, mp, mp, vp, vp, vp, size, vp]
     L.collage_token_logp.argtypes = [tp, vp, vp, vp, vp]
     L.collage_token_logp_backward.argtypes = [tp, vp, vp, mp, vp]
     L.collage_policy_loss_and_grad.argtypes = [tp, pp, vp, vp, vp, mp, vp]
@@ -656,15 +657,21 @@ def block_norm_workspace_bytes(cols: int) -> int:
 
 def block_norm_backward(dy, r, block, rstd_post, rstd_pre, dx, dblock, dr=None, gate=None, post_weight=None, pre_weight=None, dgate=None,
                         dpost_weight=None, dpre_weight=None, workspace=None, residual_scale: float = 1.0, block_scale: float = 1.0,
-                        activation: int = GATE_NONE, stream=None):
-    """Gradients of block_norm from that of y (dy) and that which reached r on its own way (dr); outputs that are None are not computed."""
+                        activation: int = GATE_NONE, stream=None, x=None):
+    """Gradients of block_norm from that of y (dy) and that which reached r on its own way (dr); outputs that are None are not computed.
+
+    With r as the forward call stored it, the gradients take in its rounding.  Where x is still there, r=None and x in its place leave that out:
+    r is formed anew from x and block.
+    """
     w, (L, dev) = "collage_block_norm_backward", _operators()
+    if x is not None and r is not None:
+        _refuse(f"{w}: r and x")
     s, rows, cols = _block_norm(block, gate, post_weight, pre_weight, 0.0, residual_scale, block_scale, activation, dev, w)
     ws, ws_bytes = _scratch(workspace, dev, w)
-    _check(L.collage_block_norm_backward(s, _matrix(dy, _BF16, dev, w), _matrix(dr, _BF16, dev, w), _matrix(r, _BF16, dev, w),
-                                         _vector(rstd_post, _F32, rows, dev, w), _vector(rstd_pre, _F32, rows, dev, w), _matrix(dx, _BF16, dev, w),
-                                         _matrix(dblock, _BF16, dev, w), _matrix(dgate, _BF16, dev, w), _vector(dpost_weight, _BF16, cols, dev, w),
-                                         _vector(dpre_weight, _BF16, cols, dev, w), ws, ws_bytes, _stream(stream, dev, w)), w)
+    f, stored = (L.collage_block_norm_backward, r) if x is None else (L.collage_block_norm_backward_from_x, x)
+    _check(f(s, _matrix(dy, _BF16, dev, w), _matrix(dr, _BF16, dev, w), _matrix(stored, _BF16, dev, w), _vector(rstd_post, _F32, rows, dev, w),
+             _vector(rstd_pre, _F32, rows, dev, w), _matrix(dx, _BF16, dev, w), _matrix(dblock, _BF16, dev, w), _matrix(dgate, _BF16, dev, w),
+             _vector(dpost_weight, _BF16, cols, dev, w), _vector(dpre_weight, _BF16, cols, dev, w), ws, ws_bytes, _stream(stream, dev, w)), w)
 
 
 def _index(t, length, dev, where):

@@ -11,7 +11,10 @@
 // A row of each array is read once and kept in registers through both of its sums.  Measured at 8191 x 4096 with a gate of channels: forward 48 us
 // (5.5 TB/s), backward with all gradients 79 us (5.1 TB/s): memory, and a row's two joins.  With a gate for each token: 2047 x 5120 forward 28
 // us (3.7), backward 55 us (3.1): the gates' exponentials, and one row on an SM at a time.
-// As in the residual norm, y belongs to r before r is rounded for the stream, and the backward pass reads the rounded r.
+// As in the residual norm, y belongs to r before r is rounded for the stream.  The backward pass reads the rounded r, or x in its place (FROM_X):
+// r is then formed anew, alpha x + (beta A w_post) no, and dw_pre, a sum of dy r, is free of a rounding of each r (relative error at 8191 x 4096
+// with a few large columns 0.0016 in place of 0.0022; one rounding of the result is 0.0016).  Same bytes, three more instructions an element:
+// backward 84 us in place of 80 at 8191 x 4096, 58 in place of 55 at 2047 x 5120 with a gate for each token.
 #include "bulk_pipe.cuh"
 #include "ops_common.cuh"
 
@@ -48,6 +51,19 @@ __device__ __forceinline__ float2 gate_value_and_slope(int kind, float g) {
     return make_float2(g * s.x, __fmaf_rn(g * s.x, s.y, s.x));
 }
 __device__ __forceinline__ float gate_slope(int kind, float g) { return gate_value_and_slope(kind, g).y; }
+// The same by way of the smaller one of 1 / (1 + exp(-g)) and what that lacks of 1, which gives both of them to a float's precision.
+__device__ __forceinline__ float gate_smaller(int kind, float g) {
+    if (kind == COLLAGE_GATE_NONE) return 0.0f;
+    const float t = __expf(-fabsf(g));
+    return __fdividef(t, 1.0f + t);
+}
+__device__ __forceinline__ float2 gate_from_smaller(int kind, float g, float small) {
+    if (kind == COLLAGE_GATE_NONE) return make_float2(g, 1.0f);
+    const float large = 1.0f - small, s = g < 0.0f ? small : large, rest = g < 0.0f ? large : small;
+    if (kind == COLLAGE_GATE_SIGMOID) return make_float2(s, s * rest);
+    if (fabsf(g) == INFINITY) return make_float2(g < 0.0f ? -0.0f : g, s);
+    return make_float2(g * s, __fmaf_rn(g * s, rest, s));
+}
 
 constexpr int kBlockThreads = 256;
 
@@ -518,6 +534,7 @@ struct BlockNormBackwardArgs {
     float alpha, beta;
     int activation, sums;                 // sums: bit 0 for pre_weight, bit 1 for post_weight and gates of channels
     int token_gate;
+    int from_x;                           // r is x (and ldr its rows' distance): the stream is formed anew
 };
 
 constexpr int kBlockParts = 320;          // blocks whose sums over rows are kept apart
@@ -534,18 +551,26 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
         const bool first = row == blockIdx.x;
         const float rstd_r = a.pre ? a.rstd_pre[row] : 0.0f, rstd_o = a.post ? a.rstd_post[row] : 1.0f;
         float mean_r = 0.0f, mean_o = 0.0f;
+        auto gate_of = [&](uint64_t j) { return bf16_value(a.gate[row * a.ldg + j]); };
+        auto stream = [&](uint64_t j) {
+            const float in = bf16_value(a.r[row * a.ldr + j]);
+            if (!a.from_x) return in;
+            float n = bf16_value(a.o[row * a.ldo + j]);
+            if (a.post) n = n * rstd_o * bf16_value(a.post[j]);
+            if (a.gate) n *= gate_value(a.activation, gate_of(j));
+            return __fmaf_rn(a.alpha, in, a.beta * n);
+        };
         if (a.pre) {
             float sum = 0.0f;
             for (uint64_t j = threadIdx.x; j < a.cols; j += kBlockThreads)
-                sum = __fmaf_rn(bf16_value(a.dy[row * a.lddy + j]) * bf16_value(a.pre[j]), bf16_value(a.r[row * a.ldr + j]) * rstd_r, sum);
+                sum = __fmaf_rn(bf16_value(a.dy[row * a.lddy + j]) * bf16_value(a.pre[j]), stream(j) * rstd_r, sum);
             mean_r = block_sum(sum, slots, kBlockThreads / 32) * per_col;
         }
         auto stream_grad = [&](uint64_t j) {
             float d = 0.0f;
-            if (a.pre) d = rstd_r * __fmaf_rn(-bf16_value(a.r[row * a.ldr + j]) * rstd_r, mean_r, bf16_value(a.dy[row * a.lddy + j]) * bf16_value(a.pre[j]));
+            if (a.pre) d = rstd_r * __fmaf_rn(-stream(j) * rstd_r, mean_r, bf16_value(a.dy[row * a.lddy + j]) * bf16_value(a.pre[j]));
             return a.dr ? d + bf16_value(a.dr[row * a.lddr + j]) : d;
         };
-        auto gate_of = [&](uint64_t j) { return bf16_value(a.gate[row * a.ldg + j]); };
         auto gated = [&](uint64_t j, float d) { return a.gate ? a.beta * d * gate_value(a.activation, gate_of(j)) : a.beta * d; };
         if (a.post && a.dblock) {
             float sum = 0.0f;
@@ -558,7 +583,7 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
             const float d = stream_grad(j), n = a.o ? bf16_value(a.o[row * a.ldo + j]) * rstd_o : 0.0f;
             const float du = gated(j, d), w = a.post ? bf16_value(a.post[j]) : 1.0f;
             if (a.sums & kSumPre) {
-                const float s = bf16_value(a.dy[row * a.lddy + j]) * (bf16_value(a.r[row * a.ldr + j]) * rstd_r);
+                const float s = bf16_value(a.dy[row * a.lddy + j]) * (stream(j) * rstd_r);
                 sum_pre[j] = first ? s : sum_pre[j] + s;
             }
             if (a.sums & kSumPost) {
@@ -573,8 +598,8 @@ __global__ void __launch_bounds__(kBlockThreads) block_norm_backward_any_kernel(
     }
 }
 
-// The same for rows that fit shared memory as floats, with the sums over the block's rows: each array is read once.  A thread has the same
-// columns in every pass.
+// The same for rows that fit shared memory as floats, with the sums over the block's rows: each array is read once (from x: o and the gate
+// twice).  A thread has the same columns in every pass.
 __global__ void __launch_bounds__(kStagedThreads) block_norm_backward_staged_kernel(const __grid_constant__ BlockNormBackwardArgs a) {
     __shared__ float slots[kStagedThreads / 32];
     extern __shared__ __align__(16) uint8_t dynamic[];
@@ -589,13 +614,22 @@ __global__ void __launch_bounds__(kStagedThreads) block_norm_backward_staged_ker
         const float rstd_r = a.dy ? a.rstd_pre[row] : 0.0f, rstd_o = a.post ? a.rstd_post[row] : 1.0f;
         float mean = 0.0f, sum = 0.0f;
         if (a.dy) {
-            each_column<3>(cols, {row_of(a.dy, a.lddy), row_of(a.r, a.ldr), a.pre}, [&](uint32_t j, const float (&v)[3]) {
-                const float no = v[1] * rstd_r, q = v[0] * v[2];
-                sum_pre[j] = __fmaf_rn(v[0], no, sum_pre[j]);
-                sum = __fmaf_rn(q, no, sum);
+            auto take = [&](uint32_t j, float dy, float r, float w) {
+                const float nr = r * rstd_r, q = dy * w;
+                sum_pre[j] = __fmaf_rn(dy, nr, sum_pre[j]);
+                sum = __fmaf_rn(q, nr, sum);
                 d[j] = q;
-                n[j] = no;
-            });
+                n[j] = nr;
+            };
+            const uint16_t *dy = row_of(a.dy, a.lddy), *r = row_of(a.r, a.ldr);
+            if (a.from_x)
+                each_column<6>(cols, {dy, r, a.pre, row_of(a.o, a.ldo), row_of(a.gate, a.ldg), a.post}, [&](uint32_t j, const float (&v)[6]) {
+                    float f = a.beta * (a.post ? v[5] : 1.0f);
+                    if (a.gate) f *= gate_value(a.activation, v[4]);
+                    take(j, v[0], __fmaf_rn(a.alpha, v[1], f * (v[3] * rstd_o)), v[2]);
+                });
+            else
+                each_column<3>(cols, {dy, r, a.pre}, [&](uint32_t j, const float (&v)[3]) { take(j, v[0], v[1], v[2]); });
             mean = block_sum(sum, slots, kStagedThreads / 32) * per_col;
         }
         sum = 0.0f;
@@ -639,7 +673,7 @@ static __device__ unsigned int g_block_norm_fault = 0;
 // them owns PER vectors of columns, worked on two elements an instruction, and keeps its columns' sums over rows in registers until the end.
 constexpr int kMaxGroups = 15, kMaxDepth = 4;
 
-template <int PER, bool TOKEN_GATE, int THREADS>
+template <int PER, bool TOKEN_GATE, bool FROM_X, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads, int depth) {
     constexpr int kArrays = TOKEN_GATE ? 5 : 4;
     __shared__ float slots[2][THREADS / 32];
@@ -722,7 +756,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
             alive = false;
             gave_up = row;
         }
-        const uint8_t* here = stages + stage * stage_bytes;
+        uint8_t* here = stages + stage * stage_bytes;
         auto vector = [&](int array, int i) {
             const int v = t + i * group_threads;
             return v < vectors ? reinterpret_cast<const uint4*>(here + array * row_bytes)[v] : none;
@@ -733,14 +767,45 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
             w[0] = lo.x; w[1] = lo.y; w[2] = hi.x; w[3] = hi.y;
         };
         uint64_t n[PER][4], d[PER][4];          // n of the stream, then of the block; the gradient on its way from y to the block
+        auto normed_block = [&](int i, uint64_t (&to)[4]) {
+            unpack_pairs(vector(3, i), to);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) to[p] = mul_pair(to[p], pair_of(rstd_o));
+        };
         float mean = 0.0f;
-        if (a.dy) {
+        if (FROM_X || a.dy) {
             uint64_t sum = 0;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 uint64_t dy[4], w[4];
                 unpack_pairs(vector(0, i), dy);
                 unpack_pairs(vector(1, i), n[i]);
+                if constexpr (FROM_X) {
+                    uint64_t no[4];
+                    normed_block(i, no);
+                    if constexpr (TOKEN_GATE) {
+                        uint64_t g[4];
+                        unpack_pairs(vector(4, i), g);
+                        unpack_pairs(qpost[i], w);
+                        float small[8];         // for the second pass, in the place of this thread's dy and x
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
+                            const float2 gf = floats_of(g[p]);
+                            small[2 * p] = gate_smaller(a.activation, gf.x);
+                            small[2 * p + 1] = gate_smaller(a.activation, gf.y);
+                            w[p] = mul_pair(mul_pair(w[p], pair_of(a.beta)),
+                                            pair_of(gate_from_smaller(a.activation, gf.x, small[2 * p]).x, gate_from_smaller(a.activation, gf.y, small[2 * p + 1]).x));
+                        }
+                        if (const int v = t + i * group_threads; v < vectors) {
+                            reinterpret_cast<float4*>(here)[v] = make_float4(small[0], small[1], small[2], small[3]);
+                            reinterpret_cast<float4*>(here + row_bytes)[v] = make_float4(small[4], small[5], small[6], small[7]);
+                        }
+                    } else {
+                        factors(post, i, w);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) n[i][p] = fma_pair(n[i][p], pair_of(a.alpha), mul_pair(no[p], w[p]));
+                }
                 factors(pre, i, w);
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
@@ -750,6 +815,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
                     sum = fma_pair(d[i][p], n[i][p], sum);
                 }
             }
+            if (TOKEN_GATE && FROM_X) pipe::fence_async_smem();        // (what was written to the stage, before a copy may come over it)
             mean = joined(sum_of(sum), 0) * per_col;
         }
         uint64_t sum = 0;
@@ -767,17 +833,29 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
                 reinterpret_cast<uint4*>(a.dx + row * a.lddx)[v] = pack_pairs(dx);
             }
             uint64_t w[4];
-            unpack_pairs(vector(3, i), n[i]);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) n[i][p] = mul_pair(n[i][p], pair_of(rstd_o));
+            normed_block(i, n[i]);
             if (TOKEN_GATE) {
                 uint64_t g[4];
                 unpack_pairs(vector(4, i), g);
                 unpack_pairs(qpost[i], w);
+                float parts[8];
+                if constexpr (FROM_X) {
+                    const uint4 lo = vector(0, i), hi = vector(1, i);
+                    const uint32_t words[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) parts[e] = __uint_as_float(words[e]);
+                }
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
                     const float2 gf = floats_of(g[p]);
-                    const float2 lo = gate_value_and_slope(a.activation, gf.x), hi = gate_value_and_slope(a.activation, gf.y);
+                    float2 lo, hi;
+                    if constexpr (FROM_X) {
+                        lo = gate_from_smaller(a.activation, gf.x, parts[2 * p]);
+                        hi = gate_from_smaller(a.activation, gf.y, parts[2 * p + 1]);
+                    } else {
+                        lo = gate_value_and_slope(a.activation, gf.x);
+                        hi = gate_value_and_slope(a.activation, gf.y);
+                    }
                     const uint64_t gated = mul_pair(d[i][p], pair_of(lo.x, hi.x));
                     sum_post[i][p] = fma_pair(gated, n[i][p], sum_post[i][p]);
                     w[p] = mul_pair(w[p], pair_of(a.beta));
@@ -858,7 +936,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
     }
 }
 
-template <int PER, bool TOKEN_GATE, int THREADS>
+template <int PER, bool TOKEN_GATE, bool FROM_X, int THREADS>
 static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
     const uint64_t v = a.cols >> 3;
     const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), most = std::max(1, std::min(THREADS / group, kMaxGroups));
@@ -869,17 +947,17 @@ static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a,
     // the stages hold the groups' sums in the end: 64 PER bytes a thread
     const size_t smem = std::max<size_t>(depth * row * groups, 64ull * PER * group * groups) + factors;
     *parts = static_cast<unsigned>(std::min<uint64_t>((a.rows + groups - 1) / groups, static_cast<uint64_t>(sm_count)));
-    return launch<&block_norm_backward_kernel<PER, TOKEN_GATE, THREADS>>(*parts, group * groups, 1, smem, s, a, group, depth);
+    return launch<&block_norm_backward_kernel<PER, TOKEN_GATE, FROM_X, THREADS>>(*parts, group * groups, 1, smem, s, a, group, depth);
 }
 // Rows of up to 256 columns are a warp's, without barriers; longer ones take two vectors a thread, half the joins of one.  Of rows that leave
 // many of 512 threads idle that way (and a second row has no registers) one vector a thread is faster: 2047 x 5120 with a gate for each
 // token 55 us against 76, 4096 x 6144 106 against 138, 8191 x 5120 without 119 against 128, but 8191 x 6144 141 against 133.
-template <bool TOKEN_GATE>
+template <bool TOKEN_GATE, bool FROM_X>
 static collage_status_t launch_block_backward(const BlockNormBackwardArgs& a, unsigned* parts, int sm_count, cudaStream_t s) {
-    if (a.cols <= 256) return launch_block_backward_as<1, TOKEN_GATE, 512>(a, parts, sm_count, s);
-    if (a.cols > 4096 && a.cols <= 5120) return launch_block_backward_as<1, TOKEN_GATE, 640>(a, parts, sm_count, s);
-    if (TOKEN_GATE && a.cols > 5120 && a.cols <= 6144) return launch_block_backward_as<1, TOKEN_GATE, 768>(a, parts, sm_count, s);
-    return launch_block_backward_as<2, TOKEN_GATE, 512>(a, parts, sm_count, s);
+    if (a.cols <= 256) return launch_block_backward_as<1, TOKEN_GATE, FROM_X, 512>(a, parts, sm_count, s);
+    if (a.cols > 4096 && a.cols <= 5120) return launch_block_backward_as<1, TOKEN_GATE, FROM_X, 640>(a, parts, sm_count, s);
+    if (TOKEN_GATE && a.cols > 5120 && a.cols <= 6144) return launch_block_backward_as<1, TOKEN_GATE, FROM_X, 768>(a, parts, sm_count, s);
+    return launch_block_backward_as<2, TOKEN_GATE, FROM_X, 512>(a, parts, sm_count, s);
 }
 
 // The blocks' parts added up in order: 32 columns a block, each of its 32 warps takes every 32nd part.  From the shared sum
@@ -1013,10 +1091,13 @@ collage_status_t collage_block_norm(const collage_block_norm_t* in, const collag
 
 size_t collage_block_norm_workspace_bytes(uint64_t cols) { return static_cast<size_t>(kBlockParts) * 8 * cols; }
 
-collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
-                                             const collage_matrix_t* r, const float* rstd_post, const float* rstd_pre,
-                                             const collage_matrix_t* dx, const collage_matrix_t* dblock, const collage_matrix_t* dgate,
-                                             void* dpost_weight, void* dpre_weight, void* workspace, size_t workspace_bytes, void* stream) {
+}  // extern "C"
+
+// Both entry points; `r` is x if from_x.
+static collage_status_t block_norm_backward(const collage_block_norm_t* in, bool from_x, const collage_matrix_t* dy, const collage_matrix_t* dr,
+                                            const collage_matrix_t* r, const float* rstd_post, const float* rstd_pre, const collage_matrix_t* dx,
+                                            const collage_matrix_t* dblock, const collage_matrix_t* dgate, void* dpost_weight, void* dpre_weight,
+                                            void* workspace, size_t workspace_bytes, void* stream) {
     if (!in) return COLLAGE_ERR_NULL;
     const collage_matrix_t* o = &in->block;
     const uint64_t rows = o->rows, cols = o->cols;
@@ -1071,6 +1152,7 @@ collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, con
         set(r, a.r, a.ldr);
         a.pre = static_cast<const uint16_t*>(in->pre_weight);
         a.rstd_pre = rstd_pre;
+        a.from_x = from_x;
     }
     set(o, a.o, a.ldo);
     if (has_gate(in)) { a.gate = static_cast<const uint16_t*>(in->gate.data); a.ldg = in->gate.rows == 1 ? 0 : in->gate.ld; }
@@ -1095,8 +1177,10 @@ collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, con
         st = launch<&block_norm_backward_staged_kernel>(parts, kStagedThreads, 1, 16 * cols, s, a);
     else if (!fit)
         st = launch<&block_norm_backward_any_kernel>(parts, kBlockThreads, 1, 0, s, a);
+    else if (a.from_x)
+        st = a.token_gate ? launch_block_backward<true, true>(a, &parts, dev.sm_count, s) : launch_block_backward<false, true>(a, &parts, dev.sm_count, s);
     else
-        st = a.token_gate ? launch_block_backward<true>(a, &parts, dev.sm_count, s) : launch_block_backward<false>(a, &parts, dev.sm_count, s);
+        st = a.token_gate ? launch_block_backward<true, false>(a, &parts, dev.sm_count, s) : launch_block_backward<false, false>(a, &parts, dev.sm_count, s);
     if (st != COLLAGE_OK || !sums) return st;
     BlockNormFinishArgs f = {};
     f.partial = a.partial;
@@ -1112,6 +1196,22 @@ collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, con
     const uint32_t column_blocks = static_cast<uint32_t>((cols + 31) / 32);
     const int kinds = (sums & kSumPre ? 1 : 0) + (sums & kSumPost ? 1 : 0);
     return launch<&block_norm_finish_kernel>(static_cast<uint64_t>(column_blocks) * kinds, kBlockFinish, 1, 0, s, f, column_blocks, sums & kSumPre ? 0 : 1);
+}
+
+extern "C" {
+
+collage_status_t collage_block_norm_backward(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
+                                             const collage_matrix_t* r, const float* rstd_post, const float* rstd_pre,
+                                             const collage_matrix_t* dx, const collage_matrix_t* dblock, const collage_matrix_t* dgate,
+                                             void* dpost_weight, void* dpre_weight, void* workspace, size_t workspace_bytes, void* stream) {
+    return block_norm_backward(in, false, dy, dr, r, rstd_post, rstd_pre, dx, dblock, dgate, dpost_weight, dpre_weight, workspace, workspace_bytes, stream);
+}
+
+collage_status_t collage_block_norm_backward_from_x(const collage_block_norm_t* in, const collage_matrix_t* dy, const collage_matrix_t* dr,
+                                                    const collage_matrix_t* x, const float* rstd_post, const float* rstd_pre,
+                                                    const collage_matrix_t* dx, const collage_matrix_t* dblock, const collage_matrix_t* dgate,
+                                                    void* dpost_weight, void* dpre_weight, void* workspace, size_t workspace_bytes, void* stream) {
+    return block_norm_backward(in, true, dy, dr, x, rstd_post, rstd_pre, dx, dblock, dgate, dpost_weight, dpre_weight, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
