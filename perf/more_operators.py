@@ -440,9 +440,10 @@ def _own(s):
     if case["backward"]:
         if "workspace" not in s:                # scratch that a training program allocates once
             s["workspace"] = torch.empty(B.block_norm_workspace_bytes(case["cols"]), dtype=torch.uint8, device="cuda")
-        B.block_norm_backward(s["dy"], s["r"], s["block"], s["rstd_post"], s["rstd_pre"], s["dx"], s["dblock"], dr=s["dr"], gate=s["gate"],
+        B.block_norm_backward(s["dy"], None, s["block"], s["rstd_post"], s["rstd_pre"], s["dx"], s["dblock"], dr=s["dr"], gate=s["gate"],
                               post_weight=s["post"], pre_weight=s["pre"], dgate=s["dgate"], dpost_weight=s["dpost"], dpre_weight=s["dpre"],
-                              workspace=s["workspace"], residual_scale=s["residual_scale"], block_scale=s["block_scale"], activation=act)
+                              workspace=s["workspace"], residual_scale=s["residual_scale"], block_scale=s["block_scale"], activation=act,
+                              x=s["x"])     # (still there: r has an array of its own)
         out.update({n: s[n] for n in ("dx", "dblock", "dpost", "dpre", "dgate") if s[n] is not None})
     return out
 
