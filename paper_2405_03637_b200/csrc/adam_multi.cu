@@ -845,7 +845,8 @@ collage_status_t create(const collage_adam_tensor_t* tensors, int num, int state
                         cudaMalloc(&plan->d_tiles, tiles.size() * sizeof(AdamChunk)) != cudaSuccess ||
                         cudaMemcpy(plan->d_tiles, tiles.data(), tiles.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(plan->d_tensors, recs.data(), recs.size() * sizeof(AdamRec), cudaMemcpyHostToDevice) != cudaSuccess ||
-                        cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess))) {
+                        cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice) != cudaSuccess ||
+                        tables_landed() != cudaSuccess))) {
         delete plan;
         return COLLAGE_ERR_CUDA;
     }

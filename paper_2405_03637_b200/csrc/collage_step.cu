@@ -989,7 +989,8 @@ collage_status_t collage_plan_create(const collage_tensor_t* tensors, int num, u
             cudaMemcpy(plan->d_sizes, sizes.data(), sizes.size() * sizeof(uint64_t), cudaMemcpyHostToDevice) !=
                 cudaSuccess ||
             cudaMemcpy(plan->d_orig_index, orig_index.data(), orig_index.size() * sizeof(uint32_t),
-                       cudaMemcpyHostToDevice) != cudaSuccess) {
+                       cudaMemcpyHostToDevice) != cudaSuccess ||
+            tables_landed() != cudaSuccess) {
             cudaFree(plan->d_tensors);
             cudaFree(plan->d_chunks);
             cudaFree(plan->d_first_chunk);

@@ -51,6 +51,10 @@ inline collage_status_t current_device(DeviceInfo* out) {
     return out->cc_major == 10 ? COLLAGE_OK : COLLAGE_ERR_ARCH;
 }
 
+// Waits for the copies that a plan's tables are made by.  cudaMemcpy from pageable memory may return when the source has been read, with the
+// bytes still under way on the legacy stream, for which a step on a stream that does not block with that one would not wait.
+inline cudaError_t tables_landed() { return cudaStreamSynchronize(cudaStreamLegacy); }
+
 // Byte ranges [begin, end) of the arrays of one call; overlap of any two is an error.
 struct ByteRange {
     uintptr_t begin, end;
