@@ -657,7 +657,8 @@ collage_status_t collage_preference_loss(const collage_preference_t* in, float* 
  *                               where v' is not 0, rounded down to a multiple of its spacing s after s * d has been added, 0 <= d < 1
  *                               random (448 at most).  The root moves by less than a code's step in a step of beta2 = 0.999; rounding to nearest would never
  *                               move it.  A group whose largest |m'| (or sqrt(v')) is below 2^-100 is stored as zeros with scale 0.
- *                               A gradient whose square is no finite float makes its group's states NaN from then on.
+ *                               A gradient whose square is no finite float makes its group's roots NaN from then on, and the group's
+ *                               parameters from the next step at the latest.  (Of F32 it makes v infinite, and the quotient 0 while m is finite.)
  * d has 16 bits, of a fixed function of seed, step and position: with mix(x) on 32 bits x ^= x >> 16, x *= 0x6A09E667,
  * x ^= x >> 15, x *= 0xB504F333, x ^= x >> 16 and key = mix(seed_lo + mix(seed_hi + mix(step_lo + mix(step_hi)))), element P of
  * the plan has the lower (even P) or upper half of mix(lo + mix(hi + key)), where hi and lo are the words of P / 2.  A plan counts its

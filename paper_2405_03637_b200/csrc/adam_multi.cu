@@ -15,6 +15,7 @@
 #include "bulk_pipe.cuh"
 #include "ops_common.cuh"
 
+#include <cfloat>
 #include <new>
 
 namespace collage {
@@ -82,13 +83,15 @@ __device__ __forceinline__ uint64_t e4m3_pair(uint32_t two) {
 }
 
 // Square roots: y = rsqrt(v) gives r = v y, and a step of Newton's method on r^2 = v, whose remainder r^2 - v is exact in an fma, the
-// correctly rounded root but for a few in a million (in half the instructions of one that always is).
+// correctly rounded root but for a few in a million (in half the instructions of one that always is).  ANY: of infinity too (r from the largest
+// float and the remainder from v; else a NaN, as infinity times 0).
+template <bool ANY>
 __device__ __forceinline__ uint64_t root_pair(uint64_t v) {
-    const float2 f = floats_of(v);
+    const float2 f = floats_of(v), most = ANY ? make_float2(fminf(f.x, FLT_MAX), fminf(f.y, FLT_MAX)) : f;
     float2 y;
-    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(f.x, 0x1p-149f)));         // (of 0: 0 times a finite number)
-    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(f.y, 0x1p-149f)));
-    const uint64_t y2 = pair_of(y.x, y.y), r = mul_pair(v, y2);
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(most.x, 0x1p-149f)));      // (of 0: 0 times a finite number)
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(most.y, 0x1p-149f)));
+    const uint64_t y2 = pair_of(y.x, y.y), r = mul_pair(pair_of(most.x, most.y), y2);
     const float2 q = floats_of(r);
     return pair_of(__fmaf_rn(__fmaf_rn(-q.x, q.x, f.x), 0.5f * y.x, q.x), __fmaf_rn(__fmaf_rn(-q.y, q.y, f.y), 0.5f * y.y, q.y));
 }
@@ -100,18 +103,18 @@ __device__ __forceinline__ uint64_t reciprocal_pair(uint64_t v) {
 }
 
 // A step of two elements' states: m', and sqrt(v') or v' itself.  Every product and sum is rounded once, so that codes hang on nothing but the
-// formulas.  Returns sqrt(v').
+// formulas.  Returns sqrt(v').  (With states in 8 bits an infinite v' makes its group NaN in any case.)
 template <int STATE>
 __device__ __forceinline__ uint64_t advance(uint64_t& m, uint64_t& v, uint64_t g, const AdamScalars& k) {
     const uint64_t squared = STATE == COLLAGE_STATE_F32 ? v : mul_pair(v, v);
     m = add_rounded(scaled_pair(m, k.f.b1), scaled_pair(g, k.f.c1));
     v = add_rounded(scaled_pair(squared, k.f.b2), scaled_pair(mul_pair(g, g), k.f.c2));
-    return root_pair(v);
+    return root_pair<STATE == COLLAGE_STATE_F32>(v);
 }
 // The update of parameters x to a few units of its last place.
 template <bool INSIDE>
 __device__ __forceinline__ uint64_t update_of(uint64_t m, uint64_t v, uint64_t root, uint64_t x, const AdamScalars& k) {
-    const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : scaled_plus(root, k.inv_root_bc2, k.f.eps);
+    const uint64_t den = INSIDE ? root_pair<true>(scaled_plus(v, k.inv_bc2, k.f.eps)) : scaled_plus(root, k.inv_root_bc2, k.f.eps);
     return scaled_plus(x, k.decay, scaled_pair(mul_pair(m, reciprocal_pair(den)), k.rate));
 }
 
@@ -120,17 +123,20 @@ __device__ __forceinline__ uint64_t update_of(uint64_t m, uint64_t v, uint64_t r
 // rest' what that lacks.  The sum is known here as s + low to about 2^-24 of the decay's part and far less of the rest's: q by Markstein's division
 // (a reciprocal by a step of Newton's method, the quotient's remainder exact in an fma), its product with a (two floats) with the
 // product's remainder, and sums with their remainders (TwoSum).
+// ANY: the divisor may be infinite (its reciprocal is 0; remainders by the largest float leave the quotient 0, and a NaN of an infinite m).
 struct PairSum {
     uint64_t s, low;
 };
-template <bool INSIDE>
+template <bool INSIDE, bool ANY>
 __device__ __forceinline__ PairSum sum_of_pair(uint64_t theta, uint64_t rest, uint64_t m, uint64_t v, uint64_t root, const AdamScalars& k) {
-    const uint64_t den = INSIDE ? root_pair(scaled_plus(v, k.inv_bc2, k.f.eps)) : add_rounded(scaled_pair(root, k.inv_root_bc2), pair_of(k.f.eps));
+    const uint64_t den = INSIDE ? root_pair<true>(scaled_plus(v, k.inv_bc2, k.f.eps)) : add_rounded(scaled_pair(root, k.inv_root_bc2), pair_of(k.f.eps));
     const uint64_t num = scaled_pair(m, k.inv_bc1);
-    const float2 d = floats_of(den), n = floats_of(num);
+    float2 d = floats_of(den);
+    const float2 n = floats_of(num);
     float2 r;
     asm("rcp.approx.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
     asm("rcp.approx.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+    if (ANY) d = make_float2(fminf(d.x, FLT_MAX), fminf(d.y, FLT_MAX));
     const uint64_t r0 = pair_of(r.x, r.y), r1 = fma_pair(pair_of(__fmaf_rn(-d.x, r.x, 1.0f), __fmaf_rn(-d.y, r.y, 1.0f)), r0, r0);
     const float2 q0 = floats_of(mul_pair(num, r1));
     const uint64_t q = fma_pair(pair_of(__fmaf_rn(-d.x, q0.x, n.x), __fmaf_rn(-d.y, q0.y, n.y)), r1, pair_of(q0.x, q0.y));
@@ -177,7 +183,7 @@ __device__ __forceinline__ bool update(Octet& o, const AdamScalars& k, float gra
         const uint64_t g = scaled_pair(o.g[p], grad_scale);
         if (REST == COLLAGE_REST_BF16) {
             const uint64_t root = advance<STATE>(o.m[p], o.v[p], g, k);
-            const PairSum sum = sum_of_pair<INSIDE>(o.theta[p], o.rest[p], o.m[p], o.v[p], root, k);
+            const PairSum sum = sum_of_pair<INSIDE, INSIDE || STATE == COLLAGE_STATE_F32>(o.theta[p], o.rest[p], o.m[p], o.v[p], root, k);
             if (STATE == COLLAGE_STATE_E4M3) o.v[p] = root;
             split_pair(sum, o.theta_out[p], o.rest_out[p]);
             const float2 s = floats_of(sum.s);
