@@ -5,8 +5,8 @@
 //   policy: coef = w (-A ratio [the unclipped term is the minimum] - kl_weight (exp(k) - 1))
 //
 // All of it is bound by memory, and the policy loss by a row's two passes too, the second of which comes from L2.  Measured: log-probabilities of
-// 4096 x 32000 bfloat16 49 us (5.4 TB/s), their backward pass 84 us (6.2), the policy loss with its gradient 101 us (5.2 TB/s for one read and one
-// write); 2049 x 50257 44, 69 and 96 us.
+// 4096 x 32000 bfloat16 49 us (5.3 TB/s), their backward pass 84 us (6.2), the policy loss with its gradient 104 us (5.0 TB/s for one read and one
+// write); 2049 x 50257 43, 69 and 96 us.
 // Rows are taken relative to their largest logit before the division by t, as in distillation.  What a row's loss needs besides is a
 // handful of scalars, which one thread computes in 64 bits: a log-probability of -10 in float would leave the ratio and the KL term
 // (a difference of nearly equal numbers) only five digits.
@@ -63,39 +63,76 @@ __device__ __forceinline__ PolicyRow policy_row(const TokenArgs& a, uint64_t row
     return {w * loss, kl, w * coef};
 }
 
-// Adds exp((f - m) / t) over a vector to `total`, with log2(e) / t in two floats: what the first one lacks would shift the log-probabilities of
-// all tokens the same way, which a sequence's sum adds up.
+// A warp's exponentials are relative to its largest logit so far, or to one that is less than 2^kLag times as likely, so that sums are hardly ever
+// rescaled.  (A larger lag would need larger offsets, in which the smaller part of log2(e) / t is lost.)
+constexpr float kLag = 1.0f;
+
+// The hardware's 2^x is off by up to 1.5e-7, for x < 0 too low by 5.0e-8 on average (for x > 0 too high by 3.3e-8), and for a given x the same way
+// each time: a row's sum would carry the average, or, of a row of few values, the errors of these.  So each thread takes its exponentials at an
+// offset of its own, 2^(x + offset) with x + offset <= 0, and divides its sum by what the hardware gives for 2^offset.  The logit that all are
+// relative to counts exactly 1; others have the difference of two errors, whose mean over offsets is 0 for any x, and a row's sum has the mean over
+// its threads.  Multiples of the golden ratio, less their whole part, are evenly spread for 64 threads as for 256 and have no period
+// in common with the hardware's intervals.
+__device__ __forceinline__ float exp_offset(uint32_t thread) { return -kLag - static_cast<float>(thread * 0x9E3779B9u >> 8) * 0x1p-24f; }
+
+// Sum of 2^offset exp((f - m) / t) over a vector, with log2(e) / t in two floats: what the first one lacks would shift the log-probabilities of
+// all tokens the same way, which a sequence's sum adds up.  Sums go by twos, here and over vectors, so that a large term meets few roundings and
+// equal terms meet none.
 template <typename T>
-__device__ __forceinline__ void add_exact_exps(const uint4& q, float m, const TokenArgs& a, uint64_t& total) {
-    uint64_t f[Vec<T>::kPairs];
+__device__ __forceinline__ uint64_t offset_exps(const uint4& q, float m, float offset, const TokenArgs& a) {
+    constexpr uint32_t kPairs = Vec<T>::kPairs;
+    uint64_t f[kPairs];
     Vec<T>::unpack(q, f);
     const float minus_m = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
-    for (uint32_t i = 0; i < Vec<T>::kPairs; ++i) {
+    for (uint32_t i = 0; i < kPairs; ++i) {
         const uint64_t d = add_pair(f[i], pair_of(minus_m));
-        const float2 x = floats_of(fma_pair(d, pair_of(a.c), mul_pair(d, pair_of(a.c_rest))));
-        total = add_pair(total, pair_of(fast_exp2(x.x), fast_exp2(x.y)));
+        const float2 x = floats_of(fma_pair(d, pair_of(a.c), fma_pair(d, pair_of(a.c_rest), pair_of(offset))));
+        f[i] = pair_of(fast_exp2(x.x), fast_exp2(x.y));
     }
+    if constexpr (kPairs == 4)
+        return add_pair(add_pair(f[0], f[1]), add_pair(f[2], f[3]));
+    else
+        return add_pair(f[0], f[1]);
 }
 
-// A part's sum, relative to its own maximum m, as one relative to `to`.
-__device__ __forceinline__ float rescaled(float s, float m, float to, const TokenArgs& a) {
-    const float d = m - to;
-    return m == to ? s : m == -INFINITY ? (s != s ? s : 0.0f) : s * exp2f(__fmaf_rn(d, a.c, d * a.c_rest));
+// s / d for 2^-3 < d <= 1, by Newton's reciprocal and the quotient's remainder: 1 where they are equal.
+__device__ __forceinline__ float quotient(float s, float d) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    const float q = s * r;
+    return __fmaf_rn(__fmaf_rn(-q, d, s), r, q);
 }
 
-// By how much the hardware's 2^x is too low on average (measured: log-probabilities of 15 to 3700 rows of 1299 to 76386 logits, temperatures 0.7
-// to 1.3, were too high by 8.5e-8 to 1.3e-7, with a spread of 5e-8).  The row's largest logit, whose exponential is 1, has no part in that.
-constexpr double kExpLow = 1.05e-7;
+// What a sum relative to m is taken times to be relative to `to`: 2^x, x = (m - to) log2(e) / t = n + f with a whole n and |f| <= 1/2, and 2^f by its
+// Taylor series, the sum of (f ln 2)^k / k!, whose terms from the eighth on are below 2^-27.  Correct but for a rounding or two, both ways.  (A sum
+// of nothing is 0 or, of NaN alone, NaN; so it is times 0.)
+__device__ __forceinline__ float factor_to(float m, float to, const TokenArgs& a) {
+    if (m == to) return 1.0f;
+    const float d = m - to, n = rintf(__fmaf_rn(d, a.c, d * a.c_rest));
+    if (n < -125.0f) return 0.0f;
+    const float f = __fmaf_rn(d, a.c_rest, __fmaf_rn(d, a.c, -n));
+    float p = 1.52527338e-5f;                    // ln(2)^7 / 7!
+    p = __fmaf_rn(p, f, 1.54035304e-4f);
+    p = __fmaf_rn(p, f, 1.33335581e-3f);
+    p = __fmaf_rn(p, f, 9.61812911e-3f);
+    p = __fmaf_rn(p, f, 5.55041087e-2f);
+    p = __fmaf_rn(p, f, 2.40226507e-1f);
+    p = __fmaf_rn(p, f, 6.93147181e-1f);
+    p = __fmaf_rn(p, f, 1.0f);
+    return __uint_as_float(__float_as_uint(p) + (static_cast<uint32_t>(static_cast<int>(n)) << 23));
+}
 
 struct TokenShared {
-    float2 warp[8];
+    float2 warp[8];                      // what each warp's sum is relative to, and the sum
+    float top[8];                        // its maximum
     float2 part[kTokenCluster];          // (maximum, sum) of each block of the cluster
     float coef, scale, at_target;
 };
 
 // A row by a cluster of blocks, each with a slice of it that it streams from global memory, once for maximum and sum and once for
-// the gradient.
+// the gradient.  Log-probabilities with 2048 threads on an SM have 32 registers and spill a few; with 1536 they are as fast (2049 x 50257 42.4 us, not
+// 42.5; 4096 x 32000 48.5, not 48.9; in float 81.0, not 87.5) but for rows of a turn or two (8192 x 8192 38.8, not 35.8).
 template <typename T, int MODE, int THREADS>
 __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREADS) token_kernel(const __grid_constant__ TokenArgs a) {
     using V = Vec<T>;
@@ -166,40 +203,48 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
     } else {
         if (a.cluster > 1) umma::cluster_arrive_all();                       // this block runs
         // maximum and sum of this thread's vectors, joined over the warp, the block and the cluster
+        float from = -INFINITY;                 // what this warp's exponentials are relative to
         m = -INFINITY;
         uint64_t total = 0;
+        const float offset = exp_offset(rank * THREADS + threadIdx.x);
         auto take = [&](const uint4 (&q)[kAhead]) {
             typename V::Most most = V::lowest();
 #pragma unroll
             for (uint32_t i = 0; i < kAhead; ++i) most = V::most(most, q[i]);
-            const float to = fmaxf(m, V::most_value(most));
-            if (to != m) {                  // a new maximum: what is summed so far is taken relative to it
-                const float2 so_far = floats_of(total);
-                total = pair_of(rescaled(so_far.x, m, to, a), rescaled(so_far.y, m, to, a));
-                m = to;
+            m = fmaxf(m, V::most_value(most));
+            if (__any_sync(0xFFFFFFFFu, (m - from) * a.c > kLag)) {
+                const float to = warp_max(m);
+                total = mul_pair(total, pair_of(factor_to(from, to, a)));
+                from = to;
             }
+            uint64_t part[kAhead];
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i) add_exact_exps<T>(q[i], m, a, total);
+            for (uint32_t i = 0; i < kAhead; ++i) part[i] = offset_exps<T>(q[i], from, offset, a);
+            total = add_pair(total, add_pair(add_pair(part[0], part[1]), add_pair(part[2], part[3])));
         };
-        for (uint32_t v = whole + threadIdx.x; v < whole_end; v += THREADS * kAhead) {
+        for (uint32_t v = whole + threadIdx.x; v - lane < whole_end; v += THREADS * kAhead) {          // (as many turns for all of a warp)
             uint4 q[kAhead];
 #pragma unroll
             for (uint32_t i = 0; i < kAhead; ++i) q[i] = v + i * THREADS < whole_end ? z.base[v + i * THREADS] : lowest;
             take(q);
         }
-        if (threadIdx.x ? threadIdx.x == 1 && whole_end < end : whole > first) {       // cut vectors: one thread for each
-            uint4 q[kAhead] = {z.edge(threadIdx.x ? end - 1 : first), lowest, lowest, lowest};
+        if (warp == 0 && (whole > first || whole_end < end)) {       // cut vectors: one thread for each
+            uint4 q[kAhead] = {lowest, lowest, lowest, lowest};
+            if (lane == 0 && whole > first) q[0] = z.edge(first);
+            if (lane == 1 && whole_end < end) q[0] = z.edge(end - 1);
             take(q);
         }
         const float2 sums = floats_of(total);
-        float sum = sums.x + sums.y;
-        const float most = warp_max(m);
-        sum = warp_sum(rescaled(sum, m, most, a));
-        if (lane == 0) sh.warp[warp] = make_float2(most, sum);
+        float sum = warp_sum(quotient(sums.x + sums.y, fast_exp2(offset)));
+        m = warp_max(m);
+        if (lane == 0) {
+            sh.warp[warp] = make_float2(from, sum);
+            sh.top[warp] = m;
+        }
         __syncthreads();
         const float2 of_warp = lane < THREADS / 32 ? sh.warp[lane] : make_float2(-INFINITY, 0.0f);
-        m = warp_max(of_warp.x);
-        sum = warp_sum(rescaled(of_warp.y, of_warp.x, m, a));
+        m = warp_max(lane < THREADS / 32 ? sh.top[lane] : -INFINITY);
+        sum = warp_sum(of_warp.y * factor_to(of_warp.x, m, a));
         if (a.cluster > 1) {
             umma::cluster_wait_all();           // all blocks of the row run
             if (threadIdx.x < a.cluster) {
@@ -209,13 +254,13 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
             umma::cluster_sync_any();           // (also: the whole row has been read before any of it is overwritten)
             const float2 r = lane < a.cluster ? sh.part[lane] : make_float2(-INFINITY, 0.0f);
             m = warp_max(r.x);
-            sum = warp_sum(rescaled(r.y, r.x, m, a));
+            sum = warp_sum(r.y * factor_to(r.x, m, a));
         }
         if (m == -INFINITY) sum = NAN;          // a row without any number in it has no distribution
         scale = 1.0f / sum;
         coef = 0.0f;
         if (threadIdx.x == 0 && (MODE == kPolicy || rank == 0)) {
-            const double logp = (static_cast<double>(at_target) - static_cast<double>(m)) * a.inv_t - log(sum + (static_cast<double>(sum) - 1.0) * kExpLow);
+            const double logp = (static_cast<double>(at_target) - static_cast<double>(m)) * a.inv_t - log(static_cast<double>(sum));
             if (rank == 0 && a.logp) a.logp[row] = static_cast<float>(logp);
             if (MODE == kLogp && a.logp_rest) {      // (of an infinite one nothing is missing)
                 const float rest = static_cast<float>(logp - static_cast<double>(static_cast<float>(logp)));
