@@ -30,7 +30,8 @@ struct TokenArgs {
     float *logp, *logp_rest, *stats, *loss, *kl;
     uint64_t ldz, ldd;
     double inv_t;
-    float c, c_rest, inv_tf;                     // log2(e) / t and what it lacks, 1 / t
+    float c, c_rest, inv_tf;                     // log2(e) / t rounded down and what it lacks, 1 / t
+    float c_near;                                // log2(e) / t to nearest, for gradients: half a unit off, as the products with it are
     float clip_low, clip_high, kl_weight;        // bounds of the ratio
     uint32_t vocab, slice, cluster;              // slice: 16-byte vectors of a row for one block; cluster: blocks of a row
     int target_bytes;
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
         return;
     }
     const float minus = -gain * scale;
-    const uint64_t m2 = pair_of(-m, -m), c2 = pair_of(a.c, a.c), g2 = pair_of(minus, minus);
+    const uint64_t m2 = pair_of(-m, -m), c2 = pair_of(a.c_near, a.c_near), g2 = pair_of(minus, minus);
     write_row(true, [&](uint64_t f) {
         const float2 e = exps(f, m2, c2);
         return mul_pair(g2, pair_of(e.x, e.y));
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLogp ? 2048 : 1280) / THREA
     const uint32_t vy = (static_cast<uint32_t>(y) + z.off) / kN;
     if (vy < first || vy >= end) return;
     __syncthreads();                        // the dense part is written; now the target over it
-    if (threadIdx.x == 0) dz.row[y] = V::rounded(__fmaf_rn(minus, fast_exp2((at_target - m) * a.c), gain));
+    if (threadIdx.x == 0) dz.row[y] = V::rounded(__fmaf_rn(minus, fast_exp2((at_target - m) * a.c_near), gain));
 }
 
 template <typename T, int MODE>
@@ -457,6 +458,7 @@ static collage_status_t prepare_tokens(const collage_tokens_t* in, const RowArra
     out->inv_t = inv_t;
     out->inv_tf = static_cast<float>(inv_t);
     out->c = c;
+    out->c_near = near_c;
     out->c_rest = std::max(static_cast<float>(exact_c - c), std::numeric_limits<float>::denorm_min());
     return COLLAGE_OK;
 }
