@@ -623,6 +623,7 @@ collage_status_t collage_policy_loss_and_grad(const collage_tokens_t* in, const 
  *   log_ratio_p = S_2p - S_2p+1,   h = beta * log_ratio_p - margin
  *   loss_p = pair_weight_p * (-(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h))
  *   grad_logp = the gradient of sum_p loss_p; 0 in rows without a target and in rows of no sequence.
+ * A pair of weight 0 takes no part: its loss and gradients are 0 whatever its log-probabilities are (log_ratio is what it is).
  * offsets ascend within [0, rows]; others are taken into that range and a sequence that would end before it begins as empty (then
  * the gradients of rows that several sequences or none would own are undefined).  Sums are in 64 bits and in a fixed order. */
 typedef struct collage_preference {

@@ -393,10 +393,11 @@ __global__ void __launch_bounds__(kPreferenceThreads) preference_kernel(const __
             loss += a.smoothing * (both + (h > 0.0 ? h : h == h ? 0.0 : h));
             slope += a.smoothing * (h > 0.0 ? 1.0 - small : small);
         }
-        a.loss[p] = static_cast<float>(w * loss);
+        // a pair of weight 0 takes no part, whatever its log-probabilities are
+        a.loss[p] = w == 0.0 ? 0.0f : static_cast<float>(w * loss);
         if (a.log_ratio) a.log_ratio[p] = static_cast<float>(log_ratio);
-        of_row[0] = static_cast<float>(w * a.beta * slope * per[0]);
-        of_row[1] = static_cast<float>(-w * a.beta * slope * per[1]);
+        of_row[0] = w == 0.0 ? 0.0f : static_cast<float>(w * a.beta * slope * per[0]);
+        of_row[1] = w == 0.0 ? 0.0f : static_cast<float>(-w * a.beta * slope * per[1]);
     }
     if (!a.grad_logp) return;
     __syncthreads();
