@@ -100,7 +100,7 @@ class Policy:
         return self.logp.clone()
 
     def preference_step(self, ids, target, offsets, ref_logp, beta):
-        """Loss of pairs of answers and its gradients."""
+        """Losses of pairs of answers, each over their number, and their gradients."""
         self.forward(ids)
         new = lambda *s: torch.empty(s, dtype=F32, device="cuda")  # noqa: E731
         stats, rest, grad, loss = new(self.tokens, 2), new(self.tokens), new(self.tokens), new(offsets.numel() // 2)
@@ -117,7 +117,7 @@ class Policy:
 
 
 def run(steps=60, tokens=512, width=256, ffn=640, layers=2, vocab=4099, lr=2e-3, pairs=8, seed=0):
-    """Mean reward of the sampled tokens after each step on rewards, and the pairs' loss after each of half as many on preferences."""
+    """Share of good answers among the sampled tokens before each step on rewards, and the pairs' mean loss before each of half as many on preferences."""
     policy = Policy(tokens, width, ffn, layers, vocab, seed)
     g = torch.Generator(device="cuda").manual_seed(seed + 1)
     known = min(64, vocab)                                                          # tokens that occur
@@ -149,7 +149,7 @@ def run(steps=60, tokens=512, width=256, ffn=640, layers=2, vocab=4099, lr=2e-3,
     B.adam_plan_destroy(policy.plan)
     if code := B.pipeline_fault():                                                  # (waits for the GPU: at the end, or at a checkpoint)
         raise RuntimeError(f"a kernel gave up a wait (code {code}): weights and losses are undefined")
-    return [x.item() for x in rewards], [x.item() / pairs for x in losses]
+    return [x.item() for x in rewards], [x.item() for x in losses]
 
 
 if __name__ == "__main__":
