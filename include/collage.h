@@ -633,7 +633,7 @@ typedef struct collage_preference {
     const void* target;              /* of collage_tokens_t, with its vocab: which rows count                */
     const void* offsets;             /* DEVICE int32_t or int64_t [2 * pairs + 1] (offset_bytes = 4 or 8)    */
     const float* pair_weight;        /* DEVICE float[pairs] or NULL: ones                                    */
-    uint64_t rows, vocab, pairs;     /* below 2^31 (ERR_LIMIT)                                               */
+    uint64_t rows, vocab, pairs;     /* rows and vocab below 2^31, pairs below 2^30 (ERR_LIMIT)              */
     uint32_t target_bytes, offset_bytes;
     double beta, margin, label_smoothing;      /* finite in float; 0 <= label_smoothing <= 1                 */
     int average;
@@ -648,13 +648,17 @@ collage_status_t collage_preference_loss(const collage_preference_t* in, float* 
  *   x' = x - lr (m' / (1 - beta1^t) / (sqrt(v' / (1 - beta2^t)) + eps) + weight_decay x)
  * The parameter, by `rest`: NONE  x = theta, theta' = RN_bf16(x');
  *                           BF16  x = theta + rest, a pair as in option B: theta' = RN_bf16(x'), rest' = RN_bf16(x' - theta'),
- *                                 with x' as the sum of theta, rest, -lr weight_decay x and -lr q, none of them rounded but q, the
- *                                 float quotient of the moments' means, so that theta' is the nearest value;
+ *                                 with x' as the sum of theta, rest, -lr q and the decay.  q is the float quotient of RN(m' k1) and
+ *                                 RN(RN(sqrt(v') k2) + eps), or of RN(m' k1) and sqrt(RN(v' k3 + eps)) with EPS_INSIDE_SQRT, where k1, k2 and k3 are
+ *                                 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t) and 1 / (1 - beta2^t) as floats; lr q is not rounded.  The decay,
+ *                                 lr weight_decay as a float times theta + rest as a float, is off by 2^-22 of itself at most, the sum by 2^-46:
+ *                                 theta' is the nearest value unless x' is that close to half-way;
  *                           F32   x = rest, a master weight: rest' = x', theta' = RN_bf16(x') (theta is not read).
  * The states, by `state`: F32   m and v are floats; with rest NONE or F32 the results are collage_adamw_step_fp32's, bit for bit.
  *                         E4M3  m and v are codes of 8 bits with a float scale for each 256 elements of their tensor (the last
  *                               group of a tensor may be shorter):  m = m_code * m_scale,  sqrt(v) = v_code * v_scale, stored again
- *                               as scale = max / 448 and codes of m' / scale, to nearest even, and of u = sqrt(v') / scale, u at least 2^-9
+ *                               as scale = max / 448 and codes of m' / scale, to nearest even, and of u = sqrt(v') / scale (by way of 1 / 448 and
+ *                               448 / max as floats: each is off by a unit or two of its last place), u at least 2^-9
  *                               where v' is not 0, rounded down to a multiple of its spacing s after s * d has been added, 0 <= d < 1
  *                               random (448 at most).  The root moves by less than a code's step in a step of beta2 = 0.999; rounding to nearest would never
  *                               move it.  A group whose largest |m'| (or sqrt(v')) is below 2^-100 is stored as zeros with scale 0.
