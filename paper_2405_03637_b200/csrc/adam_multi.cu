@@ -297,7 +297,7 @@ struct Form {
     // offsets of the arrays in a stage
     static constexpr uint32_t kG = 0, kT = kG + 2 * kTile, kR = kT + 2 * kTile, kM = kR + kRestBytes * kTile, kV = kM + kStateBytes * kTile,
                               kStage = kV + kStateBytes * kTile;
-    static constexpr uint32_t kStages = 208 * 1024 / kStage;          // two to seven
+    static constexpr uint32_t kStages = 208 * 1024 / kStage;          // two to nine
     static __device__ __forceinline__ uint32_t element(int lane, int half) { return kHalves ? half * (kGroup / 2) + lane * 4 : lane * 8 + half * 4; }
 };
 

@@ -9,12 +9,12 @@
 // where every sum without an index is over the rows.
 //
 // A row of each array is read once and kept in registers through both of its sums.  Measured at 8191 x 4096 with a gate of channels: forward 48 us
-// (5.5 TB/s), backward with all gradients 79 us (5.1 TB/s): memory, and a row's two joins.  With a gate for each token: 2047 x 5120 forward 28
-// us (3.7), backward 55 us (3.1): the gates' exponentials, and one row on an SM at a time.
+// (5.5 TB/s), backward with all gradients 80 us (5.0 TB/s): memory, and a row's two joins.  With a gate for each token: 2047 x 5120 forward 28
+// us (3.7), 45 instructions an element from 14 warps on an SM, and backward 55 us (3.1), one row on an SM at a time.
 // As in the residual norm, y belongs to r before r is rounded for the stream.  The backward pass reads the rounded r, or x in its place (FROM_X):
 // r is then formed anew, alpha x + (beta A w_post) no, and dw_pre, a sum of dy r, is free of a rounding of each r (relative error at 8191 x 4096
-// with a few large columns 0.0016 in place of 0.0022; one rounding of the result is 0.0016).  Same bytes, three more instructions an element:
-// backward 84 us in place of 80 at 8191 x 4096, 58 in place of 55 at 2047 x 5120 with a gate for each token.
+// with a few large columns 0.0016 in place of 0.0022; one rounding of the result is 0.0016).  Same bytes, a few more instructions (38 an
+// element in place of 37): backward 84 us in place of 80 at 8191 x 4096, 58 in place of 55 at 2047 x 5120 with a gate for each token.
 #include "bulk_pipe.cuh"
 #include "ops_common.cuh"
 
