@@ -672,6 +672,11 @@ static __device__ unsigned int g_block_norm_fault = 0;
 // group brings whole rows into shared memory by bulk copies, several rows ahead, so that the others have nothing to do with loads; each of
 // them owns PER vectors of columns, worked on two elements an instruction, and keeps its columns' sums over rows in registers until the end.
 constexpr int kMaxGroups = 15, kMaxDepth = 4;
+// With a gate for each token a thread keeps its part of post_weight in registers, except from x, which takes it twice a row, where that makes it
+// spill: there it is in shared memory, as it came (8191 x 4096 182 us -> 157, 8191 x 1024 54 -> 46, 4096 x 6144 146 -> 143; but 2047 x 5120, for
+// which there are registers, 58 -> 60, with a stage less).
+template <int PER, bool TOKEN_GATE, bool FROM_X, int THREADS>
+constexpr bool kSharesPost = TOKEN_GATE && FROM_X && (PER > 1 || THREADS > 640);
 
 template <int PER, bool TOKEN_GATE, bool FROM_X, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const __grid_constant__ BlockNormBackwardArgs a, int group_threads, int depth) {
@@ -690,8 +695,8 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
     __syncthreads();
     after_previous();
     uint8_t* stages = dynamic + static_cast<size_t>(group) * depth * stage_bytes;          // of this group: [depth][kArrays] rows
-    // what columns are multiplied by, in floats: pre_weight, and beta * post_weight times A(gate) of a gate of channels; a gate for each token
-    // leaves no room for the second, which is then unpacked for each row
+    // what columns are multiplied by, in floats: pre_weight, and beta * post_weight times A(gate) of a gate of channels; with a gate for each
+    // token post_weight alone, in bfloat16, or nothing
     float* pre = reinterpret_cast<float*>(dynamic + static_cast<size_t>(groups) * depth * stage_bytes);
     float* post = pre + a.cols;
     const bool second = a.post && a.dblock;
@@ -714,20 +719,28 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
     if (t == 0)
         for (int d = 0; d < depth; ++d) send_for(first + d * step, d);
     const uint4 none = make_uint4(0, 0, 0, 0);
-    uint4 qpost[PER];
+    constexpr bool kShared = kSharesPost<PER, TOKEN_GATE, FROM_X, THREADS>, kKept = TOKEN_GATE && !kShared;
+    uint4 qpost[kKept ? PER : 1];
     uint64_t sum_pre[PER][4], sum_post[PER][4];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int v = t + i * group_threads;
-        if (TOKEN_GATE) qpost[i] = a.post && v < vectors ? reinterpret_cast<const uint4*>(a.post)[v] : make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+        if constexpr (kKept) qpost[i] = a.post && v < vectors ? reinterpret_cast<const uint4*>(a.post)[v] : make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
 #pragma unroll
         for (int p = 0; p < 4; ++p) sum_pre[i][p] = sum_post[i][p] = 0;
     }
     for (uint64_t j = threadIdx.x; j < a.cols; j += blockDim.x) {
         pre[j] = a.pre ? bf16_value(a.pre[j]) : 0.0f;
+        if (kShared) reinterpret_cast<uint16_t*>(post)[j] = a.post ? a.post[j] : 0x3F80u;
         if (!TOKEN_GATE) post[j] = a.beta * (a.post ? bf16_value(a.post[j]) : 1.0f) * (a.gate ? gate_value(a.activation, bf16_value(a.gate[j])) : 1.0f);
     }
     __syncthreads();
+    auto post_of = [&](int i) {
+        if constexpr (kKept)
+            return qpost[i];
+        else
+            return reinterpret_cast<const uint4*>(post)[min(t + i * group_threads, vectors - 1)];
+    };
     const float per_col = 1.0f / static_cast<float>(a.cols);
     auto barrier = [&] {
         if (group_warps > 1)
@@ -786,7 +799,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
                     if constexpr (TOKEN_GATE) {
                         uint64_t g[4];
                         unpack_pairs(vector(4, i), g);
-                        unpack_pairs(qpost[i], w);
+                        unpack_pairs(post_of(i), w);
                         float small[8];         // for the second pass, in the place of this thread's dy and x
 #pragma unroll
                         for (int p = 0; p < 4; ++p) {
@@ -837,7 +850,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_backward_kernel(const _
             if (TOKEN_GATE) {
                 uint64_t g[4];
                 unpack_pairs(vector(4, i), g);
-                unpack_pairs(qpost[i], w);
+                unpack_pairs(post_of(i), w);
                 float parts[8];
                 if constexpr (FROM_X) {
                     const uint4 lo = vector(0, i), hi = vector(1, i);
@@ -942,7 +955,7 @@ static collage_status_t launch_block_backward_as(const BlockNormBackwardArgs& a,
     const int group = static_cast<int>((v + PER * 32 - 1) / (PER * 32) * 32), most = std::max(1, std::min(THREADS / group, kMaxGroups));
     // few rows: as many groups as give every SM some
     const int groups = static_cast<int>(std::max<uint64_t>(1, std::min<uint64_t>(most, (a.rows + sm_count - 1) / sm_count)));
-    const size_t row = (TOKEN_GATE ? 5 : 4) * 2 * a.cols, factors = (TOKEN_GATE ? 4 : 8) * a.cols;
+    const size_t row = (TOKEN_GATE ? 5 : 4) * 2 * a.cols, factors = (!TOKEN_GATE ? 8 : kSharesPost<PER, TOKEN_GATE, FROM_X, THREADS> ? 6 : 4) * a.cols;
     const int depth = static_cast<int>(std::min<size_t>(kMaxDepth, (224 * 1024 - factors) / (row * groups)));
     // the stages hold the groups' sums in the end: 64 PER bytes a thread
     const size_t smem = std::max<size_t>(depth * row * groups, 64ull * PER * group * groups) + factors;
