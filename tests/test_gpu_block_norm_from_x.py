@@ -168,3 +168,31 @@ def test_offsets_beyond_32_bits():
     for from_x, to in ((x, far), (x.clone(), near)):
         B.block_norm_backward(dy, None, o, None, rpre, to, None, pre_weight=one, x=from_x)
     assert torch.equal(far, near)
+
+
+@pytest.mark.parametrize("cols", [200, 512, 515, 4096, 5632, 16001])
+@pytest.mark.parametrize("act", [B.GATE_SIGMOID, B.GATE_SILU])
+@pytest.mark.parametrize("token", [False, True])
+def test_closed_gates_rows_of_zeros_and_values_that_are_no_numbers(cols, act, token):
+    """A gate of minus infinity lets nothing through, either way; a row's NaN stays in its row (and in the sums over rows)."""
+    rows = 7
+    x, o, dy = normal(1, rows, cols), normal(2, rows, cols), normal(3, rows, cols)
+    gate = normal(4, rows if token else 1, cols)
+    gate[:, 9], gate[:, 11] = float("-inf"), -3e38
+    x[2], o[2] = 0, 0
+    one = torch.ones(cols, dtype=BF16, device="cuda")
+    ws = torch.empty(B.block_norm_workspace_bytes(cols), dtype=torch.uint8, device="cuda")
+    kw = dict(gate=gate, post_weight=one, pre_weight=one, activation=act)
+    for bad in (None, 5):
+        if bad is not None:
+            dy[bad, 1] = float("nan")
+        r, y, rpost, rpre = torch.empty_like(x), torch.empty_like(x), vec(rows), vec(rows)
+        B.block_norm(x, o, r, y=y, rstd_post=rpost, rstd_pre=rpre, eps=EPS, **kw)
+        dx, do, dg, dpost, dpre = torch.empty_like(x), torch.empty_like(x), torch.empty_like(gate), vec(cols, BF16), vec(cols, BF16)
+        B.block_norm_backward(dy, None, o, rpost, rpre, dx, do, dgate=dg, dpost_weight=dpost, dpre_weight=dpre, workspace=ws, x=x, **kw)
+        whole = [i for i in range(rows) if i != bad]
+        assert dx[whole].isfinite().all() and do[whole].isfinite().all()
+        if bad is None:
+            assert dpost.isfinite().all() and dpre.isfinite().all() and dg.isfinite().all() and (dg[:, 9] == 0).all() and (dpost[[9, 11]] == 0).all()
+        else:
+            assert dx[bad].isnan().all() and do[bad].isnan().all() and dpre[1].isnan()
